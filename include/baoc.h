@@ -484,7 +484,8 @@ int baoc_profile_last(baoc_t* h, float* ms2);
  * bytes), 5 null pointer; kernel: 1 statistics step, 2 its combine, 3 sample
  * gather, 4 first finalize sweep, 5 later sweeps, 6 / 7 row-column reduction of
  * the window / of the step, 8 its combine, 9 fused step, 10 the self-test, 11 the norms of the
- * factored tuple's Adafactor options.
+ * factored tuple's Adafactor options, 14 / 15 gradient norm / clip, 16 / 17 grouping / sums of the
+ * token table's gradient.
  *
  * baoc_check_selftest: queues a one-thread kernel that runs the range check on
  * numbers that violate it (a 32-byte range that starts 16 bytes before the end
@@ -498,6 +499,102 @@ typedef struct {
 } baoc_check_t;
 int baoc_check_status(baoc_check_t* out);
 int baoc_check_selftest(baoc_stream_t stream);
+
+/* ---- gradient norm and clipping --------------------------------------------------
+ * The paper has no counterpart of these two.  Language-model training clips the
+ * gradient of all blocks by its global norm between the backward pass and
+ * baoc_step; both calls work on the handle's block list.
+ *
+ *   n_i = sqrt(sum of the squares of block i's gradient),  n = sqrt(sum_i n_i^2),
+ *   dst_i = c * src_i  with  c = min(1, max_norm / (n + 1e-6)).
+ *
+ * dtype: BAOC_BF16 or BAOC_F32 (the gradients that baoc_step reads are bf16;
+ * fp32 is for arrays that accumulate over micro-batches).  Squares are summed in
+ * fp32 over at most 64 elements of one thread and in double from there on, in an
+ * order that depends on the block sizes only; values whose squares leave the
+ * fp32 range are summed in double throughout, so the norm neither overflows nor
+ * underflows before it is rounded to the fp32 outputs.  c is formed in double from the unrounded norm,
+ * rounded to fp32, and each product is rounded once to fp32 and once more to a
+ * bf16 destination.
+ * A NaN gradient makes n, c and every dst NaN; an infinite one makes n infinite
+ * and c zero (its own dst is NaN, all others 0).  A zero gradient has c = 1 for
+ * max_norm >= 1e-6. */
+enum { BAOC_BF16 = 0, BAOC_F32 = 1 };
+
+/* Bytes of device workspace of the two calls: tables, partial sums, tickets. */
+int baoc_clip_workspace_bytes(const baoc_t* h, size_t* bytes);
+
+/* Give the handle that workspace (device, 256-byte aligned, >= the size above).
+ * Queues the upload of the tile table on the stream; calls on other streams have
+ * to be ordered behind it by the caller.  It may be bound again at any time. */
+int baoc_bind_clip_workspace(baoc_t* h, void* dev, size_t bytes, baoc_stream_t stream);
+
+/* norms (device, 1 + n_blocks floats, 4-byte aligned): n, then n_0 .. n_{n_blocks-1}.
+ * grads: host array of n_blocks device pointers (16-byte aligned).  Queues one
+ * kernel (and the upload of the pointers when they differ from the last call's);
+ * does not wait.  Calls that share a handle share its workspace: one stream at a
+ * time. */
+int baoc_grad_norm(baoc_t* h, const void* const* grads, int dtype, float* norms, baoc_stream_t stream);
+
+/* The norms, then dst_i = c * src_i for every block.  src / dst: host arrays of
+ * n_blocks device pointers (16-byte aligned).  dst_i may be src_i itself when the
+ * types agree (nothing is written then if c = 1) and may otherwise overlap no
+ * src or dst array.  Types: bf16 -> bf16, fp32 -> fp32, fp32 -> bf16.  max_norm:
+ * finite, >= 0.  Queues two kernels; does not wait.
+ * Errors of both: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_CUDA; BAOC_E_STATE before
+ * baoc_bind_clip_workspace. */
+int baoc_clip_grads(baoc_t* h, const void* const* src, int src_dtype, void* const* dst, int dst_dtype,
+                    double max_norm, float* norms, baoc_stream_t stream);
+
+/* ---- the token table ---------------------------------------------------------------
+ * The paper has no counterpart of these.  The token table is the largest block of
+ * a language model; its forward is a row lookup, its gradient a sum over the
+ * tokens that named the row:
+ *
+ *   out[t, :]     = scale * table[ids[t], :]
+ *   dtable[v, :]  = scale * sum over t with ids[t] = v of dout[t, :]
+ *
+ * (scale is 1 for most models, sqrt(dim) for those that scale their embeddings).
+ * An id outside [0, vocab) marks an ignored position: its output row is zero and
+ * its dout row is not read.  pad_id (-1: none) is looked up like any other id but
+ * takes no gradient: its dout rows are not read either, its dtable row is zero.
+ * Handle-free: a descriptor, device pointers and, for the gradient, a workspace. */
+typedef struct {
+    int64_t vocab;               /* rows of the table, 1 .. 2^31 - 1 */
+    int32_t dim;                 /* columns, 1 .. 2^24 */
+    int32_t table_dtype;         /* BAOC_F32 or BAOC_BF16 */
+    int32_t act_dtype;           /* of out and dout */
+    int32_t grad_dtype;          /* of dtable: BAOC_BF16 is what baoc_step reads */
+    int32_t id_bits;             /* 32 or 64: signed token ids */
+    float scale;                 /* finite */
+    int64_t pad_id;              /* -1, or in [0, vocab) */
+    int64_t table_stride;        /* elements from row to row: dim .. 2^28, 0 for dim */
+    int64_t act_stride;
+    int64_t grad_stride;
+} baoc_embed_t;
+
+/* out[n_tokens][dim].  Pointers are aligned to their elements; arrays whose base
+ * and row stride are multiples of 16 bytes take the wide path.  out must not
+ * overlap the table.  n_tokens = 0 queues nothing.  One kernel; does not wait. */
+int baoc_embed(const baoc_embed_t* e, const void* table, const void* ids, int64_t n_tokens, void* out,
+               baoc_stream_t stream);
+
+/* Bytes of device workspace baoc_embed_grad needs for n_tokens tokens. */
+int baoc_embed_grad_workspace_bytes(const baoc_embed_t* e, int64_t n_tokens, size_t* bytes);
+
+/* dtable[vocab][dim] from dout[n_tokens][dim].  accumulate = 0 writes every row
+ * (zero where no token named it); 1 adds to the rows that tokens named, formed in
+ * fp32 and rounded once, and leaves the others (a tied output layer, or
+ * micro-batches).  Sums are fp32, in an order that depends on the ids only: equal
+ * inputs give equal bits.  ws: device, 256-byte aligned, >= the size above; its
+ * contents matter to no later call.  n_tokens <= 2^30.  dtable must overlap
+ * neither dout nor ws.  Queues two kernels; does not wait.
+ * Errors of the three: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_WORKSPACE,
+ * BAOC_E_CUDA; baoc_embed_last_error() returns the message of the calling
+ * thread's last failure. */
+int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, int64_t n_tokens, void* dtable,
+                    int accumulate, void* ws, size_t ws_bytes, baoc_stream_t stream);
+const char* baoc_embed_last_error(void);
 
 /* ---- allocation-free variant ------------------------------------------------ */
 

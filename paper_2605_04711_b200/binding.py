@@ -78,6 +78,12 @@ class Sample(C.Structure):
     _fields_ = [("n_rows", C.c_int64), ("n_cols", C.c_int32), ("rows", C.c_void_p), ("cols", C.c_void_p)]
 
 
+class Embed(C.Structure):
+    _fields_ = [("vocab", C.c_int64), ("dim", C.c_int32), ("table_dtype", C.c_int32), ("act_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("id_bits", C.c_int32), ("scale", C.c_float), ("pad_id", C.c_int64),
+                ("table_stride", C.c_int64), ("act_stride", C.c_int64), ("grad_stride", C.c_int64)]
+
+
 class Info(C.Structure):
     _fields_ = [("n_blocks", C.c_int32), ("n_cfg", C.c_int32), ("numel", C.c_int64), ("n_tiles", C.c_int64),
                 ("stats_steps", C.c_int64), ("state_bytes", C.c_int64), ("kernel_launches", C.c_int64),
@@ -91,7 +97,9 @@ EXPORTS = ["baoc_default_opts", "baoc_create", "baoc_destroy", "baoc_last_error"
            "baoc_sample_stats_noalloc", "baoc_noalloc_last_error", "baoc_profile", "baoc_profile_last",
            "baoc_export", "baoc_import", "baoc_time_scratch_bytes", "baoc_measure_time_ratios",
            "baoc_set_sampling", "baoc_reconfigure", "baoc_configure_from_window", "baoc_partition",
-           "baoc_set_factored_schedule", "baoc_check_status", "baoc_check_selftest"]
+           "baoc_set_factored_schedule", "baoc_check_status", "baoc_check_selftest",
+           "baoc_clip_workspace_bytes", "baoc_bind_clip_workspace", "baoc_grad_norm", "baoc_clip_grads",
+           "baoc_embed", "baoc_embed_grad_workspace_bytes", "baoc_embed_grad", "baoc_embed_last_error"]
 
 _vp = C.c_void_p
 _lib.baoc_default_opts.argtypes = [C.POINTER(Opts)]
@@ -133,6 +141,16 @@ _lib.baoc_sample_stats_noalloc.argtypes = [_vp, _vp, _vp, _vp, C.c_int64, C.c_do
 _lib.baoc_noalloc_last_error.argtypes = []
 _lib.baoc_noalloc_last_error.restype = C.c_char_p
 NOALLOC_MAX_NUMEL = 67108864
+_lib.baoc_clip_workspace_bytes.argtypes = [_vp, C.POINTER(C.c_size_t)]
+_lib.baoc_bind_clip_workspace.argtypes = [_vp, _vp, C.c_size_t, _vp]
+_lib.baoc_grad_norm.argtypes = [_vp, _vp, C.c_int, _vp, _vp]
+_lib.baoc_clip_grads.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, C.c_double, _vp, _vp]
+_lib.baoc_embed.argtypes = [_vp, _vp, _vp, C.c_int64, _vp, _vp]
+_lib.baoc_embed_grad_workspace_bytes.argtypes = [_vp, C.c_int64, C.POINTER(C.c_size_t)]
+_lib.baoc_embed_grad.argtypes = [_vp, _vp, _vp, C.c_int64, _vp, C.c_int, _vp, C.c_size_t, _vp]
+_lib.baoc_embed_last_error.argtypes = []
+_lib.baoc_embed_last_error.restype = C.c_char_p
+DTYPES = {torch.bfloat16: 0, torch.float32: 1}              # BAOC_BF16, BAOC_F32
 
 
 def sample_stats_noalloc(grad: torch.Tensor, gprev: torch.Tensor, m: torch.Tensor, v: torch.Tensor, out4: torch.Tensor,
@@ -244,6 +262,109 @@ def _np_ptr(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data
 
 
+def _dtype_code(dtype: torch.dtype) -> int:
+    code = DTYPES.get(dtype)
+    if code is None:
+        raise BaocError(E_INVALID, f"{dtype} is not offered: bfloat16 and float32 are")
+    return code
+
+
+def _rows(t: torch.Tensor, dim: int, what: str):
+    """(rows, elements from row to row) of a device tensor [..., dim] whose leading dimensions step evenly."""
+    if not t.is_cuda:
+        raise BaocError(E_INVALID, f"{what} must be a CUDA tensor")
+    if t.dim() < 1 or t.shape[-1] != dim:
+        raise BaocError(E_INVALID, f"{what} must be [..., {dim}], not {list(t.shape)}")
+    if t.is_contiguous():
+        return t.numel() // dim, dim
+    m = t
+    if t.dim() != 2:
+        try:
+            m = t.view(-1, dim)
+        except RuntimeError:
+            m = None
+    if m is None or (dim > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < dim):
+        raise BaocError(E_INVALID, f"{what}: rows must be contiguous and step evenly without overlap")
+    return m.shape[0], (m.stride(0) if m.shape[0] > 1 else dim)
+
+
+class Embedding:
+    """The token table's lookup (``baoc_embed``) and gradient (``baoc_embed_grad``): a plan of one table's shape.
+
+    scale multiplies every looked-up row; ids outside [0, vocab) are ignored positions (zero rows, no gradient);
+    pad_id's row is looked up but takes no gradient.  Calls queue work on the current stream of the tensors' device."""
+
+    def __init__(self, vocab: int, dim: int, scale: float = 1.0, pad_id: Optional[int] = None):
+        self.vocab, self.dim = int(vocab), int(dim)
+        self._e = Embed(self.vocab, max(-1, min(self.dim, 2 ** 31 - 1)), DTYPES[torch.float32], DTYPES[torch.bfloat16], DTYPES[torch.bfloat16], 64,
+                        float(scale), -1 if pad_id is None else int(pad_id), 0, 0, 0)
+        self._ref = C.byref(self._e)
+        self._n = C.c_size_t()
+        self.grad_workspace_bytes(0)                        # the descriptor's checks
+
+    @staticmethod
+    def _check(rc: int):
+        if rc < 0:
+            raise BaocError(rc, _lib.baoc_embed_last_error().decode())
+
+    def _ids(self, ids: torch.Tensor) -> torch.Tensor:
+        if ids.dtype == torch.int64:
+            self._e.id_bits = 64
+        elif ids.dtype == torch.int32:
+            self._e.id_bits = 32
+        else:
+            raise BaocError(E_INVALID, f"token ids must be int32 or int64, not {ids.dtype}")
+        return ids if ids.is_contiguous() else ids.contiguous()
+
+    def lookup(self, table: torch.Tensor, ids: torch.Tensor, out: Optional[torch.Tensor] = None,
+               out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """out[..., :] = scale * table[ids[...], :].  table: [vocab, dim] fp32 or bf16; ids: int32 or int64 of any shape;
+        out: ids' shape + [dim] (allocated as out_dtype when not given); rows of table and out may be strided."""
+        e = self._e
+        if out is None:
+            out = torch.empty((*ids.shape, self.dim), dtype=out_dtype, device=table.device)
+        rows, e.table_stride = _rows(table, self.dim, "table")
+        n, e.act_stride = _rows(out, self.dim, "out")
+        e.table_dtype, e.act_dtype = _dtype_code(table.dtype), _dtype_code(out.dtype)
+        if rows != self.vocab or n != ids.numel() or ids.device != table.device or out.device != table.device:
+            raise BaocError(E_INVALID, "lookup: table must be [vocab, dim], out one row per id, all on one device")
+        ids = self._ids(ids)
+        self._check(_on_device(table.device, _lib.baoc_embed, self._ref, table.data_ptr(), ids.data_ptr(), n, out.data_ptr()))
+        return out
+
+    def grad_workspace_bytes(self, n_tokens: int) -> int:
+        self._check(_lib.baoc_embed_grad_workspace_bytes(self._ref, int(n_tokens), C.byref(self._n)))
+        return self._n.value
+
+    def grad(self, ids: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, accumulate: bool = False,
+             ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """dtable[v, :] = scale * sum of dout over the positions with id v (accumulate: added to dtable).  dout: ids' shape
+        + [dim], dtable: [vocab, dim] (a block's flat gradient array viewed that way), bf16 or fp32 each; ws: device bytes,
+        at least ``grad_workspace_bytes(ids.numel())`` (allocated when not given)."""
+        e = self._e
+        n, e.act_stride = _rows(dout, self.dim, "dout")
+        rows, e.grad_stride = _rows(dtable, self.dim, "dtable")
+        e.act_dtype, e.grad_dtype = _dtype_code(dout.dtype), _dtype_code(dtable.dtype)
+        if rows != self.vocab or n != ids.numel() or ids.device != dtable.device or dout.device != dtable.device:
+            raise BaocError(E_INVALID, "grad: dtable must be [vocab, dim], dout one row per id, all on one device")
+        ids = self._ids(ids)
+        if ws is None:
+            ws = torch.empty(self.grad_workspace_bytes(n), dtype=torch.uint8, device=dtable.device)
+        elif ws.device != dtable.device or not ws.is_contiguous():
+            raise BaocError(E_INVALID, "grad: ws must be a contiguous buffer on the device of the others")
+        self._check(_on_device(dtable.device, _lib.baoc_embed_grad, self._ref, ids.data_ptr(), dout.data_ptr(), n, dtable.data_ptr(),
+                               int(bool(accumulate)), ws.data_ptr(), ws.numel() * ws.element_size()))
+        return dtable
+
+
+def _on_device(device: torch.device, call, *args) -> int:
+    """call(*args, current stream of that device) with the device current."""
+    if device.index == torch.cuda.current_device():
+        return call(*args, torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return call(*args, torch.cuda.current_stream().cuda_stream)
+
+
 class Baoc:
     """One handle of the library (``baoc_create`` .. ``baoc_destroy``)."""
 
@@ -341,6 +462,52 @@ class Baoc:
         risk = np.zeros((self.n_blocks, self.n_cfg), np.float64)
         self._check(_lib.baoc_risk_from_raw(self._h, st, risk.ctypes.data))
         return risk, [s.as_dict() for s in st]
+
+    # ---- gradient norm and clipping ----------------------------------------
+    def clip_workspace_bytes(self) -> int:
+        n = C.c_size_t()
+        self._check(_lib.baoc_clip_workspace_bytes(self._h, C.byref(n)))
+        return n.value
+
+    def bind_clip_workspace(self, ws: torch.Tensor):
+        self._check(_lib.baoc_bind_clip_workspace(self._h, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
+        self._keep.append(ws)
+
+    def _clip_arrays(self, arrays, dtype, what: str):
+        """(pointer table, dtype code) of a list of device tensors, or of a table from ``pointer_table`` and its dtype."""
+        if isinstance(arrays, C.Array):
+            if len(arrays) != self.n_blocks:
+                raise BaocError(E_INVALID, f"{what}: one array per block")
+            return arrays, _dtype_code(torch.bfloat16 if dtype is None else dtype)
+        if len(arrays) != self.n_blocks:
+            raise BaocError(E_INVALID, f"{what}: one array per block")
+        for t, b in zip(arrays, self._blocks):
+            if t.numel() != b.numel or not t.is_contiguous() or t.dtype != arrays[0].dtype or not t.is_cuda:
+                raise BaocError(E_INVALID, f"{what}: contiguous device arrays of the blocks' sizes, of one dtype")
+        if dtype is not None and dtype != arrays[0].dtype:
+            raise BaocError(E_INVALID, f"{what}: the arrays are {arrays[0].dtype}, not {dtype}")
+        return pointer_table(arrays), _dtype_code(arrays[0].dtype)
+
+    def _norms(self, norms: torch.Tensor) -> int:
+        if norms.dtype != torch.float32 or norms.numel() != 1 + self.n_blocks or not norms.is_contiguous() or not norms.is_cuda:
+            raise BaocError(E_INVALID, "norms must be a contiguous float32 device tensor of 1 + n_blocks elements")
+        return norms.data_ptr()
+
+    def grad_norm(self, grads, norms: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+        """``baoc_grad_norm``: norms[0] = the global gradient norm, norms[1 + i] block i's.  grads: list of bf16 or fp32
+        device tensors, or a table from ``pointer_table`` with its dtype (bfloat16 when not given)."""
+        tab, code = self._clip_arrays(grads, dtype, "grad_norm")
+        self._check(_lib.baoc_grad_norm(self._h, tab, code, self._norms(norms), _stream()))
+        return norms
+
+    def clip_grads(self, grads, out, max_norm: float, norms: torch.Tensor, src_dtype: Optional[torch.dtype] = None,
+                   dst_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+        """``baoc_clip_grads``: the norms, then out_i = min(1, max_norm / (norms[0] + 1e-6)) * grads_i.  out None: in place.
+        Arrays as for ``grad_norm``; bf16 -> bf16, fp32 -> fp32 or fp32 -> bf16.  Returns norms."""
+        src, sc = self._clip_arrays(grads, src_dtype, "clip_grads")
+        dst, dc = (src, sc) if out is None else self._clip_arrays(out, dst_dtype, "clip_grads")
+        self._check(_lib.baoc_clip_grads(self._h, src, sc, dst, dc, float(max_norm), self._norms(norms), _stream()))
+        return norms
 
     # ---- allocation -------------------------------------------------------
     def cost_model(self):

@@ -126,6 +126,32 @@ struct Tile {
     uint32_t piece;
 };
 
+// Gradient norm and clip.  A tile is large enough for eight 16-byte loads in flight per thread of its CTA.
+constexpr int kClipTile = 16384;
+constexpr int kClipPtrChunk = 256;    // pointers that one launch of the table kernel carries by value
+
+// Per-block record (device copy lives in the clip workspace).
+struct ClipBlock {
+    int64_t numel;
+    int64_t tile0;       // index of the block's first tile
+    int32_t ntiles;
+    int32_t pad;
+};
+// The clip workspace.  tickets: one per block, then the count of finished blocks; all zero between calls.
+struct ClipBufs {
+    const ClipBlock* blocks;
+    const Tile* tiles;
+    const void** src;
+    void** dst;
+    double* partials;    // per tile: its sum of squares
+    double* bsq;         // per block: its sum of squares
+    uint32_t* tickets;
+    float* factor;       // the clip factor that the last norm left
+    int64_t n_tiles;
+    int n_blocks;
+};
+struct ClipPtrs { const void* p[kClipPtrChunk]; };
+
 // Geometry of the row/column reduction of one matrix block.  The matrix is cut
 // into chunks of 64*L rows and strips of kRedCols columns; one CTA reduces one
 // (chunk, strip) piece and writes its row sums to rowpart[strip][row] and its
@@ -348,6 +374,14 @@ struct Handle {
     std::vector<FactoredGroup> f_groups;
     int64_t n_factored_tiles = 0;
 
+    // gradient norm and clip
+    char* cw = nullptr;
+    size_t cw_bytes = 0;
+    ClipBufs clip{};
+    std::vector<const void*> last_clip_src, last_clip_dst;   // the pointers the device tables hold ...
+    void* last_clip_stream = nullptr;                        // ... for calls on this stream
+    bool clip_captured = false;                              // a graph may replay a call: the tables hold what it left
+
     // optional per-kernel timing of the step (CUDA events, owned by the CUDA translation unit)
     bool prof_on = false, prof_valid = false;
     void* prof_ev[3] = {nullptr, nullptr, nullptr};
@@ -415,6 +449,8 @@ int launch_fused_step(const StepBlock* blocks, const Tile* tiles, const void* co
 int stats_check_fetch(CheckRecord* out);
 int finalize_check_fetch(CheckRecord* out);
 int step_check_fetch(CheckRecord* out);
+int clip_check_fetch(CheckRecord* out);
+int embed_check_fetch(CheckRecord* out);
 int launch_check_selftest(cudaStream_t s);
 // Adafactor's options: per tile of the given blocks the sums of u^2 and theta^2, then per block the clip factor and the
 // step size (ids: the blocks, n of them; tiles: their stretch of the tile table).
