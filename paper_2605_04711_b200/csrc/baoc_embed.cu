@@ -14,6 +14,10 @@ namespace baoc {
 constexpr int kGroupCtas = 128;        // id classes (one CTA each) of the grouping; doubled while a class has over kGroupBins ids
 constexpr int kGroupBins = 1024;       // most ids of a class: one thread of the CTA per id
 constexpr int kGroupWarps = 32;
+constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
+constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
+constexpr int kSlab = 256;             // columns of a warp of the sums
+constexpr int kGroupRows = 8;          // rows of a warp of the sums
 constexpr int kEmbedMaxDim = 1 << 24;
 constexpr int64_t kEmbedMaxStride = 1 << 28;           // (row products stay far inside 64 bits)
 
@@ -61,6 +65,15 @@ struct EmbedArgs {
     float scale;
 };
 
+// Tokens of a chunk of a row that `count` > kShortRow tokens name: a power of two, at least as many as the row then has
+// chunks.  A row's chunks take the slots from ceil(start / kSlotTokens) on: as a chunk has at least 2 kSlotTokens tokens,
+// the last one's slot still begins inside the row, so no two rows share a slot.
+__host__ __device__ __forceinline__ int chunk_tokens(int count) {
+    int len = kShortRow;
+    while (int64_t(len) * len < count) len <<= 1;
+    return len;
+}
+
 // ---- lookup: one thread per V elements of a row -----------------------------------------------------------------
 template <int SRC, int DST, int V, typename Id>
 __global__ void __launch_bounds__(kThreads)
@@ -91,14 +104,16 @@ embed_kernel(const void* __restrict__ table, const Id* __restrict__ ids, void* _
 // per listed token.
 template <typename Id>
 __global__ void __launch_bounds__(kGroupWarps * 32)
-embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad, int shift, int bins, int32_t* __restrict__ start,
-                   int32_t* __restrict__ perm BAOC_CHECK_PARAM) {
+embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad, int shift, int bins, int slabs, int n_slots,
+                   int32_t* __restrict__ start, int32_t* __restrict__ perm, int2* __restrict__ slots,
+                   uint32_t* __restrict__ tickets BAOC_CHECK_PARAM) {
     extern __shared__ int32_t hist[];                   // [warps][bins]
     __shared__ int32_t s_warp[kGroupWarps];
-    __shared__ int32_t s_less;
+    __shared__ int32_t s_less, s_end;
 #ifdef BAOC_CHECKED
     if (!check_range(ck, kKerEmbedGroup, start + size_t(blockIdx.x) * bins, 4ll * (bins + 1), 0) ||
-        !check_range(ck, kKerEmbedGroup, perm, 4ll * n, 1))
+        !check_range(ck, kKerEmbedGroup, perm, 4ll * n, 1) || !check_range(ck, kKerEmbedGroup, slots, 8ll * n_slots, 2) ||
+        !check_range(ck, kKerEmbedGroup, tickets, 4ll * n_slots * slabs, 3))
         return;
 #endif
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -144,9 +159,22 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     if (int(threadIdx.x) < bins) {
         for (int w = 0; w < kGroupWarps; ++w) hist[w * bins + threadIdx.x] += first;
         start[size_t(cls) * bins + threadIdx.x] = first;
-        if (int(threadIdx.x) == bins - 1 && cls == mask) start[size_t(cls + 1) * bins] = first + total;
+        if (int(threadIdx.x) == bins - 1) {
+            s_end = first + total;
+            if (cls == mask) start[size_t(cls + 1) * bins] = first + total;
+        }
     }
     __syncthreads();
+    // the chunk list: the slots that begin in this class's part of the order (the last class: all that follow, too)
+    const int slot0 = (s_less + kSlotTokens - 1) / kSlotTokens;
+    const int slot1 = cls == mask ? n_slots : (s_end + kSlotTokens - 1) / kSlotTokens;
+    for (int i = slot0 + threadIdx.x; i < slot1; i += blockDim.x) slots[i] = make_int2(-1, 0);
+    for (int64_t i = int64_t(slot0) * slabs + threadIdx.x; i < int64_t(slot1) * slabs; i += blockDim.x) tickets[i] = 0u;
+    __syncthreads();
+    if (int(threadIdx.x) < bins && total > kShortRow) {
+        const int len = chunk_tokens(total), chunks = (total + len - 1) / len, at = (first + kSlotTokens - 1) / kSlotTokens;
+        for (int k = 0; k < chunks; ++k) slots[at + k] = make_int2(int(cls) * bins + int(threadIdx.x), k);
+    }
     for (int tb = t0; tb < t1; tb += 32) {
         const int t = tb + lane;
         const int64_t id = t < t1 ? int64_t(ids[t]) : -1;
@@ -165,47 +193,243 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     }
 }
 
-// ---- gradient, second kernel: one warp per row and 32 V columns -------------------------------------------------------
-template <int ACT, int GRAD, int V>
-__global__ void __launch_bounds__(kThreads)
-embed_grad_kernel(const void* __restrict__ dout, void* dtable, const int32_t* __restrict__ start, const int32_t* __restrict__ perm,
-                  int shift, int bins, int slabs, int accumulate, const EmbedArgs a BAOC_CHECK_PARAM) {
-    constexpr int as = ACT == BAOC_BF16 ? 2 : 4, gs = GRAD == BAOC_BF16 ? 2 : 4;
-    const int lane = threadIdx.x & 31;
-    const int64_t item = (int64_t(blockIdx.x) * kThreads + threadIdx.x) >> 5;
-    const int64_t v = item / slabs;
-    const int e = int(item - v * slabs) * 32 * V + lane * V;
-    if (v >= a.vocab) return;
-    const size_t slot = size_t(v & ((1 << shift) - 1)) * bins + size_t(v >> shift);
-#ifdef BAOC_CHECKED
-    if (!check_range(ck, kKerEmbedGrad, start + slot, 8, 0)) return;
-#endif
-    const int32_t p0 = start[slot], p1 = start[slot + 1];
-    if (e >= a.dim || (accumulate && p0 == p1)) return;
-    float acc[V];
+// ---- gradient, second kernel: sums of the grouped tokens ----------------------------------------------------------------
+// What the grouping leaves for the sums, all in the workspace.
+struct GradBufs {
+    const int32_t* start;      // per (class, id of the class): its first place in perm; one more at the end
+    const int32_t* perm;       // the tokens, grouped by id
+    const int2* slots;         // chunks of the rows named more than kShortRow times: {row as (class, id), chunk}, or {-1, 0}
+    uint32_t* tickets;         // [slot][slab]: chunks of the row that begins at the slot that are done
+    float* partial;            // [slot][slabs * kSlab]: a chunk's sum
+    int shift, bins, slabs, n_slots;
+};
+
+// Rows e, e + 1 .. of one thread's part of a slab: eight neighbours where rows are aligned for 16-byte loads, eight columns
+// that are 32 apart otherwise.
+template <int DT, bool WIDE>
+struct Part {
+    static constexpr int es = DT == BAOC_BF16 ? 2 : 4;
+    static constexpr int kWords = !WIDE ? 8 : (DT == BAOC_BF16 ? 4 : 8);
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char* row, int col, int dim) {
+        if constexpr (WIDE) {
+            if (col < dim) {
+                const uint4* p = reinterpret_cast<const uint4*>(row + int64_t(col) * es);
+                const uint4 a = __ldg(p);
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+                if constexpr (DT == BAOC_F32) {
+                    const uint4 b = __ldg(p + 1);
+                    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+                }
+            }
+        } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = 0.f;
-    for (int32_t p = p0; p < p1; ++p) {
-#ifdef BAOC_CHECKED
-        if (!check_range(ck, kKerEmbedGrad, perm + p, 4, 1)) return;
-        if (perm[p] < 0 || perm[p] >= a.n) { check_fail(kChkTileIndex, kKerEmbedGrad, perm[p], a.n, p, 2); return; }
-#endif
-        float x[V];
-        load_row<ACT, V>(static_cast<const char*>(dout) + int64_t(perm[p]) * a.src_stride * as, e, x);
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += x[j];
-    }
-    char* row = static_cast<char*>(dtable) + v * a.dst_stride * gs;
-#pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] *= a.scale;
-    if (accumulate) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if constexpr (GRAD == BAOC_BF16) acc[j] += bf16_bits_to_float(reinterpret_cast<const uint16_t*>(row)[e + j]);
-            else acc[j] += reinterpret_cast<const float*>(row)[e + j];
+            for (int j = 0; j < 8; ++j) {
+                const int c = col + 32 * j;
+                if (c < dim) {
+                    if constexpr (DT == BAOC_BF16) w[j] = uint32_t(__ldg(reinterpret_cast<const uint16_t*>(row) + c)) << 16;
+                    else w[j] = __ldg(reinterpret_cast<const uint32_t*>(row) + c);
+                }
+            }
         }
     }
-    store_row<GRAD, V>(row, e, acc);
+    __device__ __forceinline__ void add_to(float (&acc)[8]) const {
+        if constexpr (WIDE && DT == BAOC_BF16) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { acc[2 * j] += bf16_lo(w[j]); acc[2 * j + 1] += bf16_hi(w[j]); }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += __uint_as_float(w[j]);
+        }
+    }
+};
+
+// The finished sum of one row's slab: scaled, added to what is there or not, rounded once.
+template <int GRAD, bool WIDE>
+__device__ __forceinline__ void write_part(char* row, int col, const float (&sum)[8], int accumulate, const EmbedArgs& a) {
+    using E = typename std::conditional<GRAD == BAOC_BF16, uint16_t, float>::type;
+    E* p = reinterpret_cast<E*>(row);
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = sum[j] * a.scale;
+    if constexpr (WIDE) {
+        if (col >= a.dim) return;
+        if (accumulate) {
+            float old[8];
+            if constexpr (GRAD == BAOC_BF16) unpack8(*reinterpret_cast<const uint4*>(p + col), old);
+            else f4_to8(*reinterpret_cast<const float4*>(p + col), *reinterpret_cast<const float4*>(p + col + 4), old);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] += old[j];
+        }
+        store_row<GRAD, 8>(row, col, y);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = col + 32 * j;
+            if (c >= a.dim) continue;
+            if (accumulate) {
+                if constexpr (GRAD == BAOC_BF16) y[j] += bf16_bits_to_float(p[c]);
+                else y[j] += p[c];
+            }
+            const float one[1] = {y[j]};
+            store_row<GRAD, 1>(row, c, one);
+        }
+    }
+}
+
+// A warp's window of 32 places of perm, passed from lane to lane.
+struct Window {
+    int32_t at, mine;
+    __device__ __forceinline__ void open(const int32_t* perm, int32_t p, int32_t end, int lane) {
+        at = p;
+        mine = p + lane < end ? __ldg(perm + p + lane) : 0;
+    }
+    __device__ __forceinline__ int32_t token(int32_t p) const { return __shfl_sync(0xffffffffu, mine, p - at); }
+};
+
+// One warp works on 32 * 8 columns (a slab) of
+//   - four slots of the chunk list: each chunk's tokens are summed into the slot's partial sum, and the warp that finishes
+//     a row's last chunk adds the row's partial sums in their order;
+//   - or kGroupRows neighbours of the grouped order: the tokens of their short rows stream through, kBatch of them in
+//     flight whatever rows they belong to, and a row is written when its last token has been added.
+template <int ACT, int GRAD, bool WIDE>
+__global__ void __launch_bounds__(kThreads)
+embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b, int accumulate, const EmbedArgs a BAOC_CHECK_PARAM) {
+    constexpr int as = ACT == BAOC_BF16 ? 2 : 4, gs = GRAD == BAOC_BF16 ? 2 : 4;
+    using P = Part<ACT, WIDE>;
+    constexpr int kBatch = P::kWords == 4 ? 8 : 4;
+    const int lane = threadIdx.x & 31;
+    int item = int(blockIdx.x) * (kThreads / 32) + int(threadIdx.x >> 5);
+    const int slab = item % b.slabs;
+    item /= b.slabs;
+    const int col = slab * kSlab + lane * (WIDE ? 8 : 1);
+    const int n_idx = b.bins << b.shift;
+    const char* src = static_cast<const char*>(dout);
+    float acc[8];
+    if (item < b.n_slots / 4) {
+        for (int q = 0; q < 4; ++q) {
+            const int slot = item * 4 + q;
+#ifdef BAOC_CHECKED
+            if (!check_range(ck, kKerEmbedGrad, b.slots + slot, 8, 3)) return;
+#endif
+            const int2 d = b.slots[slot];
+            if (d.x < 0) continue;
+#ifdef BAOC_CHECKED
+            if (d.x >= n_idx) { check_fail(kChkBlockIndex, kKerEmbedGrad, d.x, n_idx, slot, 0); return; }
+#endif
+            const int32_t s0 = b.start[d.x], count = b.start[d.x + 1] - s0;
+            const int len = chunk_tokens(count), chunks = (count + len - 1) / len, first = slot - d.y;
+            const int32_t p0 = s0 + d.y * len, p1 = min(p0 + len, s0 + count);
+#ifdef BAOC_CHECKED
+            if (!check_range(ck, kKerEmbedGrad, b.perm + p0, 4ll * (p1 - p0), 1) ||
+                !check_range(ck, kKerEmbedGrad, b.partial + size_t(first) * b.slabs * kSlab, 4ll * chunks * b.slabs * kSlab, 4) ||
+                !check_range(ck, kKerEmbedGrad, b.tickets + size_t(first) * b.slabs + slab, 4, 5))
+                return;
+#endif
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+            Window win;
+            for (int32_t p = p0; p < p1; p += kBatch) {
+                if (((p - p0) & 31) == 0) win.open(b.perm, p, p1, lane);
+                P x[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const int64_t t = win.token(p + i);
+                    if (p + i < p1) x[i].load(src + t * a.src_stride * as, col, a.dim);
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (p + i < p1) x[i].add_to(acc);
+            }
+            float* mine = b.partial + (size_t(slot) * b.slabs + slab) * kSlab + lane * 8;
+            __stcg(reinterpret_cast<float4*>(mine), make_float4(acc[0], acc[1], acc[2], acc[3]));
+            __stcg(reinterpret_cast<float4*>(mine) + 1, make_float4(acc[4], acc[5], acc[6], acc[7]));
+            __threadfence();
+            __syncwarp();
+            uint32_t done = 0;
+            if (lane == 0) done = atomicAdd(b.tickets + size_t(first) * b.slabs + slab, 1u);
+            done = __shfl_sync(0xffffffffu, done, 0);
+            if (int(done) != chunks - 1) continue;
+            __threadfence();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+            const float* part = b.partial + (size_t(first) * b.slabs + slab) * kSlab + lane * 8;
+#pragma unroll 4
+            for (int k = 0; k < chunks; ++k) {
+                const float4* q4 = reinterpret_cast<const float4*>(part + size_t(k) * b.slabs * kSlab);
+                const float4 u = __ldcg(q4), v = __ldcg(q4 + 1);
+                acc[0] += u.x; acc[1] += u.y; acc[2] += u.z; acc[3] += u.w;
+                acc[4] += v.x; acc[5] += v.y; acc[6] += v.z; acc[7] += v.w;
+            }
+            const int cls = d.x / b.bins;
+            const int64_t v = (int64_t(d.x - cls * b.bins) << b.shift) + cls;
+            write_part<GRAD, WIDE>(static_cast<char*>(dtable) + v * a.dst_stride * gs, col, acc, accumulate, a);
+        }
+        return;
+    }
+    item -= b.n_slots / 4;
+    const int idx0 = item * kGroupRows;
+    if (idx0 >= n_idx) return;
+    const int rows = min(kGroupRows, n_idx - idx0);
+#ifdef BAOC_CHECKED
+    if (!check_range(ck, kKerEmbedGrad, b.start + idx0, 4ll * (rows + 1), 0)) return;
+#endif
+    const int32_t st = b.start[idx0 + min(lane, rows)];
+    int cls = idx0 / b.bins;
+    int bin = idx0 - cls * b.bins;
+    auto start_of = [&](int r) { return __shfl_sync(0xffffffffu, st, r); };
+    auto finish = [&](bool named) {                     // write the current row and step to the next
+        const int64_t v = (int64_t(bin) << b.shift) + cls;
+        if (v < a.vocab && (named || !accumulate)) write_part<GRAD, WIDE>(static_cast<char*>(dtable) + v * a.dst_stride * gs, col, acc, accumulate, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        if (++bin == b.bins) { bin = 0; ++cls; }
+    };
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    int r = 0;
+    while (r < rows) {
+        // the rows up to the next long one
+        int upto = r;
+        while (upto < rows && start_of(upto + 1) - start_of(upto) <= kShortRow) ++upto;
+        const int32_t p0 = start_of(r), p1 = start_of(upto);
+#ifdef BAOC_CHECKED
+        if (!check_range(ck, kKerEmbedGrad, b.perm + p0, 4ll * (p1 - p0), 1)) return;
+#endif
+        int32_t row0 = p0, row1 = start_of(min(r + 1, rows));
+        Window win;
+        for (int32_t p = p0; p < p1; p += kBatch) {
+            if (((p - p0) & 31) == 0) win.open(b.perm, p, p1, lane);
+            P x[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int64_t t = win.token(p + i);
+                if (p + i < p1) x[i].load(src + t * a.src_stride * as, col, a.dim);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                if (p + i < p1) {
+                    while (p + i == row1) {
+                        finish(row1 > row0);
+                        row0 = row1;
+                        ++r;
+                        row1 = start_of(r + 1);
+                    }
+                    x[i].add_to(acc);
+                }
+            }
+        }
+        while (r < upto) {
+            finish(row1 > row0);
+            row0 = row1;
+            ++r;
+            row1 = start_of(min(r + 1, rows));
+        }
+        if (r < rows) {                                   // a long row: its chunks write it
+            ++r;
+            if (++bin == b.bins) { bin = 0; ++cls; }
+        }
+    }
 }
 
 namespace {
@@ -253,14 +477,19 @@ void group_geometry(int64_t vocab, int* shift, int* bins) {
     *bins = int(ceil_div(vocab, int64_t(1) << s));
 }
 
-struct EmbedLayout { size_t start, perm, total; int shift, bins; };
+struct EmbedLayout { size_t start, perm, slots, tickets, partial, total; int shift, bins, slabs, n_slots; };
 
 EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     EmbedLayout L{};
     group_geometry(e->vocab, &L.shift, &L.bins);
     L.start = 0;
     L.perm = size_t(round_up(4 * ((int64_t(L.bins) << L.shift) + 1), 256));
-    L.total = L.perm + size_t(round_up(4 * n, 256));
+    L.slabs = int(ceil_div(e->dim, kSlab));
+    L.n_slots = int(round_up(ceil_div(n, kSlotTokens), 4));
+    L.slots = L.perm + size_t(round_up(4 * n, 256));
+    L.tickets = L.slots + size_t(round_up(8 * int64_t(L.n_slots), 256));
+    L.partial = L.tickets + size_t(round_up(4 * int64_t(L.n_slots) * L.slabs, 256));
+    L.total = L.partial + size_t(4 * int64_t(L.n_slots) * L.slabs * kSlab);
     return L;
 }
 
@@ -351,26 +580,30 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     char* w = static_cast<char*>(ws);
     int32_t* start = reinterpret_cast<int32_t*>(w + L.start);
     int32_t* perm = reinterpret_cast<int32_t*>(w + L.perm);
+    int2* slots = reinterpret_cast<int2*>(w + L.slots);
+    uint32_t* tickets = reinterpret_cast<uint32_t*>(w + L.tickets);
     const CheckCtx ck{w, w + L.total, 0, 0, 0};
     (void)ck;
+    const int64_t items = (L.n_slots / 4 + ceil_div(int64_t(L.bins) << L.shift, kGroupRows)) * L.slabs;
+    if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: too many elements for one launch");
     const int smem = 4 * kGroupWarps * L.bins;
-    const void* group = e->id_bits == 64 ? reinterpret_cast<const void*>(embed_group_kernel<int64_t>) : reinterpret_cast<const void*>(embed_group_kernel<int32_t>);
-    cudaError_t ce = cudaFuncSetAttribute(group, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kGroupWarps * kGroupBins);
-    if (ce != cudaSuccess) return fail_embed(BAOC_E_CUDA, std::string("embed_group_kernel: ") + cudaGetErrorString(ce));
-    if (e->id_bits == 64)
-        embed_group_kernel<int64_t><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const int64_t*>(ids), int(n_tokens), e->vocab, e->pad_id, L.shift, L.bins, start, perm BAOC_CHECK_ARG(ck));
-    else
-        embed_group_kernel<int32_t><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const int32_t*>(ids), int(n_tokens), e->vocab, e->pad_id, L.shift, L.bins, start, perm BAOC_CHECK_ARG(ck));
-    rc = launched("embed_group_kernel");
+    auto group = [&](auto id) {
+        using Id = decltype(id);
+        const cudaError_t ce = cudaFuncSetAttribute(embed_group_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kGroupWarps * kGroupBins);
+        if (ce != cudaSuccess) return fail_embed(BAOC_E_CUDA, std::string("embed_group_kernel: ") + cudaGetErrorString(ce));
+        embed_group_kernel<Id><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const Id*>(ids), int(n_tokens), e->vocab, e->pad_id, L.shift,
+                                                                             L.bins, L.slabs, L.n_slots, start, perm, slots, tickets BAOC_CHECK_ARG(ck));
+        return launched("embed_group_kernel");
+    };
+    rc = e->id_bits == 64 ? group(int64_t(0)) : group(int32_t(0));
     if (rc) return rc;
     const EmbedArgs a{e->vocab, n_tokens, e->pad_id, as, gs, e->dim, e->scale};
+    const GradBufs b{start, perm, slots, tickets, reinterpret_cast<float*>(w + L.partial), L.shift, L.bins, L.slabs, L.n_slots};
     const bool wd = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
-    const int slabs = int(ceil_div(e->dim, 32 * (wd ? 8 : 1)));
-    const int64_t blocks = ceil_div(e->vocab * slabs * 32, kThreads);
-    if (blocks > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: too many elements for one launch");
+    const unsigned grid = unsigned(ceil_div(items * 32, kThreads));
     return with_types(e->act_dtype, e->grad_dtype, [&](auto A, auto G) {
-        if (wd) embed_grad_kernel<A(), G(), 8><<<unsigned(blocks), kThreads, 0, s>>>(dout, dtable, start, perm, L.shift, L.bins, slabs, accumulate, a BAOC_CHECK_ARG(ck));
-        else embed_grad_kernel<A(), G(), 1><<<unsigned(blocks), kThreads, 0, s>>>(dout, dtable, start, perm, L.shift, L.bins, slabs, accumulate, a BAOC_CHECK_ARG(ck));
+        if (wd) embed_grad_kernel<A(), G(), true><<<grid, kThreads, 0, s>>>(dout, dtable, b, accumulate, a BAOC_CHECK_ARG(ck));
+        else embed_grad_kernel<A(), G(), false><<<grid, kThreads, 0, s>>>(dout, dtable, b, accumulate, a BAOC_CHECK_ARG(ck));
         return launched("embed_grad_kernel");
     });
 } catch (const std::bad_alloc&) {
