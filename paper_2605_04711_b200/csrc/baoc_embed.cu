@@ -14,6 +14,9 @@ namespace baoc {
 constexpr int kGroupCtas = 128;        // id classes (one CTA each) of the grouping; doubled while a class has over kGroupBins ids
 constexpr int kGroupBins = 1024;       // most ids of a class: one thread of the CTA per id
 constexpr int kGroupWarps = 32;
+constexpr int kIdLoads = 8;            // ids a lane of the grouping has in flight
+constexpr int kListed = 128;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
+constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
 constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
 constexpr int kSlab = 256;             // columns of a warp of the sums
@@ -110,6 +113,7 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     extern __shared__ int32_t hist[];                   // [warps][bins]
     __shared__ int32_t s_warp[kGroupWarps];
     __shared__ int32_t s_less, s_end;
+    __shared__ uint32_t list[kGroupWarps][kListed];     // tokens of the class that a warp has found: {id of the class, token}
 #ifdef BAOC_CHECKED
     if (!check_range(ck, kKerEmbedGroup, start + size_t(blockIdx.x) * bins, 4ll * (bins + 1), 0) ||
         !check_range(ck, kKerEmbedGroup, perm, 4ll * n, 1) || !check_range(ck, kKerEmbedGroup, slots, 8ll * n_slots, 2) ||
@@ -121,17 +125,34 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     for (int i = threadIdx.x; i < kGroupWarps * bins; i += blockDim.x) hist[i] = 0;
     if (threadIdx.x == 0) s_less = 0;
     __syncthreads();
-    // a warp takes one stretch of the tokens, so that its list is in their order
+    // a warp takes one stretch of the tokens, kIdLoads ids per lane at a time; what it finds it counts and lists
     const int seg = ((n + kGroupWarps - 1) / kGroupWarps + 31) / 32 * 32;
     const int t0 = min(n, warp * seg), t1 = min(n, t0 + seg);
     int32_t* mine = hist + warp * bins;
-    int less = 0;
-    for (int t = t0 + lane; t < t1; t += 32) {
-        const int64_t id = int64_t(ids[t]);
-        if (id < 0 || id >= vocab || id == pad) continue;
-        const uint32_t c = uint32_t(id) & mask;
-        less += c < cls;
-        if (c == cls) atomicAdd(&mine[uint32_t(id) >> shift], 1);
+    int less = 0, found = 0;
+    for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
+        Id id[kIdLoads];
+#pragma unroll
+        for (int u = 0; u < kIdLoads; ++u) {
+            const int t = tb + 32 * u + lane;
+            id[u] = t < t1 ? __ldg(ids + t) : Id(-1);
+        }
+#pragma unroll
+        for (int u = 0; u < kIdLoads; ++u) {
+            const bool valid = id[u] >= 0 && int64_t(id[u]) < vocab && int64_t(id[u]) != pad;
+            const uint32_t c = uint32_t(id[u]) & mask;
+            less += valid && c < cls;
+            const bool in = valid && c == cls;
+            const uint32_t who = __ballot_sync(0xffffffffu, in);
+            if (who == 0u) continue;
+            if (in) {
+                const uint32_t bin = uint32_t(id[u]) >> shift;
+                const int at = found + __popc(who & ((1u << lane) - 1u));
+                if (at < kListed) list[warp][at] = bin << kListBits | uint32_t(tb + 32 * u + lane - t0);
+                atomicAdd(&mine[bin], 1);
+            }
+            found += __popc(who);
+        }
     }
     less = __reduce_add_sync(0xffffffffu, less);
     if (lane == 0 && less) atomicAdd(&s_less, less);
@@ -139,6 +160,7 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     // one thread per id: the warps' counts become offsets within the id, the ids' totals offsets within the list
     int total = 0;
     if (int(threadIdx.x) < bins) {
+#pragma unroll 8
         for (int w = 0; w < kGroupWarps; ++w) {
             const int x = hist[w * bins + threadIdx.x];
             hist[w * bins + threadIdx.x] = total;
@@ -157,6 +179,7 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     for (int w = 0; w < warp; ++w) before += s_warp[w];
     const int first = before + incl - total;
     if (int(threadIdx.x) < bins) {
+#pragma unroll 8
         for (int w = 0; w < kGroupWarps; ++w) hist[w * bins + threadIdx.x] += first;
         start[size_t(cls) * bins + threadIdx.x] = first;
         if (int(threadIdx.x) == bins - 1) {
@@ -175,13 +198,10 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
         const int len = chunk_tokens(total), chunks = (total + len - 1) / len, at = (first + kSlotTokens - 1) / kSlotTokens;
         for (int k = 0; k < chunks; ++k) slots[at + k] = make_int2(int(cls) * bins + int(threadIdx.x), k);
     }
-    for (int tb = t0; tb < t1; tb += 32) {
-        const int t = tb + lane;
-        const int64_t id = t < t1 ? int64_t(ids[t]) : -1;
-        const bool in = id >= 0 && id < vocab && id != pad && (uint32_t(id) & mask) == cls;
+    // places: equal ids among a warp's 32 candidates take consecutive ones, in the order of the lanes
+    auto place = [&](bool in, uint32_t bin, int t) {
         const uint32_t who = __ballot_sync(0xffffffffu, in);
         if (in) {
-            const uint32_t bin = uint32_t(id) >> shift;
             const uint32_t peers = __match_any_sync(who, bin);
             const int rank = __popc(peers & ((1u << lane) - 1u));
             const int at = mine[bin];
@@ -190,6 +210,28 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
             perm[at + rank] = t;
         }
         __syncwarp();
+    };
+    if (found <= kListed && seg <= 1 << kListBits) {
+        __syncwarp();
+        for (int i = 0; i < found; i += 32) {
+            const bool in = i + lane < found;
+            const uint32_t x = in ? list[warp][i + lane] : 0u;
+            place(in, x >> kListBits, t0 + int(x & ((1u << kListBits) - 1u)));
+        }
+    } else {
+        for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
+            Id id[kIdLoads];
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u) {
+                const int t = tb + 32 * u + lane;
+                id[u] = t < t1 ? __ldg(ids + t) : Id(-1);
+            }
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u) {
+                const bool in = id[u] >= 0 && int64_t(id[u]) < vocab && int64_t(id[u]) != pad && (uint32_t(id[u]) & mask) == cls;
+                place(in, uint32_t(id[u]) >> shift, tb + 32 * u + lane);
+            }
+        }
     }
 }
 
@@ -211,25 +253,22 @@ struct Part {
     static constexpr int es = DT == BAOC_BF16 ? 2 : 4;
     static constexpr int kWords = !WIDE ? 8 : (DT == BAOC_BF16 ? 4 : 8);
     uint32_t w[kWords];
+    // (columns beyond the row read its last ones instead; they are not written)
     __device__ __forceinline__ void load(const char* row, int col, int dim) {
         if constexpr (WIDE) {
-            if (col < dim) {
-                const uint4* p = reinterpret_cast<const uint4*>(row + int64_t(col) * es);
-                const uint4 a = __ldg(p);
-                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-                if constexpr (DT == BAOC_F32) {
-                    const uint4 b = __ldg(p + 1);
-                    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-                }
+            const uint4* p = reinterpret_cast<const uint4*>(row + int64_t(min(col, dim - 8)) * es);
+            const uint4 a = __ldg(p);
+            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+            if constexpr (DT == BAOC_F32) {
+                const uint4 b = __ldg(p + 1);
+                w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = col + 32 * j;
-                if (c < dim) {
-                    if constexpr (DT == BAOC_BF16) w[j] = uint32_t(__ldg(reinterpret_cast<const uint16_t*>(row) + c)) << 16;
-                    else w[j] = __ldg(reinterpret_cast<const uint32_t*>(row) + c);
-                }
+                const int c = min(col + 32 * j, dim - 1);
+                if constexpr (DT == BAOC_BF16) w[j] = uint32_t(__ldg(reinterpret_cast<const uint16_t*>(row) + c)) << 16;
+                else w[j] = __ldg(reinterpret_cast<const uint32_t*>(row) + c);
             }
         }
     }
@@ -308,7 +347,7 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
     float acc[8];
     if (item < b.n_slots / 4) {
         for (int q = 0; q < 4; ++q) {
-            const int slot = item * 4 + q;
+            const int slot = q * (b.n_slots / 4) + item;      // (neighbours, a long row's chunks, go to different warps)
 #ifdef BAOC_CHECKED
             if (!check_range(ck, kKerEmbedGrad, b.slots + slot, 8, 3)) return;
 #endif
@@ -334,8 +373,8 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
                 P x[kBatch];
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    const int64_t t = win.token(p + i);
-                    if (p + i < p1) x[i].load(src + t * a.src_stride * as, col, a.dim);
+                    const int64_t t = win.token(min(p + i, p1 - 1));
+                    x[i].load(src + t * a.src_stride * as, col, a.dim);
                 }
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i)
@@ -403,8 +442,8 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
             P x[kBatch];
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
-                const int64_t t = win.token(p + i);
-                if (p + i < p1) x[i].load(src + t * a.src_stride * as, col, a.dim);
+                const int64_t t = win.token(min(p + i, p1 - 1));
+                x[i].load(src + t * a.src_stride * as, col, a.dim);
             }
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
