@@ -15,12 +15,12 @@ constexpr int kGroupCtas = 128;        // id classes (one CTA each) of the group
 constexpr int kGroupBins = 1024;       // most ids of a class: one thread of the CTA per id
 constexpr int kGroupWarps = 32;
 constexpr int kIdLoads = 8;            // ids a lane of the grouping has in flight
-constexpr int kListed = 128;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
+constexpr int kListed = 512;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
 constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
 constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
 constexpr int kSlab = 256;             // columns of a warp of the sums
-constexpr int kGroupRows = 8;          // rows of a warp of the sums
+constexpr int kSegment = 32;           // rows and tokens, together, of a segment of the sums; at most the warp's lanes
 constexpr int kEmbedMaxDim = 1 << 24;
 constexpr int64_t kEmbedMaxStride = 1 << 28;           // (row products stay far inside 64 bits)
 
@@ -101,27 +101,60 @@ embed_kernel(const void* __restrict__ table, const Id* __restrict__ ids, void* _
 }
 
 // ---- gradient, first kernel: group the tokens by id -----------------------------------------------------------------
-// The ids fall into n_ctas = 2^shift classes by their low bits; CTA c lists the tokens of class c, ordered by id and
-// within an id by token.  Every CTA reads all ids and counts those of lower classes too, which is where its part of the
-// list begins: no CTA waits for another.  start[] has one entry per (class, id of the class) and one more, perm[] one
-// per listed token.
+// The ids fall into 2^shift classes by their low bits; CTA c lists the tokens of class c, grouped by id.  Every CTA reads
+// all ids and counts those of lower classes too, which is where its part of the order begins: no CTA waits for another,
+// nothing is left to chance, and frequent neighbouring ids fall into different classes.
+//
+// Left for the sums, all in the workspace (a row's index is class * bins + id of the class):
+struct GradBufs {
+    int32_t* start;      // per row index: its first place in perm; one more at the end
+    int32_t* perm;       // the tokens, grouped by id
+    uint2* segs;         // per segment: {first row index, its start}; one more at the end
+    int2* slots;         // chunks of the long rows: {row index, chunk}, or {-1, 0}
+    uint32_t* tickets;   // [slot][slab]: how many chunks of the row whose first slot this is are done
+    float* partial;      // [slot][slab][kSlab]: a chunk's sum
+    int shift, bins, slabs, n_segs, n_slots;
+};
+
+// A token id as the kernels take it: below vocab, or kNoId where it takes no part.
+constexpr uint32_t kNoId = 0xffffffffu;
+__device__ __forceinline__ uint32_t id_of(int32_t id, uint32_t vocab, uint32_t pad) {
+    const uint32_t u = uint32_t(id);
+    return u < vocab && u != pad ? u : kNoId;
+}
+__device__ __forceinline__ uint32_t id_of(int64_t id, uint32_t vocab, uint32_t pad) {
+    const uint32_t u = uint32_t(id);
+    return uint32_t(uint64_t(id) >> 32) == 0u && u < vocab && u != pad ? u : kNoId;
+}
+
+// Index of the last entry of the ascending a[0 .. n] that is <= x (a[0] <= x).
+__device__ __forceinline__ int last_not_above(const int32_t* a, int n, int32_t x) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
 template <typename Id>
 __global__ void __launch_bounds__(kGroupWarps * 32)
-embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad, int shift, int bins, int slabs, int n_slots,
-                   int32_t* __restrict__ start, int32_t* __restrict__ perm, int2* __restrict__ slots,
-                   uint32_t* __restrict__ tickets BAOC_CHECK_PARAM) {
-    extern __shared__ int32_t hist[];                   // [warps][bins]
+embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t pad, const GradBufs b BAOC_CHECK_PARAM) {
+    extern __shared__ int32_t smem[];
+    int32_t* hist = smem;                                                        // [warps][bins]
+    int32_t* begin = hist + kGroupWarps * b.bins;                                // [bins + 1]: start of the class's rows
+    uint32_t* list = reinterpret_cast<uint32_t*>(begin + b.bins + 1);            // [warps][kListed]: {id of the class, token}
     __shared__ int32_t s_warp[kGroupWarps];
-    __shared__ int32_t s_less, s_end;
-    __shared__ uint32_t list[kGroupWarps][kListed];     // tokens of the class that a warp has found: {id of the class, token}
+    __shared__ int32_t s_less;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = b.bins, shift = b.shift;
+    const uint32_t cls = blockIdx.x, mask = (1u << shift) - 1u, below = (1u << lane) - 1u;
+    const int64_t row0 = int64_t(cls) * bins;
 #ifdef BAOC_CHECKED
-    if (!check_range(ck, kKerEmbedGroup, start + size_t(blockIdx.x) * bins, 4ll * (bins + 1), 0) ||
-        !check_range(ck, kKerEmbedGroup, perm, 4ll * n, 1) || !check_range(ck, kKerEmbedGroup, slots, 8ll * n_slots, 2) ||
-        !check_range(ck, kKerEmbedGroup, tickets, 4ll * n_slots * slabs, 3))
+    if (!check_range(ck, kKerEmbedGroup, b.start + row0, 4ll * (bins + 1), 0) || !check_range(ck, kKerEmbedGroup, b.perm, 4ll * n, 1) ||
+        !check_range(ck, kKerEmbedGroup, b.slots, 8ll * b.n_slots, 2) || !check_range(ck, kKerEmbedGroup, b.segs, 8ll * (b.n_segs + 1), 3) ||
+        !check_range(ck, kKerEmbedGroup, b.tickets, 4ll * b.n_slots * b.slabs, 4))
         return;
 #endif
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t cls = blockIdx.x, mask = (1u << shift) - 1u;
     for (int i = threadIdx.x; i < kGroupWarps * bins; i += blockDim.x) hist[i] = 0;
     if (threadIdx.x == 0) s_less = 0;
     __syncthreads();
@@ -129,35 +162,45 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     const int seg = ((n + kGroupWarps - 1) / kGroupWarps + 31) / 32 * 32;
     const int t0 = min(n, warp * seg), t1 = min(n, t0 + seg);
     int32_t* mine = hist + warp * bins;
-    int less = 0, found = 0;
+    uint32_t* found = list + warp * kListed;
+    int less = 0, n_found = 0;
     for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
-        Id id[kIdLoads];
+        uint32_t id[kIdLoads];
+        Id raw[kIdLoads];
+        if (tb + 32 * kIdLoads <= t1) {
 #pragma unroll
-        for (int u = 0; u < kIdLoads; ++u) {
-            const int t = tb + 32 * u + lane;
-            id[u] = t < t1 ? __ldg(ids + t) : Id(-1);
+            for (int u = 0; u < kIdLoads; ++u) raw[u] = __ldg(ids + tb + lane + 32 * u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u) raw[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
         }
 #pragma unroll
+        for (int u = 0; u < kIdLoads; ++u) id[u] = id_of(raw[u], vocab, pad);
+        bool any = false;
+#pragma unroll
         for (int u = 0; u < kIdLoads; ++u) {
-            const bool valid = id[u] >= 0 && int64_t(id[u]) < vocab && int64_t(id[u]) != pad;
-            const uint32_t c = uint32_t(id[u]) & mask;
-            less += valid && c < cls;
-            const bool in = valid && c == cls;
+            const bool valid = id[u] != kNoId;
+            less += valid && (id[u] & mask) < cls;
+            any |= valid && (id[u] & mask) == cls;
+        }
+        if (!__any_sync(0xffffffffu, any)) continue;
+#pragma unroll
+        for (int u = 0; u < kIdLoads; ++u) {
+            const bool in = id[u] != kNoId && (id[u] & mask) == cls;
             const uint32_t who = __ballot_sync(0xffffffffu, in);
             if (who == 0u) continue;
             if (in) {
-                const uint32_t bin = uint32_t(id[u]) >> shift;
-                const int at = found + __popc(who & ((1u << lane) - 1u));
-                if (at < kListed) list[warp][at] = bin << kListBits | uint32_t(tb + 32 * u + lane - t0);
-                atomicAdd(&mine[bin], 1);
+                const int at = n_found + __popc(who & below);
+                if (at < kListed) found[at] = (id[u] >> shift) << kListBits | uint32_t(tb + 32 * u + lane - t0);
+                atomicAdd(&mine[id[u] >> shift], 1);
             }
-            found += __popc(who);
+            n_found += __popc(who);
         }
     }
     less = __reduce_add_sync(0xffffffffu, less);
     if (lane == 0 && less) atomicAdd(&s_less, less);
     __syncthreads();
-    // one thread per id: the warps' counts become offsets within the id, the ids' totals offsets within the list
+    // one thread per id: the warps' counts become offsets within the id, the ids' totals offsets within the order
     int total = 0;
     if (int(threadIdx.x) < bins) {
 #pragma unroll 8
@@ -181,72 +224,76 @@ embed_group_kernel(const Id* __restrict__ ids, int n, int64_t vocab, int64_t pad
     if (int(threadIdx.x) < bins) {
 #pragma unroll 8
         for (int w = 0; w < kGroupWarps; ++w) hist[w * bins + threadIdx.x] += first;
-        start[size_t(cls) * bins + threadIdx.x] = first;
+        begin[threadIdx.x] = first;
+        b.start[row0 + threadIdx.x] = first;
         if (int(threadIdx.x) == bins - 1) {
-            s_end = first + total;
-            if (cls == mask) start[size_t(cls + 1) * bins] = first + total;
+            begin[bins] = first + total;
+            if (cls == mask) b.start[row0 + bins] = first + total;
         }
     }
     __syncthreads();
-    // the chunk list: the slots that begin in this class's part of the order (the last class: all that follow, too)
-    const int slot0 = (s_less + kSlotTokens - 1) / kSlotTokens;
-    const int slot1 = cls == mask ? n_slots : (s_end + kSlotTokens - 1) / kSlotTokens;
-    for (int i = slot0 + threadIdx.x; i < slot1; i += blockDim.x) slots[i] = make_int2(-1, 0);
-    for (int64_t i = int64_t(slot0) * slabs + threadIdx.x; i < int64_t(slot1) * slabs; i += blockDim.x) tickets[i] = 0u;
-    __syncthreads();
-    if (int(threadIdx.x) < bins && total > kShortRow) {
-        const int len = chunk_tokens(total), chunks = (total + len - 1) / len, at = (first + kSlotTokens - 1) / kSlotTokens;
-        for (int k = 0; k < chunks; ++k) slots[at + k] = make_int2(int(cls) * bins + int(threadIdx.x), k);
-    }
     // places: equal ids among a warp's 32 candidates take consecutive ones, in the order of the lanes
     auto place = [&](bool in, uint32_t bin, int t) {
         const uint32_t who = __ballot_sync(0xffffffffu, in);
         if (in) {
             const uint32_t peers = __match_any_sync(who, bin);
-            const int rank = __popc(peers & ((1u << lane) - 1u));
+            const int rank = __popc(peers & below);
             const int at = mine[bin];
             __syncwarp(who);
             if (rank == 0) mine[bin] = at + __popc(peers);
-            perm[at + rank] = t;
+            b.perm[at + rank] = t;
         }
         __syncwarp();
     };
-    if (found <= kListed && seg <= 1 << kListBits) {
-        __syncwarp();
-        for (int i = 0; i < found; i += 32) {
-            const bool in = i + lane < found;
-            const uint32_t x = in ? list[warp][i + lane] : 0u;
+    if (n_found <= kListed && seg <= 1 << kListBits) {
+        for (int i = 0; i < n_found; i += 32) {
+            const bool in = i + lane < n_found;
+            const uint32_t x = in ? found[i + lane] : 0u;
             place(in, x >> kListBits, t0 + int(x & ((1u << kListBits) - 1u)));
         }
     } else {
         for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
-            Id id[kIdLoads];
+            uint32_t id[kIdLoads];
 #pragma unroll
             for (int u = 0; u < kIdLoads; ++u) {
                 const int t = tb + 32 * u + lane;
-                id[u] = t < t1 ? __ldg(ids + t) : Id(-1);
+                id[u] = t < t1 ? id_of(__ldg(ids + t), vocab, pad) : kNoId;
             }
 #pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) {
-                const bool in = id[u] >= 0 && int64_t(id[u]) < vocab && int64_t(id[u]) != pad && (uint32_t(id[u]) & mask) == cls;
-                place(in, uint32_t(id[u]) >> shift, tb + 32 * u + lane);
-            }
+            for (int u = 0; u < kIdLoads; ++u) place(id[u] != kNoId && (id[u] & mask) == cls, id[u] >> shift, tb + 32 * u + lane);
         }
     }
+    // Segments of the sums: row index + start grows by one per row and one per token; segment j begins with the first row
+    // where it has reached kSegment j.  This class names the segments that begin behind one of its rows.
+    const int end = begin[bins];
+    const int seg_lo = int((row0 + begin[0]) / kSegment) + 1, seg_hi = cls == mask ? b.n_segs : int((row0 + bins + end) / kSegment);
+    if (cls == 0u && threadIdx.x == 0) b.segs[0] = make_uint2(0u, 0u);
+    for (int j = seg_lo + threadIdx.x; j <= seg_hi; j += blockDim.x) {
+        int lo = 0, hi = bins;                          // the first row of the class (bins: the next class's) that has reached it
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (row0 + mid + begin[mid] >= int64_t(j) * kSegment) hi = mid; else lo = mid + 1;
+        }
+        b.segs[j] = make_uint2(uint32_t(row0 + lo), uint32_t(begin[lo]));
+    }
+    // Chunk list: the slots that begin in this class's part of the order (the last class: all that follow, too).
+    const int slot_lo = (begin[0] + kSlotTokens - 1) / kSlotTokens, slot_hi = cls == mask ? b.n_slots : (end + kSlotTokens - 1) / kSlotTokens;
+    for (int j = slot_lo + threadIdx.x; j < slot_hi; j += blockDim.x) {
+        int2 d = make_int2(-1, 0);
+        if (j * kSlotTokens < end) {
+            const int r = last_not_above(begin, bins, j * kSlotTokens), count = begin[r + 1] - begin[r];
+            if (count > kShortRow) {
+                const int len = chunk_tokens(count), k = j - (begin[r] + kSlotTokens - 1) / kSlotTokens;
+                if (k < (count + len - 1) / len) d = make_int2(int(row0 + r), k);
+            }
+        }
+        b.slots[j] = d;
+    }
+    for (int64_t i = int64_t(slot_lo) * b.slabs + threadIdx.x; i < int64_t(slot_hi) * b.slabs; i += blockDim.x) b.tickets[i] = 0u;
 }
 
 // ---- gradient, second kernel: sums of the grouped tokens ----------------------------------------------------------------
-// What the grouping leaves for the sums, all in the workspace.
-struct GradBufs {
-    const int32_t* start;      // per (class, id of the class): its first place in perm; one more at the end
-    const int32_t* perm;       // the tokens, grouped by id
-    const int2* slots;         // chunks of the rows named more than kShortRow times: {row as (class, id), chunk}, or {-1, 0}
-    uint32_t* tickets;         // [slot][slab]: chunks of the row that begins at the slot that are done
-    float* partial;            // [slot][slabs * kSlab]: a chunk's sum
-    int shift, bins, slabs, n_slots;
-};
-
-// Rows e, e + 1 .. of one thread's part of a slab: eight neighbours where rows are aligned for 16-byte loads, eight columns
+// One thread's part of a slab of one row: eight neighbours where rows are aligned for 16-byte loads, eight columns
 // that are 32 apart otherwise.
 template <int DT, bool WIDE>
 struct Part {
@@ -329,7 +376,7 @@ struct Window {
 // One warp works on 32 * 8 columns (a slab) of
 //   - four slots of the chunk list: each chunk's tokens are summed into the slot's partial sum, and the warp that finishes
 //     a row's last chunk adds the row's partial sums in their order;
-//   - or kGroupRows neighbours of the grouped order: the tokens of their short rows stream through, kBatch of them in
+//   - or one segment, neighbours of the grouped order: the tokens of their short rows stream through, kBatch of them in
 //     flight whatever rows they belong to, and a row is written when its last token has been added.
 template <int ACT, int GRAD, bool WIDE>
 __global__ void __launch_bounds__(kThreads)
@@ -342,7 +389,6 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
     const int slab = item % b.slabs;
     item /= b.slabs;
     const int col = slab * kSlab + lane * (WIDE ? 8 : 1);
-    const int n_idx = b.bins << b.shift;
     const char* src = static_cast<const char*>(dout);
     float acc[8];
     if (item < b.n_slots / 4) {
@@ -354,7 +400,7 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
             const int2 d = b.slots[slot];
             if (d.x < 0) continue;
 #ifdef BAOC_CHECKED
-            if (d.x >= n_idx) { check_fail(kChkBlockIndex, kKerEmbedGrad, d.x, n_idx, slot, 0); return; }
+            if (d.x >= int64_t(b.bins) << b.shift) { check_fail(kChkBlockIndex, kKerEmbedGrad, d.x, int64_t(b.bins) << b.shift, slot, 0); return; }
 #endif
             const int32_t s0 = b.start[d.x], count = b.start[d.x + 1] - s0;
             const int len = chunk_tokens(count), chunks = (count + len - 1) / len, first = slot - d.y;
@@ -407,16 +453,22 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
         return;
     }
     item -= b.n_slots / 4;
-    const int idx0 = item * kGroupRows;
-    if (idx0 >= n_idx) return;
-    const int rows = min(kGroupRows, n_idx - idx0);
+    if (item >= b.n_segs) return;
 #ifdef BAOC_CHECKED
-    if (!check_range(ck, kKerEmbedGrad, b.start + idx0, 4ll * (rows + 1), 0)) return;
+    if (!check_range(ck, kKerEmbedGrad, b.segs + item, 16, 6)) return;
 #endif
-    const int32_t st = b.start[idx0 + min(lane, rows)];
-    int cls = idx0 / b.bins;
-    int bin = idx0 - cls * b.bins;
-    auto start_of = [&](int r) { return __shfl_sync(0xffffffffu, st, r); };
+    const uint2 d0 = b.segs[item], d1 = b.segs[item + 1];
+    const int rows = int(d1.x - d0.x);                  // at most kSegment
+#ifdef BAOC_CHECKED
+    if (rows < 0 || rows > kSegment || !check_range(ck, kKerEmbedGrad, b.start + d0.x, 4ll * rows, 0)) {
+        check_fail(kChkBlockIndex, kKerEmbedGrad, d0.x, d1.x, item, 0);
+        return;
+    }
+#endif
+    const int32_t st = lane < rows ? b.start[size_t(d0.x) + lane] : int32_t(d1.y);
+    int cls = int(d0.x / uint32_t(b.bins));
+    int bin = int(d0.x - uint32_t(cls) * uint32_t(b.bins));
+    auto start_of = [&](int r) { return r < rows ? __shfl_sync(0xffffffffu, st, r) : int32_t(d1.y); };
     auto finish = [&](bool named) {                     // write the current row and step to the next
         const int64_t v = (int64_t(bin) << b.shift) + cls;
         if (v < a.vocab && (named || !accumulate)) write_part<GRAD, WIDE>(static_cast<char*>(dtable) + v * a.dst_stride * gs, col, acc, accumulate, a);
@@ -435,7 +487,7 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
 #ifdef BAOC_CHECKED
         if (!check_range(ck, kKerEmbedGrad, b.perm + p0, 4ll * (p1 - p0), 1)) return;
 #endif
-        int32_t row0 = p0, row1 = start_of(min(r + 1, rows));
+        int32_t row0 = p0, row1 = start_of(r + 1);
         Window win;
         for (int32_t p = p0; p < p1; p += kBatch) {
             if (((p - p0) & 31) == 0) win.open(b.perm, p, p1, lane);
@@ -462,7 +514,7 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
             finish(row1 > row0);
             row0 = row1;
             ++r;
-            row1 = start_of(min(r + 1, rows));
+            row1 = start_of(r + 1);
         }
         if (r < rows) {                                   // a long row: its chunks write it
             ++r;
@@ -516,7 +568,9 @@ void group_geometry(int64_t vocab, int* shift, int* bins) {
     *bins = int(ceil_div(vocab, int64_t(1) << s));
 }
 
-struct EmbedLayout { size_t start, perm, slots, tickets, partial, total; int shift, bins, slabs, n_slots; };
+int group_smem(int bins) { return 4 * (kGroupWarps * bins + bins + 1 + kGroupWarps * kListed); }
+
+struct EmbedLayout { size_t start, perm, segs, slots, tickets, partial, total; int shift, bins, slabs, n_segs, n_slots; };
 
 EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     EmbedLayout L{};
@@ -525,7 +579,9 @@ EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     L.perm = size_t(round_up(4 * ((int64_t(L.bins) << L.shift) + 1), 256));
     L.slabs = int(ceil_div(e->dim, kSlab));
     L.n_slots = int(round_up(ceil_div(n, kSlotTokens), 4));
-    L.slots = L.perm + size_t(round_up(4 * n, 256));
+    L.n_segs = int(ceil_div((int64_t(L.bins) << L.shift) + n, kSegment));
+    L.segs = L.perm + size_t(round_up(4 * n, 256));
+    L.slots = L.segs + size_t(round_up(8 * (int64_t(L.n_segs) + 1), 256));
     L.tickets = L.slots + size_t(round_up(8 * int64_t(L.n_slots), 256));
     L.partial = L.tickets + size_t(round_up(4 * int64_t(L.n_slots) * L.slabs, 256));
     L.total = L.partial + size_t(4 * int64_t(L.n_slots) * L.slabs * kSlab);
@@ -617,27 +673,25 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
         return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: dtable overlaps dout");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     char* w = static_cast<char*>(ws);
-    int32_t* start = reinterpret_cast<int32_t*>(w + L.start);
-    int32_t* perm = reinterpret_cast<int32_t*>(w + L.perm);
-    int2* slots = reinterpret_cast<int2*>(w + L.slots);
-    uint32_t* tickets = reinterpret_cast<uint32_t*>(w + L.tickets);
+    const GradBufs b{reinterpret_cast<int32_t*>(w + L.start), reinterpret_cast<int32_t*>(w + L.perm), reinterpret_cast<uint2*>(w + L.segs),
+                     reinterpret_cast<int2*>(w + L.slots), reinterpret_cast<uint32_t*>(w + L.tickets), reinterpret_cast<float*>(w + L.partial),
+                     L.shift, L.bins, L.slabs, L.n_segs, L.n_slots};
     const CheckCtx ck{w, w + L.total, 0, 0, 0};
     (void)ck;
-    const int64_t items = (L.n_slots / 4 + ceil_div(int64_t(L.bins) << L.shift, kGroupRows)) * L.slabs;
+    const int64_t items = (L.n_slots / 4 + int64_t(L.n_segs)) * L.slabs;
     if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: too many elements for one launch");
-    const int smem = 4 * kGroupWarps * L.bins;
+    const int smem = group_smem(L.bins);
     auto group = [&](auto id) {
         using Id = decltype(id);
-        const cudaError_t ce = cudaFuncSetAttribute(embed_group_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kGroupWarps * kGroupBins);
+        const cudaError_t ce = cudaFuncSetAttribute(embed_group_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, group_smem(kGroupBins));
         if (ce != cudaSuccess) return fail_embed(BAOC_E_CUDA, std::string("embed_group_kernel: ") + cudaGetErrorString(ce));
-        embed_group_kernel<Id><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const Id*>(ids), int(n_tokens), e->vocab, e->pad_id, L.shift,
-                                                                             L.bins, L.slabs, L.n_slots, start, perm, slots, tickets BAOC_CHECK_ARG(ck));
+        embed_group_kernel<Id><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const Id*>(ids), int(n_tokens), uint32_t(e->vocab),
+                                                                             uint32_t(e->pad_id), b BAOC_CHECK_ARG(ck));
         return launched("embed_group_kernel");
     };
     rc = e->id_bits == 64 ? group(int64_t(0)) : group(int32_t(0));
     if (rc) return rc;
     const EmbedArgs a{e->vocab, n_tokens, e->pad_id, as, gs, e->dim, e->scale};
-    const GradBufs b{start, perm, slots, tickets, reinterpret_cast<float*>(w + L.partial), L.shift, L.bins, L.slabs, L.n_slots};
     const bool wd = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
     const unsigned grid = unsigned(ceil_div(items * 32, kThreads));
     return with_types(e->act_dtype, e->grad_dtype, [&](auto A, auto G) {
