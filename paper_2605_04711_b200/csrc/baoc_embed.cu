@@ -19,7 +19,6 @@ constexpr int kListed = 512;           // tokens a warp of the grouping can list
 constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
 constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
-constexpr int kSlab = 256;             // columns of a warp of the sums
 constexpr int kSegment = 32;           // rows and tokens, together, of a segment of the sums; at most the warp's lanes
 constexpr int kEmbedMaxDim = 1 << 24;
 constexpr int64_t kEmbedMaxStride = 1 << 28;           // (row products stay far inside 64 bits)
@@ -30,43 +29,142 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     return r;
 }
 
-// V consecutive elements of a bf16 or fp32 row, as floats.
-template <int DT, int V>
-__device__ __forceinline__ void load_row(const void* row, int64_t e, float (&x)[V]) {
-    if constexpr (DT == BAOC_BF16) {
-        const uint16_t* p = static_cast<const uint16_t*>(row) + e;
-        if constexpr (V == 8) unpack8(__ldg(reinterpret_cast<const uint4*>(p)), x);
-        else x[0] = bf16_bits_to_float(__ldg(p));
-    } else {
-        const float* p = static_cast<const float*>(row) + e;
-        if constexpr (V == 8) f4_to8(__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1), x);
-        else x[0] = __ldg(p);
-    }
+// Loads of rows, requested ahead of their use.  Their uses below stand on every path that follows: a use behind a test of
+// its own would let the compiler move the request behind that test.
+__device__ __forceinline__ uint4 ld_row_u4(const void* p) {
+    uint4 r;
+    asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
 }
-template <int DT, int V>
-__device__ __forceinline__ void store_row(void* row, int64_t e, const float (&x)[V]) {
-    if constexpr (DT == BAOC_BF16) {
-        uint16_t* p = static_cast<uint16_t*>(row) + e;
-        if constexpr (V == 8) st_stream_u4(p, make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])));
-        else *p = uint16_t(bf16_pair(x[0], 0.f));
-    } else {
-        float* p = static_cast<float*>(row) + e;
-        if constexpr (V == 8) {
-            st_stream_f4(p, make_float4(x[0], x[1], x[2], x[3]));
-            st_stream_f4(p + 4, make_float4(x[4], x[5], x[6], x[7]));
+__device__ __forceinline__ uint2 ld_row_u2(const void* p) {
+    uint2 r;
+    asm volatile("ld.global.nc.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ uint32_t ld_row_u1(const void* p) {
+    uint32_t r;
+    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(r) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ uint32_t ld_row_bf16(const void* p) {
+    uint16_t r;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(r) : "l"(p));
+    return r;
+}
+
+// What the kernels take of a descriptor.  Row strides in bytes: 32 bits hold them, and a row's offset is one product.
+struct EmbedArgs {
+    uint32_t src_step, dst_step;
+    int dim;
+    float scale;
+};
+
+// A warp works on 32 * V columns (a slab) of a row.  A lane has V neighbours where base, row stride and dim allow 16-byte
+// accesses (VEC), and V columns that are 32 apart otherwise.  V = 8 for dim > 128, 4 for dim > 64, else 2: a narrower table
+// leaves fewer lanes idle.
+template <int DT, int V, bool VEC>
+struct Part {
+    static constexpr int kSize = DT == BAOC_BF16 ? 2 : 4;
+    static constexpr int kWords = VEC ? V * kSize / 4 : V;
+    uint32_t w[kWords];
+
+    // p: the lane's first column; last: bytes from there to the last column that the row can be read at
+    __device__ __forceinline__ void load(const char* p, int last) {
+        if constexpr (VEC) {
+            if constexpr (kWords == 1) w[0] = ld_row_u1(p);
+            if constexpr (kWords == 2) { const uint2 a = ld_row_u2(p); w[0] = a.x; w[1] = a.y; }
+            if constexpr (kWords >= 4) { const uint4 a = ld_row_u4(p); w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; }
+            if constexpr (kWords == 8) { const uint4 a = ld_row_u4(p + 16); w[4] = a.x; w[5] = a.y; w[6] = a.z; w[7] = a.w; }
         } else {
-            *p = x[0];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const char* q = p + min(j * 32 * kSize, last);
+                if constexpr (DT == BAOC_BF16) w[j] = ld_row_bf16(q) << 16;
+                else w[j] = ld_row_u1(q);
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int j) const {
+        if constexpr (VEC && DT == BAOC_BF16) return (j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]);
+        else return __uint_as_float(w[j]);
+    }
+};
+
+// The lane's first column, and what load() takes: columns beyond the row read its last ones instead.
+template <int V, bool VEC>
+__device__ __forceinline__ int lane_col(int slab, int lane) { return slab * 32 * V + lane * (VEC ? V : 1); }
+template <int V, bool VEC>
+__device__ __forceinline__ int read_col(int col, int dim) { return min(col, VEC ? dim - V : dim - 1); }
+
+// V values of a lane into a row (p: the lane's first column).
+template <int DT, int V, bool VEC>
+__device__ __forceinline__ void store_part(char* p, int col, int dim, const float (&y)[V]) {
+    if constexpr (VEC) {
+        if (col >= dim) return;
+        if constexpr (DT == BAOC_BF16) {
+            if constexpr (V == 8) st_stream_u4(p, make_uint4(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])));
+            if constexpr (V == 4) st_stream_u2(p, make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])));
+            if constexpr (V == 2) *reinterpret_cast<uint32_t*>(p) = bf16_pair(y[0], y[1]);
+        } else {
+            if constexpr (V >= 4) st_stream_f4(p, make_float4(y[0], y[1], y[2], y[3]));
+            if constexpr (V == 8) st_stream_f4(p + 16, make_float4(y[4], y[5], y[6], y[7]));
+            if constexpr (V == 2) *reinterpret_cast<float2*>(p) = make_float2(y[0], y[1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (col + 32 * j < dim) {
+                if constexpr (DT == BAOC_BF16) reinterpret_cast<uint16_t*>(p)[32 * j] = uint16_t(bf16_pair(y[j], 0.f));
+                else reinterpret_cast<float*>(p)[32 * j] = y[j];
+            }
         }
     }
 }
 
-// What the kernels take of a descriptor.  Strides in elements.
-struct EmbedArgs {
-    int64_t vocab, n, pad;
-    int64_t src_stride, dst_stride;
-    int dim;
-    float scale;
-};
+// A token id as the kernels take it: below vocab, or kNoId where it takes no part.  (pad: kNoId where there is none)
+constexpr uint32_t kNoId = 0xffffffffu;
+__device__ __forceinline__ uint32_t id_of(int32_t id, uint32_t vocab, uint32_t pad) {
+    const uint32_t u = uint32_t(id);
+    return u < vocab && u != pad ? u : kNoId;
+}
+__device__ __forceinline__ uint32_t id_of(int64_t id, uint32_t vocab, uint32_t pad) {
+    const uint32_t u = uint32_t(id);
+    return uint32_t(uint64_t(id) >> 32) == 0u && u < vocab && u != pad ? u : kNoId;
+}
+
+// ---- lookup: one warp per slab of kTokens tokens, all of their loads in flight -----------------------------------------
+template <int SRC, int DST, int V, bool VEC, typename Id>
+__global__ void __launch_bounds__(kThreads)
+embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* __restrict__ out, uint32_t vocab, int64_t n, int slabs,
+             const EmbedArgs a) {
+    using P = Part<SRC, V, VEC>;
+    constexpr int kTokens = P::kWords == 8 ? 4 : 8;
+    const int lane = threadIdx.x & 31;
+    const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int slab = int(item % uint32_t(slabs));
+    const int64_t t0 = int64_t(item / uint32_t(slabs)) * kTokens;
+    if (t0 >= n) return;
+    const int m = int(min64(n - t0, kTokens));
+    const uint32_t mine = id_of(__ldg(ids + t0 + min(lane, m - 1)), vocab, kNoId);
+    const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
+    const char* src = table + int64_t(rc) * P::kSize;
+    P x[kTokens];
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+        const uint32_t id = __shfl_sync(0xffffffffu, mine, i);
+        x[i].load(src + uint64_t(id == kNoId ? 0u : id) * a.src_step, last);
+    }
+    char* dst = out + int64_t(col) * (DST == BAOC_BF16 ? 2 : 4) + t0 * a.dst_step;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+        if (i >= m) break;
+        const bool named = __shfl_sync(0xffffffffu, mine, i) != kNoId;
+        float y[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] = named ? x[i].at(j) * a.scale : 0.f;
+        store_part<DST, V, VEC>(dst + int64_t(i) * a.dst_step, col, a.dim, y);
+    }
+}
 
 // Tokens of a chunk of a row that `count` > kShortRow tokens name: a power of two, at least as many as the row then has
 // chunks.  A row's chunks take the slots from ceil(start / kSlotTokens) on: as a chunk has at least 2 kSlotTokens tokens,
@@ -75,29 +173,6 @@ __host__ __device__ __forceinline__ int chunk_tokens(int count) {
     int len = kShortRow;
     while (int64_t(len) * len < count) len <<= 1;
     return len;
-}
-
-// ---- lookup: one thread per V elements of a row -----------------------------------------------------------------
-template <int SRC, int DST, int V, typename Id>
-__global__ void __launch_bounds__(kThreads)
-embed_kernel(const void* __restrict__ table, const Id* __restrict__ ids, void* __restrict__ out, const EmbedArgs a) {
-    constexpr int ss = SRC == BAOC_BF16 ? 2 : 4, ds = DST == BAOC_BF16 ? 2 : 4;
-    const int per_row = a.dim / V;
-    const int64_t k = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t t = k / per_row;
-    if (t >= a.n) return;
-    const int64_t e = (k - t * per_row) * V;
-    const int64_t id = int64_t(ids[t]);
-    float x[V];
-    if (id >= 0 && id < a.vocab) {
-        load_row<SRC, V>(static_cast<const char*>(table) + id * a.src_stride * ss, e, x);
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] *= a.scale;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = 0.f;
-    }
-    store_row<DST, V>(static_cast<char*>(out) + t * a.dst_stride * ds, e, x);
 }
 
 // ---- gradient, first kernel: group the tokens by id -----------------------------------------------------------------
@@ -112,20 +187,9 @@ struct GradBufs {
     uint2* segs;         // per segment: {first row index, its start}; one more at the end
     int2* slots;         // chunks of the long rows: {row index, chunk}, or {-1, 0}
     uint32_t* tickets;   // [slot][slab]: how many chunks of the row whose first slot this is are done
-    float* partial;      // [slot][slab][kSlab]: a chunk's sum
+    float* partial;      // [slot][slab][32 V]: a chunk's sum
     int shift, bins, slabs, n_segs, n_slots;
 };
-
-// A token id as the kernels take it: below vocab, or kNoId where it takes no part.
-constexpr uint32_t kNoId = 0xffffffffu;
-__device__ __forceinline__ uint32_t id_of(int32_t id, uint32_t vocab, uint32_t pad) {
-    const uint32_t u = uint32_t(id);
-    return u < vocab && u != pad ? u : kNoId;
-}
-__device__ __forceinline__ uint32_t id_of(int64_t id, uint32_t vocab, uint32_t pad) {
-    const uint32_t u = uint32_t(id);
-    return uint32_t(uint64_t(id) >> 32) == 0u && u < vocab && u != pad ? u : kNoId;
-}
 
 // Index of the last entry of the ascending a[0 .. n] that is <= x (a[0] <= x).
 __device__ __forceinline__ int last_not_above(const int32_t* a, int n, int32_t x) {
@@ -176,26 +240,31 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
         }
 #pragma unroll
         for (int u = 0; u < kIdLoads; ++u) id[u] = id_of(raw[u], vocab, pad);
-        bool any = false;
+        uint32_t hits = 0;                              // which of the lane's ids are of the class
 #pragma unroll
         for (int u = 0; u < kIdLoads; ++u) {
             const bool valid = id[u] != kNoId;
             less += valid && (id[u] & mask) < cls;
-            any |= valid && (id[u] & mask) == cls;
+            hits |= (valid && (id[u] & mask) == cls) ? 1u << u : 0u;
         }
-        if (!__any_sync(0xffffffffu, any)) continue;
+        if (!__any_sync(0xffffffffu, hits != 0u)) continue;
+        const int k = __popc(hits);
+        int upto = k;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        int at = n_found + upto - k;
 #pragma unroll
         for (int u = 0; u < kIdLoads; ++u) {
-            const bool in = id[u] != kNoId && (id[u] & mask) == cls;
-            const uint32_t who = __ballot_sync(0xffffffffu, in);
-            if (who == 0u) continue;
-            if (in) {
-                const int at = n_found + __popc(who & below);
+            if (hits >> u & 1u) {
                 if (at < kListed) found[at] = (id[u] >> shift) << kListBits | uint32_t(tb + 32 * u + lane - t0);
+                ++at;
                 atomicAdd(&mine[id[u] >> shift], 1);
             }
-            n_found += __popc(who);
         }
+        n_found += __shfl_sync(0xffffffffu, upto, 31);
     }
     less = __reduce_add_sync(0xffffffffu, less);
     if (lane == 0 && less) atomicAdd(&s_less, less);
@@ -293,76 +362,6 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
 }
 
 // ---- gradient, second kernel: sums of the grouped tokens ----------------------------------------------------------------
-// One thread's part of a slab of one row: eight neighbours where rows are aligned for 16-byte loads, eight columns
-// that are 32 apart otherwise.
-template <int DT, bool WIDE>
-struct Part {
-    static constexpr int es = DT == BAOC_BF16 ? 2 : 4;
-    static constexpr int kWords = !WIDE ? 8 : (DT == BAOC_BF16 ? 4 : 8);
-    uint32_t w[kWords];
-    // (columns beyond the row read its last ones instead; they are not written)
-    __device__ __forceinline__ void load(const char* row, int col, int dim) {
-        if constexpr (WIDE) {
-            const uint4* p = reinterpret_cast<const uint4*>(row + int64_t(min(col, dim - 8)) * es);
-            const uint4 a = __ldg(p);
-            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-            if constexpr (DT == BAOC_F32) {
-                const uint4 b = __ldg(p + 1);
-                w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = min(col + 32 * j, dim - 1);
-                if constexpr (DT == BAOC_BF16) w[j] = uint32_t(__ldg(reinterpret_cast<const uint16_t*>(row) + c)) << 16;
-                else w[j] = __ldg(reinterpret_cast<const uint32_t*>(row) + c);
-            }
-        }
-    }
-    __device__ __forceinline__ void add_to(float (&acc)[8]) const {
-        if constexpr (WIDE && DT == BAOC_BF16) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { acc[2 * j] += bf16_lo(w[j]); acc[2 * j + 1] += bf16_hi(w[j]); }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += __uint_as_float(w[j]);
-        }
-    }
-};
-
-// The finished sum of one row's slab: scaled, added to what is there or not, rounded once.
-template <int GRAD, bool WIDE>
-__device__ __forceinline__ void write_part(char* row, int col, const float (&sum)[8], int accumulate, const EmbedArgs& a) {
-    using E = typename std::conditional<GRAD == BAOC_BF16, uint16_t, float>::type;
-    E* p = reinterpret_cast<E*>(row);
-    float y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = sum[j] * a.scale;
-    if constexpr (WIDE) {
-        if (col >= a.dim) return;
-        if (accumulate) {
-            float old[8];
-            if constexpr (GRAD == BAOC_BF16) unpack8(*reinterpret_cast<const uint4*>(p + col), old);
-            else f4_to8(*reinterpret_cast<const float4*>(p + col), *reinterpret_cast<const float4*>(p + col + 4), old);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] += old[j];
-        }
-        store_row<GRAD, 8>(row, col, y);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = col + 32 * j;
-            if (c >= a.dim) continue;
-            if (accumulate) {
-                if constexpr (GRAD == BAOC_BF16) y[j] += bf16_bits_to_float(p[c]);
-                else y[j] += p[c];
-            }
-            const float one[1] = {y[j]};
-            store_row<GRAD, 1>(row, c, one);
-        }
-    }
-}
-
 // A warp's window of 32 places of perm, passed from lane to lane.
 struct Window {
     int32_t at, mine;
@@ -370,30 +369,67 @@ struct Window {
         at = p;
         mine = p + lane < end ? __ldg(perm + p + lane) : 0;
     }
-    __device__ __forceinline__ int32_t token(int32_t p) const { return __shfl_sync(0xffffffffu, mine, p - at); }
+    __device__ __forceinline__ uint32_t token(int32_t p) const { return uint32_t(__shfl_sync(0xffffffffu, mine, p - at)); }
 };
 
-// One warp works on 32 * 8 columns (a slab) of
+template <int V>
+__device__ __forceinline__ void load_partial(const float* p, float (&x)[V]) {
+    if constexpr (V == 2) { const float2 a = __ldcg(reinterpret_cast<const float2*>(p)); x[0] = a.x; x[1] = a.y; }
+    if constexpr (V >= 4) { const float4 a = __ldcg(reinterpret_cast<const float4*>(p)); x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; }
+    if constexpr (V == 8) { const float4 a = __ldcg(reinterpret_cast<const float4*>(p) + 1); x[4] = a.x; x[5] = a.y; x[6] = a.z; x[7] = a.w; }
+}
+template <int V>
+__device__ __forceinline__ void store_partial(float* p, const float (&x)[V]) {
+    if constexpr (V == 2) __stcg(reinterpret_cast<float2*>(p), make_float2(x[0], x[1]));
+    if constexpr (V >= 4) __stcg(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
+    if constexpr (V == 8) __stcg(reinterpret_cast<float4*>(p) + 1, make_float4(x[4], x[5], x[6], x[7]));
+}
+
+// The finished sum of one row's slab: scaled, added to what is there or not, rounded once.
+template <int GRAD, int V, bool VEC>
+__device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V], int accumulate, const EmbedArgs& a) {
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[j] = sum[j] * a.scale;
+    if (accumulate) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int k = VEC ? j : 32 * j;
+            if (col + k < a.dim) {
+                if constexpr (GRAD == BAOC_BF16) y[j] += bf16_bits_to_float(reinterpret_cast<const uint16_t*>(p)[k]);
+                else y[j] += reinterpret_cast<const float*>(p)[k];
+            }
+        }
+    }
+    store_part<GRAD, V, VEC>(p, col, a.dim, y);
+}
+
+// One warp works on one slab of
 //   - four slots of the chunk list: each chunk's tokens are summed into the slot's partial sum, and the warp that finishes
 //     a row's last chunk adds the row's partial sums in their order;
-//   - or one segment, neighbours of the grouped order: the tokens of their short rows stream through, kBatch of them in
-//     flight whatever rows they belong to, and a row is written when its last token has been added.
-template <int ACT, int GRAD, bool WIDE>
+//   - or one segment, neighbours of the grouped order: its unnamed rows are zeroed, the tokens of its short rows stream
+//     through, kBatch of them in flight whatever rows they belong to, and a row is written after its last token.
+template <int ACT, int GRAD, int V, bool VEC>
 __global__ void __launch_bounds__(kThreads)
-embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b, int accumulate, const EmbedArgs a BAOC_CHECK_PARAM) {
-    constexpr int as = ACT == BAOC_BF16 ? 2 : 4, gs = GRAD == BAOC_BF16 ? 2 : 4;
-    using P = Part<ACT, WIDE>;
-    constexpr int kBatch = P::kWords == 4 ? 8 : 4;
+embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b, uint32_t vocab, int n, int accumulate,
+                  const EmbedArgs a BAOC_CHECK_PARAM) {
+    using P = Part<ACT, V, VEC>;
+    constexpr int kBatch = P::kWords >= 8 ? 4 : (P::kWords == 4 ? 8 : 16);
     const int lane = threadIdx.x & 31;
-    int item = int(blockIdx.x) * (kThreads / 32) + int(threadIdx.x >> 5);
-    const int slab = item % b.slabs;
-    item /= b.slabs;
-    const int col = slab * kSlab + lane * (WIDE ? 8 : 1);
-    const char* src = static_cast<const char*>(dout);
-    float acc[8];
-    if (item < b.n_slots / 4) {
+    const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int slab = int(item % uint32_t(b.slabs));
+    int work = int(item / uint32_t(b.slabs));
+    const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
+    const char* src = dout + int64_t(rc) * P::kSize;
+    char* dst = dtable + int64_t(col) * (GRAD == BAOC_BF16 ? 2 : 4);
+    float acc[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+
+    if (work < b.n_slots / 4) {
+#pragma unroll 1
         for (int q = 0; q < 4; ++q) {
-            const int slot = q * (b.n_slots / 4) + item;      // (neighbours, a long row's chunks, go to different warps)
+            const int slot = q * (b.n_slots / 4) + work;      // (neighbours, a long row's chunks, go to different warps)
 #ifdef BAOC_CHECKED
             if (!check_range(ck, kKerEmbedGrad, b.slots + slot, 8, 3)) return;
 #endif
@@ -407,28 +443,29 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
             const int32_t p0 = s0 + d.y * len, p1 = min(p0 + len, s0 + count);
 #ifdef BAOC_CHECKED
             if (!check_range(ck, kKerEmbedGrad, b.perm + p0, 4ll * (p1 - p0), 1) ||
-                !check_range(ck, kKerEmbedGrad, b.partial + size_t(first) * b.slabs * kSlab, 4ll * chunks * b.slabs * kSlab, 4) ||
+                !check_range(ck, kKerEmbedGrad, b.partial + size_t(first) * b.slabs * 32 * V, 4ll * chunks * b.slabs * 32 * V, 4) ||
                 !check_range(ck, kKerEmbedGrad, b.tickets + size_t(first) * b.slabs + slab, 4, 5))
                 return;
+            for (int32_t p = p0; p < p1; ++p)
+                if (b.perm[p] < 0 || b.perm[p] >= n) { check_fail(kChkTileIndex, kKerEmbedGrad, b.perm[p], n, p, 2); return; }
 #endif
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
             Window win;
+#pragma unroll 1
             for (int32_t p = p0; p < p1; p += kBatch) {
                 if (((p - p0) & 31) == 0) win.open(b.perm, p, p1, lane);
                 P x[kBatch];
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const int64_t t = win.token(min(p + i, p1 - 1));
-                    x[i].load(src + t * a.src_stride * as, col, a.dim);
-                }
+                for (int i = 0; i < kBatch; ++i) x[i].load(src + uint64_t(win.token(min(p + i, p1 - 1))) * a.src_step, last);
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i)
-                    if (p + i < p1) x[i].add_to(acc);
+                    if (p + i < p1) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) acc[j] += x[i].at(j);
+                    }
             }
-            float* mine = b.partial + (size_t(slot) * b.slabs + slab) * kSlab + lane * 8;
-            __stcg(reinterpret_cast<float4*>(mine), make_float4(acc[0], acc[1], acc[2], acc[3]));
-            __stcg(reinterpret_cast<float4*>(mine) + 1, make_float4(acc[4], acc[5], acc[6], acc[7]));
+            store_partial<V>(b.partial + (size_t(slot) * b.slabs + slab) * (32 * V) + lane * V, acc);
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = 0.f;
             __threadfence();
             __syncwarp();
             uint32_t done = 0;
@@ -436,90 +473,92 @@ embed_grad_kernel(const void* __restrict__ dout, void* dtable, const GradBufs b,
             done = __shfl_sync(0xffffffffu, done, 0);
             if (int(done) != chunks - 1) continue;
             __threadfence();
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-            const float* part = b.partial + (size_t(first) * b.slabs + slab) * kSlab + lane * 8;
-#pragma unroll 4
+            const float* part = b.partial + (size_t(first) * b.slabs + slab) * (32 * V) + lane * V;
+#pragma unroll 8
             for (int k = 0; k < chunks; ++k) {
-                const float4* q4 = reinterpret_cast<const float4*>(part + size_t(k) * b.slabs * kSlab);
-                const float4 u = __ldcg(q4), v = __ldcg(q4 + 1);
-                acc[0] += u.x; acc[1] += u.y; acc[2] += u.z; acc[3] += u.w;
-                acc[4] += v.x; acc[5] += v.y; acc[6] += v.z; acc[7] += v.w;
+                float x[V];
+                load_partial<V>(part + size_t(k) * b.slabs * (32 * V), x);
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += x[j];
             }
-            const int cls = d.x / b.bins;
-            const int64_t v = (int64_t(d.x - cls * b.bins) << b.shift) + cls;
-            write_part<GRAD, WIDE>(static_cast<char*>(dtable) + v * a.dst_stride * gs, col, acc, accumulate, a);
+            const uint32_t cls = uint32_t(d.x) / uint32_t(b.bins), bin = uint32_t(d.x) - cls * uint32_t(b.bins);
+            write_row<GRAD, V, VEC>(dst + uint64_t((bin << b.shift) + cls) * a.dst_step, col, acc, accumulate, a);
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = 0.f;
         }
         return;
     }
-    item -= b.n_slots / 4;
-    if (item >= b.n_segs) return;
+    work -= b.n_slots / 4;
+    if (work >= b.n_segs) return;
 #ifdef BAOC_CHECKED
-    if (!check_range(ck, kKerEmbedGrad, b.segs + item, 16, 6)) return;
+    if (!check_range(ck, kKerEmbedGrad, b.segs + work, 16, 6)) return;
 #endif
-    const uint2 d0 = b.segs[item], d1 = b.segs[item + 1];
-    const int rows = int(d1.x - d0.x);                  // at most kSegment
+    const uint2 d0 = b.segs[work], d1 = b.segs[work + 1];
+    const int rows = int(d1.x - d0.x);                  // at most kSegment: one per lane
+    const int32_t end = int32_t(d1.y);
 #ifdef BAOC_CHECKED
-    if (rows < 0 || rows > kSegment || !check_range(ck, kKerEmbedGrad, b.start + d0.x, 4ll * rows, 0)) {
-        check_fail(kChkBlockIndex, kKerEmbedGrad, d0.x, d1.x, item, 0);
+    if (rows < 0 || rows > kSegment || !check_range(ck, kKerEmbedGrad, b.start + size_t(d0.x), 4ll * rows, 0) ||
+        !check_range(ck, kKerEmbedGrad, b.perm + d0.y, 4ll * (end - int32_t(d0.y)), 1)) {
+        check_fail(kChkBlockIndex, kKerEmbedGrad, d0.x, d1.x, work, 0);
         return;
     }
+    for (int32_t p = int32_t(d0.y); p < end; ++p)
+        if (b.perm[p] < 0 || b.perm[p] >= n) { check_fail(kChkTileIndex, kKerEmbedGrad, b.perm[p], n, p, 2); return; }
 #endif
-    const int32_t st = lane < rows ? b.start[size_t(d0.x) + lane] : int32_t(d1.y);
-    int cls = int(d0.x / uint32_t(b.bins));
-    int bin = int(d0.x - uint32_t(cls) * uint32_t(b.bins));
-    auto start_of = [&](int r) { return r < rows ? __shfl_sync(0xffffffffu, st, r) : int32_t(d1.y); };
-    auto finish = [&](bool named) {                     // write the current row and step to the next
-        const int64_t v = (int64_t(bin) << b.shift) + cls;
-        if (v < a.vocab && (named || !accumulate)) write_part<GRAD, WIDE>(static_cast<char*>(dtable) + v * a.dst_stride * gs, col, acc, accumulate, a);
+    Window win;
+    win.open(b.perm, int32_t(d0.y), end, lane);
+    // lane r has row r of the segment: the table's row, its first place and its number of tokens
+    const int32_t st = lane < rows ? b.start[size_t(d0.x) + lane] : end;
+    const uint32_t idx = d0.x + uint32_t(lane), cls = idx / uint32_t(b.bins);
+    const uint32_t row = ((idx - cls * uint32_t(b.bins)) << b.shift) + cls;
+    const int32_t up = __shfl_down_sync(0xffffffffu, st, 1);
+    const int count = lane < rows ? (lane == 31 ? end : up) - st : 0;
+    const uint32_t longs = __ballot_sync(0xffffffffu, count > kShortRow);
+    if (!accumulate) {
+        float zero[V];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-        if (++bin == b.bins) { bin = 0; ++cls; }
-    };
+        for (int j = 0; j < V; ++j) zero[j] = 0.f;
+        uint32_t unnamed = __ballot_sync(0xffffffffu, lane < rows && count == 0 && row < vocab);
+        while (unnamed) {
+            const int r = __ffs(unnamed) - 1;
+            unnamed &= unnamed - 1u;
+            store_part<GRAD, V, VEC>(dst + uint64_t(__shfl_sync(0xffffffffu, row, r)) * a.dst_step, col, a.dim, zero);
+        }
+    }
+    // the runs of short rows between the long ones (which their chunks write)
+    int32_t p0 = int32_t(d0.y);
+    for (uint32_t rest = longs;; rest &= rest - 1u) {
+        const int next = rest ? __ffs(rest) - 1 : 0;
+        const int32_t p1 = rest ? __shfl_sync(0xffffffffu, st, next) : end;
+        if (p0 < p1) {
+            // the row of a place: the last one that begins at it or before
+            int r = __popc(__ballot_sync(0xffffffffu, lane < rows && st <= p0)) - 1;
+            int32_t row_end = __shfl_sync(0xffffffffu, st + count, r);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    int r = 0;
-    while (r < rows) {
-        // the rows up to the next long one
-        int upto = r;
-        while (upto < rows && start_of(upto + 1) - start_of(upto) <= kShortRow) ++upto;
-        const int32_t p0 = start_of(r), p1 = start_of(upto);
-#ifdef BAOC_CHECKED
-        if (!check_range(ck, kKerEmbedGrad, b.perm + p0, 4ll * (p1 - p0), 1)) return;
-#endif
-        int32_t row0 = p0, row1 = start_of(r + 1);
-        Window win;
-        for (int32_t p = p0; p < p1; p += kBatch) {
-            if (((p - p0) & 31) == 0) win.open(b.perm, p, p1, lane);
-            P x[kBatch];
+            for (int j = 0; j < V; ++j) acc[j] = 0.f;
+#pragma unroll 1
+            for (int32_t p = p0; p < p1; p += kBatch) {
+                if (((p - p0) & 31) == 0 && p != win.at) win.open(b.perm, p, p1, lane);
+                P x[kBatch];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int64_t t = win.token(min(p + i, p1 - 1));
-                x[i].load(src + t * a.src_stride * as, col, a.dim);
-            }
+                for (int i = 0; i < kBatch; ++i) x[i].load(src + uint64_t(win.token(min(p + i, p1 - 1))) * a.src_step, last);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                if (p + i < p1) {
-                    while (p + i == row1) {
-                        finish(row1 > row0);
-                        row0 = row1;
-                        ++r;
-                        row1 = start_of(r + 1);
+                for (int i = 0; i < kBatch; ++i) {
+                    // (what a last batch adds behind p1 belongs to no row: no row ends within a batch behind p1)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[j] += x[i].at(j);
+                    if (p + i + 1 == row_end) {
+                        write_row<GRAD, V, VEC>(dst + uint64_t(__shfl_sync(0xffffffffu, row, r)) * a.dst_step, col, acc, accumulate, a);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) acc[j] = 0.f;
+                        r = __popc(__ballot_sync(0xffffffffu, lane < rows && st <= row_end)) - 1;
+                        row_end = __shfl_sync(0xffffffffu, st + count, r);
                     }
-                    x[i].add_to(acc);
                 }
             }
         }
-        while (r < upto) {
-            finish(row1 > row0);
-            row0 = row1;
-            ++r;
-            row1 = start_of(r + 1);
-        }
-        if (r < rows) {                                   // a long row: its chunks write it
-            ++r;
-            if (++bin == b.bins) { bin = 0; ++cls; }
-        }
+        if (rest == 0u) break;
+        p0 = __shfl_sync(0xffffffffu, st + count, next);
     }
 }
 
@@ -551,7 +590,7 @@ int check_embed(const baoc_embed_t* e, const char* what) {
 
 bool aligned(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & uintptr_t(bytes - 1)) == 0; }
 
-// Whether rows of this array can be read and written 8 elements at a time.
+// Whether rows of this array can be read and written 16 bytes at a time.
 bool wide(const void* p, int64_t stride, int64_t eb, int dim) { return dim % 8 == 0 && aligned(p, 16) && (stride * eb) % 16 == 0; }
 
 bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
@@ -568,6 +607,7 @@ void group_geometry(int64_t vocab, int* shift, int* bins) {
     *bins = int(ceil_div(vocab, int64_t(1) << s));
 }
 
+int columns_per_warp(int dim) { return dim > 128 ? 256 : (dim > 64 ? 128 : 64); }
 int group_smem(int bins) { return 4 * (kGroupWarps * bins + bins + 1 + kGroupWarps * kListed); }
 
 struct EmbedLayout { size_t start, perm, segs, slots, tickets, partial, total; int shift, bins, slabs, n_segs, n_slots; };
@@ -577,36 +617,38 @@ EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     group_geometry(e->vocab, &L.shift, &L.bins);
     L.start = 0;
     L.perm = size_t(round_up(4 * ((int64_t(L.bins) << L.shift) + 1), 256));
-    L.slabs = int(ceil_div(e->dim, kSlab));
+    L.slabs = int(ceil_div(e->dim, columns_per_warp(e->dim)));
     L.n_slots = int(round_up(ceil_div(n, kSlotTokens), 4));
     L.n_segs = int(ceil_div((int64_t(L.bins) << L.shift) + n, kSegment));
     L.segs = L.perm + size_t(round_up(4 * n, 256));
     L.slots = L.segs + size_t(round_up(8 * (int64_t(L.n_segs) + 1), 256));
     L.tickets = L.slots + size_t(round_up(8 * int64_t(L.n_slots), 256));
     L.partial = L.tickets + size_t(round_up(4 * int64_t(L.n_slots) * L.slabs, 256));
-    L.total = L.partial + size_t(4 * int64_t(L.n_slots) * L.slabs * kSlab);
+    L.total = L.partial + size_t(4 * int64_t(L.n_slots) * L.slabs * columns_per_warp(e->dim));
     return L;
 }
 
+// f(source type, destination type, V, VEC) for the types, the row length and the alignment of a call, as constants.
+template <int S, int D, typename F>
+int with_shape(int dim, bool vec, F f) {
+    using std::integral_constant;
+    const integral_constant<int, S> s{};
+    const integral_constant<int, D> d{};
+    const std::true_type y{};
+    const std::false_type n{};
+    if (dim > 128) return vec ? f(s, d, integral_constant<int, 8>{}, y) : f(s, d, integral_constant<int, 8>{}, n);
+    if (dim > 64) return vec ? f(s, d, integral_constant<int, 4>{}, y) : f(s, d, integral_constant<int, 4>{}, n);
+    return vec ? f(s, d, integral_constant<int, 2>{}, y) : f(s, d, integral_constant<int, 2>{}, n);
+}
 template <typename F>
-int with_types(int a, int b, F f) {
-    if (a == BAOC_F32) return b == BAOC_F32 ? f(std::integral_constant<int, BAOC_F32>{}, std::integral_constant<int, BAOC_F32>{})
-                                            : f(std::integral_constant<int, BAOC_F32>{}, std::integral_constant<int, BAOC_BF16>{});
-    return b == BAOC_F32 ? f(std::integral_constant<int, BAOC_BF16>{}, std::integral_constant<int, BAOC_F32>{})
-                         : f(std::integral_constant<int, BAOC_BF16>{}, std::integral_constant<int, BAOC_BF16>{});
+int with_types(int a, int b, int dim, bool vec, F f) {
+    if (a == BAOC_F32) return b == BAOC_F32 ? with_shape<BAOC_F32, BAOC_F32>(dim, vec, f) : with_shape<BAOC_F32, BAOC_BF16>(dim, vec, f);
+    return b == BAOC_F32 ? with_shape<BAOC_BF16, BAOC_F32>(dim, vec, f) : with_shape<BAOC_BF16, BAOC_BF16>(dim, vec, f);
 }
 
 int launched(const char* kernel) {
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BAOC_OK : fail_embed(BAOC_E_CUDA, std::string(kernel) + ": " + cudaGetErrorString(e));
-}
-
-template <int S, int D, int V, typename Id>
-int launch_embed(const void* table, const void* ids, void* out, const EmbedArgs& a, cudaStream_t s) {
-    const int64_t blocks = ceil_div(a.n * (a.dim / V), kThreads);
-    if (blocks > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed: too many elements for one launch");
-    embed_kernel<S, D, V, Id><<<unsigned(blocks), kThreads, 0, s>>>(table, static_cast<const Id*>(ids), out, a);
-    return launched("embed_kernel");
 }
 
 }  // namespace
@@ -634,12 +676,21 @@ int baoc_embed(const baoc_embed_t* e, const void* table, const void* ids, int64_
     if (n_tokens > (int64_t(1) << 40) / os) return fail_embed(BAOC_E_INVALID, "baoc_embed: too many tokens");
     if (ts == e->dim && os == e->dim && overlap(table, e->vocab * ts * tb, out, n_tokens * os * ob))
         return fail_embed(BAOC_E_INVALID, "baoc_embed: out overlaps the table");
-    const EmbedArgs a{e->vocab, n_tokens, e->pad_id, ts, os, e->dim, e->scale};
-    const bool w = wide(table, ts, tb, e->dim) && wide(out, os, ob, e->dim);
+    const EmbedArgs a{uint32_t(ts * tb), uint32_t(os * ob), e->dim, e->scale};
+    const int slabs = int(ceil_div(e->dim, columns_per_warp(e->dim)));
+    const bool vec = wide(table, ts, tb, e->dim) && wide(out, os, ob, e->dim);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return with_types(e->table_dtype, e->act_dtype, [&](auto S, auto D) {
-        if (w) return e->id_bits == 64 ? launch_embed<S(), D(), 8, int64_t>(table, ids, out, a, s) : launch_embed<S(), D(), 8, int32_t>(table, ids, out, a, s);
-        return e->id_bits == 64 ? launch_embed<S(), D(), 1, int64_t>(table, ids, out, a, s) : launch_embed<S(), D(), 1, int32_t>(table, ids, out, a, s);
+    return with_types(e->table_dtype, e->act_dtype, e->dim, vec, [&](auto S, auto D, auto V, auto VEC) {
+        constexpr int kTokens = Part<S(), V(), VEC()>::kWords == 8 ? 4 : 8;
+        const int64_t items = ceil_div(n_tokens, kTokens) * slabs, blocks = ceil_div(items, kThreads / 32);
+        if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed: too many elements for one launch");
+        const char* tab = static_cast<const char*>(table);
+        char* o = static_cast<char*>(out);
+        if (e->id_bits == 64)
+            embed_kernel<S(), D(), V(), VEC(), int64_t><<<unsigned(blocks), kThreads, 0, s>>>(tab, static_cast<const int64_t*>(ids), o, uint32_t(e->vocab), n_tokens, slabs, a);
+        else
+            embed_kernel<S(), D(), V(), VEC(), int32_t><<<unsigned(blocks), kThreads, 0, s>>>(tab, static_cast<const int32_t*>(ids), o, uint32_t(e->vocab), n_tokens, slabs, a);
+        return launched("embed_kernel");
     });
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
@@ -691,12 +742,12 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     };
     rc = e->id_bits == 64 ? group(int64_t(0)) : group(int32_t(0));
     if (rc) return rc;
-    const EmbedArgs a{e->vocab, n_tokens, e->pad_id, as, gs, e->dim, e->scale};
-    const bool wd = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
-    const unsigned grid = unsigned(ceil_div(items * 32, kThreads));
-    return with_types(e->act_dtype, e->grad_dtype, [&](auto A, auto G) {
-        if (wd) embed_grad_kernel<A(), G(), true><<<grid, kThreads, 0, s>>>(dout, dtable, b, accumulate, a BAOC_CHECK_ARG(ck));
-        else embed_grad_kernel<A(), G(), false><<<grid, kThreads, 0, s>>>(dout, dtable, b, accumulate, a BAOC_CHECK_ARG(ck));
+    const EmbedArgs a{uint32_t(as * ab), uint32_t(gs * gb), e->dim, e->scale};
+    const bool vec = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
+    const unsigned grid = unsigned(ceil_div(items, kThreads / 32));
+    return with_types(e->act_dtype, e->grad_dtype, e->dim, vec, [&](auto A, auto G, auto V, auto VEC) {
+        embed_grad_kernel<A(), G(), V(), VEC()><<<grid, kThreads, 0, s>>>(static_cast<const char*>(dout), static_cast<char*>(dtable), b, uint32_t(e->vocab),
+                                                                          int(n_tokens), accumulate, a BAOC_CHECK_ARG(ck));
         return launched("embed_grad_kernel");
     });
 } catch (const std::bad_alloc&) {
