@@ -18,6 +18,9 @@ constexpr int kIdLoads = 8;            // ids a lane of the grouping has in flig
 constexpr int kListed = 512;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
 constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
+constexpr int kMostChunks = 512;
+constexpr int kJoin = 16;              // chunks whose partial sums one warp adds; a longer row's are added in two levels
+constexpr int kSlotWarps = 16;         // warps that share a run of 32 slots
 constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
 constexpr int kSegment = 32;           // rows and tokens, together, of a segment of the sums; at most the warp's lanes
 constexpr int kEmbedMaxDim = 1 << 24;
@@ -166,14 +169,16 @@ embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* _
     }
 }
 
-// Tokens of a chunk of a row that `count` > kShortRow tokens name: a power of two, at least as many as the row then has
-// chunks.  A row's chunks take the slots from ceil(start / kSlotTokens) on: as a chunk has at least 2 kSlotTokens tokens,
-// the last one's slot still begins inside the row, so no two rows share a slot.
+// A row that `count` > kShortRow tokens name is cut into chunks of kShortRow tokens, or of the next power of two that leaves
+// about kMostChunks of them; a rest of less than half a chunk goes to the last one.  Chunk k of a row takes slot
+// ceil(start / kSlotTokens) + k * len / kSlotTokens: that slot begins inside the row, as the last chunk has at least
+// len / 2 >= kSlotTokens tokens, so no two rows share a slot.
 __host__ __device__ __forceinline__ int chunk_tokens(int count) {
     int len = kShortRow;
-    while (int64_t(len) * len < count) len <<= 1;
+    while (int64_t(len) * kMostChunks < count) len <<= 1;
     return len;
 }
+__host__ __device__ __forceinline__ int chunks_of(int count, int len) { return int((int64_t(count) + len / 2) / len); }
 
 // ---- gradient, first kernel: group the tokens by id -----------------------------------------------------------------
 // The ids fall into 2^shift classes by their low bits; CTA c lists the tokens of class c, grouped by id.  Every CTA reads
@@ -186,7 +191,7 @@ struct GradBufs {
     int32_t* perm;       // the tokens, grouped by id
     uint2* segs;         // per segment: {first row index, its start}; one more at the end
     int2* slots;         // chunks of the long rows: {row index, chunk}, or {-1, 0}
-    uint32_t* tickets;   // [slot][slab]: how many chunks of the row whose first slot this is are done
+    uint32_t* tickets;   // [slot][slab][2]: chunks done of the kJoin whose first slot this is; such groups done of the row
     float* partial;      // [slot][slab][32 V]: a chunk's sum
     int shift, bins, slabs, n_segs, n_slots;
 };
@@ -216,7 +221,7 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
 #ifdef BAOC_CHECKED
     if (!check_range(ck, kKerEmbedGroup, b.start + row0, 4ll * (bins + 1), 0) || !check_range(ck, kKerEmbedGroup, b.perm, 4ll * n, 1) ||
         !check_range(ck, kKerEmbedGroup, b.slots, 8ll * b.n_slots, 2) || !check_range(ck, kKerEmbedGroup, b.segs, 8ll * (b.n_segs + 1), 3) ||
-        !check_range(ck, kKerEmbedGroup, b.tickets, 4ll * b.n_slots * b.slabs, 4))
+        !check_range(ck, kKerEmbedGroup, b.tickets, 8ll * b.n_slots * b.slabs, 4))
         return;
 #endif
     for (int i = threadIdx.x; i < kGroupWarps * bins; i += blockDim.x) hist[i] = 0;
@@ -352,13 +357,13 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
         if (j * kSlotTokens < end) {
             const int r = last_not_above(begin, bins, j * kSlotTokens), count = begin[r + 1] - begin[r];
             if (count > kShortRow) {
-                const int len = chunk_tokens(count), k = j - (begin[r] + kSlotTokens - 1) / kSlotTokens;
-                if (k < (count + len - 1) / len) d = make_int2(int(row0 + r), k);
+                const int len = chunk_tokens(count), at = j - (begin[r] + kSlotTokens - 1) / kSlotTokens, k = at / (len / kSlotTokens);
+                if (at == k * (len / kSlotTokens) && k < chunks_of(count, len)) d = make_int2(int(row0 + r), k);
             }
         }
         b.slots[j] = d;
     }
-    for (int64_t i = int64_t(slot_lo) * b.slabs + threadIdx.x; i < int64_t(slot_hi) * b.slabs; i += blockDim.x) b.tickets[i] = 0u;
+    for (int64_t i = int64_t(slot_lo) * b.slabs * 2 + threadIdx.x; i < int64_t(slot_hi) * b.slabs * 2; i += blockDim.x) b.tickets[i] = 0u;
 }
 
 // ---- gradient, second kernel: sums of the grouped tokens ----------------------------------------------------------------
@@ -385,6 +390,31 @@ __device__ __forceinline__ void store_partial(float* p, const float (&x)[V]) {
     if constexpr (V == 8) __stcg(reinterpret_cast<float4*>(p) + 1, make_float4(x[4], x[5], x[6], x[7]));
 }
 
+// After this warp has stored a sum: whether it is the last of n to come to the ticket (then it may read the others' sums).
+__device__ __forceinline__ bool last_to_come(uint32_t* ticket, int n, int lane) {
+    __threadfence();
+    __syncwarp();
+    uint32_t before = 0;
+    if (lane == 0) before = atomicAdd(ticket, 1u);
+    before = __shfl_sync(0xffffffffu, before, 0);
+    if (before != uint32_t(n - 1)) return false;
+    __threadfence();
+    return true;
+}
+
+template <int V>
+__device__ __forceinline__ void join_partials(const float* part, size_t step, int n, float (&sum)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) {
+        float x[V];
+        load_partial<V>(part + size_t(k) * step, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += x[j];
+    }
+}
+
 // The finished sum of one row's slab: scaled, added to what is there or not, rounded once.
 template <int GRAD, int V, bool VEC>
 __device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V], int accumulate, const EmbedArgs& a) {
@@ -405,8 +435,7 @@ __device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V
 }
 
 // One warp works on one slab of
-//   - four slots of the chunk list: each chunk's tokens are summed into the slot's partial sum, and the warp that finishes
-//     a row's last chunk adds the row's partial sums in their order;
+//   - some of 32 slots of the chunk list: each chunk's tokens are summed into the slot's partial sum;
 //   - or one segment, neighbours of the grouped order: its unnamed rows are zeroed, the tokens of its short rows stream
 //     through, kBatch of them in flight whatever rows they belong to, and a row is written after its last token.
 template <int ACT, int GRAD, int V, bool VEC>
@@ -426,25 +455,30 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = 0.f;
 
-    if (work < b.n_slots / 4) {
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-            const int slot = q * (b.n_slots / 4) + work;      // (neighbours, a long row's chunks, go to different warps)
+    const int slot_work = b.n_slots / 32 * kSlotWarps;
+    if (work < slot_work) {
+        const int run = work / kSlotWarps * 32;
 #ifdef BAOC_CHECKED
-            if (!check_range(ck, kKerEmbedGrad, b.slots + slot, 8, 3)) return;
+        if (!check_range(ck, kKerEmbedGrad, b.slots + run, 8ll * 32, 3)) return;
 #endif
-            const int2 d = b.slots[slot];
-            if (d.x < 0) continue;
+        const int2 listed = b.slots[run + lane];
+        const uint32_t used = __ballot_sync(0xffffffffu, listed.x >= 0);
+        // the warps of a run take its chunks in turn
+        uint32_t todo = __ballot_sync(0xffffffffu, listed.x >= 0 && __popc(used & ((1u << lane) - 1u)) % kSlotWarps == work % kSlotWarps);
+#pragma unroll 1
+        for (; todo; todo &= todo - 1u) {
+            const int at = __ffs(todo) - 1, slot = run + at;
+            const int2 d = make_int2(__shfl_sync(0xffffffffu, listed.x, at), __shfl_sync(0xffffffffu, listed.y, at));
 #ifdef BAOC_CHECKED
             if (d.x >= int64_t(b.bins) << b.shift) { check_fail(kChkBlockIndex, kKerEmbedGrad, d.x, int64_t(b.bins) << b.shift, slot, 0); return; }
 #endif
             const int32_t s0 = b.start[d.x], count = b.start[d.x + 1] - s0;
-            const int len = chunk_tokens(count), chunks = (count + len - 1) / len, first = slot - d.y;
-            const int32_t p0 = s0 + d.y * len, p1 = min(p0 + len, s0 + count);
+            const int len = chunk_tokens(count), chunks = chunks_of(count, len), apart = len / kSlotTokens, first = slot - d.y * apart;
+            const int32_t p0 = s0 + d.y * len, p1 = d.y == chunks - 1 ? s0 + count : p0 + len;
 #ifdef BAOC_CHECKED
             if (!check_range(ck, kKerEmbedGrad, b.perm + p0, 4ll * (p1 - p0), 1) ||
-                !check_range(ck, kKerEmbedGrad, b.partial + size_t(first) * b.slabs * 32 * V, 4ll * chunks * b.slabs * 32 * V, 4) ||
-                !check_range(ck, kKerEmbedGrad, b.tickets + size_t(first) * b.slabs + slab, 4, 5))
+                !check_range(ck, kKerEmbedGrad, b.partial + size_t(first) * b.slabs * 32 * V, 4ll * ((chunks - 1) * apart + 1) * b.slabs * 32 * V, 4) ||
+                !check_range(ck, kKerEmbedGrad, b.tickets + size_t(first) * b.slabs * 2, 8ll * ((chunks - 1) * apart + 1) * b.slabs, 5))
                 return;
             for (int32_t p = p0; p < p1; ++p)
                 if (b.perm[p] < 0 || b.perm[p] >= n) { check_fail(kChkTileIndex, kKerEmbedGrad, b.perm[p], n, p, 2); return; }
@@ -463,32 +497,32 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
                         for (int j = 0; j < V; ++j) acc[j] += x[i].at(j);
                     }
             }
-            store_partial<V>(b.partial + (size_t(slot) * b.slabs + slab) * (32 * V) + lane * V, acc);
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] = 0.f;
-            __threadfence();
-            __syncwarp();
-            uint32_t done = 0;
-            if (lane == 0) done = atomicAdd(b.tickets + size_t(first) * b.slabs + slab, 1u);
-            done = __shfl_sync(0xffffffffu, done, 0);
-            if (int(done) != chunks - 1) continue;
-            __threadfence();
-            const float* part = b.partial + (size_t(first) * b.slabs + slab) * (32 * V) + lane * V;
-#pragma unroll 8
-            for (int k = 0; k < chunks; ++k) {
-                float x[V];
-                load_partial<V>(part + size_t(k) * b.slabs * (32 * V), x);
-#pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] += x[j];
+            // the slot's partial sum; whoever brings the last of kJoin neighbours adds them up, and whoever brings the last
+            // of those sums writes the row.  Nobody waits, and each sum has its fixed order.
+            const size_t step = size_t(apart) * b.slabs * (32 * V);
+            float* part = b.partial + (size_t(first) * b.slabs + slab) * (32 * V) + lane * V;
+            uint32_t* tickets = b.tickets + (size_t(first) * b.slabs + slab) * 2;
+            store_partial<V>(part + size_t(d.y) * step, acc);
+            const int group = d.y / kJoin, in_group = min(kJoin, chunks - group * kJoin), groups = (chunks + kJoin - 1) / kJoin;
+            bool mine = last_to_come(tickets + size_t(group) * kJoin * apart * b.slabs * 2, in_group, lane);
+            if (mine) {
+                join_partials<V>(part + size_t(group) * kJoin * step, step, in_group, acc);
+                if (groups > 1) {
+                    store_partial<V>(part + size_t(group) * kJoin * step, acc);
+                    mine = last_to_come(tickets + 1, groups, lane);
+                    if (mine) join_partials<V>(part, size_t(kJoin) * step, groups, acc);
+                }
             }
-            const uint32_t cls = uint32_t(d.x) / uint32_t(b.bins), bin = uint32_t(d.x) - cls * uint32_t(b.bins);
-            write_row<GRAD, V, VEC>(dst + uint64_t((bin << b.shift) + cls) * a.dst_step, col, acc, accumulate, a);
+            if (mine) {
+                const uint32_t cls = uint32_t(d.x) / uint32_t(b.bins), bin = uint32_t(d.x) - cls * uint32_t(b.bins);
+                write_row<GRAD, V, VEC>(dst + uint64_t((bin << b.shift) + cls) * a.dst_step, col, acc, accumulate, a);
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] = 0.f;
         }
         return;
     }
-    work -= b.n_slots / 4;
+    work -= slot_work;
     if (work >= b.n_segs) return;
 #ifdef BAOC_CHECKED
     if (!check_range(ck, kKerEmbedGrad, b.segs + work, 16, 6)) return;
@@ -618,12 +652,12 @@ EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     L.start = 0;
     L.perm = size_t(round_up(4 * ((int64_t(L.bins) << L.shift) + 1), 256));
     L.slabs = int(ceil_div(e->dim, columns_per_warp(e->dim)));
-    L.n_slots = int(round_up(ceil_div(n, kSlotTokens), 4));
+    L.n_slots = int(round_up(ceil_div(n, kSlotTokens), 32));
     L.n_segs = int(ceil_div((int64_t(L.bins) << L.shift) + n, kSegment));
     L.segs = L.perm + size_t(round_up(4 * n, 256));
     L.slots = L.segs + size_t(round_up(8 * (int64_t(L.n_segs) + 1), 256));
     L.tickets = L.slots + size_t(round_up(8 * int64_t(L.n_slots), 256));
-    L.partial = L.tickets + size_t(round_up(4 * int64_t(L.n_slots) * L.slabs, 256));
+    L.partial = L.tickets + size_t(round_up(8 * int64_t(L.n_slots) * L.slabs, 256));
     L.total = L.partial + size_t(4 * int64_t(L.n_slots) * L.slabs * columns_per_warp(e->dim));
     return L;
 }
@@ -729,7 +763,7 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
                      L.shift, L.bins, L.slabs, L.n_segs, L.n_slots};
     const CheckCtx ck{w, w + L.total, 0, 0, 0};
     (void)ck;
-    const int64_t items = (L.n_slots / 4 + int64_t(L.n_segs)) * L.slabs;
+    const int64_t items = (int64_t(L.n_slots / 32) * kSlotWarps + L.n_segs) * L.slabs;
     if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: too many elements for one launch");
     const int smem = group_smem(L.bins);
     auto group = [&](auto id) {
