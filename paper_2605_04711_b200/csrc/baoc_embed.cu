@@ -14,7 +14,7 @@ namespace baoc {
 constexpr int kGroupCtas = 128;        // id classes (one CTA each) of the grouping; doubled while a class has over kGroupBins ids
 constexpr int kGroupBins = 1024;       // most ids of a class: one thread of the CTA per id
 constexpr int kGroupWarps = 32;
-constexpr int kIdLoads = 8;            // ids a lane of the grouping has in flight
+constexpr int kIdLoads = 16;           // ids a lane of the grouping has in flight
 constexpr int kListed = 512;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
 constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
@@ -124,16 +124,9 @@ __device__ __forceinline__ void store_part(char* p, int col, int dim, const floa
     }
 }
 
-// A token id as the kernels take it: below vocab, or kNoId where it takes no part.  (pad: kNoId where there is none)
-constexpr uint32_t kNoId = 0xffffffffu;
-__device__ __forceinline__ uint32_t id_of(int32_t id, uint32_t vocab, uint32_t pad) {
-    const uint32_t u = uint32_t(id);
-    return u < vocab && u != pad ? u : kNoId;
-}
-__device__ __forceinline__ uint32_t id_of(int64_t id, uint32_t vocab, uint32_t pad) {
-    const uint32_t u = uint32_t(id);
-    return uint32_t(uint64_t(id) >> 32) == 0u && u < vocab && u != pad ? u : kNoId;
-}
+// A token id's low word, and whether it names a row.
+__device__ __forceinline__ bool is_row(int32_t id, uint32_t vocab) { return uint32_t(id) < vocab; }
+__device__ __forceinline__ bool is_row(int64_t id, uint32_t vocab) { return uint32_t(uint64_t(id) >> 32) == 0u && uint32_t(id) < vocab; }
 
 // ---- lookup: one warp per slab of kTokens tokens, all of their loads in flight -----------------------------------------
 template <int SRC, int DST, int V, bool VEC, typename Id>
@@ -148,23 +141,20 @@ embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* _
     const int64_t t0 = int64_t(item / uint32_t(slabs)) * kTokens;
     if (t0 >= n) return;
     const int m = int(min64(n - t0, kTokens));
-    const uint32_t mine = id_of(__ldg(ids + t0 + min(lane, m - 1)), vocab, kNoId);
+    const Id own = __ldg(ids + t0 + min(lane, m - 1));
+    const uint32_t row = is_row(own, vocab) ? uint32_t(own) : 0u, named = __ballot_sync(0xffffffffu, is_row(own, vocab));
     const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
     const char* src = table + int64_t(rc) * P::kSize;
     P x[kTokens];
 #pragma unroll
-    for (int i = 0; i < kTokens; ++i) {
-        const uint32_t id = __shfl_sync(0xffffffffu, mine, i);
-        x[i].load(src + uint64_t(id == kNoId ? 0u : id) * a.src_step, last);
-    }
+    for (int i = 0; i < kTokens; ++i) x[i].load(src + uint64_t(__shfl_sync(0xffffffffu, row, i)) * a.src_step, last);
     char* dst = out + int64_t(col) * (DST == BAOC_BF16 ? 2 : 4) + t0 * a.dst_step;
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
         if (i >= m) break;
-        const bool named = __shfl_sync(0xffffffffu, mine, i) != kNoId;
         float y[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = named ? x[i].at(j) * a.scale : 0.f;
+        for (int j = 0; j < V; ++j) y[j] = named >> i & 1u ? x[i].at(j) * a.scale : 0.f;
         store_part<DST, V, VEC>(dst + int64_t(i) * a.dst_step, col, a.dim, y);
     }
 }
@@ -210,6 +200,7 @@ template <typename Id>
 __global__ void __launch_bounds__(kGroupWarps * 32)
 embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t pad, const GradBufs b BAOC_CHECK_PARAM) {
     extern __shared__ int32_t smem[];
+    let_later_kernel_start();
     int32_t* hist = smem;                                                        // [warps][bins]
     int32_t* begin = hist + kGroupWarps * b.bins;                                // [bins + 1]: start of the class's rows
     uint32_t* list = reinterpret_cast<uint32_t*>(begin + b.bins + 1);            // [warps][kListed]: {id of the class, token}
@@ -224,33 +215,33 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
         !check_range(ck, kKerEmbedGroup, b.tickets, 8ll * b.n_slots * b.slabs, 4))
         return;
 #endif
-    for (int i = threadIdx.x; i < kGroupWarps * bins; i += blockDim.x) hist[i] = 0;
+    // a warp takes one stretch of the tokens, at least one round of kIdLoads ids per lane; what it finds it counts and lists
+    const int warps = max(1, min(kGroupWarps, (n + 32 * kIdLoads - 1) / (32 * kIdLoads)));
+    const int seg = (n + warps * 32 - 1) / (warps * 32) * 32;
+    const int t0 = min(n, warp * seg), t1 = warp < warps ? min(n, t0 + seg) : t0;
+    for (int i = threadIdx.x; i < warps * bins; i += blockDim.x) hist[i] = 0;
     if (threadIdx.x == 0) s_less = 0;
     __syncthreads();
-    // a warp takes one stretch of the tokens, kIdLoads ids per lane at a time; what it finds it counts and lists
-    const int seg = ((n + kGroupWarps - 1) / kGroupWarps + 31) / 32 * 32;
-    const int t0 = min(n, warp * seg), t1 = min(n, t0 + seg);
     int32_t* mine = hist + warp * bins;
     uint32_t* found = list + warp * kListed;
     int less = 0, n_found = 0;
     for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
-        uint32_t id[kIdLoads];
-        Id raw[kIdLoads];
+        Id id[kIdLoads];
         if (tb + 32 * kIdLoads <= t1) {
 #pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) raw[u] = __ldg(ids + tb + lane + 32 * u);
+            for (int u = 0; u < kIdLoads; ++u) id[u] = __ldg(ids + tb + lane + 32 * u);
         } else {
 #pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) raw[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
+            for (int u = 0; u < kIdLoads; ++u) id[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
         }
-#pragma unroll
-        for (int u = 0; u < kIdLoads; ++u) id[u] = id_of(raw[u], vocab, pad);
         uint32_t hits = 0;                              // which of the lane's ids are of the class
 #pragma unroll
         for (int u = 0; u < kIdLoads; ++u) {
-            const bool valid = id[u] != kNoId;
-            less += valid && (id[u] & mask) < cls;
-            hits |= (valid && (id[u] & mask) == cls) ? 1u << u : 0u;
+            const uint32_t c = uint32_t(id[u]) & mask;
+            if (is_row(id[u], vocab) && uint32_t(id[u]) != pad) {
+                if (c < cls) ++less;
+                if (c == cls) hits |= 1u << u;
+            }
         }
         if (!__any_sync(0xffffffffu, hits != 0u)) continue;
         const int k = __popc(hits);
@@ -264,9 +255,9 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
 #pragma unroll
         for (int u = 0; u < kIdLoads; ++u) {
             if (hits >> u & 1u) {
-                if (at < kListed) found[at] = (id[u] >> shift) << kListBits | uint32_t(tb + 32 * u + lane - t0);
+                if (at < kListed) found[at] = (uint32_t(id[u]) >> shift) << kListBits | uint32_t(tb + 32 * u + lane - t0);
                 ++at;
-                atomicAdd(&mine[id[u] >> shift], 1);
+                atomicAdd(&mine[uint32_t(id[u]) >> shift], 1);
             }
         }
         n_found += __shfl_sync(0xffffffffu, upto, 31);
@@ -278,7 +269,7 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
     int total = 0;
     if (int(threadIdx.x) < bins) {
 #pragma unroll 8
-        for (int w = 0; w < kGroupWarps; ++w) {
+        for (int w = 0; w < warps; ++w) {
             const int x = hist[w * bins + threadIdx.x];
             hist[w * bins + threadIdx.x] = total;
             total += x;
@@ -292,12 +283,8 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
     }
     if (lane == 31) s_warp[warp] = incl;
     __syncthreads();
-    int before = s_less;
-    for (int w = 0; w < warp; ++w) before += s_warp[w];
-    const int first = before + incl - total;
+    const int first = s_less + __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0) + incl - total;
     if (int(threadIdx.x) < bins) {
-#pragma unroll 8
-        for (int w = 0; w < kGroupWarps; ++w) hist[w * bins + threadIdx.x] += first;
         begin[threadIdx.x] = first;
         b.start[row0 + threadIdx.x] = first;
         if (int(threadIdx.x) == bins - 1) {
@@ -306,37 +293,6 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
         }
     }
     __syncthreads();
-    // places: equal ids among a warp's 32 candidates take consecutive ones, in the order of the lanes
-    auto place = [&](bool in, uint32_t bin, int t) {
-        const uint32_t who = __ballot_sync(0xffffffffu, in);
-        if (in) {
-            const uint32_t peers = __match_any_sync(who, bin);
-            const int rank = __popc(peers & below);
-            const int at = mine[bin];
-            __syncwarp(who);
-            if (rank == 0) mine[bin] = at + __popc(peers);
-            b.perm[at + rank] = t;
-        }
-        __syncwarp();
-    };
-    if (n_found <= kListed && seg <= 1 << kListBits) {
-        for (int i = 0; i < n_found; i += 32) {
-            const bool in = i + lane < n_found;
-            const uint32_t x = in ? found[i + lane] : 0u;
-            place(in, x >> kListBits, t0 + int(x & ((1u << kListBits) - 1u)));
-        }
-    } else {
-        for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
-            uint32_t id[kIdLoads];
-#pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) {
-                const int t = tb + 32 * u + lane;
-                id[u] = t < t1 ? id_of(__ldg(ids + t), vocab, pad) : kNoId;
-            }
-#pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) place(id[u] != kNoId && (id[u] & mask) == cls, id[u] >> shift, tb + 32 * u + lane);
-        }
-    }
     // Segments of the sums: row index + start grows by one per row and one per token; segment j begins with the first row
     // where it has reached kSegment j.  This class names the segments that begin behind one of its rows.
     const int end = begin[bins];
@@ -352,7 +308,7 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
     }
     // Chunk list: the slots that begin in this class's part of the order (the last class: all that follow, too).
     const int slot_lo = (begin[0] + kSlotTokens - 1) / kSlotTokens, slot_hi = cls == mask ? b.n_slots : (end + kSlotTokens - 1) / kSlotTokens;
-    for (int j = slot_lo + threadIdx.x; j < slot_hi; j += blockDim.x) {
+    for (int j = slot_lo + int(blockDim.x - 1 - threadIdx.x); j < slot_hi; j += blockDim.x) {      // (other warps than the segments')
         int2 d = make_int2(-1, 0);
         if (j * kSlotTokens < end) {
             const int r = last_not_above(begin, bins, j * kSlotTokens), count = begin[r + 1] - begin[r];
@@ -364,6 +320,36 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
         b.slots[j] = d;
     }
     for (int64_t i = int64_t(slot_lo) * b.slabs * 2 + threadIdx.x; i < int64_t(slot_hi) * b.slabs * 2; i += blockDim.x) b.tickets[i] = 0u;
+
+    // places: equal ids among a warp's 32 candidates take consecutive ones, in the order of the lanes
+    auto place = [&](bool in, uint32_t bin, int t) {
+        const uint32_t who = __ballot_sync(0xffffffffu, in);
+        if (in) {
+            const uint32_t peers = __match_any_sync(who, bin);
+            const int rank = __popc(peers & below);
+            const int at = mine[bin];
+            __syncwarp(who);
+            if (rank == 0) mine[bin] = at + __popc(peers);
+            b.perm[begin[bin] + at + rank] = t;
+        }
+        __syncwarp();
+    };
+    if (n_found <= kListed && seg <= 1 << kListBits) {
+        for (int i = 0; i < n_found; i += 32) {
+            const bool in = i + lane < n_found;
+            const uint32_t x = in ? found[i + lane] : 0u;
+            place(in, x >> kListBits, t0 + int(x & ((1u << kListBits) - 1u)));
+        }
+    } else {
+        for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
+            Id id[kIdLoads];
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u) id[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u)
+                place(is_row(id[u], vocab) && uint32_t(id[u]) != pad && (uint32_t(id[u]) & mask) == cls, uint32_t(id[u]) >> shift, tb + 32 * u + lane);
+        }
+    }
 }
 
 // ---- gradient, second kernel: sums of the grouped tokens ----------------------------------------------------------------
@@ -446,6 +432,7 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
     constexpr int kBatch = P::kWords >= 8 ? 4 : (P::kWords == 4 ? 8 : 16);
     const int lane = threadIdx.x & 31;
     const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    wait_for_earlier_kernel();
     const int slab = int(item % uint32_t(b.slabs));
     int work = int(item / uint32_t(b.slabs));
     const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
@@ -780,9 +767,9 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     const bool vec = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
     const unsigned grid = unsigned(ceil_div(items, kThreads / 32));
     return with_types(e->act_dtype, e->grad_dtype, e->dim, vec, [&](auto A, auto G, auto V, auto VEC) {
-        embed_grad_kernel<A(), G(), V(), VEC()><<<grid, kThreads, 0, s>>>(static_cast<const char*>(dout), static_cast<char*>(dtable), b, uint32_t(e->vocab),
-                                                                          int(n_tokens), accumulate, a BAOC_CHECK_ARG(ck));
-        return launched("embed_grad_kernel");
+        const cudaError_t ce = launch_behind(embed_grad_kernel<A(), G(), V(), VEC()>, grid, kThreads, s, static_cast<const char*>(dout),
+                                             static_cast<char*>(dtable), b, uint32_t(e->vocab), int(n_tokens), accumulate, a BAOC_CHECK_ARG(ck));
+        return ce == cudaSuccess ? BAOC_OK : fail_embed(BAOC_E_CUDA, std::string("embed_grad_kernel: ") + cudaGetErrorString(ce));
     });
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
