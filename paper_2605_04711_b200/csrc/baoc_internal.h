@@ -126,29 +126,39 @@ struct Tile {
     uint32_t piece;
 };
 
-// Gradient norm and clip.  A tile is large enough for eight 16-byte loads in flight per thread of its CTA.
-constexpr int kClipTile = 16384;
+// Gradient norm and clip.  The blocks' elements are dealt to the CTAs in equal contiguous shares of whole tiles; what a CTA
+// has of one block is a segment.
+constexpr int kNormTile = 8192;
+constexpr int kNormCtasPerSm = 4;
+constexpr int kNormCtas = kNormCtasPerSm * 148;
+constexpr int kClipTile = 16384;      // elements of a CTA of the clip,
+constexpr int kClipTileSmall = 4096;  // and where all blocks together have fewer than
+constexpr int64_t kClipSmallTotal = 1 << 25;
 constexpr int kClipPtrChunk = 256;    // pointers that one launch of the table kernel carries by value
 
-// Per-block record (device copy lives in the clip workspace).
-struct ClipBlock {
-    int64_t numel;
-    int64_t tile0;       // index of the block's first tile
-    int32_t ntiles;
+struct ClipSeg {
+    int64_t first;       // element of the block
+    int64_t count;
+    int32_t block;
     int32_t pad;
 };
-// The clip workspace.  tickets: one per block, then the count of finished blocks; all zero between calls.
+struct ClipCta {
+    int32_t seg0, seg1;  // the share: segments seg0 .. seg1
+    ClipSeg seg;         // the first of them
+};
+// The clip workspace.  Block i has the segments block_seg[i] .. block_seg[i + 1].  ticket: CTAs of the norm that have ended; zero between calls.
 struct ClipBufs {
-    const ClipBlock* blocks;
-    const Tile* tiles;
+    const Tile* tiles;   // of the clip, in its order
+    const int64_t* numel;
+    const ClipSeg* segs;
+    const ClipCta* ctas;
+    const int32_t* block_seg;
     const void** src;
     void** dst;
-    double* partials;    // per tile: its sum of squares
-    double* bsq;         // per block: its sum of squares
-    uint32_t* tickets;
+    double* partials;    // per segment: its sum of squares
+    uint32_t* ticket;
     float* factor;       // the clip factor that the last norm left
-    int64_t n_tiles;
-    int n_blocks;
+    int n_tiles, clip_tile, n_ctas, n_segs, n_blocks;
 };
 struct ClipPtrs { const void* p[kClipPtrChunk]; };
 
