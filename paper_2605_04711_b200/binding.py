@@ -255,7 +255,16 @@ def pointer_table(tensors: Sequence[torch.Tensor]):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
+    """The current device's current stream (the default stream as long as the process has not used CUDA)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if torch.cuda.is_initialized() else 0
+
+
+def _queue(device: int, call, *args) -> int:
+    """call(*args, that device's current stream), with the device current."""
+    if device == torch._C._cuda_getDevice():
+        return call(*args, torch._C._cuda_getCurrentRawStream(device))
+    with torch.cuda.device(device):
+        return call(*args, torch._C._cuda_getCurrentRawStream(device))
 
 
 def _np_ptr(a: Optional[np.ndarray]):
@@ -271,8 +280,6 @@ def _dtype_code(dtype: torch.dtype) -> int:
 
 def _rows(t: torch.Tensor, dim: int, what: str):
     """(rows, elements from row to row) of a device tensor [..., dim] whose leading dimensions step evenly."""
-    if not t.is_cuda:
-        raise BaocError(E_INVALID, f"{what} must be a CUDA tensor")
     if t.dim() < 1 or t.shape[-1] != dim:
         raise BaocError(E_INVALID, f"{what} must be [..., {dim}], not {list(t.shape)}")
     if t.is_contiguous():
@@ -288,6 +295,9 @@ def _rows(t: torch.Tensor, dim: int, what: str):
     return m.shape[0], (m.stride(0) if m.shape[0] > 1 else dim)
 
 
+_ID_BITS = {torch.int32: 32, torch.int64: 64}
+
+
 class Embedding:
     """The token table's lookup (``baoc_embed``) and gradient (``baoc_embed_grad``): a plan of one table's shape.
 
@@ -296,73 +306,64 @@ class Embedding:
 
     def __init__(self, vocab: int, dim: int, scale: float = 1.0, pad_id: Optional[int] = None):
         self.vocab, self.dim = int(vocab), int(dim)
-        self._e = Embed(self.vocab, max(-1, min(self.dim, 2 ** 31 - 1)), DTYPES[torch.float32], DTYPES[torch.bfloat16], DTYPES[torch.bfloat16], 64,
-                        float(scale), -1 if pad_id is None else int(pad_id), 0, 0, 0)
+        self._e = Embed(self.vocab, max(-1, min(self.dim, 2 ** 31 - 1)), DTYPES[torch.float32], DTYPES[torch.bfloat16],
+                        DTYPES[torch.bfloat16], 64, float(scale), -1 if pad_id is None else int(pad_id), 0, 0, 0)
         self._ref = C.byref(self._e)
         self._n = C.c_size_t()
         self.grad_workspace_bytes(0)                        # the descriptor's checks
 
     @staticmethod
-    def _check(rc: int):
-        if rc < 0:
-            raise BaocError(rc, _lib.baoc_embed_last_error().decode())
-
-    def _ids(self, ids: torch.Tensor) -> torch.Tensor:
-        if ids.dtype == torch.int64:
-            self._e.id_bits = 64
-        elif ids.dtype == torch.int32:
-            self._e.id_bits = 32
-        else:
-            raise BaocError(E_INVALID, f"token ids must be int32 or int64, not {ids.dtype}")
-        return ids if ids.is_contiguous() else ids.contiguous()
+    def _failed(rc: int):
+        raise BaocError(rc, _lib.baoc_embed_last_error().decode())
 
     def lookup(self, table: torch.Tensor, ids: torch.Tensor, out: Optional[torch.Tensor] = None,
                out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-        """out[..., :] = scale * table[ids[...], :].  table: [vocab, dim] fp32 or bf16; ids: int32 or int64 of any shape;
-        out: ids' shape + [dim] (allocated as out_dtype when not given); rows of table and out may be strided."""
-        e = self._e
+        """out[..., :] = scale * table[ids[...], :].  table: [vocab, dim] fp32 or bf16; ids: int32 or int64 of any shape (a
+        non-contiguous one is copied first); out: ids' shape + [dim] (allocated as out_dtype when not given); rows of
+        table and out may be strided."""
         if out is None:
             out = torch.empty((*ids.shape, self.dim), dtype=out_dtype, device=table.device)
+        e, dev = self._e, table.get_device()
         rows, e.table_stride = _rows(table, self.dim, "table")
         n, e.act_stride = _rows(out, self.dim, "out")
-        e.table_dtype, e.act_dtype = _dtype_code(table.dtype), _dtype_code(out.dtype)
-        if rows != self.vocab or n != ids.numel() or ids.device != table.device or out.device != table.device:
-            raise BaocError(E_INVALID, "lookup: table must be [vocab, dim], out one row per id, all on one device")
-        ids = self._ids(ids)
-        self._check(_on_device(table.device, _lib.baoc_embed, self._ref, table.data_ptr(), ids.data_ptr(), n, out.data_ptr()))
-        return out
+        if rows != self.vocab or n != ids.numel() or dev < 0 or ids.get_device() != dev or out.get_device() != dev:
+            raise BaocError(E_INVALID, "lookup: table must be [vocab, dim], out one row per id, all on one CUDA device")
+        try:
+            e.table_dtype, e.act_dtype, e.id_bits = DTYPES[table.dtype], DTYPES[out.dtype], _ID_BITS[ids.dtype]
+        except KeyError as x:
+            raise BaocError(E_INVALID, f"lookup: {x.args[0]} is not offered (bfloat16 and float32 arrays, int32 and int64 ids are)") from None
+        if not ids.is_contiguous():
+            ids = ids.contiguous()
+        rc = _queue(dev, _lib.baoc_embed, self._ref, table.data_ptr(), ids.data_ptr(), n, out.data_ptr())
+        return out if rc >= 0 else self._failed(rc)
 
     def grad_workspace_bytes(self, n_tokens: int) -> int:
-        self._check(_lib.baoc_embed_grad_workspace_bytes(self._ref, int(n_tokens), C.byref(self._n)))
-        return self._n.value
+        rc = _lib.baoc_embed_grad_workspace_bytes(self._ref, int(n_tokens), C.byref(self._n))
+        return self._n.value if rc >= 0 else self._failed(rc)
 
     def grad(self, ids: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, accumulate: bool = False,
              ws: Optional[torch.Tensor] = None) -> torch.Tensor:
         """dtable[v, :] = scale * sum of dout over the positions with id v (accumulate: added to dtable).  dout: ids' shape
         + [dim], dtable: [vocab, dim] (a block's flat gradient array viewed that way), bf16 or fp32 each; ws: device bytes,
         at least ``grad_workspace_bytes(ids.numel())`` (allocated when not given)."""
-        e = self._e
+        e, dev = self._e, dtable.get_device()
         n, e.act_stride = _rows(dout, self.dim, "dout")
         rows, e.grad_stride = _rows(dtable, self.dim, "dtable")
-        e.act_dtype, e.grad_dtype = _dtype_code(dout.dtype), _dtype_code(dtable.dtype)
-        if rows != self.vocab or n != ids.numel() or ids.device != dtable.device or dout.device != dtable.device:
-            raise BaocError(E_INVALID, "grad: dtable must be [vocab, dim], dout one row per id, all on one device")
-        ids = self._ids(ids)
+        if rows != self.vocab or n != ids.numel() or dev < 0 or ids.get_device() != dev or dout.get_device() != dev:
+            raise BaocError(E_INVALID, "grad: dtable must be [vocab, dim], dout one row per id, all on one CUDA device")
+        try:
+            e.act_dtype, e.grad_dtype, e.id_bits = DTYPES[dout.dtype], DTYPES[dtable.dtype], _ID_BITS[ids.dtype]
+        except KeyError as x:
+            raise BaocError(E_INVALID, f"grad: {x.args[0]} is not offered (bfloat16 and float32 arrays, int32 and int64 ids are)") from None
+        if not ids.is_contiguous():
+            ids = ids.contiguous()
         if ws is None:
             ws = torch.empty(self.grad_workspace_bytes(n), dtype=torch.uint8, device=dtable.device)
-        elif ws.device != dtable.device or not ws.is_contiguous():
+        elif ws.get_device() != dev or not ws.is_contiguous():
             raise BaocError(E_INVALID, "grad: ws must be a contiguous buffer on the device of the others")
-        self._check(_on_device(dtable.device, _lib.baoc_embed_grad, self._ref, ids.data_ptr(), dout.data_ptr(), n, dtable.data_ptr(),
-                               int(bool(accumulate)), ws.data_ptr(), ws.numel() * ws.element_size()))
-        return dtable
-
-
-def _on_device(device: torch.device, call, *args) -> int:
-    """call(*args, current stream of that device) with the device current."""
-    if device.index == torch.cuda.current_device():
-        return call(*args, torch.cuda.current_stream().cuda_stream)
-    with torch.cuda.device(device):
-        return call(*args, torch.cuda.current_stream().cuda_stream)
+        rc = _queue(dev, _lib.baoc_embed_grad, self._ref, ids.data_ptr(), dout.data_ptr(), n, dtable.data_ptr(), 1 if accumulate else 0,
+                    ws.data_ptr(), ws.numel() * ws.element_size())
+        return dtable if rc >= 0 else self._failed(rc)
 
 
 class Baoc:
@@ -489,15 +490,17 @@ class Baoc:
         return pointer_table(arrays), _dtype_code(arrays[0].dtype)
 
     def _norms(self, norms: torch.Tensor) -> int:
-        if norms.dtype != torch.float32 or norms.numel() != 1 + self.n_blocks or not norms.is_contiguous() or not norms.is_cuda:
+        """The device of a valid norms array."""
+        dev = norms.get_device()
+        if dev < 0 or norms.dtype != torch.float32 or norms.numel() != 1 + self.n_blocks or not norms.is_contiguous():
             raise BaocError(E_INVALID, "norms must be a contiguous float32 device tensor of 1 + n_blocks elements")
-        return norms.data_ptr()
+        return dev
 
     def grad_norm(self, grads, norms: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
         """``baoc_grad_norm``: norms[0] = the global gradient norm, norms[1 + i] block i's.  grads: list of bf16 or fp32
         device tensors, or a table from ``pointer_table`` with its dtype (bfloat16 when not given)."""
         tab, code = self._clip_arrays(grads, dtype, "grad_norm")
-        self._check(_lib.baoc_grad_norm(self._h, tab, code, self._norms(norms), _stream()))
+        self._check(_queue(self._norms(norms), _lib.baoc_grad_norm, self._h, tab, code, norms.data_ptr()))
         return norms
 
     def clip_grads(self, grads, out, max_norm: float, norms: torch.Tensor, src_dtype: Optional[torch.dtype] = None,
@@ -506,7 +509,7 @@ class Baoc:
         Arrays as for ``grad_norm``; bf16 -> bf16, fp32 -> fp32 or fp32 -> bf16.  Returns norms."""
         src, sc = self._clip_arrays(grads, src_dtype, "clip_grads")
         dst, dc = (src, sc) if out is None else self._clip_arrays(out, dst_dtype, "clip_grads")
-        self._check(_lib.baoc_clip_grads(self._h, src, sc, dst, dc, float(max_norm), self._norms(norms), _stream()))
+        self._check(_queue(self._norms(norms), _lib.baoc_clip_grads, self._h, src, sc, dst, dc, float(max_norm), norms.data_ptr()))
         return norms
 
     # ---- allocation -------------------------------------------------------

@@ -2,6 +2,7 @@
 //
 //   out[t, :]    = scale * table[ids[t], :]
 //   dtable[v, :] = scale * sum over t with ids[t] = v of dout[t, :]
+#include <atomic>
 #include <cmath>
 #include <cuda_runtime.h>
 #include <new>
@@ -631,6 +632,20 @@ void group_geometry(int64_t vocab, int* shift, int* bins) {
 int columns_per_warp(int dim) { return dim > 128 ? 256 : (dim > 64 ? 128 : 64); }
 int group_smem(int bins) { return 4 * (kGroupWarps * bins + bins + 1 + kGroupWarps * kListed); }
 
+// The grouping's shared memory is above the default limit; the permission is per device and lasts.
+template <typename Id>
+cudaError_t allow_group_smem() {
+    static std::atomic<uint64_t> done{0};               // one bit per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(embed_group_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, group_smem(kGroupBins));
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 struct EmbedLayout { size_t start, perm, segs, slots, tickets, partial, total; int shift, bins, slabs, n_segs, n_slots; };
 
 EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
@@ -755,7 +770,7 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     const int smem = group_smem(L.bins);
     auto group = [&](auto id) {
         using Id = decltype(id);
-        const cudaError_t ce = cudaFuncSetAttribute(embed_group_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, group_smem(kGroupBins));
+        const cudaError_t ce = allow_group_smem<Id>();
         if (ce != cudaSuccess) return fail_embed(BAOC_E_CUDA, std::string("embed_group_kernel: ") + cudaGetErrorString(ce));
         embed_group_kernel<Id><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const Id*>(ids), int(n_tokens), uint32_t(e->vocab),
                                                                              uint32_t(e->pad_id), b BAOC_CHECK_ARG(ck));
