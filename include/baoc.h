@@ -588,7 +588,7 @@ int baoc_embed_grad_workspace_bytes(const baoc_embed_t* e, int64_t n_tokens, siz
  * micro-batches).  Sums are fp32, in an order that depends on the ids only: equal
  * inputs give equal bits.  ws: device, 256-byte aligned, >= the size above; its
  * contents matter to no later call.  n_tokens <= 2^30.  dtable must overlap
- * neither dout nor ws.  Queues two kernels; does not wait.
+ * neither dout nor ws.  Queues one kernel (few tokens) or two; does not wait.
  * Errors of the three: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_WORKSPACE,
  * BAOC_E_CUDA; baoc_embed_last_error() returns the message of the calling
  * thread's last failure. */

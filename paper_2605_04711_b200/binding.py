@@ -280,10 +280,10 @@ def _dtype_code(dtype: torch.dtype) -> int:
 
 def _rows(t: torch.Tensor, dim: int, what: str):
     """(rows, elements from row to row) of a device tensor [..., dim] whose leading dimensions step evenly."""
-    if t.dim() < 1 or t.shape[-1] != dim:
+    if t.dim() < 1 or t.size(-1) != dim:
         raise BaocError(E_INVALID, f"{what} must be [..., {dim}], not {list(t.shape)}")
     if t.is_contiguous():
-        return t.numel() // dim, dim
+        return t.numel() // dim, 0                          # (0: the rows follow one another)
     m = t
     if t.dim() != 2:
         try:
@@ -292,7 +292,7 @@ def _rows(t: torch.Tensor, dim: int, what: str):
             m = None
     if m is None or (dim > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < dim):
         raise BaocError(E_INVALID, f"{what}: rows must be contiguous and step evenly without overlap")
-    return m.shape[0], (m.stride(0) if m.shape[0] > 1 else dim)
+    return m.shape[0], (m.stride(0) if m.shape[0] > 1 else 0)
 
 
 _ID_BITS = {torch.int32: 32, torch.int64: 64}
@@ -309,6 +309,7 @@ class Embedding:
         self._e = Embed(self.vocab, max(-1, min(self.dim, 2 ** 31 - 1)), DTYPES[torch.float32], DTYPES[torch.bfloat16],
                         DTYPES[torch.bfloat16], 64, float(scale), -1 if pad_id is None else int(pad_id), 0, 0, 0)
         self._ref = C.byref(self._e)
+        self._form = None
         self._n = C.c_size_t()
         self.grad_workspace_bytes(0)                        # the descriptor's checks
 
@@ -324,12 +325,16 @@ class Embedding:
         if out is None:
             out = torch.empty((*ids.shape, self.dim), dtype=out_dtype, device=table.device)
         e, dev = self._e, table.get_device()
-        rows, e.table_stride = _rows(table, self.dim, "table")
-        n, e.act_stride = _rows(out, self.dim, "out")
+        rows, table_stride = _rows(table, self.dim, "table")
+        n, act_stride = _rows(out, self.dim, "out")
         if rows != self.vocab or n != ids.numel() or dev < 0 or ids.get_device() != dev or out.get_device() != dev:
             raise BaocError(E_INVALID, "lookup: table must be [vocab, dim], out one row per id, all on one CUDA device")
+        form = (table.dtype, out.dtype, ids.dtype, table_stride, act_stride)
         try:
-            e.table_dtype, e.act_dtype, e.id_bits = DTYPES[table.dtype], DTYPES[out.dtype], _ID_BITS[ids.dtype]
+            if form != self._form:                          # (the descriptor holds the last call's)
+                e.table_dtype, e.act_dtype, e.id_bits, e.table_stride, e.act_stride = (
+                    DTYPES[table.dtype], DTYPES[out.dtype], _ID_BITS[ids.dtype], table_stride, act_stride)
+                self._form = form
         except KeyError as x:
             raise BaocError(E_INVALID, f"lookup: {x.args[0]} is not offered (bfloat16 and float32 arrays, int32 and int64 ids are)") from None
         if not ids.is_contiguous():
@@ -347,12 +352,16 @@ class Embedding:
         + [dim], dtable: [vocab, dim] (a block's flat gradient array viewed that way), bf16 or fp32 each; ws: device bytes,
         at least ``grad_workspace_bytes(ids.numel())`` (allocated when not given)."""
         e, dev = self._e, dtable.get_device()
-        n, e.act_stride = _rows(dout, self.dim, "dout")
-        rows, e.grad_stride = _rows(dtable, self.dim, "dtable")
+        n, act_stride = _rows(dout, self.dim, "dout")
+        rows, grad_stride = _rows(dtable, self.dim, "dtable")
         if rows != self.vocab or n != ids.numel() or dev < 0 or ids.get_device() != dev or dout.get_device() != dev:
             raise BaocError(E_INVALID, "grad: dtable must be [vocab, dim], dout one row per id, all on one CUDA device")
+        form = (dout.dtype, dtable.dtype, ids.dtype, act_stride, grad_stride, None)
         try:
-            e.act_dtype, e.grad_dtype, e.id_bits = DTYPES[dout.dtype], DTYPES[dtable.dtype], _ID_BITS[ids.dtype]
+            if form != self._form:
+                e.act_dtype, e.grad_dtype, e.id_bits, e.act_stride, e.grad_stride = (
+                    DTYPES[dout.dtype], DTYPES[dtable.dtype], _ID_BITS[ids.dtype], act_stride, grad_stride)
+                self._form = form
         except KeyError as x:
             raise BaocError(E_INVALID, f"grad: {x.args[0]} is not offered (bfloat16 and float32 arrays, int32 and int64 ids are)") from None
         if not ids.is_contiguous():

@@ -2,6 +2,7 @@
 //
 //   out[t, :]    = scale * table[ids[t], :]
 //   dtable[v, :] = scale * sum over t with ids[t] = v of dout[t, :]
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cuda_runtime.h>
@@ -24,6 +25,9 @@ constexpr int kJoin = 16;              // chunks whose partial sums one warp add
 constexpr int kSlotWarps = 16;         // warps that share a run of 32 slots
 constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
 constexpr int kSegment = 32;           // rows and tokens, together, of a segment of the sums; at most the warp's lanes
+constexpr int kFewTokens = kThreads;    // most tokens of the one-kernel gradient: one per thread,
+constexpr int64_t kFewBytes = 512 << 10;  // and most bytes of dout, all of which one CTA may have to add up
+constexpr int kFewCtas = 8 * 148;
 constexpr int kEmbedMaxDim = 1 << 24;
 constexpr int64_t kEmbedMaxStride = 1 << 28;           // (row products stay far inside 64 bits)
 
@@ -138,9 +142,13 @@ embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* _
     constexpr int kTokens = P::kWords == 8 ? 4 : 8;
     const int lane = threadIdx.x & 31;
     const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    const int slab = int(item % uint32_t(slabs));
-    const int64_t t0 = int64_t(item / uint32_t(slabs)) * kTokens;
-    if (t0 >= n) return;
+    // fp32 tables go through slab by slab: a frequent row's kilobyte is then found in L1 (131072 tokens x 2048 of a Zipf-like
+    // stream: 128 us, 140 token by token); rows of half that size go token by token (65536 x 2048 of bf16: 54 us, 58 slab by slab).
+    constexpr bool kBySlab = SRC == BAOC_F32 && VEC;
+    const uint32_t groups = uint32_t((n + kTokens - 1) / kTokens), per = kBySlab ? groups : uint32_t(slabs), q = item / per, r = item - q * per;
+    const int slab = int(kBySlab ? q : r);
+    const int64_t t0 = int64_t(kBySlab ? r : q) * kTokens;
+    if (slab >= slabs || t0 >= n) return;
     const int m = int(min64(n - t0, kTokens));
     const Id own = __ldg(ids + t0 + min(lane, m - 1));
     const uint32_t row = is_row(own, vocab) ? uint32_t(own) : 0u, named = __ballot_sync(0xffffffffu, is_row(own, vocab));
@@ -584,6 +592,79 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
     }
 }
 
+// ---- gradient of a few tokens: one kernel ---------------------------------------------------------------------------
+// CTA c has the rows c, c + gridDim, ..; its threads look at one id each, list those of its rows in the tokens' order, and
+// its warps take (row, slab) pairs in turn: a row's tokens are found in the list by a vote.
+template <int ACT, int GRAD, int V, bool VEC>
+__global__ void __launch_bounds__(kThreads)
+embed_grad_few_kernel(const void* __restrict__ ids, int id_bits, int n, const char* __restrict__ dout, char* dtable, uint32_t vocab, uint32_t pad,
+                      int slabs, int accumulate, const EmbedArgs a) {
+    using P = Part<ACT, V, VEC>;
+    constexpr int kBatch = P::kWords >= 8 ? 4 : 8;
+    __shared__ uint32_t list_row[kFewTokens];
+    __shared__ int32_t list_token[kFewTokens];
+    __shared__ int found[kThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t step = gridDim.x;
+    uint32_t k = 0;
+    bool in = false;
+    if (int(threadIdx.x) < n) {
+        const int64_t id = id_bits == 64 ? __ldg(static_cast<const int64_t*>(ids) + threadIdx.x) : int64_t(__ldg(static_cast<const int32_t*>(ids) + threadIdx.x));
+        if (is_row(id, vocab) && uint32_t(id) != pad) {
+            k = uint32_t(id) / step;
+            in = uint32_t(id) - k * step == blockIdx.x;
+        }
+    }
+    const uint32_t who = __ballot_sync(0xffffffffu, in);
+    if (lane == 0) found[warp] = __popc(who);
+    __syncthreads();
+    int before = 0, listed = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        before += w < warp ? found[w] : 0;
+        listed += found[w];
+    }
+    if (in) {
+        const int at = before + __popc(who & ((1u << lane) - 1u));
+        list_row[at] = k;
+        list_token[at] = int32_t(threadIdx.x);
+    }
+    __syncthreads();
+    const uint32_t rows = (vocab - blockIdx.x + step - 1) / step;
+    for (int64_t item = warp; item < int64_t(rows) * slabs; item += kThreads / 32) {
+        const uint32_t r = uint32_t(item / slabs);
+        const int slab = int(item - int64_t(r) * slabs);
+        const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
+        const char* src = dout + int64_t(rc) * P::kSize;
+        float acc[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.f;
+        bool named = false;
+        for (int l0 = 0; l0 < listed; l0 += 32) {
+            uint32_t hits = __ballot_sync(0xffffffffu, l0 + lane < listed && list_row[l0 + lane] == r);
+            named |= hits != 0u;
+            while (hits) {
+                const int m = min(__popc(hits), kBatch);
+                P x[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {      // (behind the m-th token it is read again, and not added)
+                    x[i].load(src + uint64_t(uint32_t(list_token[l0 + __ffs(hits) - 1])) * a.src_step, last);
+                    if (i + 1 < m) hits &= hits - 1u;
+                }
+                hits &= hits - 1u;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (i < m) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) acc[j] += x[i].at(j);
+                    }
+            }
+        }
+        if (named || !accumulate)
+            write_row<GRAD, V, VEC>(dtable + uint64_t(blockIdx.x + r * step) * a.dst_step + int64_t(col) * (GRAD == BAOC_BF16 ? 2 : 4), col, acc, accumulate, a);
+    }
+}
+
 namespace {
 
 thread_local std::string g_embed_err;
@@ -765,6 +846,18 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
                      L.shift, L.bins, L.slabs, L.n_segs, L.n_slots};
     const CheckCtx ck{w, w + L.total, 0, 0, 0};
     (void)ck;
+    const EmbedArgs a{uint32_t(as * ab), uint32_t(gs * gb), e->dim, e->scale};
+    const bool vec = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
+    if (n_tokens <= kFewTokens && n_tokens * e->dim * ab <= kFewBytes) {
+        const int64_t pairs = e->vocab * L.slabs;
+        const unsigned ctas = unsigned(std::min<int64_t>(std::min<int64_t>(e->vocab, kFewCtas), ceil_div(pairs, kThreads / 32)));
+        return with_types(e->act_dtype, e->grad_dtype, e->dim, vec, [&](auto A, auto G, auto V, auto VEC) {
+            embed_grad_few_kernel<A(), G(), V(), VEC()><<<ctas, kThreads, 0, s>>>(ids, e->id_bits, int(n_tokens), static_cast<const char*>(dout),
+                                                                                 static_cast<char*>(dtable), uint32_t(e->vocab), uint32_t(e->pad_id),
+                                                                                 L.slabs, accumulate, a);
+            return launched("embed_grad_few_kernel");
+        });
+    }
     const int64_t items = (int64_t(L.n_slots / 32) * kSlotWarps + L.n_segs) * L.slabs;
     if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: too many elements for one launch");
     const int smem = group_smem(L.bins);
@@ -778,8 +871,6 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     };
     rc = e->id_bits == 64 ? group(int64_t(0)) : group(int32_t(0));
     if (rc) return rc;
-    const EmbedArgs a{uint32_t(as * ab), uint32_t(gs * gb), e->dim, e->scale};
-    const bool vec = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
     const unsigned grid = unsigned(ceil_div(items, kThreads / 32));
     return with_types(e->act_dtype, e->grad_dtype, e->dim, vec, [&](auto A, auto G, auto V, auto VEC) {
         const cudaError_t ce = launch_behind(embed_grad_kernel<A(), G(), V(), VEC()>, grid, kThreads, s, static_cast<const char*>(dout),
