@@ -67,22 +67,38 @@ struct EmbedArgs {
     float scale;
 };
 
-// A warp works on 32 * V columns (a slab) of a row.  A lane has V neighbours where base, row stride and dim allow 16-byte
-// accesses (VEC), and V columns that are 32 apart otherwise.  V = 8 for dim > 128, 4 for dim > 64, else 2: a narrower table
-// leaves fewer lanes idle.
-template <int DT, int V, bool VEC>
+// A warp works on 32 * V columns (a slab) of a row.  How a lane's V columns lie depends on what base, row stride and dim of
+// both arrays allow: kWide, V neighbours (16-byte accesses); kPairs, V / 2 pairs that are 64 columns apart; kSingles, V columns
+// that are 32 apart.  V = 8 for dim > 128, 4 for dim > 64, else 2: a narrower table leaves fewer lanes idle.
+enum Access : int { kSingles = 0, kPairs = 1, kWide = 2 };
+template <int V, int M>
+__device__ __forceinline__ constexpr int column_of(int j) { return M == kWide ? j : (M == kPairs ? 64 * (j / 2) + j % 2 : 32 * j); }
+
+template <int DT, int V, int M>
 struct Part {
     static constexpr int kSize = DT == BAOC_BF16 ? 2 : 4;
-    static constexpr int kWords = VEC ? V * kSize / 4 : V;
+    static constexpr int kWords = M == kSingles ? V : V * kSize / 4;
     uint32_t w[kWords];
 
-    // p: the lane's first column; last: bytes from there to the last column that the row can be read at
+    // p: the lane's first column; last: bytes from there to the last column (pair) that the row can be read at
     __device__ __forceinline__ void load(const char* p, int last) {
-        if constexpr (VEC) {
+        if constexpr (M == kWide) {
             if constexpr (kWords == 1) w[0] = ld_row_u1(p);
             if constexpr (kWords == 2) { const uint2 a = ld_row_u2(p); w[0] = a.x; w[1] = a.y; }
             if constexpr (kWords >= 4) { const uint4 a = ld_row_u4(p); w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; }
             if constexpr (kWords == 8) { const uint4 a = ld_row_u4(p + 16); w[4] = a.x; w[5] = a.y; w[6] = a.z; w[7] = a.w; }
+        } else if constexpr (M == kPairs) {
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) {
+                const char* q = p + min(j * 64 * kSize, last);
+                if constexpr (DT == BAOC_BF16) {
+                    w[j] = ld_row_u1(q);
+                } else {
+                    const uint2 a = ld_row_u2(q);
+                    w[2 * j] = a.x;
+                    w[2 * j + 1] = a.y;
+                }
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -93,21 +109,25 @@ struct Part {
         }
     }
     __device__ __forceinline__ float at(int j) const {
-        if constexpr (VEC && DT == BAOC_BF16) return (j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]);
+        if constexpr (M != kSingles && DT == BAOC_BF16) return (j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]);
         else return __uint_as_float(w[j]);
     }
 };
 
-// The lane's first column, and what load() takes: columns beyond the row read its last ones instead.
-template <int V, bool VEC>
-__device__ __forceinline__ int lane_col(int slab, int lane) { return slab * 32 * V + lane * (VEC ? V : 1); }
-template <int V, bool VEC>
-__device__ __forceinline__ int read_col(int col, int dim) { return min(col, VEC ? dim - V : dim - 1); }
+// The lane's first column, and the one that it reads from: columns beyond the row read its last ones instead.
+template <int V, int M>
+__device__ __forceinline__ int lane_col(int slab, int lane) { return slab * 32 * V + lane * (M == kWide ? V : (M == kPairs ? 2 : 1)); }
+template <int V, int M>
+__device__ __forceinline__ constexpr int run_of() { return M == kWide ? V : (M == kPairs ? 2 : 1); }      // neighbours that are read together
+template <int V, int M>
+__device__ __forceinline__ int read_col(int col, int dim) { return min(col, dim - run_of<V, M>()); }
+template <int V, int M>
+__device__ __forceinline__ int last_read(int rc, int dim, int size) { return (dim - run_of<V, M>() - rc) * size; }
 
 // V values of a lane into a row (p: the lane's first column).
-template <int DT, int V, bool VEC>
+template <int DT, int V, int M>
 __device__ __forceinline__ void store_part(char* p, int col, int dim, const float (&y)[V]) {
-    if constexpr (VEC) {
+    if constexpr (M == kWide) {
         if (col >= dim) return;
         if constexpr (DT == BAOC_BF16) {
             if constexpr (V == 8) st_stream_u4(p, make_uint4(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])));
@@ -117,6 +137,14 @@ __device__ __forceinline__ void store_part(char* p, int col, int dim, const floa
             if constexpr (V >= 4) st_stream_f4(p, make_float4(y[0], y[1], y[2], y[3]));
             if constexpr (V == 8) st_stream_f4(p + 16, make_float4(y[4], y[5], y[6], y[7]));
             if constexpr (V == 2) *reinterpret_cast<float2*>(p) = make_float2(y[0], y[1]);
+        }
+    } else if constexpr (M == kPairs) {
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            if (col + 64 * j < dim) {
+                if constexpr (DT == BAOC_BF16) reinterpret_cast<uint32_t*>(p)[32 * j] = bf16_pair(y[2 * j], y[2 * j + 1]);
+                else reinterpret_cast<float2*>(p)[32 * j] = make_float2(y[2 * j], y[2 * j + 1]);
+            }
         }
     } else {
 #pragma unroll
@@ -134,17 +162,17 @@ __device__ __forceinline__ bool is_row(int32_t id, uint32_t vocab) { return uint
 __device__ __forceinline__ bool is_row(int64_t id, uint32_t vocab) { return uint32_t(uint64_t(id) >> 32) == 0u && uint32_t(id) < vocab; }
 
 // ---- lookup: one warp per slab of kTokens tokens, all of their loads in flight -----------------------------------------
-template <int SRC, int DST, int V, bool VEC, typename Id>
+template <int SRC, int DST, int V, int M, typename Id>
 __global__ void __launch_bounds__(kThreads)
 embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* __restrict__ out, uint32_t vocab, int64_t n, int slabs,
              const EmbedArgs a) {
-    using P = Part<SRC, V, VEC>;
+    using P = Part<SRC, V, M>;
     constexpr int kTokens = P::kWords == 8 ? 4 : 8;
     const int lane = threadIdx.x & 31;
     const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     // fp32 tables go through slab by slab: a frequent row's kilobyte is then found in L1 (131072 tokens x 2048 of a Zipf-like
     // stream: 128 us, 140 token by token); rows of half that size go token by token (65536 x 2048 of bf16: 54 us, 58 slab by slab).
-    constexpr bool kBySlab = SRC == BAOC_F32 && VEC;
+    constexpr bool kBySlab = SRC == BAOC_F32 && M == kWide;
     const uint32_t groups = uint32_t((n + kTokens - 1) / kTokens), per = kBySlab ? groups : uint32_t(slabs), q = item / per, r = item - q * per;
     const int slab = int(kBySlab ? q : r);
     const int64_t t0 = int64_t(kBySlab ? r : q) * kTokens;
@@ -152,7 +180,7 @@ embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* _
     const int m = int(min64(n - t0, kTokens));
     const Id own = __ldg(ids + t0 + min(lane, m - 1));
     const uint32_t row = is_row(own, vocab) ? uint32_t(own) : 0u, named = __ballot_sync(0xffffffffu, is_row(own, vocab));
-    const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
+    const int col = lane_col<V, M>(slab, lane), rc = read_col<V, M>(col, a.dim), last = last_read<V, M>(rc, a.dim, P::kSize);
     const char* src = table + int64_t(rc) * P::kSize;
     P x[kTokens];
 #pragma unroll
@@ -164,7 +192,7 @@ embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* _
         float y[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) y[j] = named >> i & 1u ? x[i].at(j) * a.scale : 0.f;
-        store_part<DST, V, VEC>(dst + int64_t(i) * a.dst_step, col, a.dim, y);
+        store_part<DST, V, M>(dst + int64_t(i) * a.dst_step, col, a.dim, y);
     }
 }
 
@@ -411,7 +439,7 @@ __device__ __forceinline__ void join_partials(const float* part, size_t step, in
 }
 
 // The finished sum of one row's slab: scaled, added to what is there or not, rounded once.
-template <int GRAD, int V, bool VEC>
+template <int GRAD, int V, int M>
 __device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V], int accumulate, const EmbedArgs& a) {
     float y[V];
 #pragma unroll
@@ -419,32 +447,32 @@ __device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V
     if (accumulate) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int k = VEC ? j : 32 * j;
+            const int k = column_of<V, M>(j);
             if (col + k < a.dim) {
                 if constexpr (GRAD == BAOC_BF16) y[j] += bf16_bits_to_float(reinterpret_cast<const uint16_t*>(p)[k]);
                 else y[j] += reinterpret_cast<const float*>(p)[k];
             }
         }
     }
-    store_part<GRAD, V, VEC>(p, col, a.dim, y);
+    store_part<GRAD, V, M>(p, col, a.dim, y);
 }
 
 // One warp works on one slab of
 //   - some of 32 slots of the chunk list: each chunk's tokens are summed into the slot's partial sum;
 //   - or one segment, neighbours of the grouped order: its unnamed rows are zeroed, the tokens of its short rows stream
 //     through, kBatch of them in flight whatever rows they belong to, and a row is written after its last token.
-template <int ACT, int GRAD, int V, bool VEC>
+template <int ACT, int GRAD, int V, int M>
 __global__ void __launch_bounds__(kThreads)
 embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b, uint32_t vocab, int n, int accumulate,
                   const EmbedArgs a BAOC_CHECK_PARAM) {
-    using P = Part<ACT, V, VEC>;
+    using P = Part<ACT, V, M>;
     constexpr int kBatch = P::kWords >= 8 ? 4 : (P::kWords == 4 ? 8 : 16);
     const int lane = threadIdx.x & 31;
     const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     wait_for_earlier_kernel();
     const int slab = int(item % uint32_t(b.slabs));
     int work = int(item / uint32_t(b.slabs));
-    const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
+    const int col = lane_col<V, M>(slab, lane), rc = read_col<V, M>(col, a.dim), last = last_read<V, M>(rc, a.dim, P::kSize);
     const char* src = dout + int64_t(rc) * P::kSize;
     char* dst = dtable + int64_t(col) * (GRAD == BAOC_BF16 ? 2 : 4);
     float acc[V];
@@ -511,7 +539,7 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
             }
             if (mine) {
                 const uint32_t cls = uint32_t(d.x) / uint32_t(b.bins), bin = uint32_t(d.x) - cls * uint32_t(b.bins);
-                write_row<GRAD, V, VEC>(dst + uint64_t((bin << b.shift) + cls) * a.dst_step, col, acc, accumulate, a);
+                write_row<GRAD, V, M>(dst + uint64_t((bin << b.shift) + cls) * a.dst_step, col, acc, accumulate, a);
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] = 0.f;
@@ -552,7 +580,7 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
         while (unnamed) {
             const int r = __ffs(unnamed) - 1;
             unnamed &= unnamed - 1u;
-            store_part<GRAD, V, VEC>(dst + uint64_t(__shfl_sync(0xffffffffu, row, r)) * a.dst_step, col, a.dim, zero);
+            store_part<GRAD, V, M>(dst + uint64_t(__shfl_sync(0xffffffffu, row, r)) * a.dst_step, col, a.dim, zero);
         }
     }
     // the runs of short rows between the long ones (which their chunks write)
@@ -578,7 +606,7 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
 #pragma unroll
                     for (int j = 0; j < V; ++j) acc[j] += x[i].at(j);
                     if (p + i + 1 == row_end) {
-                        write_row<GRAD, V, VEC>(dst + uint64_t(__shfl_sync(0xffffffffu, row, r)) * a.dst_step, col, acc, accumulate, a);
+                        write_row<GRAD, V, M>(dst + uint64_t(__shfl_sync(0xffffffffu, row, r)) * a.dst_step, col, acc, accumulate, a);
 #pragma unroll
                         for (int j = 0; j < V; ++j) acc[j] = 0.f;
                         r = __popc(__ballot_sync(0xffffffffu, lane < rows && st <= row_end)) - 1;
@@ -595,11 +623,11 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
 // ---- gradient of a few tokens: one kernel ---------------------------------------------------------------------------
 // CTA c has the rows c, c + gridDim, ..; its threads look at one id each, list those of its rows in the tokens' order, and
 // its warps take (row, slab) pairs in turn: a row's tokens are found in the list by a vote.
-template <int ACT, int GRAD, int V, bool VEC>
+template <int ACT, int GRAD, int V, int M>
 __global__ void __launch_bounds__(kThreads)
 embed_grad_few_kernel(const void* __restrict__ ids, int id_bits, int n, const char* __restrict__ dout, char* dtable, uint32_t vocab, uint32_t pad,
                       int slabs, int accumulate, const EmbedArgs a) {
-    using P = Part<ACT, V, VEC>;
+    using P = Part<ACT, V, M>;
     constexpr int kBatch = P::kWords >= 8 ? 4 : 8;
     __shared__ uint32_t list_row[kFewTokens];
     __shared__ int32_t list_token[kFewTokens];
@@ -634,7 +662,7 @@ embed_grad_few_kernel(const void* __restrict__ ids, int id_bits, int n, const ch
     for (int64_t item = warp; item < int64_t(rows) * slabs; item += kThreads / 32) {
         const uint32_t r = uint32_t(item / slabs);
         const int slab = int(item - int64_t(r) * slabs);
-        const int col = lane_col<V, VEC>(slab, lane), rc = read_col<V, VEC>(col, a.dim), last = (a.dim - 1 - rc) * P::kSize;
+        const int col = lane_col<V, M>(slab, lane), rc = read_col<V, M>(col, a.dim), last = last_read<V, M>(rc, a.dim, P::kSize);
         const char* src = dout + int64_t(rc) * P::kSize;
         float acc[V];
 #pragma unroll
@@ -661,7 +689,7 @@ embed_grad_few_kernel(const void* __restrict__ ids, int id_bits, int n, const ch
             }
         }
         if (named || !accumulate)
-            write_row<GRAD, V, VEC>(dtable + uint64_t(blockIdx.x + r * step) * a.dst_step + int64_t(col) * (GRAD == BAOC_BF16 ? 2 : 4), col, acc, accumulate, a);
+            write_row<GRAD, V, M>(dtable + uint64_t(blockIdx.x + r * step) * a.dst_step + int64_t(col) * (GRAD == BAOC_BF16 ? 2 : 4), col, acc, accumulate, a);
     }
 }
 
@@ -693,8 +721,11 @@ int check_embed(const baoc_embed_t* e, const char* what) {
 
 bool aligned(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & uintptr_t(bytes - 1)) == 0; }
 
-// Whether rows of this array can be read and written 16 bytes at a time.
-bool wide(const void* p, int64_t stride, int64_t eb, int dim) { return dim % 8 == 0 && aligned(p, 16) && (stride * eb) % 16 == 0; }
+// What rows of an array allow (eb: bytes of an element).
+int access_of(const void* p, int64_t stride, int64_t eb, int dim) {
+    if (dim % 8 == 0 && aligned(p, 16) && (stride * eb) % 16 == 0) return kWide;
+    return dim % 2 == 0 && aligned(p, 2 * eb) && stride % 2 == 0 ? kPairs : kSingles;
+}
 
 bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
     const char* x = static_cast<const char*>(a);
@@ -745,22 +776,27 @@ EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     return L;
 }
 
-// f(source type, destination type, V, VEC) for the types, the row length and the alignment of a call, as constants.
-template <int S, int D, typename F>
-int with_shape(int dim, bool vec, F f) {
+// f(source type, destination type, V, access) for the types, the row length and the alignment of a call, as constants.
+template <int S, int D, int V, typename F>
+int with_access(int access, F f) {
     using std::integral_constant;
     const integral_constant<int, S> s{};
     const integral_constant<int, D> d{};
-    const std::true_type y{};
-    const std::false_type n{};
-    if (dim > 128) return vec ? f(s, d, integral_constant<int, 8>{}, y) : f(s, d, integral_constant<int, 8>{}, n);
-    if (dim > 64) return vec ? f(s, d, integral_constant<int, 4>{}, y) : f(s, d, integral_constant<int, 4>{}, n);
-    return vec ? f(s, d, integral_constant<int, 2>{}, y) : f(s, d, integral_constant<int, 2>{}, n);
+    const integral_constant<int, V> v{};
+    if (access == kWide) return f(s, d, v, integral_constant<int, kWide>{});
+    if (access == kPairs) return f(s, d, v, integral_constant<int, kPairs>{});
+    return f(s, d, v, integral_constant<int, kSingles>{});
+}
+template <int S, int D, typename F>
+int with_shape(int dim, int access, F f) {
+    if (dim > 128) return with_access<S, D, 8>(access, f);
+    if (dim > 64) return with_access<S, D, 4>(access, f);
+    return with_access<S, D, 2>(access, f);
 }
 template <typename F>
-int with_types(int a, int b, int dim, bool vec, F f) {
-    if (a == BAOC_F32) return b == BAOC_F32 ? with_shape<BAOC_F32, BAOC_F32>(dim, vec, f) : with_shape<BAOC_F32, BAOC_BF16>(dim, vec, f);
-    return b == BAOC_F32 ? with_shape<BAOC_BF16, BAOC_F32>(dim, vec, f) : with_shape<BAOC_BF16, BAOC_BF16>(dim, vec, f);
+int with_types(int a, int b, int dim, int access, F f) {
+    if (a == BAOC_F32) return b == BAOC_F32 ? with_shape<BAOC_F32, BAOC_F32>(dim, access, f) : with_shape<BAOC_F32, BAOC_BF16>(dim, access, f);
+    return b == BAOC_F32 ? with_shape<BAOC_BF16, BAOC_F32>(dim, access, f) : with_shape<BAOC_BF16, BAOC_BF16>(dim, access, f);
 }
 
 int launched(const char* kernel) {
@@ -795,18 +831,18 @@ int baoc_embed(const baoc_embed_t* e, const void* table, const void* ids, int64_
         return fail_embed(BAOC_E_INVALID, "baoc_embed: out overlaps the table");
     const EmbedArgs a{uint32_t(ts * tb), uint32_t(os * ob), e->dim, e->scale};
     const int slabs = int(ceil_div(e->dim, columns_per_warp(e->dim)));
-    const bool vec = wide(table, ts, tb, e->dim) && wide(out, os, ob, e->dim);
+    const int access = std::min(access_of(table, ts, tb, e->dim), access_of(out, os, ob, e->dim));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return with_types(e->table_dtype, e->act_dtype, e->dim, vec, [&](auto S, auto D, auto V, auto VEC) {
-        constexpr int kTokens = Part<S(), V(), VEC()>::kWords == 8 ? 4 : 8;
+    return with_types(e->table_dtype, e->act_dtype, e->dim, access, [&](auto S, auto D, auto V, auto M) {
+        constexpr int kTokens = Part<S(), V(), M()>::kWords == 8 ? 4 : 8;
         const int64_t items = ceil_div(n_tokens, kTokens) * slabs, blocks = ceil_div(items, kThreads / 32);
         if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed: too many elements for one launch");
         const char* tab = static_cast<const char*>(table);
         char* o = static_cast<char*>(out);
         if (e->id_bits == 64)
-            embed_kernel<S(), D(), V(), VEC(), int64_t><<<unsigned(blocks), kThreads, 0, s>>>(tab, static_cast<const int64_t*>(ids), o, uint32_t(e->vocab), n_tokens, slabs, a);
+            embed_kernel<S(), D(), V(), M(), int64_t><<<unsigned(blocks), kThreads, 0, s>>>(tab, static_cast<const int64_t*>(ids), o, uint32_t(e->vocab), n_tokens, slabs, a);
         else
-            embed_kernel<S(), D(), V(), VEC(), int32_t><<<unsigned(blocks), kThreads, 0, s>>>(tab, static_cast<const int32_t*>(ids), o, uint32_t(e->vocab), n_tokens, slabs, a);
+            embed_kernel<S(), D(), V(), M(), int32_t><<<unsigned(blocks), kThreads, 0, s>>>(tab, static_cast<const int32_t*>(ids), o, uint32_t(e->vocab), n_tokens, slabs, a);
         return launched("embed_kernel");
     });
 } catch (const std::bad_alloc&) {
@@ -847,12 +883,12 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     const CheckCtx ck{w, w + L.total, 0, 0, 0};
     (void)ck;
     const EmbedArgs a{uint32_t(as * ab), uint32_t(gs * gb), e->dim, e->scale};
-    const bool vec = wide(dout, as, ab, e->dim) && wide(dtable, gs, gb, e->dim);
+    const int access = std::min(access_of(dout, as, ab, e->dim), access_of(dtable, gs, gb, e->dim));
     if (n_tokens <= kFewTokens && n_tokens * e->dim * ab <= kFewBytes) {
         const int64_t pairs = e->vocab * L.slabs;
         const unsigned ctas = unsigned(std::min<int64_t>(std::min<int64_t>(e->vocab, kFewCtas), ceil_div(pairs, kThreads / 32)));
-        return with_types(e->act_dtype, e->grad_dtype, e->dim, vec, [&](auto A, auto G, auto V, auto VEC) {
-            embed_grad_few_kernel<A(), G(), V(), VEC()><<<ctas, kThreads, 0, s>>>(ids, e->id_bits, int(n_tokens), static_cast<const char*>(dout),
+        return with_types(e->act_dtype, e->grad_dtype, e->dim, access, [&](auto A, auto G, auto V, auto M) {
+            embed_grad_few_kernel<A(), G(), V(), M()><<<ctas, kThreads, 0, s>>>(ids, e->id_bits, int(n_tokens), static_cast<const char*>(dout),
                                                                                  static_cast<char*>(dtable), uint32_t(e->vocab), uint32_t(e->pad_id),
                                                                                  L.slabs, accumulate, a);
             return launched("embed_grad_few_kernel");
@@ -872,8 +908,8 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     rc = e->id_bits == 64 ? group(int64_t(0)) : group(int32_t(0));
     if (rc) return rc;
     const unsigned grid = unsigned(ceil_div(items, kThreads / 32));
-    return with_types(e->act_dtype, e->grad_dtype, e->dim, vec, [&](auto A, auto G, auto V, auto VEC) {
-        const cudaError_t ce = launch_behind(embed_grad_kernel<A(), G(), V(), VEC()>, grid, kThreads, s, static_cast<const char*>(dout),
+    return with_types(e->act_dtype, e->grad_dtype, e->dim, access, [&](auto A, auto G, auto V, auto M) {
+        const cudaError_t ce = launch_behind(embed_grad_kernel<A(), G(), V(), M()>, grid, kThreads, s, static_cast<const char*>(dout),
                                              static_cast<char*>(dtable), b, uint32_t(e->vocab), int(n_tokens), accumulate, a BAOC_CHECK_ARG(ck));
         return ce == cudaSuccess ? BAOC_OK : fail_embed(BAOC_E_CUDA, std::string("embed_grad_kernel: ") + cudaGetErrorString(ce));
     });

@@ -83,7 +83,7 @@ def _within(got, want, tol):
 
 # ---- lookup -------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("n,vocab,dim", [(1, 1, 1), (1, 300, 2048), (2, 7, 3), (5, 100, 8), (33, 1000, 257), (64, 130, 64), (257, 4099, 513),
-                                         (1000, 129, 136), (7, 3, 4100), (4096, 512, 100)])
+                                         (1000, 129, 136), (7, 3, 4100), (4096, 512, 100), (50, 60, 66), (50, 60, 362), (50, 60, 2)])
 @pytest.mark.parametrize("tdt,odt,idt,scale", [(F, BF, torch.int64, 45.25), (F, F, torch.int32, 1.0), (BF, BF, torch.int32, -0.3),
                                                (BF, F, torch.int64, 1.0)])
 def test_lookup(B, n, vocab, dim, tdt, odt, idt, scale):
@@ -111,7 +111,7 @@ def test_lookup_shapes_strides_and_offsets(B):
     out = e.lookup(dt, _dev(ids)[:, :-1])
     assert torch.equal(out.cpu().view(-1, 40), _want_lookup(table, ids[:, :-1].reshape(-1), 1.0).to(BF))
     # rows inside wider buffers: the wide path with strides, and odd offsets that only elements are aligned to
-    for left, width in ((8, 64), (1, 47), (3, 48)):
+    for left, width in ((8, 64), (1, 47), (3, 48), (2, 46), (4, 47)):
         wt = torch.zeros((50, width))
         wt[:, left:left + 40] = table
         wo = torch.full((24, width), 7.0, dtype=BF, device="cuda:0")
@@ -149,7 +149,8 @@ def test_lookup_offsets_beyond_32_bits(B):
 GRAD_SHAPES = [(1, 1, 1, "uniform"), (1, 300, 2048, "uniform"), (3, 5, 2, "uniform"), (64, 130, 64, "skewed"), (200, 7, 257, "uniform"),
                (333, 1000, 100, "skewed"), (1000, 129, 136, "same"), (31, 128, 8, "same"), (32, 127, 16, "same"), (33, 50, 24, "same"),
                (2049, 300, 40, "skewed"), (5000, 3, 33, "uniform"), (4099, 513, 520, "skewed"), (70000, 40, 16, "skewed"),
-               (40000, 17, 300, "same")]
+               (40000, 17, 300, "same"), (256, 50, 40, "same"), (257, 50, 40, "same"), (200, 30, 1500, "skewed"), (256, 5, 511, "uniform"),
+               (300, 90, 362, "skewed"), (5000, 100, 98, "skewed"), (900, 33, 50, "skewed"), (900, 33, 130, "skewed")]
 
 
 @pytest.mark.parametrize("n,vocab,dim,kind", GRAD_SHAPES)
@@ -238,7 +239,7 @@ def test_grad_strides_and_offsets(B):
     ids, dout = _ids(n, vocab, 15, "skewed"), _rand((n, dim), BF, 16)
     want, mag, count = _want_grad(dout, ids, vocab, 1.0, None)
     tol = (count[:, None] + 2) * U * mag
-    for left, width in ((8, 64), (1, 47), (3, 48)):
+    for left, width in ((8, 64), (1, 47), (3, 48), (2, 46), (4, 47)):
         wd = torch.full((n, width), float("nan"), dtype=BF)
         wd[:, left:left + dim] = dout
         wt = torch.full((vocab, width), 7.0, dtype=BF, device="cuda:0")
