@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <new>
 #include <string>
@@ -14,9 +15,12 @@
 namespace baoc {
 
 constexpr int kGroupCtas = 128;        // id classes (one CTA each) of the grouping; doubled while a class has over kGroupBins ids
-constexpr int kGroupBins = 1024;       // most ids of a class: one thread of the CTA per id
+constexpr int kGroupBins = 768;        // most ids of a class: one thread of the CTA per id, and what shared memory holds
 constexpr int kGroupWarps = 32;
+constexpr int kGroupSplit = 4;         // CTAs that share the reading of the ids,
+constexpr int64_t kSplitTokens = 32768; // from this many tokens on
 constexpr int kIdLoads = 16;           // ids a lane of the grouping has in flight
+constexpr int kSeen = 256;             // the same for what a warp finds of a cluster's classes together
 constexpr int kListed = 512;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
 constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
@@ -233,71 +237,139 @@ __device__ __forceinline__ int last_not_above(const int32_t* a, int n, int32_t x
     return lo;
 }
 
-template <typename Id>
+// kSplit > 1: the CTAs of a cluster, kSplit neighbouring classes, read one part of the ids each for all of them and
+// exchange what they have found through distributed shared memory.
+template <typename Id, int kSplit>
 __global__ void __launch_bounds__(kGroupWarps * 32)
 embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t pad, const GradBufs b BAOC_CHECK_PARAM) {
+    constexpr int kOffBits = kSplit > 1 ? kListBits - 3 : kListBits;      // a list entry: {id of the class, part or class, offset of the token}
+    constexpr uint32_t kOffMask = (1u << kOffBits) - 1u;
+    static_assert(kSplit <= 8, "three bits of a list entry");
     extern __shared__ int32_t smem[];
     let_later_kernel_start();
     int32_t* hist = smem;                                                        // [warps][bins]
     int32_t* begin = hist + kGroupWarps * b.bins;                                // [bins + 1]: start of the class's rows
-    uint32_t* list = reinterpret_cast<uint32_t*>(begin + b.bins + 1);            // [warps][kListed]: {id of the class, token}
-    __shared__ int32_t s_warp[kGroupWarps];
-    __shared__ int32_t s_less;
+    uint32_t* list = reinterpret_cast<uint32_t*>(begin + b.bins + 1);            // [warps][kListed] of the class; kSplit > 1: [warps][kSeen] of all
+    __shared__ int32_t s_warp[kGroupWarps], s_found[kGroupWarps];
+    __shared__ int32_t s_less, s_below;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = b.bins, shift = b.shift;
     const uint32_t cls = blockIdx.x, mask = (1u << shift) - 1u, below = (1u << lane) - 1u;
+    const uint32_t rank = kSplit > 1 ? cls % kSplit : 0u, cls0 = cls - rank;
     const int64_t row0 = int64_t(cls) * bins;
 #ifdef BAOC_CHECKED
-    if (!check_range(ck, kKerEmbedGroup, b.start + row0, 4ll * (bins + 1), 0) || !check_range(ck, kKerEmbedGroup, b.perm, 4ll * n, 1) ||
+    // (the same ranges in every CTA: if one leaves, all of a cluster do)
+    if (!check_range(ck, kKerEmbedGroup, b.start, 4 * ((int64_t(bins) << shift) + 1), 0) || !check_range(ck, kKerEmbedGroup, b.perm, 4ll * n, 1) ||
         !check_range(ck, kKerEmbedGroup, b.slots, 8ll * b.n_slots, 2) || !check_range(ck, kKerEmbedGroup, b.segs, 8ll * (b.n_segs + 1), 3) ||
         !check_range(ck, kKerEmbedGroup, b.tickets, 8ll * b.n_slots * b.slabs, 4))
         return;
 #endif
-    // a warp takes one stretch of the tokens, at least one round of kIdLoads ids per lane; what it finds it counts and lists
-    const int warps = max(1, min(kGroupWarps, (n + 32 * kIdLoads - 1) / (32 * kIdLoads)));
-    const int seg = (n + warps * 32 - 1) / (warps * 32) * 32;
-    const int t0 = min(n, warp * seg), t1 = warp < warps ? min(n, t0 + seg) : t0;
+    // part r of the tokens begins at r * part; of each, warp w has the stretch that begins w * seg further on
+    const int part = (n + kSplit * 32 - 1) / (kSplit * 32) * 32;
+    const int warps = max(1, min(kGroupWarps, (part + 32 * kIdLoads - 1) / (32 * kIdLoads)));
+    const int seg = (part + warps * 32 - 1) / (warps * 32) * 32;
+    auto stretch = [&](int r, int& t0, int& t1) {
+        const int end = int(min64(int64_t(r + 1) * part, n));
+        t0 = int(min64(int64_t(r) * part + int64_t(warp) * seg, end));
+        t1 = warp < warps ? min(t0 + seg, end) : t0;
+    };
     for (int i = threadIdx.x; i < warps * bins; i += blockDim.x) hist[i] = 0;
-    if (threadIdx.x == 0) s_less = 0;
+    if (threadIdx.x == 0) { s_less = 0; s_below = 0; }
     __syncthreads();
     int32_t* mine = hist + warp * bins;
     uint32_t* found = list + warp * kListed;
-    int less = 0, n_found = 0;
-    for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
-        Id id[kIdLoads];
-        if (tb + 32 * kIdLoads <= t1) {
+    // A warp's pass over a stretch, kIdLoads ids per lane at a time: take(class, id of the class, token, place) for every id
+    // with want(class), where place numbers them from `from` on.  Returns the number behind the last one.
+    auto pass = [&](int t0, int t1, int from, auto want, auto take) {
+        for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
+            Id id[kIdLoads];
+            if (tb + 32 * kIdLoads <= t1) {
 #pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) id[u] = __ldg(ids + tb + lane + 32 * u);
+                for (int u = 0; u < kIdLoads; ++u) id[u] = __ldg(ids + tb + lane + 32 * u);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kIdLoads; ++u) id[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
+            }
+            uint32_t hits = 0;
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u) {
+                if (is_row(id[u], vocab) && uint32_t(id[u]) != pad && want(uint32_t(id[u]) & mask)) hits |= 1u << u;
+            }
+            if (!__any_sync(0xffffffffu, hits != 0u)) continue;
+            const int k = __popc(hits);
+            int upto = k;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            int at = from + upto - k;
+#pragma unroll
+            for (int u = 0; u < kIdLoads; ++u)
+                if (hits >> u & 1u) take(uint32_t(id[u]) & mask, uint32_t(id[u]) >> shift, tb + 32 * u + lane, at++);
+            from += __shfl_sync(0xffffffffu, upto, 31);
+        }
+        return from;
+    };
+    int less = 0, n_found = 0, t0, t1;
+    if constexpr (kSplit == 1) {
+        stretch(0, t0, t1);
+        n_found = pass(t0, t1, 0, [&](uint32_t c) { less += c < cls; return c == cls; },
+                       [&](uint32_t, uint32_t bin, int t, int at) {
+                           if (at < kListed) found[at] = bin << kListBits | uint32_t(t - t0);
+                           atomicAdd(&mine[bin], 1);
+                       });
+    } else {
+        namespace cg = cooperative_groups;
+        cg::cluster_group cluster = cg::this_cluster();
+        uint32_t* all = list + kGroupWarps * kListed + warp * kSeen;
+        stretch(int(rank), t0, t1);
+        const int seen = pass(t0, t1, 0, [&](uint32_t c) { less += c < cls0; return c - cls0 < uint32_t(kSplit); },
+                              [&](uint32_t c, uint32_t bin, int t, int at) {
+                                  if (at < kSeen) all[at] = bin << kListBits | (c - cls0) << kOffBits | uint32_t(t - t0);
+                              });
+        if (lane == 0) s_found[warp] = seg <= 1 << kOffBits ? seen : kSeen + 1;
+        less = __reduce_add_sync(0xffffffffu, less);
+        if (lane == 0 && less) atomicAdd(&s_below, less);
+        less = 0;
+        cluster.sync();
+        // what all CTAs of the cluster have listed for this class; tokens of the cluster's lower classes count as less
+        const int theirs = lane < kSplit ? *cluster.map_shared_rank(s_found + warp, lane) : 0;
+        if (warp == 0 && lane < kSplit) less = *cluster.map_shared_rank(&s_below, lane);
+        if (!__any_sync(0xffffffffu, theirs > kSeen)) {
+            const int most = __reduce_max_sync(0xffffffffu, theirs);
+            for (int i = 0; i < most; i += 32) {
+                uint32_t x[kSplit];
+#pragma unroll
+                for (int r = 0; r < kSplit; ++r) {
+                    const bool in = i + lane < __shfl_sync(0xffffffffu, theirs, r);
+                    x[r] = in ? cluster.map_shared_rank(all, r)[i + lane] : 0xffffffffu;
+                }
+#pragma unroll
+                for (int r = 0; r < kSplit; ++r) {
+                    const bool in = i + lane < __shfl_sync(0xffffffffu, theirs, r);
+                    const uint32_t d = x[r] >> kOffBits & 7u;
+                    less += in && d < rank;
+                    const bool hit = in && d == rank;
+                    const uint32_t who = __ballot_sync(0xffffffffu, hit);
+                    const int at = n_found + __popc(who & below);
+                    if (hit) {
+                        if (at < kListed) found[at] = (x[r] & ~(7u << kOffBits)) | uint32_t(r) << kOffBits;
+                        atomicAdd(&mine[x[r] >> kListBits], 1);
+                    }
+                    n_found += __popc(who);
+                }
+            }
         } else {
-#pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) id[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
-        }
-        uint32_t hits = 0;                              // which of the lane's ids are of the class
-#pragma unroll
-        for (int u = 0; u < kIdLoads; ++u) {
-            const uint32_t c = uint32_t(id[u]) & mask;
-            if (is_row(id[u], vocab) && uint32_t(id[u]) != pad) {
-                if (c < cls) ++less;
-                if (c == cls) hits |= 1u << u;
+            for (int r = 0; r < kSplit; ++r) {
+                stretch(r, t0, t1);
+                n_found = pass(t0, t1, n_found, [&](uint32_t c) { less += c >= cls0 && c < cls; return c == cls; },
+                               [&](uint32_t, uint32_t bin, int t, int at) {
+                                   if (at < kListed) found[at] = bin << kListBits | uint32_t(r) << kOffBits | (uint32_t(t - t0) & kOffMask);
+                                   atomicAdd(&mine[bin], 1);
+                               });
             }
         }
-        if (!__any_sync(0xffffffffu, hits != 0u)) continue;
-        const int k = __popc(hits);
-        int upto = k;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
-        }
-        int at = n_found + upto - k;
-#pragma unroll
-        for (int u = 0; u < kIdLoads; ++u) {
-            if (hits >> u & 1u) {
-                if (at < kListed) found[at] = (uint32_t(id[u]) >> shift) << kListBits | uint32_t(tb + 32 * u + lane - t0);
-                ++at;
-                atomicAdd(&mine[uint32_t(id[u]) >> shift], 1);
-            }
-        }
-        n_found += __shfl_sync(0xffffffffu, upto, 31);
+        cluster.sync();                                 // (nobody's lists are needed any more)
     }
     less = __reduce_add_sync(0xffffffffu, less);
     if (lane == 0 && less) atomicAdd(&s_less, less);
@@ -371,20 +443,25 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
         }
         __syncwarp();
     };
-    if (n_found <= kListed && seg <= 1 << kListBits) {
+    if (n_found <= kListed && seg <= 1 << kOffBits) {
+        __syncwarp();
         for (int i = 0; i < n_found; i += 32) {
             const bool in = i + lane < n_found;
             const uint32_t x = in ? found[i + lane] : 0u;
-            place(in, x >> kListBits, t0 + int(x & ((1u << kListBits) - 1u)));
+            const int r = kSplit > 1 ? int(x >> kOffBits & 7u) : 0;
+            place(in, x >> kListBits, r * part + warp * seg + int(x & kOffMask));
         }
     } else {
-        for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
-            Id id[kIdLoads];
+        for (int r = 0; r < kSplit; ++r) {
+            stretch(r, t0, t1);
+            for (int tb = t0; tb < t1; tb += 32 * kIdLoads) {
+                Id id[kIdLoads];
 #pragma unroll
-            for (int u = 0; u < kIdLoads; ++u) id[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
+                for (int u = 0; u < kIdLoads; ++u) id[u] = tb + lane + 32 * u < t1 ? __ldg(ids + tb + lane + 32 * u) : Id(-1);
 #pragma unroll
-            for (int u = 0; u < kIdLoads; ++u)
-                place(is_row(id[u], vocab) && uint32_t(id[u]) != pad && (uint32_t(id[u]) & mask) == cls, uint32_t(id[u]) >> shift, tb + 32 * u + lane);
+                for (int u = 0; u < kIdLoads; ++u)
+                    place(is_row(id[u], vocab) && uint32_t(id[u]) != pad && (uint32_t(id[u]) & mask) == cls, uint32_t(id[u]) >> shift, tb + 32 * u + lane);
+            }
         }
     }
 }
@@ -462,7 +539,7 @@ __device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V
 //   - or one segment, neighbours of the grouped order: its unnamed rows are zeroed, the tokens of its short rows stream
 //     through, kBatch of them in flight whatever rows they belong to, and a row is written after its last token.
 template <int ACT, int GRAD, int V, int M>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, M == kWide && ACT == BAOC_BF16 && V == 8 ? 4 : 3)
 embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b, uint32_t vocab, int n, int accumulate,
                   const EmbedArgs a BAOC_CHECK_PARAM) {
     using P = Part<ACT, V, M>;
@@ -742,10 +819,10 @@ void group_geometry(int64_t vocab, int* shift, int* bins) {
 }
 
 int columns_per_warp(int dim) { return dim > 128 ? 256 : (dim > 64 ? 128 : 64); }
-int group_smem(int bins) { return 4 * (kGroupWarps * bins + bins + 1 + kGroupWarps * kListed); }
+int group_smem(int bins, int split) { return 4 * (kGroupWarps * bins + bins + 1 + kGroupWarps * (kListed + (split > 1 ? kSeen : 0))); }
 
 // The grouping's shared memory is above the default limit; the permission is per device and lasts.
-template <typename Id>
+template <typename Id, int kSplit>
 cudaError_t allow_group_smem() {
     static std::atomic<uint64_t> done{0};               // one bit per device
     int dev = 0;
@@ -753,7 +830,7 @@ cudaError_t allow_group_smem() {
     if (e != cudaSuccess) return e;
     const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
     if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
-    e = cudaFuncSetAttribute(embed_group_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, group_smem(kGroupBins));
+    e = cudaFuncSetAttribute(embed_group_kernel<Id, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, group_smem(kGroupBins, kSplit));
     if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
     return e;
 }
@@ -896,16 +973,26 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     }
     const int64_t items = (int64_t(L.n_slots / 32) * kSlotWarps + L.n_segs) * L.slabs;
     if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed_grad: too many elements for one launch");
-    const int smem = group_smem(L.bins);
-    auto group = [&](auto id) {
+    auto group = [&](auto id, auto split) {
         using Id = decltype(id);
-        const cudaError_t ce = allow_group_smem<Id>();
-        if (ce != cudaSuccess) return fail_embed(BAOC_E_CUDA, std::string("embed_group_kernel: ") + cudaGetErrorString(ce));
-        embed_group_kernel<Id><<<1u << L.shift, kGroupWarps * 32, smem, s>>>(static_cast<const Id*>(ids), int(n_tokens), uint32_t(e->vocab),
-                                                                             uint32_t(e->pad_id), b BAOC_CHECK_ARG(ck));
-        return launched("embed_group_kernel");
+        constexpr int kSplit = decltype(split)::value;
+        cudaError_t ce = allow_group_smem<Id, kSplit>();
+        if (ce == cudaSuccess) {
+            cudaLaunchAttribute at{};
+            at.id = cudaLaunchAttributeClusterDimension;
+            at.val.clusterDim.x = kSplit; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+            cudaLaunchConfig_t cfg{};
+            cfg.gridDim = dim3(1u << L.shift); cfg.blockDim = dim3(kGroupWarps * 32); cfg.dynamicSmemBytes = size_t(group_smem(L.bins, kSplit)); cfg.stream = s;
+            cfg.attrs = &at; cfg.numAttrs = kSplit > 1 ? 1 : 0;
+            ce = cudaLaunchKernelEx(&cfg, embed_group_kernel<Id, kSplit>, static_cast<const Id*>(ids), int(n_tokens), uint32_t(e->vocab),
+                                    uint32_t(e->pad_id), b BAOC_CHECK_ARG(ck));
+        }
+        return ce == cudaSuccess ? BAOC_OK : fail_embed(BAOC_E_CUDA, std::string("embed_group_kernel: ") + cudaGetErrorString(ce));
     };
-    rc = e->id_bits == 64 ? group(int64_t(0)) : group(int32_t(0));
+    const std::integral_constant<int, 1> alone{};
+    const std::integral_constant<int, kGroupSplit> shared{};
+    if (n_tokens < kSplitTokens) rc = e->id_bits == 64 ? group(int64_t(0), alone) : group(int32_t(0), alone);
+    else rc = e->id_bits == 64 ? group(int64_t(0), shared) : group(int32_t(0), shared);
     if (rc) return rc;
     const unsigned grid = unsigned(ceil_div(items, kThreads / 32));
     return with_types(e->act_dtype, e->grad_dtype, e->dim, access, [&](auto A, auto G, auto V, auto M) {

@@ -190,10 +190,11 @@ def test_grad(B, G, n, vocab, dim, kind, adt, gdt, idt, scale):
     assert G.guards_intact(guard_t) and G.guards_intact(guard_w)
 
 
-@pytest.mark.parametrize("vocab", [1, 127, 128, 129, 131071, 131073, 262145, 600000])
-def test_grad_vocabularies(B, vocab):
-    """Vocabularies around the sizes where the grouping changes its geometry."""
-    n, dim = 3000, 4
+@pytest.mark.parametrize("n", [3000, 32767, 32768, 70003])
+@pytest.mark.parametrize("vocab", [1, 127, 128, 129, 98304, 98305, 131071, 262145, 600000])
+def test_grad_vocabularies(B, vocab, n):
+    """Vocabularies and token counts around the sizes where the grouping changes its geometry."""
+    dim = 4
     ids = _ids(n, vocab, 10, "uniform")
     ids[:50] = vocab - 1
     dout = _rand((n, dim), F, 11)
