@@ -187,13 +187,9 @@ grad_norm_kernel(const ClipBufs c, double max_norm, float* __restrict__ norms BA
     }
     let_later_kernel_start();
     __shared__ bool last;
-    if (threadIdx.x == 0) {
-        __threadfence();
-        last = atomicAdd(c.ticket, 1u) == uint32_t(c.n_ctas - 1);
-    }
+    if (threadIdx.x == 0) last = take_ticket(c.ticket) == uint32_t(c.n_ctas - 1);      // (thread 0 has written the CTA's partial sums)
     __syncthreads();
     if (!last) return;
-    __threadfence();
     finish_norm(c, max_norm, norms);
 }
 

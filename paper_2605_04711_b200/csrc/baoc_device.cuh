@@ -86,6 +86,14 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int kPending>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
 
+// Adds one to a ticket and returns what it was.  Writes that this thread (or others, before a barrier with it) made are
+// visible to whoever takes a later ticket and to the threads behind a barrier with that one.
+__device__ __forceinline__ uint32_t take_ticket(uint32_t* ticket) {
+    uint32_t before;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(ticket) : "memory");
+    return before;
+}
+
 // ---- two kernels in a row -------------------------------------------------------
 // The second kernel of a pair is launched with launch_behind: its CTAs may take their places while the first one still
 // runs, and wait (in hardware) until it has ended and its writes are visible.

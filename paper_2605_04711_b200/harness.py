@@ -145,6 +145,7 @@ class Session:
         self.h.bind_stats_workspace(self.ws)
         self.state = None
         self.assign = None
+        self.clip_norms = None
         self._fixed_cache = {}
 
     def verify_guards(self) -> bool:
@@ -204,6 +205,13 @@ class Session:
         new_state = self._alloc(self.h.state_bytes(self.assign))
         self.h.reconfigure(self.assign, new_state, steps_done, inherit)
         self.state = new_state
+
+    def clip_grads(self, k: int, max_norm: float) -> torch.Tensor:
+        """Clip gradient set k in place by its global norm; returns the norms before it (the global one, then every block's)."""
+        if self.clip_norms is None:
+            self.h.bind_clip_workspace(self._alloc(self.h.clip_workspace_bytes()))
+            self.clip_norms = self._alloc(4 * (1 + len(self.wl.blocks)), True).view(torch.float32)
+        return self.h.clip_grads(self.grad_tables[k], None, max_norm, self.clip_norms)
 
     def step(self, k: int, t: int):
         self.h.step(self.grad_tables[k], self.param_table, t)

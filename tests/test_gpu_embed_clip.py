@@ -498,6 +498,20 @@ def test_binding_refuses_what_it_can_see(B):
     assert float(norms[0]) == 0.0
 
 
+def test_example_trains():
+    """The bigram model's operators together: its loss falls below half of a uniform guess's, and the clip acts."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "bigram_lm.py")
+    spec = importlib.util.spec_from_file_location("bigram_lm", path)
+    lm = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(lm)
+    losses, norms = lm.train(steps=150)
+    assert losses[0] > 0.8 * math.log(lm.VOCAB)
+    assert np.mean(losses[-10:]) < 0.5 * math.log(lm.VOCAB)
+    assert all(math.isfinite(x) and x > 0 for x in norms) and max(norms) > 0.25
+
+
 def test_these_cases_run_clean_under_the_checked_build():
     """The same cases on the library whose kernels validate their tables and workspace ranges first."""
     import os
