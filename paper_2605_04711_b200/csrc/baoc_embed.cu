@@ -28,7 +28,9 @@ constexpr int kMostChunks = 512;
 constexpr int kJoin = 16;              // chunks whose partial sums one warp adds; a longer row's are added in two levels
 constexpr int kSlotWarps = 16;         // warps that share a run of 32 slots
 constexpr int kSlotTokens = 16;        // places of the grouped order per slot of the chunk list
-constexpr int kSegment = 32;           // rows and tokens, together, of a segment of the sums; at most the warp's lanes
+constexpr int kSegShift = 5;           // log2 of the rows and tokens, together, of a segment of the sums: one row per lane at most,
+constexpr int kSegShiftLeast = 3;      // fewer while there are not
+constexpr int kSegWarps = 24 * 148;    // as many segments' slabs as warps that the GPU holds
 // The one-kernel gradient takes at most one token per thread of a CTA, and at most so many bytes of dout (one CTA may have to
 // add them all up) and of dtable.  256 tokens x 256 into 4096 rows: 3.4 us against 8.5 us in two kernels (all tokens alike:
 // 18 against 12); 64 x 257 fp32 into 1000: 2.9 against 9.4.  Into 131 MB it loses (64 x 2048 into 32000 rows: 28.7 against
@@ -229,7 +231,7 @@ struct GradBufs {
     int2* slots;         // chunks of the long rows: {row index, chunk}, or {-1, 0}
     uint32_t* tickets;   // [slot][slab][2]: chunks done of the kJoin whose first slot this is; such groups done of the row
     float* partial;      // [slot][slab][32 V]: a chunk's sum
-    int shift, bins, slabs, n_segs, n_slots;
+    int shift, bins, slabs, seg_shift, n_segs, n_slots;
 };
 
 // Index of the last entry of the ascending a[0 .. n] that is <= x (a[0] <= x).
@@ -408,15 +410,15 @@ embed_group_kernel(const Id* __restrict__ ids, int n, uint32_t vocab, uint32_t p
     }
     __syncthreads();
     // Segments of the sums: row index + start grows by one per row and one per token; segment j begins with the first row
-    // where it has reached kSegment j.  This class names the segments that begin behind one of its rows.
+    // where it has reached j segment lengths.  This class names the segments that begin behind one of its rows.
     const int end = begin[bins];
-    const int seg_lo = int((row0 + begin[0]) / kSegment) + 1, seg_hi = cls == mask ? b.n_segs : int((row0 + bins + end) / kSegment);
+    const int seg_lo = int((row0 + begin[0]) >> b.seg_shift) + 1, seg_hi = cls == mask ? b.n_segs : int((row0 + bins + end) >> b.seg_shift);
     if (cls == 0u && threadIdx.x == 0) b.segs[0] = make_uint2(0u, 0u);
     for (int j = seg_lo + threadIdx.x; j <= seg_hi; j += blockDim.x) {
         int lo = 0, hi = bins;                          // the first row of the class (bins: the next class's) that has reached it
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            if (row0 + mid + begin[mid] >= int64_t(j) * kSegment) hi = mid; else lo = mid + 1;
+            if (row0 + mid + begin[mid] >= int64_t(j) << b.seg_shift) hi = mid; else lo = mid + 1;
         }
         b.segs[j] = make_uint2(uint32_t(row0 + lo), uint32_t(begin[lo]));
     }
@@ -632,10 +634,10 @@ embed_grad_kernel(const char* __restrict__ dout, char* dtable, const GradBufs b,
     if (!check_range(ck, kKerEmbedGrad, b.segs + work, 16, 6)) return;
 #endif
     const uint2 d0 = b.segs[work], d1 = b.segs[work + 1];
-    const int rows = int(d1.x - d0.x);                  // at most kSegment: one per lane
+    const int rows = int(d1.x - d0.x);                  // at most one per lane
     const int32_t end = int32_t(d1.y);
 #ifdef BAOC_CHECKED
-    if (rows < 0 || rows > kSegment || !check_range(ck, kKerEmbedGrad, b.start + size_t(d0.x), 4ll * rows, 0) ||
+    if (rows < 0 || rows > 32 || !check_range(ck, kKerEmbedGrad, b.start + size_t(d0.x), 4ll * rows, 0) ||
         !check_range(ck, kKerEmbedGrad, b.perm + d0.y, 4ll * (end - int32_t(d0.y)), 1)) {
         check_fail(kChkBlockIndex, kKerEmbedGrad, d0.x, d1.x, work, 0);
         return;
@@ -838,16 +840,19 @@ cudaError_t allow_group_smem() {
     return e;
 }
 
-struct EmbedLayout { size_t start, perm, segs, slots, tickets, partial, total; int shift, bins, slabs, n_segs, n_slots; };
+struct EmbedLayout { size_t start, perm, segs, slots, tickets, partial, total; int shift, bins, slabs, seg_shift, n_segs, n_slots; };
 
 EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     EmbedLayout L{};
+    L.slabs = int(ceil_div(e->dim, columns_per_warp(e->dim)));
     group_geometry(e->vocab, &L.shift, &L.bins);
     L.start = 0;
     L.perm = size_t(round_up(4 * ((int64_t(L.bins) << L.shift) + 1), 256));
-    L.slabs = int(ceil_div(e->dim, columns_per_warp(e->dim)));
     L.n_slots = int(round_up(ceil_div(n, kSlotTokens), 32));
-    L.n_segs = int(ceil_div((int64_t(L.bins) << L.shift) + n, kSegment));
+    const int64_t length = (int64_t(L.bins) << L.shift) + n;
+    L.seg_shift = kSegShift;
+    while (L.seg_shift > kSegShiftLeast && (length >> L.seg_shift) * L.slabs < kSegWarps) --L.seg_shift;
+    L.n_segs = int(ceil_div(length, int64_t(1) << L.seg_shift));
     L.segs = L.perm + size_t(round_up(4 * n, 256));
     L.slots = L.segs + size_t(round_up(8 * (int64_t(L.n_segs) + 1), 256));
     L.tickets = L.slots + size_t(round_up(8 * int64_t(L.n_slots), 256));
@@ -959,7 +964,7 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     char* w = static_cast<char*>(ws);
     const GradBufs b{reinterpret_cast<int32_t*>(w + L.start), reinterpret_cast<int32_t*>(w + L.perm), reinterpret_cast<uint2*>(w + L.segs),
                      reinterpret_cast<int2*>(w + L.slots), reinterpret_cast<uint32_t*>(w + L.tickets), reinterpret_cast<float*>(w + L.partial),
-                     L.shift, L.bins, L.slabs, L.n_segs, L.n_slots};
+                     L.shift, L.bins, L.slabs, L.seg_shift, L.n_segs, L.n_slots};
     const CheckCtx ck{w, w + L.total, 0, 0, 0};
     (void)ck;
     const EmbedArgs a{uint32_t(as * ab), uint32_t(gs * gb), e->dim, e->scale};
