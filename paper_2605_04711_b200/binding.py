@@ -309,9 +309,17 @@ class Embedding:
         self._e = Embed(self.vocab, max(-1, min(self.dim, 2 ** 31 - 1)), DTYPES[torch.float32], DTYPES[torch.bfloat16],
                         DTYPES[torch.bfloat16], 64, float(scale), -1 if pad_id is None else int(pad_id), 0, 0, 0)
         self._ref = C.byref(self._e)
-        self._form = None
+        self._form, self._numel = None, self.vocab * self.dim
         self._n = C.c_size_t()
         self.grad_workspace_bytes(0)                        # the descriptor's checks
+
+    def _take_form(self, form, fields):
+        """Two array types, the ids' type and two row strides into the descriptor."""
+        if form[0] not in DTYPES or form[1] not in DTYPES or form[2] not in _ID_BITS:
+            raise BaocError(E_INVALID, f"arrays of bfloat16 or float32 and ids of int32 or int64 are offered, not {form[:3]}")
+        for name, value in zip(fields, (DTYPES[form[0]], DTYPES[form[1]], _ID_BITS[form[2]], form[3], form[4])):
+            setattr(self._e, name, value)
+        self._form = form
 
     @staticmethod
     def _failed(rc: int):
@@ -324,19 +332,18 @@ class Embedding:
         table and out may be strided."""
         if out is None:
             out = torch.empty((*ids.shape, self.dim), dtype=out_dtype, device=table.device)
-        e, dev = self._e, table.get_device()
-        rows, table_stride = _rows(table, self.dim, "table")
-        n, act_stride = _rows(out, self.dim, "out")
-        if rows != self.vocab or n != ids.numel() or dev < 0 or ids.get_device() != dev or out.get_device() != dev:
+        dim, n, dev = self.dim, ids.numel(), table.get_device()
+        if (table.is_contiguous() and out.is_contiguous() and table.numel() == self._numel and out.numel() == n * dim
+                and table.size(-1) == dim and out.size(-1) == dim):
+            rows, n_out, table_stride, act_stride = self.vocab, n, 0, 0
+        else:
+            rows, table_stride = _rows(table, dim, "table")
+            n_out, act_stride = _rows(out, dim, "out")
+        if rows != self.vocab or n_out != n or dev < 0 or ids.get_device() != dev or out.get_device() != dev:
             raise BaocError(E_INVALID, "lookup: table must be [vocab, dim], out one row per id, all on one CUDA device")
         form = (table.dtype, out.dtype, ids.dtype, table_stride, act_stride)
-        try:
-            if form != self._form:                          # (the descriptor holds the last call's)
-                e.table_dtype, e.act_dtype, e.id_bits, e.table_stride, e.act_stride = (
-                    DTYPES[table.dtype], DTYPES[out.dtype], _ID_BITS[ids.dtype], table_stride, act_stride)
-                self._form = form
-        except KeyError as x:
-            raise BaocError(E_INVALID, f"lookup: {x.args[0]} is not offered (bfloat16 and float32 arrays, int32 and int64 ids are)") from None
+        if form != self._form:                              # (the descriptor holds the last call's)
+            self._take_form(form, ("table_dtype", "act_dtype", "id_bits", "table_stride", "act_stride"))
         if not ids.is_contiguous():
             ids = ids.contiguous()
         rc = _queue(dev, _lib.baoc_embed, self._ref, table.data_ptr(), ids.data_ptr(), n, out.data_ptr())
@@ -351,19 +358,18 @@ class Embedding:
         """dtable[v, :] = scale * sum of dout over the positions with id v (accumulate: added to dtable).  dout: ids' shape
         + [dim], dtable: [vocab, dim] (a block's flat gradient array viewed that way), bf16 or fp32 each; ws: device bytes,
         at least ``grad_workspace_bytes(ids.numel())`` (allocated when not given)."""
-        e, dev = self._e, dtable.get_device()
-        n, act_stride = _rows(dout, self.dim, "dout")
-        rows, grad_stride = _rows(dtable, self.dim, "dtable")
-        if rows != self.vocab or n != ids.numel() or dev < 0 or ids.get_device() != dev or dout.get_device() != dev:
+        dim, n, dev = self.dim, ids.numel(), dtable.get_device()
+        if (dout.is_contiguous() and dtable.is_contiguous() and dtable.numel() == self._numel and dout.numel() == n * dim
+                and dtable.size(-1) == dim and dout.size(-1) == dim):
+            rows, n_out, act_stride, grad_stride = self.vocab, n, 0, 0
+        else:
+            n_out, act_stride = _rows(dout, dim, "dout")
+            rows, grad_stride = _rows(dtable, dim, "dtable")
+        if rows != self.vocab or n_out != n or dev < 0 or ids.get_device() != dev or dout.get_device() != dev:
             raise BaocError(E_INVALID, "grad: dtable must be [vocab, dim], dout one row per id, all on one CUDA device")
         form = (dout.dtype, dtable.dtype, ids.dtype, act_stride, grad_stride, None)
-        try:
-            if form != self._form:
-                e.act_dtype, e.grad_dtype, e.id_bits, e.act_stride, e.grad_stride = (
-                    DTYPES[dout.dtype], DTYPES[dtable.dtype], _ID_BITS[ids.dtype], act_stride, grad_stride)
-                self._form = form
-        except KeyError as x:
-            raise BaocError(E_INVALID, f"grad: {x.args[0]} is not offered (bfloat16 and float32 arrays, int32 and int64 ids are)") from None
+        if form != self._form:
+            self._take_form(form, ("act_dtype", "grad_dtype", "id_bits", "act_stride", "grad_stride"))
         if not ids.is_contiguous():
             ids = ids.contiguous()
         if ws is None:
