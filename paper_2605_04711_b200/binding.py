@@ -302,7 +302,8 @@ class Embedding:
     """The token table's lookup (``baoc_embed``) and gradient (``baoc_embed_grad``): a plan of one table's shape.
 
     scale multiplies every looked-up row; ids outside [0, vocab) are ignored positions (zero rows, no gradient);
-    pad_id's row is looked up but takes no gradient.  Calls queue work on the current stream of the tensors' device."""
+    pad_id's row is looked up but takes no gradient.  Calls queue work on the current stream of the tensors' device.  Like a
+    handle, a plan serves one thread at a time."""
 
     def __init__(self, vocab: int, dim: int, scale: float = 1.0, pad_id: Optional[int] = None):
         self.vocab, self.dim = int(vocab), int(dim)

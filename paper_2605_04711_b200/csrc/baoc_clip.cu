@@ -1,6 +1,9 @@
 // Global gradient norm over the handle's blocks, and clipping by it.
 //
 //   n_i = ||g_i||,  n = sqrt(sum_i n_i^2),  dst_i = min(1, max_norm / (n + 1e-6)) * src_i.
+//
+// Memory bounds both: the norm reads every gradient once, the clip reads it again (the factor exists only after the last
+// element has been read) and writes it.  Times below: one B200, device time per call in a row of calls on three sets of arrays.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -140,6 +143,12 @@ __device__ __forceinline__ void finish_norm(const ClipBufs& c, double max_norm, 
 }
 
 // A CTA per share.  Each segment's sum of squares goes to the segment's slot; the last CTA to end adds the slots.
+// One read of everything: 1.14 G bf16 elements in 316 us = 7.2 TB/s, 124 M in 43 us (bf16) and 78 us (fp32, 6.4 TB/s); 2.4 M
+// in 7.3 us, of which 2.6 us are the reading, 2.2 us the joint finish and the rest the launch.  A CTA per tile took 418 and
+// 53 us: its registers (eight loads held for the wide-range path) left three CTAs on an SM, and each ended in a reduction, a
+// fence and a ticket.  Equal shares end once, but all wait for their loads together: without the second round in flight
+// they took 392 and 52 us.  The values' squares are checked per round, not per element, and a round that leaves the fp32
+// range is read again.
 template <int DT>
 __global__ void __launch_bounds__(kThreads, kNormCtasPerSm)
 grad_norm_kernel(const ClipBufs c, double max_norm, float* __restrict__ norms BAOC_CHECK_PARAM) {
@@ -200,6 +209,11 @@ __device__ __forceinline__ void load8(const typename Vec<SRC>::Elem* p, uint4& a
     if constexpr (SRC == BAOC_F32) b = ld_stream_u4(p + 4);
 }
 
+// 1.14 G bf16 elements: 690 us behind the norm = 6.6 TB/s of one read and one write, the copy bandwidth; 124 M from fp32 to bf16:
+// 117 us = 6.4 TB/s.  Tiles of 16384 elements beat 4096 by 8 % there, and lose to it by 13 % at 2.4 M elements (12.7 against
+// 11.1 us for both kernels).  Policies that keep the norm's last bytes in L2 for this read, and orders that go with them, were
+// measured and make no difference.
+//
 // dst = factor * src, one CTA per tile, the last tiles first.  All but the factor is there before the norm has ended: a CTA
 // that finds a place by then has its first elements in hand when the factor comes.
 template <int SRC, int DST>
