@@ -25,8 +25,8 @@ constexpr int kGroupWarps = 32;
 constexpr int kGroupSplit = 4;         // CTAs that share the reading of the ids,
 constexpr int64_t kSplitTokens = 32768; // from this many tokens on
 constexpr int kIdLoads = 16;           // ids a lane of the grouping has in flight
-constexpr int kSeen = 256;             // the same for what a warp finds of a cluster's classes together
 constexpr int kListed = 512;           // tokens a warp of the grouping can list; when it finds more it reads the ids again
+constexpr int kSeen = 256;             // the same for what a warp finds of all classes of a cluster
 constexpr int kListBits = 22;          // bits of a token's offset in a list entry (the id of the class, below kGroupBins, has the others)
 constexpr int kShortRow = 32;          // tokens of a row that one warp sums by itself; longer rows are cut into chunks
 constexpr int kMostChunks = 512;
