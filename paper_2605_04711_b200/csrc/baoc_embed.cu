@@ -178,20 +178,21 @@ __device__ __forceinline__ bool is_row(int32_t id, uint32_t vocab) { return uint
 __device__ __forceinline__ bool is_row(int64_t id, uint32_t vocab) { return uint32_t(uint64_t(id) >> 32) == 0u && uint32_t(id) < vocab; }
 
 // ---- lookup: one warp per slab of kTokens tokens, all of their loads in flight -----------------------------------------
-// Four rows of fp32 or eight of bf16 are 4 KB in flight per warp: with one load per thread and a division per element the same
-// calls took 10.9 us (16384 x 768 of fp32, now 8.9: 4.9 TB/s of the distinct rows and the output), 175 us (131072 x 2048 of
-// fp32, now 127: 5.5 TB/s) and 81 us (65536 x 2048 of bf16, now 53: 6.1 TB/s).  The fp32 table's repeated rows cross L2 once
-// per use, which is what is left there.  One token: 1.9 us, a launch.
+// Two rows of fp32 or four of bf16 are 2 KB in flight per warp, in as many warps as an SM holds: with one load per thread and a
+// division per element the same calls took 10.9 us (16384 x 768 of fp32, now 9.0: 4.9 TB/s of the distinct rows and the
+// output), 175 us (131072 x 2048 of fp32, now 125: 5.6 TB/s) and 81 us (65536 x 2048 of bf16, now 53: 6.1 TB/s).  Twice the
+// tokens in half the warps: 127 us for the second, 65 us instead of 54 for 32768 x 2047 (element by element); half the tokens:
+// 160 and 57 us.  The fp32 table's repeated rows cross L2 once per use, which is what is left there.  One token: 1.9 us, a launch.
 template <int SRC, int DST, int V, int M, typename Id>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, M == kWide ? 8 : 6)
 embed_kernel(const char* __restrict__ table, const Id* __restrict__ ids, char* __restrict__ out, uint32_t vocab, int64_t n, int slabs,
              const EmbedArgs a) {
     using P = Part<SRC, V, M>;
-    constexpr int kTokens = P::kWords == 8 ? 4 : 8;
+    constexpr int kTokens = P::kWords == 8 ? 2 : 4;
     const int lane = threadIdx.x & 31;
     const uint32_t item = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     // fp32 tables go through slab by slab: a frequent row's kilobyte is then found in L1 (131072 tokens x 2048 of a Zipf-like
-    // stream: 128 us, 140 token by token); rows of half that size go token by token (65536 x 2048 of bf16: 54 us, 58 slab by slab).
+    // stream, four tokens a warp: 128 us, 140 token by token); rows of half that size go token by token (65536 x 2048 of bf16: 54 us, 58 slab by slab).
     constexpr bool kBySlab = SRC == BAOC_F32 && M == kWide;
     const uint32_t groups = uint32_t((n + kTokens - 1) / kTokens), per = kBySlab ? groups : uint32_t(slabs), q = item / per, r = item - q * per;
     const int slab = int(kBySlab ? q : r);
@@ -938,7 +939,7 @@ int baoc_embed(const baoc_embed_t* e, const void* table, const void* ids, int64_
     const int access = std::min(access_of(table, ts, tb, e->dim), access_of(out, os, ob, e->dim));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->table_dtype, e->act_dtype, e->dim, access, [&](auto S, auto D, auto V, auto M) {
-        constexpr int kTokens = Part<S(), V(), M()>::kWords == 8 ? 4 : 8;
+        constexpr int kTokens = Part<S(), V(), M()>::kWords == 8 ? 2 : 4;
         const int64_t items = ceil_div(n_tokens, kTokens) * slabs, blocks = ceil_div(items, kThreads / 32);
         if (items > int64_t(0x7fffffff)) return fail_embed(BAOC_E_INVALID, "baoc_embed: too many elements for one launch");
         const char* tab = static_cast<const char*>(table);
