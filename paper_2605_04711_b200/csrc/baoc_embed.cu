@@ -36,14 +36,16 @@ constexpr int kSlotTokens = 16;        // places of the grouped order per slot o
 constexpr int kSegShift = 5;           // log2 of the rows and tokens, together, of a segment of the sums: one row per lane at most,
 constexpr int kSegShiftLeast = 3;      // fewer while there are not
 constexpr int kSegWarps = 24 * 148;    // as many segments' slabs as warps that the GPU holds
-// The one-kernel gradient takes at most one token per thread of a CTA, and at most so many bytes of dout (one CTA may have to
-// add them all up) and of dtable.  256 tokens x 256 into 4096 rows: 3.4 us against 8.5 us in two kernels (all tokens alike:
-// 18 against 12); 64 x 257 fp32 into 1000: 2.9 against 9.4.  Into 131 MB it loses (64 x 2048 into 32000 rows: 28.7 against
-// 26.0 us), its warps being far fewer; at 66 MB the two are level.
+// The one-kernel gradient takes at most one token per thread of a CTA, and at most so many bytes of dout: one CTA may have to
+// add them all up.  Against two kernels: 256 tokens x 256 into 4096 rows 3.4 us (8.5), 64 x 257 fp32 into 1000 rows 2.9 (9.4),
+// 4 x 1280 into 41212 rows 16.4 (25.1), 64 x 2048 into 32000 rows 20.9 (25.9); all tokens alike it loses from 128 tokens on
+// (128 x 2048 into 32000 rows 27.3 against 25.6, 256 x 256 into 4096 rows 19.9 against 11.6).  Large tables want their rows
+// dealt to more CTAs than find room at once (64 x 2048 into 32000 rows: 20.9 us, 24.6 with kFewCtas), small ones do not
+// (256 x 512 into 16384 rows: 6.2 us, 8.9 with kFewCtasLarge).
 constexpr int kFewTokens = kThreads;
 constexpr int64_t kFewBytes = 512 << 10;
-constexpr int64_t kFewTableBytes = 32 << 20;
-constexpr int kFewCtas = 8 * 148;
+constexpr int64_t kFewLargeTable = 32 << 20;           // bytes of dtable from which the rows are dealt to more CTAs
+constexpr int kFewCtas = 8 * 148, kFewCtasLarge = 24 * 148;
 constexpr int kEmbedMaxDim = 1 << 24;
 constexpr int64_t kEmbedMaxStride = 1 << 28;           // (row products stay far inside 64 bits)
 
@@ -761,9 +763,28 @@ embed_grad_few_kernel(const void* __restrict__ ids, int id_bits, int n, const ch
     }
     __syncthreads();
     const uint32_t rows = (vocab - blockIdx.x + step - 1) / step;
-    for (int64_t item = warp; item < int64_t(rows) * slabs; item += kThreads / 32) {
-        const uint32_t r = uint32_t(item / slabs);
-        const int slab = int(item - int64_t(r) * slabs);
+    // the next pair of a warp is kThreads / 32 further on
+    const uint32_t row_step = uint32_t(kThreads / 32) / uint32_t(slabs);
+    const int slab_step = kThreads / 32 - int(row_step) * slabs;
+    uint32_t r = uint32_t(warp) / uint32_t(slabs);
+    int slab = warp - int(r) * slabs;
+    auto next = [&]() {
+        r += row_step;
+        slab += slab_step;
+        if (slab >= slabs) { slab -= slabs; ++r; }
+    };
+    if (listed == 0) {                                  // most CTAs: nothing but zeros to write
+        if (accumulate) return;
+        float zero[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) zero[j] = 0.f;
+        for (; r < rows; next()) {
+            const int col = lane_col<V, M>(slab, lane);
+            store_part<GRAD, V, M>(dtable + uint64_t(blockIdx.x + r * step) * a.dst_step + int64_t(col) * (GRAD == BAOC_BF16 ? 2 : 4), col, a.dim, zero);
+        }
+        return;
+    }
+    for (; r < rows; next()) {
         const int col = lane_col<V, M>(slab, lane), rc = read_col<V, M>(col, a.dim), last = last_read<V, M>(rc, a.dim, P::kSize);
         const char* src = dout + int64_t(rc) * P::kSize;
         float acc[V];
@@ -989,9 +1010,9 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
     (void)ck;
     const EmbedArgs a{uint32_t(as * ab), uint32_t(gs * gb), e->dim, e->scale};
     const int access = std::min(access_of(dout, as, ab, e->dim), access_of(dtable, gs, gb, e->dim));
-    if (n_tokens <= kFewTokens && n_tokens * e->dim * ab <= kFewBytes && e->vocab * e->dim * gb <= kFewTableBytes) {
+    if (n_tokens <= kFewTokens && n_tokens * e->dim * ab <= kFewBytes) {
         const int64_t pairs = e->vocab * L.slabs;
-        const unsigned ctas = unsigned(std::min<int64_t>(std::min<int64_t>(e->vocab, kFewCtas), ceil_div(pairs, kThreads / 32)));
+        const unsigned ctas = unsigned(std::min<int64_t>(std::min<int64_t>(e->vocab, e->vocab * e->dim * gb < kFewLargeTable ? kFewCtas : kFewCtasLarge), ceil_div(pairs, kThreads / 32)));
         return with_types(e->act_dtype, e->grad_dtype, e->dim, access, [&](auto A, auto G, auto V, auto M) {
             embed_grad_few_kernel<A(), G(), V(), M()><<<ctas, kThreads, 0, s>>>(ids, e->id_bits, int(n_tokens), static_cast<const char*>(dout),
                                                                                  static_cast<char*>(dtable), uint32_t(e->vocab), uint32_t(e->pad_id),

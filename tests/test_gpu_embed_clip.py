@@ -150,7 +150,7 @@ GRAD_SHAPES = [(1, 1, 1, "uniform"), (1, 300, 2048, "uniform"), (3, 5, 2, "unifo
                (333, 1000, 100, "skewed"), (1000, 129, 136, "same"), (31, 128, 8, "same"), (32, 127, 16, "same"), (33, 50, 24, "same"),
                (2049, 300, 40, "skewed"), (5000, 3, 33, "uniform"), (4099, 513, 520, "skewed"), (70000, 40, 16, "skewed"),
                (40000, 17, 300, "same"), (256, 50, 40, "same"), (257, 50, 40, "same"), (200, 30, 1500, "skewed"), (256, 5, 511, "uniform"),
-               (300, 90, 362, "skewed"), (5000, 100, 98, "skewed"), (900, 33, 50, "skewed"), (900, 33, 130, "skewed")]
+               (300, 90, 362, "skewed"), (5000, 100, 98, "skewed"), (900, 33, 50, "skewed"), (900, 33, 130, "skewed"), (60, 30000, 600, "skewed")]
 
 
 @pytest.mark.parametrize("n,vocab,dim,kind", GRAD_SHAPES)
