@@ -373,9 +373,8 @@ factored_combine_kernel(const StepBlock* __restrict__ blocks, const int32_t* __r
 // reciprocal (relative error 2^-23 each): the update is lr * direction, a
 // small fraction of the parameter, so the parameter keeps full fp32 accuracy,
 // and the moments themselves never pass through an approximation.  Both are
-// the flush-to-zero forms, which are single instructions (the others wrap the
-// same unit in subnormal scaling: six instructions per square root): a second
-// moment below 1.2e-38 counts as 0 under the root, far below any eps in use.
+// the flush-to-zero forms: a second moment below 1.2e-38 counts as 0 under the
+// root, far below any eps in use.
 // ============================================================================
 
 __device__ __forceinline__ void prologue(float& x, float& t, const CfgStep& P) {
