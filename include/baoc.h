@@ -579,7 +579,8 @@ typedef struct {
 int baoc_embed(const baoc_embed_t* e, const void* table, const void* ids, int64_t n_tokens, void* out,
                baoc_stream_t stream);
 
-/* Bytes of device workspace baoc_embed_grad needs for n_tokens tokens. */
+/* Bytes of device workspace baoc_embed_grad needs for n_tokens tokens; never falls
+ * as n_tokens grows, so a workspace serves every smaller batch too. */
 int baoc_embed_grad_workspace_bytes(const baoc_embed_t* e, int64_t n_tokens, size_t* bytes);
 
 /* dtable[vocab][dim] from dout[n_tokens][dim].  accumulate = 0 writes every row

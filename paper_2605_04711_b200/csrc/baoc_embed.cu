@@ -894,8 +894,13 @@ EmbedLayout embed_layout(const baoc_embed_t* e, int64_t n) {
     L.seg_shift = kSegShift;
     while (L.seg_shift > kSegShiftLeast && (length >> L.seg_shift) * L.slabs < kSegWarps) --L.seg_shift;
     L.n_segs = int(ceil_div(length, int64_t(1) << L.seg_shift));
+    // The segment table's size must not fall as n grows (a workspace serves every smaller batch), though n_segs halves where
+    // the segments get longer: a shift below kSegShift is taken only while the next one leaves fewer than ceil(kSegWarps /
+    // slabs) segments, so it has at most twice as many.
+    const int64_t most_segs = std::min(ceil_div(length, int64_t(1) << kSegShiftLeast),
+                                       std::max(ceil_div(length, int64_t(1) << kSegShift), 2 * ceil_div(int64_t(kSegWarps), L.slabs)));
     L.segs = L.perm + size_t(round_up(4 * n, 256));
-    L.slots = L.segs + size_t(round_up(8 * (int64_t(L.n_segs) + 1), 256));
+    L.slots = L.segs + size_t(round_up(8 * (most_segs + 1), 256));
     L.tickets = L.slots + size_t(round_up(8 * int64_t(L.n_slots), 256));
     L.partial = L.tickets + size_t(round_up(8 * int64_t(L.n_slots) * L.slabs, 256));
     L.total = L.partial + size_t(4 * int64_t(L.n_slots) * L.slabs * columns_per_warp(e->dim));
