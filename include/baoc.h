@@ -525,8 +525,9 @@ enum { BAOC_BF16 = 0, BAOC_F32 = 1 };
 int baoc_clip_workspace_bytes(const baoc_t* h, size_t* bytes);
 
 /* Give the handle that workspace (device, 256-byte aligned, >= the size above).
- * Queues the upload of the tile table on the stream; calls on other streams have
- * to be ordered behind it by the caller.  It may be bound again at any time. */
+ * Queues the upload of its tables on the stream; calls on other streams have to
+ * be ordered behind it by the caller.  It may be bound again at any time, but not
+ * while the stream is being captured (BAOC_E_STATE): bind before the capture. */
 int baoc_bind_clip_workspace(baoc_t* h, void* dev, size_t bytes, baoc_stream_t stream);
 
 /* norms (device, 1 + n_blocks floats, 4-byte aligned): n, then n_0 .. n_{n_blocks-1}.

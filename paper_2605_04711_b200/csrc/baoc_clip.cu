@@ -389,6 +389,11 @@ int baoc_bind_clip_workspace(baoc_t* h, void* dev, size_t bytes, baoc_stream_t s
     if (bytes < L.total) return fail(h, BAOC_E_WORKSPACE, "baoc_bind_clip_workspace: workspace too small");
     if (L.clip_tiles > int64_t(0x7fffffff)) return fail(h, BAOC_E_INVALID, "baoc_bind_clip_workspace: too many elements for one launch");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // (a captured upload would read the vectors below when the graph is replayed, long after they are gone)
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(s, &cap);
+    if (e != cudaSuccess) return cuda_error(h, "baoc_bind_clip_workspace", e);
+    if (cap != cudaStreamCaptureStatusNone) return fail(h, BAOC_E_STATE, "baoc_bind_clip_workspace: the stream is capturing; bind before the capture");
     char* ws = static_cast<char*>(dev);
     // share i: the tiles [i * tiles / ctas, (i + 1) * tiles / ctas) of all blocks in a row
     std::vector<ClipSeg> segs;
@@ -423,7 +428,7 @@ int baoc_bind_clip_workspace(baoc_t* h, void* dev, size_t bytes, baoc_stream_t s
         for (int64_t j = ceil_div(h->blocks[i].numel, L.clip_tile) - 1; j >= 0; --j) tiles.push_back(Tile{uint32_t(i), uint32_t(j)});
     std::vector<int64_t> numel;
     for (const baoc_block_t& b : h->blocks) numel.push_back(b.numel);
-    cudaError_t e = up(L.segs, segs.data(), sizeof(ClipSeg) * segs.size());
+    e = up(L.segs, segs.data(), sizeof(ClipSeg) * segs.size());
     if (e == cudaSuccess) e = up(L.tile_list, tiles.data(), sizeof(Tile) * tiles.size());
     if (e == cudaSuccess) e = up(L.numel, numel.data(), 8 * numel.size());
     if (e == cudaSuccess) e = up(L.cta_list, ctas.data(), sizeof(ClipCta) * ctas.size());

@@ -209,6 +209,8 @@ class Session:
     def clip_grads(self, k: int, max_norm: float) -> torch.Tensor:
         """Clip gradient set k in place by its global norm; returns the norms before it (the global one, then every block's)."""
         if self.clip_norms is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise B.BaocError(B.E_STATE, "clip_grads: the first call binds its workspace and cannot be captured")
             self.h.bind_clip_workspace(self._alloc(self.h.clip_workspace_bytes()))
             self.clip_norms = self._alloc(4 * (1 + len(self.wl.blocks)), True).view(torch.float32)
         return self.h.clip_grads(self.grad_tables[k], None, max_norm, self.clip_norms)
