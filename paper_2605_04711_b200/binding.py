@@ -398,6 +398,7 @@ class Baoc:
         self._cfgs = (Config * len(configs))(*configs)
         self._h = _vp()
         self._keep = []            # device buffers the handle points into
+        self._clip_device = None   # where the clip workspace is
         rc = _lib.baoc_create(C.byref(self._h), len(bl), self._blocks, len(configs), self._cfgs,
                               C.byref(opts) if opts is not None else None)
         if rc != 0:
@@ -487,11 +488,18 @@ class Baoc:
         return n.value
 
     def bind_clip_workspace(self, ws: torch.Tensor):
-        self._check(_lib.baoc_bind_clip_workspace(self._h, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
-        self._keep.append(ws)
+        """``baoc_bind_clip_workspace`` on the current stream of ws's device, where the norm and the clip have to run from then
+        on.  Workspaces bound before stay alive with the handle: a captured graph may still use one."""
+        dev = ws.get_device()
+        if dev < 0 or not ws.is_contiguous():
+            raise BaocError(E_INVALID, "bind_clip_workspace: ws must be a contiguous buffer on a CUDA device")
+        self._check(_queue(dev, _lib.baoc_bind_clip_workspace, self._h, ws.data_ptr(), ws.numel() * ws.element_size()))
+        self._clip_device = dev
+        if not any(k is ws for k in self._keep):
+            self._keep.append(ws)
 
-    def _clip_arrays(self, arrays, dtype, what: str):
-        """(pointer table, dtype code) of a list of device tensors, or of a table from ``pointer_table`` and its dtype."""
+    def _clip_arrays(self, arrays, dtype, dev: int, what: str):
+        """(pointer table, dtype code) of a list of tensors on device dev, or of a table from ``pointer_table`` and its dtype."""
         if isinstance(arrays, C.Array):
             if len(arrays) != self.n_blocks:
                 raise BaocError(E_INVALID, f"{what}: one array per block")
@@ -499,8 +507,8 @@ class Baoc:
         if len(arrays) != self.n_blocks:
             raise BaocError(E_INVALID, f"{what}: one array per block")
         for t, b in zip(arrays, self._blocks):
-            if t.numel() != b.numel or not t.is_contiguous() or t.dtype != arrays[0].dtype or not t.is_cuda:
-                raise BaocError(E_INVALID, f"{what}: contiguous device arrays of the blocks' sizes, of one dtype")
+            if t.numel() != b.numel or not t.is_contiguous() or t.dtype != arrays[0].dtype or t.get_device() != dev:
+                raise BaocError(E_INVALID, f"{what}: contiguous arrays of the blocks' sizes, of one dtype, on the device of norms")
         if dtype is not None and dtype != arrays[0].dtype:
             raise BaocError(E_INVALID, f"{what}: the arrays are {arrays[0].dtype}, not {dtype}")
         return pointer_table(arrays), _dtype_code(arrays[0].dtype)
@@ -510,22 +518,26 @@ class Baoc:
         dev = norms.get_device()
         if dev < 0 or norms.dtype != torch.float32 or norms.numel() != 1 + self.n_blocks or not norms.is_contiguous():
             raise BaocError(E_INVALID, "norms must be a contiguous float32 device tensor of 1 + n_blocks elements")
+        if dev != self._clip_device and self._clip_device is not None:
+            raise BaocError(E_INVALID, f"norms must be on the clip workspace's device, cuda:{self._clip_device}")
         return dev
 
     def grad_norm(self, grads, norms: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
         """``baoc_grad_norm``: norms[0] = the global gradient norm, norms[1 + i] block i's.  grads: list of bf16 or fp32
         device tensors, or a table from ``pointer_table`` with its dtype (bfloat16 when not given)."""
-        tab, code = self._clip_arrays(grads, dtype, "grad_norm")
-        self._check(_queue(self._norms(norms), _lib.baoc_grad_norm, self._h, tab, code, norms.data_ptr()))
+        dev = self._norms(norms)
+        tab, code = self._clip_arrays(grads, dtype, dev, "grad_norm")
+        self._check(_queue(dev, _lib.baoc_grad_norm, self._h, tab, code, norms.data_ptr()))
         return norms
 
     def clip_grads(self, grads, out, max_norm: float, norms: torch.Tensor, src_dtype: Optional[torch.dtype] = None,
                    dst_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
         """``baoc_clip_grads``: the norms, then out_i = min(1, max_norm / (norms[0] + 1e-6)) * grads_i.  out None: in place.
         Arrays as for ``grad_norm``; bf16 -> bf16, fp32 -> fp32 or fp32 -> bf16.  Returns norms."""
-        src, sc = self._clip_arrays(grads, src_dtype, "clip_grads")
-        dst, dc = (src, sc) if out is None else self._clip_arrays(out, dst_dtype, "clip_grads")
-        self._check(_queue(self._norms(norms), _lib.baoc_clip_grads, self._h, src, sc, dst, dc, float(max_norm), norms.data_ptr()))
+        dev = self._norms(norms)
+        src, sc = self._clip_arrays(grads, src_dtype, dev, "clip_grads")
+        dst, dc = (src, sc) if out is None else self._clip_arrays(out, dst_dtype, dev, "clip_grads")
+        self._check(_queue(dev, _lib.baoc_clip_grads, self._h, src, sc, dst, dc, float(max_norm), norms.data_ptr()))
         return norms
 
     # ---- allocation -------------------------------------------------------

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2605_04711_b200 import binding as B
 
@@ -22,3 +23,78 @@ def test_a_workspace_serves_every_smaller_batch(vocab, dim):
         size = _workspace(vocab, dim, n)
         assert size >= last, n
         last = size
+
+
+# ---- devices: tensors of several GPUs stood in for by what the calls look at --------------------------------------------
+class _OnDevice:
+    """A contiguous array of some GPU as the binding sees one."""
+
+    def __init__(self, device, numel, dtype, address=1 << 20):
+        self.device_index, self.n, self.dtype, self.address = device, numel, dtype, address
+        self.is_cuda = True
+
+    def get_device(self):
+        return self.device_index
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return {torch.uint8: 1, torch.bfloat16: 2, torch.float32: 4}[self.dtype]
+
+    def data_ptr(self):
+        return self.address
+
+    def is_contiguous(self):
+        return True
+
+
+@pytest.fixture
+def queued(monkeypatch):
+    """Calls that would be queued, as (device, entry point)."""
+    log = []
+
+    def queue(device, call, *args):
+        log.append((device, call))
+        return B.OK
+    monkeypatch.setattr(B, "_queue", queue)
+    monkeypatch.setattr(B, "_stream", lambda: pytest.fail("queued on whatever device is current"))
+    return log
+
+
+def test_a_clip_workspace_is_bound_on_its_own_device(queued):
+    h = B.Baoc([(64, 8, 8), (5, 5, 1)], B.default_configs())
+    h.bind_clip_workspace(_OnDevice(1, h.clip_workspace_bytes(), torch.uint8))
+    assert queued == [(1, B._lib.baoc_bind_clip_workspace)]
+
+
+def test_a_clip_workspace_is_contiguous_device_memory(queued):
+    h = B.Baoc([(64, 8, 8), (5, 5, 1)], B.default_configs())
+    with pytest.raises(B.BaocError) as err:
+        h.bind_clip_workspace(torch.empty(h.clip_workspace_bytes(), dtype=torch.uint8))
+    assert err.value.code == B.E_INVALID and queued == []
+
+
+def test_clip_arrays_are_on_the_workspaces_device(queued):
+    h = B.Baoc([(64, 8, 8), (5, 5, 1)], B.default_configs())
+    h.bind_clip_workspace(_OnDevice(1, h.clip_workspace_bytes(), torch.uint8))
+    del queued[:]
+    arrays = lambda *devices: [_OnDevice(d, n, torch.bfloat16) for d, n in zip(devices, (64, 5))]
+    here, there = _OnDevice(1, 3, torch.float32), _OnDevice(0, 3, torch.float32)
+    for call in (lambda: h.grad_norm(arrays(1, 1), there), lambda: h.grad_norm(arrays(1, 0), here), lambda: h.grad_norm(arrays(0, 0), here),
+                 lambda: h.grad_norm(arrays(0, 0), there), lambda: h.clip_grads(arrays(1, 1), arrays(0, 1), 1.0, here),
+                 lambda: h.clip_grads(arrays(1, 1), None, 1.0, there)):
+        with pytest.raises(B.BaocError) as err:
+            call()
+        assert err.value.code == B.E_INVALID and queued == []
+    h.grad_norm(arrays(1, 1), here)
+    h.clip_grads(arrays(1, 1), arrays(1, 1), 1.0, here)
+    assert queued == [(1, B._lib.baoc_grad_norm), (1, B._lib.baoc_clip_grads)]
+
+
+def test_binding_the_same_workspace_again_keeps_one_reference(queued):
+    h = B.Baoc([(64, 8, 8), (5, 5, 1)], B.default_configs())
+    ws = _OnDevice(0, h.clip_workspace_bytes(), torch.uint8)
+    for _ in range(3):
+        h.bind_clip_workspace(ws)
+    assert sum(k is ws for k in h._keep) == 1
