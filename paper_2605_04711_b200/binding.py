@@ -329,8 +329,8 @@ class Embedding:
     def lookup(self, table: torch.Tensor, ids: torch.Tensor, out: Optional[torch.Tensor] = None,
                out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """out[..., :] = scale * table[ids[...], :].  table: [vocab, dim] fp32 or bf16; ids: int32 or int64 of any shape (a
-        non-contiguous one is copied first); out: ids' shape + [dim] (allocated as out_dtype when not given); rows of
-        table and out may be strided."""
+        non-contiguous one is copied first); out: ids' shape + [dim], either of the two also flattened (allocated as
+        out_dtype when not given); rows of table and out may be strided."""
         if out is None:
             out = torch.empty((*ids.shape, self.dim), dtype=out_dtype, device=table.device)
         dim, n, dev = self.dim, ids.numel(), table.get_device()
@@ -340,6 +340,8 @@ class Embedding:
         else:
             rows, table_stride = _rows(table, dim, "table")
             n_out, act_stride = _rows(out, dim, "out")
+        if ids.dim() != 1 and out.dim() != 2 and out.shape[:-1] != ids.shape:
+            raise BaocError(E_INVALID, f"lookup: out must be of ids' shape + [{dim}], not {list(out.shape)} for {list(ids.shape)}")
         if rows != self.vocab or n_out != n or dev < 0 or ids.get_device() != dev or out.get_device() != dev:
             raise BaocError(E_INVALID, "lookup: table must be [vocab, dim], out one row per id, all on one CUDA device")
         form = (table.dtype, out.dtype, ids.dtype, table_stride, act_stride)
@@ -357,7 +359,7 @@ class Embedding:
     def grad(self, ids: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, accumulate: bool = False,
              ws: Optional[torch.Tensor] = None) -> torch.Tensor:
         """dtable[v, :] = scale * sum of dout over the positions with id v (accumulate: added to dtable).  dout: ids' shape
-        + [dim], dtable: [vocab, dim] (a block's flat gradient array viewed that way), bf16 or fp32 each; ws: device bytes,
+        + [dim], either of the two also flattened, dtable: [vocab, dim] (a block's flat gradient array viewed that way), bf16 or fp32 each; ws: device bytes,
         at least ``grad_workspace_bytes(ids.numel())`` (allocated when not given)."""
         dim, n, dev = self.dim, ids.numel(), dtable.get_device()
         if (dout.is_contiguous() and dtable.is_contiguous() and dtable.numel() == self._numel and dout.numel() == n * dim
@@ -366,6 +368,8 @@ class Embedding:
         else:
             n_out, act_stride = _rows(dout, dim, "dout")
             rows, grad_stride = _rows(dtable, dim, "dtable")
+        if ids.dim() != 1 and dout.dim() != 2 and dout.shape[:-1] != ids.shape:
+            raise BaocError(E_INVALID, f"grad: dout must be of ids' shape + [{dim}], not {list(dout.shape)} for {list(ids.shape)}")
         if rows != self.vocab or n_out != n or dev < 0 or ids.get_device() != dev or dout.get_device() != dev:
             raise BaocError(E_INVALID, "grad: dtable must be [vocab, dim], dout one row per id, all on one CUDA device")
         form = (dout.dtype, dtable.dtype, ids.dtype, act_stride, grad_stride, None)

@@ -98,3 +98,28 @@ def test_binding_the_same_workspace_again_keeps_one_reference(queued):
     for _ in range(3):
         h.bind_clip_workspace(ws)
     assert sum(k is ws for k in h._keep) == 1
+
+
+# ---- shapes -------------------------------------------------------------------------------------------------------------
+def test_ids_and_rows_that_do_not_belong_together_are_refused():
+    """As many rows as ids are not enough: [30, 3] ids and rows [3, 30] pair up wrongly."""
+    e = B.Embedding(10, 8)
+    table = torch.zeros(10, 8)
+    for ids_shape, lead in (((30, 3), (3, 30)), ((2, 3, 5), (2, 5, 3)), ((6, 1), (2, 3))):
+        ids, rows = torch.zeros(ids_shape, dtype=torch.int64), torch.zeros(*lead, 8)
+        for call in (lambda: e.lookup(table, ids, out=rows), lambda: e.grad(ids, rows, table)):
+            with pytest.raises(B.BaocError, match="shape") as err:
+                call()
+            assert err.value.code == B.E_INVALID
+
+
+@pytest.mark.parametrize("ids_shape,lead", [((6,), (6,)), ((2, 3), (2, 3)), ((2, 3), (6,)), ((6,), (2, 3)), ((), ()), ((), (1,)), ((1, 6), (6,)),
+                                            ((0, 3), (0, 3))])
+def test_ids_and_rows_that_belong_together_are_queued(queued, monkeypatch, ids_shape, lead):
+    """Equal leading shapes, or one of the two in a row."""
+    e = B.Embedding(10, 8)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    ids, rows, table = torch.zeros(ids_shape, dtype=torch.int64), torch.zeros(*lead, 8), torch.zeros(10, 8)
+    assert e.lookup(table, ids, out=rows) is rows
+    assert e.grad(ids, rows, table, ws=torch.zeros(e.grad_workspace_bytes(6), dtype=torch.uint8)) is table
+    assert queued == [(0, B._lib.baoc_embed), (0, B._lib.baoc_embed_grad)]
