@@ -322,8 +322,10 @@ class Embedding:
             setattr(self._e, name, value)
         self._form = form
 
-    @staticmethod
-    def _failed(rc: int):
+    def _failed(self, rc: int):
+        """Raises, and leaves no stride of the refused arrays in the descriptor."""
+        self._form = None
+        self._e.table_stride = self._e.act_stride = self._e.grad_stride = 0
         raise BaocError(rc, _lib.baoc_embed_last_error().decode())
 
     def lookup(self, table: torch.Tensor, ids: torch.Tensor, out: Optional[torch.Tensor] = None,

@@ -123,3 +123,20 @@ def test_ids_and_rows_that_belong_together_are_queued(queued, monkeypatch, ids_s
     assert e.lookup(table, ids, out=rows) is rows
     assert e.grad(ids, rows, table, ws=torch.zeros(e.grad_workspace_bytes(6), dtype=torch.uint8)) is table
     assert queued == [(0, B._lib.baoc_embed), (0, B._lib.baoc_embed_grad)]
+
+
+def test_a_refused_call_leaves_the_plan_as_it_was(monkeypatch):
+    """A row stride above 2^28 is refused by the library; what comes after the refusal is not refused for it."""
+    e, other = B.Embedding(2, 8), B.Embedding(2, 8)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(B, "_queue", lambda device, call, *args: call(*args, None))
+    stride = (1 << 28) + 1
+    wide = torch.empty(stride + 8, device="meta").as_strided((2, 8), (stride, 1))
+    ids, rows, ws = torch.zeros(2, dtype=torch.int64), torch.zeros(2, 8), torch.zeros(1 << 20, dtype=torch.uint8)
+    for call in (lambda: e.lookup(wide, ids, out=rows), lambda: e.lookup(torch.zeros(2, 8), ids, out=wide), lambda: e.grad(ids, wide, rows, ws=ws),
+                 lambda: e.grad(ids, rows, wide, ws=ws)):
+        for _ in range(2):
+            with pytest.raises(B.BaocError, match="row stride") as err:
+                call()
+            assert err.value.code == B.E_INVALID
+        assert e.grad_workspace_bytes(1000) == other.grad_workspace_bytes(1000)
