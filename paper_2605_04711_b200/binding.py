@@ -332,7 +332,10 @@ class Embedding:
                out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """out[..., :] = scale * table[ids[...], :].  table: [vocab, dim] fp32 or bf16; ids: int32 or int64 of any shape (a
         non-contiguous one is copied first); out: ids' shape + [dim], either of the two also flattened (allocated as
-        out_dtype when not given); rows of table and out may be strided."""
+        out_dtype when not given); rows of table and out may be strided.  The output carries no autograd history: a table
+        that requires a gradient is refused unless it is detached or gradients are off (``grad`` is the gradient)."""
+        if table.requires_grad and torch.is_grad_enabled():
+            raise BaocError(E_INVALID, "lookup: autograd does not see this call; detach the table, or call it under torch.no_grad()")
         if out is None:
             out = torch.empty((*ids.shape, self.dim), dtype=out_dtype, device=table.device)
         dim, n, dev = self.dim, ids.numel(), table.get_device()

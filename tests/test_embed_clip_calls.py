@@ -140,3 +140,17 @@ def test_a_refused_call_leaves_the_plan_as_it_was(monkeypatch):
                 call()
             assert err.value.code == B.E_INVALID
         assert e.grad_workspace_bytes(1000) == other.grad_workspace_bytes(1000)
+
+
+def test_a_lookup_that_autograd_would_lose_is_refused(queued, monkeypatch):
+    """The output carries no history: a table that requires a gradient would silently get none."""
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    e, ids, rows = B.Embedding(10, 8), torch.zeros(4, dtype=torch.int64), torch.zeros(4, 8)
+    table = torch.zeros(10, 8, requires_grad=True)
+    with pytest.raises(B.BaocError, match="detach") as err:
+        e.lookup(table, ids, out=rows)
+    assert err.value.code == B.E_INVALID and queued == []
+    e.lookup(table.detach(), ids, out=rows)
+    with torch.no_grad():
+        e.lookup(table, ids, out=rows)
+    assert len(queued) == 2
