@@ -510,12 +510,12 @@ int baoc_check_selftest(baoc_stream_t stream);
  *
  * dtype: BAOC_BF16 or BAOC_F32 (the gradients that baoc_step reads are bf16;
  * fp32 is for arrays that accumulate over micro-batches).  Squares are summed in
- * fp32 over at most 64 elements of one thread and in double from there on, in an
- * order that depends on the block sizes only; values whose squares leave the
- * fp32 range are summed in double throughout, so the norm neither overflows nor
- * underflows before it is rounded to the fp32 outputs.  c is formed in double from the unrounded norm,
- * rounded to fp32, and each product is rounded once to fp32 and once more to a
- * bf16 destination.
+ * fp32 over at most 32 bf16 or 16 fp32 elements of one thread and in double from
+ * there on, in an order that depends on the block sizes and the type only; values
+ * whose squares leave the fp32 range are summed in double throughout, so the norm
+ * neither overflows nor underflows before it is rounded to the fp32 outputs.  c is
+ * formed in double from the unrounded norm, rounded to fp32, and each product is
+ * rounded once to fp32 and once more to a bf16 destination.
  * A NaN gradient makes n, c and every dst NaN; an infinite one makes n infinite
  * and c zero (its own dst is NaN, all others 0).  A zero gradient has c = 1 for
  * max_norm >= 1e-6. */

@@ -15,8 +15,8 @@
 namespace baoc {
 
 constexpr double kClipEps = 1e-6;
-// A thread's fp32 sum of up to 64 squares is taken as it is inside this range: no square has overflowed, and what
-// squares below the smallest fp32 number have lost is under 64 * 2^-150 of at least 1e-30.
+// A thread's fp32 sum of up to 32 squares (bf16; 16 of fp32) is taken as it is inside this range: no square has overflowed,
+// and what squares below the smallest fp32 number have lost is under 32 * 2^-150 of at least 1e-30.
 constexpr float kSquaresLo = 1e-30f, kSquaresHi = 1e30f;
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
