@@ -503,7 +503,9 @@ int baoc_check_selftest(baoc_stream_t stream);
 /* ---- gradient norm and clipping --------------------------------------------------
  * The paper has no counterpart of these two.  Language-model training clips the
  * gradient of all blocks by its global norm between the backward pass and
- * baoc_step; both calls work on the handle's block list.
+ * baoc_step; both calls work on the handle's block list, so n is the norm over the
+ * blocks of this handle alone: where a model's blocks are dealt to several handles
+ * (one per rank), baoc_clip_grads does not clip by the model's norm.
  *
  *   n_i = sqrt(sum of the squares of block i's gradient),  n = sqrt(sum_i n_i^2),
  *   dst_i = c * src_i  with  c = min(1, max_norm / (n + 1e-6)).

@@ -541,8 +541,8 @@ class Baoc:
 
     def clip_grads(self, grads, out, max_norm: float, norms: torch.Tensor, src_dtype: Optional[torch.dtype] = None,
                    dst_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
-        """``baoc_clip_grads``: the norms, then out_i = min(1, max_norm / (norms[0] + 1e-6)) * grads_i.  out None: in place.
-        Arrays as for ``grad_norm``; bf16 -> bf16, fp32 -> fp32 or fp32 -> bf16.  Returns norms."""
+        """``baoc_clip_grads``: the norms over this handle's blocks (not those of other ranks' handles), then
+        out_i = min(1, max_norm / (norms[0] + 1e-6)) * grads_i.  out None: in place.  Arrays as for ``grad_norm``; bf16 -> bf16, fp32 -> fp32 or fp32 -> bf16.  Returns norms."""
         dev = self._norms(norms)
         src, sc = self._clip_arrays(grads, src_dtype, dev, "clip_grads")
         dst, dc = (src, sc) if out is None else self._clip_arrays(out, dst_dtype, dev, "clip_grads")

@@ -207,7 +207,9 @@ class Session:
         self.state = new_state
 
     def clip_grads(self, k: int, max_norm: float) -> torch.Tensor:
-        """Clip gradient set k in place by its global norm; returns the norms before it (the global one, then every block's)."""
+        """Clip gradient set k in place by the norm over all of this session's blocks; returns the norms before it (that one, then
+        every block's).  Where the blocks of a model are dealt to ranks, each rank's session knows its own blocks only: the
+        ranks would clip by different norms, none of them the model's."""
         if self.clip_norms is None:
             if torch.cuda.is_current_stream_capturing():
                 raise B.BaocError(B.E_STATE, "clip_grads: the first call binds its workspace and cannot be captured")
