@@ -589,8 +589,8 @@ int baoc_embed_grad_workspace_bytes(const baoc_embed_t* e, int64_t n_tokens, siz
 /* dtable[vocab][dim] from dout[n_tokens][dim].  accumulate = 0 writes every row
  * (zero where no token named it); 1 adds to the rows that tokens named, formed in
  * fp32 and rounded once, and leaves the others (a tied output layer, or
- * micro-batches).  Sums are fp32, in an order that depends on the ids only: equal
- * inputs give equal bits.  ws: device, 256-byte aligned, >= the size above; its
+ * micro-batches).  Sums are fp32, in an order that depends on the ids, n_tokens,
+ * vocab, dim and dout's type only: equal calls give equal bits.  ws: device, 256-byte aligned, >= the size above; its
  * contents matter to no later call.  n_tokens <= 2^30.  dtable must overlap
  * neither dout nor ws.  Queues one kernel (few tokens) or two; does not wait.
  * Errors of the three: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_WORKSPACE,

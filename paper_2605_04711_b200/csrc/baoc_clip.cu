@@ -210,11 +210,12 @@ __device__ __forceinline__ void load8(const typename Vec<SRC>::Elem* p, uint4& a
 }
 
 // 1.14 G bf16 elements: 690 us behind the norm = 6.6 TB/s of one read and one write, the copy bandwidth; 124 M from fp32 to bf16:
-// 117 us = 6.4 TB/s.  Tiles of 16384 elements beat 4096 by 8 % there, and lose to it by 13 % at 2.4 M elements (12.7 against
-// 11.1 us for both kernels).  Policies that keep the norm's last bytes in L2 for this read, and orders that go with them, were
-// measured and make no difference.
+// 117 us = 6.4 TB/s.  Tiles of 4096 elements (both kernels, bf16): 9.0 us at 2 Mi elements against 9.8 with 16384, 10.3 against 12.2
+// at 4 Mi; from 8 Mi to 32 Mi = kClipSmallTotal the two stay within 4 % of one another, and above it 16384 leads: 71.4 against
+// 72.7 us at 64 Mi, 133 against 139 at 128 Mi (fp32 to bf16: 109 against 114 and 211 against 215).  Policies that keep the
+// norm's last bytes in L2 for this read, and orders that go with them, were measured and make no difference.
 //
-// dst = factor * src, one CTA per tile, the last tiles first.  All but the factor is there before the norm has ended: a CTA
+// dst = factor * src, one CTA per tile (last tiles first: any order takes the same time).  All but the factor is there before the norm has ended: a CTA
 // that finds a place by then has its first elements in hand when the factor comes.
 template <int SRC, int DST>
 __global__ void __launch_bounds__(kThreads)

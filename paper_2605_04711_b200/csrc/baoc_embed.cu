@@ -231,10 +231,13 @@ __host__ __device__ __forceinline__ int chunk_tokens(int count) {
 __host__ __device__ __forceinline__ int chunks_of(int count, int len) { return int((int64_t(count) + len / 2) / len); }
 
 // ---- gradient, first kernel: group the tokens by id -----------------------------------------------------------------
-// Bound by instructions and latency, not by bytes (the ids come from L2): 6 us for 16384 tokens, 8 us for 65536, 11 us for
-// 131072 (ncu: issue slots half busy, DRAM idle).  Reading the ids by every class instead of sorting in passes over the GPU
-// saves the grid-wide steps in between; a cluster of four shares the reading from kSplitTokens tokens on (65536: 8 us against 11,
-// 131072: 11 against 17; at 16384 the exchange costs what it saves), clusters of eight do not all find room at once (+ 18 us).
+// Bound by instructions and latency, not by bytes (the ids come from L2): this kernel alone, launches in a row, takes 7.2 us
+// for 16384 tokens, 11.3 us for 65536, 16.2 us for 131072 (ncu: issue slots half busy, DRAM idle).  Reading the ids by every
+// class instead of sorting in passes over the GPU saves the grid-wide steps in between; a cluster of four shares the reading
+// from kSplitTokens tokens on (8192: 7.4 us against 5.8 without, 16384: 7.7 against 7.2, 24576: 8.3 against 9.5, 32768: 9.0
+// against 10.3, 65536: 11.3 against 15.3, 131072: 16.2 against 25.1), clusters of eight do not all find room at once (+ 18 us).
+// These hold up to 128 * kGroupBins = 98304 rows (16384 tokens: 7.9 us there).  Beyond, the classes double and no longer run
+// all at once: 16384 tokens into 128256 rows 12.5 us, into 256000 rows 22.1; 65536 tokens 18.5 and 32.8 (12.0 at 98304).
 // The ids fall into 2^shift classes by their low bits; CTA c lists the tokens of class c, grouped by id.  Every CTA reads
 // all ids and counts those of lower classes too, which is where its part of the order begins: no CTA waits for another,
 // nothing is left to chance, and frequent neighbouring ids fall into different classes.
@@ -556,7 +559,7 @@ __device__ __forceinline__ void write_row(char* p, int col, const float (&sum)[V
 }
 
 // The sums move all of the bytes.  65536 tokens x 2048 of bf16 into 32000 rows, ids uniform: 66 us for 400 MB = 6.1 TB/s, at the
-// copy bandwidth; Zipf-like ids with a tenth padding: 67 us for 373 MB; 16384 x 768 into 50257 rows: 22 us for 102 MB, two
+// copy bandwidth; Zipf-like ids with a tenth padding: 67 us for 373 MB; 16384 x 768 into 50257 rows: 24 us for 102 MB, two
 // waves of warps whose start and end weigh.  A warp per row took 1558 us (a frequent row is one warp's work), rows without
 // regard to their tokens 82 us more than segments of equal rows + tokens.  Segments end where rows do, so only long rows need
 // partial sums; those of 32 tokens a chunk cost 1/8 of their tokens' bytes in L2.
