@@ -600,6 +600,53 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
                     int accumulate, void* ws, size_t ws_bytes, baoc_stream_t stream);
 const char* baoc_embed_last_error(void);
 
+/* ---- log probabilities of given tokens --------------------------------------------
+ * The paper has no counterpart of these.  A language model answers with a row of
+ * logits x per token; training wants the log probability of the token that follows,
+ * a server also the row's entropy and its most probable tokens.  With
+ * t_j = scale (x_j - max x), S = sum_j e^t_j, p_j = e^t_j / S, i = ids[row]:
+ *
+ *   logp = t_i - log S
+ *   H    = -sum_j p_j log p_j
+ *   dx_j = scale (g ([j = i] - p_j) - h p_j (log p_j + H)),  g and h the gradients of logp and H
+ *
+ * An id outside [0, vocab) marks an ignored position: its logits are not read, its
+ * logp, entropy, statistics and gradients are zero, its most probable tokens -1.
+ * A logit of -inf is a token that cannot follow (p = 0; logp -inf where it is the
+ * given one).  A row of nothing else has logp -inf, entropy zero and no gradient.
+ * A row with a NaN or an infinite logit gives NaN everywhere but in top_ids, where
+ * NaN is the largest value.  Handle-free, without a workspace. */
+typedef struct {
+    int64_t vocab;               /* logits of a row, 1 .. 2^31 - 1 */
+    int32_t dtype;               /* of logits and dlogits: BAOC_F32 or BAOC_BF16 */
+    int32_t id_bits;             /* 32 or 64: signed token ids */
+    float scale;                 /* 1 / temperature: finite, > 0 */
+    int32_t top;                 /* most probable tokens wanted: 0 .. 32, at most vocab */
+    int64_t stride;              /* elements from row to row of logits: vocab .. 2^32, 0 for vocab */
+    int64_t grad_stride;         /* the same of dlogits */
+} baoc_logp_t;
+
+/* logp[n_tokens], entropy[n_tokens]; stats[n_tokens][3]: the row's largest logit,
+ * log S and H, which baoc_logp_grad takes; top_ids and top_logp [n_tokens][top]
+ * (NULL for top = 0): the row's most probable tokens in falling order, the lower
+ * token first where logits are equal, and their log probabilities.  Sums are fp32,
+ * in an order that depends on n_tokens, vocab, dtype and the row's alignment only.
+ * Pointers are aligned to their elements.  n_tokens <= 2^31 - 1, 0 queues nothing.
+ * One kernel; does not wait. */
+int baoc_logp(const baoc_logp_t* e, const void* logits, const void* ids, int64_t n_tokens, float* logp, float* entropy,
+              float* stats, int32_t* top_ids, float* top_logp, baoc_stream_t stream);
+
+/* dlogits[n_tokens][vocab] from dlogp[n_tokens] and dentropy[n_tokens] (NULL: the
+ * entropy takes no gradient).  ids, scale and logits as in the call that wrote
+ * stats; top is not read beyond its check.  dlogits may be logits itself, with the
+ * same row stride (the logits are gone then), and overlaps it in no other way.
+ * Logits and dlogits that lie alike to 16 bytes take the wide path.  One kernel;
+ * does not wait.  Errors of both: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_CUDA;
+ * baoc_logp_last_error() returns the message of the calling thread's last failure. */
+int baoc_logp_grad(const baoc_logp_t* e, const void* logits, const void* ids, const float* stats, const float* dlogp,
+                   const float* dentropy, int64_t n_tokens, void* dlogits, baoc_stream_t stream);
+const char* baoc_logp_last_error(void);
+
 /* ---- allocation-free variant ------------------------------------------------ */
 
 /* Largest block baoc_sample_stats_noalloc accepts (64 Mi elements).  The

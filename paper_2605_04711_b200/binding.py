@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence, Union
 
 import numpy as np
 import torch
@@ -84,6 +84,11 @@ class Embed(C.Structure):
                 ("table_stride", C.c_int64), ("act_stride", C.c_int64), ("grad_stride", C.c_int64)]
 
 
+class Logp(C.Structure):
+    _fields_ = [("vocab", C.c_int64), ("dtype", C.c_int32), ("id_bits", C.c_int32), ("scale", C.c_float), ("top", C.c_int32),
+                ("stride", C.c_int64), ("grad_stride", C.c_int64)]
+
+
 class Info(C.Structure):
     _fields_ = [("n_blocks", C.c_int32), ("n_cfg", C.c_int32), ("numel", C.c_int64), ("n_tiles", C.c_int64),
                 ("stats_steps", C.c_int64), ("state_bytes", C.c_int64), ("kernel_launches", C.c_int64),
@@ -99,7 +104,8 @@ EXPORTS = ["baoc_default_opts", "baoc_create", "baoc_destroy", "baoc_last_error"
            "baoc_set_sampling", "baoc_reconfigure", "baoc_configure_from_window", "baoc_partition",
            "baoc_set_factored_schedule", "baoc_check_status", "baoc_check_selftest",
            "baoc_clip_workspace_bytes", "baoc_bind_clip_workspace", "baoc_grad_norm", "baoc_clip_grads",
-           "baoc_embed", "baoc_embed_grad_workspace_bytes", "baoc_embed_grad", "baoc_embed_last_error"]
+           "baoc_embed", "baoc_embed_grad_workspace_bytes", "baoc_embed_grad", "baoc_embed_last_error",
+           "baoc_logp", "baoc_logp_grad", "baoc_logp_last_error"]
 
 _vp = C.c_void_p
 _lib.baoc_default_opts.argtypes = [C.POINTER(Opts)]
@@ -150,6 +156,10 @@ _lib.baoc_embed_grad_workspace_bytes.argtypes = [_vp, C.c_int64, C.POINTER(C.c_s
 _lib.baoc_embed_grad.argtypes = [_vp, _vp, _vp, C.c_int64, _vp, C.c_int, _vp, C.c_size_t, _vp]
 _lib.baoc_embed_last_error.argtypes = []
 _lib.baoc_embed_last_error.restype = C.c_char_p
+_lib.baoc_logp.argtypes = [_vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.baoc_logp_grad.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, C.c_int64, _vp, _vp]
+_lib.baoc_logp_last_error.argtypes = []
+_lib.baoc_logp_last_error.restype = C.c_char_p
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}              # BAOC_BF16, BAOC_F32
 
 
@@ -389,6 +399,97 @@ class Embedding:
         rc = _queue(dev, _lib.baoc_embed_grad, self._ref, ids.data_ptr(), dout.data_ptr(), n, dtable.data_ptr(), 1 if accumulate else 0,
                     ws.data_ptr(), ws.numel() * ws.element_size())
         return dtable if rc >= 0 else self._failed(rc)
+
+
+class TokenLogProbs(NamedTuple):
+    """What ``LogProbs.logprobs`` returns; top_ids and top_logp are None for a plan without alternatives."""
+    logp: torch.Tensor                       # fp32, ids' shape
+    entropy: torch.Tensor                    # fp32, ids' shape
+    stats: torch.Tensor                      # fp32, ids' shape + [3]: largest logit, log of the sum, entropy (for ``grad``)
+    top_ids: Optional[torch.Tensor]          # int32, ids' shape + [top]
+    top_logp: Optional[torch.Tensor]         # fp32, ids' shape + [top]
+
+
+class LogProbs:
+    """Log probabilities of given tokens with entropy and most probable tokens (``baoc_logp``) and the logits' gradient
+    (``baoc_logp_grad``): a plan of one vocabulary.
+
+    scale (1 / temperature) multiplies every logit; ids outside [0, vocab) are ignored positions; top: how many of the most
+    probable tokens every row returns (0 to 32).  Calls queue work on the current stream of the tensors' device.  Like a
+    handle, a plan serves one thread at a time."""
+
+    def __init__(self, vocab: int, scale: float = 1.0, top: int = 0):
+        self.vocab, self.top = int(vocab), int(top)
+        self._e = Logp(self.vocab, DTYPES[torch.bfloat16], 64, float(scale), max(-1, min(self.top, 2 ** 31 - 1)), 0, 0)
+        self._ref = C.byref(self._e)
+        self._form = None
+        if _lib.baoc_logp(self._ref, None, None, 0, None, None, None, None, None, None) < 0:     # the descriptor's checks
+            raise BaocError(E_INVALID, _lib.baoc_logp_last_error().decode())
+
+    def buffers(self, n: Union[int, Sequence[int]], device) -> TokenLogProbs:
+        """Output buffers for n rows (or rows of that shape), to be kept and handed to ``logprobs``."""
+        shape = (n,) if isinstance(n, int) else tuple(n)
+        new = lambda *more, dtype=torch.float32: torch.empty((*shape, *more), dtype=dtype, device=device)
+        top = (new(self.top, dtype=torch.int32), new(self.top)) if self.top else (None, None)
+        return TokenLogProbs(new(), new(), new(3), *top)
+
+    def _call(self, what: str, logits, ids, dlogits, floats):
+        """Checks shapes and devices and fills the descriptor; returns (device, rows, ids)."""
+        n, dev = ids.numel(), logits.get_device()
+        rows, stride = _rows(logits, self.vocab, "logits")
+        grad_rows, grad_stride = (n, 0) if dlogits is None else _rows(dlogits, self.vocab, "dlogits")
+        if rows != n or grad_rows != n or dev < 0 or ids.get_device() != dev or (dlogits is not None and dlogits.get_device() != dev):
+            raise BaocError(E_INVALID, f"{what}: one row of {self.vocab} logits per id, all on one CUDA device")
+        for t, size in floats:
+            if t is not None and (t.dtype != torch.float32 or t.numel() != size or not t.is_contiguous() or t.get_device() != dev):
+                raise BaocError(E_INVALID, f"{what}: contiguous float32 arrays of one value per id (three in stats, `top` in top_logp) on the logits' device")
+        if ids.dim() != 1 and logits.dim() != 2 and logits.shape[:-1] != ids.shape:
+            raise BaocError(E_INVALID, f"{what}: logits must be of ids' shape + [{self.vocab}], not {list(logits.shape)} for {list(ids.shape)}")
+        form = (logits.dtype, ids.dtype, stride, grad_stride)
+        if form != self._form:
+            if ids.dtype not in _ID_BITS or (dlogits is not None and dlogits.dtype != logits.dtype):
+                raise BaocError(E_INVALID, f"{what}: ids of int32 or int64, and dlogits of the logits' type")
+            self._form = None
+            self._e.dtype, self._e.id_bits, self._e.stride, self._e.grad_stride = _dtype_code(logits.dtype), _ID_BITS[ids.dtype], stride, grad_stride
+            self._form = form
+        return dev, n, ids if ids.is_contiguous() else ids.contiguous()
+
+    def _failed(self, rc: int):
+        """Raises, and leaves no stride of the refused arrays in the descriptor."""
+        self._form = None
+        self._e.stride = self._e.grad_stride = 0
+        raise BaocError(rc, _lib.baoc_logp_last_error().decode())
+
+    def logprobs(self, logits: torch.Tensor, ids: torch.Tensor, out: Optional[TokenLogProbs] = None) -> TokenLogProbs:
+        """Log probability of ids[...] under logits[..., :], entropy and most probable tokens of every row.  logits: [..., vocab]
+        bf16 or fp32, rows may be strided; ids: int32 or int64 (a non-contiguous one is copied first); out: from ``buffers``
+        (allocated when not given).  The outputs carry no autograd history: logits that require a gradient are refused unless
+        they are detached or gradients are off (``grad`` is the gradient)."""
+        if logits.requires_grad and torch.is_grad_enabled():
+            raise BaocError(E_INVALID, "logprobs: autograd does not see this call; detach the logits, or call it under torch.no_grad()")
+        if out is None:
+            out = self.buffers(ids.shape, logits.device)
+        n, k = ids.numel(), self.top
+        if k and (out.top_ids is None or out.top_ids.dtype != torch.int32 or out.top_ids.numel() != n * k or not out.top_ids.is_contiguous()
+                  or out.top_ids.get_device() != logits.get_device() or out.top_logp is None):
+            raise BaocError(E_INVALID, "logprobs: top_ids must be a contiguous int32 array of `top` tokens per id on the logits' device")
+        dev, n, ids = self._call("logprobs", logits, ids, None, ((out.logp, n), (out.entropy, n), (out.stats, 3 * n), (out.top_logp if k else None, n * k)))
+        rc = _queue(dev, _lib.baoc_logp, self._ref, logits.data_ptr(), ids.data_ptr(), n, out.logp.data_ptr(), out.entropy.data_ptr(),
+                    out.stats.data_ptr(), out.top_ids.data_ptr() if k else None, out.top_logp.data_ptr() if k else None)
+        return out if rc >= 0 else self._failed(rc)
+
+    def grad(self, logits: torch.Tensor, ids: torch.Tensor, stats: torch.Tensor, dlogp: torch.Tensor, dentropy: Optional[torch.Tensor] = None,
+             dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The logits' gradient from those of logp and (None: zero) of the entropy, fp32 and of ids' shape; stats from
+        ``logprobs`` of the same logits and ids.  dlogits: of the logits' type (allocated when not given); it may be the logits
+        themselves, which are overwritten then."""
+        if dlogits is None:
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        n = ids.numel()
+        dev, n, ids = self._call("grad", logits, ids, dlogits, ((stats, 3 * n), (dlogp, n), (dentropy, n)))
+        rc = _queue(dev, _lib.baoc_logp_grad, self._ref, logits.data_ptr(), ids.data_ptr(), stats.data_ptr(), dlogp.data_ptr(),
+                    None if dentropy is None else dentropy.data_ptr(), n, dlogits.data_ptr())
+        return dlogits if rc >= 0 else self._failed(rc)
 
 
 class Baoc:

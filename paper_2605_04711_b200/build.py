@@ -9,6 +9,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -16,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbaoc.so")
 LIB_CHECKED = os.path.join(HERE, "libbaoc_checked.so")     # the same sources with -DBAOC_CHECKED (see csrc/baoc_check.cuh)
 SOURCES = ["baoc_host.cpp", "baoc_partition.cpp", "baoc_api.cu", "baoc_stats.cu", "baoc_finalize.cu", "baoc_step.cu", "baoc_noalloc.cu",
-           "baoc_convert.cu", "baoc_clip.cu", "baoc_embed.cu"]
+           "baoc_convert.cu", "baoc_clip.cu", "baoc_embed.cu", "baoc_logp.cu"]
 HEADERS = [os.path.join(ROOT, "include", "baoc.h"), os.path.join(CSRC, "baoc_internal.h"),
            os.path.join(CSRC, "baoc_device.cuh"), os.path.join(CSRC, "baoc_check.cuh")]
 
@@ -49,15 +50,18 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     cuda_flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo"]
     if verbose:
         cuda_flags += ["-Xptxas", "-v"]
-    objs = []
-    for src in SOURCES:
+
+    def compile_one(src: str) -> str:
         obj = os.path.join(bdir, src + ".o")
         cmd = [nvcc] + common + (cuda_flags if src.endswith(".cu") else []) + \
               ["-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
-        objs.append(obj)
+        return obj
+
+    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:    # (one nvcc per source, side by side)
+        objs = list(pool.map(compile_one, SOURCES))
     subprocess.run([nvcc, "-shared", "-Wno-deprecated-gpu-targets", "-o", lib] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"], check=True)
     return lib
 
