@@ -485,7 +485,7 @@ int baoc_profile_last(baoc_t* h, float* ms2);
  * gather, 4 first finalize sweep, 5 later sweeps, 6 / 7 row-column reduction of
  * the window / of the step, 8 its combine, 9 fused step, 10 the self-test, 11 the norms of the
  * factored tuple's Adafactor options, 14 / 15 gradient norm / clip, 16 / 17 grouping / sums of the
- * token table's gradient.
+ * token table's gradient, 18 the join's gradient.
  *
  * baoc_check_selftest: queues a one-thread kernel that runs the range check on
  * numbers that violate it (a 32-byte range that starts 16 bytes before the end
@@ -599,6 +599,64 @@ int baoc_embed_grad_workspace_bytes(const baoc_embed_t* e, int64_t n_tokens, siz
 int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, int64_t n_tokens, void* dtable,
                     int accumulate, void* ws, size_t ws_bytes, baoc_stream_t stream);
 const char* baoc_embed_last_error(void);
+
+/* ---- norms around a block's join -----------------------------------------------------
+ * The paper has no counterpart of these.  Between two blocks of a language model the
+ * branch f of the one joins the residual stream x, and the other's input is normed:
+ *
+ *   y = scale x + gate * post(f),   h = pre(y)
+ *
+ * pre and post are RMS norms, n(v) = v / sqrt(mean(v^2) + eps) times a weight per
+ * column, or layer norms: n(v - mean(v)) times a weight plus a bias.  No post_w: f
+ * joins as it is.  gate (NULL: 1) is one vector for all rows, or one for every
+ * rows_per_gate rows in order (per sequence, say).  x NULL: nothing to join, y is the
+ * branch (a model's first norm).  All arithmetic is fp32; each output is rounded once,
+ * h comes from the unrounded y.  Weights, biases and gates are fp32, contiguous.
+ * Handle-free. */
+enum { BAOC_NORM_RMS = 0, BAOC_NORM_LAYER = 1 };
+typedef struct {
+    int32_t dim;                 /* columns, 1 .. 8192 */
+    int32_t kind;                /* BAOC_NORM_RMS or BAOC_NORM_LAYER, both norms */
+    int32_t stream_dtype;        /* of x, y, dx, dy: BAOC_F32 or BAOC_BF16 */
+    int32_t branch_dtype;        /* of f, h, df, dh; an fp32 branch needs an fp32 stream */
+    int32_t grad_dtype;          /* of the weights', biases' and gate's gradients */
+    float eps;                   /* finite, > 0 */
+    float scale;                 /* of the stream: finite */
+    int32_t reserved;
+    int64_t rows_per_gate;       /* 0: one gate for all rows */
+    int64_t x_stride, f_stride, y_stride, h_stride;        /* elements from row to row: dim .. 2^28, 0 for dim */
+    int64_t dx_stride, df_stride, dy_stride, dh_stride;    /* (baoc_join_grad alone) */
+} baoc_join_t;
+
+/* y[rows][dim] and h[rows][dim].  y may be x and h may be f (same pointer, type and
+ * row stride); arrays overlap in no other way.  Pointers are aligned to their
+ * elements; a dim that is a multiple of 8 in arrays whose bases and row strides are
+ * multiples of 16 bytes takes the wide path.  rows <= 2^31, 0 queues nothing.  One
+ * kernel; does not wait. */
+int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* post_w, const float* post_b, const float* gate,
+              const float* pre_w, const float* pre_b, int64_t rows, void* y, void* h, baoc_stream_t stream);
+
+/* Bytes of device workspace baoc_join_grad needs for so many rows at most; it serves
+ * every smaller number of rows of the descriptor's dim too. */
+int baoc_join_grad_workspace_bytes(const baoc_join_t* e, int64_t rows, size_t* bytes);
+
+/* Gradients from dh and dy (what reaches y by other ways; NULL: nothing):
+ *
+ *   Dy = dy + pre's gradient,  dx = scale Dy,  dgate = sum of Dy * post(f) over the gate's rows,  df = post's gradient of gate * Dy
+ *
+ * y: as baoc_join wrote it; f: not read without post_w and gate.  dx (NULL: not
+ * wanted) may be dy, df may be dh; outputs overlap nothing else.  dpost_w, dpost_b,
+ * dpre_w, dpre_b [dim] and dgate [gates][dim] are contiguous, of grad_dtype, each NULL
+ * where it is not wanted, and are written, not added to.  Sums over rows are fp32, in
+ * an order that depends on the descriptor, rows and alignment only: equal calls give
+ * equal bits.  ws: device, 256-byte aligned; its contents matter to no later call.
+ * Queues two kernels; does not wait.  Errors: BAOC_E_INVALID, BAOC_E_ALIGN,
+ * BAOC_E_WORKSPACE, BAOC_E_CUDA; baoc_join_last_error() returns the message of the
+ * calling thread's last failure. */
+int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const void* dy, const void* dh, const float* post_w,
+                   const float* post_b, const float* gate, const float* pre_w, int64_t rows, void* dx, void* df, void* dpost_w,
+                   void* dpost_b, void* dgate, void* dpre_w, void* dpre_b, void* ws, size_t ws_bytes, baoc_stream_t stream);
+const char* baoc_join_last_error(void);
 
 /* ---- log probabilities of given tokens --------------------------------------------
  * The paper has no counterpart of these.  A language model answers with a row of

@@ -89,6 +89,13 @@ class Logp(C.Structure):
                 ("stride", C.c_int64), ("grad_stride", C.c_int64)]
 
 
+class JoinForm(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("kind", C.c_int32), ("stream_dtype", C.c_int32), ("branch_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("eps", C.c_float), ("scale", C.c_float), ("reserved", C.c_int32),
+                ("rows_per_gate", C.c_int64)] + \
+               [(n + "_stride", C.c_int64) for n in ("x", "f", "y", "h", "dx", "df", "dy", "dh")]
+
+
 class Info(C.Structure):
     _fields_ = [("n_blocks", C.c_int32), ("n_cfg", C.c_int32), ("numel", C.c_int64), ("n_tiles", C.c_int64),
                 ("stats_steps", C.c_int64), ("state_bytes", C.c_int64), ("kernel_launches", C.c_int64),
@@ -105,7 +112,8 @@ EXPORTS = ["baoc_default_opts", "baoc_create", "baoc_destroy", "baoc_last_error"
            "baoc_set_factored_schedule", "baoc_check_status", "baoc_check_selftest",
            "baoc_clip_workspace_bytes", "baoc_bind_clip_workspace", "baoc_grad_norm", "baoc_clip_grads",
            "baoc_embed", "baoc_embed_grad_workspace_bytes", "baoc_embed_grad", "baoc_embed_last_error",
-           "baoc_logp", "baoc_logp_grad", "baoc_logp_last_error"]
+           "baoc_logp", "baoc_logp_grad", "baoc_logp_last_error",
+           "baoc_join", "baoc_join_grad_workspace_bytes", "baoc_join_grad", "baoc_join_last_error"]
 
 _vp = C.c_void_p
 _lib.baoc_default_opts.argtypes = [C.POINTER(Opts)]
@@ -160,6 +168,11 @@ _lib.baoc_logp.argtypes = [_vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, _vp, _v
 _lib.baoc_logp_grad.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, C.c_int64, _vp, _vp]
 _lib.baoc_logp_last_error.argtypes = []
 _lib.baoc_logp_last_error.restype = C.c_char_p
+_lib.baoc_join.argtypes = [_vp] * 8 + [C.c_int64] + [_vp] * 3
+_lib.baoc_join_grad_workspace_bytes.argtypes = [_vp, C.c_int64, C.POINTER(C.c_size_t)]
+_lib.baoc_join_grad.argtypes = [_vp] * 9 + [C.c_int64] + [_vp] * 8 + [C.c_size_t, _vp]
+_lib.baoc_join_last_error.argtypes = []
+_lib.baoc_join_last_error.restype = C.c_char_p
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}              # BAOC_BF16, BAOC_F32
 
 
@@ -399,6 +412,114 @@ class Embedding:
         rc = _queue(dev, _lib.baoc_embed_grad, self._ref, ids.data_ptr(), dout.data_ptr(), n, dtable.data_ptr(), 1 if accumulate else 0,
                     ws.data_ptr(), ws.numel() * ws.element_size())
         return dtable if rc >= 0 else self._failed(rc)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+class Join:
+    """The norms around a block's join (``baoc_join``) and their gradient (``baoc_join_grad``): a plan of one width.
+
+        y = scale * x + gate * post(f),   h = pre(y)
+
+    kind: "rms" (a weight each) or "layer" (a weight and a bias each).  x, y and their gradients are of one type (the stream:
+    fp32 or bf16), f, h and theirs of another (the branch: bf16, or fp32 on an fp32 stream); weights, biases and gates are fp32.
+    gate: [dim], or [gates, dim] for as many groups of equally many rows, in order.  Calls queue work on the current stream of
+    the tensors' device; autograd does not see them.  Like a handle, a plan serves one thread at a time."""
+
+    def __init__(self, dim: int, kind: str = "rms", eps: float = 1e-6, scale: float = 1.0):
+        if kind not in ("rms", "layer"):
+            raise BaocError(E_INVALID, f"kind must be \"rms\" or \"layer\", not {kind!r}")
+        self.dim, self.kind = int(dim), kind
+        self._e = JoinForm(max(-1, min(self.dim, 2 ** 31 - 1)), 1 if kind == "layer" else 0, 0, 0, 0, float(eps), float(scale), 0, 0)
+        self._ref, self._n = C.byref(self._e), C.c_size_t()
+        self.grad_workspace_bytes(0)                        # the descriptor's checks
+
+    def _failed(self, rc: int):
+        raise BaocError(rc, _lib.baoc_join_last_error().decode())
+
+    def _take(self, what: str, f, stream, branch, vectors, gate, dgate):
+        """Checks the arrays against one another and fills the descriptor.  stream, branch: {field: tensor or None}."""
+        dim, e = self.dim, self._e
+        n = dev = None
+        for arrays, field in ((stream, "stream_dtype"), (branch, "branch_dtype")):
+            dtype = None
+            for name, t in arrays.items():
+                if t is None:
+                    continue
+                if t.requires_grad and torch.is_grad_enabled():
+                    raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach {name}, or call it under torch.no_grad()")
+                rows, stride = _rows(t, dim, name)
+                n, dev, dtype = rows if n is None else n, t.get_device() if dev is None else dev, dtype or t.dtype
+                if rows != n or t.get_device() != dev or dev < 0 or t.dtype != dtype:
+                    raise BaocError(E_INVALID, f"{what}: arrays of equally many rows on one CUDA device, x, y, dx, dy of one type and f, h, df, dh of one type")
+                setattr(e, name + "_stride", stride)
+            setattr(e, field, _dtype_code(dtype))
+        for t in vectors:
+            if t is not None and (t.dtype != torch.float32 or t.numel() != dim or not t.is_contiguous() or t.get_device() != dev):
+                raise BaocError(E_INVALID, f"{what}: weights and biases are contiguous float32 vectors of {dim} elements on the device of the others")
+            if t is not None and t.requires_grad and torch.is_grad_enabled():
+                raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach the weights, or call it under torch.no_grad()")
+        e.rows_per_gate = 0
+        if gate is not None:
+            gates = gate.numel() // dim
+            if gate.dtype != torch.float32 or gate.size(-1) != dim or not gate.is_contiguous() or gate.get_device() != dev or gates < 1 or n % gates:
+                raise BaocError(E_INVALID, f"{what}: gate must be a contiguous float32 [{dim}] or [gates, {dim}] with equally many rows each, on the device of the others")
+            if gate.requires_grad and torch.is_grad_enabled():
+                raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach the gate, or call it under torch.no_grad()")
+            e.rows_per_gate = n // gates if gates > 1 else 0
+        if dgate is not None and (gate is None or dgate.numel() != gate.numel()):
+            raise BaocError(E_INVALID, f"{what}: dgate must be of gate's shape")
+        return n, dev
+
+    def join(self, x: Optional[torch.Tensor], f: torch.Tensor, pre_w: torch.Tensor, pre_b: Optional[torch.Tensor] = None,
+             post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+             y: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None):
+        """Returns (y, h), allocated when not given (y of x's type, or of y's own without x: fp32).  Rows [..., dim] may be
+        strided.  x None: nothing to join; post_w None: the branch joins as it is.  y may be x, h may be f."""
+        if y is None:
+            y = torch.empty(f.shape, dtype=torch.float32 if x is None else x.dtype, device=f.device)
+        if h is None:
+            h = torch.empty(f.shape, dtype=f.dtype, device=f.device)
+        n, dev = self._take("join", f, {"x": x, "y": y}, {"f": f, "h": h}, (pre_w, pre_b, post_w, post_b), gate, None)
+        rc = _queue(dev, _lib.baoc_join, self._ref, _ptr(x), f.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate), pre_w.data_ptr(), _ptr(pre_b),
+                    n, y.data_ptr(), h.data_ptr())
+        return (y, h) if rc >= 0 else self._failed(rc)
+
+    def grad_workspace_bytes(self, rows: int) -> int:
+        rc = _lib.baoc_join_grad_workspace_bytes(self._ref, int(rows), C.byref(self._n))
+        return self._n.value if rc >= 0 else self._failed(rc)
+
+    def grad(self, y: torch.Tensor, f: Optional[torch.Tensor], dh: torch.Tensor, pre_w: torch.Tensor, dy: Optional[torch.Tensor] = None,
+             post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+             dx: Optional[torch.Tensor] = None, df: Optional[torch.Tensor] = None, dpre_w: Optional[torch.Tensor] = None,
+             dpre_b: Optional[torch.Tensor] = None, dpost_w: Optional[torch.Tensor] = None, dpost_b: Optional[torch.Tensor] = None,
+             dgate: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, want_dx: bool = True):
+        """Returns (dx, df), allocated when not given (want_dx False: no dx, as for a join without x).  y: what ``join``
+        returned; f: its branch (None where neither post_w nor gate was given); dy: what reaches y by other ways.  dpre_w, dpre_b,
+        dpost_w, dpost_b and dgate, all bf16 or all fp32, are written where given.  dx may be dy, df may be dh.  ws: device bytes,
+        at least ``grad_workspace_bytes(rows)`` (allocated when not given)."""
+        if dx is None and want_dx:
+            dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        if df is None:
+            df = torch.empty(dh.shape, dtype=dh.dtype, device=dh.device)
+        n, dev = self._take("grad", f, {"y": y, "dy": dy, "dx": dx}, {"dh": dh, "f": f, "df": df}, (pre_w, post_w, post_b), gate, dgate)
+        dtype = None
+        for t in (dpre_w, dpre_b, dpost_w, dpost_b, dgate):
+            if t is not None:
+                dtype = dtype or t.dtype
+                if t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev or (t is not dgate and t.numel() != self.dim):
+                    raise BaocError(E_INVALID, f"grad: gradients of weights, biases and gate are contiguous, of one type, on the device of the others, of {self.dim} elements")
+        self._e.grad_dtype = _dtype_code(dtype or torch.float32)
+        if ws is None:
+            ws = torch.empty(self.grad_workspace_bytes(n), dtype=torch.uint8, device=y.device)
+        elif ws.get_device() != dev or not ws.is_contiguous():
+            raise BaocError(E_INVALID, "grad: ws must be a contiguous buffer on the device of the others")
+        rc = _queue(dev, _lib.baoc_join_grad, self._ref, y.data_ptr(), _ptr(f), _ptr(dy), dh.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate),
+                    pre_w.data_ptr(), n, _ptr(dx), df.data_ptr(), _ptr(dpost_w), _ptr(dpost_b), _ptr(dgate), _ptr(dpre_w), _ptr(dpre_b),
+                    ws.data_ptr(), ws.numel() * ws.element_size())
+        return (dx, df) if rc >= 0 else self._failed(rc)
 
 
 class TokenLogProbs(NamedTuple):

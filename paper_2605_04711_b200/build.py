@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbaoc.so")
 LIB_CHECKED = os.path.join(HERE, "libbaoc_checked.so")     # the same sources with -DBAOC_CHECKED (see csrc/baoc_check.cuh)
 SOURCES = ["baoc_host.cpp", "baoc_partition.cpp", "baoc_api.cu", "baoc_stats.cu", "baoc_finalize.cu", "baoc_step.cu", "baoc_noalloc.cu",
-           "baoc_convert.cu", "baoc_clip.cu", "baoc_embed.cu", "baoc_logp.cu"]
+           "baoc_convert.cu", "baoc_clip.cu", "baoc_embed.cu", "baoc_logp.cu", "baoc_join.cu"]
 HEADERS = [os.path.join(ROOT, "include", "baoc.h"), os.path.join(CSRC, "baoc_internal.h"),
            os.path.join(CSRC, "baoc_device.cuh"), os.path.join(CSRC, "baoc_check.cuh")]
 
@@ -53,6 +53,8 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
 
     def compile_one(src: str) -> str:
         obj = os.path.join(bdir, src + ".o")
+        if not force and os.path.exists(obj) and os.path.getmtime(obj) > max(os.path.getmtime(d) for d in [os.path.join(CSRC, src)] + HEADERS):
+            return obj                                     # (only its own source or a header can have changed it)
         cmd = [nvcc] + common + (cuda_flags if src.endswith(".cu") else []) + \
               ["-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:

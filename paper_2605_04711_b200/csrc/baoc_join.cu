@@ -1,0 +1,714 @@
+// The join of a block's branch into the residual stream, with the norm behind the branch and the norm before the next block.
+//
+//   y = c x + g * post(f),   h = pre(y)
+//
+// post and pre are an RMS norm (n(v) = v / sqrt(mean(v^2) + eps)) or a layer norm (the same of v - mean(v)), each with a weight
+// and, for layer norms, a bias per column; g is nothing, a vector or a vector per group of rows.  Backwards, with
+// n = n(v) and r = 1 / sqrt(..) of a norm, dn = dout * w:
+//
+//   dv = r (dn - n mean(dn n) [- mean(dn) for a layer norm]),  dw = sum over rows of dout * n,  db = sum over rows of dout
+//   Dy = dy + (dv of pre, from dh),  dx = c Dy,  du = g * Dy,  dg = sum over the group's rows of Dy * post(f),  df = (dv of post, from du)
+//
+// Memory bounds both ways: x and f in, y and h out; y, f, dy and dh in, dx and df out, and nothing else moves but the column
+// sums.  A row lies in the registers of its threads (a team: 8 columns each) from its load to its store, so statistics need no
+// second pass, and the mean is taken out before the squares are summed.  The gradient's column sums stay with the team's threads
+// over all rows of a CTA; the CTAs' sums are joined by a second kernel in a fixed order.  All arithmetic is fp32; y, h, dx and df
+// are rounded once, and h comes from the unrounded y.
+// Times below: one B200, device time per call in a row of calls on three sets of arrays.
+#include <algorithm>
+#include <cmath>
+#include <cuda_runtime.h>
+#include <new>
+#include <string>
+
+#include "baoc_device.cuh"
+
+namespace baoc {
+
+constexpr int kJoinMaxDim = 8192;
+constexpr int64_t kJoinMaxStride = int64_t(1) << 28;
+constexpr int kJoinCols = 8;                   // columns of a thread
+constexpr int kJoinSmThreads = 1024;           // threads of the gradient's CTAs per SM
+constexpr int kJoinSums = 5;                   // column sums of the gradient: weight and bias of pre, of post, and the gate
+
+__host__ __device__ constexpr int join_cta(int team) { return team > 256 ? team : 256; }
+
+template <int DT, int kTeam, bool kWide>
+struct RowPart {
+    // a thread's columns: 8 neighbours, or 8 that are kTeam apart
+    static constexpr int kSize = DT == BAOC_BF16 ? 2 : 4;
+    static constexpr int kWords = kWide ? 2 * kSize : 8;
+    uint32_t w[kWords];
+    static __device__ __forceinline__ int column(int t, int j) { return kWide ? t * kJoinCols + j : j * kTeam + t; }
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void load(const char* row, int t, int dim) {
+        if constexpr (kWide) {
+            clear();
+            if (t * kJoinCols < dim) {
+                const char* p = row + t * kJoinCols * kSize;
+                const uint4 a = ld_stream_u4(p);
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+                if constexpr (DT == BAOC_F32) {
+                    const uint4 b = ld_stream_u4(p + 16);
+                    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = j * kTeam + t;
+                if constexpr (DT == BAOC_BF16) w[j] = c < dim ? *reinterpret_cast<const uint16_t*>(row + 2 * c) : 0;
+                else w[j] = c < dim ? *reinterpret_cast<const uint32_t*>(row + 4 * c) : 0;
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        if constexpr (DT == BAOC_F32) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+        } else if constexpr (kWide) {
+            unpack8(make_uint4(w[0], w[1], w[2], w[3]), x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j] << 16);
+        }
+    }
+    static __device__ __forceinline__ void store(char* row, int t, int dim, const float (&x)[8]) {
+        if constexpr (kWide) {
+            if (t * kJoinCols >= dim) return;
+            char* p = row + t * kJoinCols * kSize;
+            if constexpr (DT == BAOC_F32) {
+                st_stream_f4(p, make_float4(x[0], x[1], x[2], x[3]));
+                st_stream_f4(p + 16, make_float4(x[4], x[5], x[6], x[7]));
+            } else {
+                uint4 r;
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x[1]), "f"(x[0]));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.y) : "f"(x[3]), "f"(x[2]));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.z) : "f"(x[5]), "f"(x[4]));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w) : "f"(x[7]), "f"(x[6]));
+                st_stream_u4(p, r);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = j * kTeam + t;
+                if (c >= dim) continue;
+                if constexpr (DT == BAOC_F32) {
+                    *reinterpret_cast<float*>(row + 4 * c) = x[j];
+                } else {
+                    uint16_t h;
+                    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(x[j]));
+                    *reinterpret_cast<uint16_t*>(row + 2 * c) = h;
+                }
+            }
+        }
+    }
+};
+
+// A thread's 8 values of a vector per column (fp32, 4-byte aligned; read over and over, from L1); `other` where there is none.
+template <int kTeam, bool kWide>
+__device__ __forceinline__ void per_column(const float* v, int t, int dim, float other, float (&x)[8]) {
+    using P = RowPart<BAOC_F32, kTeam, kWide>;
+    if (kWide && v && t * kJoinCols < dim) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(v + t * kJoinCols)), b = __ldg(reinterpret_cast<const float4*>(v + t * kJoinCols) + 1);
+        f4_to8(a, b, x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = v && P::column(t, j) < dim ? __ldg(v + P::column(t, j)) : other;
+}
+
+// Sums of K values over a team, the same in all of its threads.  Teams of more than a warp take turns of two buffers, so that
+// one barrier a round is enough; all teams of a CTA call it together.
+template <int kTeam, int kMost>
+struct TeamSum {
+    static constexpr int kWarps = kTeam / 32, kTeams = join_cta(kTeam) / kTeam;
+    float (*buf)[kTeams][kMost][kWarps];
+    int turn = 0;
+    template <int K>
+    __device__ __forceinline__ void operator()(float (&v)[K]) {
+        static_assert(K <= kMost, "");
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        if constexpr (kTeam > 32) {
+            const int lane = threadIdx.x & 31, warp = (threadIdx.x % kTeam) >> 5, team = threadIdx.x / kTeam;
+            if (lane < K) {
+                float mine = v[0];
+#pragma unroll
+                for (int k = 1; k < K; ++k) mine = lane == k ? v[k] : mine;
+                buf[turn][team][lane][warp] = mine;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = buf[turn][team][k][lane % kWarps];
+#pragma unroll
+                for (int o = kWarps / 2; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+            }
+            turn ^= 1;
+        }
+    }
+};
+
+struct JoinArgs {
+    const char *x, *f;
+    char *y, *h;
+    const float *post_w, *post_b, *gate, *pre_w, *pre_b;
+    int64_t x_step, f_step, y_step, h_step, rows, rows_per_gate;
+    int dim, layer;
+    float scale, eps;
+};
+
+template <int S, int B, int kTeam, bool kWide>
+__global__ void __launch_bounds__(join_cta(kTeam)) join_kernel(const JoinArgs g) {
+    constexpr int kTeams = join_cta(kTeam) / kTeam;
+    using Stream = RowPart<S, kTeam, kWide>;
+    using Branch = RowPart<B, kTeam, kWide>;
+    __shared__ float buf[2][kTeams][1][kTeam / 32];
+    TeamSum<kTeam, 1> sum{buf};
+    const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam, dim = g.dim;
+    const float over = 1.f / float(dim);
+    const int64_t step = int64_t(gridDim.x) * kTeams;
+    bool inside[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inside[j] = Stream::column(t, j) < dim;
+    // v without its mean (layer norm), and 1 / sqrt(mean square + eps)
+    auto normalise = [&](float (&v)[8]) {
+        float s[1];
+        if (g.layer) {
+            s[0] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[0] += v[j];
+            sum(s);
+            const float mean = s[0] * over;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = inside[j] ? v[j] - mean : 0.f;
+        }
+        s[0] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += v[j] * v[j];
+        sum(s);
+        return rsqrtf(s[0] * over + g.eps);
+    };
+    Stream next_x;
+    Branch next_f;
+    auto fetch = [&](int64_t row) {
+        if (row < g.rows) {
+            next_f.load(g.f + row * g.f_step, t, dim);
+            if (g.x) next_x.load(g.x + row * g.x_step, t, dim);
+        }
+    };
+    next_x.clear();
+    next_f.clear();
+    int64_t row = int64_t(blockIdx.x) * kTeams + team;
+    fetch(row);
+    for (int64_t first = int64_t(blockIdx.x) * kTeams; first < g.rows; first += step, row += step) {
+        float x[8], u[8], w[8];
+        next_x.get(x);
+        next_f.get(u);
+        fetch(row + step);                       // (the next row is on its way while this one is reduced)
+        if (g.post_w) {
+            const float r = normalise(u);
+            float b[8];
+            per_column<kTeam, kWide>(g.post_w, t, dim, 0.f, w);
+            per_column<kTeam, kWide>(g.post_b, t, dim, 0.f, b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = u[j] * r * w[j] + b[j];
+        }
+        per_column<kTeam, kWide>(g.gate ? g.gate + (g.rows_per_gate ? min64(row, g.rows - 1) / g.rows_per_gate : 0) * dim : nullptr, t, dim, 1.f, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = g.scale * x[j] + w[j] * u[j];
+        if (row < g.rows) Stream::store(g.y + row * g.y_step, t, dim, u);
+        const float r = normalise(u);
+        float b[8];
+        per_column<kTeam, kWide>(g.pre_w, t, dim, 0.f, w);
+        per_column<kTeam, kWide>(g.pre_b, t, dim, 0.f, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = u[j] * r * w[j] + b[j];
+        if (row < g.rows) Branch::store(g.h + row * g.h_step, t, dim, u);
+    }
+}
+
+// ---- gradient ---------------------------------------------------------------------------------------------------
+enum Sum : int { kPreW = 0, kPostW = 1, kGate = 2, kPreB = 3, kPostB = 4 };
+
+struct JoinGradArgs {
+    const char *y, *f, *dy, *dh;
+    char *dx, *df;
+    const float *post_w, *post_b, *gate, *pre_w;
+    char* out[kJoinSums];          // the sums' destinations; null: not wanted
+    float* part;                   // [CTA][kJoinSums + 1][dim]; a gate per group: slots kGate and kJoinSums, see below
+    int64_t y_step, f_step, dy_step, dh_step, dx_step, df_step, rows, rows_per_gate, rows_per_cta;
+    int dim, grad_dtype;
+    float scale, eps;
+};
+
+__device__ __forceinline__ void store_grad(char* out, int dtype, int64_t i, float v) {
+    if (dtype == BAOC_F32) {
+        reinterpret_cast<float*>(out)[i] = v;
+    } else {
+        uint16_t h;
+        asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(v));
+        reinterpret_cast<uint16_t*>(out)[i] = h;
+    }
+}
+
+// A CTA takes rows_per_cta rows in order.  A gate per group: its sums are handed out at the end of every group.  A group whose
+// rows all belong to this CTA is finished here; of the others a CTA has two at most, the one its first row is in (slot kGate)
+// and the one its last row is in (slot kJoinSums).
+template <int S, int B, bool kLayer, int kTeam, bool kWide>
+__global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
+    constexpr int kCta = join_cta(kTeam), kTeams = kCta / kTeam, kSums = kLayer ? 5 : 3;
+    constexpr bool kShared = kTeam > 512;        // (64 registers a thread: the sums lie in shared memory)
+    constexpr bool kAhead = kTeam <= 512;
+    using Stream = RowPart<S, kTeam, kWide>;
+    using Branch = RowPart<B, kTeam, kWide>;
+    extern __shared__ float dynamic[];           // kShared: [kSums][8 * kTeam]; several teams: [kTeams][8 * kTeam]
+    __shared__ float buf[2][kTeams][4][kTeam / 32];
+    TeamSum<kTeam, 4> sum{buf};
+    const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam, dim = g.dim;
+    const float over = 1.f / float(dim);
+    const int64_t begin = int64_t(blockIdx.x) * g.rows_per_cta, end = min64(g.rows, begin + g.rows_per_cta);
+    float* part = g.part + int64_t(blockIdx.x) * (kJoinSums + 1) * dim;
+#ifdef BAOC_CHECKED
+    if (!check_range(ck, kKerJoinGrad, part, int64_t(kJoinSums + 1) * dim * 4, 0)) return;
+#endif
+    const bool need_f = g.post_w || g.gate;
+    float acc[kShared ? 1 : kSums][8];
+    auto add = [&](int k, int j, float v) {
+        if constexpr (kShared) dynamic[(k * 8 + j) * kTeam + t] += v;
+        else acc[k][j] += v;
+    };
+    auto zero = [&](int k) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (kShared) dynamic[(k * 8 + j) * kTeam + t] = 0.f;
+            else acc[k][j] = 0.f;
+        }
+    };
+    // the sum k of all teams to f(column, value), each column by one thread; all threads call it
+    auto hand_out = [&](auto which, auto f) {
+        constexpr int k = decltype(which)::value;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (kShared) v[j] = dynamic[(k * 8 + j) * kTeam + t];
+            else v[j] = acc[k][j];
+        }
+        if constexpr (kTeams > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dynamic[(team * 8 + j) * kTeam + t] = v[j];
+            __syncthreads();
+            if (team) return;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                for (int o = 1; o < kTeams; ++o) v[j] += dynamic[(o * 8 + j) * kTeam + t];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (Stream::column(t, j) < dim) f(Stream::column(t, j), v[j]);
+    };
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) zero(k);
+    bool inside[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inside[j] = Stream::column(t, j) < dim;
+    Stream next_y, next_dy;
+    Branch next_f, next_dh;
+    auto fetch = [&](int64_t row, int64_t last) {
+        if (row < last) {
+            next_y.load(g.y + row * g.y_step, t, dim);
+            next_dh.load(g.dh + row * g.dh_step, t, dim);
+            if (g.dy) next_dy.load(g.dy + row * g.dy_step, t, dim);
+            if (need_f) next_f.load(g.f + row * g.f_step, t, dim);
+        } else {
+            next_y.clear();
+            next_dh.clear();
+            next_dy.clear();
+            next_f.clear();                      // (an idle team adds zeros)
+        }
+    };
+    next_dy.clear();
+    next_f.clear();
+    for (int64_t seg = begin; seg < end;) {
+        const int64_t group = g.rows_per_gate ? seg / g.rows_per_gate : 0;
+        const int64_t seg_end = g.rows_per_gate ? min64(end, (group + 1) * g.rows_per_gate) : end;
+        const float* gate = g.gate ? g.gate + group * dim : nullptr;
+        if (kAhead) fetch(seg + team, seg_end);
+        for (int64_t first = seg; first < seg_end; first += kTeams) {
+            const int64_t row = first + team;
+            if (!kAhead) fetch(row, seg_end);
+            float y[8], d[8], f[8], w[8];        // d: from dh to Dy
+            next_y.get(y);
+            next_dh.get(d);
+            next_f.get(f);
+            float dy[8];
+            next_dy.get(dy);
+            if (kAhead) fetch(row + kTeams, seg_end);
+            float mean_f = 0.f, r_y, r_f;
+            if constexpr (kLayer) {
+                float s[2] = {0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { s[0] += y[j]; s[1] += f[j]; }
+                sum(s);
+                mean_f = s[1] * over;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = inside[j] ? y[j] - s[0] * over : 0.f;
+            }
+            per_column<kTeam, kWide>(g.pre_w, t, dim, 0.f, w);
+            {
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float dn = d[j] * w[j], c = kLayer ? (inside[j] ? f[j] - mean_f : 0.f) : f[j];
+                    s[0] += y[j] * y[j];
+                    s[1] += c * c;
+                    s[2] += dn * y[j];
+                    if (kLayer) s[3] += dn;
+                }
+                sum(s);
+                r_y = rsqrtf(s[0] * over + g.eps);
+                r_f = rsqrtf(s[1] * over + g.eps);
+                const float slope = r_y * r_y * s[2] * over, mean = s[3] * over;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    add(kPreW, j, d[j] * y[j] * r_y);
+                    if (kLayer) add(kPreB, j, d[j]);
+                    d[j] = dy[j] + r_y * (d[j] * w[j] - y[j] * slope - mean);
+                    dy[j] = g.scale * d[j];
+                }
+            }
+            if (g.dx && row < seg_end) Stream::store(g.dx + row * g.dx_step, t, dim, dy);
+            float gt[8];
+            per_column<kTeam, kWide>(gate, t, dim, 1.f, gt);
+            if (g.post_w) {
+                float b[8];
+                per_column<kTeam, kWide>(g.post_w, t, dim, 0.f, w);
+                per_column<kTeam, kWide>(kLayer ? g.post_b : nullptr, t, dim, 0.f, b);
+                float s[2] = {0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float n = (kLayer ? (inside[j] ? f[j] - mean_f : 0.f) : f[j]) * r_f;
+                    const float du = gt[j] * (inside[j] ? d[j] : 0.f);
+                    add(kGate, j, d[j] * (n * w[j] + b[j]));
+                    add(kPostW, j, du * n);
+                    if (kLayer) add(kPostB, j, du);
+                    f[j] = n;
+                    d[j] = du * w[j];
+                    s[0] += d[j] * n;
+                    s[1] += d[j];
+                }
+                sum(s);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] = r_f * (d[j] - f[j] * (s[0] * over) - (kLayer ? s[1] * over : 0.f));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    add(kGate, j, d[j] * f[j]);
+                    d[j] *= gt[j];
+                }
+            }
+            if (row < seg_end) Branch::store(g.df + row * g.df_step, t, dim, d);
+        }
+        if (g.rows_per_gate && g.out[kGate]) {
+            const bool whole = group * g.rows_per_gate >= begin && min64(g.rows, (group + 1) * g.rows_per_gate) <= end;
+            float* slot = part + int64_t(group == begin / g.rows_per_gate ? kGate : kJoinSums) * dim;
+            hand_out(std::integral_constant<int, kGate>{}, [&](int c, float v) {
+                if (whole) store_grad(g.out[kGate], g.grad_dtype, group * dim + c, v);
+                else slot[c] = v;
+            });
+            zero(kGate);
+        }
+        seg = seg_end;
+    }
+    let_later_kernel_start();
+    auto finish = [&](auto which) {
+        constexpr int k = decltype(which)::value;
+        if (g.out[k]) hand_out(which, [&](int c, float v) { part[int64_t(k) * dim + c] = v; });
+    };
+    finish(std::integral_constant<int, kPreW>{});
+    finish(std::integral_constant<int, kPostW>{});
+    if (!g.rows_per_gate) finish(std::integral_constant<int, kGate>{});
+    if constexpr (kLayer) {
+        finish(std::integral_constant<int, kPreB>{});
+        finish(std::integral_constant<int, kPostB>{});
+    }
+}
+
+// The CTAs' sums, 32 columns per CTA: every warp adds each 32nd CTA's, then the warps' sums are added in order.
+// blockIdx.y: which sum; from kJoinSums on, groups of a gate that several CTAs have rows of.
+__global__ void __launch_bounds__(1024) join_sums_kernel(const JoinGradArgs g, int ctas, int64_t groups) {
+    __shared__ float sh[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = int(blockIdx.x) * 32 + lane;
+    wait_for_earlier_kernel();
+    auto total = [&](int64_t c0, int64_t c1, int64_t group, int k, int64_t at) {
+        float s = 0.f;
+        if (col < g.dim)
+            for (int64_t c = c0 + warp; c <= c1; c += 32) {
+                const int slot = group < 0 || group == c * g.rows_per_cta / g.rows_per_gate ? k : kJoinSums;
+                s += g.part[(c * (kJoinSums + 1) + slot) * g.dim + col];
+            }
+        sh[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0 && col < g.dim) {
+            for (int w = 1; w < 32; ++w) s += sh[w][lane];
+            store_grad(g.out[k], g.grad_dtype, at + col, s);
+        }
+        __syncthreads();
+    };
+    const int k = int(blockIdx.y);
+    if (k < kJoinSums) {
+        if (!g.out[k] || (k == kGate && g.rows_per_gate)) return;
+        total(0, ctas - 1, -1, k, 0);
+        return;
+    }
+    for (int64_t group = k - kJoinSums; group < groups; group += gridDim.y - kJoinSums) {
+        const int64_t c0 = group * g.rows_per_gate / g.rows_per_cta, c1 = (min64(g.rows, (group + 1) * g.rows_per_gate) - 1) / g.rows_per_cta;
+        if (c0 == c1) continue;                  // (that CTA has written it)
+        total(c0, c1, group, kGate, group * g.dim);
+    }
+}
+
+namespace {
+
+thread_local std::string g_join_err;
+
+int fail_join(int code, const std::string& msg) {
+    g_join_err = msg;
+    return code;
+}
+int64_t elem_bytes(int dtype) { return dtype == BAOC_F32 ? 4 : 2; }
+bool aligned(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & uintptr_t(bytes - 1)) == 0; }
+
+int check_join(const baoc_join_t* e, int64_t rows, const std::string& what) {
+    if (!e) return fail_join(BAOC_E_INVALID, what + ": null descriptor");
+    if (e->dim < 1 || e->dim > kJoinMaxDim) return fail_join(BAOC_E_INVALID, what + ": dim must be in 1 .. 8192");
+    if (e->kind != BAOC_NORM_RMS && e->kind != BAOC_NORM_LAYER) return fail_join(BAOC_E_INVALID, what + ": kind must be BAOC_NORM_RMS or BAOC_NORM_LAYER");
+    for (int t : {e->stream_dtype, e->branch_dtype, e->grad_dtype})
+        if (t != BAOC_BF16 && t != BAOC_F32) return fail_join(BAOC_E_INVALID, what + ": dtypes must be BAOC_BF16 or BAOC_F32");
+    if (e->stream_dtype == BAOC_BF16 && e->branch_dtype == BAOC_F32) return fail_join(BAOC_E_INVALID, what + ": an fp32 branch needs an fp32 stream");
+    if (!std::isfinite(e->scale)) return fail_join(BAOC_E_INVALID, what + ": scale must be finite");
+    if (!std::isfinite(e->eps) || !(e->eps > 0.f)) return fail_join(BAOC_E_INVALID, what + ": eps must be finite and above zero");
+    if (e->rows_per_gate < 0) return fail_join(BAOC_E_INVALID, what + ": rows_per_gate must not be negative");
+    for (int64_t s : {e->x_stride, e->f_stride, e->y_stride, e->h_stride})
+        if (s && (s < e->dim || s > kJoinMaxStride)) return fail_join(BAOC_E_INVALID, what + ": a row stride must be 0 or in dim .. 2^28");
+    if (rows < 0 || rows > (int64_t(1) << 31)) return fail_join(BAOC_E_INVALID, what + ": rows must be in 0 .. 2^31");
+    return BAOC_OK;
+}
+
+// An array of rows as the kernels see it.
+struct Rows {
+    const void* p;
+    int64_t step, width, eb;        // bytes from row to row, of a row, of an element
+    Rows(const void* p, int64_t stride, int dtype, int dim) : p(p), step((stride ? stride : dim) * elem_bytes(dtype)), width(dim * elem_bytes(dtype)), eb(elem_bytes(dtype)) {}
+    bool wide() const { return !p || (aligned(p, 16) && step % 16 == 0); }
+    bool fits() const { return aligned(p, eb); }
+};
+// Whether the rows of two arrays share bytes.  (Rows of one buffer may lie between each other's.)
+bool overlap(const Rows& a, const Rows& b, int64_t rows) {
+    if (!a.p || !b.p || rows == 0) return false;
+    const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
+    if (x >= y + (rows - 1) * b.step + b.width || y >= x + (rows - 1) * a.step + a.width) return false;
+    if (a.step != b.step) return true;
+    const int64_t off = ((y - x) % a.step + a.step) % a.step;
+    return off < a.width || off + b.width > a.step;
+}
+bool same(const Rows& a, const Rows& b, int64_t rows) { return a.p == b.p && a.width == b.width && (a.step == b.step || rows == 1); }
+
+int team_of(int dim, bool wide) {
+    if (!wide) return dim <= 256 ? 32 : (dim <= 2048 ? 256 : 1024);
+    int t = 32;
+    while (t * kJoinCols < dim) t *= 2;
+    return t;
+}
+
+// f(team, wide) as constants.
+template <typename F>
+int with_team(int team, bool wide, F f) {
+    using std::integral_constant;
+    if (!wide) {
+        if (team == 32) return f(integral_constant<int, 32>{}, std::false_type{});
+        return team == 256 ? f(integral_constant<int, 256>{}, std::false_type{}) : f(integral_constant<int, 1024>{}, std::false_type{});
+    }
+    switch (team) {
+        case 32: return f(integral_constant<int, 32>{}, std::true_type{});
+        case 64: return f(integral_constant<int, 64>{}, std::true_type{});
+        case 128: return f(integral_constant<int, 128>{}, std::true_type{});
+        case 256: return f(integral_constant<int, 256>{}, std::true_type{});
+        case 512: return f(integral_constant<int, 512>{}, std::true_type{});
+        default: return f(integral_constant<int, 1024>{}, std::true_type{});
+    }
+}
+template <typename F>
+int with_types(int stream, int branch, F f) {
+    using std::integral_constant;
+    if (stream == BAOC_BF16) return f(integral_constant<int, BAOC_BF16>{}, integral_constant<int, BAOC_BF16>{});
+    return branch == BAOC_BF16 ? f(integral_constant<int, BAOC_F32>{}, integral_constant<int, BAOC_BF16>{})
+                               : f(integral_constant<int, BAOC_F32>{}, integral_constant<int, BAOC_F32>{});
+}
+
+// The gradient's rows per CTA and CTAs: as many CTAs as find room at once (kJoinSmThreads per SM), whole rounds of their teams.
+void grad_shape(int team, int64_t rows, int64_t* per_cta, int* ctas) {
+    const int cta = join_cta(team), teams = cta / team;
+    const int64_t most = int64_t(148) * (kJoinSmThreads / cta);
+    *per_cta = std::max<int64_t>(teams, round_up(ceil_div(rows, most), teams));
+    *ctas = int(ceil_div(rows, *per_cta));
+}
+// (By the most CTAs that so many rows or fewer can get: whole rounds leave fewer of them for some larger numbers of rows.)
+int64_t grad_ws(int dim, bool wide, int64_t rows) {
+    const int team = team_of(dim, wide), cta = join_cta(team);
+    const int64_t ctas = std::min(ceil_div(rows, cta / team), int64_t(148) * (kJoinSmThreads / cta));
+    return round_up(ctas * (kJoinSums + 1) * dim * 4, 256);
+}
+
+int launched(cudaError_t ce, const char* kernel) {
+    return ce == cudaSuccess ? BAOC_OK : fail_join(BAOC_E_CUDA, std::string(kernel) + ": " + cudaGetErrorString(ce));
+}
+
+}  // namespace
+
+BAOC_DEFINE_CHECK_FETCH(join_check_fetch)
+
+}  // namespace baoc
+
+using namespace baoc;
+
+extern "C" {
+
+const char* baoc_join_last_error(void) { return g_join_err.c_str(); }
+
+int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* post_w, const float* post_b, const float* gate,
+              const float* pre_w, const float* pre_b, int64_t rows, void* y, void* h, baoc_stream_t stream) try {
+    const int rc = check_join(e, rows, "baoc_join");
+    if (rc) return rc;
+    if (rows == 0) return BAOC_OK;
+    if (!f || !pre_w || !y || !h) return fail_join(BAOC_E_INVALID, "baoc_join: null pointer");
+    if ((post_b && !post_w) || (e->kind == BAOC_NORM_RMS && (post_b || pre_b))) return fail_join(BAOC_E_INVALID, "baoc_join: biases belong to layer norms");
+    const Rows rx(x, e->x_stride, e->stream_dtype, e->dim), rf(f, e->f_stride, e->branch_dtype, e->dim), ry(y, e->y_stride, e->stream_dtype, e->dim),
+        rh(h, e->h_stride, e->branch_dtype, e->dim);
+    bool wide = e->dim % kJoinCols == 0;
+    for (const Rows* r : {&rx, &rf, &ry, &rh}) {
+        if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join: a pointer is not aligned to its elements");
+        wide = wide && r->wide();
+    }
+    for (const void* p : {static_cast<const void*>(post_w), static_cast<const void*>(post_b), static_cast<const void*>(gate), static_cast<const void*>(pre_w), static_cast<const void*>(pre_b)}) {
+        if (!aligned(p, 4)) return fail_join(BAOC_E_ALIGN, "baoc_join: a pointer is not aligned to its elements");
+        wide = wide && aligned(p, 16);
+    }
+    if ((overlap(ry, rx, rows) && !same(ry, rx, rows)) || overlap(ry, rf, rows) || (overlap(rh, rf, rows) && !same(rh, rf, rows)) || overlap(rh, rx, rows) ||
+        overlap(ry, rh, rows))
+        return fail_join(BAOC_E_INVALID, "baoc_join: y may be x and h may be f; arrays overlap in no other way");
+    const JoinArgs a{static_cast<const char*>(x), static_cast<const char*>(f), static_cast<char*>(y), static_cast<char*>(h), post_w, post_b, gate, pre_w, pre_b,
+                     rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
+        return with_team(team_of(e->dim, wide), wide, [&](auto T, auto W) {
+            constexpr int kCta = join_cta(T()), kTeams = kCta / T();
+            const unsigned grid = unsigned(std::min<int64_t>(ceil_div(rows, kTeams), int64_t(148) * (2048 / kCta)));
+            join_kernel<S(), B(), T(), W()><<<grid, kCta, 0, s>>>(a);
+            return launched(cudaGetLastError(), "join_kernel");
+        });
+    });
+} catch (const std::bad_alloc&) {
+    return BAOC_E_INVALID;
+}
+
+int baoc_join_grad_workspace_bytes(const baoc_join_t* e, int64_t rows, size_t* bytes) try {
+    const int rc = check_join(e, rows, "baoc_join_grad_workspace_bytes");
+    if (rc) return rc;
+    if (!bytes) return fail_join(BAOC_E_INVALID, "baoc_join_grad_workspace_bytes: null pointer");
+    *bytes = size_t(std::max<int64_t>(256, std::max(grad_ws(e->dim, true, rows), grad_ws(e->dim, false, rows))));
+    return BAOC_OK;
+} catch (const std::bad_alloc&) {
+    return BAOC_E_INVALID;
+}
+
+int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const void* dy, const void* dh, const float* post_w, const float* post_b,
+                   const float* gate, const float* pre_w, int64_t rows, void* dx, void* df, void* dpost_w, void* dpost_b, void* dgate,
+                   void* dpre_w, void* dpre_b, void* ws, size_t ws_bytes, baoc_stream_t stream) try {
+    const char* what = "baoc_join_grad";
+    int rc = check_join(e, rows, what);
+    if (rc) return rc;
+    for (int64_t s : {e->dy_stride, e->dh_stride, e->dx_stride, e->df_stride})
+        if (s && (s < e->dim || s > kJoinMaxStride)) return fail_join(BAOC_E_INVALID, "baoc_join_grad: a row stride must be 0 or in dim .. 2^28");
+    const bool layer = e->kind == BAOC_NORM_LAYER;
+    if (!pre_w || !ws || (rows && (!y || !dh || !df || ((post_w || gate) && !f)))) return fail_join(BAOC_E_INVALID, "baoc_join_grad: null pointer");
+    if (((post_b || dpost_w || dpost_b) && !post_w) || (dgate && !gate) || (!layer && (post_b || dpost_b || dpre_b)))
+        return fail_join(BAOC_E_INVALID, "baoc_join_grad: a bias or a gradient of something that is not there");
+    const Rows ry(y, e->y_stride, e->stream_dtype, e->dim), rf(post_w || gate ? f : nullptr, e->f_stride, e->branch_dtype, e->dim),
+        rdy(dy, e->dy_stride, e->stream_dtype, e->dim), rdh(dh, e->dh_stride, e->branch_dtype, e->dim), rdx(dx, e->dx_stride, e->stream_dtype, e->dim),
+        rdf(df, e->df_stride, e->branch_dtype, e->dim);
+    bool wide = e->dim % kJoinCols == 0;
+    for (const Rows* r : {&ry, &rf, &rdy, &rdh, &rdx, &rdf}) {
+        if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
+        wide = wide && r->wide();
+    }
+    for (const float* p : {post_w, post_b, gate, pre_w}) {
+        if (!aligned(p, 4)) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
+        wide = wide && aligned(p, 16);
+    }
+    void* outs[kJoinSums] = {};
+    outs[kPreW] = dpre_w; outs[kPreB] = dpre_b; outs[kPostW] = dpost_w; outs[kPostB] = dpost_b; outs[kGate] = dgate;
+    for (const void* p : outs)
+        if (!aligned(p, elem_bytes(e->grad_dtype))) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
+    if (!aligned(ws, 256)) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: workspace not 256-byte aligned");
+    const int64_t need = std::max<int64_t>(256, grad_ws(e->dim, wide, rows));
+    if (ws_bytes < size_t(need)) return fail_join(BAOC_E_WORKSPACE, "baoc_join_grad: workspace too small");
+    if ((overlap(rdx, rdy, rows) && !same(rdx, rdy, rows)) || (overlap(rdf, rdh, rows) && !same(rdf, rdh, rows)) || overlap(rdx, ry, rows) || overlap(rdx, rf, rows) ||
+        overlap(rdx, rdh, rows) || overlap(rdf, ry, rows) || overlap(rdf, rf, rows) || overlap(rdf, rdy, rows) || overlap(rdx, rdf, rows))
+        return fail_join(BAOC_E_INVALID, "baoc_join_grad: dx may be dy and df may be dh; outputs overlap nothing else");
+    const int team = team_of(e->dim, wide);
+    JoinGradArgs a{static_cast<const char*>(y), static_cast<const char*>(rf.p), static_cast<const char*>(dy), static_cast<const char*>(dh), static_cast<char*>(dx),
+                   static_cast<char*>(df), post_w, post_b, gate, pre_w, {}, static_cast<float*>(ws), ry.step, rf.step, rdy.step, rdh.step, rdx.step, rdf.step, rows,
+                   gate ? e->rows_per_gate : 0, 0, e->dim, e->grad_dtype, e->scale, e->eps};
+    for (int k = 0; k < kJoinSums; ++k) a.out[k] = static_cast<char*>(outs[k]);
+    int ctas;
+    grad_shape(team, std::max<int64_t>(rows, 1), &a.rows_per_cta, &ctas);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const CheckCtx ck{static_cast<char*>(ws), static_cast<char*>(ws) + need, 0, 0, 0};
+    (void)ck;
+    if (rows) {
+        rc = with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
+            return with_team(team, wide, [&](auto T, auto W) {
+                auto go = [&](auto L) {
+                    constexpr int kCta = join_cta(T()), kTeams = kCta / T();
+                    constexpr int kBytes = T() > 512 ? (L() ? 5 : 3) * 8 * T() * 4 : (kTeams > 1 ? kTeams * 8 * T() * 4 : 0);
+                    auto kernel = join_grad_kernel<S(), B(), L(), T(), W()>;
+                    if (kBytes > 48 * 1024) {
+                        const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+                        if (ce != cudaSuccess) return launched(ce, "join_grad_kernel");
+                    }
+                    kernel<<<unsigned(ctas), kCta, kBytes, s>>>(a BAOC_CHECK_ARG(ck));
+                    return launched(cudaGetLastError(), "join_grad_kernel");
+                };
+                return layer ? go(std::true_type{}) : go(std::false_type{});
+            });
+        });
+        if (rc) return rc;
+    } else {
+        ctas = 0;
+    }
+    bool any = false;
+    for (const void* p : outs) any = any || p;
+    if (!any) return BAOC_OK;
+    const int64_t groups = a.rows_per_gate && dgate ? ceil_div(rows, a.rows_per_gate) : 0;
+    const dim3 grid(unsigned(ceil_div(e->dim, 32)), unsigned(kJoinSums + std::min<int64_t>(groups, 1024)));
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = dim3(1024); cfg.stream = s; cfg.attrs = &at; cfg.numAttrs = rows ? 1 : 0;
+    return launched(cudaLaunchKernelEx(&cfg, join_sums_kernel, a, ctas, groups), "join_sums_kernel");
+} catch (const std::bad_alloc&) {
+    return BAOC_E_INVALID;
+}
+
+}  // extern "C"

@@ -1,0 +1,75 @@
+"""The C entry points of the join refuse bad arguments before anything is queued (no GPU needed: the addresses are never
+followed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2605_04711_b200 import binding as B
+
+P = 1 << 20                       # a 256-byte aligned address that nothing reads
+
+
+def _e(**kw):
+    d = {n: 0 for n, _ in B.JoinForm._fields_} | dict(dim=16, kind=1, stream_dtype=1, branch_dtype=0, grad_dtype=0, eps=1e-6, scale=1.0) | kw
+    return B.JoinForm(*[d[n] for n, _ in B.JoinForm._fields_])
+
+
+def _join(e, **kw):
+    a = dict(x=P, f=P << 1, post_w=P << 2, post_b=P << 3, gate=P << 4, pre_w=P << 5, pre_b=P << 6, rows=4, y=P << 7, h=P << 8) | kw
+    return B._lib.baoc_join(e, *a.values(), None)
+
+
+def _grad(e, **kw):
+    a = dict(y=P, f=P << 1, dy=P << 2, dh=P << 3, post_w=P << 4, post_b=P << 5, gate=P << 6, pre_w=P << 7, rows=4, dx=P << 8, df=P << 9, dpost_w=P << 10,
+             dpost_b=P << 11, dgate=P << 12, dpre_w=P << 13, dpre_b=P << 14, ws=P << 15, ws_bytes=1 << 20) | kw
+    return B._lib.baoc_join_grad(e, *a.values(), None)
+
+
+@pytest.mark.parametrize("kw", [dict(dim=0), dict(dim=8193), dict(kind=2), dict(stream_dtype=2), dict(branch_dtype=-1), dict(grad_dtype=3), dict(eps=0.0),
+                                dict(eps=float("inf")), dict(scale=float("nan")), dict(rows_per_gate=-1), dict(x_stride=15), dict(h_stride=(1 << 28) + 1),
+                                dict(stream_dtype=0, branch_dtype=1)])
+def test_descriptors(kw):
+    e, n = C.byref(_e(**kw)), C.c_size_t()
+    assert _join(e) == B.E_INVALID and _grad(e) == B.E_INVALID
+    assert B._lib.baoc_join_grad_workspace_bytes(e, 4, C.byref(n)) == B.E_INVALID
+    assert b"baoc_join_grad_workspace_bytes" in B._lib.baoc_join_last_error()
+
+
+def test_join_arguments():
+    e = C.byref(_e())
+    assert _join(None) == B.E_INVALID and _join(e, rows=-1) == B.E_INVALID and _join(e, rows=(1 << 31) + 1) == B.E_INVALID
+    for k in ("f", "pre_w", "y", "h", "post_w"):                        # (the last: a bias without its weight)
+        assert _join(e, **{k: None}) == B.E_INVALID
+    assert _join(C.byref(_e(kind=0))) == B.E_INVALID                    # biases of RMS norms
+    for k in ("x", "f", "post_w", "post_b", "gate", "pre_w", "pre_b", "y", "h"):
+        assert _join(e, **{k: (P << 10) + 1}) == B.E_ALIGN
+    for kw in (dict(y=P + 64), dict(y=(P << 1) + 32), dict(h=(P << 1) + 32), dict(h=P), dict(h=(P << 7) + 16)):
+        assert _join(e, **kw) == B.E_INVALID
+    assert _join(C.byref(_e(x_stride=32)), y=P) == B.E_INVALID          # the same array at another stride
+    assert _join(e, x=None, f=None, pre_w=None, y=None, h=None, rows=0) == B.OK
+
+
+def test_grad_arguments():
+    e, n = C.byref(_e()), C.c_size_t()
+    assert _grad(None) == B.E_INVALID and _grad(e, rows=-1) == B.E_INVALID
+    for k in ("y", "f", "dh", "pre_w", "df", "ws", "post_w", "gate"):
+        assert _grad(e, **{k: None}) == B.E_INVALID
+    for k in ("y", "f", "dy", "dh", "post_w", "post_b", "gate", "pre_w", "dx", "df"):
+        assert _grad(e, **{k: (P << 20) + 1}) == B.E_ALIGN
+    for k in ("dpost_w", "dpost_b", "dgate", "dpre_w", "dpre_b"):
+        assert _grad(e, **{k: (P << 20) + 1}) == B.E_ALIGN
+    assert _grad(e, ws=(P << 15) + 128) == B.E_ALIGN
+    for kw in (dict(dx=P), dict(dx=(P << 2) + 64), dict(df=(P << 3) + 32), dict(df=P << 1), dict(dx=P << 3), dict(df=(P << 8) + 64)):
+        assert _grad(e, **kw) == B.E_INVALID
+    assert B._lib.baoc_join_grad_workspace_bytes(e, 4, None) == B.E_INVALID
+    assert B._lib.baoc_join_grad_workspace_bytes(e, 4, C.byref(n)) == B.OK
+    assert _grad(e, ws_bytes=n.value - 1) == B.E_WORKSPACE
+    assert b"workspace too small" in B._lib.baoc_join_last_error()
+    for kw in (dict(dy_stride=15), dict(df_stride=(1 << 28) + 1)):
+        assert _grad(C.byref(_e(**kw))) == B.E_INVALID
+
+
+def test_plans():
+    for kw in (dict(dim=0), dict(dim=8193), dict(dim=8, kind="batch"), dict(dim=8, eps=0.0), dict(dim=8, scale=float("inf"))):
+        with pytest.raises(B.BaocError):
+            B.Join(**kw)
