@@ -600,6 +600,63 @@ int baoc_embed_grad(const baoc_embed_t* e, const void* ids, const void* dout, in
                     int accumulate, void* ws, size_t ws_bytes, baoc_stream_t stream);
 const char* baoc_embed_last_error(void);
 
+/* ---- matrix product with bias, activation and residual ---------------------------------
+ * The paper has no counterpart of these.  A layer of a language model and its gradient:
+ *
+ *   z = x w^T + bias,   pre = z,   out = act(z) + residual
+ *   dz = dout * act'(pre),   dx = dz w,   dw = dz^T x,   db = sum over rows of dz
+ *
+ * (residual's gradient is dout itself).  x, w, dout, pre and dx are bf16; products are
+ * formed on the tensor cores and summed in fp32, bias (fp32), activation and residual
+ * follow in fp32, and every output is rounded once.  dz, an operand of the tensor
+ * cores, is rounded to bf16; where dw is wanted in fp32 behind an activation, what that
+ * rounding leaves is multiplied too (as two more bf16: 24 bits in all, three products
+ * for one).  db is summed
+ * from the unrounded dz.  Activations: relu; gelu, z Phi(z); gelu_tanh, its tanh form;
+ * silu, z / (1 + e^-z).  Handle-free. */
+enum { BAOC_ACT_NONE = 0, BAOC_ACT_RELU = 1, BAOC_ACT_GELU = 2, BAOC_ACT_GELU_TANH = 3, BAOC_ACT_SILU = 4 };
+enum { BAOC_OUT_IN = 0, BAOC_IN_OUT = 1 };
+typedef struct {
+    int32_t n_in, n_out;         /* 1 .. 2^24 */
+    int32_t act;
+    int32_t layout;              /* BAOC_OUT_IN: w and dw are [n_out][n_in]; BAOC_IN_OUT: [n_in][n_out] */
+    int32_t out_dtype;           /* of out and residual: BAOC_BF16 or BAOC_F32 */
+    int32_t grad_dtype;          /* of dw and db */
+    int64_t x_stride, w_stride, out_stride, residual_stride, pre_stride;    /* elements from row to row: the row's length .. 2^28, 0 for it */
+    int64_t dout_stride, dx_stride, dw_stride;                             /* (baoc_linear_grad alone) */
+} baoc_linear_t;
+
+/* Bytes of device workspace (0: none, NULL will do).  x, w and dout are read by tiled
+ * copies; one whose base or row stride is no multiple of 16 bytes is first laid out in
+ * the workspace.  anywhere = 0: all bases are multiples of 16 bytes; 1: they need not
+ * be.  A workspace serves every smaller number of tokens too. */
+int baoc_linear_workspace_bytes(const baoc_linear_t* e, int64_t tokens, int anywhere, size_t* bytes);
+int baoc_linear_grad_workspace_bytes(const baoc_linear_t* e, int64_t tokens, int anywhere, size_t* bytes);
+
+/* out[tokens][n_out] and pre[tokens][n_out] (NULL: not wanted) from x[tokens][n_in];
+ * bias[n_out] and residual[tokens][n_out] may be NULL.  out may be residual (same row
+ * stride) and overlaps no other array.  Pointers are aligned to their elements, ws to
+ * 256 bytes.  tokens <= 2^30, 0 queues nothing.  Queues one kernel, two where an array
+ * is laid out first; does not wait. */
+int baoc_linear(const baoc_linear_t* e, const void* x, const void* w, const float* bias, const void* residual, int64_t tokens, void* out,
+                void* pre, void* ws, size_t ws_bytes, baoc_stream_t stream);
+
+/* dx[tokens][n_in], dw (w's layout) and db[n_out] from dout[tokens][n_out] and, behind
+ * an activation, pre as baoc_linear wrote it.  Each output may be NULL; they are
+ * written, not added to, and overlap no other array.  x is not read without dw, w not
+ * without dx.  Sums are fp32, in an order that depends on the descriptor, tokens and
+ * alignment only: equal calls give equal bits.  Does not wait.
+ * Errors of all: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_WORKSPACE, BAOC_E_CUDA;
+ * baoc_linear_last_error() returns the message of the calling thread's last failure. */
+int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const void* dout, const void* pre, int64_t tokens, void* dx,
+                     void* dw, void* db, void* ws, size_t ws_bytes, baoc_stream_t stream);
+
+/* Waits for the device, then writes and clears the number of CTAs of the products on it
+ * whose wait for a copy or a product ran out (10 s each; their outputs are not
+ * valid).  0 unless something is wrong with the device. */
+int baoc_linear_status(int32_t* gave_up);
+const char* baoc_linear_last_error(void);
+
 /* ---- norms around a block's join -----------------------------------------------------
  * The paper has no counterpart of these.  Between two blocks of a language model the
  * branch f of the one joins the residual stream x, and the other's input is normed:

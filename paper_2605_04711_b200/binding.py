@@ -96,6 +96,11 @@ class JoinForm(C.Structure):
                [(n + "_stride", C.c_int64) for n in ("x", "f", "y", "h", "dx", "df", "dy", "dh")]
 
 
+class LinearForm(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_in", "n_out", "act", "layout", "out_dtype", "grad_dtype")] + \
+               [(n + "_stride", C.c_int64) for n in ("x", "w", "out", "residual", "pre", "dout", "dx", "dw")]
+
+
 class Info(C.Structure):
     _fields_ = [("n_blocks", C.c_int32), ("n_cfg", C.c_int32), ("numel", C.c_int64), ("n_tiles", C.c_int64),
                 ("stats_steps", C.c_int64), ("state_bytes", C.c_int64), ("kernel_launches", C.c_int64),
@@ -113,7 +118,9 @@ EXPORTS = ["baoc_default_opts", "baoc_create", "baoc_destroy", "baoc_last_error"
            "baoc_clip_workspace_bytes", "baoc_bind_clip_workspace", "baoc_grad_norm", "baoc_clip_grads",
            "baoc_embed", "baoc_embed_grad_workspace_bytes", "baoc_embed_grad", "baoc_embed_last_error",
            "baoc_logp", "baoc_logp_grad", "baoc_logp_last_error",
-           "baoc_join", "baoc_join_grad_workspace_bytes", "baoc_join_grad", "baoc_join_last_error"]
+           "baoc_join", "baoc_join_grad_workspace_bytes", "baoc_join_grad", "baoc_join_last_error",
+           "baoc_linear_workspace_bytes", "baoc_linear", "baoc_linear_grad_workspace_bytes", "baoc_linear_grad",
+           "baoc_linear_status", "baoc_linear_last_error"]
 
 _vp = C.c_void_p
 _lib.baoc_default_opts.argtypes = [C.POINTER(Opts)]
@@ -173,6 +180,13 @@ _lib.baoc_join_grad_workspace_bytes.argtypes = [_vp, C.c_int64, C.POINTER(C.c_si
 _lib.baoc_join_grad.argtypes = [_vp] * 9 + [C.c_int64] + [_vp] * 8 + [C.c_size_t, _vp]
 _lib.baoc_join_last_error.argtypes = []
 _lib.baoc_join_last_error.restype = C.c_char_p
+_lib.baoc_linear_workspace_bytes.argtypes = [_vp, C.c_int64, C.c_int, C.POINTER(C.c_size_t)]
+_lib.baoc_linear_grad_workspace_bytes.argtypes = [_vp, C.c_int64, C.c_int, C.POINTER(C.c_size_t)]
+_lib.baoc_linear.argtypes = [_vp] * 5 + [C.c_int64] + [_vp] * 3 + [C.c_size_t, _vp]
+_lib.baoc_linear_grad.argtypes = [_vp] * 5 + [C.c_int64] + [_vp] * 4 + [C.c_size_t, _vp]
+_lib.baoc_linear_status.argtypes = [C.POINTER(C.c_int32)]
+_lib.baoc_linear_last_error.argtypes = []
+_lib.baoc_linear_last_error.restype = C.c_char_p
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}              # BAOC_BF16, BAOC_F32
 
 
@@ -416,6 +430,133 @@ class Embedding:
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}       # BAOC_ACT_*
+LAYOUTS = {"out_in": 0, "in_out": 1}                                               # BAOC_OUT_IN, BAOC_IN_OUT
+
+
+def linear_status() -> int:
+    """``baoc_linear_status``: waits for the current device; how many CTAs of its matrix products gave a wait up (0 on a sound
+    device), and clears the number."""
+    n = C.c_int32()
+    rc = _lib.baoc_linear_status(C.byref(n))
+    if rc < 0:
+        raise BaocError(rc, _lib.baoc_linear_last_error().decode())
+    return n.value
+
+
+class Linear:
+    """A matrix product with bias, activation and residual (``baoc_linear``) and its gradient (``baoc_linear_grad``): a plan of
+    one layer.
+
+        pre = x w^T + bias,   out = act(pre) + residual
+
+    x and w are bf16 (the parameters that the optimizer step keeps are fp32: a layer's bf16 copy is the caller's), bias fp32, out
+    and residual bf16 or fp32.  act: "none", "relu", "gelu", "gelu_tanh" or "silu"; layout: w is [n_out, n_in] ("out_in") or
+    [n_in, n_out] ("in_out").  Calls queue work on the current stream of the tensors' device; autograd does not see them.  Like a
+    handle, a plan serves one thread at a time."""
+
+    def __init__(self, n_in: int, n_out: int, act: str = "none", layout: str = "out_in"):
+        if act not in ACTIVATIONS or layout not in LAYOUTS:
+            raise BaocError(E_INVALID, f"act is one of {sorted(ACTIVATIONS)}, layout one of {sorted(LAYOUTS)}, not {act!r} and {layout!r}")
+        self.n_in, self.n_out, self.act, self.layout = int(n_in), int(n_out), act, layout
+        clamp = lambda n: max(-1, min(n, 2 ** 31 - 1))
+        self._e = LinearForm(clamp(self.n_in), clamp(self.n_out), ACTIVATIONS[act], LAYOUTS[layout], 0, 0)
+        self._ref, self._n = C.byref(self._e), C.c_size_t()
+        self.w_shape = (self.n_out, self.n_in) if layout == "out_in" else (self.n_in, self.n_out)
+        self.workspace_bytes(0)                             # the descriptor's checks
+
+    def _failed(self, rc: int):
+        raise BaocError(rc, _lib.baoc_linear_last_error().decode())
+
+    def _bytes(self, call, tokens: int, contiguous: bool, anywhere: bool) -> int:
+        if contiguous:
+            for name in ("x", "w", "dout"):
+                setattr(self._e, name + "_stride", 0)
+        rc = call(self._ref, int(tokens), 1 if anywhere else 0, C.byref(self._n))
+        return self._n.value if rc >= 0 else self._failed(rc)
+
+    def workspace_bytes(self, tokens: int) -> int:
+        """Device bytes that ``product`` of contiguous, 16-byte aligned arrays needs (0 where their rows are multiples of 16 bytes)."""
+        return self._bytes(_lib.baoc_linear_workspace_bytes, tokens, True, False)
+
+    def grad_workspace_bytes(self, tokens: int) -> int:
+        """The same of ``grad``, whatever the type of its outputs."""
+        self._e.grad_dtype = DTYPES[torch.float32]
+        return self._bytes(_lib.baoc_linear_grad_workspace_bytes, tokens, True, False)
+
+    def _take(self, what: str, rows, cols: int, dtypes, dev, **arrays):
+        """Checks arrays [.., cols] of `rows` rows (None: the first one's) and writes their strides to the descriptor; returns the rows."""
+        for name, t in arrays.items():
+            if t is None:
+                setattr(self._e, name + "_stride", 0)
+                continue
+            n, stride = _rows(t, cols, name)
+            rows = n if rows is None else rows
+            if n != rows or t.get_device() != dev or dev < 0 or t.dtype not in dtypes:
+                raise BaocError(E_INVALID, f"{what}: {name} must be [{rows}, {cols}] of {' or '.join(str(d) for d in dtypes)} on the device of x, cuda:{dev}")
+            if t.requires_grad and torch.is_grad_enabled():
+                raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach {name}, or call it under torch.no_grad()")
+            setattr(self._e, name + "_stride", stride)
+        return rows
+
+    def _workspace(self, what: str, call, tokens: int, ws, dev: int, anywhere: bool):
+        if ws is None:
+            need = self._bytes(call, tokens, False, anywhere)
+            return torch.empty(need, dtype=torch.uint8, device=f"cuda:{dev}") if need else None
+        if ws.get_device() != dev or not ws.is_contiguous():
+            raise BaocError(E_INVALID, f"{what}: ws must be a contiguous buffer on the device of the others")
+        return ws
+
+    def product(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+        """out = act(x w^T + bias) + residual; pre (bf16, where given) takes the values before the activation.  out: allocated as
+        out_dtype (residual's type, else bf16) when not given; it may be residual.  Rows of all may be strided.  ws: device bytes, at
+        least ``workspace_bytes(tokens)``, more for strided or unaligned arrays (allocated when not given and needed)."""
+        bf, dev = (torch.bfloat16,), x.get_device()
+        if out is None:
+            out = torch.empty((*x.shape[:-1], self.n_out), dtype=out_dtype or (torch.bfloat16 if residual is None else residual.dtype), device=x.device)
+        n = self._take("product", None, self.n_in, bf, dev, x=x)
+        self._take("product", self.w_shape[0], self.w_shape[1], bf, dev, w=w)
+        self._take("product", n, self.n_out, tuple(DTYPES), dev, out=out)
+        self._take("product", n, self.n_out, (out.dtype,), dev, residual=residual)
+        self._take("product", n, self.n_out, bf, dev, pre=pre)
+        if bias is not None and (bias.dtype != torch.float32 or bias.numel() != self.n_out or not bias.is_contiguous() or bias.get_device() != dev):
+            raise BaocError(E_INVALID, f"product: bias must be a contiguous float32 vector of {self.n_out} elements on the device of x")
+        if bias is not None and bias.requires_grad and torch.is_grad_enabled():
+            raise BaocError(E_INVALID, "product: autograd does not see this call; detach bias, or call it under torch.no_grad()")
+        self._e.out_dtype, px, pw = DTYPES[out.dtype], x.data_ptr(), w.data_ptr()
+        ws = self._workspace("product", _lib.baoc_linear_workspace_bytes, n, ws, dev, (px | pw) & 15 != 0)
+        rc = _queue(dev, _lib.baoc_linear, self._ref, px, pw, _ptr(bias), _ptr(residual), n, out.data_ptr(), _ptr(pre),
+                    _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+        return out if rc >= 0 else self._failed(rc)
+
+    def grad(self, x: Optional[torch.Tensor], w: Optional[torch.Tensor], dout: torch.Tensor, pre: Optional[torch.Tensor] = None,
+             dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
+             ws: Optional[torch.Tensor] = None) -> None:
+        """Writes those of dx (bf16), dw (w's layout) and db (bf16 or fp32, alike) that are given.  dout: bf16; pre: what ``product``
+        kept, for a layer with an activation; x is needed for dw, w for dx.  ws: device bytes, at least
+        ``grad_workspace_bytes(tokens)``, more for strided or unaligned arrays (allocated when not given and needed)."""
+        bf, dev = (torch.bfloat16,), dout.get_device()
+        n = self._take("grad", None, self.n_out, bf, dev, dout=dout)
+        self._take("grad", n, self.n_out, bf, dev, pre=pre)
+        self._take("grad", n, self.n_in, bf, dev, x=x, dx=dx)
+        self._take("grad", self.w_shape[0], self.w_shape[1], bf, dev, w=w)
+        dtype = dw.dtype if dw is not None else (db.dtype if db is not None else torch.float32)
+        _dtype_code(dtype)
+        self._take("grad", self.w_shape[0], self.w_shape[1], (dtype,), dev, dw=dw)
+        if db is not None and (db.dtype != dtype or db.numel() != self.n_out or not db.is_contiguous() or db.get_device() != dev):
+            raise BaocError(E_INVALID, f"grad: db must be a contiguous vector of {self.n_out} elements of dw's type on the device of the others")
+        if (dx is not None and w is None) or (dw is not None and x is None) or (self.act != "none" and pre is None):
+            raise BaocError(E_INVALID, "grad: dx needs w, dw needs x, an activation needs pre")
+        self._e.grad_dtype = DTYPES[dtype]
+        anywhere = any(t is not None and t.data_ptr() & 15 for t in (x, w, dout))
+        ws = self._workspace("grad", _lib.baoc_linear_grad_workspace_bytes, n, ws, dev, anywhere)
+        rc = _queue(dev, _lib.baoc_linear_grad, self._ref, _ptr(x), _ptr(w), dout.data_ptr(), _ptr(pre), n, _ptr(dx), _ptr(dw), _ptr(db),
+                    _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+        return None if rc >= 0 else self._failed(rc)
 
 
 class Join:

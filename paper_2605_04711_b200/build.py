@@ -17,9 +17,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbaoc.so")
 LIB_CHECKED = os.path.join(HERE, "libbaoc_checked.so")     # the same sources with -DBAOC_CHECKED (see csrc/baoc_check.cuh)
 SOURCES = ["baoc_host.cpp", "baoc_partition.cpp", "baoc_api.cu", "baoc_stats.cu", "baoc_finalize.cu", "baoc_step.cu", "baoc_noalloc.cu",
-           "baoc_convert.cu", "baoc_clip.cu", "baoc_embed.cu", "baoc_logp.cu", "baoc_join.cu"]
+           "baoc_convert.cu", "baoc_clip.cu", "baoc_embed.cu", "baoc_logp.cu", "baoc_join.cu", "baoc_linear.cu"]
 HEADERS = [os.path.join(ROOT, "include", "baoc.h"), os.path.join(CSRC, "baoc_internal.h"),
-           os.path.join(CSRC, "baoc_device.cuh"), os.path.join(CSRC, "baoc_check.cuh")]
+           os.path.join(CSRC, "baoc_device.cuh"), os.path.join(CSRC, "baoc_check.cuh"), os.path.join(CSRC, "baoc_tensor.cuh")]
 
 
 def _nvcc() -> str:

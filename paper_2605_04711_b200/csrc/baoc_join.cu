@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
     if (!check_range(ck, kKerJoinGrad, part, int64_t(kJoinSums + 1) * dim * 4, 0)) return;
 #endif
     const bool need_f = g.post_w || g.gate;
-    float acc[kShared ? 1 : kSums][8];
+    float acc[kShared ? 1 : kSums][8] = {};
     auto add = [&](int k, int j, float v) {
         if constexpr (kShared) dynamic[(k * 8 + j) * kTeam + t] += v;
         else acc[k][j] += v;
@@ -315,8 +315,8 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
         for (int j = 0; j < 8; ++j)
             if (Stream::column(t, j) < dim) f(Stream::column(t, j), v[j]);
     };
-#pragma unroll
-    for (int k = 0; k < kSums; ++k) zero(k);
+    if constexpr (kShared)
+        for (int k = 0; k < kSums; ++k) zero(k);
     bool inside[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) inside[j] = Stream::column(t, j) < dim;

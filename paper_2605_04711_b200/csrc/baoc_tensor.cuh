@@ -1,0 +1,93 @@
+// Device and host helpers of the matrix product: barriers in shared memory with bounded waits, tiled asynchronous copies, the
+// tensor cores' descriptors and instructions (sm_100a), accumulators in tensor memory.
+#pragma once
+
+#include <cstdint>
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "baoc_device.cuh"
+
+namespace baoc {
+
+// ---- barriers --------------------------------------------------------------------
+// No wait is endless: one that takes longer than this reports false, and its caller gives the whole tile loop up.  (The longest
+// sum a CTA forms between two arrivals, 2^30 tokens, takes 3 s.)
+constexpr uint64_t kWaitNs = 10000000000ull;
+
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+    if (bar_try(bar, parity)) return true;
+    const uint64_t start = now_ns();
+    for (uint32_t i = 0; i < 0xffffffffu; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if ((i & 63) == 63 && now_ns() - start > kWaitNs) return false;
+    }
+    return false;
+}
+
+// ---- tiled copies ----------------------------------------------------------------
+// x (elements of the contiguous dimension) is a multiple of 64 bf16 everywhere: copies start on 128-byte boundaries of a row.
+__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void fetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+// ---- tensor cores ----------------------------------------------------------------
+// Shared-memory operand of 128-byte rows with the 128-byte swizzle that the tiled copy writes.  K-major: rows of 64 k, groups of
+// 8 rows 1024 bytes apart.  MN-major: rows of 64 m (or n), one row per k; groups of 8 k are 1024 bytes apart, the next 64 m
+// follow after `lead` bytes.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lead) {
+    return uint64_t((addr & 0x3ffff) >> 4) | uint64_t((lead & 0x3ffff) >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+// bf16 x bf16 into fp32
+__host__ __device__ constexpr uint32_t product_desc(int m, int n, bool a_mn, bool b_mn) {
+    return 1u << 4 | 1u << 7 | 1u << 10 | uint32_t(a_mn) << 15 | uint32_t(b_mn) << 16 | uint32_t(n >> 3) << 17 | uint32_t(m >> 4) << 24;
+}
+__device__ __forceinline__ void product(uint32_t acc, uint64_t a, uint64_t b, uint32_t desc, uint32_t add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(acc), "l"(a), "l"(b), "r"(desc), "r"(add) : "memory");
+}
+// the barrier is arrived at when the products issued so far are done
+__device__ __forceinline__ void product_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void acc_alloc(uint32_t where, uint32_t columns) {         // a whole warp
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void acc_free(uint32_t acc, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(acc), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void acc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void acc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// 32 columns of a thread's row (its warp's quarter of the 128 lanes)
+__device__ __forceinline__ void acc_load(uint32_t acc, float (&v)[32]) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(acc));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+}  // namespace baoc
