@@ -27,13 +27,22 @@ constexpr int64_t kLinearMaxTokens = int64_t(1) << 30, kLinearMaxStride = int64_
 constexpr int kWriters = 8;                          // warps of the epilogue
 constexpr int kProductThreads = 128 + 32 * kWriters;
 constexpr int kBand = 16;                            // tiles along m that are worked on side by side: their operands stay in L2
-constexpr int kStageBudget = 200 * 1024;             // shared memory of the ring
+constexpr int kSmemMost = 226 * 1024;                // shared memory of a CTA: the ring of stages, outputs on their way
+constexpr int kChunk = 8;                            // steps of 64 k
 
-template <int kN>
+// kCtas CTAs (a pair shares the tensor cores' work on a tile of 256 rows: each holds its 128 rows of A, half the columns' rows
+// of B, and its rows' accumulators, so that a stage of both feeds twice the products of one CTA's).
+// kChunked, for fp32 outputs: the tensor cores cut an accumulator's low bits off at every addition (2^-25 of it on average, always
+// towards zero; at k = 8192 random products the result is off by 9e-6, at 16384 positive ones by 8e-5), so every
+// kChunk steps the sums so far are added up in registers, rounded to nearest, and the accumulator starts again (5e-7).
+template <int kCtas, int kN, bool kChunked>
 struct TileShape {
-    static constexpr int kABytes = kTileM * kRowBytes, kBBytes = kN * kRowBytes, kStage = kABytes + kBBytes;
-    static constexpr int kStages = kStageBudget / kStage > 8 ? 8 : kStageBudget / kStage;
-    static constexpr int kSmem = kStages * kStage + 1024;
+    static constexpr int kBRows = kN / kCtas;
+    static constexpr int kABytes = kTileM * kRowBytes, kBBytes = kBRows * kRowBytes, kStage = kABytes + kBBytes;
+    static constexpr int kOutBytes = kChunked ? 4096 : 2048;         // 32 x 32 outputs of a writing warp, two of them
+    static constexpr int kOuts = kWriters * 2 * kOutBytes;
+    static constexpr int kStages = (kSmemMost - 1024 - kOuts) / kStage > 8 ? 8 : (kSmemMost - 1024 - kOuts) / kStage;
+    static constexpr int kSmem = kStages * kStage + kOuts + 1024;
     static constexpr int kColumns = 2 * kN;          // of tensor memory: two accumulators
 };
 
@@ -47,19 +56,48 @@ struct ProductArgs {
     const char* residual;
     const float* bias;
     int64_t out_step, pre_step, residual_step;      // bytes
-    int out_wide, pre_wide, residual_wide;           // 16-byte accesses fit
+    int out_wide, pre_wide, residual_wide;           // 16-byte accesses fit; out and pre are then stored by tiled copies
 };
 
-struct Maps { CUtensorMap a[3], b[3]; };
+struct Maps { CUtensorMap a[3], b[3], out, pre; };
 
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float exp2_approx(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
+// The normal distribution below -|z|, as e^(-z^2/2) times a polynomial in t = 1 / (1 + 0.35 |z|): erfc(x) e^(x^2) is smooth in
+// such a t.  The coefficients are a least-maximum fit of the relative error over |z| <= 15 (3.2e-8 in exact arithmetic, 5 2^-24
+// with the coefficients and every step in fp32); two approximate functions against some forty instructions of erfcf.
+// Returns it and, in *density, e^(-z^2/2).
+__device__ __forceinline__ float lower_tail(float z, float* density) {
+    const float t = rcp_approx(fmaf(0.35f, fabsf(z), 1.f));
+    float p = -0.02916380763053894f;
+    p = fmaf(p, t, 0.14406023919582367f);
+    p = fmaf(p, t, -0.2559007406234741f);
+    p = fmaf(p, t, 0.15939167141914368f);
+    p = fmaf(p, t, -0.02326301671564579f);
+    p = fmaf(p, t, 0.10557447373867035f);
+    p = fmaf(p, t, 0.11981557309627533f);
+    p = fmaf(p, t, 0.13986432552337646f);
+    p = fmaf(p, t, 0.13962125778198242f);
+    *density = exp2_approx(-0.5f * kLog2e * (z * z));
+    return p * t * *density;
+}
+__device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.f + exp2_approx(-kLog2e * z)); }
 
 template <int kAct>
 __device__ __forceinline__ float act_of(float z) {
     if constexpr (kAct == BAOC_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
-    if constexpr (kAct == BAOC_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    if constexpr (kAct == BAOC_ACT_GELU_TANH) return __fdividef(z, 1.f + __expf(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
-    if constexpr (kAct == BAOC_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+    if constexpr (kAct == BAOC_ACT_GELU) {
+        float d;
+        const float tail = lower_tail(z, &d);
+        return z * (z > 0.f ? 1.f - tail : tail);
+    }
+    if constexpr (kAct == BAOC_ACT_GELU_TANH) return z * sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
+    if constexpr (kAct == BAOC_ACT_SILU) return z * sigmoid(z);
     return z;
 }
 template <int kAct>
@@ -80,7 +118,12 @@ __device__ __forceinline__ void apply_act(float (&v)[32], int act) {
 __device__ __forceinline__ float act_slope(float z, int act) {
     switch (act) {
         case BAOC_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
-        case BAOC_ACT_GELU: return fabsf(z) > 15.f ? (z > 0.f ? 1.f : 0.f) : 0.5f * erfcf(-0.70710678118654752f * z) + 0.3989422804014327f * z * __expf(-0.5f * z * z);
+        case BAOC_ACT_GELU: {
+            if (fabsf(z) > 15.f) return z > 0.f ? 1.f : 0.f;
+            float d;
+            const float tail = lower_tail(z, &d);
+            return (z > 0.f ? 1.f - tail : tail) + 0.3989422804014327f * z * d;
+        }
         case BAOC_ACT_GELU_TANH: {
             if (fabsf(z) > 15.f) return z > 0.f ? 1.f : 0.f;
             const float s = sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
@@ -170,58 +213,121 @@ __device__ __forceinline__ void tile_place(int tile, int m_tiles, int n_tiles, i
     *mt = first + in - *nt * height;
 }
 
-template <int kN>
+// What a writing warp does with 32 columns of its 32 rows.
+struct Writer {
+    const ProductArgs& g;
+    const Maps& maps;
+    uint32_t buf;                    // two buffers of `bytes`
+    uint32_t bytes;
+    int lane, turn = 0;
+
+    // a thread's row of 32 values into the warp's buffer, as a tiled copy with swizzled rows expects it, and off
+    __device__ __forceinline__ void send(const CUtensorMap* map, int f32, int col, int row0, const float (&v)[32]) {
+        const uint32_t to = buf + turn * bytes;
+        turn ^= 1;
+        if (lane == 0) stores_read<1>();                   // (the store before last has left this buffer)
+        __syncwarp();
+        if (f32) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(to + lane * 128 + ((c ^ (lane & 7)) << 4)), "f"(v[4 * c]), "f"(v[4 * c + 1]), "f"(v[4 * c + 2]),
+                             "f"(v[4 * c + 3]) : "memory");
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)), "r"(pair_bf16(v[8 * c], v[8 * c + 1])),
+                             "r"(pair_bf16(v[8 * c + 2], v[8 * c + 3])), "r"(pair_bf16(v[8 * c + 4], v[8 * c + 5])), "r"(pair_bf16(v[8 * c + 6], v[8 * c + 7])) : "memory");
+        }
+        shared_to_async();
+        __syncwarp();
+        if (lane == 0) store_tile(map, to, col, row0);
+    }
+    // row0: the warp's first row (below m); the whole warp calls it
+    __device__ __forceinline__ void write(int64_t row0, int col, float (&v)[32]) {
+        const int left = min(32, g.n - col);
+        const int64_t row = row0 + lane;
+        const bool mine = row < g.m;
+        if (g.bias) {
+            if (left == 32 && (reinterpret_cast<uintptr_t>(g.bias) & 15) == 0) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 b = __ldg(reinterpret_cast<const float4*>(g.bias + col + i));
+                    v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] += i < left ? __ldg(g.bias + col + i) : 0.f;
+            }
+        }
+        if (g.pre) {
+            if (g.pre_wide) send(&maps.pre, 0, col, int(row0), v);
+            else if (mine) store_columns(g.pre + row * g.pre_step, col, left, 0, 0, v);
+        }
+        apply_act(v, g.act);
+        if (g.residual && mine) add_columns(g.residual + row * g.residual_step, col, left, g.out_f32, g.residual_wide, v);
+        if (g.out_wide) send(&maps.out, g.out_f32, col, int(row0), v);
+        else if (mine) store_columns(g.out + row * g.out_step, col, left, g.out_f32, 0, v);
+        __syncwarp();
+    }
+};
+
+template <int kCtas, int kN, bool kChunked>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Maps maps, const ProductArgs g) {
-    using T = TileShape<kN>;
+    using T = TileShape<kCtas, kN, kChunked>;
     constexpr int kS = T::kStages;
     extern __shared__ char raw[];
     __shared__ uint64_t bars[2 * kS + 5];
     __shared__ uint32_t acc_at;
     __shared__ int failed;
-    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u, bar0 = smem_addr(bars);
+    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u, outs = ring + kS * T::kStage, bar0 = smem_addr(bars);
     auto full = [&](int s) { return bar0 + 8 * s; };
     auto empty = [&](int s) { return bar0 + 8 * (kS + s); };
     auto acc_full = [&](int a) { return bar0 + 8 * (2 * kS + a); };
     auto acc_empty = [&](int a) { return bar0 + 8 * (2 * kS + 2 + a); };
     const uint32_t drained = bar0 + 8 * (2 * kS + 4);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int m_tiles = (g.m + kTileM - 1) / kTileM, n_tiles = (g.n + kN - 1) / kN, tiles = m_tiles * n_tiles, steps = g.k_tiles * g.passes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = kCtas == 2 ? int(cluster_rank()) : 0;
+    const int worker = int(blockIdx.x) / kCtas, workers = int(gridDim.x) / kCtas;
+    const int m_tiles = (g.m + kTileM * kCtas - 1) / (kTileM * kCtas), n_tiles = (g.n + kN - 1) / kN, tiles = m_tiles * n_tiles, steps = g.k_tiles * g.passes;
+    const int chunk = kChunked ? kChunk : steps, chunks = (steps + chunk - 1) / chunk;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kS; ++s) { bar_init(full(s), 1); bar_init(empty(s), 1); }
-        for (int a = 0; a < 2; ++a) { bar_init(acc_full(a), 1); bar_init(acc_empty(a), kWriters); }
+        for (int a = 0; a < 2; ++a) { bar_init(acc_full(a), 1); bar_init(acc_empty(a), kWriters * kCtas); }
         bar_init(drained, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        shared_to_async();
     }
-    if (warp == 2) acc_alloc(smem_addr(&acc_at), T::kColumns);
+    if (warp == 2) acc_alloc<kCtas>(smem_addr(&acc_at), T::kColumns);
     acc_fence_before();
-    __syncthreads();
+    if constexpr (kCtas == 2) cluster_barrier();
+    else __syncthreads();
     acc_fence_after();
     const uint32_t acc = acc_at;
 
-    if (warp == 0 && lane == 0) {                     // copies
+    if (warp == 0 && lane == 0) {                     // copies: each CTA its own operands, a pair's bytes counted by its first CTA
         int s = 0, round = 0, issued = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+        for (int tile = worker; ok && tile < tiles; tile += workers) {
             int mt, nt;
             tile_place(tile, m_tiles, n_tiles, &mt, &nt);
+            const int m0 = (mt * kCtas + rank) * kTileM, n0 = nt * kN + rank * T::kBRows;
             for (int i = 0; i < steps; ++i) {
                 if (!(ok = bar_wait(empty(s), (round & 1) ^ 1))) break;
-                bar_expect(full(s), T::kStage);
+                if (rank == 0) bar_expect(full(s), T::kStage * kCtas);
+                const uint32_t bar = kCtas == 2 ? at_rank(full(s), 0) : full(s);
                 const int pass = (i >= g.k_tiles) + (i >= 2 * g.k_tiles), k = (i - pass * g.k_tiles) * kTileK;
                 const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
                 if (g.a_mn) {
 #pragma unroll
-                    for (int c = 0; c < kTileM / 64; ++c) copy_tile(a + c * 64 * kRowBytes, &maps.a[pass], mt * kTileM + c * 64, k, full(s));
+                    for (int c = 0; c < kTileM / 64; ++c) copy_tile<kCtas>(a + c * 64 * kRowBytes, &maps.a[pass], m0 + c * 64, k, bar);
                 } else {
-                    copy_tile(a, &maps.a[pass], k, mt * kTileM, full(s));
+                    copy_tile<kCtas>(a, &maps.a[pass], k, m0, bar);
                 }
                 if (g.b_mn) {
 #pragma unroll
-                    for (int c = 0; c < kN / 64; ++c) copy_tile(b + c * 64 * kRowBytes, &maps.b[pass], nt * kN + c * 64, k, full(s));
+                    for (int c = 0; c < T::kBRows / 64; ++c) copy_tile<kCtas>(b + c * 64 * kRowBytes, &maps.b[pass], n0 + c * 64, k, bar);
                 } else {
-                    copy_tile(b, &maps.b[pass], k, nt * kN, full(s));
+                    copy_tile<kCtas>(b, &maps.b[pass], k, n0, bar);
                 }
                 ++issued;
                 if (++s == kS) { s = 0; ++round; }
@@ -229,73 +335,95 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
         if (!ok) {
             failed = 1;
-            // this CTA's copies have to have landed before its shared memory goes: stage j was filled (issued - 1 - j) / kS + 1 times
-            for (int j = 0; j < min(issued, kS); ++j) bar_wait(full(j), ((issued - 1 - j) / kS) & 1);
+            // this CTA's copies have to have landed before its shared memory goes: the j-th last one was fill (issued - 1 - j) of the ring
+            if (rank == 0)
+                for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
         }
-    } else if (warp == 1 && lane == 0) {              // products
-        const uint32_t desc = product_desc(kTileM, kN, g.a_mn, g.b_mn);
+    } else if (warp == 1 && lane == 0 && rank == 0) { // products
+        const uint32_t desc = product_desc(kTileM * kCtas, kN, g.a_mn, g.b_mn);
         const uint32_t a_step = g.a_mn ? 16 * kRowBytes : 32, b_step = g.b_mn ? 16 * kRowBytes : 32;    // bytes per 16 k
         int s = 0, round = 0, count = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++count) {
-            const int half = count & 1;
-            if (!(ok = bar_wait(acc_empty(half), ((count >> 1) & 1) ^ 1))) break;
-            acc_fence_after();
-            const uint32_t d = acc + half * kN;
-            for (int i = 0; i < steps; ++i) {
-                if (!(ok = bar_wait(full(s), round & 1))) break;
-                const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
+        for (int tile = worker; ok && tile < tiles; tile += workers) {
+            for (int first = 0; ok && first < steps; first += chunk, ++count) {
+                const int half = count & 1, last = min(steps, first + chunk);
+                if (!(ok = bar_wait(acc_empty(half), ((count >> 1) & 1) ^ 1))) break;
+                acc_fence_after();
+                const uint32_t d = acc + half * kN;
+                for (int i = first; i < last; ++i) {
+                    if (!(ok = bar_wait(full(s), round & 1))) break;
+                    acc_fence_after();
+                    const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
 #pragma unroll
-                for (int k = 0; k < kTileK / 16; ++k)
-                    product(d, operand_desc(a + k * a_step, 64 * kRowBytes), operand_desc(b + k * b_step, 64 * kRowBytes), desc, i > 0 || k > 0);
-                product_commit(empty(s));
-                if (++s == kS) { s = 0; ++round; }
+                    for (int k = 0; k < kTileK / 16; ++k)
+                        product<kCtas>(d, operand_desc(a + k * a_step, 64 * kRowBytes), operand_desc(b + k * b_step, 64 * kRowBytes), desc, i > first || k > 0);
+                    product_commit<kCtas>(empty(s));
+                    if (++s == kS) { s = 0; ++round; }
+                }
+                product_commit<kCtas>(acc_full(half));
             }
-            product_commit(acc_full(half));
         }
         if (!ok) {                                    // (products in flight read shared and write tensor memory)
             failed = 1;
-            product_commit(drained);
+            product_commit<kCtas>(drained);
             bar_wait(drained, 0);
         }
     } else if (warp >= 4) {                           // write out
         const int quarter = warp & 3, side = (warp - 4) >> 2;       // a warp reads its quarter of the lanes alone
+        constexpr int kCols = kN / 2;
+        Writer writer{g, maps, outs + (warp - 4) * 2 * T::kOutBytes, T::kOutBytes, lane};
         int count = 0;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++count) {
-            const int half = count & 1;
+        bool ok = true;
+        for (int tile = worker; ok && tile < tiles; tile += workers) {
             int mt, nt;
             tile_place(tile, m_tiles, n_tiles, &mt, &nt);
-            if (!bar_wait(acc_full(half), (count >> 1) & 1)) { failed = 1; break; }
-            acc_fence_after();
-            const int64_t row = int64_t(mt) * kTileM + quarter * 32 + lane;
-            for (int c = side * (kN / 2); c < (side + 1) * (kN / 2); c += 32) {
-                const int col = nt * kN + c, left = min(32, g.n - col);
-                if (left <= 0) break;                 // (alike in the warp)
-                float v[32];
-                acc_load(acc + half * kN + (uint32_t(quarter * 32) << 16) + c, v);
-                if (row < g.m) {
-                    if (g.bias) {
+            const int64_t row0 = (int64_t(mt) * kCtas + rank) * kTileM + quarter * 32;
+            const int col0 = nt * kN + side * kCols;
+            float total[kChunked ? kCols / 32 : 1][32];
+            for (int c = 0; c < chunks; ++c, ++count) {
+                const int half = count & 1;
+                if (!(ok = bar_wait(acc_full(half), (count >> 1) & 1))) break;
+                acc_fence_after();
+                const uint32_t at = acc + half * kN + (uint32_t(quarter * 32) << 16) + side * kCols;
+                if constexpr (kChunked) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] += i < left ? __ldg(g.bias + col + i) : 0.f;
+                    for (int p = 0; p < kCols / 32; ++p) {
+                        float v[32];
+                        acc_load(at + p * 32, v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) total[p][i] = c == 0 ? v[i] : total[p][i] + v[i];
                     }
-                    if (g.pre) store_columns(g.pre + row * g.pre_step, col, left, 0, g.pre_wide, v);
-                    apply_act(v, g.act);
-                    if (g.residual) add_columns(g.residual + row * g.residual_step, col, left, g.out_f32, g.residual_wide, v);
-                    store_columns(g.out + row * g.out_step, col, left, g.out_f32, g.out_wide, v);
+                } else {
+                    for (int p = 0; p < kCols && col0 + p < g.n && row0 < g.m; p += 32) {      // (alike in the warp)
+                        acc_load(at + p, total[0]);
+                        writer.write(row0, col0 + p, total[0]);
+                    }
                 }
-                __syncwarp();                         // (the next load is the whole warp's)
+                acc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (kCtas == 2) bar_arrive_at(acc_empty(half), 0);
+                    else bar_arrive(acc_empty(half));
+                }
             }
-            acc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(acc_empty(half));
+            if constexpr (kChunked) {
+                if (ok && row0 < g.m) {
+#pragma unroll
+                    for (int p = 0; p < kCols / 32; ++p)
+                        if (col0 + p * 32 < g.n) writer.write(row0, col0 + p * 32, total[p]);
+                }
+            }
         }
+        if (!ok) failed = 1;
+        if (lane == 0) stores_read<0>();
     }
     __syncwarp();
     acc_fence_before();
-    __syncthreads();
+    if constexpr (kCtas == 2) cluster_barrier();      // (the first CTA's products read the second one's shared memory)
+    else __syncthreads();
     if (warp == 2) {
         acc_fence_after();
-        acc_free(acc, T::kColumns);
+        acc_free<kCtas>(acc, T::kColumns);
     }
     if (threadIdx.x == 0 && failed) atomicAdd(&g_gave_up, 1u);
 }
@@ -326,6 +454,7 @@ __global__ void __launch_bounds__(kThreads) repack_kernel(const Repacks g) {
 
 // dz = dout * act'(pre) as bf16 (and what the rounding left, as two bf16 more, where dw is wanted in fp32), and its column sums.
 // A CTA has 256 columns and rows_per_part rows: a lane 8 columns, a warp every eighth row.
+constexpr int kSlopeRows = 4;        // rows a warp has in flight
 struct SlopeArgs {
     const char *dout, *pre;
     char *dz, *dz_mid, *dz_low;      // null: not wanted
@@ -349,35 +478,41 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
     const int64_t first = int64_t(blockIdx.y) * g.rows_per_part, end = min64(g.rows, first + g.rows_per_part);
     float sum[8] = {};
     let_later_kernel_start();
+    auto one_row = [&](int64_t row, float (&d)[8], const float (&z)[8]) {
+        if (g.act != BAOC_ACT_NONE) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], g.act);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += d[j];
+        if (!g.dz) return;
+        const uint4 w = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
+        const int64_t at = row * g.dz_step + 2 * int64_t(col);
+        *reinterpret_cast<uint4*>(g.dz + at) = w;
+        if (!g.dz_mid) return;
+        float h[8];
+        unpack8(w, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] -= h[j];
+        const uint4 m = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
+        *reinterpret_cast<uint4*>(g.dz_mid + at) = m;
+        unpack8(m, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] -= h[j];
+        *reinterpret_cast<uint4*>(g.dz_low + at) = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
+    };
     if (col < g.n)
-        for (int64_t row = first + warp; row < end; row += 8) {
-            float d[8];
-            load8(g.dout + row * g.dout_step, col, g.n, g.wide, d);
-            if (g.act != BAOC_ACT_NONE) {
-                float z[8];
-                load8(g.pre + row * g.pre_step, col, g.n, g.wide, z);
+        for (int64_t row = first + warp; row < end; row += 8 * kSlopeRows) {
+            float d[kSlopeRows][8], z[kSlopeRows][8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], g.act);
+            for (int r = 0; r < kSlopeRows; ++r) {
+                const int64_t at = min64(row + 8 * r, end - 1);          // (a row too many is read, not used)
+                load8(g.dout + at * g.dout_step, col, g.n, g.wide, d[r]);
+                if (g.act != BAOC_ACT_NONE) load8(g.pre + at * g.pre_step, col, g.n, g.wide, z[r]);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += d[j];
-            if (g.dz) {
-                const uint4 w = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
-                *reinterpret_cast<uint4*>(g.dz + row * g.dz_step + 2 * int64_t(col)) = w;
-                if (g.dz_mid) {
-                    float h[8];
-                    unpack8(w, h);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[j] -= h[j];
-                    const uint4 m = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
-                    *reinterpret_cast<uint4*>(g.dz_mid + row * g.dz_step + 2 * int64_t(col)) = m;
-                    unpack8(m, h);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[j] -= h[j];
-                    *reinterpret_cast<uint4*>(g.dz_low + row * g.dz_step + 2 * int64_t(col)) =
-                        make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
-                }
-            }
+            for (int r = 0; r < kSlopeRows; ++r)
+                if (row + 8 * r < end) one_row(row + 8 * r, d[r], z[r]);
         }
     if (!g.part) return;
 #pragma unroll
@@ -471,47 +606,64 @@ EncodeFn encode_fn() {
     return reinterpret_cast<EncodeFn>(f);
 }
 
-// Boxes of 64 contiguous elements by box_rows rows, laid out with the 128-byte swizzle; zeros outside.
-bool encode(CUtensorMap* map, const Matrix& t, int box_rows) {
+// Boxes of box_cols contiguous elements (64 or 128 bytes, laid out with the swizzle of that width) by box_rows rows; zeros outside.
+bool encode(CUtensorMap* map, const Matrix& t, int box_rows, int box_cols = 64) {
     EncodeFn f = encode_fn();
     if (!f) return false;
     const cuuint64_t dims[2] = {cuuint64_t(t.cols), cuuint64_t(t.rows)}, strides[1] = {cuuint64_t(t.step)};
-    const cuuint32_t box[2] = {64, cuuint32_t(box_rows)}, unit[2] = {1, 1};
-    return f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<char*>(t.p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t box[2] = {cuuint32_t(box_cols), cuuint32_t(box_rows)}, unit[2] = {1, 1};
+    return f(map, t.eb == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<char*>(t.p), dims, strides, box, unit,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols * t.eb == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // A product's operands: a as [m][k] or, a_mn, as [k][m]; b as [n][k] or [k][n]; up to three pairs whose products are added.
 struct Operands { const Matrix *a[3], *b[3]; };
 
-template <int kN>
-int launch_product(const Operands& o, ProductArgs g, cudaStream_t s) {
-    using T = TileShape<kN>;
+template <int kCtas, int kN, bool kChunked>
+int launch_product(const Operands& o, const Matrix& out, const Matrix& pre, const ProductArgs& g, cudaStream_t s) {
+    using T = TileShape<kCtas, kN, kChunked>;
+    static_assert(T::kStages >= 4 && T::kSmem <= 227 * 1024 - 512, "the ring, the outputs and the barriers share 227 KB");
+    auto kernel = product_kernel<kCtas, kN, kChunked>;
     static std::atomic<uint64_t> allowed{0};         // the permission for large shared memory is per device and lasts
     int dev = 0;
     cudaError_t ce = cudaGetDevice(&dev);
     if (ce != cudaSuccess) return launched(ce, "product_kernel");
     const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        ce = cudaFuncSetAttribute(product_kernel<kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+        ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
         if (ce != cudaSuccess) return launched(ce, "product_kernel");
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
     Maps maps;
-    for (int i = 0; i < g.passes; ++i)
-        if (!encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : kTileM) || !encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : kN))
-            return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
-    const int64_t tiles = ceil_div(g.m, kTileM) * ceil_div(g.n, kN);
+    bool ok = true;
+    for (int i = 0; i < g.passes; ++i) ok = ok && encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : kTileM) && encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : T::kBRows);
+    if (g.out_wide) ok = ok && encode(&maps.out, out, 32, 32);
+    if (g.pre && g.pre_wide) ok = ok && encode(&maps.pre, pre, 32, 32);
+    if (!ok) return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
+    const int64_t tiles = ceil_div(g.m, kTileM * kCtas) * ceil_div(g.n, kN);
     if (tiles > 0x7fffffff - 148) return fail_linear(BAOC_E_INVALID, "too many tiles for one launch");
-    product_kernel<kN><<<unsigned(std::min<int64_t>(tiles, 148)), kProductThreads, T::kSmem, s>>>(maps, g);
-    return launched(cudaGetLastError(), "product_kernel");
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = kCtas; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(std::min<int64_t>(tiles, 148 / kCtas) * kCtas)); cfg.blockDim = dim3(kProductThreads); cfg.dynamicSmemBytes = T::kSmem; cfg.stream = s;
+    cfg.attrs = &at; cfg.numAttrs = kCtas > 1 ? 1 : 0;
+    return launched(cudaLaunchKernelEx(&cfg, kernel, maps, g), "product_kernel");
 }
 
-int form_product(const Operands& o, const ProductArgs& g, cudaStream_t s) {
-    const int64_t m_tiles = ceil_div(g.m, kTileM);
-    if (m_tiles * ceil_div(g.n, 256) >= 148) return launch_product<256>(o, g, s);
-    if (m_tiles * ceil_div(g.n, 128) >= 148) return launch_product<128>(o, g, s);
-    return launch_product<64>(o, g, s);
+// The largest tiles that still give every CTA one; g has its sizes and flags, out and pre are where it goes.
+int form_product(const Operands& o, const Matrix& out, const Matrix& pre, ProductArgs g, cudaStream_t s) {
+    g.out = const_cast<char*>(out.p); g.out_step = out.step; g.out_f32 = out.eb == 4; g.out_wide = out.wide();
+    g.pre = const_cast<char*>(pre.p); g.pre_step = pre.step; g.pre_wide = pre.wide();
+    const int64_t pairs = ceil_div(g.m, 2 * kTileM), ones = ceil_div(g.m, kTileM);
+    if (g.out_f32) {
+        if (pairs * ceil_div(g.n, 128) >= 74) return launch_product<2, 128, true>(o, out, pre, g, s);
+        return launch_product<1, 64, true>(o, out, pre, g, s);
+    }
+    if (pairs * ceil_div(g.n, 256) >= 74) return launch_product<2, 256, false>(o, out, pre, g, s);
+    if (ones * ceil_div(g.n, 128) >= 148) return launch_product<1, 128, false>(o, out, pre, g, s);
+    return launch_product<1, 64, false>(o, out, pre, g, s);
 }
 
 // Matrices that a tiled copy cannot read go through the workspace: `at` is where the next one may lie.
@@ -626,11 +778,9 @@ int baoc_linear(const baoc_linear_t* e, const void* x, const void* w, const floa
     ProductArgs g{};
     g.m = int(tokens); g.n = e->n_out; g.k_tiles = int(ceil_div(e->n_in, kTileK)); g.passes = 1;
     g.b_mn = !out_in;
-    g.act = e->act; g.out_f32 = e->out_dtype == BAOC_F32;
-    g.out = static_cast<char*>(out); g.pre = static_cast<char*>(pre); g.residual = mr.p; g.bias = bias;
-    g.out_step = mo.step; g.pre_step = mp.step; g.residual_step = mr.step;
-    g.out_wide = mo.wide(); g.pre_wide = mp.wide(); g.residual_wide = mr.wide();
-    return form_product(Operands{{&a}, {&b}}, g, s);
+    g.act = e->act; g.bias = bias;
+    g.residual = mr.p; g.residual_step = mr.step; g.residual_wide = mr.wide();
+    return form_product(Operands{{&a}, {&b}}, mo, mp, g, s);
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
 }
@@ -712,20 +862,19 @@ int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const
                                                    static_cast<char*>(db), int(e->grad_dtype == BAOC_F32)), "slope_sums_kernel")))
             return rc;
     }
+    const Matrix none(nullptr, 0, 0, 0, BAOC_BF16);
     if (dx) {
         ProductArgs p{};
         p.m = int(tokens); p.n = e->n_in; p.k_tiles = int(ceil_div(e->n_out, kTileK)); p.passes = 1;
         p.b_mn = out_in;
-        p.out = static_cast<char*>(dx); p.out_step = mdx.step; p.out_wide = mdx.wide();
-        if ((rc = form_product(Operands{{&dz}, {&bw}}, p, s))) return rc;
+        if ((rc = form_product(Operands{{&dz}, {&bw}}, mdx, none, p, s))) return rc;
     }
     if (dw) {
         ProductArgs p{};
         p.m = int(w_rows); p.n = int(w_cols); p.k_tiles = int(ceil_div(tokens, kTileK)); p.passes = split ? 3 : 1;
         p.a_mn = p.b_mn = 1;
-        p.out = static_cast<char*>(dw); p.out_step = mdw.step; p.out_wide = mdw.wide(); p.out_f32 = e->grad_dtype == BAOC_F32;
         const Operands o = out_in ? Operands{{&dz, &mid, &low}, {&bx, &bx, &bx}} : Operands{{&bx, &bx, &bx}, {&dz, &mid, &low}};
-        if ((rc = form_product(o, p, s))) return rc;
+        if ((rc = form_product(o, mdw, none, p, s))) return rc;
     }
     return BAOC_OK;
 } catch (const std::bad_alloc&) {
