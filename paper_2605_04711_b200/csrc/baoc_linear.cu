@@ -51,6 +51,7 @@ __device__ unsigned int g_gave_up;                   // CTAs in which a wait ran
 struct ProductArgs {
     int m, n, k_tiles, passes;       // passes: products of as many operand pairs are added up
     int a_mn, b_mn;                  // the operand's m (n) lies contiguous, not its k
+    int a_rows;                      // rows of A that a copy brings: fewer than a tile's where m is smaller
     int act, out_f32;
     char *out, *pre;
     const char* residual;
@@ -101,41 +102,38 @@ __device__ __forceinline__ float act_of(float z) {
     return z;
 }
 template <int kAct>
-__device__ __forceinline__ void act_all(float (&v)[32]) {
+__device__ __forceinline__ void act_all(float* v, int n) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = act_of<kAct>(v[i]);
+    for (int i = 0; i < n; ++i) v[i] = act_of<kAct>(v[i]);
 }
-__device__ __forceinline__ void apply_act(float (&v)[32], int act) {
+template <int kCount>
+__device__ __forceinline__ void apply_act(float (&v)[kCount], int act) {
     switch (act) {
-        case BAOC_ACT_RELU: act_all<BAOC_ACT_RELU>(v); break;
-        case BAOC_ACT_GELU: act_all<BAOC_ACT_GELU>(v); break;
-        case BAOC_ACT_GELU_TANH: act_all<BAOC_ACT_GELU_TANH>(v); break;
-        case BAOC_ACT_SILU: act_all<BAOC_ACT_SILU>(v); break;
+        case BAOC_ACT_RELU: act_all<BAOC_ACT_RELU>(v, kCount); break;
+        case BAOC_ACT_GELU: act_all<BAOC_ACT_GELU>(v, kCount); break;
+        case BAOC_ACT_GELU_TANH: act_all<BAOC_ACT_GELU_TANH>(v, kCount); break;
+        case BAOC_ACT_SILU: act_all<BAOC_ACT_SILU>(v, kCount); break;
         default: break;
     }
 }
 // (past the ends below the derivative is 0 or 1 to all bits, and its formula would form inf * 0)
-__device__ __forceinline__ float act_slope(float z, int act) {
-    switch (act) {
-        case BAOC_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
-        case BAOC_ACT_GELU: {
-            if (fabsf(z) > 15.f) return z > 0.f ? 1.f : 0.f;
-            float d;
-            const float tail = lower_tail(z, &d);
-            return (z > 0.f ? 1.f - tail : tail) + 0.3989422804014327f * z * d;
-        }
-        case BAOC_ACT_GELU_TANH: {
-            if (fabsf(z) > 15.f) return z > 0.f ? 1.f : 0.f;
-            const float s = sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
-            return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * z * z);
-        }
-        case BAOC_ACT_SILU: {
-            if (fabsf(z) > 90.f) return z > 0.f ? 1.f : 0.f;
-            const float s = sigmoid(z);
-            return s * (1.f + z * (1.f - s));
-        }
-        default: return 1.f;
+template <int kAct>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (kAct == BAOC_ACT_RELU) {
+        return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    } else if constexpr (kAct == BAOC_ACT_GELU) {
+        float d;
+        const float y = fminf(fmaxf(z, -15.f), 15.f), tail = lower_tail(y, &d), r = (y > 0.f ? 1.f - tail : tail) + 0.3989422804014327f * y * d;
+        return z != z ? z : r;
+    } else if constexpr (kAct == BAOC_ACT_GELU_TANH) {
+        const float y = fminf(fmaxf(z, -15.f), 15.f), s = sigmoid(1.5957691216057308f * (y + 0.044715f * y * y * y));
+        const float r = s + y * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * y * y);
+        return z != z ? z : r;
+    } else if constexpr (kAct == BAOC_ACT_SILU) {
+        const float y = fminf(fmaxf(z, -90.f), 90.f), s = sigmoid(y), r = s * (1.f + y * (1.f - s));
+        return z != z ? z : r;
     }
+    return 1.f;
 }
 
 __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
@@ -203,6 +201,24 @@ __device__ __forceinline__ void add_columns(const char* row, int64_t col, int co
             for (int i = 0; i < 32; ++i)
                 if (i < count) v[i] += bf16_bits_to_float(p[i]);
         }
+    }
+}
+
+__device__ __forceinline__ void store4(char* row, int64_t col, int count, int f32, int wide, const float (&v)[4]) {
+    if (f32) {
+        float* p = reinterpret_cast<float*>(row) + col;
+        if (wide && count == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) p[i] = v[i];
+    } else {
+        uint16_t* p = reinterpret_cast<uint16_t*>(row) + col;
+        if (wide && count == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]));
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) p[i] = one_bf16(v[i]);
     }
 }
 
@@ -313,7 +329,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const int m0 = (mt * kCtas + rank) * kTileM, n0 = nt * kN + rank * T::kBRows;
             for (int i = 0; i < steps; ++i) {
                 if (!(ok = bar_wait(empty(s), (round & 1) ^ 1))) break;
-                if (rank == 0) bar_expect(full(s), T::kStage * kCtas);
+                if (rank == 0) bar_expect(full(s), (g.a_rows * kRowBytes + T::kBBytes) * kCtas);
                 const uint32_t bar = kCtas == 2 ? at_rank(full(s), 0) : full(s);
                 const int pass = (i >= g.k_tiles) + (i >= 2 * g.k_tiles), k = (i - pass * g.k_tiles) * kTileK;
                 const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
@@ -428,6 +444,162 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if (threadIdx.x == 0 && failed) atomicAdd(&g_gave_up, 1u);
 }
 
+// ---- few tiles: the sum over k is split --------------------------------------------------------------------------------
+// A cluster of CTAs shares one tile of 128 x 64, each a run of the steps over k; their sums meet in shared memory, where every
+// CTA reads its part of the tile from all of them, adds in order of rank and writes it out.  One tile of few rows is bound by the
+// reading of B: two CTAs per SM keep 64 KB of it in flight.
+constexpr int kSplitN = 64, kSplitStages = 4, kSplitWriters = 4, kSplitMost = 8;
+constexpr int kSplitThreads = 128 + 32 * kSplitWriters;
+constexpr int kSplitStage = (kTileM + kSplitN) * kRowBytes, kSplitSmem = kSplitStages * kSplitStage + 1024;
+
+__device__ __forceinline__ float4 load_at_rank(uint32_t addr, uint32_t rank) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at_rank(addr, rank)) : "memory");
+    return v;
+}
+// where 16 bytes (4 sums) of the tile lie: rows of 256 bytes, spread over the banks
+__device__ __forceinline__ uint32_t sum_place(int row, int four) { return uint32_t(row * 256 + ((four ^ (row & 15)) << 4)); }
+
+__global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const __grid_constant__ Maps maps, const ProductArgs g, int parts) {
+    constexpr int kS = kSplitStages;
+    extern __shared__ char raw[];
+    __shared__ uint64_t bars[2 * kS + 5];
+    __shared__ uint32_t acc_at;
+    __shared__ int failed;
+    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u, bar0 = smem_addr(bars);
+    auto full = [&](int s) { return bar0 + 8 * s; };
+    auto empty = [&](int s) { return bar0 + 8 * (kS + s); };
+    auto acc_full = [&](int a) { return bar0 + 8 * (2 * kS + a); };
+    auto acc_empty = [&](int a) { return bar0 + 8 * (2 * kS + 2 + a); };
+    const uint32_t drained = bar0 + 8 * (2 * kS + 4);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = int(cluster_rank()), tile = int(blockIdx.x) / parts;
+    const int n_tiles = (g.n + kSplitN - 1) / kSplitN, mt = tile / n_tiles, nt = tile - mt * n_tiles;
+    const int total_steps = g.k_tiles * g.passes, from = int(int64_t(total_steps) * rank / parts), to = int(int64_t(total_steps) * (rank + 1) / parts);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kS; ++s) { bar_init(full(s), 1); bar_init(empty(s), 1); }
+        for (int a = 0; a < 2; ++a) { bar_init(acc_full(a), 1); bar_init(acc_empty(a), kSplitWriters); }
+        bar_init(drained, 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        shared_to_async();
+    }
+    if (warp == 2) acc_alloc<1>(smem_addr(&acc_at), 2 * kSplitN);
+    acc_fence_before();
+    __syncthreads();
+    acc_fence_after();
+    const uint32_t acc = acc_at;
+    if (warp == 0 && lane == 0) {
+        bool ok = true;
+        int issued = 0;
+        for (int i = from; i < to; ++i, ++issued) {
+            const int s = issued % kS;
+            if (!(ok = bar_wait(empty(s), (issued / kS & 1) ^ 1))) break;
+            bar_expect(full(s), (g.a_rows + kSplitN) * kRowBytes);
+            const int pass = (i >= g.k_tiles) + (i >= 2 * g.k_tiles), k = (i - pass * g.k_tiles) * kTileK;
+            const uint32_t a = ring + s * kSplitStage, b = a + kTileM * kRowBytes;
+            if (g.a_mn) {
+#pragma unroll
+                for (int c = 0; c < kTileM / 64; ++c) copy_tile<1>(a + c * 64 * kRowBytes, &maps.a[pass], mt * kTileM + c * 64, k, full(s));
+            } else {
+                copy_tile<1>(a, &maps.a[pass], k, mt * kTileM, full(s));
+            }
+            if (g.b_mn) copy_tile<1>(b, &maps.b[pass], nt * kSplitN, k, full(s));
+            else copy_tile<1>(b, &maps.b[pass], k, nt * kSplitN, full(s));
+        }
+        if (!ok) {
+            failed = 1;
+            for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
+        }
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t desc = product_desc(kTileM, kSplitN, g.a_mn, g.b_mn);
+        const uint32_t a_step = g.a_mn ? 16 * kRowBytes : 32, b_step = g.b_mn ? 16 * kRowBytes : 32;
+        bool ok = true;
+        for (int i = 0; ok && i < to - from; ++i) {
+            const int s = i % kS, half = (i / kChunk) & 1;
+            if (i % kChunk == 0) {
+                if (!(ok = bar_wait(acc_empty(half), (i / kChunk >> 1 & 1) ^ 1))) break;
+                acc_fence_after();
+            }
+            if (!(ok = bar_wait(full(s), i / kS & 1))) break;
+            acc_fence_after();
+            const uint32_t a = ring + s * kSplitStage, b = a + kTileM * kRowBytes;
+#pragma unroll
+            for (int k = 0; k < kTileK / 16; ++k)
+                product<1>(acc + half * kSplitN, operand_desc(a + k * a_step, 64 * kRowBytes), operand_desc(b + k * b_step, 64 * kRowBytes), desc, i % kChunk > 0 || k > 0);
+            product_commit<1>(empty(s));
+            if (i % kChunk == kChunk - 1 || i == to - from - 1) product_commit<1>(acc_full(half));
+        }
+        if (!ok) {
+            failed = 1;
+            product_commit<1>(drained);
+            bar_wait(drained, 0);
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        float total[2][32];
+        bool ok = true;
+        for (int c = 0; c * kChunk < to - from; ++c) {
+            if (!(ok = bar_wait(acc_full(c & 1), c >> 1 & 1))) break;
+            acc_fence_after();
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                float v[32];
+                acc_load(acc + (c & 1) * kSplitN + (uint32_t(quarter * 32) << 16) + p * 32, v);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) total[p][i] = c == 0 ? v[i] : total[p][i] + v[i];
+            }
+            acc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(acc_empty(c & 1));
+        }
+        if (!ok) failed = 1;
+        // (the last product is done: the ring's stages are free)
+        if (mt * kTileM + row < g.m)
+#pragma unroll
+            for (int f = 0; f < 16; ++f)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(ring + sum_place(row, f)), "f"(total[f / 8][f % 8 * 4]), "f"(total[f / 8][f % 8 * 4 + 1]),
+                             "f"(total[f / 8][f % 8 * 4 + 2]), "f"(total[f / 8][f % 8 * 4 + 3]) : "memory");
+    }
+    __syncwarp();
+    acc_fence_before();
+    cluster_barrier();
+    if (warp == 2) {
+        acc_fence_after();
+        acc_free<1>(acc, 2 * kSplitN);
+    }
+    const int rows = min(kTileM, g.m - mt * kTileM);
+    for (int i = rank * kSplitThreads + int(threadIdx.x); i < rows * 16; i += parts * kSplitThreads) {
+        const int r = i >> 4, f = i & 15, col = nt * kSplitN + f * 4;
+        if (col >= g.n) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float4 p[kSplitMost];
+#pragma unroll
+        for (int q = 0; q < kSplitMost; ++q)
+            if (q < parts) p[q] = load_at_rank(ring + sum_place(r, f), q);
+#pragma unroll
+        for (int q = 0; q < kSplitMost; ++q)
+            if (q < parts) { v[0] += p[q].x; v[1] += p[q].y; v[2] += p[q].z; v[3] += p[q].w; }
+        const int64_t row = int64_t(mt) * kTileM + r;
+        const int left = min(4, g.n - col);
+        if (g.bias)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += j < left ? __ldg(g.bias + col + j) : 0.f;
+        if (g.pre) store4(g.pre + row * g.pre_step, col, left, 0, g.pre_wide, v);
+        apply_act(v, g.act);
+        if (g.residual)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < left) {
+                    const char* at = g.residual + row * g.residual_step;
+                    v[j] += g.out_f32 ? reinterpret_cast<const float*>(at)[col + j] : bf16_bits_to_float(reinterpret_cast<const uint16_t*>(at)[col + j]);
+                }
+        store4(g.out + row * g.out_step, col, left, g.out_f32, g.out_wide, v);
+    }
+    __syncwarp();
+    cluster_barrier();                                // (its sums have been read)
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_gave_up, 1u);
+}
+
 // ---- what goes in front of the products ---------------------------------------------------------------------------
 // Rows copied to where a tiled copy can read them: base and row stride multiples of 16 bytes.
 struct Repack { const char* from; char* to; int64_t from_step, to_step, rows; int cols; };
@@ -460,11 +632,12 @@ struct SlopeArgs {
     char *dz, *dz_mid, *dz_low;      // null: not wanted
     float* part;                     // [part][n]; null: no column sums
     int64_t dout_step, pre_step, dz_step, rows, rows_per_part;
-    int n, act, wide;
+    int n;
 };
 
-__device__ __forceinline__ void load8(const char* row, int col, int n, int wide, float (&x)[8]) {
-    if (wide && col + 8 <= n) {
+template <bool kWide>
+__device__ __forceinline__ void load8(const char* row, int col, int n, float (&x)[8]) {
+    if constexpr (kWide) {
         unpack8(ld_stream_u4(row + 2 * int64_t(col)), x);
     } else {
 #pragma unroll
@@ -472,16 +645,19 @@ __device__ __forceinline__ void load8(const char* row, int col, int n, int wide,
     }
 }
 
+// kWide: n is a multiple of 8, and the rows of dout and pre start on 16-byte boundaries.
+template <int kAct, bool kWide>
 __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
+    constexpr bool kPre = kAct != BAOC_ACT_NONE;
     __shared__ float sh[8][256];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = int(blockIdx.x) * 256 + lane * 8;
     const int64_t first = int64_t(blockIdx.y) * g.rows_per_part, end = min64(g.rows, first + g.rows_per_part);
     float sum[8] = {};
     let_later_kernel_start();
     auto one_row = [&](int64_t row, float (&d)[8], const float (&z)[8]) {
-        if (g.act != BAOC_ACT_NONE) {
+        if constexpr (kPre) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], g.act);
+            for (int j = 0; j < 8; ++j) d[j] *= act_slope<kAct>(z[j]);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += d[j];
@@ -489,7 +665,7 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
         const uint4 w = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
         const int64_t at = row * g.dz_step + 2 * int64_t(col);
         *reinterpret_cast<uint4*>(g.dz + at) = w;
-        if (!g.dz_mid) return;
+        if (!kPre || !g.dz_mid) return;
         float h[8];
         unpack8(w, h);
 #pragma unroll
@@ -503,16 +679,16 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
     };
     if (col < g.n)
         for (int64_t row = first + warp; row < end; row += 8 * kSlopeRows) {
-            float d[kSlopeRows][8], z[kSlopeRows][8];
+            float d[kSlopeRows][8], z[kPre ? kSlopeRows : 1][8];
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r) {
                 const int64_t at = min64(row + 8 * r, end - 1);          // (a row too many is read, not used)
-                load8(g.dout + at * g.dout_step, col, g.n, g.wide, d[r]);
-                if (g.act != BAOC_ACT_NONE) load8(g.pre + at * g.pre_step, col, g.n, g.wide, z[r]);
+                load8<kWide>(g.dout + at * g.dout_step, col, g.n, d[r]);
+                if constexpr (kPre) load8<kWide>(g.pre + at * g.pre_step, col, g.n, z[r]);
             }
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r)
-                if (row + 8 * r < end) one_row(row + 8 * r, d[r], z[r]);
+                if (row + 8 * r < end) one_row(row + 8 * r, d[r], z[kPre ? r : 0]);
         }
     if (!g.part) return;
 #pragma unroll
@@ -637,7 +813,7 @@ int launch_product(const Operands& o, const Matrix& out, const Matrix& pre, cons
     }
     Maps maps;
     bool ok = true;
-    for (int i = 0; i < g.passes; ++i) ok = ok && encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : kTileM) && encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : T::kBRows);
+    for (int i = 0; i < g.passes; ++i) ok = ok && encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : g.a_rows) && encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : T::kBRows);
     if (g.out_wide) ok = ok && encode(&maps.out, out, 32, 32);
     if (g.pre && g.pre_wide) ok = ok && encode(&maps.pre, pre, 32, 32);
     if (!ok) return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
@@ -652,11 +828,40 @@ int launch_product(const Operands& o, const Matrix& out, const Matrix& pre, cons
     return launched(cudaLaunchKernelEx(&cfg, kernel, maps, g), "product_kernel");
 }
 
-// The largest tiles that still give every CTA one; g has its sizes and flags, out and pre are where it goes.
+int launch_split(const Operands& o, const ProductArgs& g, int64_t tiles, int parts, cudaStream_t s) {
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    cudaError_t ce = cudaGetDevice(&dev);
+    if (ce != cudaSuccess) return launched(ce, "product_split_kernel");
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        ce = cudaFuncSetAttribute(product_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
+        if (ce != cudaSuccess) return launched(ce, "product_split_kernel");
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+    Maps maps;
+    for (int i = 0; i < g.passes; ++i)
+        if (!encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : g.a_rows) || !encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : kSplitN))
+            return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = unsigned(parts); at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(tiles * parts)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = kSplitSmem; cfg.stream = s;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    return launched(cudaLaunchKernelEx(&cfg, product_split_kernel, maps, g, parts), "product_split_kernel");
+}
+
+// The largest tiles that still give every CTA one; where the smallest do not, the sum over k is split among two CTAs per SM, at
+// least four steps each.  g has its sizes and flags, out and pre are where it goes.
 int form_product(const Operands& o, const Matrix& out, const Matrix& pre, ProductArgs g, cudaStream_t s) {
     g.out = const_cast<char*>(out.p); g.out_step = out.step; g.out_f32 = out.eb == 4; g.out_wide = out.wide();
     g.pre = const_cast<char*>(pre.p); g.pre_step = pre.step; g.pre_wide = pre.wide();
-    const int64_t pairs = ceil_div(g.m, 2 * kTileM), ones = ceil_div(g.m, kTileM);
+    g.a_rows = g.a_mn ? kTileM : std::min(kTileM, int(round_up(g.m, 8)));
+    const int64_t pairs = ceil_div(g.m, 2 * kTileM), ones = ceil_div(g.m, kTileM), smallest = ones * ceil_div(g.n, kSplitN);
+    int parts = 1;
+    while (parts < kSplitMost && smallest * parts * 2 <= 2 * 148 && int64_t(g.k_tiles) * g.passes >= 8 * parts) parts *= 2;
+    if (parts > 1) return launch_split(o, g, smallest, parts, s);
     if (g.out_f32) {
         if (pairs * ceil_div(g.n, 128) >= 74) return launch_product<2, 128, true>(o, out, pre, g, s);
         return launch_product<1, 64, true>(o, out, pre, g, s);
@@ -855,8 +1060,21 @@ int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const
     if ((rc = pack.launch(s))) return rc;
     if (g.dz || g.part) {
         g.dout = md.p; g.pre = mp.p; g.dout_step = md.step; g.pre_step = mp.step; g.dz_step = packed_step(e->n_out);
-        g.rows = tokens; g.n = e->n_out; g.act = e->act; g.wide = md.wide() && (!act || mp.wide());
-        slope_kernel<<<dim3(unsigned(ceil_div(e->n_out, 256)), unsigned(parts)), kThreads, 0, s>>>(g);
+        g.rows = tokens; g.n = e->n_out;
+        const dim3 grid(unsigned(ceil_div(e->n_out, 256)), unsigned(parts));
+        const bool wide = e->n_out % 8 == 0 && md.wide() && (!act || mp.wide());
+        auto go = [&](auto a) {
+            if (wide) slope_kernel<decltype(a)::value, true><<<grid, kThreads, 0, s>>>(g);
+            else slope_kernel<decltype(a)::value, false><<<grid, kThreads, 0, s>>>(g);
+        };
+        using std::integral_constant;
+        switch (e->act) {
+            case BAOC_ACT_RELU: go(integral_constant<int, BAOC_ACT_RELU>{}); break;
+            case BAOC_ACT_GELU: go(integral_constant<int, BAOC_ACT_GELU>{}); break;
+            case BAOC_ACT_GELU_TANH: go(integral_constant<int, BAOC_ACT_GELU_TANH>{}); break;
+            case BAOC_ACT_SILU: go(integral_constant<int, BAOC_ACT_SILU>{}); break;
+            default: go(integral_constant<int, BAOC_ACT_NONE>{}); break;
+        }
         if ((rc = launched(cudaGetLastError(), "slope_kernel"))) return rc;
         if (g.part && (rc = launched(launch_behind(slope_sums_kernel, unsigned(ceil_div(e->n_out, 32)), 1024, s, static_cast<const float*>(g.part), int(parts), int(e->n_out),
                                                    static_cast<char*>(db), int(e->grad_dtype == BAOC_F32)), "slope_sums_kernel")))
