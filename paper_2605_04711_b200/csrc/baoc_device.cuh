@@ -110,6 +110,25 @@ cudaError_t launch_behind(void (*kernel)(P...), unsigned grid, unsigned threads,
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
+// A launch of a kernel that begins with begin_in_row(): it may take its places while the kernel before it in the stream still
+// runs (if that one lets it: kernels that begin with begin_in_row() do), sets up what touches no memory of others, and waits in
+// hardware for that kernel's end.  A kernel of a few microseconds in a row of such saves its start this way.
+__device__ __forceinline__ void begin_in_row() {
+    let_later_kernel_start();
+    wait_for_earlier_kernel();
+}
+template <typename... P, typename... A>
+cudaError_t launch_in_row(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t s, const A&... args) {
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = s; cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // ---- bf16 ------------------------------------------------------------------
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

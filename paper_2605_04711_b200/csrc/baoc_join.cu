@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_kernel(const JoinArgs g)
     using Branch = RowPart<B, kTeam, kWide>;
     __shared__ float buf[2][kTeams][1][kTeam / 32];
     TeamSum<kTeam, 1> sum{buf};
+    begin_in_row();
     const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam, dim = g.dim;
     const float over = 1.f / float(dim);
     const int64_t step = int64_t(gridDim.x) * kTeams;
@@ -272,6 +273,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
     extern __shared__ float dynamic[];           // kShared: [kSums][8 * kTeam]; several teams: [kTeams][8 * kTeam]
     __shared__ float buf[2][kTeams][4][kTeam / 32];
     TeamSum<kTeam, 4> sum{buf};
+    begin_in_row();
     const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam, dim = g.dim;
     const float over = 1.f / float(dim);
     const int64_t begin = int64_t(blockIdx.x) * g.rows_per_cta, end = min64(g.rows, begin + g.rows_per_cta);
@@ -428,7 +430,6 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
         }
         seg = seg_end;
     }
-    let_later_kernel_start();
     auto finish = [&](auto which) {
         constexpr int k = decltype(which)::value;
         if (g.out[k]) hand_out(which, [&](int c, float v) { part[int64_t(k) * dim + c] = v; });
@@ -448,7 +449,7 @@ __global__ void __launch_bounds__(1024) join_sums_kernel(const JoinGradArgs g, i
     __shared__ float sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int col = int(blockIdx.x) * 32 + lane;
-    wait_for_earlier_kernel();
+    begin_in_row();
     auto total = [&](int64_t c0, int64_t c1, int64_t group, int k, int64_t at) {
         float s = 0.f;
         if (col < g.dim)
@@ -613,8 +614,7 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
         return with_team(team_of(e->dim, wide), wide, [&](auto T, auto W) {
             constexpr int kCta = join_cta(T()), kTeams = kCta / T();
             const unsigned grid = unsigned(std::min<int64_t>(ceil_div(rows, kTeams), int64_t(148) * (2048 / kCta)));
-            join_kernel<S(), B(), T(), W()><<<grid, kCta, 0, s>>>(a);
-            return launched(cudaGetLastError(), "join_kernel");
+            return launched(launch_in_row(join_kernel<S(), B(), T(), W()>, dim3(grid), kCta, 0, 1, s, a), "join_kernel");
         });
     });
 } catch (const std::bad_alloc&) {
@@ -686,8 +686,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
                         const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
                         if (ce != cudaSuccess) return launched(ce, "join_grad_kernel");
                     }
-                    kernel<<<unsigned(ctas), kCta, kBytes, s>>>(a BAOC_CHECK_ARG(ck));
-                    return launched(cudaGetLastError(), "join_grad_kernel");
+                    return launched(launch_in_row(kernel, dim3(unsigned(ctas)), kCta, kBytes, 1, s, a BAOC_CHECK_ARG(ck)), "join_grad_kernel");
                 };
                 return layer ? go(std::true_type{}) : go(std::false_type{});
             });
@@ -701,12 +700,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
     if (!any) return BAOC_OK;
     const int64_t groups = a.rows_per_gate && dgate ? ceil_div(rows, a.rows_per_gate) : 0;
     const dim3 grid(unsigned(ceil_div(e->dim, 32)), unsigned(kJoinSums + std::min<int64_t>(groups, 1024)));
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid; cfg.blockDim = dim3(1024); cfg.stream = s; cfg.attrs = &at; cfg.numAttrs = rows ? 1 : 0;
-    return launched(cudaLaunchKernelEx(&cfg, join_sums_kernel, a, ctas, groups), "join_sums_kernel");
+    return launched(launch_in_row(join_sums_kernel, grid, 1024, 0, 1, s, a, ctas, groups), "join_sums_kernel");
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
 }

@@ -318,6 +318,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if constexpr (kCtas == 2) cluster_barrier();
     else __syncthreads();
     acc_fence_after();
+    begin_in_row();
     const uint32_t acc = acc_at;
 
     if (warp == 0 && lane == 0) {                     // copies: each CTA its own operands, a pair's bytes counted by its first CTA
@@ -487,6 +488,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
     acc_fence_before();
     __syncthreads();
     acc_fence_after();
+    begin_in_row();
     const uint32_t acc = acc_at;
     if (warp == 0 && lane == 0) {
         bool ok = true;
@@ -606,6 +608,7 @@ struct Repack { const char* from; char* to; int64_t from_step, to_step, rows; in
 struct Repacks { Repack r[3]; int64_t ends[3]; int n; };       // ends: running counts of 8-column pieces
 
 __global__ void __launch_bounds__(kThreads) repack_kernel(const Repacks g) {
+    begin_in_row();
     for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < g.ends[g.n - 1]; i += int64_t(gridDim.x) * kThreads) {
         int which = 0;
         while (i >= g.ends[which]) ++which;
@@ -653,7 +656,7 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = int(blockIdx.x) * 256 + lane * 8;
     const int64_t first = int64_t(blockIdx.y) * g.rows_per_part, end = min64(g.rows, first + g.rows_per_part);
     float sum[8] = {};
-    let_later_kernel_start();
+    begin_in_row();
     auto one_row = [&](int64_t row, float (&d)[8], const float (&z)[8]) {
         if constexpr (kPre) {
 #pragma unroll
@@ -706,7 +709,7 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
 __global__ void __launch_bounds__(1024) slope_sums_kernel(const float* __restrict__ part, int parts, int n, char* db, int f32) {
     __shared__ float sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = int(blockIdx.x) * 32 + lane;
-    wait_for_earlier_kernel();
+    begin_in_row();
     float s = 0.f;
     if (col < n)
         for (int p = warp; p < parts; p += 32) s += part[int64_t(p) * n + col];
@@ -819,13 +822,7 @@ int launch_product(const Operands& o, const Matrix& out, const Matrix& pre, cons
     if (!ok) return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
     const int64_t tiles = ceil_div(g.m, kTileM * kCtas) * ceil_div(g.n, kN);
     if (tiles > 0x7fffffff - 148) return fail_linear(BAOC_E_INVALID, "too many tiles for one launch");
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = kCtas; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(unsigned(std::min<int64_t>(tiles, 148 / kCtas) * kCtas)); cfg.blockDim = dim3(kProductThreads); cfg.dynamicSmemBytes = T::kSmem; cfg.stream = s;
-    cfg.attrs = &at; cfg.numAttrs = kCtas > 1 ? 1 : 0;
-    return launched(cudaLaunchKernelEx(&cfg, kernel, maps, g), "product_kernel");
+    return launched(launch_in_row(kernel, dim3(unsigned(std::min<int64_t>(tiles, 148 / kCtas) * kCtas)), kProductThreads, T::kSmem, kCtas, s, maps, g), "product_kernel");
 }
 
 int launch_split(const Operands& o, const ProductArgs& g, int64_t tiles, int parts, cudaStream_t s) {
@@ -843,13 +840,7 @@ int launch_split(const Operands& o, const ProductArgs& g, int64_t tiles, int par
     for (int i = 0; i < g.passes; ++i)
         if (!encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : g.a_rows) || !encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : kSplitN))
             return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = unsigned(parts); at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(unsigned(tiles * parts)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = kSplitSmem; cfg.stream = s;
-    cfg.attrs = &at; cfg.numAttrs = 1;
-    return launched(cudaLaunchKernelEx(&cfg, product_split_kernel, maps, g, parts), "product_split_kernel");
+    return launched(launch_in_row(product_split_kernel, dim3(unsigned(tiles * parts)), kSplitThreads, kSplitSmem, unsigned(parts), s, maps, g, parts), "product_split_kernel");
 }
 
 // The largest tiles that still give every CTA one; where the smallest do not, the sum over k is split among two CTAs per SM, at
@@ -896,8 +887,7 @@ struct Packer {
     int launch(cudaStream_t s) const {
         if (!todo.n) return BAOC_OK;
         const unsigned grid = unsigned(std::min<int64_t>(ceil_div(todo.ends[todo.n - 1], kThreads), 148 * 16));
-        repack_kernel<<<grid, kThreads, 0, s>>>(todo);
-        return launched(cudaGetLastError(), "repack_kernel");
+        return launched(launch_in_row(repack_kernel, dim3(grid), kThreads, 0, 1, s, todo), "repack_kernel");
     }
 };
 
@@ -1064,20 +1054,19 @@ int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const
         const dim3 grid(unsigned(ceil_div(e->n_out, 256)), unsigned(parts));
         const bool wide = e->n_out % 8 == 0 && md.wide() && (!act || mp.wide());
         auto go = [&](auto a) {
-            if (wide) slope_kernel<decltype(a)::value, true><<<grid, kThreads, 0, s>>>(g);
-            else slope_kernel<decltype(a)::value, false><<<grid, kThreads, 0, s>>>(g);
+            return launched(launch_in_row(wide ? slope_kernel<decltype(a)::value, true> : slope_kernel<decltype(a)::value, false>, grid, kThreads, 0, 1, s, g), "slope_kernel");
         };
         using std::integral_constant;
         switch (e->act) {
-            case BAOC_ACT_RELU: go(integral_constant<int, BAOC_ACT_RELU>{}); break;
-            case BAOC_ACT_GELU: go(integral_constant<int, BAOC_ACT_GELU>{}); break;
-            case BAOC_ACT_GELU_TANH: go(integral_constant<int, BAOC_ACT_GELU_TANH>{}); break;
-            case BAOC_ACT_SILU: go(integral_constant<int, BAOC_ACT_SILU>{}); break;
-            default: go(integral_constant<int, BAOC_ACT_NONE>{}); break;
+            case BAOC_ACT_RELU: rc = go(integral_constant<int, BAOC_ACT_RELU>{}); break;
+            case BAOC_ACT_GELU: rc = go(integral_constant<int, BAOC_ACT_GELU>{}); break;
+            case BAOC_ACT_GELU_TANH: rc = go(integral_constant<int, BAOC_ACT_GELU_TANH>{}); break;
+            case BAOC_ACT_SILU: rc = go(integral_constant<int, BAOC_ACT_SILU>{}); break;
+            default: rc = go(integral_constant<int, BAOC_ACT_NONE>{}); break;
         }
-        if ((rc = launched(cudaGetLastError(), "slope_kernel"))) return rc;
-        if (g.part && (rc = launched(launch_behind(slope_sums_kernel, unsigned(ceil_div(e->n_out, 32)), 1024, s, static_cast<const float*>(g.part), int(parts), int(e->n_out),
-                                                   static_cast<char*>(db), int(e->grad_dtype == BAOC_F32)), "slope_sums_kernel")))
+        if (rc) return rc;
+        if (g.part && (rc = launched(launch_in_row(slope_sums_kernel, dim3(unsigned(ceil_div(e->n_out, 32))), 1024, 0, 1, s, static_cast<const float*>(g.part), int(parts),
+                                                   int(e->n_out), static_cast<char*>(db), int(e->grad_dtype == BAOC_F32)), "slope_sums_kernel")))
             return rc;
     }
     const Matrix none(nullptr, 0, 0, 0, BAOC_BF16);

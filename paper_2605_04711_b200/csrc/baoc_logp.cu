@@ -289,6 +289,7 @@ __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
     constexpr int kVec = Logits<DT>::kVec;
     __shared__ Sums warp_sums[kT / 32], cta_sums;
     __shared__ TopShared<kT> top_shared;
+    begin_in_row();
     const int tid = threadIdx.x, lane = tid & 31, part = kC > 1 ? int(blockIdx.x % kC) : 0;
     const int64_t row = blockIdx.x / kC, vocab = g.vocab;
     const int64_t id = given_token(g.ids, g.id_bits, row);
@@ -419,6 +420,7 @@ struct LogpGradArgs {
 template <int DT, bool kWide>
 __global__ void __launch_bounds__(kThreads) logp_grad_kernel(const LogpGradArgs g) {
     constexpr int kVec = Logits<DT>::kVec, kSize = Logits<DT>::kSize;
+    begin_in_row();
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / g.segments;
     const int seg = int(blockIdx.x - row * g.segments);
@@ -522,13 +524,7 @@ int check_logp(const baoc_logp_t* e, int64_t n, const std::string& what) {
 template <int DT, int kC, int kT>
 int launch_logp(const LogpArgs& a, int64_t n, cudaStream_t s) {
     if (n * kC > 0x7fffffff) return fail_logp(BAOC_E_INVALID, "baoc_logp: too many rows for one launch");
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = kC; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(unsigned(n * kC)); cfg.blockDim = dim3(kT); cfg.stream = s;
-    cfg.attrs = &at; cfg.numAttrs = kC > 1 ? 1 : 0;
-    const cudaError_t ce = cudaLaunchKernelEx(&cfg, logp_kernel<DT, kC, kT>, a);
+    const cudaError_t ce = launch_in_row(logp_kernel<DT, kC, kT>, dim3(unsigned(n * kC)), kT, 0, kC, s, a);
     return ce == cudaSuccess ? BAOC_OK : fail_logp(BAOC_E_CUDA, std::string("logp_kernel: ") + cudaGetErrorString(ce));
 }
 
@@ -594,14 +590,9 @@ int baoc_logp_grad(const baoc_logp_t* e, const void* logits, const void* ids, co
     const bool wide = ((d - x) & 15) == 0 && ((out_step - step) & 15) == 0;
     const unsigned grid = unsigned(n_tokens * segments);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (e->dtype == BAOC_BF16) {
-        if (wide) logp_grad_kernel<BAOC_BF16, true><<<grid, kThreads, 0, s>>>(a);
-        else logp_grad_kernel<BAOC_BF16, false><<<grid, kThreads, 0, s>>>(a);
-    } else {
-        if (wide) logp_grad_kernel<BAOC_F32, true><<<grid, kThreads, 0, s>>>(a);
-        else logp_grad_kernel<BAOC_F32, false><<<grid, kThreads, 0, s>>>(a);
-    }
-    const cudaError_t ce = cudaGetLastError();
+    const auto kernel = e->dtype == BAOC_BF16 ? (wide ? logp_grad_kernel<BAOC_BF16, true> : logp_grad_kernel<BAOC_BF16, false>)
+                                              : (wide ? logp_grad_kernel<BAOC_F32, true> : logp_grad_kernel<BAOC_F32, false>);
+    const cudaError_t ce = launch_in_row(kernel, dim3(grid), kThreads, 0, 1, s, a);
     return ce == cudaSuccess ? BAOC_OK : fail_logp(BAOC_E_CUDA, std::string("logp_grad_kernel: ") + cudaGetErrorString(ce));
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
