@@ -28,18 +28,23 @@ namespace baoc {
 constexpr int kJoinMaxDim = 8192;
 constexpr int64_t kJoinMaxStride = int64_t(1) << 28;
 constexpr int kJoinCols = 8;                   // columns of a thread
-constexpr int kJoinSmThreads = 1024;           // threads of the gradient's CTAs per SM
+constexpr int kSoloWarps = 4;                  // rows of up to 256 columns: one warp each, so many per CTA
+constexpr int kJoinWarps = 32, kJoinGradWarps = 16;    // warps per SM that the registers allow
 constexpr int kJoinSums = 5;                   // column sums of the gradient: weight and bias of pre, of post, and the gate
 
-__host__ __device__ constexpr int join_cta(int team) { return team > 256 ? team : 256; }
+// How a row is spread: kClass 0, one warp; 1, 2 and 3, a CTA of as many warps as it needs, up to 8, 16 and 32 (what differs is
+// the registers a thread may have).
+__host__ __device__ constexpr int class_threads(int c) { return c == 0 ? 32 * kSoloWarps : 128 << c; }
+template <int kClass>
+__device__ __forceinline__ int team_size() { return kClass == 0 ? 32 : int(blockDim.x); }
 
-template <int DT, int kTeam, bool kWide>
+template <int DT, int kClass, bool kWide>
 struct RowPart {
-    // a thread's columns: 8 neighbours, or 8 that are kTeam apart
+    // a thread's columns: 8 neighbours, or 8 that are a team's size apart
     static constexpr int kSize = DT == BAOC_BF16 ? 2 : 4;
     static constexpr int kWords = kWide ? 2 * kSize : 8;
     uint32_t w[kWords];
-    static __device__ __forceinline__ int column(int t, int j) { return kWide ? t * kJoinCols + j : j * kTeam + t; }
+    static __device__ __forceinline__ int column(int t, int j) { return kWide ? t * kJoinCols + j : j * team_size<kClass>() + t; }
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -60,7 +65,7 @@ struct RowPart {
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = j * kTeam + t;
+                const int c = column(t, j);
                 if constexpr (DT == BAOC_BF16) w[j] = c < dim ? *reinterpret_cast<const uint16_t*>(row + 2 * c) : 0;
                 else w[j] = c < dim ? *reinterpret_cast<const uint32_t*>(row + 4 * c) : 0;
             }
@@ -95,7 +100,7 @@ struct RowPart {
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = j * kTeam + t;
+                const int c = column(t, j);
                 if (c >= dim) continue;
                 if constexpr (DT == BAOC_F32) {
                     *reinterpret_cast<float*>(row + 4 * c) = x[j];
@@ -110,9 +115,9 @@ struct RowPart {
 };
 
 // A thread's 8 values of a vector per column (fp32, 4-byte aligned; read over and over, from L1); `other` where there is none.
-template <int kTeam, bool kWide>
+template <int kClass, bool kWide>
 __device__ __forceinline__ void per_column(const float* v, int t, int dim, float other, float (&x)[8]) {
-    using P = RowPart<BAOC_F32, kTeam, kWide>;
+    using P = RowPart<BAOC_F32, kClass, kWide>;
     if (kWide && v && t * kJoinCols < dim) {
         const float4 a = __ldg(reinterpret_cast<const float4*>(v + t * kJoinCols)), b = __ldg(reinterpret_cast<const float4*>(v + t * kJoinCols) + 1);
         f4_to8(a, b, x);
@@ -122,34 +127,41 @@ __device__ __forceinline__ void per_column(const float* v, int t, int dim, float
     for (int j = 0; j < 8; ++j) x[j] = v && P::column(t, j) < dim ? __ldg(v + P::column(t, j)) : other;
 }
 
-// Sums of K values over a team, the same in all of its threads.  Teams of more than a warp take turns of two buffers, so that
-// one barrier a round is enough; all teams of a CTA call it together.
-template <int kTeam, int kMost>
+// Sums of K <= 4 values over a team, the same in all of its threads.  A CTA's warps take turns of two buffers, so that one
+// barrier a round is enough; all of its threads call it.
+template <int kClass>
 struct TeamSum {
-    static constexpr int kWarps = kTeam / 32, kTeams = join_cta(kTeam) / kTeam;
-    float (*buf)[kTeams][kMost][kWarps];
+    float4 (*buf)[32];               // [2][warps]
     int turn = 0;
     template <int K>
     __device__ __forceinline__ void operator()(float (&v)[K]) {
-        static_assert(K <= kMost, "");
+        static_assert(K <= 4, "");
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        if constexpr (kTeam > 32) {
-            const int lane = threadIdx.x & 31, warp = (threadIdx.x % kTeam) >> 5, team = threadIdx.x / kTeam;
-            if (lane < K) {
-                float mine = v[0];
-#pragma unroll
-                for (int k = 1; k < K; ++k) mine = lane == k ? v[k] : mine;
-                buf[turn][team][lane][warp] = mine;
-            }
+            for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        if constexpr (kClass > 0) {
+            const int lane = threadIdx.x & 31, warps = int(blockDim.x) >> 5;
+            if (lane == 0) buf[turn][threadIdx.x >> 5] = make_float4(v[0], K > 1 ? v[K > 1 ? 1 : 0] : 0.f, K > 2 ? v[K > 2 ? 2 : 0] : 0.f, K > 3 ? v[K > 3 ? 3 : 0] : 0.f);
             __syncthreads();
+            if constexpr (kClass == 1) {             // up to 8 warps: every thread adds them up
+                float4 s = buf[turn][0];
+                for (int w = 1; w < warps; ++w) {
+                    const float4 o = buf[turn][w];
+                    s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+                }
+                const float all[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                v[k] = buf[turn][team][k][lane % kWarps];
+                for (int k = 0; k < K; ++k) v[k] = all[k];
+            } else {
+                const float4 s = lane < warps ? buf[turn][lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+                const float all[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-                for (int o = kWarps / 2; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+                for (int k = 0; k < K; ++k) v[k] = all[k];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
             }
             turn ^= 1;
         }
@@ -165,20 +177,21 @@ struct JoinArgs {
     float scale, eps;
 };
 
-template <int S, int B, int kTeam, bool kWide>
-__global__ void __launch_bounds__(join_cta(kTeam)) join_kernel(const JoinArgs g) {
-    constexpr int kTeams = join_cta(kTeam) / kTeam;
-    using Stream = RowPart<S, kTeam, kWide>;
-    using Branch = RowPart<B, kTeam, kWide>;
-    __shared__ float buf[2][kTeams][1][kTeam / 32];
-    TeamSum<kTeam, 1> sum{buf};
+template <int S, int B, int kClass, bool kWide>
+__global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps * 32 / class_threads(kClass) : 1) join_kernel(const JoinArgs g) {
+    constexpr int kTeams = kClass == 0 ? kSoloWarps : 1;
+    using Stream = RowPart<S, kClass, kWide>;
+    using Branch = RowPart<B, kClass, kWide>;
+    __shared__ float4 buf[kClass > 0 ? 2 : 1][32];
+    TeamSum<kClass> sum{buf};
     begin_in_row();
-    const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam, dim = g.dim;
+    const int t = kClass == 0 ? int(threadIdx.x & 31) : int(threadIdx.x), team = kClass == 0 ? int(threadIdx.x >> 5) : 0, dim = g.dim;
     const float over = 1.f / float(dim);
     const int64_t step = int64_t(gridDim.x) * kTeams;
+    const bool in = kWide ? t * kJoinCols < dim : true;
     bool inside[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) inside[j] = Stream::column(t, j) < dim;
+    for (int j = 0; j < 8; ++j) inside[j] = kWide ? in : Stream::column(t, j) < dim;
     // v without its mean (layer norm), and 1 / sqrt(mean square + eps)
     auto normalise = [&](float (&v)[8]) {
         float s[1];
@@ -209,7 +222,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_kernel(const JoinArgs g)
     next_f.clear();
     int64_t row = int64_t(blockIdx.x) * kTeams + team;
     fetch(row);
-    for (int64_t first = int64_t(blockIdx.x) * kTeams; first < g.rows; first += step, row += step) {
+    for (; row < g.rows; row += step) {          // (alike in a team)
         float x[8], u[8], w[8];
         next_x.get(x);
         next_f.get(u);
@@ -217,22 +230,22 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_kernel(const JoinArgs g)
         if (g.post_w) {
             const float r = normalise(u);
             float b[8];
-            per_column<kTeam, kWide>(g.post_w, t, dim, 0.f, w);
-            per_column<kTeam, kWide>(g.post_b, t, dim, 0.f, b);
+            per_column<kClass, kWide>(g.post_w, t, dim, 0.f, w);
+            per_column<kClass, kWide>(g.post_b, t, dim, 0.f, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[j] = u[j] * r * w[j] + b[j];
         }
-        per_column<kTeam, kWide>(g.gate ? g.gate + (g.rows_per_gate ? min64(row, g.rows - 1) / g.rows_per_gate : 0) * dim : nullptr, t, dim, 1.f, w);
+        per_column<kClass, kWide>(g.gate ? g.gate + (g.rows_per_gate ? int64_t(uint32_t(row) / uint32_t(g.rows_per_gate)) : 0) * dim : nullptr, t, dim, 1.f, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) u[j] = g.scale * x[j] + w[j] * u[j];
-        if (row < g.rows) Stream::store(g.y + row * g.y_step, t, dim, u);
+        Stream::store(g.y + row * g.y_step, t, dim, u);
         const float r = normalise(u);
         float b[8];
-        per_column<kTeam, kWide>(g.pre_w, t, dim, 0.f, w);
-        per_column<kTeam, kWide>(g.pre_b, t, dim, 0.f, b);
+        per_column<kClass, kWide>(g.pre_w, t, dim, 0.f, w);
+        per_column<kClass, kWide>(g.pre_b, t, dim, 0.f, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) u[j] = u[j] * r * w[j] + b[j];
-        if (row < g.rows) Branch::store(g.h + row * g.h_step, t, dim, u);
+        Branch::store(g.h + row * g.h_step, t, dim, u);
     }
 }
 
@@ -263,18 +276,18 @@ __device__ __forceinline__ void store_grad(char* out, int dtype, int64_t i, floa
 // A CTA takes rows_per_cta rows in order.  A gate per group: its sums are handed out at the end of every group.  A group whose
 // rows all belong to this CTA is finished here; of the others a CTA has two at most, the one its first row is in (slot kGate)
 // and the one its last row is in (slot kJoinSums).
-template <int S, int B, bool kLayer, int kTeam, bool kWide>
-__global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
-    constexpr int kCta = join_cta(kTeam), kTeams = kCta / kTeam, kSums = kLayer ? 5 : 3;
-    constexpr bool kShared = kTeam > 512;        // (64 registers a thread: the sums lie in shared memory)
-    constexpr bool kAhead = kTeam <= 512;
-    using Stream = RowPart<S, kTeam, kWide>;
-    using Branch = RowPart<B, kTeam, kWide>;
-    extern __shared__ float dynamic[];           // kShared: [kSums][8 * kTeam]; several teams: [kTeams][8 * kTeam]
-    __shared__ float buf[2][kTeams][4][kTeam / 32];
-    TeamSum<kTeam, 4> sum{buf};
+template <int S, int B, bool kLayer, int kClass, bool kWide>
+__global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kClass < 3 ? kJoinGradWarps * 32 / class_threads(kClass) : 1)) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
+    constexpr int kTeams = kClass == 0 ? kSoloWarps : 1, kSums = kLayer ? 5 : 3;
+    constexpr bool kShared = kClass == 3;        // (64 registers a thread: the sums lie in shared memory, and no row is fetched ahead)
+    constexpr bool kAhead = !kShared;
+    using Stream = RowPart<S, kClass, kWide>;
+    using Branch = RowPart<B, kClass, kWide>;
+    extern __shared__ float dynamic[];           // kShared: [kSums][8][threads]; several teams: [kTeams][8][32]
+    __shared__ float4 buf[kClass > 0 ? 2 : 1][32];
+    TeamSum<kClass> sum{buf};
     begin_in_row();
-    const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam, dim = g.dim;
+    const int kTeam = team_size<kClass>(), t = kClass == 0 ? int(threadIdx.x & 31) : int(threadIdx.x), team = kClass == 0 ? int(threadIdx.x >> 5) : 0, dim = g.dim;
     const float over = 1.f / float(dim);
     const int64_t begin = int64_t(blockIdx.x) * g.rows_per_cta, end = min64(g.rows, begin + g.rows_per_cta);
     float* part = g.part + int64_t(blockIdx.x) * (kJoinSums + 1) * dim;
@@ -321,7 +334,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
         for (int k = 0; k < kSums; ++k) zero(k);
     bool inside[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) inside[j] = Stream::column(t, j) < dim;
+    for (int j = 0; j < 8; ++j) inside[j] = kWide ? t * kJoinCols < dim : Stream::column(t, j) < dim;
     Stream next_y, next_dy;
     Branch next_f, next_dh;
     auto fetch = [&](int64_t row, int64_t last) {
@@ -330,13 +343,10 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
             next_dh.load(g.dh + row * g.dh_step, t, dim);
             if (g.dy) next_dy.load(g.dy + row * g.dy_step, t, dim);
             if (need_f) next_f.load(g.f + row * g.f_step, t, dim);
-        } else {
-            next_y.clear();
-            next_dh.clear();
-            next_dy.clear();
-            next_f.clear();                      // (an idle team adds zeros)
         }
     };
+    next_y.clear();
+    next_dh.clear();
     next_dy.clear();
     next_f.clear();
     for (int64_t seg = begin; seg < end;) {
@@ -344,8 +354,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
         const int64_t seg_end = g.rows_per_gate ? min64(end, (group + 1) * g.rows_per_gate) : end;
         const float* gate = g.gate ? g.gate + group * dim : nullptr;
         if (kAhead) fetch(seg + team, seg_end);
-        for (int64_t first = seg; first < seg_end; first += kTeams) {
-            const int64_t row = first + team;
+        for (int64_t row = seg + team; row < seg_end; row += kTeams) {       // (alike in a team)
             if (!kAhead) fetch(row, seg_end);
             float y[8], d[8], f[8], w[8];        // d: from dh to Dy
             next_y.get(y);
@@ -364,7 +373,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = inside[j] ? y[j] - s[0] * over : 0.f;
             }
-            per_column<kTeam, kWide>(g.pre_w, t, dim, 0.f, w);
+            per_column<kClass, kWide>(g.pre_w, t, dim, 0.f, w);
             {
                 float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -387,13 +396,13 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
                     dy[j] = g.scale * d[j];
                 }
             }
-            if (g.dx && row < seg_end) Stream::store(g.dx + row * g.dx_step, t, dim, dy);
+            if (g.dx) Stream::store(g.dx + row * g.dx_step, t, dim, dy);
             float gt[8];
-            per_column<kTeam, kWide>(gate, t, dim, 1.f, gt);
+            per_column<kClass, kWide>(gate, t, dim, 1.f, gt);
             if (g.post_w) {
                 float b[8];
-                per_column<kTeam, kWide>(g.post_w, t, dim, 0.f, w);
-                per_column<kTeam, kWide>(kLayer ? g.post_b : nullptr, t, dim, 0.f, b);
+                per_column<kClass, kWide>(g.post_w, t, dim, 0.f, w);
+                per_column<kClass, kWide>(kLayer ? g.post_b : nullptr, t, dim, 0.f, b);
                 float s[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -417,7 +426,7 @@ __global__ void __launch_bounds__(join_cta(kTeam)) join_grad_kernel(const JoinGr
                     d[j] *= gt[j];
                 }
             }
-            if (row < seg_end) Branch::store(g.df + row * g.df_step, t, dim, d);
+            Branch::store(g.df + row * g.df_step, t, dim, d);
         }
         if (g.rows_per_gate && g.out[kGate]) {
             const bool whole = group * g.rows_per_gate >= begin && min64(g.rows, (group + 1) * g.rows_per_gate) <= end;
@@ -524,28 +533,28 @@ bool overlap(const Rows& a, const Rows& b, int64_t rows) {
 }
 bool same(const Rows& a, const Rows& b, int64_t rows) { return a.p == b.p && a.width == b.width && (a.step == b.step || rows == 1); }
 
-int team_of(int dim, bool wide) {
-    if (!wide) return dim <= 256 ? 32 : (dim <= 2048 ? 256 : 1024);
-    int t = 32;
-    while (t * kJoinCols < dim) t *= 2;
-    return t;
+// Warps of a row's CTA and its class (see class_threads).
+int warps_of(int dim) { return int(ceil_div(dim, 32 * kJoinCols)); }
+int class_of(int dim) {
+    const int w = warps_of(dim);
+    return w == 1 ? 0 : (w <= 8 ? 1 : (w <= 16 ? 2 : 3));
 }
+int cta_of(int dim) { return warps_of(dim) == 1 ? 32 * kSoloWarps : 32 * warps_of(dim); }
+int rows_of(int dim) { return warps_of(dim) == 1 ? kSoloWarps : 1; }         // rows that a CTA works on at a time
 
-// f(team, wide) as constants.
+// f(class, wide) as constants.
+template <int kClass, typename F>
+int with_width(bool wide, F f) {
+    std::integral_constant<int, kClass> c{};
+    return wide ? f(c, std::true_type{}) : f(c, std::false_type{});
+}
 template <typename F>
-int with_team(int team, bool wide, F f) {
-    using std::integral_constant;
-    if (!wide) {
-        if (team == 32) return f(integral_constant<int, 32>{}, std::false_type{});
-        return team == 256 ? f(integral_constant<int, 256>{}, std::false_type{}) : f(integral_constant<int, 1024>{}, std::false_type{});
-    }
-    switch (team) {
-        case 32: return f(integral_constant<int, 32>{}, std::true_type{});
-        case 64: return f(integral_constant<int, 64>{}, std::true_type{});
-        case 128: return f(integral_constant<int, 128>{}, std::true_type{});
-        case 256: return f(integral_constant<int, 256>{}, std::true_type{});
-        case 512: return f(integral_constant<int, 512>{}, std::true_type{});
-        default: return f(integral_constant<int, 1024>{}, std::true_type{});
+int with_class(int dim, bool wide, F f) {
+    switch (class_of(dim)) {
+        case 0: return with_width<0>(wide, f);
+        case 1: return with_width<1>(wide, f);
+        case 2: return with_width<2>(wide, f);
+        default: return with_width<3>(wide, f);
     }
 }
 template <typename F>
@@ -556,18 +565,19 @@ int with_types(int stream, int branch, F f) {
                                : f(integral_constant<int, BAOC_F32>{}, integral_constant<int, BAOC_F32>{});
 }
 
-// The gradient's rows per CTA and CTAs: as many CTAs as find room at once (kJoinSmThreads per SM), whole rounds of their teams.
-void grad_shape(int team, int64_t rows, int64_t* per_cta, int* ctas) {
-    const int cta = join_cta(team), teams = cta / team;
-    const int64_t most = int64_t(148) * (kJoinSmThreads / cta);
-    *per_cta = std::max<int64_t>(teams, round_up(ceil_div(rows, most), teams));
+// CTAs of a kernel that find room at once, sm_warps per SM.
+int64_t ctas_at_once(int dim, int sm_warps) { return int64_t(148) * std::max(1, sm_warps * 32 / cta_of(dim)); }
+
+// The gradient's rows per CTA and CTAs: whole rounds of a CTA's teams, all CTAs at once.
+void grad_shape(int dim, int64_t rows, int64_t* per_cta, int* ctas) {
+    const int teams = rows_of(dim);
+    *per_cta = std::max<int64_t>(teams, round_up(ceil_div(rows, ctas_at_once(dim, kJoinGradWarps)), teams));
     *ctas = int(ceil_div(rows, *per_cta));
 }
 // (By the most CTAs that so many rows or fewer can get: whole rounds leave fewer of them for some larger numbers of rows.)
-int64_t grad_ws(int dim, bool wide, int64_t rows) {
-    const int team = team_of(dim, wide), cta = join_cta(team);
-    const int64_t ctas = std::min(ceil_div(rows, cta / team), int64_t(148) * (kJoinSmThreads / cta));
-    return round_up(ctas * (kJoinSums + 1) * dim * 4, 256);
+int64_t grad_ws(int dim, int64_t rows) {
+    const int64_t ctas = std::min(ceil_div(rows, rows_of(dim)), ctas_at_once(dim, kJoinGradWarps));
+    return std::max<int64_t>(256, round_up(ctas * (kJoinSums + 1) * dim * 4, 256));
 }
 
 int launched(cudaError_t ce, const char* kernel) {
@@ -611,10 +621,9 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
                      rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
-        return with_team(team_of(e->dim, wide), wide, [&](auto T, auto W) {
-            constexpr int kCta = join_cta(T()), kTeams = kCta / T();
-            const unsigned grid = unsigned(std::min<int64_t>(ceil_div(rows, kTeams), int64_t(148) * (2048 / kCta)));
-            return launched(launch_in_row(join_kernel<S(), B(), T(), W()>, dim3(grid), kCta, 0, 1, s, a), "join_kernel");
+        return with_class(e->dim, wide, [&](auto C, auto W) {
+            const unsigned grid = unsigned(std::min(ceil_div(rows, rows_of(e->dim)), ctas_at_once(e->dim, kJoinWarps)));
+            return launched(launch_in_row(join_kernel<S(), B(), C(), W()>, dim3(grid), unsigned(cta_of(e->dim)), 0, 1, s, a), "join_kernel");
         });
     });
 } catch (const std::bad_alloc&) {
@@ -625,7 +634,7 @@ int baoc_join_grad_workspace_bytes(const baoc_join_t* e, int64_t rows, size_t* b
     const int rc = check_join(e, rows, "baoc_join_grad_workspace_bytes");
     if (rc) return rc;
     if (!bytes) return fail_join(BAOC_E_INVALID, "baoc_join_grad_workspace_bytes: null pointer");
-    *bytes = size_t(std::max<int64_t>(256, std::max(grad_ws(e->dim, true, rows), grad_ws(e->dim, false, rows))));
+    *bytes = size_t(grad_ws(e->dim, rows));
     return BAOC_OK;
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
@@ -660,33 +669,31 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
     for (const void* p : outs)
         if (!aligned(p, elem_bytes(e->grad_dtype))) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
     if (!aligned(ws, 256)) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: workspace not 256-byte aligned");
-    const int64_t need = std::max<int64_t>(256, grad_ws(e->dim, wide, rows));
+    const int64_t need = grad_ws(e->dim, rows);
     if (ws_bytes < size_t(need)) return fail_join(BAOC_E_WORKSPACE, "baoc_join_grad: workspace too small");
     if ((overlap(rdx, rdy, rows) && !same(rdx, rdy, rows)) || (overlap(rdf, rdh, rows) && !same(rdf, rdh, rows)) || overlap(rdx, ry, rows) || overlap(rdx, rf, rows) ||
         overlap(rdx, rdh, rows) || overlap(rdf, ry, rows) || overlap(rdf, rf, rows) || overlap(rdf, rdy, rows) || overlap(rdx, rdf, rows))
         return fail_join(BAOC_E_INVALID, "baoc_join_grad: dx may be dy and df may be dh; outputs overlap nothing else");
-    const int team = team_of(e->dim, wide);
     JoinGradArgs a{static_cast<const char*>(y), static_cast<const char*>(rf.p), static_cast<const char*>(dy), static_cast<const char*>(dh), static_cast<char*>(dx),
                    static_cast<char*>(df), post_w, post_b, gate, pre_w, {}, static_cast<float*>(ws), ry.step, rf.step, rdy.step, rdh.step, rdx.step, rdf.step, rows,
                    gate ? e->rows_per_gate : 0, 0, e->dim, e->grad_dtype, e->scale, e->eps};
     for (int k = 0; k < kJoinSums; ++k) a.out[k] = static_cast<char*>(outs[k]);
     int ctas;
-    grad_shape(team, std::max<int64_t>(rows, 1), &a.rows_per_cta, &ctas);
+    grad_shape(e->dim, std::max<int64_t>(rows, 1), &a.rows_per_cta, &ctas);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CheckCtx ck{static_cast<char*>(ws), static_cast<char*>(ws) + need, 0, 0, 0};
     (void)ck;
     if (rows) {
         rc = with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
-            return with_team(team, wide, [&](auto T, auto W) {
+            return with_class(e->dim, wide, [&](auto C, auto W) {
                 auto go = [&](auto L) {
-                    constexpr int kCta = join_cta(T()), kTeams = kCta / T();
-                    constexpr int kBytes = T() > 512 ? (L() ? 5 : 3) * 8 * T() * 4 : (kTeams > 1 ? kTeams * 8 * T() * 4 : 0);
-                    auto kernel = join_grad_kernel<S(), B(), L(), T(), W()>;
-                    if (kBytes > 48 * 1024) {
-                        const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+                    const int cta = cta_of(e->dim), bytes = C() == 3 ? (L() ? 5 : 3) * 8 * cta * 4 : (C() == 0 ? 8 * cta * 4 : 0);
+                    auto kernel = join_grad_kernel<S(), B(), L(), C(), W()>;
+                    if (bytes > 48 * 1024) {
+                        const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
                         if (ce != cudaSuccess) return launched(ce, "join_grad_kernel");
                     }
-                    return launched(launch_in_row(kernel, dim3(unsigned(ctas)), kCta, kBytes, 1, s, a BAOC_CHECK_ARG(ck)), "join_grad_kernel");
+                    return launched(launch_in_row(kernel, dim3(unsigned(ctas)), unsigned(cta), size_t(bytes), 1, s, a BAOC_CHECK_ARG(ck)), "join_grad_kernel");
                 };
                 return layer ? go(std::true_type{}) : go(std::false_type{});
             });
