@@ -35,6 +35,7 @@ constexpr int kJoinSums = 5;                   // column sums of the gradient: w
 // How a row is spread: kClass 0, one warp; 1, 2 and 3, a CTA of as many warps as it needs, up to 8, 16 and 32 (what differs is
 // the registers a thread may have).
 __host__ __device__ constexpr int class_threads(int c) { return c == 0 ? 32 * kSoloWarps : 128 << c; }
+__host__ __device__ constexpr int join_rows(int c) { return c < 3 ? 2 : 1; }       // rows of a team at a time, forwards
 template <int kClass>
 __device__ __forceinline__ int team_size() { return kClass == 0 ? 32 : int(blockDim.x); }
 
@@ -71,18 +72,22 @@ struct RowPart {
             }
         }
     }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
+    __device__ __forceinline__ void get(f32x2 (&x)[4]) const {
         if constexpr (DT == BAOC_F32) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+            for (int j = 0; j < 4; ++j) x[j] = pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
         } else if constexpr (kWide) {
-            unpack8(make_uint4(w[0], w[1], w[2], w[3]), x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = pack2(bf16_lo(w[j]), bf16_hi(w[j]));
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j] << 16);
+            for (int j = 0; j < 4; ++j) x[j] = pack2(bf16_lo(w[2 * j]), bf16_lo(w[2 * j + 1]));
         }
     }
-    static __device__ __forceinline__ void store(char* row, int t, int dim, const float (&x)[8]) {
+    static __device__ __forceinline__ void store(char* row, int t, int dim, const f32x2 (&v)[4]) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) unpack2(v[j], x[2 * j], x[2 * j + 1]);
         if constexpr (kWide) {
             if (t * kJoinCols >= dim) return;
             char* p = row + t * kJoinCols * kSize;
@@ -112,57 +117,105 @@ struct RowPart {
             }
         }
     }
+    // v less m, and zero where there is no column.  (kWide: a thread has all of its columns or none; one without any leaves the
+    // sums at zero and the rest alone.)
+    static __device__ __forceinline__ void centre(f32x2 (&v)[4], float m, int t, int dim) {
+        const f32x2 m2 = splat2(-m);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = add2(v[j], m2);
+        if constexpr (!kWide) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float a, b;
+                unpack2(v[j], a, b);
+                v[j] = pack2(column(t, 2 * j) < dim ? a : 0.f, column(t, 2 * j + 1) < dim ? b : 0.f);
+            }
+        }
+    }
 };
+
+__device__ __forceinline__ float sum8(const f32x2 (&v)[4]) {
+    float a, b;
+    unpack2(add2(add2(v[0], v[1]), add2(v[2], v[3])), a, b);
+    return a + b;
+}
+__device__ __forceinline__ float dot8(const f32x2 (&v)[4], const f32x2 (&w)[4]) {
+    float a, b;
+    unpack2(fma2(v[3], w[3], fma2(v[2], w[2], fma2(v[1], w[1], mul2(v[0], w[0])))), a, b);
+    return a + b;
+}
 
 // A thread's 8 values of a vector per column (fp32, 4-byte aligned; read over and over, from L1); `other` where there is none.
 template <int kClass, bool kWide>
-__device__ __forceinline__ void per_column(const float* v, int t, int dim, float other, float (&x)[8]) {
+__device__ __forceinline__ void per_column(const float* v, int t, int dim, float other, f32x2 (&x)[4]) {
     using P = RowPart<BAOC_F32, kClass, kWide>;
     if (kWide && v && t * kJoinCols < dim) {
         const float4 a = __ldg(reinterpret_cast<const float4*>(v + t * kJoinCols)), b = __ldg(reinterpret_cast<const float4*>(v + t * kJoinCols) + 1);
-        f4_to8(a, b, x);
+        x[0] = pack2(a.x, a.y); x[1] = pack2(a.z, a.w); x[2] = pack2(b.x, b.y); x[3] = pack2(b.z, b.w);
         return;
     }
+    auto one = [&](int j) { return v && P::column(t, j) < dim ? __ldg(v + P::column(t, j)) : other; };
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = v && P::column(t, j) < dim ? __ldg(v + P::column(t, j)) : other;
+    for (int j = 0; j < 4; ++j) x[j] = pack2(one(2 * j), one(2 * j + 1));
 }
 
-// Sums of K <= 4 values over a team, the same in all of its threads.  A CTA's warps take turns of two buffers, so that one
-// barrier a round is enough; all of its threads call it.
+// Sums of K = 1, 2 or 4 values over a team, the same in all of its threads.  In a warp the lanes first share the values out (a
+// lane keeps half of them and adds its neighbour's half, so 4 values cost 6 shuffles and not 20).  A CTA's warps take turns of
+// two buffers, so that one barrier a round is enough; all of its threads call it.
 template <int kClass>
 struct TeamSum {
     float4 (*buf)[32];               // [2][warps]
     int turn = 0;
     template <int K>
     __device__ __forceinline__ void operator()(float (&v)[K]) {
-        static_assert(K <= 4, "");
+        static_assert(K == 1 || K == 2 || K == 4, "");
+        constexpr uint32_t kAll = 0xffffffffu;
+        const int lane = threadIdx.x & 31;
+        float r = v[0];
+        int at = 0;                  // which of the values this lane ends up with
+        if constexpr (K == 4) {
+            const bool odd = lane & 1;
+            const float a = (odd ? v[2] : v[0]) + __shfl_xor_sync(kAll, odd ? v[0] : v[2], 1), b = (odd ? v[3] : v[1]) + __shfl_xor_sync(kAll, odd ? v[1] : v[3], 1);
+            const bool up = lane & 2;
+            r = (up ? b : a) + __shfl_xor_sync(kAll, up ? a : b, 2);
+            at = (odd ? 2 : 0) + (up ? 1 : 0);
+        } else if constexpr (K == 2) {
+            const bool odd = lane & 1;
+            r = (odd ? v[1] : v[0]) + __shfl_xor_sync(kAll, odd ? v[0] : v[1], 1);
+            at = odd;
+        }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
+        for (int o = K; o < 32; o <<= 1) r += __shfl_xor_sync(kAll, r, o);
+        if constexpr (kClass == 0) {
+            v[0] = r;
+            if constexpr (K > 1) {
+                constexpr int kFrom[4] = {0, K == 4 ? 2 : 1, 1, 3};      // a lane that has value k
 #pragma unroll
-            for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        if constexpr (kClass > 0) {
-            const int lane = threadIdx.x & 31, warps = int(blockDim.x) >> 5;
-            if (lane == 0) buf[turn][threadIdx.x >> 5] = make_float4(v[0], K > 1 ? v[K > 1 ? 1 : 0] : 0.f, K > 2 ? v[K > 2 ? 2 : 0] : 0.f, K > 3 ? v[K > 3 ? 3 : 0] : 0.f);
+                for (int k = 0; k < K; ++k) v[k] = __shfl_sync(kAll, r, kFrom[k]);
+            }
+        } else {
+            const int warps = int(blockDim.x) >> 5;
+            if (lane < K) reinterpret_cast<float*>(&buf[turn][threadIdx.x >> 5])[at] = r;
             __syncthreads();
+            float4 s;
             if constexpr (kClass == 1) {             // up to 8 warps: every thread adds them up
-                float4 s = buf[turn][0];
+                s = buf[turn][0];
                 for (int w = 1; w < warps; ++w) {
                     const float4 o = buf[turn][w];
                     s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
                 }
-                const float all[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-                for (int k = 0; k < K; ++k) v[k] = all[k];
             } else {
-                const float4 s = lane < warps ? buf[turn][lane] : make_float4(0.f, 0.f, 0.f, 0.f);
-                const float all[4] = {s.x, s.y, s.z, s.w};
+                s = lane < warps ? buf[turn][lane] : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int k = 0; k < K; ++k) v[k] = all[k];
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-                    for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+                for (int o = 16; o > 0; o >>= 1) {
+                    s.x += __shfl_xor_sync(kAll, s.x, o);
+                    if constexpr (K > 1) s.y += __shfl_xor_sync(kAll, s.y, o);
+                    if constexpr (K > 2) { s.z += __shfl_xor_sync(kAll, s.z, o); s.w += __shfl_xor_sync(kAll, s.w, o); }
+                }
             }
+            const float all[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = all[k];
             turn ^= 1;
         }
     }
@@ -177,9 +230,10 @@ struct JoinArgs {
     float scale, eps;
 };
 
+// kRows rows of a team at a time: their sums share a barrier, and a weight is loaded once for them.
 template <int S, int B, int kClass, bool kWide>
 __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps * 32 / class_threads(kClass) : 1) join_kernel(const JoinArgs g) {
-    constexpr int kTeams = kClass == 0 ? kSoloWarps : 1;
+    constexpr int kTeams = kClass == 0 ? kSoloWarps : 1, kRows = join_rows(kClass);
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;
     __shared__ float4 buf[kClass > 0 ? 2 : 1][32];
@@ -187,65 +241,76 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps
     begin_in_row();
     const int t = kClass == 0 ? int(threadIdx.x & 31) : int(threadIdx.x), team = kClass == 0 ? int(threadIdx.x >> 5) : 0, dim = g.dim;
     const float over = 1.f / float(dim);
-    const int64_t step = int64_t(gridDim.x) * kTeams;
-    const bool in = kWide ? t * kJoinCols < dim : true;
-    bool inside[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) inside[j] = kWide ? in : Stream::column(t, j) < dim;
-    // v without its mean (layer norm), and 1 / sqrt(mean square + eps)
-    auto normalise = [&](float (&v)[8]) {
-        float s[1];
+    const int64_t step = int64_t(gridDim.x) * kTeams * kRows;
+    const bool in = !kWide || t * kJoinCols < dim;
+    // v without its mean (layer norm), times 1 / sqrt(mean square + eps) * w + b
+    auto norm = [&](f32x2 (&v)[kRows][4], const float* weight, const float* bias) {
+        float s[kRows];
         if (g.layer) {
-            s[0] = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[0] += v[j];
+            for (int r = 0; r < kRows; ++r) s[r] = sum8(v[r]);
             sum(s);
-            const float mean = s[0] * over;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = inside[j] ? v[j] - mean : 0.f;
+            for (int r = 0; r < kRows; ++r) Stream::centre(v[r], s[r] * over, t, dim);
         }
-        s[0] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += v[j] * v[j];
+        for (int r = 0; r < kRows; ++r) s[r] = in ? dot8(v[r], v[r]) : 0.f;
         sum(s);
-        return rsqrtf(s[0] * over + g.eps);
+        f32x2 w[4];
+        per_column<kClass, kWide>(weight, t, dim, 0.f, w);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const f32x2 k = splat2(rsqrtf(s[r] * over + g.eps));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[r][j] = mul2(mul2(v[r][j], k), w[j]);
+        }
+        if (bias) {
+            per_column<kClass, kWide>(bias, t, dim, 0.f, w);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[r][j] = add2(v[r][j], w[j]);
+        }
     };
-    Stream next_x;
-    Branch next_f;
+    Stream next_x[kRows];
+    Branch next_f[kRows];
     auto fetch = [&](int64_t row) {
-        if (row < g.rows) {
-            next_f.load(g.f + row * g.f_step, t, dim);
-            if (g.x) next_x.load(g.x + row * g.x_step, t, dim);
-        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (row + r < g.rows) {
+                next_f[r].load(g.f + (row + r) * g.f_step, t, dim);
+                if (g.x) next_x[r].load(g.x + (row + r) * g.x_step, t, dim);
+            }
     };
-    next_x.clear();
-    next_f.clear();
-    int64_t row = int64_t(blockIdx.x) * kTeams + team;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        next_x[r].clear();
+        next_f[r].clear();
+    }
+    int64_t row = (int64_t(blockIdx.x) * kTeams + team) * kRows;
     fetch(row);
-    for (; row < g.rows; row += step) {          // (alike in a team)
-        float x[8], u[8], w[8];
-        next_x.get(x);
-        next_f.get(u);
-        fetch(row + step);                       // (the next row is on its way while this one is reduced)
-        if (g.post_w) {
-            const float r = normalise(u);
-            float b[8];
-            per_column<kClass, kWide>(g.post_w, t, dim, 0.f, w);
-            per_column<kClass, kWide>(g.post_b, t, dim, 0.f, b);
+    const f32x2 scale = splat2(g.scale);
+    for (; row < g.rows; row += step) {          // (alike in a team; a last row without a second computes on zeros or an old row)
+        f32x2 x[kRows][4], u[kRows][4], w[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = u[j] * r * w[j] + b[j];
+        for (int r = 0; r < kRows; ++r) {
+            next_x[r].get(x[r]);
+            next_f[r].get(u[r]);
         }
-        per_column<kClass, kWide>(g.gate ? g.gate + (g.rows_per_gate ? int64_t(uint32_t(row) / uint32_t(g.rows_per_gate)) : 0) * dim : nullptr, t, dim, 1.f, w);
+        fetch(row + step);                       // (the next rows are on their way while these are reduced)
+        if (g.post_w) norm(u, g.post_w, g.post_b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = g.scale * x[j] + w[j] * u[j];
-        Stream::store(g.y + row * g.y_step, t, dim, u);
-        const float r = normalise(u);
-        float b[8];
-        per_column<kClass, kWide>(g.pre_w, t, dim, 0.f, w);
-        per_column<kClass, kWide>(g.pre_b, t, dim, 0.f, b);
+        for (int r = 0; r < kRows; ++r) {
+            if (r == 0 || g.rows_per_gate)
+                per_column<kClass, kWide>(g.gate ? g.gate + (g.rows_per_gate ? int64_t(uint32_t(min64(row + r, g.rows - 1)) / uint32_t(g.rows_per_gate)) : 0) * dim : nullptr, t, dim, 1.f, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = u[j] * r * w[j] + b[j];
-        Branch::store(g.h + row * g.h_step, t, dim, u);
+            for (int j = 0; j < 4; ++j) u[r][j] = fma2(scale, x[r][j], mul2(w[j], u[r][j]));
+            if (row + r < g.rows) Stream::store(g.y + (row + r) * g.y_step, t, dim, u[r]);
+        }
+        norm(u, g.pre_w, g.pre_b);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (row + r < g.rows) Branch::store(g.h + (row + r) * g.h_step, t, dim, u[r]);
     }
 }
 
@@ -295,16 +360,23 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
     if (!check_range(ck, kKerJoinGrad, part, int64_t(kJoinSums + 1) * dim * 4, 0)) return;
 #endif
     const bool need_f = g.post_w || g.gate;
-    float acc[kShared ? 1 : kSums][8] = {};
-    auto add = [&](int k, int j, float v) {
-        if constexpr (kShared) dynamic[(k * 8 + j) * kTeam + t] += v;
-        else acc[k][j] += v;
+    f32x2 acc[kShared ? 1 : kSums][4] = {};
+    auto add = [&](int k, int j, f32x2 a, f32x2 b) {             // a * b to the sums of columns 2 j and 2 j + 1
+        if constexpr (kShared) {
+            float* p = dynamic + (k * 8 + 2 * j) * kTeam + t;
+            float x, y;
+            unpack2(fma2(a, b, pack2(p[0], p[kTeam])), x, y);
+            p[0] = x;
+            p[kTeam] = y;
+        } else {
+            acc[k][j] = fma2(a, b, acc[k][j]);
+        }
     };
     auto zero = [&](int k) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (kShared) dynamic[(k * 8 + j) * kTeam + t] = 0.f;
-            else acc[k][j] = 0.f;
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (kShared) dynamic[(k * 8 + 2 * j) * kTeam + t] = dynamic[(k * 8 + 2 * j + 1) * kTeam + t] = 0.f;
+            else acc[k][j] = 0;
         }
     };
     // the sum k of all teams to f(column, value), each column by one thread; all threads call it
@@ -312,9 +384,13 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
         constexpr int k = decltype(which)::value;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (kShared) v[j] = dynamic[(k * 8 + j) * kTeam + t];
-            else v[j] = acc[k][j];
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (kShared) {
+                v[2 * j] = dynamic[(k * 8 + 2 * j) * kTeam + t];
+                v[2 * j + 1] = dynamic[(k * 8 + 2 * j + 1) * kTeam + t];
+            } else {
+                unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
+            }
         }
         if constexpr (kTeams > 1) {
             __syncthreads();
@@ -332,9 +408,7 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
     };
     if constexpr (kShared)
         for (int k = 0; k < kSums; ++k) zero(k);
-    bool inside[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) inside[j] = kWide ? t * kJoinCols < dim : Stream::column(t, j) < dim;
+    const bool in = !kWide || t * kJoinCols < dim;
     Stream next_y, next_dy;
     Branch next_f, next_dh;
     auto fetch = [&](int64_t row, int64_t last) {
@@ -356,74 +430,73 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
         if (kAhead) fetch(seg + team, seg_end);
         for (int64_t row = seg + team; row < seg_end; row += kTeams) {       // (alike in a team)
             if (!kAhead) fetch(row, seg_end);
-            float y[8], d[8], f[8], w[8];        // d: from dh to Dy
+            f32x2 y[4], d[4], f[4], dy[4], w[4];         // d: from dh to Dy
             next_y.get(y);
             next_dh.get(d);
             next_f.get(f);
-            float dy[8];
             next_dy.get(dy);
             if (kAhead) fetch(row + kTeams, seg_end);
-            float mean_f = 0.f, r_y, r_f;
             if constexpr (kLayer) {
-                float s[2] = {0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { s[0] += y[j]; s[1] += f[j]; }
+                float s[2] = {sum8(y), sum8(f)};
                 sum(s);
-                mean_f = s[1] * over;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = inside[j] ? y[j] - s[0] * over : 0.f;
+                Stream::centre(y, s[0] * over, t, dim);
+                Stream::centre(f, s[1] * over, t, dim);
             }
             per_column<kClass, kWide>(g.pre_w, t, dim, 0.f, w);
+            float r_f;
             {
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                f32x2 dn[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float dn = d[j] * w[j], c = kLayer ? (inside[j] ? f[j] - mean_f : 0.f) : f[j];
-                    s[0] += y[j] * y[j];
-                    s[1] += c * c;
-                    s[2] += dn * y[j];
-                    if (kLayer) s[3] += dn;
-                }
+                for (int j = 0; j < 4; ++j) dn[j] = mul2(d[j], w[j]);
+                float s[4] = {in ? dot8(y, y) : 0.f, in ? dot8(f, f) : 0.f, dot8(dn, y), kLayer ? sum8(dn) : 0.f};
                 sum(s);
-                r_y = rsqrtf(s[0] * over + g.eps);
+                const float r_y = rsqrtf(s[0] * over + g.eps);
                 r_f = rsqrtf(s[1] * over + g.eps);
-                const float slope = r_y * r_y * s[2] * over, mean = s[3] * over;
+                const f32x2 r2 = splat2(r_y), slope = splat2(-r_y * r_y * s[2] * over), mean = splat2(-s[3] * over);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    add(kPreW, j, d[j] * y[j] * r_y);
-                    if (kLayer) add(kPreB, j, d[j]);
-                    d[j] = dy[j] + r_y * (d[j] * w[j] - y[j] * slope - mean);
-                    dy[j] = g.scale * d[j];
+                for (int j = 0; j < 4; ++j) {
+                    add(kPreW, j, d[j], mul2(y[j], r2));
+                    if (kLayer) add(kPreB, j, d[j], splat2(1.f));
+                    d[j] = fma2(r2, kLayer ? add2(fma2(y[j], slope, dn[j]), mean) : fma2(y[j], slope, dn[j]), dy[j]);
                 }
             }
-            if (g.dx) Stream::store(g.dx + row * g.dx_step, t, dim, dy);
-            float gt[8];
-            per_column<kClass, kWide>(gate, t, dim, 1.f, gt);
+            if (g.dx) {
+                const f32x2 scale = splat2(g.scale);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dy[j] = mul2(scale, d[j]);
+                Stream::store(g.dx + row * g.dx_step, t, dim, dy);
+            }
             if (g.post_w) {
-                float b[8];
+                const f32x2 r2 = splat2(r_f);
+                f32x2 b[4];
                 per_column<kClass, kWide>(g.post_w, t, dim, 0.f, w);
-                per_column<kClass, kWide>(kLayer ? g.post_b : nullptr, t, dim, 0.f, b);
-                float s[2] = {0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float n = (kLayer ? (inside[j] ? f[j] - mean_f : 0.f) : f[j]) * r_f;
-                    const float du = gt[j] * (inside[j] ? d[j] : 0.f);
-                    add(kGate, j, d[j] * (n * w[j] + b[j]));
-                    add(kPostW, j, du * n);
-                    if (kLayer) add(kPostB, j, du);
-                    f[j] = n;
-                    d[j] = du * w[j];
-                    s[0] += d[j] * n;
-                    s[1] += d[j];
+                for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], r2);
+                if (gate) {
+                    if (kLayer) per_column<kClass, kWide>(g.post_b, t, dim, 0.f, b);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) add(kGate, j, d[j], kLayer ? fma2(f[j], w[j], b[j]) : mul2(f[j], w[j]));
+                    per_column<kClass, kWide>(gate, t, dim, 1.f, b);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[j] = mul2(d[j], b[j]);
                 }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    add(kPostW, j, d[j], f[j]);
+                    if (kLayer) add(kPostB, j, d[j], splat2(1.f));
+                    d[j] = mul2(d[j], w[j]);
+                }
+                float s[2] = {dot8(d, f), kLayer ? sum8(d) : 0.f};
                 sum(s);
+                const f32x2 slope = splat2(-s[0] * over), mean = splat2(-s[1] * over);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] = r_f * (d[j] - f[j] * (s[0] * over) - (kLayer ? s[1] * over : 0.f));
-            } else {
+                for (int j = 0; j < 4; ++j) d[j] = mul2(r2, kLayer ? add2(fma2(f[j], slope, d[j]), mean) : fma2(f[j], slope, d[j]));
+            } else if (gate) {
+                per_column<kClass, kWide>(gate, t, dim, 1.f, w);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    add(kGate, j, d[j] * f[j]);
-                    d[j] *= gt[j];
+                for (int j = 0; j < 4; ++j) {
+                    add(kGate, j, d[j], f[j]);
+                    d[j] = mul2(d[j], w[j]);
                 }
             }
             Branch::store(g.df + row * g.df_step, t, dim, d);
@@ -622,7 +695,7 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
         return with_class(e->dim, wide, [&](auto C, auto W) {
-            const unsigned grid = unsigned(std::min(ceil_div(rows, rows_of(e->dim)), ctas_at_once(e->dim, kJoinWarps)));
+            const unsigned grid = unsigned(std::min(ceil_div(rows, rows_of(e->dim) * join_rows(C())), ctas_at_once(e->dim, kJoinWarps)));
             return launched(launch_in_row(join_kernel<S(), B(), C(), W()>, dim3(grid), unsigned(cta_of(e->dim)), 0, 1, s, a), "join_kernel");
         });
     });
