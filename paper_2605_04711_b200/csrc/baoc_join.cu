@@ -35,7 +35,7 @@ constexpr int kJoinSums = 5;                   // column sums of the gradient: w
 // How a row is spread: kClass 0, one warp; 1, 2 and 3, a CTA of as many warps as it needs, up to 8, 16 and 32 (what differs is
 // the registers a thread may have).
 __host__ __device__ constexpr int class_threads(int c) { return c == 0 ? 32 * kSoloWarps : 128 << c; }
-__host__ __device__ constexpr int join_rows(int c) { return c < 3 ? 2 : 1; }       // rows of a team at a time, forwards
+__host__ __device__ constexpr int join_rows(int c) { return c < 0 ? 2 : 1; }       // rows of a team at a time, forwards
 template <int kClass>
 __device__ __forceinline__ int team_size() { return kClass == 0 ? 32 : int(blockDim.x); }
 
@@ -145,7 +145,7 @@ __device__ __forceinline__ float dot8(const f32x2 (&v)[4], const f32x2 (&w)[4]) 
     return a + b;
 }
 
-// A thread's 8 values of a vector per column (fp32, 4-byte aligned; read over and over, from L1); `other` where there is none.
+// A thread's 8 values of a vector per column (fp32, 4-byte aligned); `other` where there is none.
 template <int kClass, bool kWide>
 __device__ __forceinline__ void per_column(const float* v, int t, int dim, float other, f32x2 (&x)[4]) {
     using P = RowPart<BAOC_F32, kClass, kWide>;
@@ -158,6 +158,27 @@ __device__ __forceinline__ void per_column(const float* v, int t, int dim, float
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = pack2(one(2 * j), one(2 * j + 1));
 }
+
+// The same, read row after row: kept in the thread's own places of shared memory (from L1 or L2 each would cost its latency in
+// every row, and registers have the row).
+struct Kept {
+    float4* at;                      // [vector][2][threads]
+    __device__ __forceinline__ float4* place(int which) const { return at + which * 2 * int(blockDim.x) + int(threadIdx.x); }
+    __device__ __forceinline__ void put(int which, const f32x2 (&x)[4]) const {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) unpack2(x[j], v[2 * j], v[2 * j + 1]);
+        float4* p = place(which);
+        p[0] = make_float4(v[0], v[1], v[2], v[3]);
+        p[blockDim.x] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    __device__ __forceinline__ void get(int which, f32x2 (&x)[4]) const {
+        const float4* p = place(which);
+        const float4 a = p[0], b = p[blockDim.x];
+        x[0] = pack2(a.x, a.y); x[1] = pack2(a.z, a.w); x[2] = pack2(b.x, b.y); x[3] = pack2(b.z, b.w);
+    }
+};
+enum Vector : int { kVPreW = 0, kVPostW = 1, kVGate = 2, kVPostB = 3, kVPreB = 4 };
 
 // Sums of K = 1, 2 or 4 values over a team, the same in all of its threads.  In a warp the lanes first share the values out (a
 // lane keeps half of them and adds its neighbour's half, so 4 values cost 6 shuffles and not 20).  A CTA's warps take turns of
@@ -225,7 +246,7 @@ struct JoinArgs {
     const char *x, *f;
     char *y, *h;
     const float *post_w, *post_b, *gate, *pre_w, *pre_b;
-    int64_t x_step, f_step, y_step, h_step, rows, rows_per_gate;
+    int64_t x_step, f_step, y_step, h_step, rows, rows_per_gate, rows_per_cta;
     int dim, layer;
     float scale, eps;
 };
@@ -241,10 +262,18 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps
     begin_in_row();
     const int t = kClass == 0 ? int(threadIdx.x & 31) : int(threadIdx.x), team = kClass == 0 ? int(threadIdx.x >> 5) : 0, dim = g.dim;
     const float over = 1.f / float(dim);
-    const int64_t step = int64_t(gridDim.x) * kTeams * kRows;
+    constexpr int64_t step = kTeams * kRows;
+    const int64_t end = min64(g.rows, (int64_t(blockIdx.x) + 1) * g.rows_per_cta);
     const bool in = !kWide || t * kJoinCols < dim;
+    extern __shared__ float4 dynamic4[];
+    const Kept kept{dynamic4};
+    auto keep = [&](int which, const float* v, float other) {
+        f32x2 x[4];
+        per_column<kClass, kWide>(v, t, dim, other, x);
+        kept.put(which, x);
+    };
     // v without its mean (layer norm), times 1 / sqrt(mean square + eps) * w + b
-    auto norm = [&](f32x2 (&v)[kRows][4], const float* weight, const float* bias) {
+    auto norm = [&](f32x2 (&v)[kRows][4], int weight, int bias) {
         float s[kRows];
         if (g.layer) {
 #pragma unroll
@@ -257,15 +286,15 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps
         for (int r = 0; r < kRows; ++r) s[r] = in ? dot8(v[r], v[r]) : 0.f;
         sum(s);
         f32x2 w[4];
-        per_column<kClass, kWide>(weight, t, dim, 0.f, w);
+        kept.get(weight, w);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             const f32x2 k = splat2(rsqrtf(s[r] * over + g.eps));
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[r][j] = mul2(mul2(v[r][j], k), w[j]);
         }
-        if (bias) {
-            per_column<kClass, kWide>(bias, t, dim, 0.f, w);
+        if (g.layer) {
+            kept.get(bias, w);
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -277,7 +306,7 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps
     auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
-            if (row + r < g.rows) {
+            if (row + r < end) {
                 next_f[r].load(g.f + (row + r) * g.f_step, t, dim);
                 if (g.x) next_x[r].load(g.x + (row + r) * g.x_step, t, dim);
             }
@@ -287,10 +316,20 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps
         next_x[r].clear();
         next_f[r].clear();
     }
-    int64_t row = (int64_t(blockIdx.x) * kTeams + team) * kRows;
+    int64_t row = int64_t(blockIdx.x) * g.rows_per_cta + team * kRows, gate_row = 0;      // gate_row: the first that the kept gate is not for
     fetch(row);
+    keep(kVPreW, g.pre_w, 0.f);
+    if (g.post_w) keep(kVPostW, g.post_w, 0.f);
+    if (g.layer) {
+        keep(kVPreB, g.pre_b, 0.f);
+        if (g.post_w) keep(kVPostB, g.post_b, 0.f);
+    }
+    if (g.gate && !g.rows_per_gate) {
+        keep(kVGate, g.gate, 0.f);
+        gate_row = g.rows;
+    }
     const f32x2 scale = splat2(g.scale);
-    for (; row < g.rows; row += step) {          // (alike in a team; a last row without a second computes on zeros or an old row)
+    for (; row < end; row += step) {             // (alike in a team; a last row without a second computes on zeros or an old row)
         f32x2 x[kRows][4], u[kRows][4], w[4];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -298,19 +337,27 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps
             next_f[r].get(u[r]);
         }
         fetch(row + step);                       // (the next rows are on their way while these are reduced)
-        if (g.post_w) norm(u, g.post_w, g.post_b);
+        if (g.post_w) norm(u, kVPostW, kVPostB);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            if (r == 0 || g.rows_per_gate)
-                per_column<kClass, kWide>(g.gate ? g.gate + (g.rows_per_gate ? int64_t(uint32_t(min64(row + r, g.rows - 1)) / uint32_t(g.rows_per_gate)) : 0) * dim : nullptr, t, dim, 1.f, w);
+            if (g.gate) {
+                if (row + r >= gate_row && row + r < end) {
+                    const int64_t group = uint32_t(row + r) / uint32_t(g.rows_per_gate);
+                    gate_row = (group + 1) * g.rows_per_gate;
+                    keep(kVGate, g.gate + group * dim, 0.f);
+                }
+                if (r == 0 || g.rows_per_gate) kept.get(kVGate, w);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) u[r][j] = fma2(scale, x[r][j], mul2(w[j], u[r][j]));
-            if (row + r < g.rows) Stream::store(g.y + (row + r) * g.y_step, t, dim, u[r]);
+                for (int j = 0; j < 4; ++j) u[r][j] = mul2(w[j], u[r][j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[r][j] = fma2(scale, x[r][j], u[r][j]);
+            if (row + r < end) Stream::store(g.y + (row + r) * g.y_step, t, dim, u[r]);
         }
-        norm(u, g.pre_w, g.pre_b);
+        norm(u, kVPreW, kVPreB);
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
-            if (row + r < g.rows) Branch::store(g.h + (row + r) * g.h_step, t, dim, u[r]);
+            if (row + r < end) Branch::store(g.h + (row + r) * g.h_step, t, dim, u[r]);
     }
 }
 
@@ -345,10 +392,12 @@ template <int S, int B, bool kLayer, int kClass, bool kWide>
 __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kClass < 3 ? kJoinGradWarps * 32 / class_threads(kClass) : 1)) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
     constexpr int kTeams = kClass == 0 ? kSoloWarps : 1, kSums = kLayer ? 5 : 3;
     constexpr bool kShared = kClass == 3;        // (64 registers a thread: the sums lie in shared memory, and no row is fetched ahead)
-    constexpr bool kAhead = !kShared;
+    constexpr bool kAhead = !kShared, kKeep = !kShared;     // (shared memory has no room for the sums and the vectors)
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;
-    extern __shared__ float dynamic[];           // kShared: [kSums][8][threads]; several teams: [kTeams][8][32]
+    extern __shared__ float4 dynamic4[];         // kKeep: [3 or 4 vectors][2][threads]; then floats, kShared: [kSums][8][threads]; several teams: [kTeams][8][32]
+    const Kept kept{dynamic4};
+    float* dynamic = reinterpret_cast<float*>(dynamic4 + (kKeep ? (kLayer ? 4 : 3) * 2 * int(blockDim.x) : 0));
     __shared__ float4 buf[kClass > 0 ? 2 : 1][32];
     TeamSum<kClass> sum{buf};
     begin_in_row();
@@ -423,11 +472,27 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
     next_dh.clear();
     next_dy.clear();
     next_f.clear();
+    auto keep = [&](int which, const float* v) {
+        f32x2 x[4];
+        per_column<kClass, kWide>(v, t, dim, 0.f, x);
+        kept.put(which, x);
+    };
+    auto vector = [&](int which, const float* v, f32x2 (&x)[4]) {
+        if constexpr (kKeep) kept.get(which, x);
+        else per_column<kClass, kWide>(v, t, dim, 0.f, x);
+    };
+    if constexpr (kKeep) {
+        keep(kVPreW, g.pre_w);
+        if (g.post_w) keep(kVPostW, g.post_w);
+        if (kLayer && g.post_w) keep(kVPostB, g.post_b);
+        if (g.gate && !g.rows_per_gate) keep(kVGate, g.gate);
+    }
     for (int64_t seg = begin; seg < end;) {
         const int64_t group = g.rows_per_gate ? seg / g.rows_per_gate : 0;
         const int64_t seg_end = g.rows_per_gate ? min64(end, (group + 1) * g.rows_per_gate) : end;
         const float* gate = g.gate ? g.gate + group * dim : nullptr;
         if (kAhead) fetch(seg + team, seg_end);
+        if (kKeep && g.rows_per_gate) keep(kVGate, gate);
         for (int64_t row = seg + team; row < seg_end; row += kTeams) {       // (alike in a team)
             if (!kAhead) fetch(row, seg_end);
             f32x2 y[4], d[4], f[4], dy[4], w[4];         // d: from dh to Dy
@@ -442,7 +507,7 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
                 Stream::centre(y, s[0] * over, t, dim);
                 Stream::centre(f, s[1] * over, t, dim);
             }
-            per_column<kClass, kWide>(g.pre_w, t, dim, 0.f, w);
+            vector(kVPreW, g.pre_w, w);
             float r_f;
             {
                 f32x2 dn[4];
@@ -469,14 +534,14 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
             if (g.post_w) {
                 const f32x2 r2 = splat2(r_f);
                 f32x2 b[4];
-                per_column<kClass, kWide>(g.post_w, t, dim, 0.f, w);
+                vector(kVPostW, g.post_w, w);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], r2);
                 if (gate) {
-                    if (kLayer) per_column<kClass, kWide>(g.post_b, t, dim, 0.f, b);
+                    if (kLayer) vector(kVPostB, g.post_b, b);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) add(kGate, j, d[j], kLayer ? fma2(f[j], w[j], b[j]) : mul2(f[j], w[j]));
-                    per_column<kClass, kWide>(gate, t, dim, 1.f, b);
+                    vector(kVGate, gate, b);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[j] = mul2(d[j], b[j]);
                 }
@@ -492,7 +557,7 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
 #pragma unroll
                 for (int j = 0; j < 4; ++j) d[j] = mul2(r2, kLayer ? add2(fma2(f[j], slope, d[j]), mean) : fma2(f[j], slope, d[j]));
             } else if (gate) {
-                per_column<kClass, kWide>(gate, t, dim, 1.f, w);
+                vector(kVGate, gate, w);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     add(kGate, j, d[j], f[j]);
@@ -535,6 +600,7 @@ __global__ void __launch_bounds__(1024) join_sums_kernel(const JoinGradArgs g, i
     auto total = [&](int64_t c0, int64_t c1, int64_t group, int k, int64_t at) {
         float s = 0.f;
         if (col < g.dim)
+#pragma unroll 8
             for (int64_t c = c0 + warp; c <= c1; c += 32) {
                 const int slot = group < 0 || group == c * g.rows_per_cta / g.rows_per_gate ? k : kJoinSums;
                 s += g.part[(c * (kJoinSums + 1) + slot) * g.dim + col];
@@ -690,13 +756,20 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
     if ((overlap(ry, rx, rows) && !same(ry, rx, rows)) || overlap(ry, rf, rows) || (overlap(rh, rf, rows) && !same(rh, rf, rows)) || overlap(rh, rx, rows) ||
         overlap(ry, rh, rows))
         return fail_join(BAOC_E_INVALID, "baoc_join: y may be x and h may be f; arrays overlap in no other way");
-    const JoinArgs a{static_cast<const char*>(x), static_cast<const char*>(f), static_cast<char*>(y), static_cast<char*>(h), post_w, post_b, gate, pre_w, pre_b,
-                     rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
+    JoinArgs a{static_cast<const char*>(x), static_cast<const char*>(f), static_cast<char*>(y), static_cast<char*>(h), post_w, post_b, gate, pre_w, pre_b,
+                     rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate, 0, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
         return with_class(e->dim, wide, [&](auto C, auto W) {
-            const unsigned grid = unsigned(std::min(ceil_div(rows, rows_of(e->dim) * join_rows(C())), ctas_at_once(e->dim, kJoinWarps)));
-            return launched(launch_in_row(join_kernel<S(), B(), C(), W()>, dim3(grid), unsigned(cta_of(e->dim)), 0, 1, s, a), "join_kernel");
+            // whole rounds of a CTA's teams; all CTAs at once
+            const int cta = cta_of(e->dim), round = rows_of(e->dim) * join_rows(C()), bytes = 5 * 8 * cta * 4;
+            a.rows_per_cta = round_up(ceil_div(rows, ctas_at_once(e->dim, kJoinWarps)), round);
+            auto kernel = join_kernel<S(), B(), C(), W()>;
+            if (bytes > 40 * 1024) {             // (48 KB go without asking, the kernel's own arrays included)
+                const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                if (ce != cudaSuccess) return launched(ce, "join_kernel");
+            }
+            return launched(launch_in_row(kernel, dim3(unsigned(ceil_div(rows, a.rows_per_cta))), unsigned(cta), size_t(bytes), 1, s, a), "join_kernel");
         });
     });
 } catch (const std::bad_alloc&) {
@@ -760,9 +833,10 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
         rc = with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
             return with_class(e->dim, wide, [&](auto C, auto W) {
                 auto go = [&](auto L) {
-                    const int cta = cta_of(e->dim), bytes = C() == 3 ? (L() ? 5 : 3) * 8 * cta * 4 : (C() == 0 ? 8 * cta * 4 : 0);
+                    const int cta = cta_of(e->dim), sums = C() == 3 ? (L() ? 5 : 3) : (C() == 0 ? 1 : 0), kept = C() == 3 ? 0 : (L() ? 4 : 3);
+                    const int bytes = (sums + kept) * 8 * cta * 4;
                     auto kernel = join_grad_kernel<S(), B(), L(), C(), W()>;
-                    if (bytes > 48 * 1024) {
+                    if (bytes > 40 * 1024) {
                         const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
                         if (ce != cudaSuccess) return launched(ce, "join_grad_kernel");
                     }
