@@ -688,7 +688,7 @@ typedef struct {
 /* y[rows][dim] and h[rows][dim].  y may be x and h may be f (same pointer, type and
  * row stride); arrays overlap in no other way.  Pointers are aligned to their
  * elements; a dim that is a multiple of 8 in arrays whose bases and row strides are
- * multiples of 16 bytes takes the wide path.  rows <= 2^31, 0 queues nothing.  One
+ * multiples of 8 elements (weights: of 16 bytes) takes the wide path.  rows <= 2^31, 0 queues nothing.  One
  * kernel; does not wait. */
 int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* post_w, const float* post_b, const float* gate,
               const float* pre_w, const float* pre_b, int64_t rows, void* y, void* h, baoc_stream_t stream);

@@ -28,20 +28,27 @@ namespace baoc {
 constexpr int kJoinMaxDim = 8192;
 constexpr int64_t kJoinMaxStride = int64_t(1) << 28;
 constexpr int kJoinCols = 8;                   // columns of a thread
-constexpr int kSoloWarps = 4;                  // rows of up to 256 columns: one warp each, so many per CTA
-constexpr int kJoinWarps = 32, kJoinGradWarps = 16;    // warps per SM that the registers allow
+constexpr int kSoloWarps = 4;                  // rows that a warp takes alone: so many warps per CTA
+constexpr int kJoinWarps = 32, kJoinGradWarps = 16;    // warps per SM of the other rows' kernels
 constexpr int kJoinSums = 5;                   // column sums of the gradient: weight and bias of pre, of post, and the gate
 
-// How a row is spread: kClass 0, one warp; 1, 2 and 3, a CTA of as many warps as it needs, up to 8, 16 and 32 (what differs is
-// the registers a thread may have).
-__host__ __device__ constexpr int class_threads(int c) { return c == 0 ? 32 * kSoloWarps : 128 << c; }
-__host__ __device__ constexpr int join_rows(int c) { return c < 0 ? 2 : 1; }       // rows of a team at a time, forwards
+// How a row is spread.  Classes 1 to 3: one warp, each lane 1 to 3 times 8 columns (no barrier, and a sum's shuffles are paid
+// once a row: 16384 x 768 backwards 56 -> FIGURE us against three warps).  Classes 4, 5 and 6: a CTA of as many warps as the row
+// needs, up to 8, 16 and 32, 8 columns a thread (what differs is the registers that a thread may have).
+__host__ __device__ constexpr bool solo(int c) { return c <= 3; }
+__host__ __device__ constexpr int chunks_of(int c) { return c <= 3 ? c : 1; }
+__host__ __device__ constexpr int class_threads(int c) { return c <= 3 ? 32 * kSoloWarps : (c == 4 ? 256 : (c == 5 ? 512 : 1024)); }
+// warps per SM that the registers (and, backwards, the shared memory) allow
+__host__ __device__ constexpr int class_warps(int c) { return c == 1 ? 32 : (c == 2 ? 24 : (c == 3 ? 16 : kJoinWarps)); }
+__host__ __device__ constexpr int class_grad_warps(int c) { return c <= 2 ? 12 : (c == 3 ? 8 : kJoinGradWarps); }
+__host__ __device__ constexpr int class_blocks(int c, int warps) { return c == 6 ? 1 : warps * 32 / class_threads(c); }
+// Threads of a team as the columns are counted: a lane with several times 8 columns counts as so many threads.
 template <int kClass>
-__device__ __forceinline__ int team_size() { return kClass == 0 ? 32 : int(blockDim.x); }
+__device__ __forceinline__ int team_size() { return solo(kClass) ? 32 * chunks_of(kClass) : int(blockDim.x); }
 
 template <int DT, int kClass, bool kWide>
 struct RowPart {
-    // a thread's columns: 8 neighbours, or 8 that are a team's size apart
+    // a thread's 8 columns: neighbours, or a team's size apart
     static constexpr int kSize = DT == BAOC_BF16 ? 2 : 4;
     static constexpr int kWords = kWide ? 2 * kSize : 8;
     uint32_t w[kWords];
@@ -56,11 +63,11 @@ struct RowPart {
             clear();
             if (t * kJoinCols < dim) {
                 const char* p = row + t * kJoinCols * kSize;
-                const uint4 a = ld_stream_u4(p);
-                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
                 if constexpr (DT == BAOC_F32) {
-                    const uint4 b = ld_stream_u4(p + 16);
-                    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+                    ld_stream_u8(p, w);
+                } else {
+                    const uint4 a = ld_stream_u4(p);
+                    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
                 }
             }
         } else {
@@ -71,6 +78,12 @@ struct RowPart {
                 else w[j] = c < dim ? *reinterpret_cast<const uint32_t*>(row + 4 * c) : 0;
             }
         }
+    }
+    // The same of a bf16 row by way of shared memory: requested ahead, without a register.  A thread reads back what it requested
+    // itself.
+    static __device__ __forceinline__ void request(uint32_t slot, const char* row, int t) { cp_async16(slot + t * 16, row + t * 16); }
+    __device__ __forceinline__ void take(uint32_t slot, int t) {
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(slot + t * 16) : "memory");
     }
     __device__ __forceinline__ void get(f32x2 (&x)[4]) const {
         if constexpr (DT == BAOC_F32) {
@@ -92,8 +105,7 @@ struct RowPart {
             if (t * kJoinCols >= dim) return;
             char* p = row + t * kJoinCols * kSize;
             if constexpr (DT == BAOC_F32) {
-                st_stream_f4(p, make_float4(x[0], x[1], x[2], x[3]));
-                st_stream_f4(p + 16, make_float4(x[4], x[5], x[6], x[7]));
+                st_stream_f8(p, x);
             } else {
                 uint4 r;
                 asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x[1]), "f"(x[0]));
@@ -159,26 +171,27 @@ __device__ __forceinline__ void per_column(const float* v, int t, int dim, float
     for (int j = 0; j < 4; ++j) x[j] = pack2(one(2 * j), one(2 * j + 1));
 }
 
-// The same, read row after row: kept in the thread's own places of shared memory (from L1 or L2 each would cost its latency in
-// every row, and registers have the row).
+// The same, read row after row: kept in shared memory, every thread its own (from L1 or L2 each would cost its latency in every
+// row, and registers have the row).  Warps that work alone share one copy, but for the gate.
+template <int kClass>
 struct Kept {
-    float4* at;                      // [vector][2][threads]
-    __device__ __forceinline__ float4* place(int which) const { return at + which * 2 * int(blockDim.x) + int(threadIdx.x); }
-    __device__ __forceinline__ void put(int which, const f32x2 (&x)[4]) const {
+    float4* at;                      // [vector][2][team's threads]
+    __device__ __forceinline__ float4* place(int which, int t) const { return at + which * 2 * team_size<kClass>() + t; }
+    __device__ __forceinline__ void put(int which, int t, const f32x2 (&x)[4]) const {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) unpack2(x[j], v[2 * j], v[2 * j + 1]);
-        float4* p = place(which);
+        float4* p = place(which, t);
         p[0] = make_float4(v[0], v[1], v[2], v[3]);
-        p[blockDim.x] = make_float4(v[4], v[5], v[6], v[7]);
+        p[team_size<kClass>()] = make_float4(v[4], v[5], v[6], v[7]);
     }
-    __device__ __forceinline__ void get(int which, f32x2 (&x)[4]) const {
-        const float4* p = place(which);
-        const float4 a = p[0], b = p[blockDim.x];
+    __device__ __forceinline__ void get(int which, int t, f32x2 (&x)[4]) const {
+        const float4* p = place(which, t);
+        const float4 a = p[0], b = p[team_size<kClass>()];
         x[0] = pack2(a.x, a.y); x[1] = pack2(a.z, a.w); x[2] = pack2(b.x, b.y); x[3] = pack2(b.z, b.w);
     }
 };
-enum Vector : int { kVPreW = 0, kVPostW = 1, kVGate = 2, kVPostB = 3, kVPreB = 4 };
+enum Vector : int { kVPreW = 0, kVPostW = 1, kVGate = 2, kVPreB = 2, kVPostB = 3 };      // (forwards every team keeps a gate of its own, behind these)
 
 // Sums of K = 1, 2 or 4 values over a team, the same in all of its threads.  In a warp the lanes first share the values out (a
 // lane keeps half of them and adds its neighbour's half, so 4 values cost 6 shuffles and not 20).  A CTA's warps take turns of
@@ -207,7 +220,7 @@ struct TeamSum {
         }
 #pragma unroll
         for (int o = K; o < 32; o <<= 1) r += __shfl_xor_sync(kAll, r, o);
-        if constexpr (kClass == 0) {
+        if constexpr (solo(kClass)) {
             v[0] = r;
             if constexpr (K > 1) {
                 constexpr int kFrom[4] = {0, K == 4 ? 2 : 1, 1, 3};      // a lane that has value k
@@ -219,7 +232,7 @@ struct TeamSum {
             if (lane < K) reinterpret_cast<float*>(&buf[turn][threadIdx.x >> 5])[at] = r;
             __syncthreads();
             float4 s;
-            if constexpr (kClass == 1) {             // up to 8 warps: every thread adds them up
+            if constexpr (kClass == 4) {             // up to 8 warps: every thread adds them up
                 s = buf[turn][0];
                 for (int w = 1; w < warps; ++w) {
                     const float4 o = buf[turn][w];
@@ -251,113 +264,116 @@ struct JoinArgs {
     float scale, eps;
 };
 
-// kRows rows of a team at a time: their sums share a barrier, and a weight is loaded once for them.
 template <int S, int B, int kClass, bool kWide>
-__global__ void __launch_bounds__(class_threads(kClass), kClass < 3 ? kJoinWarps * 32 / class_threads(kClass) : 1) join_kernel(const JoinArgs g) {
-    constexpr int kTeams = kClass == 0 ? kSoloWarps : 1, kRows = join_rows(kClass);
+__global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, class_warps(kClass))) join_kernel(const JoinArgs g) {
+    constexpr bool kSolo = solo(kClass);
+    constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass);
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;
-    __shared__ float4 buf[kClass > 0 ? 2 : 1][32];
+    __shared__ float4 buf[kSolo ? 1 : 2][32];
     TeamSum<kClass> sum{buf};
     begin_in_row();
-    const int t = kClass == 0 ? int(threadIdx.x & 31) : int(threadIdx.x), team = kClass == 0 ? int(threadIdx.x >> 5) : 0, dim = g.dim;
+    const int t = kSolo ? int(threadIdx.x & 31) : int(threadIdx.x), team = kSolo ? int(threadIdx.x >> 5) : 0, dim = g.dim;
     const float over = 1.f / float(dim);
-    constexpr int64_t step = kTeams * kRows;
     const int64_t end = min64(g.rows, (int64_t(blockIdx.x) + 1) * g.rows_per_cta);
-    const bool in = !kWide || t * kJoinCols < dim;
-    extern __shared__ float4 dynamic4[];
-    const Kept kept{dynamic4};
-    auto keep = [&](int which, const float* v, float other) {
-        f32x2 x[4];
-        per_column<kClass, kWide>(v, t, dim, other, x);
-        kept.put(which, x);
+    extern __shared__ float4 dynamic4[];             // the vectors, then a gate per team
+    const Kept<kClass> kept{dynamic4}, gates{dynamic4 + ((g.layer ? 4 : 2) + team) * 2 * team_size<kClass>()};
+    auto keep = [&](const Kept<kClass>& to, int which, const float* v) {
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            f32x2 x[4];
+            per_column<kClass, kWide>(v, t + 32 * c, dim, 0.f, x);
+            to.put(which, t + 32 * c, x);
+        }
     };
     // v without its mean (layer norm), times 1 / sqrt(mean square + eps) * w + b
-    auto norm = [&](f32x2 (&v)[kRows][4], int weight, int bias) {
-        float s[kRows];
+    auto norm = [&](f32x2 (&v)[kC][4], int weight, int bias) {
+        float s[1] = {0.f};
         if (g.layer) {
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) s[r] = sum8(v[r]);
+            for (int c = 0; c < kC; ++c) s[0] += sum8(v[c]);
             sum(s);
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) Stream::centre(v[r], s[r] * over, t, dim);
+            for (int c = 0; c < kC; ++c) Stream::centre(v[c], s[0] * over, t + 32 * c, dim);
         }
+        s[0] = 0.f;
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) s[r] = in ? dot8(v[r], v[r]) : 0.f;
+        for (int c = 0; c < kC; ++c) s[0] += !kWide || (t + 32 * c) * kJoinCols < dim ? dot8(v[c], v[c]) : 0.f;
         sum(s);
-        f32x2 w[4];
-        kept.get(weight, w);
+        const f32x2 k = splat2(rsqrtf(s[0] * over + g.eps));
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const f32x2 k = splat2(rsqrtf(s[r] * over + g.eps));
+        for (int c = 0; c < kC; ++c) {
+            f32x2 w[4];
+            kept.get(weight, t + 32 * c, w);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[r][j] = mul2(mul2(v[r][j], k), w[j]);
-        }
-        if (g.layer) {
-            kept.get(bias, w);
+            for (int j = 0; j < 4; ++j) v[c][j] = mul2(mul2(v[c][j], k), w[j]);
+            if (g.layer) {
+                kept.get(bias, t + 32 * c, w);
 #pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[r][j] = add2(v[r][j], w[j]);
+                for (int j = 0; j < 4; ++j) v[c][j] = add2(v[c][j], w[j]);
+            }
         }
     };
-    Stream next_x[kRows];
-    Branch next_f[kRows];
+    Stream next_x[kC];
+    Branch next_f[kC];
     auto fetch = [&](int64_t row) {
+        if (row < end)
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
-            if (row + r < end) {
-                next_f[r].load(g.f + (row + r) * g.f_step, t, dim);
-                if (g.x) next_x[r].load(g.x + (row + r) * g.x_step, t, dim);
+            for (int c = 0; c < kC; ++c) {
+                next_f[c].load(g.f + row * g.f_step, t + 32 * c, dim);
+                if (g.x) next_x[c].load(g.x + row * g.x_step, t + 32 * c, dim);
             }
     };
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        next_x[r].clear();
-        next_f[r].clear();
-    }
-    int64_t row = int64_t(blockIdx.x) * g.rows_per_cta + team * kRows, gate_row = 0;      // gate_row: the first that the kept gate is not for
+    for (int c = 0; c < kC; ++c) next_x[c].clear();
+    int64_t row = int64_t(blockIdx.x) * g.rows_per_cta + team, gate_row = 0;       // gate_row: the first that the kept gate is not for
     fetch(row);
-    keep(kVPreW, g.pre_w, 0.f);
-    if (g.post_w) keep(kVPostW, g.post_w, 0.f);
-    if (g.layer) {
-        keep(kVPreB, g.pre_b, 0.f);
-        if (g.post_w) keep(kVPostB, g.post_b, 0.f);
+    if (team == 0) {
+        keep(kept, kVPreW, g.pre_w);
+        if (g.post_w) keep(kept, kVPostW, g.post_w);
+        if (g.layer) {
+            keep(kept, kVPreB, g.pre_b);
+            if (g.post_w) keep(kept, kVPostB, g.post_b);
+        }
     }
     if (g.gate && !g.rows_per_gate) {
-        keep(kVGate, g.gate, 0.f);
+        keep(gates, 0, g.gate);
         gate_row = g.rows;
     }
+    if (kSolo) __syncthreads();
     const f32x2 scale = splat2(g.scale);
-    for (; row < end; row += step) {             // (alike in a team; a last row without a second computes on zeros or an old row)
-        f32x2 x[kRows][4], u[kRows][4], w[4];
+    for (; row < end; row += kTeams) {               // (alike in a team)
+        f32x2 x[kC][4], u[kC][4];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            next_x[r].get(x[r]);
-            next_f[r].get(u[r]);
+        for (int c = 0; c < kC; ++c) {
+            next_x[c].get(x[c]);
+            next_f[c].get(u[c]);
         }
-        fetch(row + step);                       // (the next rows are on their way while these are reduced)
+        fetch(row + kTeams);                         // (the next row is on its way while this one is reduced)
         if (g.post_w) norm(u, kVPostW, kVPostB);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            if (g.gate) {
-                if (row + r >= gate_row && row + r < end) {
-                    const int64_t group = uint32_t(row + r) / uint32_t(g.rows_per_gate);
-                    gate_row = (group + 1) * g.rows_per_gate;
-                    keep(kVGate, g.gate + group * dim, 0.f);
-                }
-                if (r == 0 || g.rows_per_gate) kept.get(kVGate, w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) u[r][j] = mul2(w[j], u[r][j]);
+        if (g.gate) {
+            if (row >= gate_row) {
+                const int64_t group = uint32_t(row) / uint32_t(g.rows_per_gate);
+                gate_row = (group + 1) * g.rows_per_gate;
+                keep(gates, 0, g.gate + group * dim);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) u[r][j] = fma2(scale, x[r][j], u[r][j]);
-            if (row + r < end) Stream::store(g.y + (row + r) * g.y_step, t, dim, u[r]);
+            for (int c = 0; c < kC; ++c) {
+                f32x2 w[4];
+                gates.get(0, t + 32 * c, w);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[c][j] = mul2(w[j], u[c][j]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[c][j] = fma2(scale, x[c][j], u[c][j]);
+            Stream::store(g.y + row * g.y_step, t + 32 * c, dim, u[c]);
         }
         norm(u, kVPreW, kVPreB);
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
-            if (row + r < end) Branch::store(g.h + (row + r) * g.h_step, t, dim, u[r]);
+        for (int c = 0; c < kC; ++c) Branch::store(g.h + row * g.h_step, t + 32 * c, dim, u[c]);
     }
 }
 
@@ -389,19 +405,23 @@ __device__ __forceinline__ void store_grad(char* out, int dtype, int64_t i, floa
 // rows all belong to this CTA is finished here; of the others a CTA has two at most, the one its first row is in (slot kGate)
 // and the one its last row is in (slot kJoinSums).
 template <int S, int B, bool kLayer, int kClass, bool kWide>
-__global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kClass < 3 ? kJoinGradWarps * 32 / class_threads(kClass) : 1)) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
-    constexpr int kTeams = kClass == 0 ? kSoloWarps : 1, kSums = kLayer ? 5 : 3;
-    constexpr bool kShared = kClass == 3;        // (64 registers a thread: the sums lie in shared memory, and no row is fetched ahead)
-    constexpr bool kAhead = !kShared, kKeep = !kShared;     // (shared memory has no room for the sums and the vectors)
+__global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, class_grad_warps(kClass))) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
+    constexpr bool kSolo = solo(kClass);
+    constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass), kSums = kLayer ? 5 : 3;
+    constexpr bool kShared = kSolo || kClass == 6;   // the sums lie in shared memory: the registers have a row, or are few
+    constexpr bool kAhead = kClass == 4 || kClass == 5;      // the next row is fetched into registers,
+    constexpr bool kStaged = kSolo && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)
+    constexpr bool kKeep = kClass != 6;              // (there shared memory has no room for the vectors beside the sums)
+    constexpr int kVectors = kLayer ? 4 : 3;         // kept ones, the gate (of a segment) among them
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;
-    extern __shared__ float4 dynamic4[];         // kKeep: [3 or 4 vectors][2][threads]; then floats, kShared: [kSums][8][threads]; several teams: [kTeams][8][32]
-    const Kept kept{dynamic4};
-    float* dynamic = reinterpret_cast<float*>(dynamic4 + (kKeep ? (kLayer ? 4 : 3) * 2 * int(blockDim.x) : 0));
-    __shared__ float4 buf[kClass > 0 ? 2 : 1][32];
+    extern __shared__ float4 dynamic4[];             // kKeep: the vectors; kShared: [team][sum][2][team's threads]; kStaged: a row per team
+    __shared__ float4 buf[kSolo ? 1 : 2][32];
     TeamSum<kClass> sum{buf};
     begin_in_row();
-    const int kTeam = team_size<kClass>(), t = kClass == 0 ? int(threadIdx.x & 31) : int(threadIdx.x), team = kClass == 0 ? int(threadIdx.x >> 5) : 0, dim = g.dim;
+    const int size = team_size<kClass>(), t = kSolo ? int(threadIdx.x & 31) : int(threadIdx.x), team = kSolo ? int(threadIdx.x >> 5) : 0, dim = g.dim;
+    const Kept<kClass> kept{dynamic4};
+    float4* sums = dynamic4 + (kKeep ? kVectors * 2 * size : 0);
     const float over = 1.f / float(dim);
     const int64_t begin = int64_t(blockIdx.x) * g.rows_per_cta, end = min64(g.rows, begin + g.rows_per_cta);
     float* part = g.part + int64_t(blockIdx.x) * (kJoinSums + 1) * dim;
@@ -410,161 +430,260 @@ __global__ void __launch_bounds__(class_threads(kClass), kClass == 0 ? 3 : (kCla
 #endif
     const bool need_f = g.post_w || g.gate;
     f32x2 acc[kShared ? 1 : kSums][4] = {};
-    auto add = [&](int k, int j, f32x2 a, f32x2 b) {             // a * b to the sums of columns 2 j and 2 j + 1
+    // a * b to the sums k of a thread's columns
+    auto add = [&](int k, int c, const f32x2 (&a)[4], const f32x2 (&b)[4]) {
         if constexpr (kShared) {
-            float* p = dynamic + (k * 8 + 2 * j) * kTeam + t;
-            float x, y;
-            unpack2(fma2(a, b, pack2(p[0], p[kTeam])), x, y);
-            p[0] = x;
-            p[kTeam] = y;
+            float4* p = sums + (team * kSums + k) * 2 * size + t + 32 * c;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float4 v = p[h * size];
+                unpack2(fma2(a[2 * h], b[2 * h], pack2(v.x, v.y)), v.x, v.y);
+                unpack2(fma2(a[2 * h + 1], b[2 * h + 1], pack2(v.z, v.w)), v.z, v.w);
+                p[h * size] = v;
+            }
         } else {
-            acc[k][j] = fma2(a, b, acc[k][j]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[k][j] = fma2(a[j], b[j], acc[k][j]);
         }
     };
     auto zero = [&](int k) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (kShared) dynamic[(k * 8 + 2 * j) * kTeam + t] = dynamic[(k * 8 + 2 * j + 1) * kTeam + t] = 0.f;
-            else acc[k][j] = 0;
+        for (int c = 0; c < kC; ++c) {
+            if constexpr (kShared) {
+                float4* p = sums + (team * kSums + k) * 2 * size + t + 32 * c;
+                p[0] = p[size] = make_float4(0.f, 0.f, 0.f, 0.f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[k][j] = 0;
+            }
         }
     };
     // the sum k of all teams to f(column, value), each column by one thread; all threads call it
     auto hand_out = [&](auto which, auto f) {
         constexpr int k = decltype(which)::value;
-        float v[8];
+        if constexpr (kSolo) {
+            __syncthreads();
+            for (int i = int(threadIdx.x); i < 2 * size; i += int(blockDim.x)) {
+                float4 v = sums[k * 2 * size + i];
+                for (int o = 1; o < kTeams; ++o) {
+                    const float4 w = sums[(o * kSums + k) * 2 * size + i];
+                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                }
+                const int of = i % size, j = 4 * (i / size);
+                const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (kShared) {
-                v[2 * j] = dynamic[(k * 8 + 2 * j) * kTeam + t];
-                v[2 * j + 1] = dynamic[(k * 8 + 2 * j + 1) * kTeam + t];
-            } else {
-                unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
+                for (int e = 0; e < 4; ++e)
+                    if (Stream::column(of, j + e) < dim) f(Stream::column(of, j + e), x[e]);
             }
-        }
-        if constexpr (kTeams > 1) {
             __syncthreads();
+        } else {
+            float v[8];
+            if constexpr (kShared) {
+                const float4 a = sums[k * 2 * size + t], b = sums[(k * 2 + 1) * size + t];
+                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) dynamic[(team * 8 + j) * kTeam + t] = v[j];
-            __syncthreads();
-            if (team) return;
+                for (int j = 0; j < 4; ++j) unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                for (int o = 1; o < kTeams; ++o) v[j] += dynamic[(o * 8 + j) * kTeam + t];
+                if (Stream::column(t, j) < dim) f(Stream::column(t, j), v[j]);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (Stream::column(t, j) < dim) f(Stream::column(t, j), v[j]);
     };
+    auto in = [&](int c) { return !kWide || (t + 32 * c) * kJoinCols < dim; };
+    auto keep = [&](int which, const float* v) {
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            f32x2 x[4];
+            per_column<kClass, kWide>(v, t + 32 * c, dim, 0.f, x);
+            kept.put(which, t + 32 * c, x);
+        }
+    };
+    auto vector = [&](int which, const float* v, int c, f32x2 (&x)[4]) {
+        if constexpr (kKeep) kept.get(which, t + 32 * c, x);
+        else per_column<kClass, kWide>(v, t + 32 * c, dim, 0.f, x);
+    };
+    Stream next_y[kC], next_dy[kC];
+    Branch next_f[kC], next_dh[kC];
+    auto fetch = [&](int64_t row) {
+        if (row < end)
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                next_y[c].load(g.y + row * g.y_step, t + 32 * c, dim);
+                next_dh[c].load(g.dh + row * g.dh_step, t + 32 * c, dim);
+                if (g.dy) next_dy[c].load(g.dy + row * g.dy_step, t + 32 * c, dim);
+                if (need_f) next_f[c].load(g.f + row * g.f_step, t + 32 * c, dim);
+            }
+    };
+    // the staged row: y, dy, dh, f
+    const uint32_t ahead = smem_addr(sums + kTeams * kSums * 2 * size) + team * 4 * 16 * size;
+    const uint32_t at_dy = ahead + 16 * size, at_dh = ahead + 32 * size, at_f = ahead + 48 * size;
+    auto request = [&](int64_t row) {
+        (void)at_f;
+        if (row < end)
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                if (!in(c)) continue;
+                Stream::request(ahead, g.y + row * g.y_step, t + 32 * c);
+                if (g.dy) Stream::request(at_dy, g.dy + row * g.dy_step, t + 32 * c);
+                Branch::request(at_dh, g.dh + row * g.dh_step, t + 32 * c);
+                if (need_f) Branch::request(at_f, g.f + row * g.f_step, t + 32 * c);
+            }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+        next_y[c].clear();
+        next_dh[c].clear();
+        next_dy[c].clear();
+        next_f[c].clear();
+    }
+    int64_t row = begin + team;
+    if constexpr (kStaged) request(row);
+    else fetch(row);
+    if constexpr (kKeep) {
+        if (team == 0) {
+            keep(kVPreW, g.pre_w);
+            if (g.post_w) keep(kVPostW, g.post_w);
+            if (kLayer && g.post_w) keep(kVPostB, g.post_b);
+            if (g.gate && !g.rows_per_gate) keep(kVGate, g.gate);
+        }
+    }
     if constexpr (kShared)
         for (int k = 0; k < kSums; ++k) zero(k);
-    const bool in = !kWide || t * kJoinCols < dim;
-    Stream next_y, next_dy;
-    Branch next_f, next_dh;
-    auto fetch = [&](int64_t row, int64_t last) {
-        if (row < last) {
-            next_y.load(g.y + row * g.y_step, t, dim);
-            next_dh.load(g.dh + row * g.dh_step, t, dim);
-            if (g.dy) next_dy.load(g.dy + row * g.dy_step, t, dim);
-            if (need_f) next_f.load(g.f + row * g.f_step, t, dim);
-        }
-    };
-    next_y.clear();
-    next_dh.clear();
-    next_dy.clear();
-    next_f.clear();
-    auto keep = [&](int which, const float* v) {
-        f32x2 x[4];
-        per_column<kClass, kWide>(v, t, dim, 0.f, x);
-        kept.put(which, x);
-    };
-    auto vector = [&](int which, const float* v, f32x2 (&x)[4]) {
-        if constexpr (kKeep) kept.get(which, x);
-        else per_column<kClass, kWide>(v, t, dim, 0.f, x);
-    };
-    if constexpr (kKeep) {
-        keep(kVPreW, g.pre_w);
-        if (g.post_w) keep(kVPostW, g.post_w);
-        if (kLayer && g.post_w) keep(kVPostB, g.post_b);
-        if (g.gate && !g.rows_per_gate) keep(kVGate, g.gate);
-    }
+    if (kSolo) __syncthreads();
+    const f32x2 ones[4] = {splat2(1.f), splat2(1.f), splat2(1.f), splat2(1.f)};
     for (int64_t seg = begin; seg < end;) {
         const int64_t group = g.rows_per_gate ? seg / g.rows_per_gate : 0;
         const int64_t seg_end = g.rows_per_gate ? min64(end, (group + 1) * g.rows_per_gate) : end;
         const float* gate = g.gate ? g.gate + group * dim : nullptr;
-        if (kAhead) fetch(seg + team, seg_end);
-        if (kKeep && g.rows_per_gate) keep(kVGate, gate);
-        for (int64_t row = seg + team; row < seg_end; row += kTeams) {       // (alike in a team)
-            if (!kAhead) fetch(row, seg_end);
-            f32x2 y[4], d[4], f[4], dy[4], w[4];         // d: from dh to Dy
-            next_y.get(y);
-            next_dh.get(d);
-            next_f.get(f);
-            next_dy.get(dy);
-            if (kAhead) fetch(row + kTeams, seg_end);
-            if constexpr (kLayer) {
-                float s[2] = {sum8(y), sum8(f)};
-                sum(s);
-                Stream::centre(y, s[0] * over, t, dim);
-                Stream::centre(f, s[1] * over, t, dim);
+        if (kKeep && g.rows_per_gate) {
+            if (kSolo) __syncthreads();              // (no warp reads the last group's any more)
+            if (team == 0) keep(kVGate, gate);
+            if (kSolo) __syncthreads();
+        }
+        for (; row < seg_end; row += kTeams) {       // (alike in a team)
+            f32x2 y[kC][4], d[kC][4], f[kC][4], dy[kC][4];       // d: from dh to Dy
+            if constexpr (kStaged) {
+                cp_async_wait<0>();
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    if (!in(c)) continue;
+                    next_y[c].take(ahead, t + 32 * c);
+                    if (g.dy) next_dy[c].take(at_dy, t + 32 * c);
+                    next_dh[c].take(at_dh, t + 32 * c);
+                    if (need_f) next_f[c].take(at_f, t + 32 * c);
+                }
             }
-            vector(kVPreW, g.pre_w, w);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                next_y[c].get(y[c]);
+                next_dh[c].get(d[c]);
+                next_f[c].get(f[c]);
+                next_dy[c].get(dy[c]);
+            }
+            if (kAhead) fetch(row + kTeams);
+            if constexpr (kLayer) {
+                float s[2] = {0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    s[0] += sum8(y[c]);
+                    s[1] += sum8(f[c]);
+                }
+                sum(s);
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    Stream::centre(y[c], s[0] * over, t + 32 * c, dim);
+                    Stream::centre(f[c], s[1] * over, t + 32 * c, dim);
+                }
+            }
             float r_f;
             {
-                f32x2 dn[4];
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) dn[j] = mul2(d[j], w[j]);
-                float s[4] = {in ? dot8(y, y) : 0.f, in ? dot8(f, f) : 0.f, dot8(dn, y), kLayer ? sum8(dn) : 0.f};
+                for (int c = 0; c < kC; ++c) {
+                    f32x2 w[4];
+                    vector(kVPreW, g.pre_w, c, w);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = mul2(d[c][j], w[j]);
+                    s[0] += in(c) ? dot8(y[c], y[c]) : 0.f;
+                    s[1] += in(c) ? dot8(f[c], f[c]) : 0.f;
+                    s[2] += dot8(w, y[c]);
+                    if (kLayer) s[3] += sum8(w);
+                }
                 sum(s);
+                if constexpr (kStaged) request(row + kTeams);       // (the sums are made of all that has been taken: its place is free)
                 const float r_y = rsqrtf(s[0] * over + g.eps);
                 r_f = rsqrtf(s[1] * over + g.eps);
                 const f32x2 r2 = splat2(r_y), slope = splat2(-r_y * r_y * s[2] * over), mean = splat2(-s[3] * over);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    add(kPreW, j, d[j], mul2(y[j], r2));
-                    if (kLayer) add(kPreB, j, d[j], splat2(1.f));
-                    d[j] = fma2(r2, kLayer ? add2(fma2(y[j], slope, dn[j]), mean) : fma2(y[j], slope, dn[j]), dy[j]);
+                for (int c = 0; c < kC; ++c) {
+                    f32x2 w[4], n[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) n[j] = mul2(y[c][j], r2);
+                    add(kPreW, c, d[c], n);
+                    if (kLayer) add(kPreB, c, d[c], ones);
+                    vector(kVPreW, g.pre_w, c, w);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x2 dn = mul2(d[c][j], w[j]);
+                        d[c][j] = fma2(r2, kLayer ? add2(fma2(y[c][j], slope, dn), mean) : fma2(y[c][j], slope, dn), dy[c][j]);
+                    }
                 }
             }
             if (g.dx) {
                 const f32x2 scale = splat2(g.scale);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) dy[j] = mul2(scale, d[j]);
-                Stream::store(g.dx + row * g.dx_step, t, dim, dy);
+                for (int c = 0; c < kC; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dy[c][j] = mul2(scale, d[c][j]);
+                    Stream::store(g.dx + row * g.dx_step, t + 32 * c, dim, dy[c]);
+                }
             }
             if (g.post_w) {
                 const f32x2 r2 = splat2(r_f);
-                f32x2 b[4];
-                vector(kVPostW, g.post_w, w);
+                float s[2] = {0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], r2);
-                if (gate) {
-                    if (kLayer) vector(kVPostB, g.post_b, b);
+                for (int c = 0; c < kC; ++c) {
+                    f32x2 w[4], b[4];
+                    vector(kVPostW, g.post_w, c, w);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) add(kGate, j, d[j], kLayer ? fma2(f[j], w[j], b[j]) : mul2(f[j], w[j]));
-                    vector(kVGate, gate, b);
+                    for (int j = 0; j < 4; ++j) f[c][j] = mul2(f[c][j], r2);
+                    if (gate) {
+                        if (kLayer) vector(kVPostB, g.post_b, c, b);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) d[j] = mul2(d[j], b[j]);
+                        for (int j = 0; j < 4; ++j) b[j] = kLayer ? fma2(f[c][j], w[j], b[j]) : mul2(f[c][j], w[j]);
+                        add(kGate, c, d[c], b);
+                        vector(kVGate, gate, c, b);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) d[c][j] = mul2(d[c][j], b[j]);
+                    }
+                    add(kPostW, c, d[c], f[c]);
+                    if (kLayer) add(kPostB, c, d[c], ones);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[c][j] = mul2(d[c][j], w[j]);
+                    s[0] += dot8(d[c], f[c]);
+                    if (kLayer) s[1] += sum8(d[c]);
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    add(kPostW, j, d[j], f[j]);
-                    if (kLayer) add(kPostB, j, d[j], splat2(1.f));
-                    d[j] = mul2(d[j], w[j]);
-                }
-                float s[2] = {dot8(d, f), kLayer ? sum8(d) : 0.f};
                 sum(s);
                 const f32x2 slope = splat2(-s[0] * over), mean = splat2(-s[1] * over);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) d[j] = mul2(r2, kLayer ? add2(fma2(f[j], slope, d[j]), mean) : fma2(f[j], slope, d[j]));
-            } else if (gate) {
-                vector(kVGate, gate, w);
+                for (int c = 0; c < kC; ++c)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    add(kGate, j, d[j], f[j]);
-                    d[j] = mul2(d[j], w[j]);
+                    for (int j = 0; j < 4; ++j) d[c][j] = mul2(r2, kLayer ? add2(fma2(f[c][j], slope, d[c][j]), mean) : fma2(f[c][j], slope, d[c][j]));
+            } else if (gate) {
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    f32x2 w[4];
+                    vector(kVGate, gate, c, w);
+                    add(kGate, c, d[c], f[c]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[c][j] = mul2(d[c][j], w[j]);
                 }
             }
-            Branch::store(g.df + row * g.df_step, t, dim, d);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) Branch::store(g.df + row * g.df_step, t + 32 * c, dim, d[c]);
+            if (!kAhead && !kStaged) fetch(row + kTeams);
         }
         if (g.rows_per_gate && g.out[kGate]) {
             const bool whole = group * g.rows_per_gate >= begin && min64(g.rows, (group + 1) * g.rows_per_gate) <= end;
@@ -658,7 +777,7 @@ struct Rows {
     const void* p;
     int64_t step, width, eb;        // bytes from row to row, of a row, of an element
     Rows(const void* p, int64_t stride, int dtype, int dim) : p(p), step((stride ? stride : dim) * elem_bytes(dtype)), width(dim * elem_bytes(dtype)), eb(elem_bytes(dtype)) {}
-    bool wide() const { return !p || (aligned(p, 16) && step % 16 == 0); }
+    bool wide() const { return !p || (aligned(p, kJoinCols * eb) && step % (kJoinCols * eb) == 0); }     // a thread's columns in one access
     bool fits() const { return aligned(p, eb); }
 };
 // Whether the rows of two arrays share bytes.  (Rows of one buffer may lie between each other's.)
@@ -672,14 +791,13 @@ bool overlap(const Rows& a, const Rows& b, int64_t rows) {
 }
 bool same(const Rows& a, const Rows& b, int64_t rows) { return a.p == b.p && a.width == b.width && (a.step == b.step || rows == 1); }
 
-// Warps of a row's CTA and its class (see class_threads).
-int warps_of(int dim) { return int(ceil_div(dim, 32 * kJoinCols)); }
 int class_of(int dim) {
-    const int w = warps_of(dim);
-    return w == 1 ? 0 : (w <= 8 ? 1 : (w <= 16 ? 2 : 3));
+    const int w = int(ceil_div(dim, 32 * kJoinCols));
+    return w <= 3 ? w : (w <= 8 ? 4 : (w <= 16 ? 5 : 6));
 }
-int cta_of(int dim) { return warps_of(dim) == 1 ? 32 * kSoloWarps : 32 * warps_of(dim); }
-int rows_of(int dim) { return warps_of(dim) == 1 ? kSoloWarps : 1; }         // rows that a CTA works on at a time
+int cta_of(int dim) { return solo(class_of(dim)) ? 32 * kSoloWarps : int(32 * ceil_div(dim, 32 * kJoinCols)); }
+int team_of(int dim) { return solo(class_of(dim)) ? 32 * class_of(dim) : cta_of(dim); }      // (see team_size)
+int rows_of(int dim) { return solo(class_of(dim)) ? kSoloWarps : 1; }                        // rows that a CTA works on at a time
 
 // f(class, wide) as constants.
 template <int kClass, typename F>
@@ -690,10 +808,12 @@ int with_width(bool wide, F f) {
 template <typename F>
 int with_class(int dim, bool wide, F f) {
     switch (class_of(dim)) {
-        case 0: return with_width<0>(wide, f);
         case 1: return with_width<1>(wide, f);
         case 2: return with_width<2>(wide, f);
-        default: return with_width<3>(wide, f);
+        case 3: return with_width<3>(wide, f);
+        case 4: return with_width<4>(wide, f);
+        case 5: return with_width<5>(wide, f);
+        default: return with_width<6>(wide, f);
     }
 }
 template <typename F>
@@ -710,12 +830,12 @@ int64_t ctas_at_once(int dim, int sm_warps) { return int64_t(148) * std::max(1, 
 // The gradient's rows per CTA and CTAs: whole rounds of a CTA's teams, all CTAs at once.
 void grad_shape(int dim, int64_t rows, int64_t* per_cta, int* ctas) {
     const int teams = rows_of(dim);
-    *per_cta = std::max<int64_t>(teams, round_up(ceil_div(rows, ctas_at_once(dim, kJoinGradWarps)), teams));
+    *per_cta = std::max<int64_t>(teams, round_up(ceil_div(rows, ctas_at_once(dim, class_grad_warps(class_of(dim)))), teams));
     *ctas = int(ceil_div(rows, *per_cta));
 }
 // (By the most CTAs that so many rows or fewer can get: whole rounds leave fewer of them for some larger numbers of rows.)
 int64_t grad_ws(int dim, int64_t rows) {
-    const int64_t ctas = std::min(ceil_div(rows, rows_of(dim)), ctas_at_once(dim, kJoinGradWarps));
+    const int64_t ctas = std::min(ceil_div(rows, rows_of(dim)), ctas_at_once(dim, class_grad_warps(class_of(dim))));
     return std::max<int64_t>(256, round_up(ctas * (kJoinSums + 1) * dim * 4, 256));
 }
 
@@ -761,9 +881,8 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
         return with_class(e->dim, wide, [&](auto C, auto W) {
-            // whole rounds of a CTA's teams; all CTAs at once
-            const int cta = cta_of(e->dim), round = rows_of(e->dim) * join_rows(C()), bytes = 5 * 8 * cta * 4;
-            a.rows_per_cta = round_up(ceil_div(rows, ctas_at_once(e->dim, kJoinWarps)), round);
+            const int cta = cta_of(e->dim), bytes = ((a.layer ? 4 : 2) + rows_of(e->dim)) * 8 * team_of(e->dim) * 4;
+            a.rows_per_cta = round_up(ceil_div(rows, ctas_at_once(e->dim, class_warps(C()))), rows_of(e->dim));      // all CTAs at once
             auto kernel = join_kernel<S(), B(), C(), W()>;
             if (bytes > 40 * 1024) {             // (48 KB go without asking, the kernel's own arrays included)
                 const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -833,8 +952,9 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
         rc = with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
             return with_class(e->dim, wide, [&](auto C, auto W) {
                 auto go = [&](auto L) {
-                    const int cta = cta_of(e->dim), sums = C() == 3 ? (L() ? 5 : 3) : (C() == 0 ? 1 : 0), kept = C() == 3 ? 0 : (L() ? 4 : 3);
-                    const int bytes = (sums + kept) * 8 * cta * 4;
+                    const int cta = cta_of(e->dim), teams = rows_of(e->dim), sums = solo(C()) || C() == 6 ? teams * (L() ? 5 : 3) : 0;
+                    const int staged = solo(C()) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? teams * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
+                    const int bytes = (sums + (C() == 6 ? 0 : (L() ? 4 : 3)) + staged) * 8 * team_of(e->dim) * 4;
                     auto kernel = join_grad_kernel<S(), B(), L(), C(), W()>;
                     if (bytes > 40 * 1024) {
                         const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
