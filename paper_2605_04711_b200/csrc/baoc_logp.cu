@@ -90,20 +90,14 @@ struct RowSplit {
 };
 
 // A maximum m, and the sums of 2^u and 2^u u over elements x with u = a (x - m), a = scale log2(e).
+__device__ __forceinline__ float finite_ref(float m) { return fmaxf(m, -3.402823466e38f); }    // (where nothing but -inf has been seen)
 struct Sums {
     float m, s, q;
-    // (the subtraction's reference stays finite where nothing but -inf has been seen)
-    __device__ __forceinline__ float ref() const { return fmaxf(m, -3.402823466e38f); }
     __device__ __forceinline__ void raise(float to, float a) {
-        const float d = fmaxf(a * (ref() - fmaxf(to, -3.402823466e38f)), kLeastExponent), f = exp2_approx(d);
+        const float d = fmaxf(a * (finite_ref(m) - finite_ref(to)), kLeastExponent), f = exp2_approx(d);
         q = f * (q + d * s);
         s *= f;
         m = to;
-    }
-    __device__ __forceinline__ void add(float x, float a) {
-        const float u = fmaxf(a * (x - ref()), kLeastExponent), e = exp2_approx(u);
-        s += e;
-        q += e * u;
     }
     __device__ __forceinline__ void join(Sums o, float a) {
         const float to = max_nan(m, o.m);
@@ -111,6 +105,96 @@ struct Sums {
         o.raise(to, a);
         s += o.s;
         q += o.q;
+    }
+};
+
+// A thread's sums, two of each side by side, and the largest and smallest of a few vectors in front of them.
+template <int DT>
+struct ThreadSums {
+    static constexpr int kVec = Logits<DT>::kVec;
+    float m = -INFINITY;
+    f32x2 s = 0, q = 0;
+
+    __device__ __forceinline__ void raise(float to, float a) {
+        const float d = fmaxf(a * (finite_ref(m) - finite_ref(to)), kLeastExponent);
+        const f32x2 f = splat2(exp2_approx(d));
+        q = mul2(f, fma2(splat2(d), s, q));
+        s = mul2(f, s);
+        m = to;
+    }
+    __device__ __forceinline__ void one(float x, float a) {
+        const float to = max_nan(m, x);
+        if (!(to <= m)) raise(to, a);
+        const float u = fmaxf(a * (x - finite_ref(m)), kLeastExponent), e = exp2_approx(u);
+        s = add2(s, pack2(e, 0.f));
+        q = add2(q, pack2(e * u, 0.f));
+    }
+    // kClamp: some exponents are out of reach (a masked logit's is -inf, and 0 * -inf has no place in q)
+    template <bool kClamp>
+    __device__ __forceinline__ void vector(const uint4& w, f32x2 minus_ref, f32x2 a) {
+        float x[kVec];
+        Logits<DT>::vec(w, x);
+#pragma unroll
+        for (int j = 0; j < kVec; j += 2) {
+            const f32x2 u2 = mul2(a, add2(pack2(x[j], x[j + 1]), minus_ref));
+            float u, v;
+            unpack2(u2, u, v);
+            if constexpr (kClamp) {
+                u = fmaxf(u, kLeastExponent);
+                v = fmaxf(v, kLeastExponent);
+            }
+            const f32x2 e = pack2(exp2_approx(u), exp2_approx(v));
+            s = add2(s, e);
+            q = fma2(e, kClamp ? pack2(u, v) : u2, q);
+        }
+    }
+    // n of the vectors count; the others repeat one of those
+    __device__ __forceinline__ void batch(const uint4 (&w)[kLogpBatch], int n, float a) {
+        float most, least;
+        if constexpr (DT == BAOC_BF16) {
+            uint32_t hi = w[0].x, lo = w[0].x;
+#pragma unroll
+            for (int u = 0; u < kLogpBatch; ++u)
+#pragma unroll
+                for (int i = u == 0 ? 1 : 0; i < 4; ++i) {
+                    const uint32_t x = i == 0 ? w[u].x : (i == 1 ? w[u].y : (i == 2 ? w[u].z : w[u].w));
+                    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(hi) : "r"(hi), "r"(x));
+                    asm("min.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(lo), "r"(x));
+                }
+            most = max_nan(bf16_lo(hi), bf16_hi(hi));
+            least = fminf(bf16_lo(lo), bf16_hi(lo));
+        } else {
+            most = least = __uint_as_float(w[0].x);
+#pragma unroll
+            for (int u = 0; u < kLogpBatch; ++u) {
+                float x[kVec];
+                Logits<DT>::vec(w[u], x);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) {
+                    most = max_nan(most, x[j]);
+                    least = fminf(least, x[j]);
+                }
+            }
+        }
+        most = max_nan(most, m);
+        if (!(most <= m)) raise(most, a);
+        const float ref = finite_ref(m);
+        const f32x2 minus_ref = splat2(-ref), a2 = splat2(a);
+        if (a * (least - ref) >= kLeastExponent) {
+#pragma unroll
+            for (int u = 0; u < kLogpBatch; ++u)
+                if (u < n) vector<false>(w[u], minus_ref, a2);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kLogpBatch; ++u)
+                if (u < n) vector<true>(w[u], minus_ref, a2);
+        }
+    }
+    __device__ __forceinline__ Sums total() const {
+        float s0, s1, q0, q1;
+        unpack2(s, s0, s1);
+        unpack2(q, q0, q1);
+        return Sums{m, s0 + s1, q0 + q1};
     }
 };
 
@@ -220,8 +304,9 @@ struct TopFinder {
         }
         __syncthreads();
     }
-    // own: the thread's largest logit, has: it had any.  All threads call it; best is filled behind it.
-    __device__ __forceinline__ void find(float own, bool has, int top) const {
+    // own: the thread's largest logit, has: it had any; w: its last vectors, which are all it had where the share has one batch of
+    // them.  All threads call it; best is filled behind it.
+    __device__ __forceinline__ void find(float own, bool has, int top, const uint4 (&w)[kLogpBatch]) const {
         const int tid = threadIdx.x, lane = tid & 31;
         const uint32_t mine = has ? Logits<DT>::key(own) : 0u;
         sh->key[tid] = mine;
@@ -270,8 +355,34 @@ struct TopFinder {
             }
             __syncthreads();
         }
-        if (has && (mine > last || (mine == last && (!ties || ~sh->first[tid] <= sh->last_first)))) sh->chosen[atomicAdd(&sh->n_chosen, 1)] = uint16_t(tid);
-        collect(last == 0 ? 0 : uint64_t(last) << 32 | uint32_t(~sh->last_first));
+        const bool chosen = has && (mine > last || (mine == last && (!ties || ~sh->first[tid] <= sh->last_first)));
+        const uint64_t least = last == 0 ? 0 : uint64_t(last) << 32 | uint32_t(~sh->last_first);
+        if (chosen) sh->chosen[atomicAdd(&sh->n_chosen, 1)] = uint16_t(tid);
+        if (hi - lo <= kLogpBatch * kT) {
+            if (tid == 0) sh->n_found = 0;
+            __syncthreads();
+            if (chosen) {
+                auto take = [&](float x, uint32_t j) {
+                    const uint64_t k = Logits<DT>::key(x, j);
+                    if (k >= least) {
+                        const int at = atomicAdd(&sh->n_found, 1);
+                        if (at < kLogpFound) sh->found[at] = k;
+                    }
+                };
+#pragma unroll
+                for (int u = 0; u < kLogpBatch; ++u)
+                    if (lo + tid + u * kT < hi) {
+                        float x[Logits<DT>::kVec];
+                        Logits<DT>::vec(w[u], x);
+#pragma unroll
+                        for (int j = 0; j < Logits<DT>::kVec; ++j) take(x[j], uint32_t(split.head + (lo + tid + u * kT) * Logits<DT>::kVec + j));
+                    }
+                if (edges && tid < split.head + split.tail) take(Logits<DT>::one(row, split.edge(vocab, tid)), uint32_t(split.edge(vocab, tid)));
+            }
+            __syncthreads();
+        } else {
+            collect(least);
+        }
         if (sh->n_found > kLogpFound) {      // some threads hold many: the exact key of the last token looked for, bit by bit
             uint64_t t = 0;
             for (int bit = 63; bit >= 0; --bit)
@@ -286,12 +397,15 @@ struct TopFinder {
 template <int DT, int kC, int kT>
 __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
     namespace cg = cooperative_groups;
-    constexpr int kVec = Logits<DT>::kVec;
     __shared__ Sums warp_sums[kT / 32], cta_sums;
     __shared__ TopShared<kT> top_shared;
     begin_in_row();
     const int tid = threadIdx.x, lane = tid & 31, part = kC > 1 ? int(blockIdx.x % kC) : 0;
     const int64_t row = blockIdx.x / kC, vocab = g.vocab;
+    const char* x = g.logits + row * g.step;
+    const RowSplit split = RowSplit::of<DT>(x, vocab);
+    const int64_t lo = split.vecs * part / kC, hi = split.vecs * (part + 1) / kC;
+    const char* body = x + int64_t(split.head) * Logits<DT>::kSize;
     const int64_t id = given_token(g.ids, g.id_bits, row);
     if (id < 0 || id >= vocab) {             // (alike in all CTAs of the cluster)
         if (part == 0) {
@@ -301,69 +415,41 @@ __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
         }
         return;
     }
-    const char* x = g.logits + row * g.step;
-    const RowSplit split = RowSplit::of<DT>(x, vocab);
-    const int64_t lo = split.vecs * part / kC, hi = split.vecs * (part + 1) / kC;
-    const char* body = x + int64_t(split.head) * Logits<DT>::kSize;
     const float a = g.scale * kLog2e;
-    Sums sum{-INFINITY, 0.f, 0.f};
+    ThreadSums<DT> own;
     bool has = lo + tid < hi;
     if (part == 0 && tid < split.head + split.tail) {
         has = true;
-        sum.m = Logits<DT>::one(x, split.edge(vocab, tid));
-        sum.add(sum.m, a);
+        own.one(Logits<DT>::one(x, split.edge(vocab, tid)), a);
     }
-    auto batch = [&](const uint4 (&w)[kLogpBatch], int n) {
-        float most = sum.m;
+    // whole batches, one requested while the one before is summed; the last one may have fewer vectors
+    const int64_t left = hi - lo - tid;
+    int64_t batches = left > 0 ? (left + kT - 1) / kT : 0;       // (vectors of this thread)
+    const int last = batches == 0 ? 0 : int((batches - 1) % kLogpBatch) + 1;
+    batches = (batches + kLogpBatch - 1) / kLogpBatch;
+    uint4 w[kLogpBatch];
+    const char* at = body + (lo + tid) * 16;
+    auto load = [&](uint4 (&to)[kLogpBatch], int n) {
 #pragma unroll
-        for (int u = 0; u < kLogpBatch; ++u) {
-            float y[kVec];
-            Logits<DT>::vec(w[u], y);
-            if (u < n) {
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) most = max_nan(most, y[j]);
-            }
-        }
-        if (!(most <= sum.m)) sum.raise(most, a);
-        const float ref = sum.ref();
-#pragma unroll
-        for (int u = 0; u < kLogpBatch; ++u) {
-            float y[kVec];
-            Logits<DT>::vec(w[u], y);
-            if (u < n) {
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) {
-                    const float e2 = fmaxf(a * (y[j] - ref), kLeastExponent), e = exp2_approx(e2);
-                    sum.s += e;
-                    sum.q += e * e2;
-                }
-            }
-        }
+        for (int u = 0; u < kLogpBatch; ++u) to[u] = ld_stream_u4(at + (u < n ? u : 0) * (kT * 16));
+        at += kLogpBatch * kT * 16;
     };
-    int64_t v = lo + tid;
-    for (; v + (kLogpBatch - 1) * kT < hi; v += kLogpBatch * kT) {
-        uint4 w[kLogpBatch];
+    if (batches > 0) load(w, batches == 1 ? last : kLogpBatch);
+    for (int64_t i = 1; i < batches; ++i) {
+        uint4 next[kLogpBatch];
+        load(next, i == batches - 1 ? last : kLogpBatch);
+        own.batch(w, kLogpBatch, a);
 #pragma unroll
-        for (int u = 0; u < kLogpBatch; ++u) w[u] = ld_stream_u4(body + (v + u * kT) * 16);
-        batch(w, kLogpBatch);
+        for (int u = 0; u < kLogpBatch; ++u) w[u] = next[u];
     }
-    {
-        uint4 w[kLogpBatch];
-        int n = 0;
-#pragma unroll
-        for (int u = 0; u < kLogpBatch; ++u) {
-            w[u] = make_uint4(0, 0, 0, 0);
-            if (v + u * kT < hi) { w[u] = ld_stream_u4(body + (v + u * kT) * 16); n = u + 1; }
-        }
-        if (n) batch(w, n);
-    }
-    const float own = sum.m;
+    if (batches > 0) own.batch(w, last, a);
+    Sums sum = own.total();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         sum.join(Sums{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.q, o)}, a);
     if (lane == 0) warp_sums[tid >> 5] = sum;
     if (g.top) {
-        TopFinder<DT, kT>{x, split, lo, hi, vocab, part == 0, &top_shared}.find(own, has, g.top);
+        TopFinder<DT, kT>{x, split, lo, hi, vocab, part == 0, &top_shared}.find(own.m, has, g.top, w);
     } else {
         __syncthreads();
     }
@@ -534,9 +620,9 @@ int logp_of(const LogpArgs& a, int64_t n, cudaStream_t s) {
     while (c < kLogpMostCtas && n * c * 2 <= 2 * 148 && a.vocab >= int64_t(c) * 2 * kLogpCtaLogits) c *= 2;
     switch (c) {
         case 1: return launch_logp<DT, 1, kThreads>(a, n, s);
-        case 2: return launch_logp<DT, 2, kThreads>(a, n, s);
-        case 4: return launch_logp<DT, 4, kThreads>(a, n, s);
-        default: return launch_logp<DT, 8, kThreads>(a, n, s);
+        case 2: return launch_logp<DT, 2, 2 * kThreads>(a, n, s);
+        case 4: return launch_logp<DT, 4, 2 * kThreads>(a, n, s);
+        default: return launch_logp<DT, 8, 2 * kThreads>(a, n, s);
     }
 }
 
