@@ -14,6 +14,7 @@
 #include <cuda_runtime.h>
 #include <new>
 #include <string>
+#include <type_traits>
 
 #include "baoc_device.cuh"
 
@@ -21,9 +22,9 @@ namespace baoc {
 
 constexpr int kLogpMaxTop = 32;
 constexpr int kLogpBatch = 4;                  // 16-byte loads a thread has in flight
-constexpr int kLogpFound = 1024;               // candidates for the most probable tokens that shared memory holds
 constexpr int kLogpMostCtas = 8;               // CTAs (a cluster) that share a row where there are few rows,
 constexpr int kLogpCtaLogits = 4096;           // each with at least so many logits
+constexpr int kLogpShort = 64;                  // vectors a thread for which a row is given to fewer threads
 constexpr int64_t kLogpMaxStride = int64_t(1) << 32;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeastExponent = -10000.f;     // 2^this is zero; it keeps 0 * -inf out of the entropy's sum
@@ -148,8 +149,8 @@ struct ThreadSums {
             q = fma2(e, kClamp ? pack2(u, v) : u2, q);
         }
     }
-    // n of the vectors count; the others repeat one of those
-    __device__ __forceinline__ void batch(const uint4 (&w)[kLogpBatch], int n, float a) {
+    // n of the vectors count, the others repeat one of those; returns the largest
+    __device__ __forceinline__ float batch(const uint4 (&w)[kLogpBatch], int n, float a) {
         float most, least;
         if constexpr (DT == BAOC_BF16) {
             uint32_t hi = w[0].x, lo = w[0].x;
@@ -176,8 +177,7 @@ struct ThreadSums {
                 }
             }
         }
-        most = max_nan(most, m);
-        if (!(most <= m)) raise(most, a);
+        if (!(most <= m)) raise(max_nan(most, m), a);
         const float ref = finite_ref(m);
         const f32x2 minus_ref = splat2(-ref), a2 = splat2(a);
         if (a * (least - ref) >= kLeastExponent) {
@@ -189,6 +189,7 @@ struct ThreadSums {
             for (int u = 0; u < kLogpBatch; ++u)
                 if (u < n) vector<true>(w[u], minus_ref, a2);
         }
+        return most;
     }
     __device__ __forceinline__ Sums total() const {
         float s0, s1, q0, q1;
@@ -227,17 +228,22 @@ __device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[kPer], int ne
     return t;
 }
 
-// The most probable tokens of a CTA's share of a row, in two looks.  Every thread knows its largest logit from the sums'
-// pass.  The `top` threads with the largest ones hold `top` tokens that are at least as large as the last of those, so all
-// tokens looked for are among the elements of these threads: only those are read again (top / kT of the share, from L2), and
-// what reaches the last maximum is ranked.  Order: larger logit, then lower token; a token and its logit make one 64-bit key.
+// The most probable tokens of a CTA's share of a row, in two looks.  Every thread knows its largest logit from the sums' pass.
+// The `top` groups of threads with the largest ones hold `top` tokens at least as large as the last of those, so all tokens
+// looked for reach it: only threads whose largest does are looked through again (a few in the hundred, from L2, or from
+// registers where a thread had one batch), and what reaches it is ranked.  Where that is more than shared memory holds (many equal
+// logits, or a few threads with most of the large ones), the threads' largest are told apart by their tokens, and then the tokens
+// themselves are counted bit by bit.  Order: larger logit, then lower token; a token and its logit make one 64-bit key.
+constexpr int kTopGroups = 64, kTopSlots = 16;               // slots: runs of a thread's batches whose largest is noted
 template <int kT>
 struct TopShared {
-    uint32_t key[kT], first[kT];
+    static constexpr int kFound = kT >= 256 ? 1024 : 256;        // candidates that it holds
+    uint32_t key[kT], first[kT];             // the threads' (first: groups') largest; the lowest tokens that have it
     uint32_t last, last_first;               // the last of the chosen threads' maxima, and the token up to which equal ones count
     int ties, need, n_chosen, n_found;
-    uint16_t chosen[kT];
-    uint64_t found[kLogpFound], best[kLogpMaxTop];
+    uint16_t chosen[kT];                     // threads (up to 512), or slot * kT + thread
+    float slot[kTopSlots][kT];
+    uint64_t found[kFound], best[kLogpMaxTop];
 };
 
 template <int DT, int kT>
@@ -246,6 +252,7 @@ struct TopFinder {
     RowSplit split;
     int64_t lo, hi, vocab;                   // the CTA's vectors
     bool edges;                              // the CTA has the elements outside the vectors
+    uint32_t run;                            // batches of a slot
     TopShared<kT>* sh;
 
     // f(logit, token) for every element of thread t, the elements dealt to the lanes of the calling warp
@@ -278,21 +285,53 @@ struct TopFinder {
         __syncthreads();
         return sh->n_found;
     }
+    // their keys that reach `least` into found (all threads call it; n_found is zero): the vectors dealt out to all threads, four
+    // in flight each
+    __device__ __forceinline__ void take(float x, uint32_t j, uint64_t least) const {
+        const uint64_t k = Logits<DT>::key(x, j);
+        if (k >= least) {
+            const int at = atomicAdd(&sh->n_found, 1);
+            if (at < TopShared<kT>::kFound) sh->found[at] = k;
+        }
+    }
+    __device__ __forceinline__ void take(const uint4& w, int64_t v, uint64_t least) const {
+        constexpr int kVec = Logits<DT>::kVec;
+        float x[kVec];
+        Logits<DT>::vec(w, x);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) take(x[j], uint32_t(split.head + v * kVec + j), least);
+    }
+    __device__ __forceinline__ void take_edges(uint64_t least) const {
+        if (edges && int(threadIdx.x) < split.head + split.tail) {
+            const int64_t j = split.edge(vocab, threadIdx.x);
+            take(Logits<DT>::one(row, j), uint32_t(j), least);
+        }
+    }
+    template <bool kSlots>
     __device__ __forceinline__ void collect(uint64_t least) const {
-        __syncthreads();
-        if (threadIdx.x == 0) sh->n_found = 0;
-        __syncthreads();
-        for (int c = threadIdx.x >> 5; c < sh->n_chosen; c += kT / 32)
-            each(sh->chosen[c], [&](float x, uint32_t j) {
-                const uint64_t k = Logits<DT>::key(x, j);
-                if (k >= least) {
-                    const int at = atomicAdd(&sh->n_found, 1);
-                    if (at < kLogpFound) sh->found[at] = k;
+        const char* body = row + int64_t(split.head) * Logits<DT>::kSize;
+        const uint32_t per = kSlots ? run * kLogpBatch : uint32_t((hi - lo + kT - 1) / kT), all = uint32_t(sh->n_chosen) * per;
+        for (uint32_t i = threadIdx.x; i < all; i += 4 * kT) {
+            uint4 w[4];
+            int64_t v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t at = i + u * kT, c = at / per;
+                v[u] = hi;
+                if (at < all) {
+                    const uint32_t which = sh->chosen[c];
+                    v[u] = lo + (which & (kT - 1)) + (int64_t(at - c * per) + (kSlots ? int64_t(which / kT) * per : 0)) * kT;
                 }
-            });
+                if (v[u] < hi) w[u] = *reinterpret_cast<const uint4*>(body + v[u] * 16);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v[u] < hi) take(w[u], v[u], least);
+        }
+        take_edges(least);
         __syncthreads();
     }
-    // n keys of `from` (n <= kLogpFound), the largest `top` of them in descending order into best; zeros behind the last
+    // n keys of `from` (n <= kFound), the largest `top` of them in descending order into best; zeros behind the last
     __device__ __forceinline__ static void rank(TopShared<kT>* sh, const uint64_t* from, int n, int top) {
         for (int i = threadIdx.x; i < top; i += kT)
             if (i >= n) sh->best[i] = 0;
@@ -304,13 +343,64 @@ struct TopFinder {
         }
         __syncthreads();
     }
+    // The keys that reach `least` of the chosen threads into found; all threads call it.
+    __device__ __forceinline__ void gather(bool chosen, uint64_t least, const uint4 (&w)[kLogpBatch]) const {
+        const int tid = threadIdx.x;
+        if (hi - lo <= kLogpBatch * kT) {
+            if (chosen) {
+#pragma unroll
+                for (int u = 0; u < kLogpBatch; ++u)
+                    if (lo + tid + u * kT < hi) take(w[u], lo + tid + u * kT, least);
+            }
+            take_edges(least);
+            __syncthreads();
+        } else {
+            if (chosen) {
+                const uint32_t slots = (uint32_t((hi - lo - tid + kT - 1) / kT) + run * kLogpBatch - 1) / (run * kLogpBatch);
+                for (uint32_t i = 0; i < slots; ++i)
+                    if (Logits<DT>::key(sh->slot[i][tid]) >= uint32_t(least >> 32)) {
+                        const int at = atomicAdd(&sh->n_chosen, 1);
+                        if (at < kT) sh->chosen[at] = uint16_t(i * kT + tid);
+                    }
+            }
+            __syncthreads();
+            if (sh->n_chosen <= kT) collect<true>(least);
+            else if (tid == 0) sh->n_found = TopShared<kT>::kFound + 1;      // (more than the list holds: the same as too many found)
+            __syncthreads();
+        }
+    }
     // own: the thread's largest logit, has: it had any; w: its last vectors, which are all it had where the share has one batch of
     // them.  All threads call it; best is filled behind it.
     __device__ __forceinline__ void find(float own, bool has, int top, const uint4 (&w)[kLogpBatch]) const {
+        constexpr int kGroups = kT < kTopGroups ? kT : kTopGroups, kMembers = kT / kGroups;
         const int tid = threadIdx.x, lane = tid & 31;
         const uint32_t mine = has ? Logits<DT>::key(own) : 0u;
+        uint32_t group = mine;
+#pragma unroll
+        for (int o = 1; o < kMembers; o <<= 1) group = max(group, __shfl_xor_sync(0xffffffffu, group, o));
+        if (tid % kMembers == 0) sh->first[tid / kMembers] = group;
+        if (tid == 0) sh->n_chosen = sh->n_found = 0;
+        __syncthreads();
+        if (tid < 32) {
+            uint32_t v[kGroups / 32];
+#pragma unroll
+            for (int i = 0; i < kGroups / 32; ++i) v[i] = sh->first[i * 32 + lane];
+            const uint32_t last = reached_by(v, top, Logits<DT>::kKeyBit);
+            if (lane == 0) sh->last = last;
+        }
+        __syncthreads();
+        const uint32_t bound = sh->last;
+        gather(has && mine >= bound, uint64_t(bound) << 32, w);
+        if (sh->n_found > TopShared<kT>::kFound) find_exact(mine, has, top);
+        rank(sh, sh->found, min(sh->n_found, TopShared<kT>::kFound), top);
+    }
+    // As few threads as tokens are looked for, and then, if some hold many, the exact key of the last of these.
+    __device__ __noinline__ void find_exact(uint32_t mine, bool has, int top) const {
+        const int tid = threadIdx.x, lane = tid & 31;
+        __syncthreads();
         sh->key[tid] = mine;
-        if (tid == 0) sh->n_chosen = 0;
+        sh->first[tid] = 0;
+        if (tid == 0) sh->n_chosen = sh->n_found = 0;
         __syncthreads();
         if (tid < 32) {
             uint32_t v[kT / 32];
@@ -336,8 +426,6 @@ struct TopFinder {
         const uint32_t last = sh->last;
         const int ties = sh->ties;
         if (ties) {                          // more threads than looked for: of the equal ones, those with the lowest tokens
-            sh->first[tid] = 0;
-            __syncthreads();
             for (int t = tid >> 5; t < kT; t += kT / 32) {
                 if (sh->key[t] != last) continue;
                 uint32_t first = 0xffffffffu;
@@ -356,49 +444,27 @@ struct TopFinder {
             __syncthreads();
         }
         const bool chosen = has && (mine > last || (mine == last && (!ties || ~sh->first[tid] <= sh->last_first)));
-        const uint64_t least = last == 0 ? 0 : uint64_t(last) << 32 | uint32_t(~sh->last_first);
         if (chosen) sh->chosen[atomicAdd(&sh->n_chosen, 1)] = uint16_t(tid);
-        if (hi - lo <= kLogpBatch * kT) {
-            if (tid == 0) sh->n_found = 0;
-            __syncthreads();
-            if (chosen) {
-                auto take = [&](float x, uint32_t j) {
-                    const uint64_t k = Logits<DT>::key(x, j);
-                    if (k >= least) {
-                        const int at = atomicAdd(&sh->n_found, 1);
-                        if (at < kLogpFound) sh->found[at] = k;
-                    }
-                };
-#pragma unroll
-                for (int u = 0; u < kLogpBatch; ++u)
-                    if (lo + tid + u * kT < hi) {
-                        float x[Logits<DT>::kVec];
-                        Logits<DT>::vec(w[u], x);
-#pragma unroll
-                        for (int j = 0; j < Logits<DT>::kVec; ++j) take(x[j], uint32_t(split.head + (lo + tid + u * kT) * Logits<DT>::kVec + j));
-                    }
-                if (edges && tid < split.head + split.tail) take(Logits<DT>::one(row, split.edge(vocab, tid)), uint32_t(split.edge(vocab, tid)));
-            }
-            __syncthreads();
-        } else {
-            collect(least);
-        }
-        if (sh->n_found > kLogpFound) {      // some threads hold many: the exact key of the last token looked for, bit by bit
+        __syncthreads();
+        collect<false>(last == 0 ? 0 : uint64_t(last) << 32 | uint32_t(~sh->last_first));
+        if (sh->n_found > TopShared<kT>::kFound) {
             uint64_t t = 0;
             for (int bit = 63; bit >= 0; --bit)
                 if (count(t | uint64_t(1) << bit) >= top) t |= uint64_t(1) << bit;
-            collect(t);
+            __syncthreads();
+            if (tid == 0) sh->n_found = 0;
+            __syncthreads();
+            collect<false>(t);
         }
-        rank(sh, sh->found, min(sh->n_found, kLogpFound), top);
     }
 };
 
 // One row per cluster of kC CTAs, kT threads each.
-template <int DT, int kC, int kT>
+template <int DT, int kC, int kT, bool kTop>
 __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
     namespace cg = cooperative_groups;
     __shared__ Sums warp_sums[kT / 32], cta_sums;
-    __shared__ TopShared<kT> top_shared;
+    __shared__ typename std::conditional<kTop, TopShared<kT>, int>::type top_shared;
     begin_in_row();
     const int tid = threadIdx.x, lane = tid & 31, part = kC > 1 ? int(blockIdx.x % kC) : 0;
     const int64_t row = blockIdx.x / kC, vocab = g.vocab;
@@ -434,22 +500,37 @@ __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
         for (int u = 0; u < kLogpBatch; ++u) to[u] = ld_stream_u4(at + (u < n ? u : 0) * (kT * 16));
         at += kLogpBatch * kT * 16;
     };
+    // (the largest of every run of batches is noted where the most probable tokens are looked for)
+    const uint32_t run = uint32_t((hi - lo + int64_t(kLogpBatch * kTopSlots) * kT - 1) / (int64_t(kLogpBatch * kTopSlots) * kT));
+    uint32_t in_run = 0, slot = 0;
+    float slot_max = -INFINITY;
+    auto sum_up = [&](int n, bool end) {
+        const float most = own.batch(w, n, a);
+        if constexpr (kTop) {
+            slot_max = max_nan(slot_max, most);
+            if (++in_run == run || end) {
+                top_shared.slot[slot++][tid] = slot_max;
+                slot_max = -INFINITY;
+                in_run = 0;
+            }
+        }
+    };
     if (batches > 0) load(w, batches == 1 ? last : kLogpBatch);
     for (int64_t i = 1; i < batches; ++i) {
         uint4 next[kLogpBatch];
         load(next, i == batches - 1 ? last : kLogpBatch);
-        own.batch(w, kLogpBatch, a);
+        sum_up(kLogpBatch, false);
 #pragma unroll
         for (int u = 0; u < kLogpBatch; ++u) w[u] = next[u];
     }
-    if (batches > 0) own.batch(w, last, a);
+    if (batches > 0) sum_up(last, true);
     Sums sum = own.total();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         sum.join(Sums{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.q, o)}, a);
     if (lane == 0) warp_sums[tid >> 5] = sum;
-    if (g.top) {
-        TopFinder<DT, kT>{x, split, lo, hi, vocab, part == 0, &top_shared}.find(own.m, has, g.top, w);
+    if constexpr (kTop) {
+        TopFinder<DT, kT>{x, split, lo, hi, vocab, part == 0, run, &top_shared}.find(own.m, has, g.top, w);
     } else {
         __syncthreads();
     }
@@ -464,7 +545,7 @@ __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
         if (part == 0) {
             if (tid == 0)
                 for (int c = 1; c < kC; ++c) cta_sums.join(*cluster.map_shared_rank(&cta_sums, c), a);
-            if (g.top) {
+            if constexpr (kTop) {
                 for (int i = tid; i < kC * g.top; i += kT) top_shared.found[i] = cluster.map_shared_rank(&top_shared, i / g.top)->best[i % g.top];
                 __syncthreads();
                 TopFinder<DT, kT>::rank(&top_shared, top_shared.found, kC * g.top, g.top);
@@ -485,10 +566,12 @@ __global__ void __launch_bounds__(kT) logp_kernel(const LogpArgs g) {
         g.stats[row * 3 + 1] = log_sum;
         g.stats[row * 3 + 2] = h;
     }
-    if (tid < g.top) {
-        const uint64_t k = top_shared.best[tid];
-        g.top_ids[row * g.top + tid] = int32_t(~uint32_t(k));
-        g.top_logp[row * g.top + tid] = empty ? -INFINITY : g.scale * (Logits<DT>::value(uint32_t(k >> 32)) - all.m) - log_sum;
+    if constexpr (kTop) {
+        if (tid < g.top) {
+            const uint64_t k = top_shared.best[tid];
+            g.top_ids[row * g.top + tid] = int32_t(~uint32_t(k));
+            g.top_logp[row * g.top + tid] = empty ? -INFINITY : g.scale * (Logits<DT>::value(uint32_t(k >> 32)) - all.m) - log_sum;
+        }
     }
 }
 
@@ -610,20 +693,26 @@ int check_logp(const baoc_logp_t* e, int64_t n, const std::string& what) {
 template <int DT, int kC, int kT>
 int launch_logp(const LogpArgs& a, int64_t n, cudaStream_t s) {
     if (n * kC > 0x7fffffff) return fail_logp(BAOC_E_INVALID, "baoc_logp: too many rows for one launch");
-    const cudaError_t ce = launch_in_row(logp_kernel<DT, kC, kT>, dim3(unsigned(n * kC)), kT, 0, kC, s, a);
+    const cudaError_t ce = launch_in_row(a.top ? logp_kernel<DT, kC, kT, true> : logp_kernel<DT, kC, kT, false>, dim3(unsigned(n * kC)), kT, 0, kC, s, a);
     return ce == cudaSuccess ? BAOC_OK : fail_logp(BAOC_E_CUDA, std::string("logp_kernel: ") + cudaGetErrorString(ce));
 }
 
+// Few rows: each is shared by a cluster.  Else one CTA a row, of fewer threads where rows are short: a CTA's barriers and the
+// search for the most probable tokens cost the same for any row (65536 x 1000 with five of them: FIGURE us with 256 threads).
 template <int DT>
 int logp_of(const LogpArgs& a, int64_t n, cudaStream_t s) {
     int c = 1;
     while (c < kLogpMostCtas && n * c * 2 <= 2 * 148 && a.vocab >= int64_t(c) * 2 * kLogpCtaLogits) c *= 2;
     switch (c) {
-        case 1: return launch_logp<DT, 1, kThreads>(a, n, s);
-        case 2: return launch_logp<DT, 2, 2 * kThreads>(a, n, s);
-        case 4: return launch_logp<DT, 4, 2 * kThreads>(a, n, s);
-        default: return launch_logp<DT, 8, 2 * kThreads>(a, n, s);
+        case 2: return launch_logp<DT, 2, 512>(a, n, s);
+        case 4: return launch_logp<DT, 4, 512>(a, n, s);
+        case 8: return launch_logp<DT, 8, 512>(a, n, s);
+        default: break;
     }
+    const int64_t vecs = a.vocab / Logits<DT>::kVec;
+    if (vecs <= kLogpShort * 32) return launch_logp<DT, 1, 32>(a, n, s);
+    if (vecs <= kLogpShort * 128) return launch_logp<DT, 1, 128>(a, n, s);
+    return launch_logp<DT, 1, 256>(a, n, s);
 }
 
 }  // namespace
