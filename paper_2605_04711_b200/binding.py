@@ -432,6 +432,16 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _form(*tensors):
+    """All that a plan's checks of a call look at: equal forms need no second check (addresses are the library's to check)."""
+    return [t if t is None else (t.shape, t.stride(), t.dtype, t.get_device(), t.requires_grad) for t in tensors]
+
+
+def _no_autograd(what: str, name: str, t: Optional[torch.Tensor]):
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach {name}, or call it under torch.no_grad()")
+
+
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}       # BAOC_ACT_*
 LAYOUTS = {"out_in": 0, "in_out": 1}                                               # BAOC_OUT_IN, BAOC_IN_OUT
 
@@ -462,48 +472,47 @@ class Linear:
             raise BaocError(E_INVALID, f"act is one of {sorted(ACTIVATIONS)}, layout one of {sorted(LAYOUTS)}, not {act!r} and {layout!r}")
         self.n_in, self.n_out, self.act, self.layout = int(n_in), int(n_out), act, layout
         clamp = lambda n: max(-1, min(n, 2 ** 31 - 1))
-        self._e = LinearForm(clamp(self.n_in), clamp(self.n_out), ACTIVATIONS[act], LAYOUTS[layout], 0, 0)
-        self._ref, self._n = C.byref(self._e), C.c_size_t()
+        new = lambda: LinearForm(clamp(self.n_in), clamp(self.n_out), ACTIVATIONS[act], LAYOUTS[layout], 0, 0)
+        self._e, self._g, self._w = new(), new(), new()     # the descriptors of product, grad and the workspaces' sizes
+        self._ref, self._gref, self._wref = C.byref(self._e), C.byref(self._g), C.byref(self._w)
+        self._n, self._seen, self._gseen = C.c_size_t(), None, None
         self.w_shape = (self.n_out, self.n_in) if layout == "out_in" else (self.n_in, self.n_out)
         self.workspace_bytes(0)                             # the descriptor's checks
 
     def _failed(self, rc: int):
         raise BaocError(rc, _lib.baoc_linear_last_error().decode())
 
-    def _bytes(self, call, tokens: int, contiguous: bool, anywhere: bool) -> int:
-        if contiguous:
-            for name in ("x", "w", "dout"):
-                setattr(self._e, name + "_stride", 0)
-        rc = call(self._ref, int(tokens), 1 if anywhere else 0, C.byref(self._n))
+    def _bytes(self, call, ref, tokens: int, anywhere: bool) -> int:
+        rc = call(ref, int(tokens), 1 if anywhere else 0, C.byref(self._n))
         return self._n.value if rc >= 0 else self._failed(rc)
 
     def workspace_bytes(self, tokens: int) -> int:
         """Device bytes that ``product`` of contiguous, 16-byte aligned arrays needs (0 where their rows are multiples of 16 bytes)."""
-        return self._bytes(_lib.baoc_linear_workspace_bytes, tokens, True, False)
+        return self._bytes(_lib.baoc_linear_workspace_bytes, self._wref, tokens, False)
 
     def grad_workspace_bytes(self, tokens: int) -> int:
         """The same of ``grad``, whatever the type of its outputs."""
-        self._e.grad_dtype = DTYPES[torch.float32]
-        return self._bytes(_lib.baoc_linear_grad_workspace_bytes, tokens, True, False)
+        self._w.grad_dtype = DTYPES[torch.float32]
+        return self._bytes(_lib.baoc_linear_grad_workspace_bytes, self._wref, tokens, False)
 
-    def _take(self, what: str, rows, cols: int, dtypes, dev, **arrays):
-        """Checks arrays [.., cols] of `rows` rows (None: the first one's) and writes their strides to the descriptor; returns the rows."""
+    @staticmethod
+    def _take(e, what: str, rows, cols: int, dtypes, dev, **arrays):
+        """Checks arrays [.., cols] of `rows` rows (None: the first one's) and writes their strides to descriptor e; returns the rows."""
         for name, t in arrays.items():
             if t is None:
-                setattr(self._e, name + "_stride", 0)
+                setattr(e, name + "_stride", 0)
                 continue
             n, stride = _rows(t, cols, name)
             rows = n if rows is None else rows
             if n != rows or t.get_device() != dev or dev < 0 or t.dtype not in dtypes:
                 raise BaocError(E_INVALID, f"{what}: {name} must be [{rows}, {cols}] of {' or '.join(str(d) for d in dtypes)} on the device of x, cuda:{dev}")
-            if t.requires_grad and torch.is_grad_enabled():
-                raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach {name}, or call it under torch.no_grad()")
-            setattr(self._e, name + "_stride", stride)
+            _no_autograd(what, name, t)
+            setattr(e, name + "_stride", stride)
         return rows
 
-    def _workspace(self, what: str, call, tokens: int, ws, dev: int, anywhere: bool):
+    def _workspace(self, what: str, call, ref, tokens: int, ws, dev: int, arrays):
         if ws is None:
-            need = self._bytes(call, tokens, False, anywhere)
+            need = self._bytes(call, ref, tokens, any(t is not None and t.data_ptr() & 15 for t in arrays))
             return torch.empty(need, dtype=torch.uint8, device=f"cuda:{dev}") if need else None
         if ws.get_device() != dev or not ws.is_contiguous():
             raise BaocError(E_INVALID, f"{what}: ws must be a contiguous buffer on the device of the others")
@@ -515,21 +524,26 @@ class Linear:
         """out = act(x w^T + bias) + residual; pre (bf16, where given) takes the values before the activation.  out: allocated as
         out_dtype (residual's type, else bf16) when not given; it may be residual.  Rows of all may be strided.  ws: device bytes, at
         least ``workspace_bytes(tokens)``, more for strided or unaligned arrays (allocated when not given and needed)."""
-        bf, dev = (torch.bfloat16,), x.get_device()
+        dev = x.get_device()
         if out is None:
             out = torch.empty((*x.shape[:-1], self.n_out), dtype=out_dtype or (torch.bfloat16 if residual is None else residual.dtype), device=x.device)
-        n = self._take("product", None, self.n_in, bf, dev, x=x)
-        self._take("product", self.w_shape[0], self.w_shape[1], bf, dev, w=w)
-        self._take("product", n, self.n_out, tuple(DTYPES), dev, out=out)
-        self._take("product", n, self.n_out, (out.dtype,), dev, residual=residual)
-        self._take("product", n, self.n_out, bf, dev, pre=pre)
-        if bias is not None and (bias.dtype != torch.float32 or bias.numel() != self.n_out or not bias.is_contiguous() or bias.get_device() != dev):
-            raise BaocError(E_INVALID, f"product: bias must be a contiguous float32 vector of {self.n_out} elements on the device of x")
-        if bias is not None and bias.requires_grad and torch.is_grad_enabled():
-            raise BaocError(E_INVALID, "product: autograd does not see this call; detach bias, or call it under torch.no_grad()")
-        self._e.out_dtype, px, pw = DTYPES[out.dtype], x.data_ptr(), w.data_ptr()
-        ws = self._workspace("product", _lib.baoc_linear_workspace_bytes, n, ws, dev, (px | pw) & 15 != 0)
-        rc = _queue(dev, _lib.baoc_linear, self._ref, px, pw, _ptr(bias), _ptr(residual), n, out.data_ptr(), _ptr(pre),
+        form = _form(x, w, bias, residual, out, pre)
+        if form != self._seen:
+            self._seen, bf, e = None, (torch.bfloat16,), self._e
+            n = self._take(e, "product", None, self.n_in, bf, dev, x=x)
+            self._take(e, "product", self.w_shape[0], self.w_shape[1], bf, dev, w=w)
+            self._take(e, "product", n, self.n_out, tuple(DTYPES), dev, out=out)
+            self._take(e, "product", n, self.n_out, (out.dtype,), dev, residual=residual)
+            self._take(e, "product", n, self.n_out, bf, dev, pre=pre)
+            if bias is not None and (bias.dtype != torch.float32 or bias.numel() != self.n_out or not bias.is_contiguous() or bias.get_device() != dev):
+                raise BaocError(E_INVALID, f"product: bias must be a contiguous float32 vector of {self.n_out} elements on the device of x")
+            _no_autograd("product", "bias", bias)
+            e.out_dtype, self._tokens = DTYPES[out.dtype], n
+            if not any(t is not None and t[4] for t in form):       # (whether autograd is on is looked at anew)
+                self._seen = form
+        n = self._tokens
+        ws = self._workspace("product", _lib.baoc_linear_workspace_bytes, self._ref, n, ws, dev, (x, w))
+        rc = _queue(dev, _lib.baoc_linear, self._ref, x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), n, out.data_ptr(), _ptr(pre),
                     _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
         return out if rc >= 0 else self._failed(rc)
 
@@ -539,22 +553,26 @@ class Linear:
         """Writes those of dx (bf16), dw (w's layout) and db (bf16 or fp32, alike) that are given.  dout: bf16; pre: what ``product``
         kept, for a layer with an activation; x is needed for dw, w for dx.  ws: device bytes, at least
         ``grad_workspace_bytes(tokens)``, more for strided or unaligned arrays (allocated when not given and needed)."""
-        bf, dev = (torch.bfloat16,), dout.get_device()
-        n = self._take("grad", None, self.n_out, bf, dev, dout=dout)
-        self._take("grad", n, self.n_out, bf, dev, pre=pre)
-        self._take("grad", n, self.n_in, bf, dev, x=x, dx=dx)
-        self._take("grad", self.w_shape[0], self.w_shape[1], bf, dev, w=w)
-        dtype = dw.dtype if dw is not None else (db.dtype if db is not None else torch.float32)
-        _dtype_code(dtype)
-        self._take("grad", self.w_shape[0], self.w_shape[1], (dtype,), dev, dw=dw)
-        if db is not None and (db.dtype != dtype or db.numel() != self.n_out or not db.is_contiguous() or db.get_device() != dev):
-            raise BaocError(E_INVALID, f"grad: db must be a contiguous vector of {self.n_out} elements of dw's type on the device of the others")
-        if (dx is not None and w is None) or (dw is not None and x is None) or (self.act != "none" and pre is None):
-            raise BaocError(E_INVALID, "grad: dx needs w, dw needs x, an activation needs pre")
-        self._e.grad_dtype = DTYPES[dtype]
-        anywhere = any(t is not None and t.data_ptr() & 15 for t in (x, w, dout))
-        ws = self._workspace("grad", _lib.baoc_linear_grad_workspace_bytes, n, ws, dev, anywhere)
-        rc = _queue(dev, _lib.baoc_linear_grad, self._ref, _ptr(x), _ptr(w), dout.data_ptr(), _ptr(pre), n, _ptr(dx), _ptr(dw), _ptr(db),
+        dev, form = dout.get_device(), _form(x, w, dout, pre, dx, dw, db)
+        if form != self._gseen:
+            self._gseen, bf, e = None, (torch.bfloat16,), self._g
+            n = self._take(e, "grad", None, self.n_out, bf, dev, dout=dout)
+            self._take(e, "grad", n, self.n_out, bf, dev, pre=pre)
+            self._take(e, "grad", n, self.n_in, bf, dev, x=x, dx=dx)
+            self._take(e, "grad", self.w_shape[0], self.w_shape[1], bf, dev, w=w)
+            dtype = dw.dtype if dw is not None else (db.dtype if db is not None else torch.float32)
+            _dtype_code(dtype)
+            self._take(e, "grad", self.w_shape[0], self.w_shape[1], (dtype,), dev, dw=dw)
+            if db is not None and (db.dtype != dtype or db.numel() != self.n_out or not db.is_contiguous() or db.get_device() != dev):
+                raise BaocError(E_INVALID, f"grad: db must be a contiguous vector of {self.n_out} elements of dw's type on the device of the others")
+            if (dx is not None and w is None) or (dw is not None and x is None) or (self.act != "none" and pre is None):
+                raise BaocError(E_INVALID, "grad: dx needs w, dw needs x, an activation needs pre")
+            e.grad_dtype, self._gtokens = DTYPES[dtype], n
+            if not any(t is not None and t[4] for t in form):
+                self._gseen = form
+        n = self._gtokens
+        ws = self._workspace("grad", _lib.baoc_linear_grad_workspace_bytes, self._gref, n, ws, dev, (x, w, dout))
+        rc = _queue(dev, _lib.baoc_linear_grad, self._gref, _ptr(x), _ptr(w), dout.data_ptr(), _ptr(pre), n, _ptr(dx), _ptr(dw), _ptr(db),
                     _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
         return None if rc >= 0 else self._failed(rc)
 
@@ -573,24 +591,25 @@ class Join:
         if kind not in ("rms", "layer"):
             raise BaocError(E_INVALID, f"kind must be \"rms\" or \"layer\", not {kind!r}")
         self.dim, self.kind = int(dim), kind
-        self._e = JoinForm(max(-1, min(self.dim, 2 ** 31 - 1)), 1 if kind == "layer" else 0, 0, 0, 0, float(eps), float(scale), 0, 0)
-        self._ref, self._n = C.byref(self._e), C.c_size_t()
+        new = lambda: JoinForm(max(-1, min(self.dim, 2 ** 31 - 1)), 1 if kind == "layer" else 0, 0, 0, 0, float(eps), float(scale), 0, 0)
+        self._e, self._g = new(), new()                     # the descriptors of join and grad
+        self._ref, self._gref, self._n = C.byref(self._e), C.byref(self._g), C.c_size_t()
+        self._seen, self._gseen = None, None
         self.grad_workspace_bytes(0)                        # the descriptor's checks
 
     def _failed(self, rc: int):
         raise BaocError(rc, _lib.baoc_join_last_error().decode())
 
-    def _take(self, what: str, f, stream, branch, vectors, gate, dgate):
-        """Checks the arrays against one another and fills the descriptor.  stream, branch: {field: tensor or None}."""
-        dim, e = self.dim, self._e
+    def _take(self, e, what: str, stream, branch, vectors, gate, dgate):
+        """Checks the arrays against one another and fills descriptor e; returns the rows.  stream, branch: {field: tensor or None}."""
+        dim = self.dim
         n = dev = None
         for arrays, field in ((stream, "stream_dtype"), (branch, "branch_dtype")):
             dtype = None
             for name, t in arrays.items():
                 if t is None:
                     continue
-                if t.requires_grad and torch.is_grad_enabled():
-                    raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach {name}, or call it under torch.no_grad()")
+                _no_autograd(what, name, t)
                 rows, stride = _rows(t, dim, name)
                 n, dev, dtype = rows if n is None else n, t.get_device() if dev is None else dev, dtype or t.dtype
                 if rows != n or t.get_device() != dev or dev < 0 or t.dtype != dtype:
@@ -600,19 +619,17 @@ class Join:
         for t in vectors:
             if t is not None and (t.dtype != torch.float32 or t.numel() != dim or not t.is_contiguous() or t.get_device() != dev):
                 raise BaocError(E_INVALID, f"{what}: weights and biases are contiguous float32 vectors of {dim} elements on the device of the others")
-            if t is not None and t.requires_grad and torch.is_grad_enabled():
-                raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach the weights, or call it under torch.no_grad()")
+            _no_autograd(what, "the weights", t)
         e.rows_per_gate = 0
         if gate is not None:
             gates = gate.numel() // dim
             if gate.dtype != torch.float32 or gate.size(-1) != dim or not gate.is_contiguous() or gate.get_device() != dev or gates < 1 or n % gates:
                 raise BaocError(E_INVALID, f"{what}: gate must be a contiguous float32 [{dim}] or [gates, {dim}] with equally many rows each, on the device of the others")
-            if gate.requires_grad and torch.is_grad_enabled():
-                raise BaocError(E_INVALID, f"{what}: autograd does not see this call; detach the gate, or call it under torch.no_grad()")
+            _no_autograd(what, "the gate", gate)
             e.rows_per_gate = n // gates if gates > 1 else 0
         if dgate is not None and (gate is None or dgate.numel() != gate.numel()):
             raise BaocError(E_INVALID, f"{what}: dgate must be of gate's shape")
-        return n, dev
+        return n
 
     def join(self, x: Optional[torch.Tensor], f: torch.Tensor, pre_w: torch.Tensor, pre_b: Optional[torch.Tensor] = None,
              post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
@@ -623,9 +640,14 @@ class Join:
             y = torch.empty(f.shape, dtype=torch.float32 if x is None else x.dtype, device=f.device)
         if h is None:
             h = torch.empty(f.shape, dtype=f.dtype, device=f.device)
-        n, dev = self._take("join", f, {"x": x, "y": y}, {"f": f, "h": h}, (pre_w, pre_b, post_w, post_b), gate, None)
-        rc = _queue(dev, _lib.baoc_join, self._ref, _ptr(x), f.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate), pre_w.data_ptr(), _ptr(pre_b),
-                    n, y.data_ptr(), h.data_ptr())
+        form = _form(x, f, pre_w, pre_b, post_w, post_b, gate, y, h)
+        if form != self._seen:
+            self._seen = None
+            self._rows = self._take(self._e, "join", {"x": x, "y": y}, {"f": f, "h": h}, (pre_w, pre_b, post_w, post_b), gate, None)
+            if not any(t is not None and t[4] for t in form):       # (whether autograd is on is looked at anew)
+                self._seen = form
+        rc = _queue(f.get_device(), _lib.baoc_join, self._ref, _ptr(x), f.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate), pre_w.data_ptr(), _ptr(pre_b),
+                    self._rows, y.data_ptr(), h.data_ptr())
         return (y, h) if rc >= 0 else self._failed(rc)
 
     def grad_workspace_bytes(self, rows: int) -> int:
@@ -645,19 +667,25 @@ class Join:
             dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
         if df is None:
             df = torch.empty(dh.shape, dtype=dh.dtype, device=dh.device)
-        n, dev = self._take("grad", f, {"y": y, "dy": dy, "dx": dx}, {"dh": dh, "f": f, "df": df}, (pre_w, post_w, post_b), gate, dgate)
-        dtype = None
-        for t in (dpre_w, dpre_b, dpost_w, dpost_b, dgate):
-            if t is not None:
-                dtype = dtype or t.dtype
-                if t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev or (t is not dgate and t.numel() != self.dim):
-                    raise BaocError(E_INVALID, f"grad: gradients of weights, biases and gate are contiguous, of one type, on the device of the others, of {self.dim} elements")
-        self._e.grad_dtype = _dtype_code(dtype or torch.float32)
+        form = _form(y, f, dh, pre_w, dy, post_w, post_b, gate, dx, df, dpre_w, dpre_b, dpost_w, dpost_b, dgate)
+        dev = y.get_device()
+        if form != self._gseen:
+            self._gseen, dtype = None, None
+            n = self._take(self._g, "grad", {"y": y, "dy": dy, "dx": dx}, {"dh": dh, "f": f, "df": df}, (pre_w, post_w, post_b), gate, dgate)
+            for t in (dpre_w, dpre_b, dpost_w, dpost_b, dgate):
+                if t is not None:
+                    dtype = dtype or t.dtype
+                    if t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev or (t is not dgate and t.numel() != self.dim):
+                        raise BaocError(E_INVALID, f"grad: gradients of weights, biases and gate are contiguous, of one type, on the device of the others, of {self.dim} elements")
+            self._g.grad_dtype, self._grows = _dtype_code(dtype or torch.float32), n
+            if not any(t is not None and t[4] for t in form):
+                self._gseen = form
+        n = self._grows
         if ws is None:
             ws = torch.empty(self.grad_workspace_bytes(n), dtype=torch.uint8, device=y.device)
         elif ws.get_device() != dev or not ws.is_contiguous():
             raise BaocError(E_INVALID, "grad: ws must be a contiguous buffer on the device of the others")
-        rc = _queue(dev, _lib.baoc_join_grad, self._ref, y.data_ptr(), _ptr(f), _ptr(dy), dh.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate),
+        rc = _queue(dev, _lib.baoc_join_grad, self._gref, y.data_ptr(), _ptr(f), _ptr(dy), dh.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate),
                     pre_w.data_ptr(), n, _ptr(dx), df.data_ptr(), _ptr(dpost_w), _ptr(dpost_b), _ptr(dgate), _ptr(dpre_w), _ptr(dpre_b),
                     ws.data_ptr(), ws.numel() * ws.element_size())
         return (dx, df) if rc >= 0 else self._failed(rc)
@@ -682,9 +710,10 @@ class LogProbs:
 
     def __init__(self, vocab: int, scale: float = 1.0, top: int = 0):
         self.vocab, self.top = int(vocab), int(top)
-        self._e = Logp(self.vocab, DTYPES[torch.bfloat16], 64, float(scale), max(-1, min(self.top, 2 ** 31 - 1)), 0, 0)
-        self._ref = C.byref(self._e)
-        self._form = None
+        new = lambda: Logp(self.vocab, DTYPES[torch.bfloat16], 64, float(scale), max(-1, min(self.top, 2 ** 31 - 1)), 0, 0)
+        self._e, self._g = new(), new()                     # the descriptors of logprobs and grad
+        self._ref, self._gref = C.byref(self._e), C.byref(self._g)
+        self._seen, self._gseen = None, None
         if _lib.baoc_logp(self._ref, None, None, 0, None, None, None, None, None, None) < 0:     # the descriptor's checks
             raise BaocError(E_INVALID, _lib.baoc_logp_last_error().decode())
 
@@ -695,8 +724,9 @@ class LogProbs:
         top = (new(self.top, dtype=torch.int32), new(self.top)) if self.top else (None, None)
         return TokenLogProbs(new(), new(), new(3), *top)
 
-    def _call(self, what: str, logits, ids, dlogits, floats):
-        """Checks shapes and devices and fills the descriptor; returns (device, rows, ids)."""
+    def _call(self, e, what: str, logits, ids, dlogits, floats):
+        """Checks shapes, types and devices and fills descriptor e; returns (device, rows, ids)."""
+        self._seen = self._seen if e is self._g else None
         n, dev = ids.numel(), logits.get_device()
         rows, stride = _rows(logits, self.vocab, "logits")
         grad_rows, grad_stride = (n, 0) if dlogits is None else _rows(dlogits, self.vocab, "dlogits")
@@ -707,19 +737,12 @@ class LogProbs:
                 raise BaocError(E_INVALID, f"{what}: contiguous float32 arrays of one value per id (three in stats, `top` in top_logp) on the logits' device")
         if ids.dim() != 1 and logits.dim() != 2 and logits.shape[:-1] != ids.shape:
             raise BaocError(E_INVALID, f"{what}: logits must be of ids' shape + [{self.vocab}], not {list(logits.shape)} for {list(ids.shape)}")
-        form = (logits.dtype, ids.dtype, stride, grad_stride)
-        if form != self._form:
-            if ids.dtype not in _ID_BITS or (dlogits is not None and dlogits.dtype != logits.dtype):
-                raise BaocError(E_INVALID, f"{what}: ids of int32 or int64, and dlogits of the logits' type")
-            self._form = None
-            self._e.dtype, self._e.id_bits, self._e.stride, self._e.grad_stride = _dtype_code(logits.dtype), _ID_BITS[ids.dtype], stride, grad_stride
-            self._form = form
+        if ids.dtype not in _ID_BITS or (dlogits is not None and dlogits.dtype != logits.dtype):
+            raise BaocError(E_INVALID, f"{what}: ids of int32 or int64, and dlogits of the logits' type")
+        e.dtype, e.id_bits, e.stride, e.grad_stride = _dtype_code(logits.dtype), _ID_BITS[ids.dtype], stride, grad_stride
         return dev, n, ids if ids.is_contiguous() else ids.contiguous()
 
     def _failed(self, rc: int):
-        """Raises, and leaves no stride of the refused arrays in the descriptor."""
-        self._form = None
-        self._e.stride = self._e.grad_stride = 0
         raise BaocError(rc, _lib.baoc_logp_last_error().decode())
 
     def logprobs(self, logits: torch.Tensor, ids: torch.Tensor, out: Optional[TokenLogProbs] = None) -> TokenLogProbs:
@@ -732,10 +755,18 @@ class LogProbs:
         if out is None:
             out = self.buffers(ids.shape, logits.device)
         n, k = ids.numel(), self.top
+        form = _form(logits, ids, *out)
+        if form == self._seen:
+            rc = _queue(logits.get_device(), _lib.baoc_logp, self._ref, logits.data_ptr(), ids.data_ptr(), n, out.logp.data_ptr(), out.entropy.data_ptr(),
+                        out.stats.data_ptr(), out.top_ids.data_ptr() if k else None, out.top_logp.data_ptr() if k else None)
+            return out if rc >= 0 else self._failed(rc)
         if k and (out.top_ids is None or out.top_ids.dtype != torch.int32 or out.top_ids.numel() != n * k or not out.top_ids.is_contiguous()
                   or out.top_ids.get_device() != logits.get_device() or out.top_logp is None):
             raise BaocError(E_INVALID, "logprobs: top_ids must be a contiguous int32 array of `top` tokens per id on the logits' device")
-        dev, n, ids = self._call("logprobs", logits, ids, None, ((out.logp, n), (out.entropy, n), (out.stats, 3 * n), (out.top_logp if k else None, n * k)))
+        same = ids
+        dev, n, ids = self._call(self._e, "logprobs", logits, ids, None, ((out.logp, n), (out.entropy, n), (out.stats, 3 * n), (out.top_logp if k else None, n * k)))
+        if ids is same and not logits.requires_grad:        # (a copy of the ids is made anew)
+            self._seen = form
         rc = _queue(dev, _lib.baoc_logp, self._ref, logits.data_ptr(), ids.data_ptr(), n, out.logp.data_ptr(), out.entropy.data_ptr(),
                     out.stats.data_ptr(), out.top_ids.data_ptr() if k else None, out.top_logp.data_ptr() if k else None)
         return out if rc >= 0 else self._failed(rc)
@@ -747,9 +778,13 @@ class LogProbs:
         themselves, which are overwritten then."""
         if dlogits is None:
             dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        n = ids.numel()
-        dev, n, ids = self._call("grad", logits, ids, dlogits, ((stats, 3 * n), (dlogp, n), (dentropy, n)))
-        rc = _queue(dev, _lib.baoc_logp_grad, self._ref, logits.data_ptr(), ids.data_ptr(), stats.data_ptr(), dlogp.data_ptr(),
+        n, dev, form = ids.numel(), logits.get_device(), _form(logits, ids, stats, dlogp, dentropy, dlogits)
+        if form != self._gseen:
+            self._gseen, same = None, ids
+            dev, n, ids = self._call(self._g, "grad", logits, ids, dlogits, ((stats, 3 * n), (dlogp, n), (dentropy, n)))
+            if ids is same:                                 # (a copy of the ids is made anew)
+                self._gseen = form
+        rc = _queue(dev, _lib.baoc_logp_grad, self._gref, logits.data_ptr(), ids.data_ptr(), stats.data_ptr(), dlogp.data_ptr(),
                     None if dentropy is None else dentropy.data_ptr(), n, dlogits.data_ptr())
         return dlogits if rc >= 0 else self._failed(rc)
 
