@@ -15,6 +15,7 @@
 #include <cuda_runtime.h>
 #include <new>
 #include <string>
+#include <utility>
 
 #include "baoc_tensor.cuh"
 
@@ -50,6 +51,7 @@ __device__ unsigned int g_gave_up;                   // CTAs in which a wait ran
 
 struct ProductArgs {
     int m, n, k_tiles, passes;       // passes: products of as many operand pairs are added up
+    int m_tiles, n_tiles;
     int a_mn, b_mn;                  // the operand's m (n) lies contiguous, not its k
     int a_rows;                      // rows of A that a copy brings: fewer than a tile's where m is smaller
     int act, out_f32;
@@ -62,6 +64,18 @@ struct ProductArgs {
 
 struct Maps { CUtensorMap a[3], b[3], out, pre; };
 
+// One or two products of one launch (two where a gradient's both are formed: the second's tiles fill the places that the first's
+// last round leaves empty).
+struct Problem {
+    Maps maps;
+    ProductArgs g;
+};
+struct Problems {
+    Problem p[2];
+    int tiles[2];
+    int fewer;                       // tiles of the second that the workers take which have one more of the first's (see Walk)
+};
+
 __device__ __forceinline__ float exp2_approx(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -71,40 +85,64 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // The normal distribution below -|z|, as e^(-z^2/2) times a polynomial in t = 1 / (1 + 0.35 |z|): erfc(x) e^(x^2) is smooth in
 // such a t.  The coefficients are a least-maximum fit of the relative error over |z| <= 15 (3.2e-8 in exact arithmetic, 5 2^-24
-// with the coefficients and every step in fp32); two approximate functions against some forty instructions of erfcf.
-// Returns it and, in *density, e^(-z^2/2).
-__device__ __forceinline__ float lower_tail(float z, float* density) {
-    const float t = rcp_approx(fmaf(0.35f, fabsf(z), 1.f));
-    float p = -0.02916380763053894f;
-    p = fmaf(p, t, 0.14406023919582367f);
-    p = fmaf(p, t, -0.2559007406234741f);
-    p = fmaf(p, t, 0.15939167141914368f);
-    p = fmaf(p, t, -0.02326301671564579f);
-    p = fmaf(p, t, 0.10557447373867035f);
-    p = fmaf(p, t, 0.11981557309627533f);
-    p = fmaf(p, t, 0.13986432552337646f);
-    p = fmaf(p, t, 0.13962125778198242f);
-    *density = exp2_approx(-0.5f * kLog2e * (z * z));
-    return p * t * *density;
+// with the coefficients and every step in fp32); two approximate functions against some forty instructions of erfcf.  Two at a
+// time.  Returns it and, in *density, e^(-z^2/2).
+__device__ __forceinline__ f32x2 exp2_pair(f32x2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return pack2(exp2_approx(a), exp2_approx(b));
 }
-__device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.f + exp2_approx(-kLog2e * z)); }
+__device__ __forceinline__ f32x2 rcp_pair(f32x2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return pack2(rcp_approx(a), rcp_approx(b));
+}
+__device__ __forceinline__ f32x2 lower_tail(f32x2 z, f32x2* density) {
+    float a, b;
+    unpack2(z, a, b);
+    const f32x2 t = rcp_pair(fma2(splat2(0.35f), pack2(fabsf(a), fabsf(b)), splat2(1.f)));
+    f32x2 p = splat2(-0.02916380763053894f);
+    p = fma2(p, t, splat2(0.14406023919582367f));
+    p = fma2(p, t, splat2(-0.2559007406234741f));
+    p = fma2(p, t, splat2(0.15939167141914368f));
+    p = fma2(p, t, splat2(-0.02326301671564579f));
+    p = fma2(p, t, splat2(0.10557447373867035f));
+    p = fma2(p, t, splat2(0.11981557309627533f));
+    p = fma2(p, t, splat2(0.13986432552337646f));
+    p = fma2(p, t, splat2(0.13962125778198242f));
+    *density = exp2_pair(mul2(splat2(-0.5f * kLog2e), mul2(z, z)));
+    return mul2(mul2(p, t), *density);
+}
+// the normal distribution below z from its tail below -|z|
+__device__ __forceinline__ f32x2 below(f32x2 z, f32x2 tail) {
+    float a, b, s, t;
+    unpack2(z, a, b);
+    unpack2(tail, s, t);
+    return pack2(a > 0.f ? 1.f - s : s, b > 0.f ? 1.f - t : t);
+}
+__device__ __forceinline__ f32x2 sigmoid(f32x2 z) { return rcp_pair(add2(splat2(1.f), exp2_pair(mul2(splat2(-kLog2e), z)))); }
+// the exponent of gelu's tanh form, 2 sqrt(2 / pi) (z + 0.044715 z^3)
+__device__ __forceinline__ f32x2 tanh_form(f32x2 z) { return mul2(splat2(1.5957691216057308f), fma2(mul2(mul2(splat2(0.044715f), z), z), z, z)); }
 
 template <int kAct>
-__device__ __forceinline__ float act_of(float z) {
-    if constexpr (kAct == BAOC_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
-    if constexpr (kAct == BAOC_ACT_GELU) {
-        float d;
-        const float tail = lower_tail(z, &d);
-        return z * (z > 0.f ? 1.f - tail : tail);
+__device__ __forceinline__ f32x2 act_of(f32x2 z) {
+    if constexpr (kAct == BAOC_ACT_RELU) {
+        float a, b;
+        unpack2(z, a, b);
+        return pack2(a > 0.f || a != a ? a : 0.f, b > 0.f || b != b ? b : 0.f);
     }
-    if constexpr (kAct == BAOC_ACT_GELU_TANH) return z * sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
-    if constexpr (kAct == BAOC_ACT_SILU) return z * sigmoid(z);
+    if constexpr (kAct == BAOC_ACT_GELU) {
+        f32x2 d;
+        return mul2(z, below(z, lower_tail(z, &d)));
+    }
+    if constexpr (kAct == BAOC_ACT_GELU_TANH) return mul2(z, sigmoid(tanh_form(z)));
+    if constexpr (kAct == BAOC_ACT_SILU) return mul2(z, sigmoid(z));
     return z;
 }
 template <int kAct>
 __device__ __forceinline__ void act_all(float* v, int n) {
 #pragma unroll
-    for (int i = 0; i < n; ++i) v[i] = act_of<kAct>(v[i]);
+    for (int i = 0; i < n; i += 2) unpack2(act_of<kAct>(pack2(v[i], v[i + 1])), v[i], v[i + 1]);
 }
 template <int kCount>
 __device__ __forceinline__ void apply_act(float (&v)[kCount], int act) {
@@ -118,22 +156,30 @@ __device__ __forceinline__ void apply_act(float (&v)[kCount], int act) {
 }
 // (past the ends below the derivative is 0 or 1 to all bits, and its formula would form inf * 0)
 template <int kAct>
-__device__ __forceinline__ float act_slope(float z) {
+__device__ __forceinline__ f32x2 act_slope(f32x2 z) {
+    float a, b;
+    unpack2(z, a, b);
     if constexpr (kAct == BAOC_ACT_RELU) {
-        return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    } else if constexpr (kAct == BAOC_ACT_GELU) {
-        float d;
-        const float y = fminf(fmaxf(z, -15.f), 15.f), tail = lower_tail(y, &d), r = (y > 0.f ? 1.f - tail : tail) + 0.3989422804014327f * y * d;
-        return z != z ? z : r;
-    } else if constexpr (kAct == BAOC_ACT_GELU_TANH) {
-        const float y = fminf(fmaxf(z, -15.f), 15.f), s = sigmoid(1.5957691216057308f * (y + 0.044715f * y * y * y));
-        const float r = s + y * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * y * y);
-        return z != z ? z : r;
-    } else if constexpr (kAct == BAOC_ACT_SILU) {
-        const float y = fminf(fmaxf(z, -90.f), 90.f), s = sigmoid(y), r = s * (1.f + y * (1.f - s));
-        return z != z ? z : r;
+        auto one = [](float x) { return x > 0.f ? 1.f : (x != x ? x : 0.f); };
+        return pack2(one(a), one(b));
     }
-    return 1.f;
+    constexpr float kEnd = kAct == BAOC_ACT_SILU ? 90.f : 15.f;
+    auto clamp = [](float x) { return x != x ? x : fminf(fmaxf(x, -kEnd), kEnd); };
+    const f32x2 y = pack2(clamp(a), clamp(b));
+    if constexpr (kAct == BAOC_ACT_GELU) {
+        f32x2 d;
+        const f32x2 p = below(y, lower_tail(y, &d));
+        return fma2(mul2(splat2(0.3989422804014327f), y), d, p);
+    }
+    if constexpr (kAct == BAOC_ACT_GELU_TANH) {
+        const f32x2 s = sigmoid(tanh_form(y)), rest = fma2(mul2(splat2(-1.f), s), s, s);      // s (1 - s)
+        return fma2(mul2(y, rest), mul2(splat2(1.5957691216057308f), fma2(mul2(splat2(0.134145f), y), y, splat2(1.f))), s);
+    }
+    if constexpr (kAct == BAOC_ACT_SILU) {
+        const f32x2 s = sigmoid(y);
+        return mul2(s, fma2(y, add2(splat2(1.f), mul2(splat2(-1.f), s)), splat2(1.f)));
+    }
+    return splat2(1.f);
 }
 
 __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
@@ -229,13 +275,34 @@ __device__ __forceinline__ void tile_place(int tile, int m_tiles, int n_tiles, i
     *mt = first + in - *nt * height;
 }
 
+// The tiles of a worker, in the order that all of its roles go through them: the first product's every workers-th, then the
+// second's.  Workers that the first left with a tile more take `fewer` of the second's, the others go on until all are taken.
+struct Walk {
+    int worker, workers, longer, fewer, problem = 0, i = -1;
+    __device__ __forceinline__ Walk(const Problems& all, int worker, int workers)
+        : worker(worker), workers(workers), longer(all.tiles[0] % workers), fewer(all.fewer) {}
+    __device__ __forceinline__ bool next(const Problems& all, int* tile) {
+        ++i;
+        if (problem == 0) {
+            *tile = worker + i * workers;
+            if (*tile < all.tiles[0]) return true;
+            problem = 1;
+            i = 0;
+        }
+        if (i < fewer) *tile = i * workers + worker;
+        else if (worker >= longer) *tile = fewer * workers + (i - fewer) * (workers - longer) + worker - longer;
+        else return false;
+        return *tile < all.tiles[1];
+    }
+};
+
 // What a writing warp does with 32 columns of its 32 rows.
 struct Writer {
     const ProductArgs& g;
     const Maps& maps;
     uint32_t buf;                    // two buffers of `bytes`
     uint32_t bytes;
-    int lane, turn = 0;
+    int lane, turn;
 
     // a thread's row of 32 values into the warp's buffer, as a tiled copy with swizzled rows expects it, and off
     __device__ __forceinline__ void send(const CUtensorMap* map, int f32, int col, int row0, const float (&v)[32]) {
@@ -288,7 +355,7 @@ struct Writer {
 };
 
 template <int kCtas, int kN, bool kChunked>
-__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Maps maps, const ProductArgs g) {
+__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Problems all) {
     using T = TileShape<kCtas, kN, kChunked>;
     constexpr int kS = T::kStages;
     extern __shared__ char raw[];
@@ -302,9 +369,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     auto acc_empty = [&](int a) { return bar0 + 8 * (2 * kS + 2 + a); };
     const uint32_t drained = bar0 + 8 * (2 * kS + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = kCtas == 2 ? int(cluster_rank()) : 0;
-    const int worker = int(blockIdx.x) / kCtas, workers = int(gridDim.x) / kCtas;
-    const int m_tiles = (g.m + kTileM * kCtas - 1) / (kTileM * kCtas), n_tiles = (g.n + kN - 1) / kN, tiles = m_tiles * n_tiles, steps = g.k_tiles * g.passes;
-    const int chunk = kChunked ? kChunk : steps, chunks = (steps + chunk - 1) / chunk;
+    Walk walk(all, int(blockIdx.x) / kCtas, int(gridDim.x) / kCtas);
+    int tile;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kS; ++s) { bar_init(full(s), 1); bar_init(empty(s), 1); }
         for (int a = 0; a < 2; ++a) { bar_init(acc_full(a), 1); bar_init(acc_empty(a), kWriters * kCtas); }
@@ -324,23 +390,26 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if (warp == 0 && lane == 0) {                     // copies: each CTA its own operands, a pair's bytes counted by its first CTA
         int s = 0, round = 0, issued = 0;
         bool ok = true;
-        for (int tile = worker; ok && tile < tiles; tile += workers) {
+        while (ok && walk.next(all, &tile)) {
+            const ProductArgs& g = all.p[walk.problem].g;
+            const Maps& maps = all.p[walk.problem].maps;
             int mt, nt;
-            tile_place(tile, m_tiles, n_tiles, &mt, &nt);
-            const int m0 = (mt * kCtas + rank) * kTileM, n0 = nt * kN + rank * T::kBRows;
+            tile_place(tile, g.m_tiles, g.n_tiles, &mt, &nt);
+            const int m0 = (mt * kCtas + rank) * kTileM, n0 = nt * kN + rank * T::kBRows, k_tiles = g.k_tiles, steps = k_tiles * g.passes, a_mn = g.a_mn, b_mn = g.b_mn;
+            const uint32_t bytes = (g.a_rows * kRowBytes + T::kBBytes) * kCtas;
             for (int i = 0; i < steps; ++i) {
                 if (!(ok = bar_wait(empty(s), (round & 1) ^ 1))) break;
-                if (rank == 0) bar_expect(full(s), (g.a_rows * kRowBytes + T::kBBytes) * kCtas);
+                if (rank == 0) bar_expect(full(s), bytes);
                 const uint32_t bar = kCtas == 2 ? at_rank(full(s), 0) : full(s);
-                const int pass = (i >= g.k_tiles) + (i >= 2 * g.k_tiles), k = (i - pass * g.k_tiles) * kTileK;
+                const int pass = (i >= k_tiles) + (i >= 2 * k_tiles), k = (i - pass * k_tiles) * kTileK;
                 const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
-                if (g.a_mn) {
+                if (a_mn) {
 #pragma unroll
                     for (int c = 0; c < kTileM / 64; ++c) copy_tile<kCtas>(a + c * 64 * kRowBytes, &maps.a[pass], m0 + c * 64, k, bar);
                 } else {
                     copy_tile<kCtas>(a, &maps.a[pass], k, m0, bar);
                 }
-                if (g.b_mn) {
+                if (b_mn) {
 #pragma unroll
                     for (int c = 0; c < T::kBRows / 64; ++c) copy_tile<kCtas>(b + c * 64 * kRowBytes, &maps.b[pass], n0 + c * 64, k, bar);
                 } else {
@@ -357,11 +426,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
         }
     } else if (warp == 1 && lane == 0 && rank == 0) { // products
-        const uint32_t desc = product_desc(kTileM * kCtas, kN, g.a_mn, g.b_mn);
-        const uint32_t a_step = g.a_mn ? 16 * kRowBytes : 32, b_step = g.b_mn ? 16 * kRowBytes : 32;    // bytes per 16 k
         int s = 0, round = 0, count = 0;
         bool ok = true;
-        for (int tile = worker; ok && tile < tiles; tile += workers) {
+        while (ok && walk.next(all, &tile)) {
+            const ProductArgs& g = all.p[walk.problem].g;
+            const uint32_t desc = product_desc(kTileM * kCtas, kN, g.a_mn, g.b_mn);
+            const uint32_t a_step = g.a_mn ? 16 * kRowBytes : 32, b_step = g.b_mn ? 16 * kRowBytes : 32;    // bytes per 16 k
+            const int steps = g.k_tiles * g.passes, chunk = kChunked ? kChunk : steps;
             for (int first = 0; ok && first < steps; first += chunk, ++count) {
                 const int half = count & 1, last = min(steps, first + chunk);
                 if (!(ok = bar_wait(acc_empty(half), ((count >> 1) & 1) ^ 1))) break;
@@ -388,14 +459,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     } else if (warp >= 4) {                           // write out
         const int quarter = warp & 3, side = (warp - 4) >> 2;       // a warp reads its quarter of the lanes alone
         constexpr int kCols = kN / 2;
-        Writer writer{g, maps, outs + (warp - 4) * 2 * T::kOutBytes, T::kOutBytes, lane};
-        int count = 0;
+        int count = 0, turn = 0;
         bool ok = true;
-        for (int tile = worker; ok && tile < tiles; tile += workers) {
+        while (ok && walk.next(all, &tile)) {
+            const ProductArgs& g = all.p[walk.problem].g;
+            Writer writer{g, all.p[walk.problem].maps, outs + (warp - 4) * 2 * T::kOutBytes, T::kOutBytes, lane, turn};
             int mt, nt;
-            tile_place(tile, m_tiles, n_tiles, &mt, &nt);
+            tile_place(tile, g.m_tiles, g.n_tiles, &mt, &nt);
             const int64_t row0 = (int64_t(mt) * kCtas + rank) * kTileM + quarter * 32;
-            const int col0 = nt * kN + side * kCols;
+            const int col0 = nt * kN + side * kCols, chunks = kChunked ? (g.k_tiles * g.passes + kChunk - 1) / kChunk : 1;
             float total[kChunked ? kCols / 32 : 1][32];
             for (int c = 0; c < chunks; ++c, ++count) {
                 const int half = count & 1;
@@ -430,6 +502,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         if (col0 + p * 32 < g.n) writer.write(row0, col0 + p * 32, total[p]);
                 }
             }
+            turn = writer.turn;
         }
         if (!ok) failed = 1;
         if (lane == 0) stores_read<0>();
@@ -461,7 +534,7 @@ __device__ __forceinline__ float4 load_at_rank(uint32_t addr, uint32_t rank) {
 // where 16 bytes (4 sums) of the tile lie: rows of 256 bytes, spread over the banks
 __device__ __forceinline__ uint32_t sum_place(int row, int four) { return uint32_t(row * 256 + ((four ^ (row & 15)) << 4)); }
 
-__global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const __grid_constant__ Maps maps, const ProductArgs g, int parts) {
+__global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const __grid_constant__ Problems all, int parts) {
     constexpr int kS = kSplitStages;
     extern __shared__ char raw[];
     __shared__ uint64_t bars[2 * kS + 5];
@@ -473,8 +546,11 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
     auto acc_full = [&](int a) { return bar0 + 8 * (2 * kS + a); };
     auto acc_empty = [&](int a) { return bar0 + 8 * (2 * kS + 2 + a); };
     const uint32_t drained = bar0 + 8 * (2 * kS + 4);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = int(cluster_rank()), tile = int(blockIdx.x) / parts;
-    const int n_tiles = (g.n + kSplitN - 1) / kSplitN, mt = tile / n_tiles, nt = tile - mt * n_tiles;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = int(cluster_rank()), number = int(blockIdx.x) / parts;
+    const int which = number >= all.tiles[0], tile = number - (which ? all.tiles[0] : 0);
+    const ProductArgs& g = all.p[which].g;
+    const Maps& maps = all.p[which].maps;
+    const int n_tiles = g.n_tiles, mt = tile / n_tiles, nt = tile - mt * n_tiles;
     const int total_steps = g.k_tiles * g.passes, from = int(int64_t(total_steps) * rank / parts), to = int(int64_t(total_steps) * (rank + 1) / parts);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kS; ++s) { bar_init(full(s), 1); bar_init(empty(s), 1); }
@@ -638,14 +714,38 @@ struct SlopeArgs {
     int n;
 };
 
+// a thread's 8 of 256 columns: neighbours (kWide), or 32 apart
 template <bool kWide>
-__device__ __forceinline__ void load8(const char* row, int col, int n, float (&x)[8]) {
+__device__ __forceinline__ int slope_column(int lane, int j) { return kWide ? lane * 8 + j : j * 32 + lane; }
+template <bool kWide>
+__device__ __forceinline__ void load8(const char* row, int base, int lane, int n, float (&x)[8]) {
     if constexpr (kWide) {
-        unpack8(ld_stream_u4(row + 2 * int64_t(col)), x);
+        unpack8(ld_stream_u4(row + 2 * int64_t(base + lane * 8)), x);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = col + j < n ? bf16_bits_to_float(reinterpret_cast<const uint16_t*>(row)[col + j]) : 0.f;
+        for (int j = 0; j < 8; ++j) {
+            const int c = base + slope_column<false>(lane, j);
+            x[j] = c < n ? bf16_bits_to_float(reinterpret_cast<const uint16_t*>(row)[c]) : 0.f;
+        }
     }
+}
+// as bf16 into a row, and what the rounding left into d
+template <bool kWide>
+__device__ __forceinline__ void store8(char* row, int base, int lane, int n, float (&d)[8]) {
+    const uint4 w = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
+    float h[8];
+    unpack8(w, h);
+    if constexpr (kWide) {
+        *reinterpret_cast<uint4*>(row + 2 * int64_t(base + lane * 8)) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = base + slope_column<false>(lane, j);
+            if (c < n) reinterpret_cast<uint16_t*>(row)[c] = uint16_t(__float_as_uint(h[j]) >> 16);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d[j] -= h[j];
 }
 
 // kWide: n is a multiple of 8, and the rows of dout and pre start on 16-byte boundaries.
@@ -653,41 +753,31 @@ template <int kAct, bool kWide>
 __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
     constexpr bool kPre = kAct != BAOC_ACT_NONE;
     __shared__ float sh[8][256];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = int(blockIdx.x) * 256 + lane * 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, base = int(blockIdx.x) * 256;
     const int64_t first = int64_t(blockIdx.y) * g.rows_per_part, end = min64(g.rows, first + g.rows_per_part);
     float sum[8] = {};
     begin_in_row();
     auto one_row = [&](int64_t row, float (&d)[8], const float (&z)[8]) {
         if constexpr (kPre) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] *= act_slope<kAct>(z[j]);
+            for (int j = 0; j < 8; j += 2) unpack2(mul2(pack2(d[j], d[j + 1]), act_slope<kAct>(pack2(z[j], z[j + 1]))), d[j], d[j + 1]);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += d[j];
         if (!g.dz) return;
-        const uint4 w = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
-        const int64_t at = row * g.dz_step + 2 * int64_t(col);
-        *reinterpret_cast<uint4*>(g.dz + at) = w;
+        store8<kWide>(g.dz + row * g.dz_step, base, lane, g.n, d);
         if (!kPre || !g.dz_mid) return;
-        float h[8];
-        unpack8(w, h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] -= h[j];
-        const uint4 m = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
-        *reinterpret_cast<uint4*>(g.dz_mid + at) = m;
-        unpack8(m, h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] -= h[j];
-        *reinterpret_cast<uint4*>(g.dz_low + at) = make_uint4(pair_bf16(d[0], d[1]), pair_bf16(d[2], d[3]), pair_bf16(d[4], d[5]), pair_bf16(d[6], d[7]));
+        store8<kWide>(g.dz_mid + row * g.dz_step, base, lane, g.n, d);
+        store8<kWide>(g.dz_low + row * g.dz_step, base, lane, g.n, d);
     };
-    if (col < g.n)
+    if (base + slope_column<kWide>(lane, 0) < g.n)
         for (int64_t row = first + warp; row < end; row += 8 * kSlopeRows) {
             float d[kSlopeRows][8], z[kPre ? kSlopeRows : 1][8];
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r) {
                 const int64_t at = min64(row + 8 * r, end - 1);          // (a row too many is read, not used)
-                load8<kWide>(g.dout + at * g.dout_step, col, g.n, d[r]);
-                if constexpr (kPre) load8<kWide>(g.pre + at * g.pre_step, col, g.n, z[r]);
+                load8<kWide>(g.dout + at * g.dout_step, base, lane, g.n, d[r]);
+                if constexpr (kPre) load8<kWide>(g.pre + at * g.pre_step, base, lane, g.n, z[r]);
             }
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r)
@@ -695,9 +785,9 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
         }
     if (!g.part) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sh[warp][lane * 8 + j] = sum[j];
+    for (int j = 0; j < 8; ++j) sh[warp][slope_column<kWide>(lane, j)] = sum[j];
     __syncthreads();
-    const int c = int(blockIdx.x) * 256 + int(threadIdx.x);
+    const int c = base + int(threadIdx.x);
     if (c < g.n) {
         float s = sh[0][threadIdx.x];
         for (int w = 1; w < 8; ++w) s += sh[w][threadIdx.x];
@@ -799,67 +889,116 @@ bool encode(CUtensorMap* map, const Matrix& t, int box_rows, int box_cols = 64) 
 // A product's operands: a as [m][k] or, a_mn, as [k][m]; b as [n][k] or [k][n]; up to three pairs whose products are added.
 struct Operands { const Matrix *a[3], *b[3]; };
 
+// A product to be formed: sizes, flags and the epilogue in g, where it goes in out and pre.
+struct Product {
+    Operands o;
+    Matrix out, pre;
+    ProductArgs g;
+    int64_t tiles(int m, int n) const { return ceil_div(g.m, m) * ceil_div(g.n, n); }
+    int64_t steps() const { return int64_t(g.k_tiles) * g.passes; }
+};
+
+// A product as a kernel with tiles of m x n takes it (b_rows: of a CTA's copy of B).
+int fill_problem(const Product& d, int m, int n, int b_rows, bool stores, Problem* p, int* tiles) {
+    p->g = d.g;
+    p->g.m_tiles = int(ceil_div(d.g.m, m));
+    p->g.n_tiles = int(ceil_div(d.g.n, n));
+    const int64_t t = d.tiles(m, n);
+    if (t > 0x7fffffff / 4) return fail_linear(BAOC_E_INVALID, "too many tiles for one launch");
+    *tiles = int(t);
+    bool ok = true;
+    for (int i = 0; i < d.g.passes; ++i) ok = ok && encode(&p->maps.a[i], *d.o.a[i], d.g.a_mn ? kTileK : d.g.a_rows) && encode(&p->maps.b[i], *d.o.b[i], d.g.b_mn ? kTileK : b_rows);
+    if (stores && d.g.out_wide) ok = ok && encode(&p->maps.out, d.out, 32, 32);
+    if (stores && d.g.pre && d.g.pre_wide) ok = ok && encode(&p->maps.pre, d.pre, 32, 32);
+    return ok ? BAOC_OK : fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
+}
+
+// The permission for large shared memory is per kernel and device and lasts.
+template <typename K>
+int allow_shared(K kernel, int bytes, std::atomic<uint64_t>* allowed) {
+    int dev = 0;
+    cudaError_t ce = cudaGetDevice(&dev);
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (ce == cudaSuccess && !(allowed->load(std::memory_order_relaxed) & bit)) {
+        ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (ce == cudaSuccess) allowed->fetch_or(bit, std::memory_order_relaxed);
+    }
+    return launched(ce, "product_kernel");
+}
+
 template <int kCtas, int kN, bool kChunked>
-int launch_product(const Operands& o, const Matrix& out, const Matrix& pre, const ProductArgs& g, cudaStream_t s) {
+int launch_product(const Product* d, int count, cudaStream_t s) {
     using T = TileShape<kCtas, kN, kChunked>;
     static_assert(T::kStages >= 4 && T::kSmem <= 227 * 1024 - 512, "the ring, the outputs and the barriers share 227 KB");
     auto kernel = product_kernel<kCtas, kN, kChunked>;
-    static std::atomic<uint64_t> allowed{0};         // the permission for large shared memory is per device and lasts
-    int dev = 0;
-    cudaError_t ce = cudaGetDevice(&dev);
-    if (ce != cudaSuccess) return launched(ce, "product_kernel");
-    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
-        if (ce != cudaSuccess) return launched(ce, "product_kernel");
-        allowed.fetch_or(bit, std::memory_order_relaxed);
-    }
-    Maps maps;
-    bool ok = true;
-    for (int i = 0; i < g.passes; ++i) ok = ok && encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : g.a_rows) && encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : T::kBRows);
-    if (g.out_wide) ok = ok && encode(&maps.out, out, 32, 32);
-    if (g.pre && g.pre_wide) ok = ok && encode(&maps.pre, pre, 32, 32);
-    if (!ok) return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
-    const int64_t tiles = ceil_div(g.m, kTileM * kCtas) * ceil_div(g.n, kN);
-    if (tiles > 0x7fffffff - 148) return fail_linear(BAOC_E_INVALID, "too many tiles for one launch");
-    return launched(launch_in_row(kernel, dim3(unsigned(std::min<int64_t>(tiles, 148 / kCtas) * kCtas)), kProductThreads, T::kSmem, kCtas, s, maps, g), "product_kernel");
-}
-
-int launch_split(const Operands& o, const ProductArgs& g, int64_t tiles, int parts, cudaStream_t s) {
     static std::atomic<uint64_t> allowed{0};
-    int dev = 0;
-    cudaError_t ce = cudaGetDevice(&dev);
-    if (ce != cudaSuccess) return launched(ce, "product_split_kernel");
-    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        ce = cudaFuncSetAttribute(product_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
-        if (ce != cudaSuccess) return launched(ce, "product_split_kernel");
-        allowed.fetch_or(bit, std::memory_order_relaxed);
+    int rc = allow_shared(kernel, T::kSmem, &allowed);
+    Problems all;
+    all.tiles[1] = all.fewer = 0;
+    for (int i = 0; i < count && !rc; ++i) rc = fill_problem(d[i], kTileM * kCtas, kN, T::kBRows, true, &all.p[i], &all.tiles[i]);
+    if (rc) return rc;
+    const int workers = int(std::min<int64_t>(int64_t(all.tiles[0]) + all.tiles[1], 148 / kCtas));
+    if (count == 2) {                                // the share of the second that ends soonest (see Walk)
+        const int64_t longer = all.tiles[0] % workers, rounds = all.tiles[0] / workers, s0 = d[0].steps(), s1 = d[1].steps();
+        int64_t best = -1;
+        for (int q = 0; q <= ceil_div(all.tiles[1], workers); ++q) {
+            const int64_t rest = std::max<int64_t>(0, all.tiles[1] - int64_t(q) * workers);
+            const int64_t end = std::max((rounds + (longer > 0)) * s0 + q * s1, rounds * s0 + (q + ceil_div(rest, workers - longer)) * s1);
+            if (best < 0 || end < best) { best = end; all.fewer = q; }
+        }
     }
-    Maps maps;
-    for (int i = 0; i < g.passes; ++i)
-        if (!encode(&maps.a[i], *o.a[i], g.a_mn ? kTileK : g.a_rows) || !encode(&maps.b[i], *o.b[i], g.b_mn ? kTileK : kSplitN))
-            return fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
-    return launched(launch_in_row(product_split_kernel, dim3(unsigned(tiles * parts)), kSplitThreads, kSplitSmem, unsigned(parts), s, maps, g, parts), "product_split_kernel");
+    return launched(launch_in_row(kernel, dim3(unsigned(workers * kCtas)), kProductThreads, T::kSmem, kCtas, s, all), "product_kernel");
 }
 
-// The largest tiles that still give every CTA one; where the smallest do not, the sum over k is split among two CTAs per SM, at
-// least four steps each.  g has its sizes and flags, out and pre are where it goes.
-int form_product(const Operands& o, const Matrix& out, const Matrix& pre, ProductArgs g, cudaStream_t s) {
-    g.out = const_cast<char*>(out.p); g.out_step = out.step; g.out_f32 = out.eb == 4; g.out_wide = out.wide();
-    g.pre = const_cast<char*>(pre.p); g.pre_step = pre.step; g.pre_wide = pre.wide();
-    g.a_rows = g.a_mn ? kTileM : std::min(kTileM, int(round_up(g.m, 8)));
-    const int64_t pairs = ceil_div(g.m, 2 * kTileM), ones = ceil_div(g.m, kTileM), smallest = ones * ceil_div(g.n, kSplitN);
+int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
+    static std::atomic<uint64_t> allowed{0};
+    int rc = allow_shared(product_split_kernel, kSplitSmem, &allowed);
+    Problems all;
+    all.tiles[1] = all.fewer = 0;
+    for (int i = 0; i < count && !rc; ++i) rc = fill_problem(d[i], kTileM, kSplitN, kSplitN, false, &all.p[i], &all.tiles[i]);
+    if (rc) return rc;
+    return launched(launch_in_row(product_split_kernel, dim3(unsigned((all.tiles[0] + all.tiles[1]) * parts)), kSplitThreads, kSplitSmem, unsigned(parts), s, all, parts),
+                    "product_split_kernel");
+}
+
+// CTAs that share a tile's sum over k where the smallest tiles are few: `most` in all, four steps each at least.
+int parts_of(int64_t tiles, int64_t steps, int64_t most) {
     int parts = 1;
-    while (parts < kSplitMost && smallest * parts * 2 <= 2 * 148 && int64_t(g.k_tiles) * g.passes >= 8 * parts) parts *= 2;
-    if (parts > 1) return launch_split(o, g, smallest, parts, s);
-    if (g.out_f32) {
-        if (pairs * ceil_div(g.n, 128) >= 74) return launch_product<2, 128, true>(o, out, pre, g, s);
-        return launch_product<1, 64, true>(o, out, pre, g, s);
+    while (parts < kSplitMost && tiles * parts * 2 <= most && steps >= 8 * parts) parts *= 2;
+    return parts;
+}
+
+// Each product by the largest tiles that still give every CTA one; two of one kind in one launch.  split_most: CTAs (of which an
+// SM holds two) that one product's sums may be split among: by it, not by what else is formed, so that a product's bits do not
+// depend on that.
+int form_products(Product* d, int count, int split_most, cudaStream_t s) {
+    int parts[2];
+    enum Kind { kSplit, kPairs, kPairsChunked, kOnes128, kOnes64, kOnes64Chunked } kind[2];
+    for (int i = 0; i < count; ++i) {
+        ProductArgs& g = d[i].g;
+        g.out = const_cast<char*>(d[i].out.p); g.out_step = d[i].out.step; g.out_f32 = d[i].out.eb == 4; g.out_wide = d[i].out.wide();
+        g.pre = const_cast<char*>(d[i].pre.p); g.pre_step = d[i].pre.step; g.pre_wide = d[i].pre.wide();
+        g.a_rows = g.a_mn ? kTileM : std::min(kTileM, int(round_up(g.m, 8)));
+        parts[i] = parts_of(d[i].tiles(kTileM, kSplitN), d[i].steps(), split_most);
+        if (parts[i] > 1) kind[i] = kSplit;
+        else if (g.out_f32) kind[i] = d[i].tiles(2 * kTileM, 128) >= 74 ? kPairsChunked : kOnes64Chunked;
+        else if (d[i].tiles(2 * kTileM, 256) >= 74) kind[i] = kPairs;
+        else kind[i] = d[i].tiles(kTileM, 128) >= 148 ? kOnes128 : kOnes64;
     }
-    if (pairs * ceil_div(g.n, 256) >= 74) return launch_product<2, 256, false>(o, out, pre, g, s);
-    if (ones * ceil_div(g.n, 128) >= 148) return launch_product<1, 128, false>(o, out, pre, g, s);
-    return launch_product<1, 64, false>(o, out, pre, g, s);
+    const int step = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] ? 2 : 1;
+    for (int i = 0; i < count; i += step) {
+        int rc;
+        switch (kind[i]) {
+            case kSplit: rc = launch_split(d + i, step, parts[i], s); break;
+            case kPairs: rc = launch_product<2, 256, false>(d + i, step, s); break;
+            case kPairsChunked: rc = launch_product<2, 128, true>(d + i, step, s); break;
+            case kOnes128: rc = launch_product<1, 128, false>(d + i, step, s); break;
+            case kOnes64: rc = launch_product<1, 64, false>(d + i, step, s); break;
+            default: rc = launch_product<1, 64, true>(d + i, step, s); break;
+        }
+        if (rc) return rc;
+    }
+    return BAOC_OK;
 }
 
 // Matrices that a tiled copy cannot read go through the workspace: `at` is where the next one may lie.
@@ -970,12 +1109,13 @@ int baoc_linear(const baoc_linear_t* e, const void* x, const void* w, const floa
     const Matrix a = pack.operand(mx), b = pack.operand(mw);
     if (!pack.fits) return fail_linear(BAOC_E_WORKSPACE, "baoc_linear: workspace too small");
     if ((rc = pack.launch(s))) return rc;
-    ProductArgs g{};
+    Product d{Operands{{&a}, {&b}}, mo, mp, {}};
+    ProductArgs& g = d.g;
     g.m = int(tokens); g.n = e->n_out; g.k_tiles = int(ceil_div(e->n_in, kTileK)); g.passes = 1;
     g.b_mn = !out_in;
     g.act = e->act; g.bias = bias;
     g.residual = mr.p; g.residual_step = mr.step; g.residual_wide = mr.wide();
-    return form_product(Operands{{&a}, {&b}}, mo, mp, g, s);
+    return form_products(&d, 1, 2 * 148, s);
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
 }
@@ -1069,20 +1209,26 @@ int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const
                                                    int(e->n_out), static_cast<char*>(db), int(e->grad_dtype == BAOC_F32)), "slope_sums_kernel")))
             return rc;
     }
+    // (the longer sums first: what the second product's shorter ones leave uneven is less)
     const Matrix none(nullptr, 0, 0, 0, BAOC_BF16);
-    if (dx) {
-        ProductArgs p{};
-        p.m = int(tokens); p.n = e->n_in; p.k_tiles = int(ceil_div(e->n_out, kTileK)); p.passes = 1;
-        p.b_mn = out_in;
-        if ((rc = form_product(Operands{{&dz}, {&bw}}, mdx, none, p, s))) return rc;
-    }
+    Product d[2]{{{}, none, none, {}}, {{}, none, none, {}}};
+    int count = 0;
     if (dw) {
-        ProductArgs p{};
-        p.m = int(w_rows); p.n = int(w_cols); p.k_tiles = int(ceil_div(tokens, kTileK)); p.passes = split ? 3 : 1;
-        p.a_mn = p.b_mn = 1;
-        const Operands o = out_in ? Operands{{&dz, &mid, &low}, {&bx, &bx, &bx}} : Operands{{&bx, &bx, &bx}, {&dz, &mid, &low}};
-        if ((rc = form_product(o, mdw, none, p, s))) return rc;
+        Product& q = d[count++];
+        q.o = out_in ? Operands{{&dz, &mid, &low}, {&bx, &bx, &bx}} : Operands{{&bx, &bx, &bx}, {&dz, &mid, &low}};
+        q.out = mdw;
+        q.g.m = int(w_rows); q.g.n = int(w_cols); q.g.k_tiles = int(ceil_div(tokens, kTileK)); q.g.passes = split ? 3 : 1;
+        q.g.a_mn = q.g.b_mn = 1;
     }
+    if (dx) {
+        Product& q = d[count++];
+        q.o = Operands{{&dz}, {&bw}};
+        q.out = mdx;
+        q.g.m = int(tokens); q.g.n = e->n_in; q.g.k_tiles = int(ceil_div(e->n_out, kTileK)); q.g.passes = 1;
+        q.g.b_mn = out_in;
+    }
+    if (count == 2 && d[0].steps() < d[1].steps()) std::swap(d[0], d[1]);
+    if (count) return form_products(d, count, 148, s);
     return BAOC_OK;
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
