@@ -961,40 +961,62 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
                     "product_split_kernel");
 }
 
-// CTAs that share a tile's sum over k where the smallest tiles are few: `most` in all, four steps each at least.
-int parts_of(int64_t tiles, int64_t steps, int64_t most) {
-    int parts = 1;
-    while (parts < kSplitMost && tiles * parts * 2 <= most && steps >= 8 * parts) parts *= 2;
-    return parts;
+// The kernel for a product: the one that is expected to end first.  A step (64 k of a tile) takes the tensor cores 4 products'
+// time or the copies their bytes at 64 a clock and SM (what L2 gives one); steps follow one another in every CTA, rounds of tiles
+// too, and everything together takes at least the operands' bytes at 3400 a clock (HBM).  Measured against the largest tiles that
+// give every CTA one: FIGURES.
+enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit };
+struct Choice {
+    Kind kind;
+    int parts;
+};
+Choice choose(const Product& d, int split_most) {
+    const ProductArgs& g = d.g;
+    const int64_t steps = d.steps(), a_bytes = int64_t(g.a_rows) * kRowBytes, bytes = 2 * (int64_t(g.m) + g.n) * 64 * steps;
+    Choice best{kSplit, 0};
+    int64_t least = 0;
+    auto consider = [&](Kind kind, int parts, int64_t rounds, int64_t own_steps, int64_t step, int64_t fixed) {
+        const int64_t cost = std::max(rounds * own_steps * step, bytes / 3400) + fixed;
+        if (best.parts == 0 || cost < least) { best = Choice{kind, parts}; least = cost; }
+    };
+    auto whole = [&](Kind kind, int ctas, int n, int64_t products) {
+        consider(kind, 1, ceil_div(d.tiles(kTileM * ctas, n), 148 / ctas), steps, std::max(products, (a_bytes + n / ctas * kRowBytes) / 64), 3000);
+    };
+    if (!g.out_f32) whole(kPairs256, 2, 256, 512);
+    whole(kPairs128, 2, 128, 256);
+    if (!g.out_f32) whole(kOnes128, 1, 128, 256);
+    whole(kOnes64, 1, 64, 128);
+    const int64_t tiles = d.tiles(kTileM, kSplitN), step = std::max<int64_t>(128, (a_bytes + kSplitN * kRowBytes) / 64);
+    for (int parts = 2; parts <= kSplitMost && tiles * parts <= split_most && steps >= 4 * parts; parts *= 2)
+        consider(kSplit, parts, 1, ceil_div(steps, parts), tiles * parts > 148 ? 2 * step : step, 6000);
+    return best;
 }
 
-// Each product by the largest tiles that still give every CTA one; two of one kind in one launch.  split_most: CTAs (of which an
-// SM holds two) that one product's sums may be split among: by it, not by what else is formed, so that a product's bits do not
-// depend on that.
+// split_most: CTAs (of which an SM holds two) that one product's sums may be split among: by it, not by what else is formed, so
+// that a product's bits do not depend on that.
 int form_products(Product* d, int count, int split_most, cudaStream_t s) {
+    Kind kind[2];
     int parts[2];
-    enum Kind { kSplit, kPairs, kPairsChunked, kOnes128, kOnes64, kOnes64Chunked } kind[2];
     for (int i = 0; i < count; ++i) {
         ProductArgs& g = d[i].g;
         g.out = const_cast<char*>(d[i].out.p); g.out_step = d[i].out.step; g.out_f32 = d[i].out.eb == 4; g.out_wide = d[i].out.wide();
         g.pre = const_cast<char*>(d[i].pre.p); g.pre_step = d[i].pre.step; g.pre_wide = d[i].pre.wide();
         g.a_rows = g.a_mn ? kTileM : std::min(kTileM, int(round_up(g.m, 8)));
-        parts[i] = parts_of(d[i].tiles(kTileM, kSplitN), d[i].steps(), split_most);
-        if (parts[i] > 1) kind[i] = kSplit;
-        else if (g.out_f32) kind[i] = d[i].tiles(2 * kTileM, 128) >= 74 ? kPairsChunked : kOnes64Chunked;
-        else if (d[i].tiles(2 * kTileM, 256) >= 74) kind[i] = kPairs;
-        else kind[i] = d[i].tiles(kTileM, 128) >= 148 ? kOnes128 : kOnes64;
+        const Choice c = choose(d[i], split_most);
+        kind[i] = c.kind;
+        parts[i] = c.parts;
     }
-    const int step = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] ? 2 : 1;
+    // two of one kind in one launch (fp32 and bf16 outputs are two kinds but for split sums)
+    const bool alike = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] && (kind[0] == kSplit || d[0].g.out_f32 == d[1].g.out_f32);
+    const int step = alike ? 2 : 1;
     for (int i = 0; i < count; i += step) {
         int rc;
         switch (kind[i]) {
             case kSplit: rc = launch_split(d + i, step, parts[i], s); break;
-            case kPairs: rc = launch_product<2, 256, false>(d + i, step, s); break;
-            case kPairsChunked: rc = launch_product<2, 128, true>(d + i, step, s); break;
+            case kPairs256: rc = launch_product<2, 256, false>(d + i, step, s); break;
+            case kPairs128: rc = d[i].g.out_f32 ? launch_product<2, 128, true>(d + i, step, s) : launch_product<2, 128, false>(d + i, step, s); break;
             case kOnes128: rc = launch_product<1, 128, false>(d + i, step, s); break;
-            case kOnes64: rc = launch_product<1, 64, false>(d + i, step, s); break;
-            default: rc = launch_product<1, 64, true>(d + i, step, s); break;
+            default: rc = d[i].g.out_f32 ? launch_product<1, 64, true>(d + i, step, s) : launch_product<1, 64, false>(d + i, step, s); break;
         }
         if (rc) return rc;
     }
