@@ -388,6 +388,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     const uint32_t acc = acc_at;
 
     if (warp == 0 && lane == 0) {                     // copies: each CTA its own operands, a pair's bytes counted by its first CTA
+        const uint32_t first_full = kCtas == 2 ? at_rank(full(0), 0) : full(0);
         int s = 0, round = 0, issued = 0;
         bool ok = true;
         while (ok && walk.next(all, &tile)) {
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             for (int i = 0; i < steps; ++i) {
                 if (!(ok = bar_wait(empty(s), (round & 1) ^ 1))) break;
                 if (rank == 0) bar_expect(full(s), bytes);
-                const uint32_t bar = kCtas == 2 ? at_rank(full(s), 0) : full(s);
+                const uint32_t bar = first_full + 8 * s;
                 const int pass = (i >= k_tiles) + (i >= 2 * k_tiles), k = (i - pass * k_tiles) * kTileK;
                 const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
                 if (a_mn) {
@@ -426,12 +427,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
         }
     } else if (warp == 1 && lane == 0 && rank == 0) { // products
+        // (one thread issues them: what it computes per product is an addition to a descriptor)
+        const uint64_t first_a = operand_desc(ring, 64 * kRowBytes);
         int s = 0, round = 0, count = 0;
         bool ok = true;
         while (ok && walk.next(all, &tile)) {
             const ProductArgs& g = all.p[walk.problem].g;
             const uint32_t desc = product_desc(kTileM * kCtas, kN, g.a_mn, g.b_mn);
-            const uint32_t a_step = g.a_mn ? 16 * kRowBytes : 32, b_step = g.b_mn ? 16 * kRowBytes : 32;    // bytes per 16 k
+            const uint32_t a_step = (g.a_mn ? 16 * kRowBytes : 32) >> 4, b_step = (g.b_mn ? 16 * kRowBytes : 32) >> 4;    // per 16 k, in units of 16 bytes
             const int steps = g.k_tiles * g.passes, chunk = kChunked ? kChunk : steps;
             for (int first = 0; ok && first < steps; first += chunk, ++count) {
                 const int half = count & 1, last = min(steps, first + chunk);
@@ -440,11 +443,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 const uint32_t d = acc + half * kN;
                 for (int i = first; i < last; ++i) {
                     if (!(ok = bar_wait(full(s), round & 1))) break;
-                    acc_fence_after();
-                    const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
+                    const uint64_t a = first_a + uint32_t(s) * (T::kStage >> 4), b = a + (T::kABytes >> 4);
+                    product<kCtas>(d, a, b, desc, i > first);
 #pragma unroll
-                    for (int k = 0; k < kTileK / 16; ++k)
-                        product<kCtas>(d, operand_desc(a + k * a_step, 64 * kRowBytes), operand_desc(b + k * b_step, 64 * kRowBytes), desc, i > first || k > 0);
+                    for (uint32_t k = 1; k < kTileK / 16; ++k) product<kCtas>(d, a + k * a_step, b + k * b_step, desc, 1);
                     product_commit<kCtas>(empty(s));
                     if (++s == kS) { s = 0; ++round; }
                 }
@@ -590,7 +592,8 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
         }
     } else if (warp == 1 && lane == 0) {
         const uint32_t desc = product_desc(kTileM, kSplitN, g.a_mn, g.b_mn);
-        const uint32_t a_step = g.a_mn ? 16 * kRowBytes : 32, b_step = g.b_mn ? 16 * kRowBytes : 32;
+        const uint32_t a_step = (g.a_mn ? 16 * kRowBytes : 32) >> 4, b_step = (g.b_mn ? 16 * kRowBytes : 32) >> 4;
+        const uint64_t first_a = operand_desc(ring, 64 * kRowBytes);
         bool ok = true;
         for (int i = 0; ok && i < to - from; ++i) {
             const int s = i % kS, half = (i / kChunk) & 1;
@@ -599,11 +602,10 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
                 acc_fence_after();
             }
             if (!(ok = bar_wait(full(s), i / kS & 1))) break;
-            acc_fence_after();
-            const uint32_t a = ring + s * kSplitStage, b = a + kTileM * kRowBytes;
+            const uint64_t a = first_a + uint32_t(s) * (kSplitStage >> 4), b = a + (kTileM * kRowBytes >> 4);
+            product<1>(acc + half * kSplitN, a, b, desc, i % kChunk > 0);
 #pragma unroll
-            for (int k = 0; k < kTileK / 16; ++k)
-                product<1>(acc + half * kSplitN, operand_desc(a + k * a_step, 64 * kRowBytes), operand_desc(b + k * b_step, 64 * kRowBytes), desc, i % kChunk > 0 || k > 0);
+            for (uint32_t k = 1; k < kTileK / 16; ++k) product<1>(acc + half * kSplitN, a + k * a_step, b + k * b_step, desc, 1);
             product_commit<1>(empty(s));
             if (i % kChunk == kChunk - 1 || i == to - from - 1) product_commit<1>(acc_full(half));
         }
