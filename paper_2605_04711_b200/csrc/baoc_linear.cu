@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     auto acc_full = [&](int a) { return bar0 + 8 * (2 * kS + a); };
     auto acc_empty = [&](int a) { return bar0 + 8 * (2 * kS + 2 + a); };
     const uint32_t drained = bar0 + 8 * (2 * kS + 4);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = kCtas == 2 ? int(cluster_rank()) : 0;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31, rank = kCtas == 2 ? int(cluster_rank()) : 0;
     Walk walk(all, int(blockIdx.x) / kCtas, int(gridDim.x) / kCtas);
     int tile;
     if (threadIdx.x == 0) {
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     begin_in_row();
     const uint32_t acc = acc_at;
 
-    if (warp == 0 && lane == 0) {                     // copies: each CTA its own operands, a pair's bytes counted by its first CTA
+    if (warp == 0) {                                  // copies: each CTA its own operands, a pair's bytes counted by its first CTA
         const uint32_t first_full = kCtas == 2 ? at_rank(full(0), 0) : full(0);
         int s = 0, round = 0, issued = 0;
         bool ok = true;
@@ -399,23 +399,26 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const int m0 = (mt * kCtas + rank) * kTileM, n0 = nt * kN + rank * T::kBRows, k_tiles = g.k_tiles, steps = k_tiles * g.passes, a_mn = g.a_mn, b_mn = g.b_mn;
             const uint32_t bytes = (g.a_rows * kRowBytes + T::kBBytes) * kCtas;
             for (int i = 0; i < steps; ++i) {
-                if (!(ok = bar_wait(empty(s), (round & 1) ^ 1))) break;
-                if (rank == 0) bar_expect(full(s), bytes);
+                if (!(ok = warp_wait(empty(s), (round & 1) ^ 1))) break;
                 const uint32_t bar = first_full + 8 * s;
                 const int pass = (i >= k_tiles) + (i >= 2 * k_tiles), k = (i - pass * k_tiles) * kTileK;
                 const uint32_t a = ring + s * T::kStage, b = a + T::kABytes;
-                if (a_mn) {
+                if (elected()) {
+                    if (rank == 0) bar_expect(full(s), bytes);
+                    if (a_mn) {
 #pragma unroll
-                    for (int c = 0; c < kTileM / 64; ++c) copy_tile<kCtas>(a + c * 64 * kRowBytes, &maps.a[pass], m0 + c * 64, k, bar);
-                } else {
-                    copy_tile<kCtas>(a, &maps.a[pass], k, m0, bar);
-                }
-                if (b_mn) {
+                        for (int c = 0; c < kTileM / 64; ++c) copy_tile<kCtas>(a + c * 64 * kRowBytes, &maps.a[pass], m0 + c * 64, k, bar);
+                    } else {
+                        copy_tile<kCtas>(a, &maps.a[pass], k, m0, bar);
+                    }
+                    if (b_mn) {
 #pragma unroll
-                    for (int c = 0; c < T::kBRows / 64; ++c) copy_tile<kCtas>(b + c * 64 * kRowBytes, &maps.b[pass], n0 + c * 64, k, bar);
-                } else {
-                    copy_tile<kCtas>(b, &maps.b[pass], k, n0, bar);
+                        for (int c = 0; c < T::kBRows / 64; ++c) copy_tile<kCtas>(b + c * 64 * kRowBytes, &maps.b[pass], n0 + c * 64, k, bar);
+                    } else {
+                        copy_tile<kCtas>(b, &maps.b[pass], k, n0, bar);
+                    }
                 }
+                __syncwarp();
                 ++issued;
                 if (++s == kS) { s = 0; ++round; }
             }
@@ -426,8 +429,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             if (rank == 0)
                 for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) { // products
-        // (one thread issues them: what it computes per product is an addition to a descriptor)
+    } else if (warp == 1 && rank == 0) {              // products: what is computed for each is an addition to a descriptor
         const uint64_t first_a = operand_desc(ring, 64 * kRowBytes);
         int s = 0, round = 0, count = 0;
         bool ok = true;
@@ -438,24 +440,27 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const int steps = g.k_tiles * g.passes, chunk = kChunked ? kChunk : steps;
             for (int first = 0; ok && first < steps; first += chunk, ++count) {
                 const int half = count & 1, last = min(steps, first + chunk);
-                if (!(ok = bar_wait(acc_empty(half), ((count >> 1) & 1) ^ 1))) break;
+                if (!(ok = warp_wait(acc_empty(half), ((count >> 1) & 1) ^ 1))) break;
                 acc_fence_after();
                 const uint32_t d = acc + half * kN;
                 for (int i = first; i < last; ++i) {
-                    if (!(ok = bar_wait(full(s), round & 1))) break;
+                    if (!(ok = warp_wait(full(s), round & 1))) break;
                     const uint64_t a = first_a + uint32_t(s) * (T::kStage >> 4), b = a + (T::kABytes >> 4);
-                    product<kCtas>(d, a, b, desc, i > first);
+                    if (elected()) {
+                        product<kCtas>(d, a, b, desc, i > first);
 #pragma unroll
-                    for (uint32_t k = 1; k < kTileK / 16; ++k) product<kCtas>(d, a + k * a_step, b + k * b_step, desc, 1);
-                    product_commit<kCtas>(empty(s));
+                        for (uint32_t k = 1; k < kTileK / 16; ++k) product<kCtas>(d, a + k * a_step, b + k * b_step, desc, 1);
+                        product_commit<kCtas>(empty(s));
+                        if (i == last - 1) product_commit<kCtas>(acc_full(half));
+                    }
+                    __syncwarp();
                     if (++s == kS) { s = 0; ++round; }
                 }
-                product_commit<kCtas>(acc_full(half));
             }
         }
         if (!ok) {                                    // (products in flight read shared and write tensor memory)
             failed = 1;
-            product_commit<kCtas>(drained);
+            if (elected()) product_commit<kCtas>(drained);
             bar_wait(drained, 0);
         }
     } else if (warp >= 4) {                           // write out
@@ -473,7 +478,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             float total[kChunked ? kCols / 32 : 1][32];
             for (int c = 0; c < chunks; ++c, ++count) {
                 const int half = count & 1;
-                if (!(ok = bar_wait(acc_full(half), (count >> 1) & 1))) break;
+                if (!(ok = warp_wait(acc_full(half), (count >> 1) & 1))) break;
                 acc_fence_after();
                 const uint32_t at = acc + half * kN + (uint32_t(quarter * 32) << 16) + side * kCols;
                 if constexpr (kChunked) {
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
     auto acc_full = [&](int a) { return bar0 + 8 * (2 * kS + a); };
     auto acc_empty = [&](int a) { return bar0 + 8 * (2 * kS + 2 + a); };
     const uint32_t drained = bar0 + 8 * (2 * kS + 4);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = int(cluster_rank()), number = int(blockIdx.x) / parts;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31, rank = int(cluster_rank()), number = int(blockIdx.x) / parts;
     const int which = number >= all.tiles[0], tile = number - (which ? all.tiles[0] : 0);
     const ProductArgs& g = all.p[which].g;
     const Maps& maps = all.p[which].maps;
@@ -568,29 +573,32 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
     acc_fence_after();
     begin_in_row();
     const uint32_t acc = acc_at;
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         bool ok = true;
         int issued = 0;
         for (int i = from; i < to; ++i, ++issued) {
             const int s = issued % kS;
-            if (!(ok = bar_wait(empty(s), (issued / kS & 1) ^ 1))) break;
-            bar_expect(full(s), (g.a_rows + kSplitN) * kRowBytes);
+            if (!(ok = warp_wait(empty(s), (issued / kS & 1) ^ 1))) break;
             const int pass = (i >= g.k_tiles) + (i >= 2 * g.k_tiles), k = (i - pass * g.k_tiles) * kTileK;
             const uint32_t a = ring + s * kSplitStage, b = a + kTileM * kRowBytes;
-            if (g.a_mn) {
+            if (elected()) {
+                bar_expect(full(s), (g.a_rows + kSplitN) * kRowBytes);
+                if (g.a_mn) {
 #pragma unroll
-                for (int c = 0; c < kTileM / 64; ++c) copy_tile<1>(a + c * 64 * kRowBytes, &maps.a[pass], mt * kTileM + c * 64, k, full(s));
-            } else {
-                copy_tile<1>(a, &maps.a[pass], k, mt * kTileM, full(s));
+                    for (int c = 0; c < kTileM / 64; ++c) copy_tile<1>(a + c * 64 * kRowBytes, &maps.a[pass], mt * kTileM + c * 64, k, full(s));
+                } else {
+                    copy_tile<1>(a, &maps.a[pass], k, mt * kTileM, full(s));
+                }
+                if (g.b_mn) copy_tile<1>(b, &maps.b[pass], nt * kSplitN, k, full(s));
+                else copy_tile<1>(b, &maps.b[pass], k, nt * kSplitN, full(s));
             }
-            if (g.b_mn) copy_tile<1>(b, &maps.b[pass], nt * kSplitN, k, full(s));
-            else copy_tile<1>(b, &maps.b[pass], k, nt * kSplitN, full(s));
+            __syncwarp();
         }
         if (!ok) {
             failed = 1;
             for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         const uint32_t desc = product_desc(kTileM, kSplitN, g.a_mn, g.b_mn);
         const uint32_t a_step = (g.a_mn ? 16 * kRowBytes : 32) >> 4, b_step = (g.b_mn ? 16 * kRowBytes : 32) >> 4;
         const uint64_t first_a = operand_desc(ring, 64 * kRowBytes);
@@ -598,20 +606,23 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
         for (int i = 0; ok && i < to - from; ++i) {
             const int s = i % kS, half = (i / kChunk) & 1;
             if (i % kChunk == 0) {
-                if (!(ok = bar_wait(acc_empty(half), (i / kChunk >> 1 & 1) ^ 1))) break;
+                if (!(ok = warp_wait(acc_empty(half), (i / kChunk >> 1 & 1) ^ 1))) break;
                 acc_fence_after();
             }
-            if (!(ok = bar_wait(full(s), i / kS & 1))) break;
+            if (!(ok = warp_wait(full(s), i / kS & 1))) break;
             const uint64_t a = first_a + uint32_t(s) * (kSplitStage >> 4), b = a + (kTileM * kRowBytes >> 4);
-            product<1>(acc + half * kSplitN, a, b, desc, i % kChunk > 0);
+            if (elected()) {
+                product<1>(acc + half * kSplitN, a, b, desc, i % kChunk > 0);
 #pragma unroll
-            for (uint32_t k = 1; k < kTileK / 16; ++k) product<1>(acc + half * kSplitN, a + k * a_step, b + k * b_step, desc, 1);
-            product_commit<1>(empty(s));
-            if (i % kChunk == kChunk - 1 || i == to - from - 1) product_commit<1>(acc_full(half));
+                for (uint32_t k = 1; k < kTileK / 16; ++k) product<1>(acc + half * kSplitN, a + k * a_step, b + k * b_step, desc, 1);
+                product_commit<1>(empty(s));
+                if (i % kChunk == kChunk - 1 || i == to - from - 1) product_commit<1>(acc_full(half));
+            }
+            __syncwarp();
         }
         if (!ok) {
             failed = 1;
-            product_commit<1>(drained);
+            if (elected()) product_commit<1>(drained);
             bar_wait(drained, 0);
         }
     } else if (warp >= 4) {
@@ -619,7 +630,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
         float total[2][32];
         bool ok = true;
         for (int c = 0; c * kChunk < to - from; ++c) {
-            if (!(ok = bar_wait(acc_full(c & 1), c >> 1 & 1))) break;
+            if (!(ok = warp_wait(acc_full(c & 1), c >> 1 & 1))) break;
             acc_fence_after();
 #pragma unroll
             for (int p = 0; p < 2; ++p) {

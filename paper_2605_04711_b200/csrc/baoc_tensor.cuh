@@ -10,6 +10,17 @@
 
 namespace baoc {
 
+// One lane of a converged warp, the same at every call.  Copies and products are issued under it by a warp whose lanes all go
+// through the loop with the same values: the compiler then keeps descriptors and addresses in uniform registers, where these
+// instructions take them from.  (Under a test of the lane's number it moves them there for every instruction: a step of four
+// products took 530 clocks of its issuing thread, whatever the tile.)
+__device__ __forceinline__ bool elected() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one;
+}
+__device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0); }
+
 // ---- barriers --------------------------------------------------------------------
 // No wait is endless: one that takes longer than this reports false, and its caller gives the whole tile loop up.  (The longest
 // sum a CTA forms between two arrivals, 2^30 tokens, takes 3 s.)
@@ -58,6 +69,9 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     }
     return false;
 }
+
+// a whole warp's wait: its lanes agree
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
 
 // ---- tiled copies ----------------------------------------------------------------
 // x (elements of the contiguous dimension) is a multiple of 64 bf16 everywhere: copies start on 128-byte boundaries of a row.
