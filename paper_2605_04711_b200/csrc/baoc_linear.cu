@@ -193,63 +193,6 @@ __device__ __forceinline__ uint16_t one_bf16(float x) {
     return h;
 }
 
-// `count` of a row's 32 columns from column col on
-__device__ __forceinline__ void store_columns(char* row, int64_t col, int count, int f32, int wide, const float (&v)[32]) {
-    if (f32) {
-        float* p = reinterpret_cast<float*>(row) + col;
-        if (wide && count == 32) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < count) p[i] = v[i];
-        }
-    } else {
-        uint16_t* p = reinterpret_cast<uint16_t*>(row) + col;
-        if (wide && count == 32) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8)
-                *reinterpret_cast<uint4*>(p + i) = make_uint4(pair_bf16(v[i], v[i + 1]), pair_bf16(v[i + 2], v[i + 3]), pair_bf16(v[i + 4], v[i + 5]), pair_bf16(v[i + 6], v[i + 7]));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < count) p[i] = one_bf16(v[i]);
-        }
-    }
-}
-__device__ __forceinline__ void add_columns(const char* row, int64_t col, int count, int f32, int wide, float (&v)[32]) {
-    if (f32) {
-        const float* p = reinterpret_cast<const float*>(row) + col;
-        if (wide && count == 32) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const float4 a = *reinterpret_cast<const float4*>(p + i);
-                v[i] += a.x; v[i + 1] += a.y; v[i + 2] += a.z; v[i + 3] += a.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < count) v[i] += p[i];
-        }
-    } else {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + col;
-        if (wide && count == 32) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-                float x[8];
-                unpack8(*reinterpret_cast<const uint4*>(p + i), x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i + j] += x[j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < count) v[i] += bf16_bits_to_float(p[i]);
-        }
-    }
-}
-
 __device__ __forceinline__ void store4(char* row, int64_t col, int count, int f32, int wide, const float (&v)[4]) {
     if (f32) {
         float* p = reinterpret_cast<float*>(row) + col;
@@ -325,11 +268,69 @@ struct Writer {
         __syncwarp();
         if (lane == 0) store_tile(map, to, col, row0);
     }
+    // Arrays that no tiled copy fits (rows off the 16-byte grid): the warp's 32 x 32 values pass through both buffers, so that its
+    // lanes go along the columns of a row outside and along the rows inside.
+    __device__ __forceinline__ uint32_t cell(int row, int col) const { return buf + (row * 32 + (col ^ row)) * 4; }
+    __device__ __forceinline__ void store_rows(char* to, int64_t step, int f32, int64_t row0, int col, int left, const float (&v)[32]) {
+        if (lane == 0) stores_read<0>();
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 32; ++c) asm volatile("st.shared.f32 [%0], %1;" ::"r"(cell(lane, c)), "f"(v[c]) : "memory");
+        __syncwarp();
+        const int rows = int(min64(32, g.m - row0));
+        if (lane < left)
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r) {
+                if (r >= rows) break;
+                float x;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(cell(r, lane)) : "memory");
+                char* p = to + (row0 + r) * step;
+                if (f32) reinterpret_cast<float*>(p)[col + lane] = x;
+                else reinterpret_cast<uint16_t*>(p)[col + lane] = one_bf16(x);
+            }
+        __syncwarp();
+    }
+    __device__ __forceinline__ void add_rows(const char* from, int64_t step, int f32, int64_t row0, int col, int left, float (&v)[32]) {
+        if (lane == 0) stores_read<0>();
+        __syncwarp();
+        const int rows = int(min64(32, g.m - row0));
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) {
+            const char* p = from + (row0 + r) * step;
+            float x = 0.f;
+            if (r < rows && lane < left) x = f32 ? reinterpret_cast<const float*>(p)[col + lane] : bf16_bits_to_float(reinterpret_cast<const uint16_t*>(p)[col + lane]);
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(cell(r, lane)), "f"(x) : "memory");
+        }
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            float x;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(cell(lane, c)) : "memory");
+            v[c] += x;
+        }
+        __syncwarp();
+    }
+    // a thread's row of a residual on the 16-byte grid, all 32 columns there
+    __device__ __forceinline__ void add_wide(const char* p, int f32, float (&v)[32]) {
+        if (f32) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const float4 a = reinterpret_cast<const float4*>(p)[i / 4];
+                v[i] += a.x; v[i + 1] += a.y; v[i + 2] += a.z; v[i + 3] += a.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                float x[8];
+                unpack8(reinterpret_cast<const uint4*>(p)[i / 8], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i + j] += x[j];
+            }
+        }
+    }
     // row0: the warp's first row (below m); the whole warp calls it
     __device__ __forceinline__ void write(int64_t row0, int col, float (&v)[32]) {
         const int left = min(32, g.n - col);
-        const int64_t row = row0 + lane;
-        const bool mine = row < g.m;
         if (g.bias) {
             if (left == 32 && (reinterpret_cast<uintptr_t>(g.bias) & 15) == 0) {
 #pragma unroll
@@ -344,12 +345,16 @@ struct Writer {
         }
         if (g.pre) {
             if (g.pre_wide) send(&maps.pre, 0, col, int(row0), v);
-            else if (mine) store_columns(g.pre + row * g.pre_step, col, left, 0, 0, v);
+            else store_rows(g.pre, g.pre_step, 0, row0, col, left, v);
         }
         apply_act(v, g.act);
-        if (g.residual && mine) add_columns(g.residual + row * g.residual_step, col, left, g.out_f32, g.residual_wide, v);
+        if (g.residual) {
+            if (!g.residual_wide || left < 32) add_rows(g.residual, g.residual_step, g.out_f32, row0, col, left, v);
+            else if (row0 + lane < g.m) add_wide(g.residual + (row0 + lane) * g.residual_step + int64_t(col) * (g.out_f32 ? 4 : 2), g.out_f32, v);
+            __syncwarp();
+        }
         if (g.out_wide) send(&maps.out, g.out_f32, col, int(row0), v);
-        else if (mine) store_columns(g.out + row * g.out_step, col, left, g.out_f32, 0, v);
+        else store_rows(g.out, g.out_step, g.out_f32, row0, col, left, v);
         __syncwarp();
     }
 };
@@ -975,8 +980,9 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
 }
 
 // The kernel for a product: the one that is expected to end first.  A step (64 k of a tile) takes the tensor cores 4 products'
-// time or the copies their bytes at 64 a clock and SM (what L2 gives one); steps follow one another in every CTA, rounds of tiles
-// too, and everything together takes at least the operands' bytes at 3400 a clock (HBM).  Measured against the largest tiles that
+// time or the copies their bytes at 64 a clock and SM (what L2 gives one), and no less than a copy's way (2800 clocks) over the
+// stages in flight; steps follow one another in every CTA, rounds of tiles too, and everything together takes at least the
+// operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.  Measured against the largest tiles that
 // give every CTA one: FIGURES.
 enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit };
 struct Choice {
@@ -993,15 +999,15 @@ Choice choose(const Product& d, int split_most) {
         if (best.parts == 0 || cost < least) { best = Choice{kind, parts}; least = cost; }
     };
     auto whole = [&](Kind kind, int ctas, int n, int64_t products) {
-        consider(kind, 1, ceil_div(d.tiles(kTileM * ctas, n), 148 / ctas), steps, std::max(products, (a_bytes + n / ctas * kRowBytes) / 64), 3000);
+        consider(kind, 1, ceil_div(d.tiles(kTileM * ctas, n), 148 / ctas), steps, std::max<int64_t>({products, (a_bytes + n / ctas * kRowBytes) / 64, 2800 / 6}), 3000 + (g.out_wide ? 0 : 32 * n));
     };
     if (!g.out_f32) whole(kPairs256, 2, 256, 512);
     whole(kPairs128, 2, 128, 256);
     if (!g.out_f32) whole(kOnes128, 1, 128, 256);
     whole(kOnes64, 1, 64, 128);
-    const int64_t tiles = d.tiles(kTileM, kSplitN), step = std::max<int64_t>(128, (a_bytes + kSplitN * kRowBytes) / 64);
+    const int64_t tiles = d.tiles(kTileM, kSplitN), step = (a_bytes + kSplitN * kRowBytes) / 64;
     for (int parts = 2; parts <= kSplitMost && tiles * parts <= split_most && steps >= 4 * parts; parts *= 2)
-        consider(kSplit, parts, 1, ceil_div(steps, parts), tiles * parts > 148 ? 2 * step : step, 6000);
+        consider(kSplit, parts, 1, ceil_div(steps, parts), std::max<int64_t>(tiles * parts > 148 ? 2 * step : step, 2800 / kSplitStages), 6000);
     return best;
 }
 
