@@ -1,9 +1,10 @@
 """A bigram language model trained with the library's operators around its optimizer step.
 
 One token table (fp32 [vocab, dim]) and one output matrix (fp32 [dim, vocab]) are two blocks of a handle.  Every step looks
-the tokens up (``Embedding.lookup``), forms the logits and the gradients of the cross entropy with torch products, sums the
-table's gradient by token (``Embedding.grad``) into the block's bf16 array, clips all blocks by the global norm
-(``Baoc.clip_grads``) and hands them on: to the sampling window first, and after the allocation to the optimizer step.
+the tokens up (``Embedding.lookup``), forms the logits with a torch product, the log probabilities of the next tokens and the
+logits' gradient (``LogProbs.logprobs`` and ``LogProbs.grad``), sums the table's gradient by token (``Embedding.grad``) into the
+block's bf16 array, clips all blocks by the global norm (``Baoc.clip_grads``) and hands them on: to the sampling window first, and
+after the allocation to the optimizer step.
 
     python examples/bigram_lm.py [--steps 60]
 """
@@ -40,7 +41,7 @@ def train(steps: int = 60, window: int = 8, max_norm: float = 0.25, seed: int = 
     sess.init_params()
     table, weight = sess.param_views[0].view(VOCAB, DIM), sess.param_views[1].view(DIM, VOCAB)
     dtable, dweight = sess.grad_views[0][0].view(VOCAB, DIM), sess.grad_views[0][1].view(DIM, VOCAB)
-    embed = B.Embedding(VOCAB, DIM, scale=DIM ** 0.5, pad_id=PAD)
+    embed, answer = B.Embedding(VOCAB, DIM, scale=DIM ** 0.5, pad_id=PAD), B.LogProbs(VOCAB)
     gen = torch.Generator().manual_seed(seed)
     losses, norms = [], []
     for t in range(1 - window, steps + 1):
@@ -48,12 +49,11 @@ def train(steps: int = 60, window: int = 8, max_norm: float = 0.25, seed: int = 
         inputs, targets = ids[:, :-1], ids[:, 1:]
         kept = ((inputs != PAD) & (targets != PAD)).reshape(-1, 1)
         h = embed.lookup(table, inputs, out_dtype=torch.float32).view(-1, DIM)
-        logp = torch.log_softmax(h @ weight, -1)
-        count = kept.sum()
-        loss = -(logp.gather(1, targets.reshape(-1, 1)) * kept).sum() / count
-        dlogits = logp.exp()
-        dlogits.scatter_add_(1, targets.reshape(-1, 1), -torch.ones_like(kept, dtype=torch.float32))
-        dlogits *= kept / count
+        logits, count = h @ weight, kept.sum()
+        follow = torch.where(kept[:, 0], targets.reshape(-1), -1)          # -1: no answer is asked for
+        out = answer.logprobs(logits, follow)
+        loss = -out.logp.sum() / count
+        dlogits = answer.grad(logits, follow, out.stats, torch.where(kept[:, 0], -1.0 / count, 0.0), dlogits=logits)
         dweight.copy_(h.t() @ dlogits)
         embed.grad(inputs, (dlogits @ weight.t()).view(*inputs.shape, DIM), dtable)
         norm = sess.clip_grads(0, max_norm)[0]
