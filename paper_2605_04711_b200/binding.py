@@ -434,7 +434,7 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _form(*tensors):
     """All that a plan's checks of a call look at: equal forms need no second check (addresses are the library's to check)."""
-    return [t if t is None else (t.shape, t.stride(), t.dtype, t.get_device(), t.requires_grad) for t in tensors]
+    return [t if t is None else (t.shape, t.is_contiguous() or t.stride(), t.dtype, t.get_device(), t.requires_grad) for t in tensors]
 
 
 def _no_autograd(what: str, name: str, t: Optional[torch.Tensor]):

@@ -228,6 +228,29 @@ __device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[kPer], int ne
     return t;
 }
 
+// The same by taking the largest `need` times: a maximum and a ballot each, against 16 or 32 steps of a sum each above.
+constexpr int kTopByMaxima = 8;
+template <int kPer>
+__device__ __forceinline__ uint32_t reached_by_maxima(uint32_t (&v)[kPer], int need) {
+    const int lane = threadIdx.x & 31;
+    for (;;) {
+        uint32_t own = v[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) own = max(own, v[i]);
+        const uint32_t most = __reduce_max_sync(0xffffffffu, own);
+        if (--need == 0 || most == 0) return most;
+        if (lane == __ffs(int(__ballot_sync(0xffffffffu, own == most))) - 1) {       // one of the largest goes
+            bool gone = false;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (!gone && v[i] == most) {
+                    v[i] = 0;
+                    gone = true;
+                }
+        }
+    }
+}
+
 // The most probable tokens of a CTA's share of a row, in two looks.  Every thread knows its largest logit from the sums' pass.
 // The `top` groups of threads with the largest ones hold `top` tokens at least as large as the last of those, so all tokens
 // looked for reach it: only threads whose largest does are looked through again (a few in the hundred, from L2, or from
@@ -385,7 +408,7 @@ struct TopFinder {
             uint32_t v[kGroups / 32];
 #pragma unroll
             for (int i = 0; i < kGroups / 32; ++i) v[i] = sh->first[i * 32 + lane];
-            const uint32_t last = reached_by(v, top, Logits<DT>::kKeyBit);
+            const uint32_t last = top <= kTopByMaxima ? reached_by_maxima(v, top) : reached_by(v, top, Logits<DT>::kKeyBit);
             if (lane == 0) sh->last = last;
         }
         __syncthreads();
