@@ -30,12 +30,14 @@ constexpr int kProductThreads = 128 + 32 * kWriters;
 constexpr int kBand = 16;                            // tiles along m that are worked on side by side: their operands stay in L2
 constexpr int kSmemMost = 226 * 1024;                // shared memory of a CTA: the ring of stages, outputs on their way
 constexpr int kChunk = 8;                            // steps of 64 k
+constexpr int kLongSum = 1024;                       // steps: positive sums of 65536 products are off by 3e-4, a tenth of half a bf16 step
 
 // kCtas CTAs (a pair shares the tensor cores' work on a tile of 256 rows: each holds its 128 rows of A, half the columns' rows
 // of B, and its rows' accumulators, so that a stage of both feeds twice the products of one CTA's).
-// kChunked, for fp32 outputs: the tensor cores cut an accumulator's low bits off at every addition (2^-25 of it on average, always
-// towards zero; at k = 8192 random products the result is off by 9e-6, at 16384 positive ones by 8e-5), so every
-// kChunk steps the sums so far are added up in registers, rounded to nearest, and the accumulator starts again (5e-7).
+// kChunked, for fp32 outputs and for sums over more than kLongSum steps: the tensor cores cut an accumulator's low bits off at
+// every addition (2^-25 of it on average, always towards zero; at k = 8192 random products the result is off by 9e-6, at 16384
+// positive ones by 8e-5), so every kChunk steps the sums so far are added up in registers, rounded to nearest, and the accumulator
+// starts again (5e-7).
 template <int kCtas, int kN, bool kChunked>
 struct TileShape {
     static constexpr int kBRows = kN / kCtas;
@@ -75,6 +77,7 @@ struct Problems {
     int tiles[2];
     int fewer;                       // tiles of the second that the workers take which have one more of the first's (see Walk)
 };
+static_assert(sizeof(Problems) <= 4096, "a kernel's parameters");
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float r;
@@ -914,6 +917,7 @@ struct Product {
     ProductArgs g;
     int64_t tiles(int m, int n) const { return ceil_div(g.m, m) * ceil_div(g.n, n); }
     int64_t steps() const { return int64_t(g.k_tiles) * g.passes; }
+    bool chunked() const { return out.eb == 4 || steps() > kLongSum; }
 };
 
 // A product as a kernel with tiles of m x n takes it (b_rows: of a CTA's copy of B).
@@ -982,8 +986,9 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
 // The kernel for a product: the one that is expected to end first.  A step (64 k of a tile) takes the tensor cores 4 products'
 // time or the copies their bytes at 64 a clock and SM (what L2 gives one), and no less than a copy's way (2800 clocks) over the
 // stages in flight; steps follow one another in every CTA, rounds of tiles too, and everything together takes at least the
-// operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.  Measured against the largest tiles that
-// give every CTA one: FIGURES.
+// operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.
+// Against the largest tiles that give every CTA one: 512 x 4096 into 4096 47 -> 20 us, the gradient of 4096 x 768 into 2304
+// 74 -> 39 us.
 enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit };
 struct Choice {
     Kind kind;
@@ -1001,9 +1006,9 @@ Choice choose(const Product& d, int split_most) {
     auto whole = [&](Kind kind, int ctas, int n, int64_t products) {
         consider(kind, 1, ceil_div(d.tiles(kTileM * ctas, n), 148 / ctas), steps, std::max<int64_t>({products, (a_bytes + n / ctas * kRowBytes) / 64, 2800 / 6}), 3000 + (g.out_wide ? 0 : 32 * n));
     };
-    if (!g.out_f32) whole(kPairs256, 2, 256, 512);
+    if (!d.chunked()) whole(kPairs256, 2, 256, 512);
     whole(kPairs128, 2, 128, 256);
-    if (!g.out_f32) whole(kOnes128, 1, 128, 256);
+    if (!d.chunked()) whole(kOnes128, 1, 128, 256);
     whole(kOnes64, 1, 64, 128);
     const int64_t tiles = d.tiles(kTileM, kSplitN), step = (a_bytes + kSplitN * kRowBytes) / 64;
     for (int parts = 2; parts <= kSplitMost && tiles * parts <= split_most && steps >= 4 * parts; parts *= 2)
@@ -1025,17 +1030,17 @@ int form_products(Product* d, int count, int split_most, cudaStream_t s) {
         kind[i] = c.kind;
         parts[i] = c.parts;
     }
-    // two of one kind in one launch (fp32 and bf16 outputs are two kinds but for split sums)
-    const bool alike = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] && (kind[0] == kSplit || d[0].g.out_f32 == d[1].g.out_f32);
+    // two of one kind in one launch (chunked and other sums are two kinds)
+    const bool alike = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] && (kind[0] == kSplit || d[0].chunked() == d[1].chunked());
     const int step = alike ? 2 : 1;
     for (int i = 0; i < count; i += step) {
         int rc;
         switch (kind[i]) {
             case kSplit: rc = launch_split(d + i, step, parts[i], s); break;
             case kPairs256: rc = launch_product<2, 256, false>(d + i, step, s); break;
-            case kPairs128: rc = d[i].g.out_f32 ? launch_product<2, 128, true>(d + i, step, s) : launch_product<2, 128, false>(d + i, step, s); break;
+            case kPairs128: rc = d[i].chunked() ? launch_product<2, 128, true>(d + i, step, s) : launch_product<2, 128, false>(d + i, step, s); break;
             case kOnes128: rc = launch_product<1, 128, false>(d + i, step, s); break;
-            default: rc = d[i].g.out_f32 ? launch_product<1, 64, true>(d + i, step, s) : launch_product<1, 64, false>(d + i, step, s); break;
+            default: rc = d[i].chunked() ? launch_product<1, 64, true>(d + i, step, s) : launch_product<1, 64, false>(d + i, step, s); break;
         }
         if (rc) return rc;
     }

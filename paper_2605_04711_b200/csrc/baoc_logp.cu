@@ -721,7 +721,8 @@ int launch_logp(const LogpArgs& a, int64_t n, cudaStream_t s) {
 }
 
 // Few rows: each is shared by a cluster.  Else one CTA a row, of fewer threads where rows are short: a CTA's barriers and the
-// search for the most probable tokens cost the same for any row (65536 x 1000 with five of them: FIGURE us with 256 threads).
+// search for the most probable tokens cost the same for any row (65536 x 1000 with five of them: 128 us with a warp each, 650 with 256 threads; 8192 x 50257, a third masked: 146 us with 128
+// threads, 165 with 256).
 template <int DT>
 int logp_of(const LogpArgs& a, int64_t n, cudaStream_t s) {
     int c = 1;

@@ -349,3 +349,22 @@ def test_refusals(B):
         with pytest.raises(B.BaocError):
             p.grad(y, c["f"], c["dh"], c["pre_w"], **kw)
     _check(B, d, True)                                                              # the plan's module works on
+
+
+def test_one_gate_for_more_rows_than_there_are(B):
+    """rows_per_gate at and beyond the number of rows, beyond 32 bits too, through the C entries."""
+    import ctypes as C
+    d = _data(6, 64, False, True, 1, F, BF)
+    p, c = B.Join(64), _dev(d)
+    y, h = p.join(c["x"], c["f"], c["pre_w"], **_vectors(c))
+    want = _run_grad(p, c, y)
+    for rpg in (6, 7, 1 << 31, 1 << 32, (1 << 63) - 1):
+        p._e.rows_per_gate = p._g.rows_per_gate = rpg
+        y2, h2, dx, df, dg = torch.empty_like(y), torch.empty_like(h), torch.empty_like(y), torch.empty_like(h), torch.empty(64, device=DEV)
+        ws = torch.empty(p.grad_workspace_bytes(6), dtype=torch.uint8, device=DEV)
+        q = lambda t: t.data_ptr()
+        p._g.grad_dtype = 1
+        assert B._lib.baoc_join(p._ref, q(c["x"]), q(c["f"]), q(c["post_w"]), None, q(c["gate"]), q(c["pre_w"]), None, 6, q(y2), q(h2), B._stream()) == 0
+        assert B._lib.baoc_join_grad(p._gref, q(y), q(c["f"]), q(c["dy"]), q(c["dh"]), q(c["post_w"]), None, q(c["gate"]), q(c["pre_w"]), 6, q(dx), q(df), None, None,
+                                     q(dg), None, None, q(ws), ws.numel(), B._stream()) == 0
+        assert torch.equal(y2, y) and torch.equal(h2, h) and torch.equal(dx, want["dx"]) and torch.equal(df, want["df"]) and torch.equal(dg, want["dgate"][0])

@@ -386,3 +386,26 @@ def test_refusals(B):
         with pytest.raises(B.BaocError):
             p.grad(**(dict(x=x, w=w, dout=dout, pre=pre) | kw))
     assert torch.equal(p.product(x, w), (x.double() @ w.double().t()).clamp(min=0).to(BF))
+
+
+@pytest.mark.parametrize("m,k,n", [(9, 16, 8), (130, 40, 24), (257, 8, 40), (40, 264, 8)])
+def test_narrow_outputs_on_the_grid(B, m, k, n):
+    """Fewer columns than an output copy's box, on the 16-byte grid, between guards."""
+    x, w = _ints((m, k), 1), _ints((n, k), 2)
+    want = x.double() @ w.double().t()
+    for dtype in (BF, F):
+        wide = torch.full((m + 2, n + 16), 7.0, dtype=dtype, device=DEV)
+        B.Linear(k, n).product(x, w, out=wide[1:m + 1, :n])
+        assert torch.equal(wide[1:m + 1, :n], want.to(dtype)) and bool((wide[:, n:] == 7).all()) and bool((wide[0] == 7).all()) and bool((wide[m + 1] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_long_sums_keep_their_low_bits(B, dtype):
+    """131072 positive products: within a chunk of 512, 32 additions of 16 products cut at most 2^-23 each (2^-18 of the sum); 256
+    chunks are added up to nearest, 2^-24 each (2^-16): below 2^-15 in all.  (Additions cut throughout would lose 2^-12.)"""
+    m, k, n = 131072, 128, 192
+    x, d = _rand((m, k), 1).abs() + 0.5, _rand((m, n), 2).abs() + 0.5
+    dw = torch.empty((n, k), dtype=dtype, device=DEV)
+    B.Linear(k, n).grad(x, None, d, dw=dw)
+    want = d.double().t() @ x.double()
+    _within(dw, want, want * 2.0 ** -15)

@@ -73,3 +73,10 @@ def test_plans():
     for kw in (dict(dim=0), dict(dim=8193), dict(dim=8, kind="batch"), dict(dim=8, eps=0.0), dict(dim=8, scale=float("inf"))):
         with pytest.raises(B.BaocError):
             B.Join(**kw)
+
+
+def test_groups_longer_than_the_rows():
+    """A gate for more rows than there are, however many, is one gate: the descriptor is taken."""
+    n = C.c_size_t()
+    for rows_per_gate in (4, 5, 1 << 31, 1 << 32, (1 << 63) - 1):
+        assert B._lib.baoc_join_grad_workspace_bytes(C.byref(_e(rows_per_gate=rows_per_gate)), 4, C.byref(n)) == B.OK
