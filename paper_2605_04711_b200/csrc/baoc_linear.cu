@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             turn = writer.turn;
         }
         if (!ok) failed = 1;
-        if (lane == 0) stores_read<0>();
+        if (lane == 0) stores_done();
     }
     __syncwarp();
     acc_fence_before();

@@ -253,7 +253,7 @@ __device__ __forceinline__ uint32_t reached_by_maxima(uint32_t (&v)[kPer], int n
 
 // The most probable tokens of a CTA's share of a row, in two looks.  Every thread knows its largest logit from the sums' pass.
 // The `top` groups of threads with the largest ones hold `top` tokens at least as large as the last of those, so all tokens
-// looked for reach it: only threads whose largest does are looked through again (a few in the hundred, from L2, or from
+// looked for reach it: only the batches whose largest does are looked through again (a few in the hundred, from L2, or from
 // registers where a thread had one batch), and what reaches it is ranked.  Where that is more than shared memory holds (many equal
 // logits, or a few threads with most of the large ones), the threads' largest are told apart by their tokens, and then the tokens
 // themselves are counted bit by bit.  Order: larger logit, then lower token; a token and its logit make one 64-bit key.
