@@ -408,14 +408,16 @@ template <int S, int B, bool kLayer, int kClass, bool kWide>
 __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, class_grad_warps(kClass))) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
     constexpr bool kSolo = solo(kClass);
     constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass), kSums = kLayer ? 5 : 3;
-    constexpr bool kShared = kSolo || kClass == 6;   // the sums lie in shared memory: the registers have a row, or are few
+    // The sums lie in shared memory where the registers have a row of several chunks, or are few (65536 x 512 with a gate: 110 us, in
+    // registers 122), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
+    constexpr bool kShared = kClass == 2 || kClass == 3 || kClass == 6;
     constexpr bool kAhead = kClass == 4 || kClass == 5;      // the next row is fetched into registers,
     constexpr bool kStaged = kSolo && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)
     constexpr bool kKeep = kClass != 6;              // (there shared memory has no room for the vectors beside the sums)
     constexpr int kVectors = kLayer ? 4 : 3;         // kept ones, the gate (of a segment) among them
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;
-    extern __shared__ float4 dynamic4[];             // kKeep: the vectors; kShared: [team][sum][2][team's threads]; kStaged: a row per team
+    extern __shared__ float4 dynamic4[];             // kKeep: the vectors; the sums, [team][sum][2][team's threads]; kStaged: a row per team
     __shared__ float4 buf[kSolo ? 1 : 2][32];
     TeamSum<kClass> sum{buf};
     begin_in_row();
@@ -458,11 +460,22 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             }
         }
     };
-    // the sum k of all teams to f(column, value), each column by one thread; all threads call it
+    // The sum k of all teams to f(column, value), each column by one thread: behind a barrier that follows what the teams have
+    // added, and publish(k) of sums in registers.
+    auto publish = [&](auto which) {
+        if constexpr (kSolo && !kShared) {
+            constexpr int k = decltype(which)::value;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
+            float4* p = sums + (team * kSums + k) * 2 * size + t;
+            p[0] = make_float4(v[0], v[1], v[2], v[3]);
+            p[size] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+    };
     auto hand_out = [&](auto which, auto f) {
         constexpr int k = decltype(which)::value;
         if constexpr (kSolo) {
-            __syncthreads();
             for (int i = int(threadIdx.x); i < 2 * size; i += int(blockDim.x)) {
                 float4 v = sums[k * 2 * size + i];
                 for (int o = 1; o < kTeams; ++o) {
@@ -475,7 +488,6 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                 for (int e = 0; e < 4; ++e)
                     if (Stream::column(of, j + e) < dim) f(Stream::column(of, j + e), x[e]);
             }
-            __syncthreads();
         } else {
             float v[8];
             if constexpr (kShared) {
@@ -688,14 +700,25 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
         if (g.rows_per_gate && g.out[kGate]) {
             const bool whole = group * g.rows_per_gate >= begin && min64(g.rows, (group + 1) * g.rows_per_gate) <= end;
             float* slot = part + int64_t(group == begin / g.rows_per_gate ? kGate : kJoinSums) * dim;
+            publish(std::integral_constant<int, kGate>{});
+            if (kSolo) __syncthreads();
             hand_out(std::integral_constant<int, kGate>{}, [&](int c, float v) {
                 if (whole) store_grad(g.out[kGate], g.grad_dtype, group * dim + c, v);
                 else slot[c] = v;
             });
+            if (kSolo) __syncthreads();
             zero(kGate);
         }
         seg = seg_end;
     }
+    publish(std::integral_constant<int, kPreW>{});
+    publish(std::integral_constant<int, kPostW>{});
+    publish(std::integral_constant<int, kGate>{});
+    if constexpr (kLayer) {
+        publish(std::integral_constant<int, kPreB>{});
+        publish(std::integral_constant<int, kPostB>{});
+    }
+    if (kSolo) __syncthreads();
     auto finish = [&](auto which) {
         constexpr int k = decltype(which)::value;
         if (g.out[k]) hand_out(which, [&](int c, float v) { part[int64_t(k) * dim + c] = v; });
