@@ -592,8 +592,8 @@ class Join:
             raise BaocError(E_INVALID, f"kind must be \"rms\" or \"layer\", not {kind!r}")
         self.dim, self.kind = int(dim), kind
         new = lambda: JoinForm(max(-1, min(self.dim, 2 ** 31 - 1)), 1 if kind == "layer" else 0, 0, 0, 0, float(eps), float(scale), 0, 0)
-        self._e, self._g = new(), new()                     # the descriptors of join and grad
-        self._ref, self._gref, self._n = C.byref(self._e), C.byref(self._g), C.c_size_t()
+        self._e, self._g, self._w = new(), new(), new()     # the descriptors of join, grad and the workspace's size
+        self._ref, self._gref, self._wref, self._n = C.byref(self._e), C.byref(self._g), C.byref(self._w), C.c_size_t()
         self._seen, self._gseen = None, None
         self.grad_workspace_bytes(0)                        # the descriptor's checks
 
@@ -622,8 +622,8 @@ class Join:
             _no_autograd(what, "the weights", t)
         e.rows_per_gate = 0
         if gate is not None:
-            gates = gate.numel() // dim
-            if gate.dtype != torch.float32 or gate.size(-1) != dim or not gate.is_contiguous() or gate.get_device() != dev or gates < 1 or n % gates:
+            gates = gate.numel() // dim                     # (no gates: no rows)
+            if gate.dtype != torch.float32 or gate.dim() < 1 or gate.size(-1) != dim or not gate.is_contiguous() or gate.get_device() != dev or n % max(gates, 1) or (n and not gates):
                 raise BaocError(E_INVALID, f"{what}: gate must be a contiguous float32 [{dim}] or [gates, {dim}] with equally many rows each, on the device of the others")
             _no_autograd(what, "the gate", gate)
             e.rows_per_gate = n // gates if gates > 1 else 0
@@ -651,7 +651,7 @@ class Join:
         return (y, h) if rc >= 0 else self._failed(rc)
 
     def grad_workspace_bytes(self, rows: int) -> int:
-        rc = _lib.baoc_join_grad_workspace_bytes(self._ref, int(rows), C.byref(self._n))
+        rc = _lib.baoc_join_grad_workspace_bytes(self._wref, int(rows), C.byref(self._n))
         return self._n.value if rc >= 0 else self._failed(rc)
 
     def grad(self, y: torch.Tensor, f: Optional[torch.Tensor], dh: torch.Tensor, pre_w: torch.Tensor, dy: Optional[torch.Tensor] = None,
@@ -688,6 +688,8 @@ class Join:
         rc = _queue(dev, _lib.baoc_join_grad, self._gref, y.data_ptr(), _ptr(f), _ptr(dy), dh.data_ptr(), _ptr(post_w), _ptr(post_b), _ptr(gate),
                     pre_w.data_ptr(), n, _ptr(dx), df.data_ptr(), _ptr(dpost_w), _ptr(dpost_b), _ptr(dgate), _ptr(dpre_w), _ptr(dpre_b),
                     ws.data_ptr(), ws.numel() * ws.element_size())
+        if n == 0 and rc >= 0 and dgate is not None:        # (without rows the library cannot tell how many gates there are)
+            dgate.zero_()
         return (dx, df) if rc >= 0 else self._failed(rc)
 
 
@@ -760,6 +762,8 @@ class LogProbs:
             rc = _queue(logits.get_device(), _lib.baoc_logp, self._ref, logits.data_ptr(), ids.data_ptr(), n, out.logp.data_ptr(), out.entropy.data_ptr(),
                         out.stats.data_ptr(), out.top_ids.data_ptr() if k else None, out.top_logp.data_ptr() if k else None)
             return out if rc >= 0 else self._failed(rc)
+        if out.logp is None or out.entropy is None or out.stats is None:
+            raise BaocError(E_INVALID, "logprobs: out must have logp, entropy and stats")
         if k and (out.top_ids is None or out.top_ids.dtype != torch.int32 or out.top_ids.numel() != n * k or not out.top_ids.is_contiguous()
                   or out.top_ids.get_device() != logits.get_device() or out.top_logp is None):
             raise BaocError(E_INVALID, "logprobs: top_ids must be a contiguous int32 array of `top` tokens per id on the logits' device")

@@ -368,3 +368,27 @@ def test_one_gate_for_more_rows_than_there_are(B):
         assert B._lib.baoc_join_grad(p._gref, q(y), q(c["f"]), q(c["dy"]), q(c["dh"]), q(c["post_w"]), None, q(c["gate"]), q(c["pre_w"]), 6, q(dx), q(df), None, None,
                                      q(dg), None, None, q(ws), ws.numel(), B._stream()) == 0
         assert torch.equal(y2, y) and torch.equal(h2, h) and torch.equal(dx, want["dx"]) and torch.equal(df, want["df"]) and torch.equal(dg, want["dgate"][0])
+
+
+@pytest.mark.parametrize("gates", [0, 3])
+def test_gates_without_rows(B, gates):
+    """An empty batch (no sequences, or sequences of no tokens): nothing to join, and every gate's gradient is zero."""
+    p, x, f, w = B.Join(40), torch.empty(0, 40, device=DEV), torch.empty(0, 40, dtype=BF, device=DEV), torch.ones(40, device=DEV)
+    gate, dgate, dw = torch.ones(gates, 40, device=DEV), torch.full((gates, 40), 7.0, dtype=BF, device=DEV), torch.full((40,), 7.0, dtype=BF, device=DEV)
+    y, h = p.join(x, f, w, gate=gate)
+    dx, df = p.grad(y, f, h, w, gate=gate, dgate=dgate, dpre_w=dw)
+    assert y.shape == h.shape == dx.shape == df.shape == (0, 40) and not dgate.any() and not dw.any()
+    with pytest.raises(B.BaocError):
+        p.join(torch.zeros(2, 40, device=DEV), torch.zeros(2, 40, dtype=BF, device=DEV), w, gate=torch.ones(0, 40, device=DEV))
+    with pytest.raises(B.BaocError):
+        p.join(x, f, w, gate=torch.ones((), device=DEV))
+
+
+def test_a_refused_join_leaves_the_gradient_alone(B):
+    """A form of the join that is refused (an fp32 branch on a bf16 stream) says nothing of the gradient's form."""
+    p, w = B.Join(32), torch.ones(32, device=DEV)
+    x, f = torch.ones(4, 32, dtype=BF, device=DEV), torch.ones(4, 32, dtype=BF, device=DEV)
+    with pytest.raises(B.BaocError, match="fp32 stream"):
+        p.join(x, f.float(), w)
+    dx, df = p.grad(x, None, f, w)
+    assert torch.isfinite(dx).all() and torch.equal(dx, df)

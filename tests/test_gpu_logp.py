@@ -285,3 +285,11 @@ def test_refusals(B):
     plan.grad(both[:, :10], ids, out.stats, torch.ones(4, device=dev), dlogits=both[:, 10:])
     empty = plan.logprobs(x[:0], ids[:0])
     assert empty.logp.numel() == 0 and plan.grad(x[:0], ids[:0], empty.stats, empty.logp).numel() == 0
+
+
+def test_outputs_that_are_not_there(B):
+    dev = "cuda:0"
+    x, ids, plan = torch.zeros((4, 10), device=dev), torch.zeros(4, dtype=torch.int64, device=dev), B.LogProbs(10)
+    for name in ("logp", "entropy", "stats"):
+        with pytest.raises(B.BaocError):
+            plan.logprobs(x, ids, out=plan.buffers(4, dev)._replace(**{name: None}))
