@@ -30,11 +30,14 @@ constexpr int64_t kJoinMaxStride = int64_t(1) << 28;
 constexpr int kJoinCols = 8;                   // columns of a thread
 constexpr int kSoloWarps = 4;                  // rows that a warp takes alone: so many warps per CTA
 constexpr int kJoinWarps = 32, kJoinGradWarps = 16;    // warps per SM of the other rows' kernels
+constexpr int kFewRows = 592;                  // few rows: up to 4 per SM
 constexpr int kJoinSums = 5;                   // column sums of the gradient: weight and bias of pre, of post, and the gate
 
 // How a row is spread.  Classes 1 to 3: one warp, each lane 1 to 3 times 8 columns (no barrier, and a sum's shuffles are paid
 // once a row: 65536 x 768 bf16 layer norms forwards 110 -> 73 us against three warps).  Classes 4, 5 and 6: a CTA of as many warps as the row
-// needs, up to 8, 16 and 32, 8 columns a thread (what differs is the registers that a thread may have).
+// needs, up to 8, 16 and 32, 8 columns a thread (what differs is the registers that a thread may have).  Few rows of 2 or 3 times
+// 256 columns are of class 4 too: with one row a warp at most there is nothing to pay shuffles for, and a lane's loads wait for one another
+// (one bf16 row of 768, layer norms: 4.9 -> 3.3 us, its gradient 8.3 -> 5.9, of 296 rows 10.8 -> 9.2; at 592 both ways take as long).
 __host__ __device__ constexpr bool solo(int c) { return c <= 3; }
 __host__ __device__ constexpr int chunks_of(int c) { return c <= 3 ? c : 1; }
 __host__ __device__ constexpr int class_threads(int c) { return c <= 3 ? 32 * kSoloWarps : (c == 4 ? 256 : (c == 5 ? 512 : 1024)); }
@@ -460,8 +463,9 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             }
         }
     };
-    // The sum k of all teams to f(column, value), each column by one thread: behind a barrier that follows what the teams have
-    // added, and publish(k) of sums in registers.
+    // The sum k of all teams to `to` (a vector of dim), each column by one thread: behind a barrier that follows what the teams have
+    // added, and publish(k) of sums in registers.  (Four neighbours in one access where that can be: one by one, a CTA's sums of
+    // 768 columns took as long as a row.)
     auto publish = [&](auto which) {
         if constexpr (kSolo && !kShared) {
             constexpr int k = decltype(which)::value;
@@ -473,7 +477,17 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             p[size] = make_float4(v[4], v[5], v[6], v[7]);
         }
     };
-    auto hand_out = [&](auto which, auto f) {
+    auto store4 = [&](char* to, int dtype, int of, int j, float4 v) {        // columns j to j + 3 of place `of`
+        if (kWide && dtype == BAOC_F32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+            if (Stream::column(of, j) < dim) *reinterpret_cast<float4*>(to + 4 * Stream::column(of, j)) = v;
+            return;
+        }
+        const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (Stream::column(of, j + i) < dim) store_grad(to, dtype, Stream::column(of, j + i), x[i]);
+    };
+    auto hand_out = [&](auto which, char* to, int dtype) {
         constexpr int k = decltype(which)::value;
         if constexpr (kSolo) {
             for (int i = int(threadIdx.x); i < 2 * size; i += int(blockDim.x)) {
@@ -482,24 +496,17 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                     const float4 w = sums[(o * kSums + k) * 2 * size + i];
                     v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
                 }
-                const int of = i % size, j = 4 * (i / size);
-                const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (Stream::column(of, j + e) < dim) f(Stream::column(of, j + e), x[e]);
+                store4(to, dtype, i % size, 4 * (i / size), v);
             }
+        } else if constexpr (kShared) {
+            store4(to, dtype, t, 0, sums[k * 2 * size + t]);
+            store4(to, dtype, t, 4, sums[(k * 2 + 1) * size + t]);
         } else {
             float v[8];
-            if constexpr (kShared) {
-                const float4 a = sums[k * 2 * size + t], b = sums[(k * 2 + 1) * size + t];
-                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-            } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (Stream::column(t, j) < dim) f(Stream::column(t, j), v[j]);
+            for (int j = 0; j < 4; ++j) unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
+            store4(to, dtype, t, 0, make_float4(v[0], v[1], v[2], v[3]));
+            store4(to, dtype, t, 4, make_float4(v[4], v[5], v[6], v[7]));
         }
     };
     auto in = [&](int c) { return !kWide || (t + 32 * c) * kJoinCols < dim; };
@@ -702,10 +709,8 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             float* slot = part + int64_t(group == begin / g.rows_per_gate ? kGate : kJoinSums) * dim;
             publish(std::integral_constant<int, kGate>{});
             if (kSolo) __syncthreads();
-            hand_out(std::integral_constant<int, kGate>{}, [&](int c, float v) {
-                if (whole) store_grad(g.out[kGate], g.grad_dtype, group * dim + c, v);
-                else slot[c] = v;
-            });
+            hand_out(std::integral_constant<int, kGate>{}, whole ? g.out[kGate] + group * dim * (g.grad_dtype == BAOC_F32 ? 4 : 2) : reinterpret_cast<char*>(slot),
+                     whole ? g.grad_dtype : int(BAOC_F32));
             if (kSolo) __syncthreads();
             zero(kGate);
         }
@@ -721,7 +726,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
     if (kSolo) __syncthreads();
     auto finish = [&](auto which) {
         constexpr int k = decltype(which)::value;
-        if (g.out[k]) hand_out(which, [&](int c, float v) { part[int64_t(k) * dim + c] = v; });
+        if (g.out[k]) hand_out(which, reinterpret_cast<char*>(part + int64_t(k) * dim), BAOC_F32);
     };
     finish(std::integral_constant<int, kPreW>{});
     finish(std::integral_constant<int, kPostW>{});
@@ -814,13 +819,18 @@ bool overlap(const Rows& a, const Rows& b, int64_t rows) {
 }
 bool same(const Rows& a, const Rows& b, int64_t rows) { return a.p == b.p && a.width == b.width && (a.step == b.step || rows == 1); }
 
-int class_of(int dim) {
-    const int w = int(ceil_div(dim, 32 * kJoinCols));
-    return w <= 3 ? w : (w <= 8 ? 4 : (w <= 16 ? 5 : 6));
-}
-int cta_of(int dim) { return solo(class_of(dim)) ? 32 * kSoloWarps : int(32 * ceil_div(dim, 32 * kJoinCols)); }
-int team_of(int dim) { return solo(class_of(dim)) ? 32 * class_of(dim) : cta_of(dim); }      // (see team_size)
-int rows_of(int dim) { return solo(class_of(dim)) ? kSoloWarps : 1; }                        // rows that a CTA works on at a time
+// How rows are spread over threads: their class, and what follows from it.
+struct Spread {
+    int c, cta, team, rows;         // class, threads of a CTA, columns' threads of a team (see team_size), rows that a CTA works on at a time
+    Spread(int dim, int64_t n_rows) {
+        const int w = int(ceil_div(dim, 32 * kJoinCols));
+        c = w == 1 || (w <= 3 && n_rows > kFewRows) ? w : (w <= 8 ? 4 : (w <= 16 ? 5 : 6));
+        cta = solo(c) ? 32 * kSoloWarps : 32 * w;
+        team = solo(c) ? 32 * c : cta;
+        rows = solo(c) ? kSoloWarps : 1;
+    }
+    int64_t at_once(int sm_warps) const { return int64_t(148) * std::max(1, sm_warps * 32 / cta); }     // CTAs that find room, sm_warps per SM
+};
 
 // f(class, wide) as constants.
 template <int kClass, typename F>
@@ -829,8 +839,8 @@ int with_width(bool wide, F f) {
     return wide ? f(c, std::true_type{}) : f(c, std::false_type{});
 }
 template <typename F>
-int with_class(int dim, bool wide, F f) {
-    switch (class_of(dim)) {
+int with_class(int c, bool wide, F f) {
+    switch (c) {
         case 1: return with_width<1>(wide, f);
         case 2: return with_width<2>(wide, f);
         case 3: return with_width<3>(wide, f);
@@ -847,18 +857,19 @@ int with_types(int stream, int branch, F f) {
                                : f(integral_constant<int, BAOC_F32>{}, integral_constant<int, BAOC_F32>{});
 }
 
-// CTAs of a kernel that find room at once, sm_warps per SM.
-int64_t ctas_at_once(int dim, int sm_warps) { return int64_t(148) * std::max(1, sm_warps * 32 / cta_of(dim)); }
-
 // The gradient's rows per CTA and CTAs: whole rounds of a CTA's teams, all CTAs at once.
-void grad_shape(int dim, int64_t rows, int64_t* per_cta, int* ctas) {
-    const int teams = rows_of(dim);
-    *per_cta = std::max<int64_t>(teams, round_up(ceil_div(rows, ctas_at_once(dim, class_grad_warps(class_of(dim)))), teams));
+void grad_shape(const Spread& d, int64_t rows, int64_t* per_cta, int* ctas) {
+    *per_cta = std::max<int64_t>(d.rows, round_up(ceil_div(rows, d.at_once(class_grad_warps(d.c))), d.rows));
     *ctas = int(ceil_div(rows, *per_cta));
 }
-// (By the most CTAs that so many rows or fewer can get: whole rounds leave fewer of them for some larger numbers of rows.)
+// (By the most CTAs that so many rows or fewer can get: whole rounds leave fewer of them for some larger numbers of rows, and few
+// rows are spread in another way.)
 int64_t grad_ws(int dim, int64_t rows) {
-    const int64_t ctas = std::min(ceil_div(rows, rows_of(dim)), ctas_at_once(dim, class_grad_warps(class_of(dim))));
+    int64_t ctas = 0;
+    for (int64_t n : {rows, std::min<int64_t>(rows, kFewRows)}) {
+        const Spread d(dim, n);
+        ctas = std::max(ctas, std::min(ceil_div(n, d.rows), d.at_once(class_grad_warps(d.c))));
+    }
     return std::max<int64_t>(256, round_up(ctas * (kJoinSums + 1) * dim * 4, 256));
 }
 
@@ -903,15 +914,16 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
                      rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate < rows ? e->rows_per_gate : 0, 0, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
-        return with_class(e->dim, wide, [&](auto C, auto W) {
-            const int cta = cta_of(e->dim), bytes = ((a.layer ? 4 : 2) + rows_of(e->dim)) * 8 * team_of(e->dim) * 4;
-            a.rows_per_cta = round_up(ceil_div(rows, ctas_at_once(e->dim, class_warps(C()))), rows_of(e->dim));      // all CTAs at once
+        const Spread d(e->dim, rows);
+        return with_class(d.c, wide, [&](auto C, auto W) {
+            const int bytes = ((a.layer ? 4 : 2) + d.rows) * 8 * d.team * 4;
+            a.rows_per_cta = round_up(ceil_div(rows, d.at_once(class_warps(C()))), d.rows);      // all CTAs at once
             auto kernel = join_kernel<S(), B(), C(), W()>;
             if (bytes > 40 * 1024) {             // (48 KB go without asking, the kernel's own arrays included)
                 const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
                 if (ce != cudaSuccess) return launched(ce, "join_kernel");
             }
-            return launched(launch_in_row(kernel, dim3(unsigned(ceil_div(rows, a.rows_per_cta))), unsigned(cta), size_t(bytes), 1, s, a), "join_kernel");
+            return launched(launch_in_row(kernel, dim3(unsigned(ceil_div(rows, a.rows_per_cta))), unsigned(d.cta), size_t(bytes), 1, s, a), "join_kernel");
         });
     });
 } catch (const std::bad_alloc&) {
@@ -967,23 +979,24 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
                    gate && e->rows_per_gate < rows ? e->rows_per_gate : 0, 0, e->dim, e->grad_dtype, e->scale, e->eps};
     for (int k = 0; k < kJoinSums; ++k) a.out[k] = static_cast<char*>(outs[k]);
     int ctas;
-    grad_shape(e->dim, std::max<int64_t>(rows, 1), &a.rows_per_cta, &ctas);
+    const Spread d(e->dim, rows);
+    grad_shape(d, std::max<int64_t>(rows, 1), &a.rows_per_cta, &ctas);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CheckCtx ck{static_cast<char*>(ws), static_cast<char*>(ws) + need, 0, 0, 0};
     (void)ck;
     if (rows) {
         rc = with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
-            return with_class(e->dim, wide, [&](auto C, auto W) {
+            return with_class(d.c, wide, [&](auto C, auto W) {
                 auto go = [&](auto L) {
-                    const int cta = cta_of(e->dim), teams = rows_of(e->dim), sums = solo(C()) || C() == 6 ? teams * (L() ? 5 : 3) : 0;
-                    const int staged = solo(C()) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? teams * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
-                    const int bytes = (sums + (C() == 6 ? 0 : (L() ? 4 : 3)) + staged) * 8 * team_of(e->dim) * 4;
+                    const int sums = solo(C()) || C() == 6 ? d.rows * (L() ? 5 : 3) : 0;
+                    const int staged = solo(C()) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? d.rows * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
+                    const int bytes = (sums + (C() == 6 ? 0 : (L() ? 4 : 3)) + staged) * 8 * d.team * 4;
                     auto kernel = join_grad_kernel<S(), B(), L(), C(), W()>;
                     if (bytes > 40 * 1024) {
                         const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
                         if (ce != cudaSuccess) return launched(ce, "join_grad_kernel");
                     }
-                    return launched(launch_in_row(kernel, dim3(unsigned(ctas)), unsigned(cta), size_t(bytes), 1, s, a BAOC_CHECK_ARG(ck)), "join_grad_kernel");
+                    return launched(launch_in_row(kernel, dim3(unsigned(ctas)), unsigned(d.cta), size_t(bytes), 1, s, a BAOC_CHECK_ARG(ck)), "join_grad_kernel");
                 };
                 return layer ? go(std::true_type{}) : go(std::false_type{});
             });

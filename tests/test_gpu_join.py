@@ -392,3 +392,10 @@ def test_a_refused_join_leaves_the_gradient_alone(B):
         p.join(x, f.float(), w)
     dx, df = p.grad(x, None, f, w)
     assert torch.isfinite(dx).all() and torch.equal(dx, df)
+
+
+@pytest.mark.parametrize("n,dim", [(592, 768), (593, 768), (594, 513), (1500, 300), (1201, 512), (700, 765), (2000, 600)])
+@pytest.mark.parametrize("stream,branch,layer,gates", [(F, BF, False, 1), (BF, BF, True, 1), (F, F, True, 1), (BF, BF, False, 0), (BF, BF, True, 2)])
+def test_more_than_a_few_rows(B, n, dim, stream, branch, layer, gates):
+    """Rows of 257 to 768 columns: from some number of them on, a warp takes one alone."""
+    _check(B, _data(n // max(gates, 1) * max(gates, 1), dim, layer, True, gates, stream, branch), layer, grad=F)

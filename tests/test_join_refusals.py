@@ -80,3 +80,13 @@ def test_groups_longer_than_the_rows():
     n = C.c_size_t()
     for rows_per_gate in (4, 5, 1 << 31, 1 << 32, (1 << 63) - 1):
         assert B._lib.baoc_join_grad_workspace_bytes(C.byref(_e(rows_per_gate=rows_per_gate)), 4, C.byref(n)) == B.OK
+
+
+@pytest.mark.parametrize("dim", [1, 200, 256, 257, 512, 513, 768, 769, 2048, 8192])
+def test_a_workspace_serves_fewer_rows(dim):
+    """The size never falls as rows rise (rows around every change of how they are spread)."""
+    n, last = C.c_size_t(), 0
+    for rows in [0, 1, 2, 3, 4, 5, 147, 148, 149, 295, 296, 297, 443, 444, 445, 591, 592, 593, 596, 597, 740, 888, 1184, 1185, 1776, 2368, 2369, 5000, 1 << 20, 1 << 31]:
+        assert B._lib.baoc_join_grad_workspace_bytes(C.byref(_e(dim=dim)), rows, C.byref(n)) == B.OK
+        assert n.value >= last
+        last = n.value
