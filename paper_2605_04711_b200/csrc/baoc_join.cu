@@ -819,12 +819,12 @@ bool overlap(const Rows& a, const Rows& b, int64_t rows) {
 }
 bool same(const Rows& a, const Rows& b, int64_t rows) { return a.p == b.p && a.width == b.width && (a.step == b.step || rows == 1); }
 
-// How rows are spread over threads: their class, and what follows from it.
+// How rows are spread over threads: their class, and what follows from it.  alone: a warp may take a row of 2 or 3 times 256 columns alone.
 struct Spread {
     int c, cta, team, rows;         // class, threads of a CTA, columns' threads of a team (see team_size), rows that a CTA works on at a time
-    Spread(int dim, int64_t n_rows) {
+    Spread(int dim, int64_t n_rows, bool alone) {
         const int w = int(ceil_div(dim, 32 * kJoinCols));
-        c = w == 1 || (w <= 3 && n_rows > kFewRows) ? w : (w <= 8 ? 4 : (w <= 16 ? 5 : 6));
+        c = w == 1 || (w <= 3 && alone && n_rows > kFewRows) ? w : (w <= 8 ? 4 : (w <= 16 ? 5 : 6));
         cta = solo(c) ? 32 * kSoloWarps : 32 * w;
         team = solo(c) ? 32 * c : cta;
         rows = solo(c) ? kSoloWarps : 1;
@@ -862,13 +862,16 @@ void grad_shape(const Spread& d, int64_t rows, int64_t* per_cta, int* ctas) {
     *per_cta = std::max<int64_t>(d.rows, round_up(ceil_div(rows, d.at_once(class_grad_warps(d.c))), d.rows));
     *ctas = int(ceil_div(rows, *per_cta));
 }
-// (By the most CTAs that so many rows or fewer can get: whole rounds leave fewer of them for some larger numbers of rows, and few
-// rows are spread in another way.)
+// Backwards a row of the wide path is not taken alone where the stream is fp32: its lanes' loads fill their sectors as they are, and a
+// CTA's sums stay in registers (65536 x 768: 158 -> 152 us, 64 gates of 1024 x 640: 166 -> 148; bf16 streams 144 -> 166, rows
+// element by element 302 -> 359 at 513 columns).
+constexpr bool grad_alone(int stream, bool wide) { return !wide || stream == BAOC_BF16; }
+// (By the most CTAs that so many rows or fewer can get in any type: whole rounds leave fewer of them for some larger numbers of rows.)
 int64_t grad_ws(int dim, int64_t rows) {
     int64_t ctas = 0;
-    for (int64_t n : {rows, std::min<int64_t>(rows, kFewRows)}) {
-        const Spread d(dim, n);
-        ctas = std::max(ctas, std::min(ceil_div(n, d.rows), d.at_once(class_grad_warps(d.c))));
+    for (bool alone : {true, false}) {
+        const Spread d(dim, rows, alone);
+        ctas = std::max(ctas, std::min(ceil_div(rows, d.rows), d.at_once(class_grad_warps(d.c))));
     }
     return std::max<int64_t>(256, round_up(ctas * (kJoinSums + 1) * dim * 4, 256));
 }
@@ -914,7 +917,7 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
                      rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate < rows ? e->rows_per_gate : 0, 0, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
-        const Spread d(e->dim, rows);
+        const Spread d(e->dim, rows, true);
         return with_class(d.c, wide, [&](auto C, auto W) {
             const int bytes = ((a.layer ? 4 : 2) + d.rows) * 8 * d.team * 4;
             a.rows_per_cta = round_up(ceil_div(rows, d.at_once(class_warps(C()))), d.rows);      // all CTAs at once
@@ -979,7 +982,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
                    gate && e->rows_per_gate < rows ? e->rows_per_gate : 0, 0, e->dim, e->grad_dtype, e->scale, e->eps};
     for (int k = 0; k < kJoinSums; ++k) a.out[k] = static_cast<char*>(outs[k]);
     int ctas;
-    const Spread d(e->dim, rows);
+    const Spread d(e->dim, rows, grad_alone(e->stream_dtype, wide));
     grad_shape(d, std::max<int64_t>(rows, 1), &a.rows_per_cta, &ctas);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const CheckCtx ck{static_cast<char*>(ws), static_cast<char*>(ws) + need, 0, 0, 0};
@@ -991,7 +994,8 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
                     const int sums = solo(C()) || C() == 6 ? d.rows * (L() ? 5 : 3) : 0;
                     const int staged = solo(C()) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? d.rows * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
                     const int bytes = (sums + (C() == 6 ? 0 : (L() ? 4 : 3)) + staged) * 8 * d.team * 4;
-                    auto kernel = join_grad_kernel<S(), B(), L(), C(), W()>;
+                    constexpr int kClass = (C() == 2 || C() == 3) && !grad_alone(S(), W()) ? 4 : C();      // (one that no call has is not made)
+                    auto kernel = join_grad_kernel<S(), B(), L(), kClass, W()>;
                     if (bytes > 40 * 1024) {
                         const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
                         if (ce != cudaSuccess) return launched(ce, "join_grad_kernel");
