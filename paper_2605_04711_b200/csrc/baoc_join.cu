@@ -411,8 +411,8 @@ template <int S, int B, bool kLayer, int kClass, bool kWide>
 __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, class_grad_warps(kClass))) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
     constexpr bool kSolo = solo(kClass);
     constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass), kSums = kLayer ? 5 : 3;
-    // The sums lie in shared memory where the registers have a row of several chunks, or are few (65536 x 512 with a gate: 110 us, in
-    // registers 122), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
+    // The sums lie in shared memory where the registers have a row of several chunks, or are few (65536 x 512 bf16 layer norms: 109 us, in
+    // registers 126), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
     constexpr bool kShared = kClass == 2 || kClass == 3 || kClass == 6;
     constexpr bool kAhead = kClass == 4 || kClass == 5;      // the next row is fetched into registers,
     constexpr bool kStaged = kSolo && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)

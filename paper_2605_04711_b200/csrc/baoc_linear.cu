@@ -534,23 +534,32 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 }
 
 // ---- few tiles: the sum over k is split --------------------------------------------------------------------------------
-// A cluster of CTAs shares one tile of 128 x 64, each a run of the steps over k; their sums meet in shared memory, where every
+// A cluster of CTAs shares one tile of 128 x kN, each a run of the steps over k; their sums meet in shared memory, where every
 // CTA reads its part of the tile from all of them, adds in order of rank and writes it out.  One tile of few rows is bound by the
-// reading of B: two CTAs per SM keep 64 KB of it in flight.
-constexpr int kSplitN = 64, kSplitStages = 4, kSplitWriters = 4, kSplitMost = 8;
-constexpr int kSplitThreads = 128 + 32 * kSplitWriters;
-constexpr int kSplitStage = (kTileM + kSplitN) * kRowBytes, kSplitSmem = kSplitStages * kSplitStage + 1024;
+// reading of B: two CTAs per SM, of 64 columns each, keep 64 KB of it in flight.  Sums over many rows (a narrow layer's dw) are bound by what
+// L2 gives an SM: 256 columns, and one CTA per SM, need half the bytes a product.
+constexpr int kSplitMost = 8;
+template <int kN>
+struct SplitShape {
+    static constexpr int kStages = 4, kWriters = kN == 64 ? 4 : 8, kThreads = 128 + 32 * kWriters;
+    static constexpr int kStage = (kTileM + kN) * kRowBytes, kSmem = kStages * kStage + 1024;
+    static constexpr int kOwn = kN * 4 / kWriters, kPiece = kN == 64 ? 32 : 16;      // columns of a writing thread, and at a time
+};
 
 __device__ __forceinline__ float4 load_at_rank(uint32_t addr, uint32_t rank) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at_rank(addr, rank)) : "memory");
     return v;
 }
-// where 16 bytes (4 sums) of the tile lie: rows of 256 bytes, spread over the banks
-__device__ __forceinline__ uint32_t sum_place(int row, int four) { return uint32_t(row * 256 + ((four ^ (row & 15)) << 4)); }
+// where 16 bytes (4 sums) of the tile lie: a row's are spread over the banks
+template <int kN>
+__device__ __forceinline__ uint32_t sum_place(int row, int four) { return uint32_t(row * kN * 4 + ((four ^ (row & 15)) << 4)); }
 
-__global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const __grid_constant__ Problems all, int parts) {
-    constexpr int kS = kSplitStages;
+template <int kN>
+__global__ void __launch_bounds__(SplitShape<kN>::kThreads, kN == 64 ? 2 : 1) product_split_kernel(const __grid_constant__ Problems all, int parts) {
+    using T = SplitShape<kN>;
+    static_assert(kTileM * kN * 4 <= T::kStages * T::kStage, "the sums lie where the ring was");
+    constexpr int kS = T::kStages;
     extern __shared__ char raw[];
     __shared__ uint64_t bars[2 * kS + 5];
     __shared__ uint32_t acc_at;
@@ -569,13 +578,13 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
     const int total_steps = g.k_tiles * g.passes, from = int(int64_t(total_steps) * rank / parts), to = int(int64_t(total_steps) * (rank + 1) / parts);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kS; ++s) { bar_init(full(s), 1); bar_init(empty(s), 1); }
-        for (int a = 0; a < 2; ++a) { bar_init(acc_full(a), 1); bar_init(acc_empty(a), kSplitWriters); }
+        for (int a = 0; a < 2; ++a) { bar_init(acc_full(a), 1); bar_init(acc_empty(a), T::kWriters); }
         bar_init(drained, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         shared_to_async();
     }
-    if (warp == 2) acc_alloc<1>(smem_addr(&acc_at), 2 * kSplitN);
+    if (warp == 2) acc_alloc<1>(smem_addr(&acc_at), 2 * kN);
     acc_fence_before();
     __syncthreads();
     acc_fence_after();
@@ -588,17 +597,21 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
             const int s = issued % kS;
             if (!(ok = warp_wait(empty(s), (issued / kS & 1) ^ 1))) break;
             const int pass = (i >= g.k_tiles) + (i >= 2 * g.k_tiles), k = (i - pass * g.k_tiles) * kTileK;
-            const uint32_t a = ring + s * kSplitStage, b = a + kTileM * kRowBytes;
+            const uint32_t a = ring + s * T::kStage, b = a + kTileM * kRowBytes;
             if (elected()) {
-                bar_expect(full(s), (g.a_rows + kSplitN) * kRowBytes);
+                bar_expect(full(s), (g.a_rows + kN) * kRowBytes);
                 if (g.a_mn) {
 #pragma unroll
                     for (int c = 0; c < kTileM / 64; ++c) copy_tile<1>(a + c * 64 * kRowBytes, &maps.a[pass], mt * kTileM + c * 64, k, full(s));
                 } else {
                     copy_tile<1>(a, &maps.a[pass], k, mt * kTileM, full(s));
                 }
-                if (g.b_mn) copy_tile<1>(b, &maps.b[pass], nt * kSplitN, k, full(s));
-                else copy_tile<1>(b, &maps.b[pass], k, nt * kSplitN, full(s));
+                if (g.b_mn) {
+#pragma unroll
+                    for (int c = 0; c < kN / 64; ++c) copy_tile<1>(b + c * 64 * kRowBytes, &maps.b[pass], nt * kN + c * 64, k, full(s));
+                } else {
+                    copy_tile<1>(b, &maps.b[pass], k, nt * kN, full(s));
+                }
             }
             __syncwarp();
         }
@@ -607,7 +620,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
             for (int j = 0; j < min(issued, kS); ++j) bar_wait(full((issued - 1 - j) % kS), ((issued - 1 - j) / kS) & 1);
         }
     } else if (warp == 1) {
-        const uint32_t desc = product_desc(kTileM, kSplitN, g.a_mn, g.b_mn);
+        const uint32_t desc = product_desc(kTileM, kN, g.a_mn, g.b_mn);
         const uint32_t a_step = (g.a_mn ? 16 * kRowBytes : 32) >> 4, b_step = (g.b_mn ? 16 * kRowBytes : 32) >> 4;
         const uint64_t first_a = operand_desc(ring, 64 * kRowBytes);
         bool ok = true;
@@ -618,11 +631,11 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
                 acc_fence_after();
             }
             if (!(ok = warp_wait(full(s), i / kS & 1))) break;
-            const uint64_t a = first_a + uint32_t(s) * (kSplitStage >> 4), b = a + (kTileM * kRowBytes >> 4);
+            const uint64_t a = first_a + uint32_t(s) * (T::kStage >> 4), b = a + (kTileM * kRowBytes >> 4);
             if (elected()) {
-                product<1>(acc + half * kSplitN, a, b, desc, i % kChunk > 0);
+                product<1>(acc + half * kN, a, b, desc, i % kChunk > 0);
 #pragma unroll
-                for (uint32_t k = 1; k < kTileK / 16; ++k) product<1>(acc + half * kSplitN, a + k * a_step, b + k * b_step, desc, 1);
+                for (uint32_t k = 1; k < kTileK / 16; ++k) product<1>(acc + half * kN, a + k * a_step, b + k * b_step, desc, 1);
                 product_commit<1>(empty(s));
                 if (i % kChunk == kChunk - 1 || i == to - from - 1) product_commit<1>(acc_full(half));
             }
@@ -634,18 +647,18 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
             bar_wait(drained, 0);
         }
     } else if (warp >= 4) {
-        const int quarter = warp & 3, row = quarter * 32 + lane;
-        float total[2][32];
+        const int quarter = warp & 3, row = quarter * 32 + lane, own = (warp - 4) / 4 * T::kOwn;
+        float total[T::kOwn] = {};
         bool ok = true;
         for (int c = 0; c * kChunk < to - from; ++c) {
             if (!(ok = warp_wait(acc_full(c & 1), c >> 1 & 1))) break;
             acc_fence_after();
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                float v[32];
-                acc_load(acc + (c & 1) * kSplitN + (uint32_t(quarter * 32) << 16) + p * 32, v);
+            for (int p = 0; p < T::kOwn; p += T::kPiece) {
+                float v[T::kPiece];
+                acc_load(acc + (c & 1) * kN + (uint32_t(quarter * 32) << 16) + own + p, v);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) total[p][i] = c == 0 ? v[i] : total[p][i] + v[i];
+                for (int i = 0; i < T::kPiece; ++i) total[p + i] += v[i];
             }
             acc_fence_before();
             __syncwarp();
@@ -655,26 +668,26 @@ __global__ void __launch_bounds__(kSplitThreads, 2) product_split_kernel(const _
         // (the last product is done: the ring's stages are free)
         if (mt * kTileM + row < g.m)
 #pragma unroll
-            for (int f = 0; f < 16; ++f)
-                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(ring + sum_place(row, f)), "f"(total[f / 8][f % 8 * 4]), "f"(total[f / 8][f % 8 * 4 + 1]),
-                             "f"(total[f / 8][f % 8 * 4 + 2]), "f"(total[f / 8][f % 8 * 4 + 3]) : "memory");
+            for (int f = 0; f < T::kOwn / 4; ++f)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(ring + sum_place<kN>(row, own / 4 + f)), "f"(total[4 * f]), "f"(total[4 * f + 1]), "f"(total[4 * f + 2]),
+                             "f"(total[4 * f + 3]) : "memory");
     }
     __syncwarp();
     acc_fence_before();
     cluster_barrier();
     if (warp == 2) {
         acc_fence_after();
-        acc_free<1>(acc, 2 * kSplitN);
+        acc_free<1>(acc, 2 * kN);
     }
     const int rows = min(kTileM, g.m - mt * kTileM);
-    for (int i = rank * kSplitThreads + int(threadIdx.x); i < rows * 16; i += parts * kSplitThreads) {
-        const int r = i >> 4, f = i & 15, col = nt * kSplitN + f * 4;
+    for (int i = rank * T::kThreads + int(threadIdx.x); i < rows * (kN / 4); i += parts * T::kThreads) {
+        const int r = i / (kN / 4), f = i % (kN / 4), col = nt * kN + f * 4;
         if (col >= g.n) continue;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         float4 p[kSplitMost];
 #pragma unroll
         for (int q = 0; q < kSplitMost; ++q)
-            if (q < parts) p[q] = load_at_rank(ring + sum_place(r, f), q);
+            if (q < parts) p[q] = load_at_rank(ring + sum_place<kN>(r, f), q);
 #pragma unroll
         for (int q = 0; q < kSplitMost; ++q)
             if (q < parts) { v[0] += p[q].x; v[1] += p[q].y; v[2] += p[q].z; v[3] += p[q].w; }
@@ -972,14 +985,16 @@ int launch_product(const Product* d, int count, cudaStream_t s) {
     return launched(launch_in_row(kernel, dim3(unsigned(workers * kCtas)), kProductThreads, T::kSmem, kCtas, s, all), "product_kernel");
 }
 
+template <int kN>
 int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
+    using T = SplitShape<kN>;
     static std::atomic<uint64_t> allowed{0};
-    int rc = allow_shared(product_split_kernel, kSplitSmem, &allowed);
+    int rc = allow_shared(product_split_kernel<kN>, T::kSmem, &allowed);
     Problems all;
     all.tiles[1] = all.fewer = 0;
-    for (int i = 0; i < count && !rc; ++i) rc = fill_problem(d[i], kTileM, kSplitN, kSplitN, false, &all.p[i], &all.tiles[i]);
+    for (int i = 0; i < count && !rc; ++i) rc = fill_problem(d[i], kTileM, kN, kN, false, &all.p[i], &all.tiles[i]);
     if (rc) return rc;
-    return launched(launch_in_row(product_split_kernel, dim3(unsigned((all.tiles[0] + all.tiles[1]) * parts)), kSplitThreads, kSplitSmem, unsigned(parts), s, all, parts),
+    return launched(launch_in_row(product_split_kernel<kN>, dim3(unsigned((all.tiles[0] + all.tiles[1]) * parts)), T::kThreads, T::kSmem, unsigned(parts), s, all, parts),
                     "product_split_kernel");
 }
 
@@ -988,8 +1003,9 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
 // stages in flight; steps follow one another in every CTA, rounds of tiles too, and everything together takes at least the
 // operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.
 // Against the largest tiles that give every CTA one: 512 x 4096 into 4096 47 -> 20 us, the gradient of 4096 x 768 into 2304
-// 74 -> 39 us.
-enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit };
+// 74 -> 39 us.  A split's sums meet at 6000 clocks, those of tiles of 256 columns at 9000 (with 6000, 512 x 4096 into 4096 would be split
+// and take 22 us instead of 20.5); dw of 16384 x 768 into 768, split six ways, takes 25 us instead of 41.
+enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit64, kSplit256 };
 struct Choice {
     Kind kind;
     int parts;
@@ -997,7 +1013,7 @@ struct Choice {
 Choice choose(const Product& d, int split_most) {
     const ProductArgs& g = d.g;
     const int64_t steps = d.steps(), a_bytes = int64_t(g.a_rows) * kRowBytes, bytes = 2 * (int64_t(g.m) + g.n) * 64 * steps;
-    Choice best{kSplit, 0};
+    Choice best{kSplit64, 0};
     int64_t least = 0;
     auto consider = [&](Kind kind, int parts, int64_t rounds, int64_t own_steps, int64_t step, int64_t fixed) {
         const int64_t cost = std::max(rounds * own_steps * step, bytes / 3400) + fixed;
@@ -1010,9 +1026,14 @@ Choice choose(const Product& d, int split_most) {
     whole(kPairs128, 2, 128, 256);
     if (!d.chunked()) whole(kOnes128, 1, 128, 256);
     whole(kOnes64, 1, 64, 128);
-    const int64_t tiles = d.tiles(kTileM, kSplitN), step = (a_bytes + kSplitN * kRowBytes) / 64;
+    const int64_t tiles = d.tiles(kTileM, 64), step = (a_bytes + 64 * kRowBytes) / 64;
     for (int parts = 2; parts <= kSplitMost && tiles * parts <= split_most && steps >= 4 * parts; parts *= 2)
-        consider(kSplit, parts, 1, ceil_div(steps, parts), std::max<int64_t>(tiles * parts > 148 ? 2 * step : step, 2800 / kSplitStages), 6000);
+        consider(kSplit64, parts, 1, ceil_div(steps, parts), std::max<int64_t>(tiles * parts > 148 ? 2 * step : step, 2800 / SplitShape<64>::kStages), 6000);
+    constexpr int kClusters[kSplitMost + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};      // that find room at once with an SM per CTA
+    const int64_t wide_tiles = d.tiles(kTileM, 256);
+    for (int parts = 2; parts <= kSplitMost && steps >= 4 * parts; ++parts)
+        if (wide_tiles <= kClusters[parts])
+            consider(kSplit256, parts, 1, ceil_div(steps, parts), std::max<int64_t>((a_bytes + 256 * kRowBytes) / 64, 2800 / SplitShape<256>::kStages), 9000);
     return best;
 }
 
@@ -1031,12 +1052,13 @@ int form_products(Product* d, int count, int split_most, cudaStream_t s) {
         parts[i] = c.parts;
     }
     // two of one kind in one launch (chunked and other sums are two kinds)
-    const bool alike = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] && (kind[0] == kSplit || d[0].chunked() == d[1].chunked());
+    const bool alike = count == 2 && kind[0] == kind[1] && parts[0] == parts[1] && (kind[0] >= kSplit64 || d[0].chunked() == d[1].chunked());
     const int step = alike ? 2 : 1;
     for (int i = 0; i < count; i += step) {
         int rc;
         switch (kind[i]) {
-            case kSplit: rc = launch_split(d + i, step, parts[i], s); break;
+            case kSplit64: rc = launch_split<64>(d + i, step, parts[i], s); break;
+            case kSplit256: rc = launch_split<256>(d + i, step, parts[i], s); break;
             case kPairs256: rc = launch_product<2, 256, false>(d + i, step, s); break;
             case kPairs128: rc = d[i].chunked() ? launch_product<2, 128, true>(d + i, step, s) : launch_product<2, 128, false>(d + i, step, s); break;
             case kOnes128: rc = launch_product<1, 128, false>(d + i, step, s); break;

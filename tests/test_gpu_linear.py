@@ -409,3 +409,22 @@ def test_long_sums_keep_their_low_bits(B, dtype):
     B.Linear(k, n).grad(x, None, d, dw=dw)
     want = d.double().t() @ x.double()
     _within(dw, want, want * 2.0 ** -15)
+
+
+@pytest.mark.parametrize("m,k,n", [(8192, 768, 768), (16384, 776, 520), (9001, 600, 1000), (16384, 2304, 768), (4096, 1024, 1030), (12288, 256, 250), (130, 8192, 2048), (300, 8000, 1025)])
+@pytest.mark.parametrize("layout", ["out_in", "in_out"])
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_long_sums_of_few_tiles(B, m, k, n, layout, dtype):
+    """Sums over many steps of outputs with few tiles, which several CTAs share: dw of narrow layers, products of few rows."""
+    x, w, dout = _ints((m, k), 1), _ints((n, k), 2), _ints((m, n), 5)
+    p, r = B.Linear(k, n, "none", layout), _ints((m, n), 4, 9, dtype)
+    out = p.product(x, _w(w, layout), residual=r)
+    assert torch.equal(out, (x.double() @ w.double().t() + r.double()).to(dtype))
+    dx, dw, db = torch.empty((m, k), dtype=BF, device=DEV), torch.empty_like(_w(w, layout), dtype=dtype), torch.empty(n, dtype=dtype, device=DEV)
+    p.grad(x, _w(w, layout), dout, dx=dx, dw=dw, db=db)
+    want = dout.double().t() @ x.double()
+    assert torch.equal(dx, (dout.double() @ w.double()).to(BF)) and torch.equal(db, dout.double().sum(0).to(dtype))
+    assert torch.equal(dw, (want if layout == "out_in" else want.t()).to(dtype))
+    again = torch.empty_like(dw)
+    p.grad(x, _w(w, layout), dout, dw=again)
+    assert torch.equal(dw, again)
