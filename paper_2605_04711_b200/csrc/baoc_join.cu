@@ -382,6 +382,9 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
 enum Sum : int { kPreW = 0, kPostW = 1, kGate = 2, kPreB = 3, kPostB = 4 };
+// What is summed row by row.  A gate is the same for all rows of its group, so its gradient and those of post's weight and bias follow
+// from two sums a column at the group's end: with A = sum of Dy n(f) and B = sum of Dy, dgate = w A + b B, dw = g A, db = g B.
+enum Running : int { kDhN = 0, kDyN = 1, kDh = 2, kDy = 3 };
 
 struct JoinGradArgs {
     const char *y, *f, *dy, *dh;
@@ -410,7 +413,7 @@ __device__ __forceinline__ void store_grad(char* out, int dtype, int64_t i, floa
 template <int S, int B, bool kLayer, int kClass, bool kWide>
 __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, class_grad_warps(kClass))) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
     constexpr bool kSolo = solo(kClass);
-    constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass), kSums = kLayer ? 5 : 3;
+    constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass), kSums = kLayer ? 4 : 2;
     // The sums lie in shared memory where the registers have a row of several chunks, or are few (65536 x 512 bf16 layer norms: 109 us, in
     // registers 126), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
     constexpr bool kShared = kClass == 2 || kClass == 3 || kClass == 6;
@@ -463,9 +466,8 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             }
         }
     };
-    // The sum k of all teams to `to` (a vector of dim), each column by one thread: behind a barrier that follows what the teams have
-    // added, and publish(k) of sums in registers.  (Four neighbours in one access where that can be: one by one, a CTA's sums of
-    // 768 columns took as long as a row.)
+    // At a group's end and a CTA's: the sums of all teams, each column's in one thread (half_sum, over `places`), behind a barrier that
+    // follows what the teams have added and publish() of sums in registers.
     auto publish = [&](auto which) {
         if constexpr (kSolo && !kShared) {
             constexpr int k = decltype(which)::value;
@@ -477,38 +479,56 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             p[size] = make_float4(v[4], v[5], v[6], v[7]);
         }
     };
-    auto store4 = [&](char* to, int dtype, int of, int j, float4 v) {        // columns j to j + 3 of place `of`
+    // (four neighbours in one access where that can be: one by one, a CTA's sums of 768 columns took as long as a row)
+    auto store4 = [&](char* to, int dtype, int of, int j, float4 v, bool add) {        // columns j to j + 3 of place `of`
         if (kWide && dtype == BAOC_F32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
-            if (Stream::column(of, j) < dim) *reinterpret_cast<float4*>(to + 4 * Stream::column(of, j)) = v;
+            if (Stream::column(of, j) >= dim) return;
+            float4* p = reinterpret_cast<float4*>(to + 4 * Stream::column(of, j));
+            if (add) { const float4 o = *p; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
+            *p = v;
             return;
         }
         const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (Stream::column(of, j + i) < dim) store_grad(to, dtype, Stream::column(of, j + i), x[i]);
-    };
-    auto hand_out = [&](auto which, char* to, int dtype) {
-        constexpr int k = decltype(which)::value;
-        if constexpr (kSolo) {
-            for (int i = int(threadIdx.x); i < 2 * size; i += int(blockDim.x)) {
-                float4 v = sums[k * 2 * size + i];
-                for (int o = 1; o < kTeams; ++o) {
-                    const float4 w = sums[(o * kSums + k) * 2 * size + i];
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-                }
-                store4(to, dtype, i % size, 4 * (i / size), v);
-            }
-        } else if constexpr (kShared) {
-            store4(to, dtype, t, 0, sums[k * 2 * size + t]);
-            store4(to, dtype, t, 4, sums[(k * 2 + 1) * size + t]);
-        } else {
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) unpack2(acc[k][j], v[2 * j], v[2 * j + 1]);
-            store4(to, dtype, t, 0, make_float4(v[0], v[1], v[2], v[3]));
-            store4(to, dtype, t, 4, make_float4(v[4], v[5], v[6], v[7]));
+        for (int i = 0; i < 4; ++i) {
+            const int c = Stream::column(of, j + i);
+            if (c < dim) store_grad(to, dtype, c, add ? reinterpret_cast<const float*>(to)[c] + x[i] : x[i]);      // (add: fp32)
         }
     };
+    auto half_sum = [&](auto which, int i) {         // sum `which`, float4 i of its 2 * size
+        constexpr int k = decltype(which)::value;
+        float4 v;
+        if constexpr (kSolo || kShared) {
+            v = sums[k * 2 * size + i];
+            for (int o = 1; o < kTeams; ++o) {
+                const float4 w = sums[(o * kSums + k) * 2 * size + i];
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+        } else {
+            const int j = i == t ? 0 : 2;
+            unpack2(j ? acc[k][2] : acc[k][0], v.x, v.y);
+            unpack2(j ? acc[k][3] : acc[k][1], v.z, v.w);
+        }
+        return v;
+    };
+    auto places = [&](auto f) {                      // f(i) for this thread's share of the 2 * size
+        if constexpr (kSolo) {
+            for (int i = int(threadIdx.x); i < 2 * size; i += int(blockDim.x)) f(i);
+        } else {
+            f(t);
+            f(size + t);
+        }
+    };
+    auto four_of = [&](int which, const float* v, int i) {       // a kept vector's columns
+        if constexpr (kKeep) return kept.at[which * 2 * size + i];
+        else {
+            const int of = i % size, j = 4 * (i / size);
+            auto one = [&](int e) { return v && Stream::column(of, j + e) < dim ? __ldg(v + Stream::column(of, j + e)) : 0.f; };
+            return make_float4(one(0), one(1), one(2), one(3));
+        }
+    };
+    auto times = [](float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); };
+    auto plus = [](float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); };
     auto in = [&](int c) { return !kWide || (t + 32 * c) * kJoinCols < dim; };
     auto keep = [&](int which, const float* v) {
 #pragma unroll
@@ -640,8 +660,8 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                     f32x2 w[4], n[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) n[j] = mul2(y[c][j], r2);
-                    add(kPreW, c, d[c], n);
-                    if (kLayer) add(kPreB, c, d[c], ones);
+                    add(kDhN, c, d[c], n);
+                    if (kLayer) add(kDh, c, d[c], ones);
                     vector(kVPreW, g.pre_w, c, w);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -668,17 +688,13 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                     vector(kVPostW, g.post_w, c, w);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) f[c][j] = mul2(f[c][j], r2);
+                    add(kDyN, c, d[c], f[c]);
+                    if (kLayer) add(kDy, c, d[c], ones);
                     if (gate) {
-                        if (kLayer) vector(kVPostB, g.post_b, c, b);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) b[j] = kLayer ? fma2(f[c][j], w[j], b[j]) : mul2(f[c][j], w[j]);
-                        add(kGate, c, d[c], b);
                         vector(kVGate, gate, c, b);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) d[c][j] = mul2(d[c][j], b[j]);
                     }
-                    add(kPostW, c, d[c], f[c]);
-                    if (kLayer) add(kPostB, c, d[c], ones);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[c][j] = mul2(d[c][j], w[j]);
                     s[0] += dot8(d[c], f[c]);
@@ -695,7 +711,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                 for (int c = 0; c < kC; ++c) {
                     f32x2 w[4];
                     vector(kVGate, gate, c, w);
-                    add(kGate, c, d[c], f[c]);
+                    add(kDyN, c, d[c], f[c]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[c][j] = mul2(d[c][j], w[j]);
                 }
@@ -704,37 +720,46 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             for (int c = 0; c < kC; ++c) Branch::store(g.df + row * g.df_step, t + 32 * c, dim, d[c]);
             if (!kAhead && !kStaged) fetch(row + kTeams);
         }
-        if (g.rows_per_gate && g.out[kGate]) {
-            const bool whole = group * g.rows_per_gate >= begin && min64(g.rows, (group + 1) * g.rows_per_gate) <= end;
-            float* slot = part + int64_t(group == begin / g.rows_per_gate ? kGate : kJoinSums) * dim;
-            publish(std::integral_constant<int, kGate>{});
+        if (g.out[kGate] || g.out[kPostW] || g.out[kPostB]) {
+            const bool whole = g.rows_per_gate && group * g.rows_per_gate >= begin && min64(g.rows, (group + 1) * g.rows_per_gate) <= end;
+            float* slot = part + int64_t(!g.rows_per_gate || group == begin / g.rows_per_gate ? kGate : kJoinSums) * dim;
+            publish(std::integral_constant<int, kDyN>{});
+            if constexpr (kLayer) publish(std::integral_constant<int, kDy>{});
             if (kSolo) __syncthreads();
-            hand_out(std::integral_constant<int, kGate>{}, whole ? g.out[kGate] + group * dim * (g.grad_dtype == BAOC_F32 ? 4 : 2) : reinterpret_cast<char*>(slot),
-                     whole ? g.grad_dtype : int(BAOC_F32));
+            places([&](int i) {
+                float4 a = half_sum(std::integral_constant<int, kDyN>{}, i), b = make_float4(0.f, 0.f, 0.f, 0.f);
+                if constexpr (kLayer) b = half_sum(std::integral_constant<int, kDy>{}, i);
+                const int of = i % size, j = 4 * (i / size);
+                if (g.out[kGate]) {
+                    float4 v = a;
+                    if (g.post_w) v = times(v, four_of(kVPostW, g.post_w, i));
+                    if (kLayer && g.post_w) v = plus(v, times(b, four_of(kVPostB, g.post_b, i)));
+                    if (whole) store4(g.out[kGate] + group * dim * (g.grad_dtype == BAOC_F32 ? 4 : 2), g.grad_dtype, of, j, v, false);
+                    else store4(reinterpret_cast<char*>(slot), BAOC_F32, of, j, v, false);
+                }
+                if (gate) {
+                    const float4 w = four_of(kVGate, gate, i);
+                    a = times(a, w);
+                    b = times(b, w);
+                }
+                if (g.out[kPostW]) store4(reinterpret_cast<char*>(part + int64_t(kPostW) * dim), BAOC_F32, of, j, a, seg != begin);
+                if (kLayer && g.out[kPostB]) store4(reinterpret_cast<char*>(part + int64_t(kPostB) * dim), BAOC_F32, of, j, b, seg != begin);
+            });
             if (kSolo) __syncthreads();
-            zero(kGate);
+            zero(kDyN);
+            if constexpr (kLayer) zero(kDy);
         }
         seg = seg_end;
     }
-    publish(std::integral_constant<int, kPreW>{});
-    publish(std::integral_constant<int, kPostW>{});
-    publish(std::integral_constant<int, kGate>{});
-    if constexpr (kLayer) {
-        publish(std::integral_constant<int, kPreB>{});
-        publish(std::integral_constant<int, kPostB>{});
-    }
+    publish(std::integral_constant<int, kDhN>{});
+    if constexpr (kLayer) publish(std::integral_constant<int, kDh>{});
     if (kSolo) __syncthreads();
-    auto finish = [&](auto which) {
-        constexpr int k = decltype(which)::value;
-        if (g.out[k]) hand_out(which, reinterpret_cast<char*>(part + int64_t(k) * dim), BAOC_F32);
-    };
-    finish(std::integral_constant<int, kPreW>{});
-    finish(std::integral_constant<int, kPostW>{});
-    if (!g.rows_per_gate) finish(std::integral_constant<int, kGate>{});
-    if constexpr (kLayer) {
-        finish(std::integral_constant<int, kPreB>{});
-        finish(std::integral_constant<int, kPostB>{});
-    }
+    places([&](int i) {
+        const int of = i % size, j = 4 * (i / size);
+        if (g.out[kPreW]) store4(reinterpret_cast<char*>(part + int64_t(kPreW) * dim), BAOC_F32, of, j, half_sum(std::integral_constant<int, kDhN>{}, i), false);
+        if constexpr (kLayer)
+            if (g.out[kPreB]) store4(reinterpret_cast<char*>(part + int64_t(kPreB) * dim), BAOC_F32, of, j, half_sum(std::integral_constant<int, kDh>{}, i), false);
+    });
 }
 
 // The CTAs' sums, 32 columns per CTA: every warp adds each 32nd CTA's, then the warps' sums are added in order.
@@ -991,7 +1016,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
         rc = with_types(e->stream_dtype, e->branch_dtype, [&](auto S, auto B) {
             return with_class(d.c, wide, [&](auto C, auto W) {
                 auto go = [&](auto L) {
-                    const int sums = solo(C()) || C() == 6 ? d.rows * (L() ? 5 : 3) : 0;
+                    const int sums = solo(C()) || C() == 6 ? d.rows * (L() ? 4 : 2) : 0;
                     const int staged = solo(C()) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? d.rows * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
                     const int bytes = (sums + (C() == 6 ? 0 : (L() ? 4 : 3)) + staged) * 8 * d.team * 4;
                     constexpr int kClass = (C() == 2 || C() == 3) && !grad_alone(S(), W()) ? 4 : C();      // (one that no call has is not made)
