@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
     // registers 126), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
     constexpr bool kShared = kClass == 2 || kClass == 3 || kClass == 6;
     constexpr bool kAhead = kClass == 4 || kClass == 5;      // the next row is fetched into registers,
-    constexpr bool kStaged = kSolo && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)
+    constexpr bool kStaged = (kSolo || kClass == 6) && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)
     constexpr bool kKeep = kClass != 6 || !kLayer;   // (a layer norm of class 6: shared memory has no room for the vectors beside the sums)
     constexpr int kVectors = kLayer ? 4 : 3;         // kept ones, the gate (of a segment) among them
     using Stream = RowPart<S, kClass, kWide>;
@@ -1017,7 +1017,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
             return with_class(d.c, wide, [&](auto C, auto W) {
                 auto go = [&](auto L) {
                     const int sums = solo(C()) || C() == 6 ? d.rows * (L() ? 4 : 2) : 0;
-                    const int staged = solo(C()) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? d.rows * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
+                    const int staged = (solo(C()) || C() == 6) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? d.rows * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
                     const int bytes = (sums + (L() ? (C() == 6 ? 0 : 4) : 3) + staged) * 8 * d.team * 4;
                     constexpr int kClass = (C() == 2 || C() == 3) && !grad_alone(S(), W()) ? 4 : C();      // (one that no call has is not made)
                     auto kernel = join_grad_kernel<S(), B(), L(), kClass, W()>;
