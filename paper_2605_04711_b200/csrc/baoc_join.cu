@@ -419,17 +419,18 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
     constexpr bool kShared = kClass == 2 || kClass == 3 || kClass == 6;
     constexpr bool kAhead = kClass == 4 || kClass == 5;      // the next row is fetched into registers,
     constexpr bool kStaged = (kSolo || kClass == 6) && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)
-    constexpr bool kKeep = kClass != 6 || !kLayer;   // (a layer norm of class 6: shared memory has no room for the vectors beside the sums)
-    constexpr int kVectors = kLayer ? 4 : 3;         // kept ones, the gate (of a segment) among them
+    // Kept vectors: the weights and the gate (of a segment); pre's weight alone where shared memory has no room for all of them, the sums and a
+    // staged row (8192 x 8192 bf16 layer norms: 296 us, 357 with the vectors and no staged row).
+    constexpr int kVectors = kClass == 6 && kLayer ? 1 : 3;
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;
-    extern __shared__ float4 dynamic4[];             // kKeep: the vectors; the sums, [team][sum][2][team's threads]; kStaged: a row per team
+    extern __shared__ float4 dynamic4[];             // the vectors; kShared or kSolo: the sums, [team][sum][2][team's threads]; kStaged: a row per team
     __shared__ float4 buf[kSolo ? 1 : 2][32];
     TeamSum<kClass> sum{buf};
     begin_in_row();
     const int size = team_size<kClass>(), t = kSolo ? int(threadIdx.x & 31) : int(threadIdx.x), team = kSolo ? int(threadIdx.x >> 5) : 0, dim = g.dim;
     const Kept<kClass> kept{dynamic4};
-    float4* sums = dynamic4 + (kKeep ? kVectors * 2 * size : 0);
+    float4* sums = dynamic4 + kVectors * 2 * size;
     const float over = 1.f / float(dim);
     const int64_t begin = int64_t(blockIdx.x) * g.rows_per_cta, end = min64(g.rows, begin + g.rows_per_cta);
     float* part = g.part + int64_t(blockIdx.x) * (kJoinSums + 1) * dim;
@@ -519,14 +520,14 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             f(size + t);
         }
     };
-    auto four_of = [&](int which, const float* v, int i) {       // a kept vector's columns
-        if constexpr (kKeep) return kept.at[which * 2 * size + i];
-        else {
-            const int of = i % size, j = 4 * (i / size);
-            auto one = [&](int e) { return v && Stream::column(of, j + e) < dim ? __ldg(v + Stream::column(of, j + e)) : 0.f; };
-            return make_float4(one(0), one(1), one(2), one(3));
-        }
+    auto columns_of = [&](const float* v, int i) {
+        auto one = [&](int e) {
+            const int c = Stream::column(i % size, 4 * (i / size) + e);
+            return v && c < dim ? __ldg(v + c) : 0.f;
+        };
+        return make_float4(one(0), one(1), one(2), one(3));
     };
+    auto four_of = [&](int which, const float* v, int i) { return which < kVectors ? kept.at[which * 2 * size + i] : columns_of(v, i); };
     auto times = [](float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); };
     auto plus = [](float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); };
     auto in = [&](int c) { return !kWide || (t + 32 * c) * kJoinCols < dim; };
@@ -539,7 +540,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
         }
     };
     auto vector = [&](int which, const float* v, int c, f32x2 (&x)[4]) {
-        if constexpr (kKeep) kept.get(which, t + 32 * c, x);
+        if (which < kVectors) kept.get(which, t + 32 * c, x);
         else per_column<kClass, kWide>(v, t + 32 * c, dim, 0.f, x);
     };
     Stream next_y[kC], next_dy[kC];
@@ -580,13 +581,10 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
     int64_t row = begin + team;
     if constexpr (kStaged) request(row);
     else fetch(row);
-    if constexpr (kKeep) {
-        if (team == 0) {
-            keep(kVPreW, g.pre_w);
-            if (g.post_w) keep(kVPostW, g.post_w);
-            if (kLayer && g.post_w) keep(kVPostB, g.post_b);
-            if (g.gate && !g.rows_per_gate) keep(kVGate, g.gate);
-        }
+    if (team == 0) {
+        keep(kVPreW, g.pre_w);
+        if (kVectors == 3 && g.post_w) keep(kVPostW, g.post_w);
+        if (kVectors == 3 && g.gate && !g.rows_per_gate) keep(kVGate, g.gate);
     }
     if constexpr (kShared)
         for (int k = 0; k < kSums; ++k) zero(k);
@@ -596,7 +594,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
         const int64_t group = g.rows_per_gate ? seg / g.rows_per_gate : 0;
         const int64_t seg_end = g.rows_per_gate ? min64(end, (group + 1) * g.rows_per_gate) : end;
         const float* gate = g.gate ? g.gate + group * dim : nullptr;
-        if (kKeep && g.rows_per_gate) {
+        if (kVectors == 3 && g.rows_per_gate) {
             if (kSolo) __syncthreads();              // (no warp reads the last group's any more)
             if (team == 0) keep(kVGate, gate);
             if (kSolo) __syncthreads();
@@ -733,7 +731,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                 if (g.out[kGate]) {
                     float4 v = a;
                     if (g.post_w) v = times(v, four_of(kVPostW, g.post_w, i));
-                    if (kLayer && g.post_w) v = plus(v, times(b, four_of(kVPostB, g.post_b, i)));
+                    if (kLayer && g.post_w) v = plus(v, times(b, columns_of(g.post_b, i)));
                     if (whole) store4(g.out[kGate] + group * dim * (g.grad_dtype == BAOC_F32 ? 4 : 2), g.grad_dtype, of, j, v, false);
                     else store4(reinterpret_cast<char*>(slot), BAOC_F32, of, j, v, false);
                 }
@@ -1018,7 +1016,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
                 auto go = [&](auto L) {
                     const int sums = solo(C()) || C() == 6 ? d.rows * (L() ? 4 : 2) : 0;
                     const int staged = (solo(C()) || C() == 6) && W() && S() == BAOC_BF16 && B() == BAOC_BF16 ? d.rows * 4 / 2 : 0;        // four rows of 2 bytes a column, counted as vectors of 4
-                    const int bytes = (sums + (L() ? (C() == 6 ? 0 : 4) : 3) + staged) * 8 * d.team * 4;
+                    const int bytes = (sums + (C() == 6 && L() ? 1 : 3) + staged) * 8 * d.team * 4;
                     constexpr int kClass = (C() == 2 || C() == 3) && !grad_alone(S(), W()) ? 4 : C();      // (one that no call has is not made)
                     auto kernel = join_grad_kernel<S(), B(), L(), kClass, W()>;
                     if (bytes > 40 * 1024) {
