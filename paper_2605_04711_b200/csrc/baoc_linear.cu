@@ -1003,8 +1003,10 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
 // stages in flight; steps follow one another in every CTA, rounds of tiles too, and everything together takes at least the
 // operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.
 // Against the largest tiles that give every CTA one: 512 x 4096 into 4096 47 -> 20 us, the gradient of 4096 x 768 into 2304
-// 74 -> 39 us.  A split's sums meet at 6000 clocks, those of tiles of 256 columns at 9000 (with 6000, 512 x 4096 into 4096 would be split
-// and take 22 us instead of 20.5); dw of 16384 x 768 into 768, split six ways, takes 25 us instead of 41.
+// 74 -> 39 us.  A split's sums meet at 6000 clocks.  Tiles of 256 columns are charged 18000: their sums take
+// longer to meet, and a gradient's two products in tiles of 64 share a launch (1000 x 513 into 1001 with gelu's fp32 dw takes 31 us with
+// 14000, 25 with 18000; 9000 also splits 512 x 4096 into 4096, 22 us instead of 20.5).  dw of 16384 x 768 into 768, split six ways, takes 24 us instead of 39, of
+// 16384 x 1024 into 1024 32 instead of 56.
 enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit64, kSplit256 };
 struct Choice {
     Kind kind;
@@ -1033,7 +1035,7 @@ Choice choose(const Product& d, int split_most) {
     const int64_t wide_tiles = d.tiles(kTileM, 256);
     for (int parts = 2; parts <= kSplitMost && steps >= 4 * parts; ++parts)
         if (wide_tiles <= kClusters[parts])
-            consider(kSplit256, parts, 1, ceil_div(steps, parts), std::max<int64_t>((a_bytes + 256 * kRowBytes) / 64, 2800 / SplitShape<256>::kStages), 9000);
+            consider(kSplit256, parts, 1, ceil_div(steps, parts), std::max<int64_t>((a_bytes + 256 * kRowBytes) / 64, 2800 / SplitShape<256>::kStages), 18000);
     return best;
 }
 
