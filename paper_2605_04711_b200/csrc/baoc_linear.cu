@@ -807,12 +807,17 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
     if (base + slope_column<kWide>(lane, 0) < g.n)
         for (int64_t row = first + warp; row < end; row += 8 * kSlopeRows) {
             float d[kSlopeRows][8], z[kPre ? kSlopeRows : 1][8];
-#pragma unroll
-            for (int r = 0; r < kSlopeRows; ++r) {
-                const int64_t at = min64(row + 8 * r, end - 1);          // (a row too many is read, not used)
+            auto load = [&](int64_t at, int r) {
                 load8<kWide>(g.dout + at * g.dout_step, base, lane, g.n, d[r]);
                 if constexpr (kPre) load8<kWide>(g.pre + at * g.pre_step, base, lane, g.n, z[r]);
+            };
+            if (row + 8 >= end) {                    // a warp's last row (of few, its only one) alone
+                load(row, 0);
+                one_row(row, d[0], z[0]);
+                break;
             }
+#pragma unroll
+            for (int r = 0; r < kSlopeRows; ++r) load(min64(row + 8 * r, end - 1), r);       // (a row too many is read, not used)
 #pragma unroll
             for (int r = 0; r < kSlopeRows; ++r)
                 if (row + 8 * r < end) one_row(row + 8 * r, d[r], z[kPre ? r : 0]);
