@@ -555,7 +555,8 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                 if (need_f) next_f[c].load(g.f + row * g.f_step, t + 32 * c, dim);
             }
     };
-    // the staged row: y, dy, dh, f
+    // The staged row: y, dy, dh, f.  What a thread has taken may be overwritten once it has gone into something that is done before
+    // the request: y, dh and f into the row's sums, dy into a store of dx or df (see below), which is why it is requested later.
     const uint32_t ahead = smem_addr(sums + kTeams * kSums * 2 * size) + team * 4 * 16 * size;
     const uint32_t at_dy = ahead + 16 * size, at_dh = ahead + 32 * size, at_f = ahead + 48 * size;
     auto request = [&](int64_t row) {
@@ -565,10 +566,18 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             for (int c = 0; c < kC; ++c) {
                 if (!in(c)) continue;
                 Stream::request(ahead, g.y + row * g.y_step, t + 32 * c);
-                if (g.dy) Stream::request(at_dy, g.dy + row * g.dy_step, t + 32 * c);
                 Branch::request(at_dh, g.dh + row * g.dh_step, t + 32 * c);
                 if (need_f) Branch::request(at_f, g.f + row * g.f_step, t + 32 * c);
             }
+        cp_async_commit();
+    };
+    auto request_dy = [&](int64_t row) {
+        (void)at_dy;
+        if (!g.dy) return;
+        if (row < end)
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+                if (in(c)) Stream::request(at_dy, g.dy + row * g.dy_step, t + 32 * c);
         cp_async_commit();
     };
 #pragma unroll
@@ -579,8 +588,12 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
         next_f[c].clear();
     }
     int64_t row = begin + team;
-    if constexpr (kStaged) request(row);
-    else fetch(row);
+    if constexpr (kStaged) {
+        request(row);
+        request_dy(row);
+    } else {
+        fetch(row);
+    }
     if (team == 0) {
         keep(kVPreW, g.pre_w);
         if (kVectors == 3 && g.post_w) keep(kVPostW, g.post_w);
@@ -649,7 +662,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                     if (kLayer) s[3] += sum8(w);
                 }
                 sum(s);
-                if constexpr (kStaged) request(row + kTeams);       // (the sums are made of all that has been taken: its place is free)
+                if constexpr (kStaged) request(row + kTeams);       // (the sums are made of all of y, dh and f: their places are free)
                 const float r_y = rsqrtf(s[0] * over + g.eps);
                 r_f = rsqrtf(s[1] * over + g.eps);
                 const f32x2 r2 = splat2(r_y), slope = splat2(-r_y * r_y * s[2] * over), mean = splat2(-s[3] * over);
@@ -676,6 +689,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
                     for (int j = 0; j < 4; ++j) dy[c][j] = mul2(scale, d[c][j]);
                     Stream::store(g.dx + row * g.dx_step, t + 32 * c, dim, dy[c]);
                 }
+                if constexpr (kStaged) request_dy(row + kTeams);    // (dy has left in dx)
             }
             if (g.post_w) {
                 const f32x2 r2 = splat2(r_f);
@@ -716,6 +730,8 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
             }
 #pragma unroll
             for (int c = 0; c < kC; ++c) Branch::store(g.df + row * g.df_step, t + 32 * c, dim, d[c]);
+            if constexpr (kStaged)
+                if (!g.dx) request_dy(row + kTeams);                // (without dx it has left in df)
             if (!kAhead && !kStaged) fetch(row + kTeams);
         }
         if (g.out[kGate] || g.out[kPostW] || g.out[kPostB]) {

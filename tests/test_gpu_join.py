@@ -399,3 +399,24 @@ def test_a_refused_join_leaves_the_gradient_alone(B):
 def test_more_than_a_few_rows(B, n, dim, stream, branch, layer, gates):
     """Rows of 257 to 768 columns: from some number of them on, a warp takes one alone."""
     _check(B, _data(n // max(gates, 1) * max(gates, 1), dim, layer, True, gates, stream, branch), layer, grad=F)
+
+
+@pytest.mark.parametrize("n,dim", [(9000, 256), (7000, 512), (5000, 768), (1500, 5000), (1500, 8192)])
+@pytest.mark.parametrize("layer,gates", [(False, 0), (True, 5)])
+@pytest.mark.parametrize("want_dx", [True, False])
+def test_rows_requested_ahead(B, n, dim, layer, gates, want_dx):
+    """Many bf16 rows per CTA, each requested while the one before is worked on, dy's place behind the store that holds it: dy itself
+    in place of dx, dx apart, and no dx."""
+    d = _data(n, dim, layer, True, gates, BF, BF)
+    d["dy"] *= 100
+    p, c = B.Join(dim, "layer" if layer else "rms"), _dev(d)
+    y, _ = p.join(c["x"], c["f"], c["pre_w"], **_vectors(c))
+    want, first = _want_grad(d, y.cpu(), layer, 1.0, 1e-6), None
+    for dx in (None, "dy", None) if want_dx else (None, None):
+        call = c | {"dy": c["dy"].clone()}
+        got = _run_grad(p, call, y, **({"dx": call["dy"]} if dx else {}), want_dx=want_dx)
+        for k, w in want.items() if first is None else ():
+            if k != "dx" or want_dx:
+                _within(got[k], w)
+        first = first or got
+        assert all(torch.equal(got[k], first[k]) for k in first if first[k] is not None)
