@@ -383,7 +383,8 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
 // ---- gradient ---------------------------------------------------------------------------------------------------
 enum Sum : int { kPreW = 0, kPostW = 1, kGate = 2, kPreB = 3, kPostB = 4 };
 // What is summed row by row.  A gate is the same for all rows of its group, so its gradient and those of post's weight and bias follow
-// from two sums a column at the group's end: with A = sum of Dy n(f) and B = sum of Dy, dgate = w A + b B, dw = g A, db = g B.
+// from two sums a column at the group's end: with A = sum of Dy n(f) and B = sum of Dy, dgate = w A + b B, dw = g A, db = g B.  (Without
+// post A is the sum of Dy f, and dgate.)
 enum Running : int { kDhN = 0, kDyN = 1, kDh = 2, kDy = 3 };
 
 struct JoinGradArgs {
@@ -644,7 +645,7 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
 #pragma unroll
                 for (int c = 0; c < kC; ++c) {
                     Stream::centre(y[c], s[0] * over, t + 32 * c, dim);
-                    Stream::centre(f[c], s[1] * over, t + 32 * c, dim);
+                    if (g.post_w) Stream::centre(f[c], s[1] * over, t + 32 * c, dim);        // (post(f) is f itself without a norm)
                 }
             }
             float r_f;

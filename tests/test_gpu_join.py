@@ -420,3 +420,38 @@ def test_rows_requested_ahead(B, n, dim, layer, gates, want_dx):
                 _within(got[k], w)
         first = first or got
         assert all(torch.equal(got[k], first[k]) for k in first if first[k] is not None)
+
+
+@pytest.mark.parametrize("n,dim", [(1, 1), (3, 2), (5, 7), (33, 64), (9, 257), (300, 513), (40, 768), (594, 513), (700, 765), (2000, 600), (3000, 128), (700, 1024), (6, 2049), (12, 4096),
+                                   (6, 4104), (300, 8192), (5, 8191)])
+@pytest.mark.parametrize("stream,branch,layer,groups", [(F, BF, True, 1), (F, F, True, 1), (F, BF, True, 3), (F, F, False, 2), (BF, BF, True, 1), (BF, BF, True, 4), (BF, BF, False, 3)])
+def test_gates_of_a_branch_without_a_norm(B, n, dim, stream, branch, layer, groups):
+    """post(f) is f itself, whatever its mean: the gate's gradient sums Dy f, not Dy (f - mean(f))."""
+    groups = min(groups, n)
+    d = _data(n // groups * groups, dim, layer, False, groups, stream, branch)
+    d["f"] += 1
+    _check(B, d, layer, scale=0.7, grad=F)
+
+
+def test_gate_gradient_of_a_branch_without_a_norm_against_differences(B):
+    """<dy, y> + <dh, h> by differences of the 64-bit form along every gate."""
+    n, dim, scale, eps = 4, 12, 0.8, 1e-5
+    d = _data(n, dim, True, False, 2, F, F, offset=0.5)
+    p, c = B.Join(dim, "layer", eps=eps, scale=scale), _dev(d)
+    y, _ = p.join(c["x"], c["f"], c["pre_w"], **_vectors(c))
+    got = _run_grad(p, c, y)
+
+    def value(q):
+        v, w = _want(q, True, scale, eps)
+        return float((v.v * d["dy"].double()).sum() + (w.v * d["dh"].double()).sum())
+
+    step = 1e-4                              # third derivatives of order 0.01 at most: off by 1e-10
+    for of, k in (("gate", "dgate"), ("f", "df"), ("x", "dx")):
+        base = {a: None if b is None else b.double() for a, b in d.items()}
+        flat = got[k].reshape(-1).cpu().double()
+        for i in range(flat.numel()):
+            at = [base | {of: base[of].clone()} for _ in range(2)]
+            for q, s in zip(at, (step, -step)):
+                q[of].view(-1)[i] += s
+            # fp32 terms below 0.1 each, a few roundings; y itself was rounded once
+            assert abs((value(at[0]) - value(at[1])) / (2 * step) - float(flat[i])) <= 2e-6, (k, i)
