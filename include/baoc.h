@@ -686,7 +686,7 @@ typedef struct {
 } baoc_join_t;
 
 /* y[rows][dim] and h[rows][dim].  y may be x and h may be f (same pointer, type and
- * row stride); arrays overlap in no other way.  Pointers are aligned to their
+ * row stride); outputs overlap no other array, vectors and gates among them.  Pointers are aligned to their
  * elements; a dim that is a multiple of 8 in arrays whose bases and row strides are
  * multiples of 8 elements (weights: of 16 bytes) takes the wide path.  rows <= 2^31, 0 queues nothing.  One
  * kernel; does not wait. */
@@ -702,7 +702,7 @@ int baoc_join_grad_workspace_bytes(const baoc_join_t* e, int64_t rows, size_t* b
  *   Dy = dy + pre's gradient,  dx = scale Dy,  dgate = sum of Dy * post(f) over the gate's rows,  df = post's gradient of gate * Dy
  *
  * y: as baoc_join wrote it; f: not read without post_w and gate.  dx (NULL: not
- * wanted) may be dy, df may be dh; outputs overlap nothing else.  dpost_w, dpost_b,
+ * wanted) may be dy, df may be dh; outputs and ws overlap no other array.  dpost_w, dpost_b,
  * dpre_w, dpre_b [dim] and dgate [gates][dim] are contiguous, of grad_dtype, each NULL
  * where it is not wanted, and are written, not added to.  Sums over rows are fp32, in
  * an order that depends on the descriptor, rows and alignment only: equal calls give

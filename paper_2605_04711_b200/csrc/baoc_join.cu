@@ -840,24 +840,42 @@ int check_join(const baoc_join_t* e, int64_t rows, const std::string& what) {
     return BAOC_OK;
 }
 
-// An array of rows as the kernels see it.
+// An array of rows (or a vector per column: one row) as the kernels see it.
 struct Rows {
     const void* p;
-    int64_t step, width, eb;        // bytes from row to row, of a row, of an element
-    Rows(const void* p, int64_t stride, int dtype, int dim) : p(p), step((stride ? stride : dim) * elem_bytes(dtype)), width(dim * elem_bytes(dtype)), eb(elem_bytes(dtype)) {}
+    int64_t step, width, eb, n;     // bytes from row to row, of a row, of an element; rows
+    Rows(const void* p, int64_t stride, int dtype, int dim, int64_t n)
+        : p(p), step((stride ? stride : dim) * elem_bytes(dtype)), width(dim * elem_bytes(dtype)), eb(elem_bytes(dtype)), n(n) {}
     bool wide() const { return !p || (aligned(p, kJoinCols * eb) && step % (kJoinCols * eb) == 0); }     // a thread's columns in one access
     bool fits() const { return aligned(p, eb); }
 };
 // Whether the rows of two arrays share bytes.  (Rows of one buffer may lie between each other's.)
-bool overlap(const Rows& a, const Rows& b, int64_t rows) {
-    if (!a.p || !b.p || rows == 0) return false;
+bool overlap(const Rows& a, const Rows& b) {
+    if (!a.p || !b.p || a.n == 0 || b.n == 0) return false;
     const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
-    if (x >= y + (rows - 1) * b.step + b.width || y >= x + (rows - 1) * a.step + a.width) return false;
+    if (x >= y + (b.n - 1) * b.step + b.width || y >= x + (a.n - 1) * a.step + a.width) return false;
     if (a.step != b.step) return true;
     const int64_t off = ((y - x) % a.step + a.step) % a.step;
     return off < a.width || off + b.width > a.step;
 }
-bool same(const Rows& a, const Rows& b, int64_t rows) { return a.p == b.p && a.width == b.width && (a.step == b.step || rows == 1); }
+bool same(const Rows& a, const Rows& b) { return a.p == b.p && a.width == b.width && (a.step == b.step || a.n == 1); }
+// An output, and the input that it may be (null: none).
+struct Written {
+    const Rows* out;
+    const Rows* instead_of;
+};
+// Whether an output shares bytes with an input or another output in a way that is not allowed.
+template <int kOuts, int kIns>
+bool collide(const Written (&outs)[kOuts], const Rows* const (&ins)[kIns]) {
+    for (int i = 0; i < kOuts; ++i) {
+        for (const Rows* in : ins)
+            if (overlap(*outs[i].out, *in) && !(in == outs[i].instead_of && same(*outs[i].out, *in))) return true;
+        for (int j = 0; j < i; ++j)
+            if (overlap(*outs[i].out, *outs[j].out)) return true;
+    }
+    return false;
+}
+int64_t gates_of(int64_t rows, int64_t rows_per_gate) { return rows_per_gate > 0 && rows_per_gate < rows ? ceil_div(rows, rows_per_gate) : 1; }
 
 // How rows are spread over threads: their class, and what follows from it.  alone: a warp may take a row of 2 or 3 times 256 columns alone.
 struct Spread {
@@ -939,20 +957,21 @@ int baoc_join(const baoc_join_t* e, const void* x, const void* f, const float* p
     if (rows == 0) return BAOC_OK;
     if (!f || !pre_w || !y || !h) return fail_join(BAOC_E_INVALID, "baoc_join: null pointer");
     if ((post_b && !post_w) || (e->kind == BAOC_NORM_RMS && (post_b || pre_b))) return fail_join(BAOC_E_INVALID, "baoc_join: biases belong to layer norms");
-    const Rows rx(x, e->x_stride, e->stream_dtype, e->dim), rf(f, e->f_stride, e->branch_dtype, e->dim), ry(y, e->y_stride, e->stream_dtype, e->dim),
-        rh(h, e->h_stride, e->branch_dtype, e->dim);
+    const Rows rx(x, e->x_stride, e->stream_dtype, e->dim, rows), rf(f, e->f_stride, e->branch_dtype, e->dim, rows), ry(y, e->y_stride, e->stream_dtype, e->dim, rows),
+        rh(h, e->h_stride, e->branch_dtype, e->dim, rows);
+    auto vector = [&](const float* p) { return Rows(p, 0, BAOC_F32, e->dim, 1); };
+    const Rows rpost_w = vector(post_w), rpost_b = vector(post_b), rpre_w = vector(pre_w), rpre_b = vector(pre_b), rgate(gate, 0, BAOC_F32, e->dim, gates_of(rows, e->rows_per_gate));
     bool wide = e->dim % kJoinCols == 0;
     for (const Rows* r : {&rx, &rf, &ry, &rh}) {
         if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join: a pointer is not aligned to its elements");
         wide = wide && r->wide();
     }
-    for (const void* p : {static_cast<const void*>(post_w), static_cast<const void*>(post_b), static_cast<const void*>(gate), static_cast<const void*>(pre_w), static_cast<const void*>(pre_b)}) {
-        if (!aligned(p, 4)) return fail_join(BAOC_E_ALIGN, "baoc_join: a pointer is not aligned to its elements");
-        wide = wide && aligned(p, 16);
+    for (const Rows* r : {&rpost_w, &rpost_b, &rgate, &rpre_w, &rpre_b}) {
+        if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join: a pointer is not aligned to its elements");
+        wide = wide && aligned(r->p, 16);
     }
-    if ((overlap(ry, rx, rows) && !same(ry, rx, rows)) || overlap(ry, rf, rows) || (overlap(rh, rf, rows) && !same(rh, rf, rows)) || overlap(rh, rx, rows) ||
-        overlap(ry, rh, rows))
-        return fail_join(BAOC_E_INVALID, "baoc_join: y may be x and h may be f; arrays overlap in no other way");
+    if (collide({{&ry, &rx}, {&rh, &rf}}, {&rx, &rf, &rpost_w, &rpost_b, &rgate, &rpre_w, &rpre_b}))
+        return fail_join(BAOC_E_INVALID, "baoc_join: y may be x and h may be f; outputs overlap nothing else");
     JoinArgs a{static_cast<const char*>(x), static_cast<const char*>(f), static_cast<char*>(y), static_cast<char*>(h), post_w, post_b, gate, pre_w, pre_b,
                      rx.step, rf.step, ry.step, rh.step, rows, e->rows_per_gate < rows ? e->rows_per_gate : 0, 0, e->dim, e->kind == BAOC_NORM_LAYER, e->scale, e->eps};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -995,28 +1014,34 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
     if (!pre_w || !ws || (rows && (!y || !dh || !df || ((post_w || gate) && !f)))) return fail_join(BAOC_E_INVALID, "baoc_join_grad: null pointer");
     if (((post_b || dpost_w || dpost_b) && !post_w) || (dgate && !gate) || (!layer && (post_b || dpost_b || dpre_b)))
         return fail_join(BAOC_E_INVALID, "baoc_join_grad: a bias or a gradient of something that is not there");
-    const Rows ry(y, e->y_stride, e->stream_dtype, e->dim), rf(post_w || gate ? f : nullptr, e->f_stride, e->branch_dtype, e->dim),
-        rdy(dy, e->dy_stride, e->stream_dtype, e->dim), rdh(dh, e->dh_stride, e->branch_dtype, e->dim), rdx(dx, e->dx_stride, e->stream_dtype, e->dim),
-        rdf(df, e->df_stride, e->branch_dtype, e->dim);
+    const Rows ry(y, e->y_stride, e->stream_dtype, e->dim, rows), rf(post_w || gate ? f : nullptr, e->f_stride, e->branch_dtype, e->dim, rows),
+        rdy(dy, e->dy_stride, e->stream_dtype, e->dim, rows), rdh(dh, e->dh_stride, e->branch_dtype, e->dim, rows), rdx(dx, e->dx_stride, e->stream_dtype, e->dim, rows),
+        rdf(df, e->df_stride, e->branch_dtype, e->dim, rows);
+    const int64_t gates = gates_of(rows, e->rows_per_gate);
+    auto vector = [&](const void* p, int dtype) { return Rows(p, 0, dtype, e->dim, 1); };
+    const Rows rpost_w = vector(post_w, BAOC_F32), rpost_b = vector(post_b, BAOC_F32), rpre_w = vector(pre_w, BAOC_F32), rgate(gate, 0, BAOC_F32, e->dim, gates),
+        rdpost_w = vector(dpost_w, e->grad_dtype), rdpost_b = vector(dpost_b, e->grad_dtype), rdpre_w = vector(dpre_w, e->grad_dtype), rdpre_b = vector(dpre_b, e->grad_dtype),
+        rdgate(dgate, 0, e->grad_dtype, e->dim, gates);
     bool wide = e->dim % kJoinCols == 0;
     for (const Rows* r : {&ry, &rf, &rdy, &rdh, &rdx, &rdf}) {
         if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
         wide = wide && r->wide();
     }
-    for (const float* p : {post_w, post_b, gate, pre_w}) {
-        if (!aligned(p, 4)) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
-        wide = wide && aligned(p, 16);
+    for (const Rows* r : {&rpost_w, &rpost_b, &rgate, &rpre_w}) {
+        if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
+        wide = wide && aligned(r->p, 16);
     }
     void* outs[kJoinSums] = {};
     outs[kPreW] = dpre_w; outs[kPreB] = dpre_b; outs[kPostW] = dpost_w; outs[kPostB] = dpost_b; outs[kGate] = dgate;
-    for (const void* p : outs)
-        if (!aligned(p, elem_bytes(e->grad_dtype))) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
+    for (const Rows* r : {&rdpost_w, &rdpost_b, &rdgate, &rdpre_w, &rdpre_b})
+        if (!r->fits()) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: a pointer is not aligned to its elements");
     if (!aligned(ws, 256)) return fail_join(BAOC_E_ALIGN, "baoc_join_grad: workspace not 256-byte aligned");
     const int64_t need = grad_ws(e->dim, rows);
     if (ws_bytes < size_t(need)) return fail_join(BAOC_E_WORKSPACE, "baoc_join_grad: workspace too small");
-    if ((overlap(rdx, rdy, rows) && !same(rdx, rdy, rows)) || (overlap(rdf, rdh, rows) && !same(rdf, rdh, rows)) || overlap(rdx, ry, rows) || overlap(rdx, rf, rows) ||
-        overlap(rdx, rdh, rows) || overlap(rdf, ry, rows) || overlap(rdf, rf, rows) || overlap(rdf, rdy, rows) || overlap(rdx, rdf, rows))
-        return fail_join(BAOC_E_INVALID, "baoc_join_grad: dx may be dy and df may be dh; outputs overlap nothing else");
+    const Rows space(ws, 0, BAOC_F32, int(need / 4), 1);
+    if (collide({{&rdx, &rdy}, {&rdf, &rdh}, {&rdpost_w, nullptr}, {&rdpost_b, nullptr}, {&rdgate, nullptr}, {&rdpre_w, nullptr}, {&rdpre_b, nullptr}, {&space, nullptr}},
+                {&ry, &rf, &rdy, &rdh, &rpost_w, &rpost_b, &rgate, &rpre_w}))
+        return fail_join(BAOC_E_INVALID, "baoc_join_grad: dx may be dy and df may be dh; outputs and the workspace overlap nothing else");
     JoinGradArgs a{static_cast<const char*>(y), static_cast<const char*>(rf.p), static_cast<const char*>(dy), static_cast<const char*>(dh), static_cast<char*>(dx),
                    static_cast<char*>(df), post_w, post_b, gate, pre_w, {}, static_cast<float*>(ws), ry.step, rf.step, rdy.step, rdh.step, rdx.step, rdf.step, rows,
                    gate && e->rows_per_gate < rows ? e->rows_per_gate : 0, 0, e->dim, e->grad_dtype, e->scale, e->eps};

@@ -90,3 +90,51 @@ def test_a_workspace_serves_fewer_rows(dim):
         assert B._lib.baoc_join_grad_workspace_bytes(C.byref(_e(dim=dim)), rows, C.byref(n)) == B.OK
         assert n.value >= last
         last = n.value
+
+
+VECTORS = ("post_w", "post_b", "gate", "pre_w", "pre_b")
+
+
+@pytest.mark.parametrize("v", VECTORS)
+def test_outputs_that_lie_on_a_vector(v):
+    """A row of another CTA would be normed by what one has written: 4 rows of 16 columns, 256 bytes of y and 128 of h."""
+    e = C.byref(_e())
+    for out, size in (("y", 256), ("h", 128)):
+        for off in (0, 60, size - 4, -60):
+            assert _join(e, **{v: P << 9, out: (P << 9) - off // 4 * 4}) == B.E_INVALID
+    assert b"overlap" in B._lib.baoc_join_last_error()
+
+
+def test_gates_that_an_output_lies_on():
+    """Every group's gate counts: 2 rows a gate are 2 gates of 64 bytes, one a gate are 4."""
+    for per, gates in ((2, 2), (1, 4), (3, 2)):
+        e = C.byref(_e(rows_per_gate=per))
+        assert _join(e, y=(P << 4) + 64 * gates - 64) == B.E_INVALID and _grad(e, dx=(P << 6) + 64 * gates - 64) == B.E_INVALID
+        assert _grad(e, dpre_w=(P << 12) + 32 * gates - 32) == B.E_INVALID
+
+
+SUMS = ("dpost_w", "dpost_b", "dgate", "dpre_w", "dpre_b")
+
+
+@pytest.mark.parametrize("out", SUMS)
+def test_column_sums_that_lie_on_another_array(out):
+    e = C.byref(_e())
+    for at in (P, (P << 1) + 96, (P << 2) + 224, P << 3, P << 4, P << 5, (P << 6) + 32, P << 7, P << 8, (P << 9) + 96, (P << 15) + 256):
+        assert _grad(e, **{out: at}) == B.E_INVALID
+        assert b"overlap" in B._lib.baoc_join_last_error()
+    for other in SUMS:
+        if other != out:
+            assert _grad(e, **{out: P << 20, other: (P << 20) + 16}) == B.E_INVALID
+
+
+def test_a_workspace_that_lies_on_another_array():
+    e = C.byref(_e())
+    for at in (P, P << 1, P << 2, P << 3, P << 4, P << 5, P << 6, P << 7, P << 8, P << 9):
+        assert _grad(e, ws=at) == B.E_INVALID
+    for at in (P, P << 2):
+        assert _grad(e, ws=at - 256) == B.E_INVALID
+
+
+def test_a_gate_for_its_own_gradient():
+    e = C.byref(_e(grad_dtype=1, rows_per_gate=2))
+    assert _grad(e, dgate=P << 6) == B.E_INVALID and b"overlap" in B._lib.baoc_join_last_error()
