@@ -1167,17 +1167,17 @@ int baoc_linear(const baoc_linear_t* e, const void* x, const void* w, const floa
     if (!x || !w || !out || (!ws && ws_bytes)) return fail_linear(BAOC_E_INVALID, "baoc_linear: null pointer");
     const bool out_in = e->layout == BAOC_OUT_IN;
     const Matrix mx(x, tokens, e->n_in, e->x_stride, BAOC_BF16), mw(w, out_in ? e->n_out : e->n_in, out_in ? e->n_in : e->n_out, e->w_stride, BAOC_BF16),
-        mo(out, tokens, e->n_out, e->out_stride, e->out_dtype), mr(residual, tokens, e->n_out, e->residual_stride, e->out_dtype), mp(pre, tokens, e->n_out, e->pre_stride, BAOC_BF16);
-    for (const Matrix* t : {&mx, &mw, &mo, &mr, &mp})
+        mo(out, tokens, e->n_out, e->out_stride, e->out_dtype), mr(residual, tokens, e->n_out, e->residual_stride, e->out_dtype), mp(pre, tokens, e->n_out, e->pre_stride, BAOC_BF16),
+        mb(bias, 1, e->n_out, 0, BAOC_F32);
+    for (const Matrix* t : {&mx, &mw, &mo, &mr, &mp, &mb})
         if (!t->fits()) return fail_linear(BAOC_E_ALIGN, "baoc_linear: a pointer is not aligned to its elements");
-    if (!aligned(bias, 4)) return fail_linear(BAOC_E_ALIGN, "baoc_linear: a pointer is not aligned to its elements");
     if (!aligned(ws, 256)) return fail_linear(BAOC_E_ALIGN, "baoc_linear: workspace not 256-byte aligned");
     const Matrix space(ws, 1, int64_t(ws_bytes) / 2, 0, BAOC_BF16);
-    if (overlap(mo, mx) || overlap(mo, mw) || overlap(mp, mx) || overlap(mp, mw) || overlap(mo, mp) || overlap(mp, mr) ||
-        (overlap(mo, mr) && !(mo.p == mr.p && (mo.step == mr.step || tokens == 1))))
+    if (overlap(mo, mx) || overlap(mo, mw) || overlap(mp, mx) || overlap(mp, mw) || overlap(mo, mp) || overlap(mp, mr) || overlap(mo, mb) ||
+        overlap(mp, mb) || (overlap(mo, mr) && !(mo.p == mr.p && (mo.step == mr.step || tokens == 1))))
         return fail_linear(BAOC_E_INVALID, "baoc_linear: out may be residual; outputs overlap nothing else");
     if (ws_bytes)
-        for (const Matrix* t : {&mx, &mw, &mo, &mr, &mp})
+        for (const Matrix* t : {&mx, &mw, &mo, &mr, &mp, &mb})
             if (overlap(space, *t)) return fail_linear(BAOC_E_INVALID, "baoc_linear: the workspace overlaps an array");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     Packer pack(ws, ws_bytes);

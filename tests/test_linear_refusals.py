@@ -78,3 +78,12 @@ def test_plans():
         with pytest.raises(B.BaocError):
             B.Linear(**kw)
     assert B.Linear(64, 128).workspace_bytes(1000) == 0 and B.Linear(65, 128).workspace_bytes(1000) > 0
+
+
+def test_outputs_that_lie_on_the_bias():
+    """4 rows of 24 columns, 192 bytes of out and pre; 96 bytes of bias."""
+    e = C.byref(_e())
+    for out in ("out", "pre"):
+        for off in (0, 92, -188):
+            assert _product(e, **{out: (P << 2) + off}) == B.E_INVALID and b"overlap" in B._lib.baoc_linear_last_error()
+    assert _product(e, bias=(P << 8) + 4096, ws=P << 8, ws_bytes=8192) == B.E_INVALID
