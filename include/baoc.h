@@ -746,7 +746,7 @@ typedef struct {
  * (NULL for top = 0): the row's most probable tokens in falling order, the lower
  * token first where logits are equal, and their log probabilities.  Sums are fp32,
  * in an order that depends on n_tokens, vocab, dtype and the row's alignment only.
- * Pointers are aligned to their elements.  n_tokens <= 2^31 - 1, 0 queues nothing.
+ * Outputs overlap no other array.  Pointers are aligned to their elements.  n_tokens <= 2^31 - 1, 0 queues nothing.
  * One kernel; does not wait. */
 int baoc_logp(const baoc_logp_t* e, const void* logits, const void* ids, int64_t n_tokens, float* logp, float* entropy,
               float* stats, int32_t* top_ids, float* top_logp, baoc_stream_t stream);
@@ -754,7 +754,7 @@ int baoc_logp(const baoc_logp_t* e, const void* logits, const void* ids, int64_t
 /* dlogits[n_tokens][vocab] from dlogp[n_tokens] and dentropy[n_tokens] (NULL: the
  * entropy takes no gradient).  ids, scale and logits as in the call that wrote
  * stats; top is not read beyond its check.  dlogits may be logits itself, with the
- * same row stride (the logits are gone then), and overlaps it in no other way.
+ * same row stride (the logits are gone then), and overlaps nothing else.
  * Logits and dlogits that lie alike to 16 bytes take the wide path.  One kernel;
  * does not wait.  Errors of both: BAOC_E_INVALID, BAOC_E_ALIGN, BAOC_E_CUDA;
  * baoc_logp_last_error() returns the message of the calling thread's last failure. */

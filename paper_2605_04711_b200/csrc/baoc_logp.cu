@@ -713,6 +713,23 @@ int check_logp(const baoc_logp_t* e, int64_t n, const std::string& what) {
     return BAOC_OK;
 }
 
+// n rows of `row` bytes, `step` bytes apart.
+struct Extent {
+    const void* p;
+    int64_t n, step, row;
+};
+Extent vector_of(const void* p, int64_t n, int64_t elem) { return Extent{p, 1, n * elem, n * elem}; }
+// Whether two arrays share bytes.  (Rows of one buffer may lie between each other's, a vector behind the columns of a row.)
+bool overlap(const Extent& a, const Extent& b) {
+    if (!a.p || !b.p || a.n == 0 || b.n == 0) return false;
+    if (a.n == 1 && b.n > 1) return overlap(b, a);
+    const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
+    if (x >= y + (b.n - 1) * b.step + b.row || y >= x + (a.n - 1) * a.step + a.row) return false;
+    if (b.n > 1 && a.step != b.step) return true;
+    const int64_t off = ((y - x) % a.step + a.step) % a.step;
+    return off < a.row || off + b.row > a.step;
+}
+
 template <int DT, int kC, int kT>
 int launch_logp(const LogpArgs& a, int64_t n, cudaStream_t s) {
     if (n * kC > 0x7fffffff) return fail_logp(BAOC_E_INVALID, "baoc_logp: too many rows for one launch");
@@ -759,6 +776,15 @@ int baoc_logp(const baoc_logp_t* e, const void* logits, const void* ids, int64_t
     if (!aligned(logits, eb) || !aligned(ids, e->id_bits / 8) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 4) ||
         (e->top && (!aligned(top_ids, 4) || !aligned(top_logp, 4))))
         return fail_logp(BAOC_E_ALIGN, "baoc_logp: a pointer is not aligned to its elements");
+    const Extent ins[] = {{logits, n_tokens, stride * eb, e->vocab * eb}, vector_of(ids, n_tokens, e->id_bits / 8)},
+                 outs[] = {vector_of(logp, n_tokens, 4), vector_of(entropy, n_tokens, 4), vector_of(stats, n_tokens * 3, 4),
+                           vector_of(e->top ? top_ids : nullptr, n_tokens * e->top, 4), vector_of(e->top ? top_logp : nullptr, n_tokens * e->top, 4)};
+    for (const Extent& o : outs) {
+        for (const Extent& i : ins)
+            if (overlap(o, i)) return fail_logp(BAOC_E_INVALID, "baoc_logp: an output overlaps another array");
+        for (const Extent* q = outs; q != &o; ++q)
+            if (overlap(o, *q)) return fail_logp(BAOC_E_INVALID, "baoc_logp: an output overlaps another array");
+    }
     const LogpArgs a{static_cast<const char*>(logits), ids, e->id_bits, e->top, e->vocab, stride * eb, e->scale, logp, entropy, stats, top_ids, top_logp};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return e->dtype == BAOC_BF16 ? logp_of<BAOC_BF16>(a, n_tokens, s) : logp_of<BAOC_F32>(a, n_tokens, s);
@@ -778,11 +804,11 @@ int baoc_logp_grad(const baoc_logp_t* e, const void* logits, const void* ids, co
     const char* x = static_cast<const char*>(logits);
     char* d = static_cast<char*>(dlogits);
     const int64_t row = e->vocab * eb;
-    if (x < d + (n_tokens - 1) * out_step + row && d < x + (n_tokens - 1) * step + row && !(x == d && (step == out_step || n_tokens == 1))) {
-        // the rows of two arrays may still lie between each other's
-        const int64_t off = ((d - x) % step + step) % step;
-        if (step != out_step || off < row || off + row > step) return fail_logp(BAOC_E_INVALID, "baoc_logp_grad: dlogits overlaps logits and is not the same array");
-    }
+    const Extent to{d, n_tokens, out_step, row};
+    if (overlap(to, Extent{x, n_tokens, step, row}) && !(x == d && (step == out_step || n_tokens == 1)))
+        return fail_logp(BAOC_E_INVALID, "baoc_logp_grad: dlogits overlaps logits and is not the same array");
+    for (const Extent& v : {vector_of(ids, n_tokens, e->id_bits / 8), vector_of(stats, n_tokens * 3, 4), vector_of(dlogp, n_tokens, 4), vector_of(dentropy, n_tokens, 4)})
+        if (overlap(to, v)) return fail_logp(BAOC_E_INVALID, "baoc_logp_grad: dlogits overlaps an array of one value per token");
     const int64_t segments = ceil_div(row, int64_t(16) * kLogpBatch * kThreads);
     if (n_tokens * segments > 0x7fffffff) return fail_logp(BAOC_E_INVALID, "baoc_logp_grad: too many logits for one launch");
     const LogpGradArgs a{x, ids, stats, dlogp, dentropy, d, e->id_bits, int(segments), e->vocab, step, out_step, e->scale};

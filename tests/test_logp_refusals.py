@@ -51,3 +51,24 @@ def test_plans():
     for kw in (dict(vocab=0), dict(vocab=10, top=11), dict(vocab=10, scale=0.0), dict(vocab=1 << 31), dict(vocab=10, top=-1)):
         with pytest.raises(B.BaocError):
             B.LogProbs(**kw)
+
+
+def test_outputs_that_lie_on_another_array():
+    """4 rows of 100 bf16 logits (800 bytes), 32 bytes of ids, 16 of logp and entropy, 48 of stats, 32 of each of the alternatives."""
+    e, f = C.byref(_e()), B._lib.baoc_logp
+    good = [P, P << 1, 4, P << 2, P << 3, P << 4, P << 5, P << 6]
+    for i in (3, 4, 5, 6, 7):
+        for at in [P, P + 796, P << 1, (P << 1) + 28] + [a for j, a in enumerate(good) if j > 2 and j != i]:
+            assert f(e, *(at if j == i else a for j, a in enumerate(good)), None) == B.E_INVALID
+            assert b"overlaps" in B._lib.baoc_logp_last_error()
+
+
+def test_gradients_that_lie_on_another_array():
+    e, g = C.byref(_e()), B._lib.baoc_logp_grad
+    good = [P, P << 1, P << 2, P << 3, P << 4, 4, P << 5]
+    for i, size in ((1, 32), (2, 48), (3, 16), (4, 16)):
+        for at in (good[i], good[i] + size - 4, good[i] - 796):
+            assert g(e, *good[:6], at, None) == B.E_INVALID and b"overlaps" in B._lib.baoc_logp_last_error()
+    wide = C.byref(_e(stride=128, grad_stride=128))                     # 256 bytes from row to row, 200 of them logits
+    for at in (P + 192, P + 216, P - 4):                                # (48 bytes of stats: from 200 to 208 on they would lie in a gap)
+        assert g(wide, P, P << 1, at, P << 3, P << 4, 4, P, None) == B.E_INVALID
