@@ -779,14 +779,17 @@ class LogProbs:
              dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The logits' gradient from those of logp and (None: zero) of the entropy, fp32 and of ids' shape; stats from
         ``logprobs`` of the same logits and ids.  dlogits: of the logits' type (allocated when not given); it may be the logits
-        themselves, which are overwritten then."""
+        themselves, which are overwritten then.  Arrays that require a gradient are refused unless they are detached or gradients
+        are off."""
         if dlogits is None:
             dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
         n, dev, form = ids.numel(), logits.get_device(), _form(logits, ids, stats, dlogp, dentropy, dlogits)
         if form != self._gseen:
             self._gseen, same = None, ids
+            for name, t in (("logits", logits), ("stats", stats), ("dlogp", dlogp), ("dentropy", dentropy), ("dlogits", dlogits)):
+                _no_autograd("grad", name, t)
             dev, n, ids = self._call(self._g, "grad", logits, ids, dlogits, ((stats, 3 * n), (dlogp, n), (dentropy, n)))
-            if ids is same:                                 # (a copy of the ids is made anew)
+            if ids is same and not any(t is not None and t[4] for t in form):      # (a copy of the ids is made anew, whether autograd is on looked at anew)
                 self._gseen = form
         rc = _queue(dev, _lib.baoc_logp_grad, self._gref, logits.data_ptr(), ids.data_ptr(), stats.data_ptr(), dlogp.data_ptr(),
                     None if dentropy is None else dentropy.data_ptr(), n, dlogits.data_ptr())

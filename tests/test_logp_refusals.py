@@ -72,3 +72,16 @@ def test_gradients_that_lie_on_another_array():
     wide = C.byref(_e(stride=128, grad_stride=128))                     # 256 bytes from row to row, 200 of them logits
     for at in (P + 192, P + 216, P - 4):                                # (48 bytes of stats: from 200 to 208 on they would lie in a gap)
         assert g(wide, P, P << 1, at, P << 3, P << 4, 4, P, None) == B.E_INVALID
+
+
+@pytest.mark.parametrize("name", ["logits", "dlogp", "dentropy", "dlogits"])
+def test_gradients_that_autograd_would_lose(name):
+    """Like the other plans: what requires a gradient is refused while gradients are on (before the devices are looked at)."""
+    import torch
+    t = dict(logits=torch.zeros(4, 10), ids=torch.zeros(4, dtype=torch.int64), stats=torch.zeros(4, 3), dlogp=torch.zeros(4), dentropy=torch.zeros(4), dlogits=torch.zeros(4, 10))
+    t[name].requires_grad_(True)
+    with pytest.raises(B.BaocError, match="autograd does not see.*detach " + name):
+        B.LogProbs(10).grad(**t)
+    for call in (dict(t), t | {name: t[name].detach()}):
+        with torch.no_grad(), pytest.raises(B.BaocError, match="CUDA device"):
+            B.LogProbs(10).grad(**call)
