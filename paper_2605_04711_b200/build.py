@@ -5,6 +5,7 @@ Compiles every source under ``csrc/`` for sm_100a with nvcc and links
 """
 from __future__ import annotations
 
+import hashlib
 import os
 import shutil
 import subprocess
@@ -33,8 +34,16 @@ def needs_build(lib: str = LIB) -> bool:
     if not os.path.exists(lib):
         return True
     t = os.path.getmtime(lib)
-    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
+    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS + [os.path.abspath(__file__)]       # (the last holds the flags)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _read(path: str) -> bytes:
+    try:
+        with open(path, "rb") as f:
+            return f.read()
+    except FileNotFoundError:
+        return b""
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
@@ -48,18 +57,28 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     common = ["-std=c++17", "-O3", "-Wno-deprecated-gpu-targets", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
               "-Xcompiler", "-fPIC,-ffp-contract=off,-Wall"] + (["-DBAOC_CHECKED"] if checked else [])
     cuda_flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo"]
-    if verbose:
-        cuda_flags += ["-Xptxas", "-v"]
+    version = subprocess.run([nvcc, "--version"], check=True, capture_output=True).stdout
+    headers = [_read(h) for h in HEADERS]
 
     def compile_one(src: str) -> str:
+        """The source's object: kept while a digest of all that decides its content (compiler, command, source, headers) is the one beside it."""
         obj = os.path.join(bdir, src + ".o")
-        if not force and os.path.exists(obj) and os.path.getmtime(obj) > max(os.path.getmtime(d) for d in [os.path.join(CSRC, src)] + HEADERS):
-            return obj                                     # (only its own source or a header can have changed it)
         cmd = [nvcc] + common + (cuda_flags if src.endswith(".cu") else []) + \
               ["-c", os.path.join(CSRC, src), "-o", obj]
+        digest = hashlib.sha256()
+        for part in [version, *(c.encode() for c in cmd), _read(os.path.join(CSRC, src)), *headers]:
+            digest.update(len(part).to_bytes(8, "little") + part)
+        mark, now = obj + ".made_of", digest.hexdigest().encode()
+        if not force and os.path.exists(obj) and _read(mark) == now:
+            return obj
+        if os.path.exists(mark):
+            os.remove(mark)                                # (an interrupted compilation leaves none)
         if verbose:
+            cmd += ["-Xptxas", "-v"] if src.endswith(".cu") else []
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
+        with open(mark, "wb") as f:
+            f.write(now)
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:    # (one nvcc per source, side by side)
