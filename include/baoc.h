@@ -735,7 +735,7 @@ typedef struct {
     int64_t vocab;               /* logits of a row, 1 .. 2^31 - 1 */
     int32_t dtype;               /* of logits and dlogits: BAOC_F32 or BAOC_BF16 */
     int32_t id_bits;             /* 32 or 64: signed token ids */
-    float scale;                 /* 1 / temperature: finite, > 0 */
+    float scale;                 /* 1 / temperature: > 0, at most 2^127 */
     int32_t top;                 /* most probable tokens wanted: 0 .. 32, at most vocab */
     int64_t stride;              /* elements from row to row of logits: vocab .. 2^32, 0 for vocab */
     int64_t grad_stride;         /* the same of dlogits */

@@ -26,6 +26,7 @@ constexpr int kLogpMostCtas = 8;               // CTAs (a cluster) that share a 
 constexpr int kLogpCtaLogits = 4096;           // each with at least so many logits
 constexpr int kLogpShort = 64;                  // vectors a thread for which a row is given to fewer threads
 constexpr int64_t kLogpMaxStride = int64_t(1) << 32;
+constexpr float kLogpMaxScale = 1.7014118346046923e38f;      // 2^127: scale log2(e) stays finite
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeastExponent = -10000.f;     // 2^this is zero; it keeps 0 * -inf out of the entropy's sum
 
@@ -705,7 +706,7 @@ int check_logp(const baoc_logp_t* e, int64_t n, const std::string& what) {
     if (e->vocab < 1 || e->vocab > 0x7fffffff) return fail_logp(BAOC_E_INVALID, what + ": vocab must be in 1 .. 2^31 - 1");
     if (e->dtype != BAOC_BF16 && e->dtype != BAOC_F32) return fail_logp(BAOC_E_INVALID, what + ": dtype must be BAOC_BF16 or BAOC_F32");
     if (e->id_bits != 32 && e->id_bits != 64) return fail_logp(BAOC_E_INVALID, what + ": id_bits must be 32 or 64");
-    if (!std::isfinite(e->scale) || !(e->scale > 0.f)) return fail_logp(BAOC_E_INVALID, what + ": scale must be finite and above zero");
+    if (!(e->scale > 0.f) || !(e->scale <= kLogpMaxScale)) return fail_logp(BAOC_E_INVALID, what + ": scale must be above zero and at most 2^127");
     if (e->top < 0 || e->top > kLogpMaxTop || e->top > e->vocab) return fail_logp(BAOC_E_INVALID, what + ": top must be in 0 .. 32 and at most vocab");
     for (int64_t s : {e->stride, e->grad_stride})
         if (s && (s < e->vocab || s > kLogpMaxStride)) return fail_logp(BAOC_E_INVALID, what + ": a row stride must be 0 or in vocab .. 2^32");

@@ -293,3 +293,17 @@ def test_outputs_that_are_not_there(B):
     for name in ("logp", "entropy", "stats"):
         with pytest.raises(B.BaocError):
             plan.logprobs(x, ids, out=plan.buffers(4, dev)._replace(**{name: None}))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_scales_at_their_ends(B, dtype):
+    """All of the probability with the largest logits, or the same for every token."""
+    dev = "cuda:0"
+    x = torch.tensor([[0.0, 1.0, 1.0, -INF, 0.99]], device=dev).to(dtype)
+    ids = torch.tensor([1], device=dev)
+    cold, hot = B.LogProbs(5, scale=2.0 ** 127, top=3), B.LogProbs(5, scale=2.0 ** -149, top=3)
+    for plan, kept in ((cold, 2), (hot, 4)):
+        out = plan.logprobs(x, ids)
+        assert abs(float(out.logp) + math.log(kept)) <= 1e-6 and abs(float(out.entropy) - math.log(kept)) <= 1e-6 and out.top_ids.tolist() == [[1, 2, 4]]
+        one = torch.ones(1, device=dev)
+        assert bool(torch.isfinite(plan.grad(x, ids, out.stats, one)).all())

@@ -85,3 +85,15 @@ def test_gradients_that_autograd_would_lose(name):
     for call in (dict(t), t | {name: t[name].detach()}):
         with torch.no_grad(), pytest.raises(B.BaocError, match="CUDA device"):
             B.LogProbs(10).grad(**call)
+
+
+def test_scales_that_leave_the_numbers():
+    """Above 2^127 the scale in base 2 is infinite, and every row was NaN."""
+    for scale in (2.4e38, 3.4e38):
+        e = C.byref(_e(scale=scale))
+        assert B._lib.baoc_logp(e, None, None, 0, None, None, None, None, None, None) == B.E_INVALID
+        assert B._lib.baoc_logp_grad(e, None, None, None, None, None, 0, None, None) == B.E_INVALID
+        with pytest.raises(B.BaocError, match="2\\^127"):
+            B.LogProbs(10, scale=scale)
+    for scale in (2.0 ** 127, 1e-45):
+        B.LogProbs(10, scale=scale)
