@@ -1008,10 +1008,11 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
 // stages in flight; steps follow one another in every CTA, rounds of tiles too, and everything together takes at least the
 // operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.
 // Against the largest tiles that give every CTA one: 512 x 4096 into 4096 47 -> 20 us, the gradient of 4096 x 768 into 2304
-// 74 -> 39 us.  A split's sums meet at 6000 clocks.  Tiles of 256 columns are charged 18000: their sums take
-// longer to meet, and a gradient's two products in tiles of 64 share a launch (1000 x 513 into 1001 with gelu's fp32 dw takes 31 us with
-// 14000, 25 with 18000; 9000 also splits 512 x 4096 into 4096, 22 us instead of 20.5).  dw of 16384 x 768 into 768, split six ways, takes 24 us instead of 39, of
-// 16384 x 1024 into 1024 32 instead of 56.
+// 74 -> 39 us.  A split's sums meet at 6000 clocks.  Tiles of 256 columns are charged more: their sums take longer to meet, and they
+// have an SM to themselves.  How much is fitted to 800 calls (products and gradients of 1 to 16384 tokens, 48 to 8192 columns, drawn
+// evenly over the logarithms, where these tiles are within reach): the mean time over that of each call's best choice is 1.9 % with
+// 9000 clocks, 0.9 with 14000 to 16000, 1.0 with 18000, 1.5 with 24000 and 2.8 without such tiles.  dw of 16384 x 768 into 768, split
+// six ways, takes 25 us instead of 41, of 16384 x 1024 into 1024 32 instead of 56.
 enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit64, kSplit256 };
 struct Choice {
     Kind kind;
@@ -1040,7 +1041,7 @@ Choice choose(const Product& d, int split_most) {
     const int64_t wide_tiles = d.tiles(kTileM, 256);
     for (int parts = 2; parts <= kSplitMost && steps >= 4 * parts; ++parts)
         if (wide_tiles <= kClusters[parts])
-            consider(kSplit256, parts, 1, ceil_div(steps, parts), std::max<int64_t>((a_bytes + 256 * kRowBytes) / 64, 2800 / SplitShape<256>::kStages), 18000);
+            consider(kSplit256, parts, 1, ceil_div(steps, parts), std::max<int64_t>((a_bytes + 256 * kRowBytes) / 64, 2800 / SplitShape<256>::kStages), 16000);
     return best;
 }
 
