@@ -485,7 +485,8 @@ int baoc_profile_last(baoc_t* h, float* ms2);
  * gather, 4 first finalize sweep, 5 later sweeps, 6 / 7 row-column reduction of
  * the window / of the step, 8 its combine, 9 fused step, 10 the self-test, 11 the norms of the
  * factored tuple's Adafactor options, 14 / 15 gradient norm / clip, 16 / 17 grouping / sums of the
- * token table's gradient, 18 the join's gradient.
+ * token table's gradient, 18 the join's gradient and its sums, 19 the laying out of a matrix product's operands, 20 its gradient's
+ * slopes and column sums.
  *
  * baoc_check_selftest: queues a one-thread kernel that runs the range check on
  * numbers that violate it (a 32-byte range that starts 16 bytes before the end

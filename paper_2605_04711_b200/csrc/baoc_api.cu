@@ -1034,7 +1034,7 @@ int baoc_check_status(baoc_check_t* out) {
 #ifdef BAOC_CHECKED
     out->enabled = 1;
     if (cudaDeviceSynchronize() != cudaSuccess) return BAOC_E_CUDA;
-    int (*const fetch[])(CheckRecord*) = {stats_check_fetch, finalize_check_fetch, step_check_fetch, clip_check_fetch, embed_check_fetch, join_check_fetch};
+    int (*const fetch[])(CheckRecord*) = {stats_check_fetch, finalize_check_fetch, step_check_fetch, clip_check_fetch, embed_check_fetch, join_check_fetch, linear_check_fetch};
     for (auto f : fetch) {
         CheckRecord r{};
         if (f(&r) != 0) return BAOC_E_CUDA;

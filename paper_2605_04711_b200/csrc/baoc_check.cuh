@@ -7,7 +7,8 @@
 // offending numbers) and the CTA returns without touching memory: nothing traps, nothing asserts, the context stays
 // usable, and the host reads the record with baoc_check_status().  Caller-owned arrays (gradients, parameters), whose
 // true extents the library cannot know, are covered from the outside: the test harness surrounds every buffer with
-// guard words and verifies them after the launches.
+// guard words and verifies them after the launches; the log probabilities and the forward join touch nothing else.  The
+// matrix products read their operands, laid out in the workspace or not, through tensor maps, which bound every copy.
 //
 // In a normal build the macros below expand to nothing, the kernels keep their signatures and no check is compiled.
 #pragma once
@@ -23,7 +24,8 @@ enum CheckCode : unsigned int { kChkNone = 0, kChkTileIndex = 1, kChkBlockIndex 
 enum CheckKernel : unsigned int {
     kKerStatsStep = 1, kKerStatsCombine = 2, kKerSampleGather = 3, kKerFinalSums = 4, kKerFinalHist = 5, kKerMomentReduce = 6,
     kKerFactoredReduce = 7, kKerFactoredCombine = 8, kKerFusedStep = 9, kKerSelfTest = 10, kKerFactoredNorms = 11, kKerFinalLast = 12, kKerSelectFirst = 13,
-    kKerGradNorm = 14, kKerGradClip = 15, kKerEmbedGroup = 16, kKerEmbedGrad = 17, kKerJoinGrad = 18
+    kKerGradNorm = 14, kKerGradClip = 15, kKerEmbedGroup = 16, kKerEmbedGrad = 17, kKerJoinGrad = 18,
+    kKerLinearRepack = 19, kKerLinearSlope = 20
 };
 #ifdef BAOC_CHECKED
 #define BAOC_CHECK_PARAM , const CheckCtx ck

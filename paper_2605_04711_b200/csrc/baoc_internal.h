@@ -462,6 +462,7 @@ int step_check_fetch(CheckRecord* out);
 int clip_check_fetch(CheckRecord* out);
 int embed_check_fetch(CheckRecord* out);
 int join_check_fetch(CheckRecord* out);
+int linear_check_fetch(CheckRecord* out);
 int launch_check_selftest(cudaStream_t s);
 // Adafactor's options: per tile of the given blocks the sums of u^2 and theta^2, then per block the clip factor and the
 // step size (ids: the blocks, n of them; tiles: their stretch of the tile table).

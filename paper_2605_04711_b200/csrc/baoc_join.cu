@@ -779,13 +779,16 @@ __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, cl
 
 // The CTAs' sums, 32 columns per CTA: every warp adds each 32nd CTA's, then the warps' sums are added in order.
 // blockIdx.y: which sum; from kJoinSums on, groups of a gate that several CTAs have rows of.
-__global__ void __launch_bounds__(1024) join_sums_kernel(const JoinGradArgs g, int ctas, int64_t groups) {
+__global__ void __launch_bounds__(1024) join_sums_kernel(const JoinGradArgs g, int ctas, int64_t groups BAOC_CHECK_PARAM) {
     __shared__ float sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int col = int(blockIdx.x) * 32 + lane;
     begin_in_row();
     auto total = [&](int64_t c0, int64_t c1, int64_t group, int k, int64_t at) {
         float s = 0.f;
+#ifdef BAOC_CHECKED
+        if (c0 <= c1 && !check_range(ck, kKerJoinGrad, g.part + c0 * (kJoinSums + 1) * g.dim, 4 * (c1 - c0 + 1) * (kJoinSums + 1) * g.dim, 1)) return;
+#endif
         if (col < g.dim)
 #pragma unroll 8
             for (int64_t c = c0 + warp; c <= c1; c += 32) {
@@ -1079,7 +1082,7 @@ int baoc_join_grad(const baoc_join_t* e, const void* y, const void* f, const voi
     if (!any) return BAOC_OK;
     const int64_t groups = a.rows_per_gate && dgate ? ceil_div(rows, a.rows_per_gate) : 0;
     const dim3 grid(unsigned(ceil_div(e->dim, 32)), unsigned(kJoinSums + std::min<int64_t>(groups, 1024)));
-    return launched(launch_in_row(join_sums_kernel, grid, 1024, 0, 1, s, a, ctas, groups), "join_sums_kernel");
+    return launched(launch_in_row(join_sums_kernel, grid, 1024, 0, 1, s, a, ctas, groups BAOC_CHECK_ARG(ck)), "join_sums_kernel");
 } catch (const std::bad_alloc&) {
     return BAOC_E_INVALID;
 }

@@ -17,6 +17,7 @@
 #include <string>
 #include <utility>
 
+#include "baoc_check.cuh"
 #include "baoc_tensor.cuh"
 
 namespace baoc {
@@ -717,7 +718,7 @@ __global__ void __launch_bounds__(SplitShape<kN>::kThreads, kN == 64 ? 2 : 1) pr
 struct Repack { const char* from; char* to; int64_t from_step, to_step, rows; int cols; };
 struct Repacks { Repack r[3]; int64_t ends[3]; int n; };       // ends: running counts of 8-column pieces
 
-__global__ void __launch_bounds__(kThreads) repack_kernel(const Repacks g) {
+__global__ void __launch_bounds__(kThreads) repack_kernel(const Repacks g BAOC_CHECK_PARAM) {
     begin_in_row();
     for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < g.ends[g.n - 1]; i += int64_t(gridDim.x) * kThreads) {
         int which = 0;
@@ -727,6 +728,9 @@ __global__ void __launch_bounds__(kThreads) repack_kernel(const Repacks g) {
         const int pieces = (r.cols + 7) / 8;
         const int64_t row = at / pieces;
         const int col = int(at - row * pieces) * 8;
+#ifdef BAOC_CHECKED
+        if (!check_range(ck, kKerLinearRepack, r.to + row * r.to_step + 2 * col, 16, which)) return;
+#endif
         const uint16_t* p = reinterpret_cast<const uint16_t*>(r.from + row * r.from_step) + col;
         uint16_t v[8];
 #pragma unroll
@@ -784,13 +788,24 @@ __device__ __forceinline__ void store8(char* row, int base, int lane, int n, flo
 
 // kWide: n is a multiple of 8, and the rows of dout and pre start on 16-byte boundaries.
 template <int kAct, bool kWide>
-__global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
+__global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g BAOC_CHECK_PARAM) {
     constexpr bool kPre = kAct != BAOC_ACT_NONE;
     __shared__ float sh[8][256];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, base = int(blockIdx.x) * 256;
     const int64_t first = int64_t(blockIdx.y) * g.rows_per_part, end = min64(g.rows, first + g.rows_per_part);
     float sum[8] = {};
     begin_in_row();
+#ifdef BAOC_CHECKED
+    {
+        const int cols = min(256, g.n - base);
+        int what = 0;
+        for (char* dz : {g.dz, g.dz_mid, g.dz_low}) {
+            if (dz && first < end && !check_range(ck, kKerLinearSlope, dz + first * g.dz_step + 2 * base, (end - 1 - first) * g.dz_step + 2 * cols, what)) return;
+            ++what;
+        }
+        if (g.part && !check_range(ck, kKerLinearSlope, g.part + int64_t(blockIdx.y) * g.n + base, 4ll * cols, 3)) return;
+    }
+#endif
     auto one_row = [&](int64_t row, float (&d)[8], const float (&z)[8]) {
         if constexpr (kPre) {
 #pragma unroll
@@ -835,10 +850,13 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeArgs g) {
 }
 
 // The parts' column sums, 32 columns per CTA: every warp adds each 32nd part, then the warps' sums are added in order.
-__global__ void __launch_bounds__(1024) slope_sums_kernel(const float* __restrict__ part, int parts, int n, char* db, int f32) {
+__global__ void __launch_bounds__(1024) slope_sums_kernel(const float* __restrict__ part, int parts, int n, char* db, int f32 BAOC_CHECK_PARAM) {
     __shared__ float sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = int(blockIdx.x) * 32 + lane;
     begin_in_row();
+#ifdef BAOC_CHECKED
+    if (!check_range(ck, kKerLinearSlope, part, 4ll * parts * n, 4)) return;
+#endif
     float s = 0.f;
     if (col < n)
         for (int p = warp; p < parts; p += 32) s += part[int64_t(p) * n + col];
@@ -1099,10 +1117,11 @@ struct Packer {
         }
         return Matrix(p, t.rows, t.cols, packed_step(t.cols) / 2, BAOC_BF16);
     }
-    int launch(cudaStream_t s) const {
+    int launch(cudaStream_t s, const CheckCtx& ck) const {
+        (void)ck;
         if (!todo.n) return BAOC_OK;
         const unsigned grid = unsigned(std::min<int64_t>(ceil_div(todo.ends[todo.n - 1], kThreads), 148 * 16));
-        return launched(launch_in_row(repack_kernel, dim3(grid), kThreads, 0, 1, s, todo), "repack_kernel");
+        return launched(launch_in_row(repack_kernel, dim3(grid), kThreads, 0, 1, s, todo BAOC_CHECK_ARG(ck)), "repack_kernel");
     }
 };
 
@@ -1121,6 +1140,8 @@ int64_t slope_bytes(int64_t tokens, int64_t n) {
 bool off_grid(int64_t stride, int64_t cols, int anywhere) { return anywhere || (stride ? stride : cols) % 8; }
 
 }  // namespace
+
+BAOC_DEFINE_CHECK_FETCH(linear_check_fetch)
 
 }  // namespace baoc
 
@@ -1184,7 +1205,8 @@ int baoc_linear(const baoc_linear_t* e, const void* x, const void* w, const floa
     Packer pack(ws, ws_bytes);
     const Matrix a = pack.operand(mx), b = pack.operand(mw);
     if (!pack.fits) return fail_linear(BAOC_E_WORKSPACE, "baoc_linear: workspace too small");
-    if ((rc = pack.launch(s))) return rc;
+    const CheckCtx ck{static_cast<char*>(ws), static_cast<char*>(ws) + ws_bytes, 0, 0, 0};
+    if ((rc = pack.launch(s, ck))) return rc;
     Product d{Operands{{&a}, {&b}}, mo, mp, {}};
     ProductArgs& g = d.g;
     g.m = int(tokens); g.n = e->n_out; g.k_tiles = int(ceil_div(e->n_in, kTileK)); g.passes = 1;
@@ -1263,14 +1285,15 @@ int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const
     const int64_t parts = slope_parts(tokens, e->n_out, &g.rows_per_part);
     if (db) g.part = reinterpret_cast<float*>(pack.take(slope_bytes(tokens, e->n_out)));
     if (!pack.fits) return fail_linear(BAOC_E_WORKSPACE, "baoc_linear_grad: workspace too small");
-    if ((rc = pack.launch(s))) return rc;
+    const CheckCtx ck{static_cast<char*>(ws), static_cast<char*>(ws) + ws_bytes, 0, 0, 0};
+    if ((rc = pack.launch(s, ck))) return rc;
     if (g.dz || g.part) {
         g.dout = md.p; g.pre = mp.p; g.dout_step = md.step; g.pre_step = mp.step; g.dz_step = packed_step(e->n_out);
         g.rows = tokens; g.n = e->n_out;
         const dim3 grid(unsigned(ceil_div(e->n_out, 256)), unsigned(parts));
         const bool wide = e->n_out % 8 == 0 && md.wide() && (!act || mp.wide());
         auto go = [&](auto a) {
-            return launched(launch_in_row(wide ? slope_kernel<decltype(a)::value, true> : slope_kernel<decltype(a)::value, false>, grid, kThreads, 0, 1, s, g), "slope_kernel");
+            return launched(launch_in_row(wide ? slope_kernel<decltype(a)::value, true> : slope_kernel<decltype(a)::value, false>, grid, kThreads, 0, 1, s, g BAOC_CHECK_ARG(ck)), "slope_kernel");
         };
         using std::integral_constant;
         switch (e->act) {
@@ -1282,7 +1305,7 @@ int baoc_linear_grad(const baoc_linear_t* e, const void* x, const void* w, const
         }
         if (rc) return rc;
         if (g.part && (rc = launched(launch_in_row(slope_sums_kernel, dim3(unsigned(ceil_div(e->n_out, 32))), 1024, 0, 1, s, static_cast<const float*>(g.part), int(parts),
-                                                   int(e->n_out), static_cast<char*>(db), int(e->grad_dtype == BAOC_F32)), "slope_sums_kernel")))
+                                                   int(e->n_out), static_cast<char*>(db), int(e->grad_dtype == BAOC_F32) BAOC_CHECK_ARG(ck)), "slope_sums_kernel")))
             return rc;
     }
     // (the longer sums first: what the second product's shorter ones leave uneven is less)

@@ -428,3 +428,19 @@ def test_long_sums_of_few_tiles(B, m, k, n, layout, dtype):
     again = torch.empty_like(dw)
     p.grad(x, _w(w, layout), dout, dw=again)
     assert torch.equal(dw, again)
+
+
+def test_these_cases_run_clean_under_the_checked_build():
+    """Shapes whose operands go through the workspace, on the library whose kernels validate what they touch of it first."""
+    import os
+    import subprocess
+    import sys
+    from paper_2605_04711_b200 import build
+    if os.environ.get("BAOC_CHECKED") == "1":
+        return                                                          # this is the child
+    build.build(checked=True)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_linear.py", "-m", "gpu", "-x", "-q", "-k", "exact or random or strides or workspaces or few_tiles"],
+                       cwd=root, env=dict(os.environ, BAOC_CHECKED="1"), capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+    assert " passed" in r.stdout and "failed" not in r.stdout
