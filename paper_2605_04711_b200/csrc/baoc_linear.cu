@@ -62,8 +62,10 @@ struct ProductArgs {
     const char* residual;
     const float* bias;
     int64_t out_step, pre_step, residual_step;      // bytes
-    int out_wide, pre_wide, residual_wide;           // 16-byte accesses fit; out and pre are then stored by tiled copies
+    int out_wide, pre_wide, residual_wide;           // 16-byte accesses fit; kTiled (out, pre): tiled copies store it
 };
+
+constexpr int kTiled = 2;
 
 struct Maps { CUtensorMap a[3], b[3], out, pre; };
 
@@ -348,7 +350,7 @@ struct Writer {
             }
         }
         if (g.pre) {
-            if (g.pre_wide) send(&maps.pre, 0, col, int(row0), v);
+            if (g.pre_wide == kTiled) send(&maps.pre, 0, col, int(row0), v);
             else store_rows(g.pre, g.pre_step, 0, row0, col, left, v);
         }
         apply_act(v, g.act);
@@ -357,7 +359,7 @@ struct Writer {
             else if (row0 + lane < g.m) add_wide(g.residual + (row0 + lane) * g.residual_step + int64_t(col) * (g.out_f32 ? 4 : 2), g.out_f32, v);
             __syncwarp();
         }
-        if (g.out_wide) send(&maps.out, g.out_f32, col, int(row0), v);
+        if (g.out_wide == kTiled) send(&maps.out, g.out_f32, col, int(row0), v);
         else store_rows(g.out, g.out_step, g.out_f32, row0, col, left, v);
         __syncwarp();
     }
@@ -906,6 +908,8 @@ struct Matrix {
     Matrix(const void* p, int64_t rows, int64_t cols, int64_t stride, int dtype)
         : p(static_cast<const char*>(p)), rows(rows), cols(cols), step((stride ? stride : cols) * elem_bytes(dtype)), eb(elem_bytes(dtype)) {}
     bool wide() const { return aligned(p, 16) && step % 16 == 0; }
+    // A tiled store writes whole units of 16 bytes: rows that end inside one, in a buffer of wider rows, would lose what lies behind them.
+    int width() const { return !wide() ? 0 : (cols * eb % 16 ? 1 : kTiled); }
     bool fits() const { return aligned(p, eb); }
     int64_t end() const { return (rows - 1) * step + cols * eb; }
 };
@@ -966,8 +970,8 @@ int fill_problem(const Product& d, int m, int n, int b_rows, bool stores, Proble
     *tiles = int(t);
     bool ok = true;
     for (int i = 0; i < d.g.passes; ++i) ok = ok && encode(&p->maps.a[i], *d.o.a[i], d.g.a_mn ? kTileK : d.g.a_rows) && encode(&p->maps.b[i], *d.o.b[i], d.g.b_mn ? kTileK : b_rows);
-    if (stores && d.g.out_wide) ok = ok && encode(&p->maps.out, d.out, 32, 32);
-    if (stores && d.g.pre && d.g.pre_wide) ok = ok && encode(&p->maps.pre, d.pre, 32, 32);
+    if (stores && d.g.out_wide == kTiled) ok = ok && encode(&p->maps.out, d.out, 32, 32);
+    if (stores && d.g.pre && d.g.pre_wide == kTiled) ok = ok && encode(&p->maps.pre, d.pre, 32, 32);
     return ok ? BAOC_OK : fail_linear(BAOC_E_CUDA, "the driver refused a tensor map");
 }
 
@@ -1046,7 +1050,7 @@ Choice choose(const Product& d, int split_most) {
         if (best.parts == 0 || cost < least) { best = Choice{kind, parts}; least = cost; }
     };
     auto whole = [&](Kind kind, int ctas, int n, int64_t products) {
-        consider(kind, 1, ceil_div(d.tiles(kTileM * ctas, n), 148 / ctas), steps, std::max<int64_t>({products, (a_bytes + n / ctas * kRowBytes) / 64, 2800 / 6}), 3000 + (g.out_wide ? 0 : 32 * n));
+        consider(kind, 1, ceil_div(d.tiles(kTileM * ctas, n), 148 / ctas), steps, std::max<int64_t>({products, (a_bytes + n / ctas * kRowBytes) / 64, 2800 / 6}), 3000 + (g.out_wide == kTiled ? 0 : 32 * n));
     };
     if (!d.chunked()) whole(kPairs256, 2, 256, 512);
     whole(kPairs128, 2, 128, 256);
@@ -1070,8 +1074,8 @@ int form_products(Product* d, int count, int split_most, cudaStream_t s) {
     int parts[2];
     for (int i = 0; i < count; ++i) {
         ProductArgs& g = d[i].g;
-        g.out = const_cast<char*>(d[i].out.p); g.out_step = d[i].out.step; g.out_f32 = d[i].out.eb == 4; g.out_wide = d[i].out.wide();
-        g.pre = const_cast<char*>(d[i].pre.p); g.pre_step = d[i].pre.step; g.pre_wide = d[i].pre.wide();
+        g.out = const_cast<char*>(d[i].out.p); g.out_step = d[i].out.step; g.out_f32 = d[i].out.eb == 4; g.out_wide = d[i].out.width();
+        g.pre = const_cast<char*>(d[i].pre.p); g.pre_step = d[i].pre.step; g.pre_wide = d[i].pre.width();
         g.a_rows = g.a_mn ? kTileM : std::min(kTileM, int(round_up(g.m, 8)));
         const Choice c = choose(d[i], split_most);
         kind[i] = c.kind;

@@ -444,3 +444,49 @@ def test_these_cases_run_clean_under_the_checked_build():
                        cwd=root, env=dict(os.environ, BAOC_CHECKED="1"), capture_output=True, text=True, timeout=600)
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
     assert " passed" in r.stdout and "failed" not in r.stdout
+
+
+@pytest.mark.parametrize("m,k,n,stride", [(391, 11, 7, 8), (80, 6, 7, 8), (1, 64, 5, 8), (3, 2048, 513, 520), (300, 64, 257, 264), (1000, 72, 1001, 1008), (4000, 200, 1005, 1024), (4096, 2048, 770, 784)])
+@pytest.mark.parametrize("act", ["none", "relu"])
+def test_what_lies_behind_a_rows_end_stays(B, m, k, n, stride, act):
+    """Rows on the 16-byte grid that end off it, in buffers of wider rows: the columns behind them and the row behind the last stay."""
+    x, w, dout = _ints((m, k), 1), _ints((n, k), 2), _ints((m, n), 3)
+    z = x.double() @ w.double().t()
+    for dtype in (BF, F):
+        r = _ints((m, n), 4, 9, dtype)
+        out, res, pre = (torch.full((m + 1, stride), 7.0, dtype=t, device=DEV) for t in (dtype, dtype, BF))
+        res[:m, :n] = r
+        p = B.Linear(k, n, act)
+        p.product(x, w, residual=res[:m, :n], out=out[:m, :n], pre=pre[:m, :n])
+        assert torch.equal(out[:m, :n], (_act(z, act) + r.double()).to(dtype)) and torch.equal(pre[:m, :n], z.to(BF))
+        p.product(x, w, residual=res[:m, :n], out=res[:m, :n])
+        assert torch.equal(res[:m, :n], out[:m, :n])
+        for a in (out, res, pre):
+            assert bool((a[:, n:] == 7).all()) and bool((a[m] == 7).all())
+        # dx is [m, n] of a layer from n to k columns, dw [n, k] or [k, n]
+        dz = dout.double().t() @ x.double()
+        dw, dx = torch.full((k + 1, stride), 7.0, dtype=dtype, device=DEV), torch.full((m + 1, stride), 7.0, dtype=BF, device=DEV)
+        B.Linear(k, n, layout="in_out").grad(x, None, dout, dw=dw[:k, :n])
+        B.Linear(n, k).grad(None, w.t().contiguous(), x, dx=dx[:m, :n])
+        assert torch.equal(dw[:k, :n], dz.t().to(dtype)) and torch.equal(dx[:m, :n], z.to(BF))
+        for a, rows in ((dw, k), (dx, m)):
+            assert bool((a[:, n:] == 7).all()) and bool((a[rows] == 7).all())
+
+
+@pytest.mark.parametrize("m,k,n,stride", [(40, 7, 16, 8), (391, 13, 64, 16), (5, 513, 512, 520), (300, 1001, 256, 1008), (1000, 70, 520, 80), (2000, 515, 1024, 1024)])
+def test_what_lies_behind_a_rows_end_is_not_read(B, m, k, n, stride):
+    """The same of operands: NaN behind their rows reaches no sum, whichever of their dimensions is summed over."""
+    def cut(t):
+        wide = torch.full((t.shape[0] + 1, stride), float("nan"), dtype=BF, device=DEV)
+        wide[:t.shape[0], :t.shape[1]] = t
+        return wide[:t.shape[0], :t.shape[1]]
+
+    x, w, d = _ints((m, k), 1), _ints((n, k), 2), _ints((m, n), 3)
+    p, dw, dx = B.Linear(k, n), torch.empty((n, k), device=DEV), torch.empty((m, n), dtype=BF, device=DEV)
+    assert torch.equal(p.product(cut(x), cut(w), out_dtype=F), (x.double() @ w.double().t()).float())
+    p.grad(cut(x), None, d, dw=dw)                                                 # dw = d^T x
+    assert torch.equal(dw, (d.double().t() @ x.double()).float())
+    back = B.Linear(n, k, layout="in_out")                                         # w [n, k]: dx = dz w^T, summed over k
+    back.grad(None, cut(w), cut(x), dx=dx)
+    assert torch.equal(dx, (x.double() @ w.double().t()).to(BF))
+    assert torch.equal(B.Linear(n, k, layout="in_out").product(d, cut(w), out_dtype=F), (d.double() @ w.double()).float())
