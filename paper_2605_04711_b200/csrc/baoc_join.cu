@@ -37,7 +37,7 @@ constexpr int kJoinSums = 5;                   // column sums of the gradient: w
 // once a row: 65536 x 768 bf16 layer norms forwards 110 -> 73 us against three warps).  Classes 4, 5 and 6: a CTA of as many warps as the row
 // needs, up to 8, 16 and 32, 8 columns a thread (what differs is the registers that a thread may have).  Few rows of 2 or 3 times
 // 256 columns are of class 4 too: with one row a warp at most there is nothing to pay shuffles for, and a lane's loads wait for one another
-// (one bf16 row of 768, layer norms: 4.9 -> 3.3 us, its gradient 8.3 -> 5.9, of 296 rows 10.8 -> 9.2; at 592 both ways take as long).
+// (one bf16 row of 768, layer norms: 4.9 -> 3.3 us, its gradient 8.3 -> 6.1, of 296 rows 10.8 -> 9.4; at 592 both ways take as long).
 __host__ __device__ constexpr bool solo(int c) { return c <= 3; }
 __host__ __device__ constexpr int chunks_of(int c) { return c <= 3 ? c : 1; }
 __host__ __device__ constexpr int class_threads(int c) { return c <= 3 ? 32 * kSoloWarps : (c == 4 ? 256 : (c == 5 ? 512 : 1024)); }
@@ -415,13 +415,13 @@ template <int S, int B, bool kLayer, int kClass, bool kWide>
 __global__ void __launch_bounds__(class_threads(kClass), class_blocks(kClass, class_grad_warps(kClass))) join_grad_kernel(const JoinGradArgs g BAOC_CHECK_PARAM) {
     constexpr bool kSolo = solo(kClass);
     constexpr int kTeams = kSolo ? kSoloWarps : 1, kC = chunks_of(kClass), kSums = kLayer ? 4 : 2;
-    // The sums lie in shared memory where the registers have a row of several chunks, or are few (65536 x 512 bf16 layer norms: 109 us, in
-    // registers 126), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
+    // The sums lie in shared memory where the registers have a row of several chunks, or are few (65536 x 512 bf16 layer norms with a
+    // gate: 109 us against 126 in registers, 95 with what came later), else in registers (65536 x 256 bf16 layer norms: 56 us, in shared memory 68).
     constexpr bool kShared = kClass == 2 || kClass == 3 || kClass == 6;
     constexpr bool kAhead = kClass == 4 || kClass == 5;      // the next row is fetched into registers,
     constexpr bool kStaged = (kSolo || kClass == 6) && kWide && S == BAOC_BF16 && B == BAOC_BF16;     // or into shared memory (16 bytes a thread and array)
     // Kept vectors: the weights and the gate (of a segment); pre's weight alone where shared memory has no room for all of them, the sums and a
-    // staged row (8192 x 8192 bf16 layer norms: 296 us, 357 with the vectors and no staged row).
+    // staged row (8192 x 8192 bf16 layer norms: 312 us, 357 with the vectors and no staged row).
     constexpr int kVectors = kClass == 6 && kLayer ? 1 : 3;
     using Stream = RowPart<S, kClass, kWide>;
     using Branch = RowPart<B, kClass, kWide>;

@@ -1029,12 +1029,12 @@ int launch_split(const Product* d, int count, int parts, cudaStream_t s) {
 // time or the copies their bytes at 64 a clock and SM (what L2 gives one), and no less than a copy's way (2800 clocks) over the
 // stages in flight; steps follow one another in every CTA, rounds of tiles too, and everything together takes at least the
 // operands' bytes at 3400 a clock (HBM).  Rows off the 16-byte grid are written by the warps themselves, 32 clocks a column.
-// Against the largest tiles that give every CTA one: 512 x 4096 into 4096 47 -> 20 us, the gradient of 4096 x 768 into 2304
-// 74 -> 39 us.  A split's sums meet at 6000 clocks.  Tiles of 256 columns are charged more: their sums take longer to meet, and they
+// Against the largest tiles that give every CTA one: 512 x 4096 into 4096 47 -> 18 us, the gradient of 4096 x 768 into 2304
+// 74 -> 36 us.  A split's sums meet at 6000 clocks.  Tiles of 256 columns are charged more: their sums take longer to meet, and they
 // have an SM to themselves.  How much is fitted to 800 calls (products and gradients of 1 to 16384 tokens, 48 to 8192 columns, drawn
 // evenly over the logarithms, where these tiles are within reach): the mean time over that of each call's best choice is 1.9 % with
 // 9000 clocks, 0.9 with 14000 to 16000, 1.0 with 18000, 1.5 with 24000 and 2.8 without such tiles.  dw of 16384 x 768 into 768, split
-// six ways, takes 25 us instead of 41, of 16384 x 1024 into 1024 32 instead of 56.
+// six ways, takes 26 us instead of 41, of 16384 x 1024 into 1024 33 instead of 56.
 enum Kind : int { kPairs256, kPairs128, kOnes128, kOnes64, kSplit64, kSplit256 };
 struct Choice {
     Kind kind;
