@@ -455,3 +455,26 @@ def test_gate_gradient_of_a_branch_without_a_norm_against_differences(B):
                 q[of].view(-1)[i] += s
             # fp32 terms below 0.1 each, a few roundings; y itself was rounded once
             assert abs((value(at[0]) - value(at[1])) / (2 * step) - float(flat[i])) <= 2e-6, (k, i)
+
+
+@pytest.mark.parametrize("n,dim,stream,branch", [(6, 40, F, BF), (21, 513, F, F), (702, 768, BF, BF), (6, 8192, BF, BF)])
+@pytest.mark.parametrize("layer,post,gates", [(a, b, c) for a in (False, True) for b in (False, True) for c in (0, 1, 3)])
+def test_every_form(B, n, dim, stream, branch, layer, post, gates):
+    """Each of what may be left out, left out: the stream, dy, the biases; each column sum wanted alone or not at all."""
+    n -= n % 3
+    full = _data(n, dim, layer, post, gates, stream, branch)
+    for without in ((), ("dy",), ("x",), ("x", "dy"), ("pre_b",), ("post_b",), ("pre_b", "post_b", "dy")):
+        d = full | {k: None for k in without}
+        p, c = B.Join(dim, "layer" if layer else "rms", scale=0.7), _dev(d)
+        y, h = p.join(c["x"], c["f"], c["pre_w"], **_vectors(c), y=torch.empty((n, dim), dtype=stream, device=DEV))
+        for got, want in zip((y, h), _want(d, layer, 0.7, 1e-6)):
+            _within(got, want)
+        want, all_ = _want_grad(d, y.cpu(), layer, 0.7, 1e-6), _run_grad(p, c, y)
+        for k, w in want.items():
+            if k in all_:                            # (a bias that was left out has no gradient's place in it)
+                _within(all_[k], w)
+        for k in all_:
+            if k not in ("dx", "df"):
+                one = torch.full_like(all_[k], float("nan"))
+                _, df = p.grad(y, c["f"], c["dh"], c["pre_w"], dy=c["dy"], post_w=c["post_w"], post_b=c["post_b"], gate=c["gate"], want_dx=False, **{k: one})
+                assert torch.equal(one, all_[k]) and torch.equal(df, all_["df"])
